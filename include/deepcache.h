@@ -311,6 +311,66 @@ int dc_search_blocks_noalloc(const uint8_t* frame_dev, const uint8_t* prev_dev, 
                              int32_t search, double psnr_db, int16_t* block_mv_dev, uint32_t* block_sse_dev,
                              int32_t* global_mv_dev, void* cuda_stream);
 
+/* ---- layer normalisation and 8-bit rows ----
+ * The operators behind the layers DC_LAYER_NORM and DC_CONV_QUANT, on a caller's own maps and without a cache.  A map is [rows][channels]: a
+ * row is a pixel, rows lie `pitch` bytes apart (at least a row; any larger stride), elements of a row side by side.  Pointers
+ * and pitches are aligned to an element; 16-byte aligned ones, with rows of whole 16 bytes, are the fast case.  dtype is the map's
+ * (DC_FP32, DC_BF16); sums, means and scales are float32 or wider.  Zero rows: DC_OK, nothing is done.  Nothing is allocated, and the work is enqueued on cuda_stream
+ * (a cudaStream_t of the current device); the calls may be captured into a graph and may overlap, unless they share memory that one of them
+ * writes.  Results do not depend on what runs beside them.  Errors: DC_ERR_ARG, DC_ERR_CONFIG (dtype), DC_ERR_LIMIT (sizes), DC_ERR_CUDA. */
+
+/* Layer normalisation over the channels of each row:
+ *   mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps), y = (x - mean) rstd gamma + beta
+ *   gamma_dev, beta_dev   float32 [channels] or NULL (ones, zeros)
+ *   mean_dev, rstd_dev    float32 [rows] or NULL: for dc_layer_norm_backward
+ * y_dev may be x_dev with the same pitch.  eps >= 0.  A row with a NaN or an infinity becomes NaN, no other row changes.
+ * DC_ERR_LIMIT: more than 16384 channels. */
+int dc_layer_norm(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t rows, int32_t channels,
+                  double eps, int32_t dtype, void* y_dev, size_t y_pitch, float* mean_dev, float* rstd_dev, void* cuda_stream);
+
+/* Its gradients, for the gradient dy of the output, with xh = (x - mean) rstd and g = dy gamma:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),  dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
+ *   mean_dev, rstd_dev    float32 [rows], as dc_layer_norm gave them
+ *   dx_dev                the map's type, or NULL; may be dy_dev or x_dev with the same pitch
+ *   dgamma_dev, dbeta_dev float32 [channels], or NULL; overwritten (zeros for zero rows)
+ *   workspace_dev         dc_layer_norm_workspace bytes (4-byte aligned; not needed, and may be NULL, where both are NULL);
+ *                         its content does not matter before or after the call; two calls that may overlap need one each
+ * The sums of dgamma and dbeta are made in one order whatever the timing: equal calls give equal bits. */
+int dc_layer_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_dev, size_t x_pitch, const float* gamma_dev,
+                           const float* mean_dev, const float* rstd_dev, int64_t rows, int32_t channels, int32_t dtype,
+                           void* dx_dev, size_t dx_pitch, float* dgamma_dev, float* dbeta_dev,
+                           void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+int dc_layer_norm_workspace(int32_t channels, size_t* bytes);
+
+/* Rows in 8 bits, each in 127 steps of its largest value either way, a = max |x|: scale = a / 127, q = the integer next to 127 x / a (the
+ * exact quotient, halves to even).  q_dev: int8, 16-byte aligned, q_pitch a multiple of 16; what lies between a row's end and the next
+ * row is not written.  A row of zeros has the scale 0.  A row with a NaN or an infinity gets the scale NaN and zeros, so everything
+ * computed from it is NaN, and nothing else is.  Weights [cout][cin] are put into 8 bits by the same call (DC_FP32), once. */
+int dc_quantize_rows(const void* x_dev, size_t x_pitch, int64_t rows, int32_t channels, int32_t dtype,
+                     int8_t* q_dev, size_t q_pitch, float* scale_dev, void* cuda_stream);
+
+/* dc_layer_norm and dc_quantize_rows of its output in one pass: the same bits as the two calls one after the other.  y_dev may be NULL. */
+int dc_layer_norm_quantize(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t rows, int32_t channels,
+                           double eps, int32_t dtype, void* y_dev, size_t y_pitch, int8_t* q_dev, size_t q_pitch, float* scale_dev,
+                           void* cuda_stream);
+
+/* out[r][j] = relu(a_scale[r] b_scale[j] sum over k of a[r][k] b[j][k] + bias[j]): the product of two matrices of 8-bit rows.
+ *   a_dev int8 [m][a_pitch], b_dev int8 [n][b_pitch] (weights: one row per output channel): 16-byte aligned, pitches multiples of 16;
+ *   nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
+ * The sums are exact (int32); scales, bias and ReLU are applied in float32, with one rounding to dtype.
+ * DC_ERR_LIMIT: k > 131071 (a sum could pass 32 bits), m > 2^31 - 256, n > 2^28. */
+int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const int8_t* b_dev, size_t b_pitch,
+                        const float* b_scale_dev, const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
+                        void* out_dev, size_t out_pitch, void* cuda_stream);
+
+/* A whole layer: the rows of x [m][k] (dtype) into 8 bits, then the product with weights w: the same bits as dc_quantize_rows and
+ * dc_matmul_quantized.  workspace_dev: dc_linear_workspace bytes, any alignment; its content does not matter before or after the call; two calls that may overlap
+ * need one each. */
+int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, size_t w_pitch, const float* w_scale_dev,
+                        const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
+                        void* out_dev, size_t out_pitch, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+int dc_linear_workspace(int64_t m, int32_t k, size_t* bytes);
+
 const char* dc_strerror(int status);
 
 #ifdef __cplusplus

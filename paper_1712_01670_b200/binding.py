@@ -53,7 +53,9 @@ EXPORTS = ["dc_cache_create", "dc_cache_destroy", "dc_cache_reset", "dc_cache_by
            "dc_match_blocks", "dc_propagate_regions", "dc_conv_partial", "dc_infer_frame", "dc_infer_frame_host",
            "dc_prefetch_frame_host", "dc_lookahead_frame",
            "dc_cache_layer_map", "dc_cache_layer_regions", "dc_cache_layer_conv_scheme", "dc_get_status", "dc_cache_launches",
-           "dc_cache_set_profiling", "dc_cache_profile", "dc_cache_counters", "dc_search_blocks_noalloc", "dc_strerror"]
+           "dc_cache_set_profiling", "dc_cache_profile", "dc_cache_counters", "dc_search_blocks_noalloc",
+           "dc_layer_norm", "dc_layer_norm_backward", "dc_layer_norm_workspace", "dc_quantize_rows", "dc_layer_norm_quantize",
+           "dc_matmul_quantized", "dc_linear_quantized", "dc_linear_workspace", "dc_strerror"]
 PROFILE_STAGES = ["search", "verify", "merge", "propagate", "classify_copy", "conv", "input", "pointwise", "key_update"]
 
 _lib = None
@@ -96,6 +98,15 @@ def load():
         L.dc_cache_counters.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
         L.dc_search_blocks_noalloc.argtypes = [vp, vp, sz, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                                C.c_int32, C.c_double, vp, vp, vp, vp]
+        i32, i64, f64 = C.c_int32, C.c_int64, C.c_double
+        L.dc_layer_norm.argtypes = [vp, sz, vp, vp, i64, i32, f64, i32, vp, sz, vp, vp, vp]
+        L.dc_layer_norm_backward.argtypes = [vp, sz, vp, sz, vp, vp, vp, i64, i32, i32, vp, sz, vp, vp, vp, sz, vp]
+        L.dc_layer_norm_workspace.argtypes = [i32, C.POINTER(sz)]
+        L.dc_quantize_rows.argtypes = [vp, sz, i64, i32, i32, vp, sz, vp, vp]
+        L.dc_layer_norm_quantize.argtypes = [vp, sz, vp, vp, i64, i32, f64, i32, vp, sz, vp, sz, vp, vp]
+        L.dc_matmul_quantized.argtypes = [vp, sz, vp, vp, sz, vp, vp, i64, i32, i32, i32, i32, vp, sz, vp]
+        L.dc_linear_quantized.argtypes = [vp, sz, vp, sz, vp, vp, i64, i32, i32, i32, i32, vp, sz, vp, sz, vp]
+        L.dc_linear_workspace.argtypes = [i64, i32, C.POINTER(sz)]
         L.dc_strerror.argtypes = [i]
         L.dc_strerror.restype = C.c_char_p
         for name in EXPORTS[:-1]:
@@ -256,3 +267,166 @@ def dc_search_blocks_noalloc(frame, prev, pitch, width, height, n_streams, block
     _check(load().dc_search_blocks_noalloc(_ptr(frame), _ptr(prev), pitch, width, height, n_streams, block,
                                            search_range, search, psnr_db, _ptr(block_mv), _ptr(block_sse),
                                            _ptr(global_mv), C.c_void_p(st)), "dc_search_blocks_noalloc")
+
+
+# --------------------------------------------------------------------------
+# layer normalisation and 8-bit rows: maps as torch tensors [..., channels]
+# --------------------------------------------------------------------------
+_DTYPES = {torch.float32: DC_FP32, torch.bfloat16: DC_BF16}
+
+
+def _rows(t, what, dtypes=_DTYPES):
+    """(address, pitch in bytes, rows, channels) of a map whose rows lie a constant stride apart."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what}: unsupported type {t.dtype}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) < 1 or (shape[-1] > 1 and stride[-1] != 1):
+        raise ValueError(f"{what}: a row's elements have to lie side by side")
+    c, size = shape[-1], t.element_size()
+    if len(shape) == 2:
+        return t.data_ptr(), (stride[0] if shape[0] > 1 else c) * size, shape[0], c
+    rows = 1
+    pitch = None
+    for n, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if n == 0:
+            return t.data_ptr(), c * size, 0, c
+        if n > 1:
+            if pitch is None:
+                pitch = s
+            elif s != pitch * rows:
+                raise ValueError(f"{what}: rows do not lie a constant stride apart")
+            rows *= n
+    return t.data_ptr(), (c if pitch is None else pitch) * size, rows, c
+
+
+def _vector(t, n, what):
+    """Address of a float32 vector of n values, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous float32 vector of {n} values is needed")
+    return t.data_ptr()
+
+
+def _on_device(where, stream, tensors, *args):
+    """One call of the library on the device that the tensors are on; stream: a cudaStream_t, or None for torch's current one there."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != dev):
+            raise ValueError(f"{where}: all tensors have to be on one CUDA device")
+    st = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
+    fn = getattr(load(), where)
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, st)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, st)
+    if rc != DC_OK:
+        raise DeepCacheError(rc, where)
+
+
+def _same_rows(a, b, what):
+    if a[2:] != b[2:]:
+        raise ValueError(f"{what}: {b[2]} rows of {b[3]} where {a[2]} of {a[3]} are needed")
+
+
+def dc_layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, stream=None):
+    """y = layer normalisation of x's rows; gamma, beta (or None), mean, rstd (or None): float32."""
+    xr, yr = _rows(x, "x"), _rows(y, "y")
+    _same_rows(xr, yr, "y")
+    if x.dtype != y.dtype:
+        raise TypeError("x and y differ in type")
+    _on_device("dc_layer_norm", stream, (x, y, gamma, beta, mean, rstd), xr[0], xr[1], _vector(gamma, xr[3], "gamma"), _vector(beta, xr[3], "beta"),
+               xr[2], xr[3], eps, _DTYPES[x.dtype], yr[0], yr[1], _vector(mean, xr[2], "mean"), _vector(rstd, xr[2], "rstd"))
+
+
+def dc_layer_norm_workspace(channels: int) -> int:
+    v = C.c_size_t()
+    _check(load().dc_layer_norm_workspace(channels, C.byref(v)), "dc_layer_norm_workspace")
+    return v.value
+
+
+def _scratch(t, what):
+    if t is None:
+        return None, 0
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: has to be contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def dc_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, workspace=None, stream=None):
+    """Gradients of dc_layer_norm; workspace: any tensor of dc_layer_norm_workspace(channels) bytes (for dgamma, dbeta)."""
+    xr, dr = _rows(x, "x"), _rows(dy, "dy")
+    _same_rows(xr, dr, "dy")
+    ox = (None, 0)
+    if dx is not None:
+        ox = _rows(dx, "dx")
+        _same_rows(xr, ox, "dx")
+    if x.dtype != dy.dtype or (dx is not None and dx.dtype != x.dtype):
+        raise TypeError("x, dy and dx differ in type")
+    if mean is None or rstd is None:
+        raise ValueError("mean and rstd are needed")
+    wp, wn = _scratch(workspace, "workspace")
+    _on_device("dc_layer_norm_backward", stream, (x, dy, gamma, mean, rstd, dx, dgamma, dbeta, workspace), dr[0], dr[1], xr[0], xr[1], _vector(gamma, xr[3], "gamma"),
+               _vector(mean, xr[2], "mean"), _vector(rstd, xr[2], "rstd"), xr[2], xr[3], _DTYPES[x.dtype], ox[0], ox[1], _vector(dgamma, xr[3], "dgamma"),
+               _vector(dbeta, xr[3], "dbeta"), wp, wn)
+
+
+_INT8 = (torch.int8,)
+
+
+def dc_quantize_rows(x, q, scale, stream=None):
+    """x's rows in 8 bits: q int8 (rows 16 bytes or a multiple apart), scale float32 [rows]."""
+    xr, qr = _rows(x, "x"), _rows(q, "q", _INT8)
+    _same_rows(xr, qr, "q")
+    _on_device("dc_quantize_rows", stream, (x, q, scale), xr[0], xr[1], xr[2], xr[3], _DTYPES[x.dtype], qr[0], _pitch8(qr), _vector(scale, xr[2], "scale"))
+
+
+def _pitch8(r):
+    """The pitch of 8-bit rows; a single row's is whatever the row needs."""
+    return r[1] if r[2] > 1 else -(-r[3] // 16) * 16
+
+
+def dc_layer_norm_quantize(x, gamma, beta, q, scale, y=None, eps=1e-5, stream=None):
+    """Layer normalisation straight into 8-bit rows (and y, if given)."""
+    xr, qr = _rows(x, "x"), _rows(q, "q", _INT8)
+    _same_rows(xr, qr, "q")
+    yr = (None, 0)
+    if y is not None:
+        yr = _rows(y, "y")
+        _same_rows(xr, yr, "y")
+        if y.dtype != x.dtype:
+            raise TypeError("x and y differ in type")
+    _on_device("dc_layer_norm_quantize", stream, (x, q, scale, gamma, beta, y), xr[0], xr[1], _vector(gamma, xr[3], "gamma"), _vector(beta, xr[3], "beta"), xr[2], xr[3], eps,
+               _DTYPES[x.dtype], yr[0], yr[1], qr[0], _pitch8(qr), _vector(scale, xr[2], "scale"))
+
+
+def dc_matmul_quantized(a, a_scale, b, b_scale, bias, out, relu=False, stream=None):
+    """out = relu((a * a_scale) @ (b * b_scale).T + bias) for int8 rows a [m, k] and b [n, k]."""
+    ar, br, o = _rows(a, "a", _INT8), _rows(b, "b", _INT8), _rows(out, "out")
+    if br[3] != ar[3] or o[2] != ar[2] or o[3] != br[2]:
+        raise ValueError(f"a {tuple(a.shape)}, b {tuple(b.shape)} and out {tuple(out.shape)} do not fit together")
+    if a_scale is None or b_scale is None:
+        raise ValueError("both scales are needed")
+    _on_device("dc_matmul_quantized", stream, (a, b, a_scale, b_scale, bias, out), ar[0], _pitch8(ar), _vector(a_scale, ar[2], "a_scale"), br[0], _pitch8(br),
+               _vector(b_scale, br[2], "b_scale"), _vector(bias, br[2], "bias"), ar[2], br[2], ar[3], int(relu), _DTYPES[out.dtype], o[0], o[1])
+
+
+def dc_linear_workspace(rows: int, k: int) -> int:
+    v = C.c_size_t()
+    _check(load().dc_linear_workspace(rows, k, C.byref(v)), "dc_linear_workspace")
+    return v.value
+
+
+def dc_linear_quantized(x, w, w_scale, bias, out, relu=False, workspace=None, stream=None):
+    """out = relu(x @ (w * w_scale).T + bias) with x's rows put into 8 bits; workspace: any tensor of dc_linear_workspace(rows, k) bytes."""
+    xr, wr, o = _rows(x, "x"), _rows(w, "w", _INT8), _rows(out, "out")
+    if wr[3] != xr[3] or o[2] != xr[2] or o[3] != wr[2]:
+        raise ValueError(f"x {tuple(x.shape)}, w {tuple(w.shape)} and out {tuple(out.shape)} do not fit together")
+    if x.dtype != out.dtype:
+        raise TypeError("x and out differ in type")
+    if w_scale is None:
+        raise ValueError("w_scale is needed")
+    wp, wn = _scratch(workspace, "workspace")
+    _on_device("dc_linear_quantized", stream, (x, w, w_scale, bias, out, workspace), xr[0], xr[1], wr[0], _pitch8(wr), _vector(w_scale, wr[2], "w_scale"),
+               _vector(bias, wr[2], "bias"), xr[2], wr[2], xr[3], int(relu), _DTYPES[x.dtype], o[0], o[1], wp, wn)

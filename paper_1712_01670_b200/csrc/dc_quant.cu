@@ -1,0 +1,436 @@
+// Matrix products in 8-bit integers with a scale for each row of either side: fully connected layers and 1 x 1 convolutions whose
+// pixels and weights are held in 8 bits.
+//
+//   out[r][j] = relu(a_scale[r] b_scale[j] sum_k a[r][k] b[j][k] + bias[j])
+//
+// The sums are int32 and exact (at most 131071 terms, so that even 128 * 128 in every term fits); they are scaled and the bias is
+// added in float32 and rounded once, to the map's type.
+//
+// k_product: tcgen05.mma kind::i8 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, accumulators double
+// buffered in tensor memory, so that the eight warps that scale and store a tile work beside the MMAs of the next.  Large products run on
+// CTA pairs: 256 rows x 256 columns, each CTA loading its own 128 rows of a and half of b's, which is a third less traffic from L2 per
+// product than a CTA alone has.
+#include "dc_rows.cuh"
+#include "dc_tcgen05.cuh"
+
+namespace {
+
+constexpr unsigned long long kWaitNs = 2000000000ull;        // every wait on the device
+constexpr int kBytesK = 128;                                  // a stage: 128 values of K
+constexpr int kTileM = 128, kATile = kTileM * kBytesK;
+constexpr int kRing = 184 * 1024, kMaxStages = 7;
+constexpr int kEpiWarps = 8, kThreads = (2 + kEpiWarps) * 32;
+constexpr int kStage = 32 * 128;                              // a warp's 32 rows on their way out, 128 bytes each
+
+__device__ int32_t g_status;                                  // the status word of launches without a cache
+
+struct ProductArgs {
+    dc_product_args p;
+    int BN, NB, stages, stage_bytes, kchunks, k_last;         // columns per tile, column blocks; k_last: MMAs (32 values) of the last chunk
+    long long m_tiles;
+    uint32_t idesc, tmem_cols;
+    int wide;                                                 // out takes 16-byte stores
+};
+
+struct Ctl {
+    unsigned long long full[kMaxStages], empty[kMaxStages], tmem_full[2], tmem_empty[2];
+    alignas(16) float scale[2][256], bias[2][256];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    unsigned long long wait_ns;
+};
+constexpr size_t kSmem = kRing + kEpiWarps * kStage + sizeof(Ctl) + 1024;
+static_assert(kSmem <= 227 * 1024, "shared memory of an SM");
+
+// As DC_UMMA_CHUNK, for 8-bit integers: n (1 to 4) MMAs of K = 32.
+#define DC_UMMA_I8(name, group)                                                                                                                 \
+    __device__ __forceinline__ void name(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate, int n)       \
+    {                                                                                                                                           \
+        _Pragma("unroll") for (int k = 0; k < 4; ++k)                                                                                           \
+            if (k < n)                                                                                                                          \
+                asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t" \
+                             "tcgen05.mma." group ".kind::i8 [%0], da, db, %4, p;\n\t}"                                                         \
+                             ::"r"(d), "r"(a_lo + 2u * k), "r"(b_lo + 2u * k), "r"(hi), "r"(idesc), "r"(k == 0 ? accumulate : 1u) : "memory");   \
+    }
+DC_UMMA_I8(umma_i8, "cta_group::1")
+DC_UMMA_I8(umma_i8_pair, "cta_group::2")
+#undef DC_UMMA_I8
+
+__device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ bool wait_at(uint32_t bar, uint32_t parity, Ctl* ctl, int32_t* status)
+{
+    return mbar_wait_at(bar, parity, &ctl->abort_flag, &ctl->wait_ns, status);
+}
+
+template <typename T> struct Out;
+template <> struct Out<float> { static __device__ __forceinline__ uint32_t pack(float a, float) { return __float_as_uint(a); } };
+template <> struct Out<__nv_bfloat16> {
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { const __nv_bfloat162 t = __floats2bfloat162_rn(a, b); return *(const uint32_t*)&t; }
+};
+
+// Sixteen bytes of a row of out from column `col` on; n: the row's length.
+template <typename T>
+__device__ __forceinline__ void store_unit(char* row, int col, int n, uint4 v, int wide)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (wide && col + E <= n) { *(uint4*)(row + (size_t)col * sizeof(T)) = v; return; }
+    const T* const e = (const T*)&v;
+#pragma unroll
+    for (int k = 0; k < E; ++k)
+        if (col + k < n) ((T*)row)[col + k] = e[k];
+}
+
+// The place of row r of a tile-ordered map in the map itself, or -1: beyond the map, in the gap behind a line of pixels, or reused.
+__device__ __forceinline__ int64_t out_row(const dc_product_args& p, int64_t tile, int r)
+{
+    const int64_t row = tile * kTileM + r;
+    if (row >= p.m) return -1;
+    if (p.masks && ((__ldcg(p.masks + tile * 4 + (r >> 5)) >> (r & 31)) & 1u)) return -1;
+    if (p.padded == 0) return row;
+    const int64_t line = row / p.padded;
+    const int x = (int)(row - line * p.padded);
+    return x < p.width ? line * p.width + x : -1;
+}
+
+template <bool PAIR, typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const ProductArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* staging = ring + kRing;
+    Ctl* ctl = (Ctl*)(staging + kEpiWarps * kStage);
+    const dc_product_args& p = a.p;
+    int32_t* const status = p.status ? p.status : &g_status;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+    constexpr int M = PAIR ? 2 : 1;                           // tiles per item
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], kEpiWarps * M); }
+        ctl->abort_flag = 0;
+        ctl->wait_ns = kWaitNs;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmB) : "memory");
+    }
+    if (warp == 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(a.tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(a.tmem_cols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                             // both CTAs' barriers exist before either is signalled from outside
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    dc_pdl_wait();
+    dc_pdl_release();
+    const long long n_tiles = p.tile_list ? (long long)__ldcg(p.tile_count) : a.m_tiles;
+    const long long n_items = (n_tiles + M - 1) / M * a.NB;
+    // tile `rank` of an item; an absent second tile repeats the first, and nothing of it is stored
+    auto tile_of = [&](long long item, bool* there) -> long long {
+        const long long idx = item / a.NB * M + rank;
+        *there = idx < n_tiles;
+        const long long at = *there ? idx : idx - rank;
+        return p.tile_list ? (long long)__ldcg(p.tile_list + at) : at;
+    };
+    const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
+
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        if (elect_one()) {
+            const uint32_t lead_full = PAIR ? map_to_cta(&ctl->full[0], 0) : full0;
+            RingPos r;
+            r.start(ring0, (uint32_t)a.stages);
+            bool ok = true, there;
+            for (long long item = first; item < n_items && ok; item += step) {
+                const int row = (int)(tile_of(item, &there) * kTileM), col = (int)(item % a.NB) * a.BN + rank * (a.BN / 2);
+                for (int kc = 0; kc < a.kchunks; ++kc) {
+                    ok = wait_at(empty0 + r.off, r.phase ^ 1u, ctl, status);
+                    if (!ok) break;
+                    if (PAIR) {
+                        if (rank == 0) mbar_expect_tx(full0 + r.off, 2u * (uint32_t)a.stage_bytes);
+                        load_pair(r.data, &tmA, kc * kBytesK, row, lead_full + r.off);
+                        load_pair(r.data + kATile, &tmB, kc * kBytesK, col, lead_full + r.off);
+                    } else {
+                        mbar_expect_tx(full0 + r.off, (uint32_t)a.stage_bytes);
+                        tma_load_2d(r.data, &tmA, kc * kBytesK, row, full0 + r.off);
+                        tma_load_2d(r.data + kATile, &tmB, kc * kBytesK, col, full0 + r.off);
+                    }
+                    r.next(ring0, (uint32_t)a.stages, (uint32_t)a.stage_bytes);
+                }
+            }
+            // on an abort: give the copies already issued a bounded chance to land before the CTA exits
+            if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------- MMA issuer (of a pair: the leader's, for both CTAs) ----------------
+        if (rank == 0 && elect_one()) {
+            const uint64_t dconst = umma_desc(0, 1024, 2);
+            const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
+            RingPos r;
+            r.start(r0, (uint32_t)a.stages);
+            uint32_t acc = 0, acc_ph = 0;
+            bool ok = true;
+            for (long long item = first; item < n_items && ok; item += step) {
+                const uint32_t d = tmem_base + acc * (uint32_t)a.BN;
+                ok = wait_at(smem_u32(&ctl->tmem_empty[acc]), acc_ph ^ 1u, ctl, status);
+                tc_fence_after();
+                for (int kc = 0; kc < a.kchunks && ok; ++kc) {
+                    ok = wait_at(full0 + r.off, r.phase, ctl, status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int n = kc + 1 < a.kchunks ? 4 : a.k_last;
+                    if (PAIR) { umma_i8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, kc != 0, n); commit_pair(empty0 + r.off); }
+                    else { umma_i8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, kc != 0, n); umma_commit_at(empty0 + r.off); }
+                    r.next(r0, (uint32_t)a.stages, slot);
+                }
+                if (ok) { if (PAIR) commit_pair(smem_u32(&ctl->tmem_full[acc])); else umma_commit(&ctl->tmem_full[acc]); }
+                if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- scales, bias, ReLU, rounding, store ----------------
+        // A warp has 32 rows (the quadrant of tensor memory that it may read) and chunks of 128 bytes of their columns: of two warps with the
+        // same rows, each every second chunk.  It turns them through shared memory, so that eight lanes store 128 bytes of a row.
+        const int q = warp & 3, half = (warp - 2) >> 2, tid = threadIdx.x - 64;
+        constexpr int CW = 128 / (int)sizeof(T);              // columns of a chunk
+        const uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 2) * kStage;
+        const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
+        uint32_t acc = 0, acc_ph = 0;
+        bool ok = true, there;
+        for (long long item = first; item < n_items; item += step) {
+            const long long tile = tile_of(item, &there);
+            const int n0 = (int)(item % a.NB) * a.BN;
+            if (tid < a.BN) {
+                const int j = n0 + tid;
+                ctl->scale[acc][tid] = j < p.n ? __ldg(p.b_scale + j) : 0.f;
+                ctl->bias[acc][tid] = j < p.n && p.bias ? __ldg(p.bias + j) : 0.f;
+            }
+            const int64_t mine = there ? out_row(p, tile, q * 32 + lane) : -1;
+            const int64_t at = tile * kTileM + q * 32 + lane;
+            float sa = at < p.m ? p.a_scale[at] : 0.f;
+            asm volatile("bar.sync 1, %0;" ::"n"(kEpiWarps * 32) : "memory");
+            if (ok) ok = wait_at(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, status);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) sa = __uint_as_float(0x7fffffffu);       // a wait ran out: what is stored says so
+            tc_fence_after();
+            const uint32_t from = tmem_base + acc * (uint32_t)a.BN + ((uint32_t)(q * 32) << 16);
+            const unsigned rows = __ballot_sync(0xffffffffu, mine >= 0);
+            for (int c0 = half * CW; c0 < a.BN; c0 += 2 * CW) {
+                if (n0 + c0 >= p.n || rows == 0) break;
+#pragma unroll
+                for (int h = 0; h < CW / 32; ++h) {
+                    uint32_t v[32];
+                    tmem_ld32(from + c0 + h * 32, v);
+                    tmem_ld_wait();
+                    float f[32];
+                    const float4* const sc = (const float4*)&ctl->scale[acc][c0 + h * 32];
+                    const float4* const bi = (const float4*)&ctl->bias[acc][c0 + h * 32];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float4 s4 = sc[k], b4 = bi[k];
+                        f[4 * k] = fmaf((float)(int)v[4 * k] * sa, s4.x, b4.x);
+                        f[4 * k + 1] = fmaf((float)(int)v[4 * k + 1] * sa, s4.y, b4.y);
+                        f[4 * k + 2] = fmaf((float)(int)v[4 * k + 2] * sa, s4.z, b4.z);
+                        f[4 * k + 3] = fmaf((float)(int)v[4 * k + 3] * sa, s4.w, b4.w);
+                    }
+                    if (p.relu)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) f[k] = f[k] < 0.f ? 0.f : f[k];      // a NaN stays
+                    constexpr int E = 4 / (int)sizeof(T), U = 8 / E;                      // columns per word, units of 16 bytes per 32 columns
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) w[k] = Out<T>::pack(f[(u * 4 + k) * E], f[(u * 4 + k) * E + E - 1]);
+                        sts128(stage + lane * 128 + (((h * U + u) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
+                    }
+                }
+                __syncwarp();
+                for (int it = 0; it < 8; ++it) {
+                    const int r = it * 4 + (lane >> 3), u = lane & 7;
+                    const int64_t to = __shfl_sync(0xffffffffu, mine, r);
+                    if (to >= 0) store_unit<T>((char*)p.out + (size_t)to * p.out_pitch, n0 + c0 + u * (16 / (int)sizeof(T)), p.n, lds128(stage + r * 128 + ((u ^ (r & 7)) << 4)), a.wide);
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (PAIR) mbar_arrive_remote(lead_empty + 8u * acc);
+                else mbar_arrive(&ctl->tmem_empty[acc]);
+            }
+            if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                             // neither CTA frees tensor memory or leaves while the other may still use it
+    if (warp == 1) {
+        tc_fence_after();
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(a.tmem_cols) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(a.tmem_cols) : "memory");
+    }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn()
+{
+    static EncodeFn fn = nullptr;
+    if (!fn) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = (EncodeFn)p;
+        cudaGetLastError();
+    }
+    return fn;
+}
+
+// Rows of 8-bit values in boxes of box_rows x 128 bytes; zeros beyond the last row and the last value.
+bool encode_rows(CUtensorMap* tm, const void* base, size_t pitch, int64_t rows, int k, int box_rows)
+{
+    EncodeFn enc = encode_fn();
+    if (!enc) return false;
+    if (rows < 2 && pitch < dc_quant_pitch(k)) pitch = dc_quant_pitch(k);      // a single row's pitch is anything
+    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {(cuuint32_t)kBytesK, (cuuint32_t)box_rows}, elem[2] = {1, 1};
+    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool PAIR, typename T>
+int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const ProductArgs& a, int ctas, int device, cudaStream_t stream)
+{
+    static dc_once_per_device attr_set;
+    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product<PAIR, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PAIR ? 2 : 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmem; cfg.stream = stream;
+    // g_dc_pdl off: see dc_launch_pdl
+    cfg.attrs = g_dc_pdl ? attr : attr + 1; cfg.numAttrs = g_dc_pdl ? 2 : 1;
+    DC_CUDA(cudaLaunchKernelEx(&cfg, k_product<PAIR, T>, tmA, tmB, a));
+    return DC_OK;
+}
+
+}  // namespace
+
+int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_sms, cudaStream_t stream)
+{
+    if (p.m <= 0) return DC_OK;
+    ProductArgs a = {};
+    a.p = p;
+    a.m_tiles = (p.m + kTileM - 1) / kTileM;
+    const long long tiles = p.tile_list ? p.max_tiles : a.m_tiles;
+    // Pairs where their items of 256 x 256 fill the SMs; else the columns per tile that take the fewest turns, a tile counting its columns and the
+    // quarter of a tile that it takes to fill and drain.
+    const bool pair = p.n > 128 && (tiles + 1) / 2 * dc_div_up(p.n, 256) >= num_sms / 2;
+    a.BN = 256;
+    if (!pair) {
+        long long best = -1;
+        for (int bn = 64; bn <= 128; bn *= 2) {
+            const long long turns = (tiles * dc_div_up(p.n, bn) + num_sms - 1) / num_sms, cost = turns * (bn + 64);
+            if (best < 0 || cost <= best) { best = cost; a.BN = bn; }
+        }
+    }
+    a.NB = dc_div_up(p.n, a.BN);
+    const int b_rows = pair ? a.BN / 2 : a.BN;
+    a.stage_bytes = kATile + b_rows * kBytesK;
+    a.stages = kRing / a.stage_bytes < kMaxStages ? kRing / a.stage_bytes : kMaxStages;
+    a.kchunks = dc_div_up(p.k, kBytesK);
+    a.k_last = dc_div_up(p.k - (a.kchunks - 1) * kBytesK, 32);
+    // int32 accumulators, both operands signed 8-bit integers, K-major
+    a.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)((pair ? 256 : 128) >> 4) << 24);
+    a.tmem_cols = (uint32_t)(2 * a.BN);
+    a.wide = (uintptr_t)p.out % 16 == 0 && p.out_pitch % 16 == 0;
+    CUtensorMap tmA, tmB;
+    if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
+    const long long items = (pair ? (tiles + 1) / 2 : tiles) * a.NB, cap = pair ? num_sms / 2 : num_sms;
+    const int ctas = (int)(items < cap ? items : cap) * (pair ? 2 : 1);
+    if (dtype == DC_BF16) return pair ? launch_product<true, __nv_bfloat16>(tmA, tmB, a, ctas, device, stream) : launch_product<false, __nv_bfloat16>(tmA, tmB, a, ctas, device, stream);
+    return pair ? launch_product<true, float>(tmA, tmB, a, ctas, device, stream) : launch_product<false, float>(tmA, tmB, a, ctas, device, stream);
+}
+
+constexpr int kMostTerms = 131071;
+constexpr int64_t kMostRows = 0x7fffff00;
+
+// What both products ask of their operands.
+static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, const float* bias, int64_t m, int32_t n, int32_t k, int32_t dtype, const void* out, size_t out_pitch)
+{
+    if (dtype != DC_FP32 && dtype != DC_BF16) return DC_ERR_CONFIG;
+    const int elt = dtype == DC_BF16 ? 2 : 4;
+    if (m < 0 || n < 1 || k < 1) return DC_ERR_ARG;
+    if (k > kMostTerms || m > kMostRows || n > (1 << 28)) return DC_ERR_LIMIT;
+    if (m == 0) return DC_OK;
+    if (!b || !b_scale || !out || (uintptr_t)b % 16 || b_pitch % 16 || (n > 1 && b_pitch < (size_t)k)) return DC_ERR_ARG;
+    if ((uintptr_t)b_scale % 4 || (uintptr_t)bias % 4 || (uintptr_t)out % elt || out_pitch % elt || (m > 1 && out_pitch < (size_t)n * elt)) return DC_ERR_ARG;
+    return DC_OK;
+}
+
+extern "C" {
+
+int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const int8_t* b_dev, size_t b_pitch, const float* b_scale_dev, const float* bias_dev,
+                        int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype, void* out_dev, size_t out_pitch, void* cuda_stream)
+{
+    int rc = product_check(b_dev, b_pitch, b_scale_dev, bias_dev, m, n, k, dtype, out_dev, out_pitch);
+    if (rc != DC_OK || m == 0) return rc;
+    if (!a_dev || !a_scale_dev || (uintptr_t)a_dev % 16 || a_pitch % 16 || (m > 1 && a_pitch < (size_t)k) || (uintptr_t)a_scale_dev % 4) return DC_ERR_ARG;
+    int device = 0, sms = 0;
+    if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
+    dc_product_args p = {};
+    p.a = a_dev; p.a_pitch = a_pitch; p.a_scale = a_scale_dev; p.b = b_dev; p.b_pitch = b_pitch; p.b_scale = b_scale_dev; p.bias = bias_dev;
+    p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch;
+    return dc_launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
+}
+
+int dc_linear_workspace(int64_t m, int32_t k, size_t* bytes)
+{
+    if (m < 0 || k < 1 || !bytes) return DC_ERR_ARG;
+    *bytes = (size_t)m * (dc_quant_pitch(k) + sizeof(float)) + 256;
+    return DC_OK;
+}
+
+int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, size_t w_pitch, const float* w_scale_dev, const float* bias_dev, int64_t m, int32_t n, int32_t k,
+                        int32_t relu, int32_t dtype, void* out_dev, size_t out_pitch, void* workspace_dev, size_t workspace_bytes, void* cuda_stream)
+{
+    int rc = product_check(w_dev, w_pitch, w_scale_dev, bias_dev, m, n, k, dtype, out_dev, out_pitch);
+    if (rc != DC_OK || m == 0) return rc;
+    const int elt = dtype == DC_BF16 ? 2 : 4;
+    size_t need = 0;
+    dc_linear_workspace(m, k, &need);
+    if (!x_dev || (uintptr_t)x_dev % elt || x_pitch % elt || (m > 1 && x_pitch < (size_t)k * elt) || !workspace_dev || workspace_bytes < need) return DC_ERR_ARG;
+    int device = 0, sms = 0;
+    if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
+    const size_t pitch = dc_quant_pitch(k);
+    int8_t* const q = (int8_t*)(((uintptr_t)workspace_dev + 255) & ~(uintptr_t)255);
+    float* const scale = (float*)(q + (size_t)m * pitch);
+    dc_rows_args r = {};
+    r.x = x_dev; r.x_pitch = x_pitch; r.rows = m; r.channels = k; r.q = q; r.q_pitch = pitch; r.scale = scale;
+    if ((rc = dc_launch_rows(r, false, dtype, sms, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
+    dc_product_args p = {};
+    p.a = q; p.a_pitch = pitch; p.a_scale = scale; p.b = w_dev; p.b_pitch = w_pitch; p.b_scale = w_scale_dev; p.bias = bias_dev;
+    p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch;
+    return dc_launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

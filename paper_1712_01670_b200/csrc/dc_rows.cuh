@@ -1,0 +1,37 @@
+// Rows of channels: layer normalisation, and rows in 8 bits with a scale of their own (dc_norm.cu), and the products of such
+// rows (dc_quant.cu).  The layers DC_LAYER_NORM and DC_CONV_QUANT and the entry points of the same names call these.
+#pragma once
+#include "dc_common.cuh"
+
+// Rows [rows][channels] to be normalised (norm), quantised (q) or both.  Pitches in bytes.
+struct dc_rows_args {
+    const void* x; size_t x_pitch;
+    const float *gamma, *beta;          // or NULL: ones, zeros
+    int64_t rows; int channels;
+    float eps;
+    void* y; size_t y_pitch;            // or NULL
+    float *mean, *rstd;                 // or NULL
+    int8_t* q; size_t q_pitch; float* scale;   // or NULL
+    // Pixels of maps of `width` columns, of which each image row begins at a multiple of `padded` rows of q and scale; 0: dense
+    int width, padded;
+};
+// norm: false: the rows are quantised as they are.  *launches counts the kernels.
+int dc_launch_rows(const dc_rows_args& a, bool norm, int dtype, int num_sms, cudaStream_t stream);
+
+// out[r][j] = relu(a_scale[r] * b_scale[j] * sum_k a[r][k] b[j][k] + bias[j])
+struct dc_product_args {
+    const int8_t* a; size_t a_pitch; const float* a_scale;
+    const int8_t* b; size_t b_pitch; const float* b_scale;
+    const float* bias;                  // or NULL
+    int64_t m; int n, k, relu;
+    void* out; size_t out_pitch;
+    int32_t* status;                    // device status word, or NULL
+    // A partial convolution's pixels (NULL, 0: every row): tiles of 128 rows of a, in images of `padded` rows per line of `width` pixels
+    const int32_t *tile_list, *tile_count; const uint32_t* masks;
+    int width, padded, max_tiles;
+};
+int dc_launch_product(const dc_product_args& a, int dtype, int device, int num_sms, cudaStream_t stream);
+
+static inline size_t dc_quant_pitch(int64_t k) { return (size_t)(k + 15) / 16 * 16; }
+// The device that is current, and its number of SMs (looked up once per device).
+int dc_current_device(int* device, int* num_sms);

@@ -1,0 +1,747 @@
+"""Layer normalisation, its gradients, 8-bit rows and their products, against plain 64-bit implementations.
+
+Tolerances: u = 2^-24 is half a step of float32, T(t) half a step of the map's type (2^-24, bfloat16 2^-8), relative to the value.
+A sum of n float32 terms made in a tree of depth d is off by at most d u sum|terms|; no lane adds more than 64 terms one behind another,
+and at most 16 joins (lanes, warps) follow, so d = 80 is used throughout.
+"""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_1712_01670_b200 import binding as B
+
+U = 2.0 ** -24
+DEPTH = 80
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+gpu = pytest.mark.gpu
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def make_map(rows, c, dtype, seed, shift=0.7):
+    g = gen(seed)
+    x = torch.randn(rows, c, generator=g, device="cuda") * torch.exp(torch.randn(c, generator=g, device="cuda")) + shift
+    return x.to(dtype)
+
+
+def spread(x, pitch, offset=0):
+    """The same rows `pitch` elements apart, `offset` elements behind the start of an allocation."""
+    rows, c = x.shape
+    buf = torch.full((rows * pitch + offset + 64,), 77, dtype=x.dtype, device=x.device)
+    view = buf[offset:offset + rows * pitch].view(rows, pitch)[:, :c]
+    view.copy_(x)
+    return view, buf
+
+
+def q_like(rows, k):
+    return torch.full((rows, (k + 15) // 16 * 16), 55, dtype=torch.int8, device="cuda")[:, :k]
+
+
+def scratch(n):
+    return torch.empty(n, dtype=torch.uint8, device="cuda")
+
+
+def norm64(x, gamma, beta, eps):
+    """(y, mean, rstd, bound of y's error before it is rounded to the map's type)"""
+    x = x.double()
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    rstd = 1.0 / torch.sqrt((d * d).mean(1, keepdim=True) + eps)
+    g = torch.ones(x.shape[1], device=x.device, dtype=torch.float64) if gamma is None else gamma.double()
+    b = torch.zeros_like(g) if beta is None else beta.double()
+    y = d * rstd * g + b
+    # the mean is off by DEPTH u mean|x|, each difference by half a step more, the sum of squares by DEPTH u and by the square of the mean's
+    # error, the root, division, two products and the sum by half a step each
+    dm = (DEPTH + 2) * U * x.abs().mean(1, keepdim=True)
+    bound = g.abs() * rstd * (dm * (1 + (d * rstd).abs() * dm * rstd) + d.abs() * (DEPTH / 2 + 8) * U) + 2 * U * (y.abs() + b.abs())
+    return y, mean[:, 0], rstd[:, 0], bound
+
+
+def check_norm(x, gamma, beta, eps=1e-5, y=None):
+    rows, c = x.shape
+    y = torch.empty(rows, c, dtype=x.dtype, device="cuda") if y is None else y
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    want, wmean, wrstd, bound = norm64(x, gamma, beta, eps)
+    B.dc_layer_norm(x, gamma, beta, y, mean, rstd, eps)
+    T = half_step(x.dtype)
+    over = (y.double() - want).abs() - (bound * (1 + T) + T * want.abs() + 1e-38)
+    assert over.max() <= 0, f"y off by {over.max():.3e} more than the bound"
+    xd = x.double()
+    assert ((mean.double() - wmean).abs() <= (DEPTH + 2) * U * xd.abs().mean(1)).all()
+    assert ((rstd.double() - wrstd).abs() <= wrstd * ((DEPTH / 2 + 8) * U + ((DEPTH + 2) * U * xd.abs().mean(1) * wrstd) ** 2)).all()
+    return y
+
+
+NORM_SHAPES = [(1, 1), (1, 7), (3, 8), (5, 16), (33, 24), (130, 48), (257, 96), (64, 100), (1000, 256), (31, 257), (77, 512), (19, 513), (9, 1000), (50, 1024),
+               (49, 2048), (6, 2049), (5, 4096), (3, 4100), (3, 8192), (2, 8193), (2, 16384), (700, 64), (40000, 32)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", NORM_SHAPES)
+def test_norm(rows, c, dtype):
+    g = gen(rows + c)
+    gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+    check_norm(make_map(rows, c, TYPES[dtype], rows * 7 + c), gamma, beta)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gamma,beta", [(True, False), (False, True), (False, False)])
+def test_norm_without_weights(gamma, beta, dtype):
+    w = torch.randn(96, generator=gen(1), device="cuda")
+    check_norm(make_map(70, 96, TYPES[dtype], 2), w if gamma else None, w if beta else None)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c,pitch,offset", [(20, 64, 64, 1), (20, 64, 80, 0), (20, 64, 72, 3), (20, 64, 65, 0), (11, 256, 264, 8), (9, 1024, 1032, 4), (3, 4096, 4097, 2)])
+def test_norm_of_strided_and_shifted_rows(rows, c, pitch, offset, dtype):
+    g = gen(5)
+    x, _ = spread(make_map(rows, c, TYPES[dtype], 9), pitch, offset)
+    y, buf = spread(torch.zeros(rows, c, dtype=TYPES[dtype], device="cuda"), pitch, offset)
+    gamma = torch.randn(c + 1, generator=g, device="cuda")[1:]        # not 16-byte aligned either
+    check_norm(x, gamma, None, y=y)
+    rest = buf.clone()
+    rest[offset:offset + rows * pitch].view(rows, pitch)[:, :c] = 77
+    assert (rest == 77).all(), "something beside the rows was written"
+
+
+@gpu
+def test_norm_in_place_equals_out_of_place():
+    x = make_map(333, 192, torch.bfloat16, 3)
+    y = torch.empty_like(x)
+    B.dc_layer_norm(x, None, None, y)
+    B.dc_layer_norm(x, None, None, x)
+    assert torch.equal(x, y)
+
+
+@gpu
+def test_norm_of_rows_with_large_means_and_constant_rows():
+    g = gen(8)
+    x = torch.randn(64, 384, generator=g, device="cuda") + 1000.0     # the squares' difference would have nothing left here
+    x[5] = 3.25
+    x[6] = 0.0
+    check_norm(x, torch.randn(384, generator=g, device="cuda"), None)
+
+
+@gpu
+@pytest.mark.parametrize("c", [64, 257, 2048, 5000])
+def test_norm_keeps_what_is_not_finite_to_its_row(c):
+    x = make_map(12, c, torch.float32, 4)
+    clean = torch.empty_like(x)
+    B.dc_layer_norm(x, None, None, clean)
+    x[3, c // 2], x[7, 0], x[8, c - 1] = float("nan"), float("inf"), float("-inf")
+    y = torch.empty_like(x)
+    B.dc_layer_norm(x, None, None, y)
+    bad = torch.zeros(12, dtype=torch.bool, device="cuda")
+    bad[[3, 7, 8]] = True
+    assert torch.isnan(y[bad]).all() and torch.equal(y[~bad], clean[~bad])
+
+
+@gpu
+def test_norm_of_rows_far_apart():
+    """Rows 2^31 bytes apart and more: offsets that 32 bits do not hold."""
+    c, pitch, rows = 64, (1 << 29) + 4, 4
+    buf = torch.empty(pitch * (rows - 1) + c, device="cuda")
+    x = buf.as_strided((rows, c), (pitch, 1))
+    x.copy_(make_map(rows, c, torch.float32, 6))
+    check_norm(x, None, None)
+
+
+@gpu
+def test_norm_of_a_map_of_more_than_two_billion_elements():
+    rows, c = (1 << 23) + 5, 256
+    x = torch.zeros(rows, c, dtype=torch.bfloat16, device="cuda")
+    tail = make_map(64, c, torch.bfloat16, 11)
+    x[-64:] = tail
+    q, scale = torch.zeros(rows, c, dtype=torch.int8, device="cuda"), torch.zeros(rows, device="cuda")
+    B.dc_layer_norm_quantize(x, None, None, q, scale, x)
+    y, q2, s2 = torch.empty_like(tail), q_like(64, c), torch.empty(64, device="cuda")
+    B.dc_layer_norm_quantize(tail, None, None, q2, s2, y)
+    assert torch.equal(x[-64:], y) and torch.equal(q[-64:], q2) and torch.equal(scale[-64:], s2)
+    assert int(x[:-64].float().abs().max()) == 0
+
+
+# ---------------------------------------------------------------------------
+# gradients
+# ---------------------------------------------------------------------------
+def backward64(dy, x, gamma, mean, rstd):
+    dy, x, mean, rstd = dy.double(), x.double(), mean.double()[:, None], rstd.double()[:, None]
+    g = torch.ones(x.shape[1], device=x.device, dtype=torch.float64) if gamma is None else gamma.double()
+    xh, gy = (x - mean) * rstd, dy * g
+    m1, m2 = gy.mean(1, keepdim=True), (gy * xh).mean(1, keepdim=True)
+    dx = rstd * (gy - m1 - xh * m2)
+    # xh is off by 3 u of itself, the means by DEPTH u and their terms' own 4 u
+    bound = U * rstd * (8 * gy.abs() + (DEPTH + 8) * gy.abs().mean(1, keepdim=True) + (DEPTH + 16) * xh.abs() * (gy * xh).abs().mean(1, keepdim=True))
+    return dx, (dy * xh).sum(0), dy.sum(0), bound, (dy * xh).abs().sum(0), dy.abs().sum(0)
+
+
+def run_backward(dy, x, gamma, mean, rstd, dx=None):
+    c = x.shape[1]
+    dx = torch.empty(x.shape, dtype=x.dtype, device="cuda") if dx is None else dx
+    dg, db = torch.full((c,), 9.0, device="cuda"), torch.full((c,), 9.0, device="cuda")
+    work = scratch(B.dc_layer_norm_workspace(c))
+    work.fill_(0x7f)                                                   # large floats: what is not written is not read
+    B.dc_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dg, db, work)
+    return dx, dg, db
+
+
+def check_backward(dy, x, gamma, dx=None):
+    _, mean, rstd, _ = norm64(x, None, None, 1e-5)
+    mean, rstd = mean.float(), rstd.float()
+    want, wg, wb, bound, sg, sb = backward64(dy, x, gamma, mean, rstd)
+    dx, dg, db = run_backward(dy, x, gamma, mean, rstd, dx)
+    T = half_step(x.dtype)
+    assert ((dx.double() - want).abs() <= bound * (1 + T) + T * want.abs() + 1e-38).all()
+    # rows that one lane adds one behind another, and the joins of warps and CTAs
+    depth = DEPTH + 4 + x.shape[0] / 64
+    assert ((dg.double() - wg).abs() <= depth * U * sg).all()
+    assert ((db.double() - wb).abs() <= depth * U * sb).all()
+    return mean, rstd, dx, dg, db
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", NORM_SHAPES)
+def test_backward(rows, c, dtype):
+    g = gen(3 * rows + c)
+    x = make_map(rows, c, TYPES[dtype], rows + 5 * c)
+    dy = torch.randn(rows, c, generator=g, device="cuda").to(TYPES[dtype])
+    check_backward(dy, x, torch.randn(c, generator=g, device="cuda"))
+
+
+@gpu
+@pytest.mark.parametrize("rows", [2000, 12345])
+@pytest.mark.parametrize("c", [20, 256, 640])
+def test_backward_of_many_rows_is_the_same_every_time(rows, c):
+    g = gen(rows)
+    x, dy = make_map(rows, c, torch.bfloat16, 1), torch.randn(rows, c, generator=g, device="cuda").to(torch.bfloat16)
+    mean, rstd, *first = check_backward(dy, x, None)
+    for _ in range(3):
+        again = run_backward(dy, x, None, mean, rstd)
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_backward_of_strided_rows_and_of_a_part_of_the_gradients(dtype):
+    g = gen(2)
+    rows, c = 37, 120
+    x, _ = spread(make_map(rows, c, TYPES[dtype], 9), 131, 1)
+    dy, _ = spread(torch.randn(rows, c, generator=g, device="cuda").to(TYPES[dtype]), 125, 0)
+    gamma = torch.randn(c, generator=g, device="cuda")
+    out, buf = spread(torch.zeros(rows, c, dtype=TYPES[dtype], device="cuda"), 129, 2)
+    mean, rstd, dx, dg, db = check_backward(dy, x, gamma, dx=out)
+    rest = buf.clone()
+    rest[2:2 + rows * 129].view(rows, 129)[:, :c] = 77
+    assert (rest == 77).all()
+    work = scratch(B.dc_layer_norm_workspace(c))
+    only = torch.empty(rows, c, dtype=TYPES[dtype], device="cuda")
+    B.dc_layer_norm_backward(dy, x, gamma, mean, rstd, dx=only)       # no workspace needed
+    assert torch.equal(only, dx)
+    g2, b2 = torch.empty(c, device="cuda"), torch.empty(c, device="cuda")
+    B.dc_layer_norm_backward(dy, x, gamma, mean, rstd, dgamma=g2, workspace=work)
+    B.dc_layer_norm_backward(dy, x, gamma, mean, rstd, dbeta=b2, workspace=work)
+    assert torch.equal(g2, dg) and torch.equal(b2, db)
+    inplace = dy.clone()
+    B.dc_layer_norm_backward(inplace, x, gamma, mean, rstd, dx=inplace)
+    assert torch.equal(inplace, dx)
+
+
+@gpu
+def test_backward_against_differences():
+    """Central differences of sum(dy * y) of the 64-bit forward formula, of step h: their own error is h^2 / 6 of a third derivative of
+    order one here, and 2^-52 / h of the sum's size."""
+    rows, c, h = 3, 10, 1e-4
+    g = gen(7)
+    x = torch.randn(rows, c, generator=g, device="cuda")
+    gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+    dy = torch.randn(rows, c, generator=g, device="cuda")
+
+    def value(x, gamma, beta):
+        d = x - x.mean(1, keepdim=True)
+        return float((dy.double() * (d / torch.sqrt((d * d).mean(1, keepdim=True) + 1e-5) * gamma + beta)).sum())
+
+    _, mean, rstd, _ = norm64(x, gamma, beta, 1e-5)
+    got = run_backward(dy, x, gamma, mean.float(), rstd.float())
+    args = [x.double(), gamma.double(), beta.double()]
+    for k, grad in enumerate(got):
+        want = torch.empty_like(args[k])
+        for i in range(want.numel()):
+            moved = []
+            for s in (h, -h):
+                a = [t.clone() for t in args]
+                a[k].view(-1)[i] += s
+                moved.append(value(*a))
+            want.view(-1)[i] = (moved[0] - moved[1]) / (2 * h)
+        assert (grad.double() - want).abs().max() < 5e-6
+
+
+@gpu
+def test_backward_of_no_rows():
+    c = 40
+    x = torch.empty(0, c, device="cuda")
+    dg, db = torch.full((c,), 5.0, device="cuda"), torch.full((c,), 5.0, device="cuda")
+    B.dc_layer_norm_backward(x, x, None, torch.empty(0, device="cuda"), torch.empty(0, device="cuda"), x, dg, db, scratch(B.dc_layer_norm_workspace(c)))
+    assert (dg == 0).all() and (db == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# rows in 8 bits
+# ---------------------------------------------------------------------------
+def quantise64(x):
+    """127 x / max|x| to the nearest integer: 127 x is exact in 64 bits, and a quotient of two numbers of at most 31 and 24 bits that is not a
+    half lies further from it than 64 bits round."""
+    x = x.double()
+    most = x.abs().amax(1, keepdim=True)
+    q = torch.round(127.0 * x / torch.where(most > 0, most, torch.ones_like(most)))
+    scale = (most[:, 0] / 127.0).float()
+    bad = ~torch.isfinite(x).all(1)
+    q[bad], scale[bad] = 0.0, float("nan")
+    return q.to(torch.int8), scale
+
+
+def check_quantise(x, q=None):
+    rows, k = x.shape
+    q = q_like(rows, k) if q is None else q
+    scale = torch.full((rows,), 9.0, device="cuda")
+    wq, ws = quantise64(x)
+    B.dc_quantize_rows(x, q, scale)
+    assert torch.equal(q, wq)
+    assert torch.equal(torch.nan_to_num(scale, nan=-1.0), torch.nan_to_num(ws, nan=-1.0))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k", NORM_SHAPES + [(3, 25088), (2, 30011), (2, 40000), (1, 131071)])
+def test_quantise(rows, k, dtype):
+    x = make_map(rows, k, TYPES[dtype], rows + k)
+    x[rows // 2] = 0
+    check_quantise(x)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantise_halves_and_their_neighbours(dtype):
+    """Every half between two steps, for many largest values, and the numbers next to it."""
+    t = TYPES[dtype]
+    g = gen(12)
+    most = torch.cat([torch.tensor([127.0, 254.0, 1.0, 3.0, 2.0 ** -100, 2.0 ** -130, 2.0 ** -149, 2.0 ** 127], device="cuda"),
+                      torch.exp(4 * torch.randn(300, generator=g, device="cuda"))]).to(t).float()
+    half = torch.arange(-126, 127, device="cuda").double() + 0.5
+    x = (most.double()[:, None] * half / 127.0).to(t)
+    x = torch.cat([most.to(t)[:, None], x], 1)
+    step = torch.finfo(t).eps
+    for f in (1.0, 1.0 + step, 1.0 - step):
+        y = (x.double() * f).to(t)
+        y[:, 0] = most.to(t)
+        check_quantise(y)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [9, 64, 2048, 5000, 40000])
+def test_quantise_smallest_largest_and_not_finite(k, dtype):
+    t = TYPES[dtype]
+    x = make_map(10, k, t, 21)
+    x[1] = (x[1].float() * 2.0 ** -140).to(t)                          # numbers below the normal range
+    x[2] = (x[2].float() * 1e34).to(t)
+    x[3, 0] = torch.finfo(t).max
+    x[4, k // 2] = float("nan")
+    x[5, k - 1] = float("inf")
+    x[6, 0], x[6, 1] = float("-inf"), float("nan")
+    x[7] = 0
+    x[7, 3] = -torch.finfo(t).tiny
+    check_quantise(x)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantise_strided_rows_and_what_lies_behind_them(dtype):
+    x, _ = spread(make_map(21, 70, TYPES[dtype], 3), 83, 5)
+    full = torch.full((21, 96), 55, dtype=torch.int8, device="cuda")
+    check_quantise(x, full[:, :70])
+    assert (full[:, 70:] == 55).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(1, 5), (40, 64), (33, 257), (50, 1024), (7, 4096), (3, 9000), (2, 16384)])
+def test_norm_and_quantise_in_one_pass_has_the_bits_of_two(rows, c, dtype):
+    g = gen(rows)
+    x = make_map(rows, c, TYPES[dtype], c)
+    if rows > 2:
+        x[2, 0] = float("nan")
+    gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+    y, q, scale = torch.empty_like(x), q_like(rows, c), torch.empty(rows, device="cuda")
+    B.dc_layer_norm(x, gamma, beta, y)
+    B.dc_quantize_rows(y, q, scale)
+    y1, q1, s1 = torch.empty_like(x), q_like(rows, c), torch.empty(rows, device="cuda")
+    B.dc_layer_norm_quantize(x, gamma, beta, q1, s1, y1)
+    q2, s2 = q_like(rows, c), torch.empty(rows, device="cuda")
+    B.dc_layer_norm_quantize(x, gamma, beta, q2, s2)
+
+    def bits(t):
+        return t.view(torch.int16 if t.element_size() == 2 else torch.int32) & (0x7fff if t.element_size() == 2 else 0x7fffffff)
+
+    assert torch.equal(torch.nan_to_num(y.float(), nan=3.0), torch.nan_to_num(y1.float(), nan=3.0))
+    assert torch.equal(q, q1) and torch.equal(q, q2) and torch.equal(bits(scale), bits(s1)) and torch.equal(bits(scale), bits(s2))
+
+
+# ---------------------------------------------------------------------------
+# products
+# ---------------------------------------------------------------------------
+def random_q(rows, k, seed, pitch=None):
+    g = gen(seed)
+    q = torch.full((rows, pitch or (k + 15) // 16 * 16), 101, dtype=torch.int8, device="cuda")
+    q[:, :k] = torch.randint(-128, 128, (rows, k), generator=g, device="cuda").to(torch.int8)
+    return q[:, :k], torch.rand(rows, generator=g, device="cuda") * 0.01
+
+
+def product64(a, sa, b, sb, bias, relu):
+    """(out, bound of its error before it is rounded to the map's type): the sum to float32, two products and a sum, half a step each"""
+    acc = (a.double() @ b.double().t()) * sa.double()[:, None] * sb.double()
+    out = acc + (0.0 if bias is None else bias.double())
+    bound = 4 * U * acc.abs() + U * out.abs()
+    return (torch.where(out < 0, torch.zeros_like(out), out) if relu else out), bound
+
+
+def check_product(a, sa, b, sb, bias, relu, dtype, out=None):
+    out = torch.empty(a.shape[0], b.shape[0], dtype=dtype, device="cuda") if out is None else out
+    B.dc_matmul_quantized(a, sa, b, sb, bias, out, relu)
+    want, bound = product64(a, sa, b, sb, bias, relu)
+    T = half_step(dtype)
+    assert ((out.double() - want).abs() <= bound * (1 + T) + T * want.abs() + 1e-38).all()
+    return out
+
+
+PRODUCTS = [(1, 1, 1), (1, 16, 8), (1, 300, 77), (1, 4096, 1000), (2, 64, 64), (3, 1000, 130), (7, 128, 256), (8, 2048, 513), (9, 96, 40), (16, 512, 1024), (31, 4096, 200),
+            (33, 160, 96), (64, 9216, 512), (100, 31, 33), (127, 129, 127), (128, 128, 128), (129, 257, 65), (200, 384, 1536), (256, 64, 1000), (300, 700, 17), (1000, 256, 64),
+            (5000, 48, 24), (4096, 512, 2048), (4100, 520, 2050), (21952, 64, 256), (40000, 16, 8)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", PRODUCTS)
+def test_product(m, k, n, dtype):
+    a, sa = random_q(m, k, m + k)
+    b, sb = random_q(n, k, n + k + 1)
+    g = gen(n)
+    relu = (m + n) % 2 == 0
+    check_product(a, sa, b, sb, torch.randn(n, generator=g, device="cuda") if k % 3 else None, relu, TYPES[dtype])
+
+
+@gpu
+@pytest.mark.parametrize("m", [1, 5, 40, 300])
+def test_product_of_the_longest_rows_and_the_largest_values(m):
+    k, n = 131071, 40
+    a = torch.full((m, 131072), -128, dtype=torch.int8, device="cuda")[:, :k]
+    b = torch.full((n, 131072), -128, dtype=torch.int8, device="cuda")[:, :k]
+    b[1::2] = 127
+    one = torch.ones(max(m, n), device="cuda")
+    out = check_product(a, one[:m], b, one[:n], None, False, torch.float32)
+    assert float(out[0, 0]) == 131071.0 * 16384.0
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n,pitch,offset", [(20, 100, 40, 48, 0), (20, 100, 40, 41, 3), (150, 256, 250, 250, 1), (150, 256, 250, 301, 0), (1, 200, 33, 33, 1), (6, 200, 300, 333, 0)])
+def test_product_into_strided_and_shifted_rows(m, k, n, pitch, offset, dtype):
+    a, sa = random_q(m, k, 1, pitch=(k + 15) // 16 * 16 + 32)
+    b, sb = random_q(n, k, 2, pitch=(k + 15) // 16 * 16 + 16)
+    out, buf = spread(torch.zeros(m, n, dtype=TYPES[dtype], device="cuda"), pitch, offset)
+    check_product(a, sa, b, sb, None, False, TYPES[dtype], out=out)
+    rest = buf.clone()
+    rest[offset:offset + m * pitch].view(m, pitch)[:, :n] = 77
+    assert (rest == 77).all(), "something beside the rows was written"
+
+
+@gpu
+@pytest.mark.parametrize("m", [1, 6, 64, 700])
+@pytest.mark.parametrize("relu", [False, True])
+def test_linear_has_the_bits_of_its_two_steps_and_keeps_what_is_not_finite_to_its_row(m, relu):
+    k, n = 384, 200
+    for dtype in TYPES.values():
+        x = make_map(m, k, dtype, m)
+        if m > 5:
+            x[2, 7], x[4, 0], x[5] = float("nan"), float("inf"), 0.0
+        w = torch.randn(n, k, generator=gen(3), device="cuda")
+        wq, ws = q_like(n, k), torch.empty(n, device="cuda")
+        B.dc_quantize_rows(w, wq, ws)
+        bias = torch.randn(n, generator=gen(4), device="cuda")
+        q, s, out = q_like(m, k), torch.empty(m, device="cuda"), torch.empty(m, n, dtype=dtype, device="cuda")
+        B.dc_quantize_rows(x, q, s)
+        B.dc_matmul_quantized(q, s, wq, ws, bias, out, relu)
+        got = torch.empty_like(out)
+        work = scratch(B.dc_linear_workspace(m, k) + 3)
+        work.fill_(0x5a)
+        B.dc_linear_quantized(x, wq, ws, bias, got, relu, work[3:])
+        bad = ~torch.isfinite(x.float()).all(1)
+        assert torch.isnan(got[bad].float()).all() and torch.isnan(out[bad].float()).all()
+        assert torch.equal(got[~bad], out[~bad])
+        good = ~bad
+        check = product64(q[good], s[good], wq, ws, bias, relu)
+        T = half_step(dtype)
+        assert ((got[good].double() - check[0]).abs() <= check[1] * (1 + T) + T * check[0].abs()).all()
+        if m > 5:
+            row = torch.where(bias < 0, torch.zeros_like(bias), bias) if relu else bias
+            assert torch.equal(got[5], row.to(dtype))                  # a row of zeros leaves the bias
+
+
+@gpu
+@pytest.mark.parametrize("k,n", [(20000, 33), (25088, 256), (70000, 16)])
+def test_linear_of_long_rows(k, n):
+    for m in (1, 3, 33):
+        x = make_map(m, k, torch.bfloat16, m).relu()
+        wq, ws = random_q(n, k, 5)
+        out = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+        B.dc_linear_quantized(x, wq, ws, None, out, False, scratch(B.dc_linear_workspace(m, k)))
+        q, s = quantise64(x)
+        want, bound = product64(q, s, wq, ws, None, False)
+        T = half_step(torch.bfloat16)
+        assert ((out.double() - want).abs() <= bound * (1 + T) + T * want.abs()).all()
+
+
+# ---------------------------------------------------------------------------
+# together, on streams, in graphs
+# ---------------------------------------------------------------------------
+def chain(x, gamma, beta, w1, s1, w2, s2, out, q, qs, mid, work):
+    B.dc_layer_norm_quantize(x, gamma, beta, q, qs)
+    B.dc_matmul_quantized(q, qs, w1, s1, None, mid, True)
+    B.dc_linear_quantized(mid, w2, s2, beta, out, False, work)
+
+
+def chain_buffers(m, c, seed, dtype=torch.bfloat16):
+    wide = 4 * c
+    w1, s1 = random_q(wide, c, seed + 1)
+    w2, s2 = random_q(c, wide, seed + 2)
+    g = gen(seed)
+    return (make_map(m, c, dtype, seed), 1 + 0.1 * torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda"), w1, s1, w2, s2,
+            torch.empty(m, c, dtype=dtype, device="cuda"), q_like(m, c), torch.empty(m, device="cuda"), torch.empty(m, wide, dtype=dtype, device="cuda"),
+            scratch(B.dc_linear_workspace(m, wide)))
+
+
+@gpu
+@pytest.mark.parametrize("m", [1, 4, 50, 900])
+def test_a_run_of_them_eager_on_another_stream_and_replayed(m):
+    c = 96
+    b = chain_buffers(m, c, 30 + m)
+    x, gamma, beta, w1, s1, w2, s2, out, q, qs, mid, work = b
+    chain(*b)
+    eager = out.clone()
+    y = torch.empty_like(x)
+    B.dc_layer_norm(x, gamma, beta, y)
+    q64, sc64 = quantise64(y)
+    assert torch.equal(q, q64) and torch.equal(qs, sc64)
+    q64, sc64 = quantise64(mid)
+    want, bound = product64(q64, sc64, w2, s2, beta, False)
+    T = half_step(torch.bfloat16)
+    assert ((out.double() - want).abs() <= bound * (1 + T) + T * want.abs()).all()
+    side = torch.cuda.Stream()
+    out.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain(*b)
+    side.synchronize()
+    assert torch.equal(out, eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain(*b)
+    keep = x.clone()
+    for _ in range(3):
+        x.copy_(torch.flip(keep, [0]))
+        graph.replay()
+        assert torch.equal(out, torch.flip(eager, [0]))
+        x.copy_(keep)
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, eager)
+
+
+@gpu
+def test_gradients_captured_into_a_graph():
+    x, dy = make_map(400, 160, torch.bfloat16, 1), make_map(400, 160, torch.bfloat16, 2)
+    _, mean, rstd, _ = norm64(x, None, None, 1e-5)
+    mean, rstd = mean.float(), rstd.float()
+    want = run_backward(dy, x, None, mean, rstd)
+    dx, dg, db, work = torch.empty_like(x), torch.empty(160, device="cuda"), torch.empty(160, device="cuda"), scratch(B.dc_layer_norm_workspace(160))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.dc_layer_norm_backward(dy, x, None, mean, rstd, dx, dg, db, work)
+    for _ in range(2):
+        dx.zero_(), dg.zero_(), db.zero_()
+        graph.replay()
+        assert torch.equal(dx, want[0]) and torch.equal(dg, want[1]) and torch.equal(db, want[2])
+
+
+@gpu
+def test_two_calls_at_once_on_two_streams():
+    a, b = chain_buffers(700, 128, 1), chain_buffers(333, 64, 2)
+    chain(*a), chain(*b)
+    want = a[7].clone(), b[7].clone()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    a[7].zero_(), b[7].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        with torch.cuda.stream(s1):
+            chain(*a)
+        with torch.cuda.stream(s2):
+            chain(*b)
+    torch.cuda.synchronize()
+    assert torch.equal(a[7], want[0]) and torch.equal(b[7], want[1])
+
+
+@gpu
+def test_nothing_is_done_with_no_rows():
+    x = torch.empty(0, 32, device="cuda")
+    w, s = random_q(8, 32, 1)
+    B.dc_layer_norm(x, None, None, x)
+    q, qs = torch.empty(0, 32, dtype=torch.int8, device="cuda"), torch.empty(0, device="cuda")
+    B.dc_quantize_rows(x, q, qs)
+    B.dc_layer_norm_quantize(x, None, None, q, qs)
+    out = torch.empty(0, 8, device="cuda")
+    B.dc_matmul_quantized(q, qs, w, s, None, out)
+    B.dc_linear_quantized(x, w, s, None, out, workspace=scratch(256))
+    torch.cuda.synchronize()
+
+
+@gpu
+def test_maps_of_several_dimensions():
+    x = make_map(2 * 5 * 7, 64, torch.float32, 1).view(2, 5, 7, 64)
+    y, z = torch.empty_like(x), torch.empty(70, 64, device="cuda")
+    B.dc_layer_norm(x, None, None, y)
+    B.dc_layer_norm(x.reshape(70, 64), None, None, z)
+    assert torch.equal(y.view(70, 64), z)
+    with pytest.raises(ValueError):
+        B.dc_layer_norm(x.transpose(1, 2), None, None, y.transpose(1, 2))
+
+
+# ---------------------------------------------------------------------------
+# refusals (no GPU: an argument is refused before any CUDA call)
+# ---------------------------------------------------------------------------
+P = C.c_void_p(1 << 20)                # an aligned address that nothing reads
+
+
+def call(name, **kw):
+    order = {
+        "dc_layer_norm": ["x", "xp", "gamma", "beta", "rows", "c", "eps", "dtype", "y", "yp", "mean", "rstd", "stream"],
+        "dc_layer_norm_backward": ["dy", "dyp", "x", "xp", "gamma", "mean", "rstd", "rows", "c", "dtype", "dx", "dxp", "dgamma", "dbeta", "work", "bytes", "stream"],
+        "dc_quantize_rows": ["x", "xp", "rows", "c", "dtype", "q", "qp", "scale", "stream"],
+        "dc_layer_norm_quantize": ["x", "xp", "gamma", "beta", "rows", "c", "eps", "dtype", "y", "yp", "q", "qp", "scale", "stream"],
+        "dc_matmul_quantized": ["q", "qp", "scale", "w", "wp", "ws", "bias", "rows", "n", "c", "relu", "dtype", "y", "yp", "stream"],
+        "dc_linear_quantized": ["x", "xp", "w", "wp", "ws", "bias", "rows", "n", "c", "relu", "dtype", "y", "yp", "work", "bytes", "stream"],
+    }[name]
+    base = dict(x=P, xp=256, gamma=P, beta=P, rows=0, c=64, n=64, eps=1e-5, dtype=B.DC_FP32, y=P, yp=256, mean=P, rstd=P, dy=P, dyp=256, dx=P, dxp=256, dgamma=P, dbeta=P,
+                work=P, bytes=1 << 30, q=P, qp=64, scale=P, w=P, wp=64, ws=P, bias=P, relu=0, stream=None)
+    base.update(kw)
+    return getattr(B.load(), name)(*[base[k] for k in order])
+
+
+ODD = C.c_void_p((1 << 20) + 2)
+ODD1 = C.c_void_p((1 << 20) + 1)
+
+
+@pytest.mark.parametrize("name,kw,status", [
+    ("dc_layer_norm", dict(), B.DC_OK),                               # no rows
+    ("dc_layer_norm", dict(rows=-1), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(c=0), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(c=16385), B.DC_ERR_LIMIT),
+    ("dc_layer_norm", dict(dtype=2), B.DC_ERR_CONFIG),
+    ("dc_layer_norm", dict(eps=-1e-9), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(eps=float("nan")), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, x=None), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, y=None), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, xp=252), B.DC_ERR_ARG),            # rows would overlap
+    ("dc_layer_norm", dict(rows=2, yp=0), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, xp=258), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, x=ODD), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, x=ODD1, dtype=B.DC_BF16), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, gamma=ODD), B.DC_ERR_ARG),
+    ("dc_layer_norm", dict(rows=2, mean=ODD), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=-5), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(c=20000), B.DC_ERR_LIMIT),
+    ("dc_layer_norm_backward", dict(dtype=-1), B.DC_ERR_CONFIG),
+    ("dc_layer_norm_backward", dict(rows=3, work=None), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, bytes=296 * 8 * 64 - 1), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, mean=None), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, rstd=None), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, dy=None), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, dxp=128), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, dx=None, dgamma=None, dbeta=None, work=None), B.DC_OK),   # nothing wanted
+    ("dc_quantize_rows", dict(rows=-1), B.DC_ERR_ARG),
+    ("dc_quantize_rows", dict(rows=2, q=None), B.DC_ERR_ARG),
+    ("dc_quantize_rows", dict(rows=2, scale=None), B.DC_ERR_ARG),
+    ("dc_quantize_rows", dict(rows=2, qp=72), B.DC_ERR_ARG),
+    ("dc_quantize_rows", dict(rows=2, qp=48), B.DC_ERR_ARG),
+    ("dc_quantize_rows", dict(rows=2, q=C.c_void_p((1 << 20) + 8)), B.DC_ERR_ARG),
+    ("dc_quantize_rows", dict(rows=2, dtype=5), B.DC_ERR_CONFIG),
+    ("dc_layer_norm_quantize", dict(rows=2, q=None), B.DC_ERR_ARG),
+    ("dc_layer_norm_quantize", dict(rows=2, yp=4), B.DC_ERR_ARG),
+    ("dc_layer_norm_quantize", dict(rows=2, c=16400, qp=16400, xp=65600, y=None), B.DC_ERR_LIMIT),
+    ("dc_matmul_quantized", dict(rows=-1), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(n=0), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(c=0), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(c=131072, qp=131072, wp=131072), B.DC_ERR_LIMIT),
+    ("dc_matmul_quantized", dict(rows=1 << 31), B.DC_ERR_LIMIT),
+    ("dc_matmul_quantized", dict(rows=2, scale=None), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(rows=2, w=None), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(rows=2, wp=56), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(rows=2, qp=32), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(rows=2, q=ODD), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(rows=2, yp=128), B.DC_ERR_ARG),
+    ("dc_matmul_quantized", dict(rows=2, dtype=7), B.DC_ERR_CONFIG),
+    ("dc_linear_quantized", dict(rows=2, work=None), B.DC_ERR_ARG),
+    ("dc_linear_quantized", dict(rows=2, bytes=2 * 68 + 255), B.DC_ERR_ARG),
+    ("dc_linear_quantized", dict(rows=2, x=None), B.DC_ERR_ARG),
+    ("dc_linear_quantized", dict(rows=2, xp=128), B.DC_ERR_ARG),
+    ("dc_linear_quantized", dict(rows=2, bias=ODD), B.DC_ERR_ARG),
+])
+def test_refusals(name, kw, status):
+    assert call(name, **kw) == status
+
+
+def test_workspaces():
+    assert B.dc_layer_norm_workspace(100) == 296 * 2 * 4 * 100
+    assert B.dc_linear_workspace(3, 17) == 3 * 36 + 256
+    n = C.c_size_t()
+    assert B.load().dc_layer_norm_workspace(0, C.byref(n)) == B.DC_ERR_ARG
+    assert B.load().dc_linear_workspace(1, 0, C.byref(n)) == B.DC_ERR_ARG
+    assert B.load().dc_linear_workspace(1, 1, None) == B.DC_ERR_ARG
+
+
+def test_binding_refuses_what_does_not_fit_together():
+    x, q, s = torch.zeros(3, 32), torch.zeros(3, 32, dtype=torch.int8), torch.zeros(3)
+    with pytest.raises(ValueError):
+        B.dc_layer_norm(x, None, None, torch.zeros(3, 31))
+    with pytest.raises(TypeError):
+        B.dc_layer_norm(x, None, None, torch.zeros(3, 32, dtype=torch.bfloat16))
+    with pytest.raises(TypeError):
+        B.dc_layer_norm(x.double(), None, None, x.double())
+    with pytest.raises(ValueError):
+        B.dc_layer_norm(x, torch.zeros(31), None, x)
+    with pytest.raises(ValueError):
+        B.dc_layer_norm(x.t(), None, None, x.t())
+    with pytest.raises(ValueError):
+        B.dc_layer_norm(x, None, None, x)                              # no CUDA tensors
+    with pytest.raises(ValueError):
+        B.dc_layer_norm_backward(x, x, None, None, s, x)
+    with pytest.raises(ValueError):
+        B.dc_quantize_rows(x, q[:2], s)
+    with pytest.raises(TypeError):
+        B.dc_quantize_rows(x, x, s)
+    with pytest.raises(ValueError):
+        B.dc_matmul_quantized(q, s, torch.zeros(5, 31, dtype=torch.int8), torch.zeros(5), None, torch.zeros(3, 5))
+    with pytest.raises(ValueError):
+        B.dc_matmul_quantized(q, s, torch.zeros(5, 32, dtype=torch.int8), torch.zeros(4), None, torch.zeros(3, 5))
+    with pytest.raises(ValueError):
+        B.dc_linear_quantized(x, torch.zeros(5, 32, dtype=torch.int8), torch.zeros(5), None, torch.zeros(3, 4))
