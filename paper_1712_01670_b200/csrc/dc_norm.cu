@@ -8,61 +8,100 @@
 // registers, by a group of 1 to 32 lanes or by a CTA, and everything that it needs (the mean, the squares around it, the largest value) is
 // reduced among those.  Sums are float32 whatever the map's type; the squares are taken around the mean, not from a sum of squares,
 // which loses what a row with a large mean has left.
+#include <string.h>
+
 #include "dc_rows.cuh"
 
 namespace {
 
 constexpr int kBackwardCtas = 296;      // partial sums of a gradient's columns: two CTAs for each SM of a B200
 
-// VE elements of a row as floats: 16 bytes at once, or one element where alignment or the row's length do not allow that.
+// Two floats at once: what bounds these kernels next to memory is the instructions per element.
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+// The same of a single element, for rows that are read one by one.
+__device__ __forceinline__ float add2(float a, float b) { return a + b; }
+__device__ __forceinline__ float mul2(float a, float b) { return a * b; }
+__device__ __forceinline__ float fma2(float a, float b, float c) { return fmaf(a, b, c); }
+template <typename F> __device__ __forceinline__ F both(float a);
+template <> __device__ __forceinline__ float both<float>(float a) { return a; }
+template <> __device__ __forceinline__ float2 both<float2>(float a) { return make_float2(a, a); }
+__device__ __forceinline__ float sum_of(float a) { return a; }
+__device__ __forceinline__ float sum_of(float2 a) { return a.x + a.y; }
+__device__ __forceinline__ uint32_t size_bits(float a) { return __float_as_uint(a) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t size_bits(float2 a) { return max(size_bits(a.x), size_bits(a.y)); }
+__device__ __forceinline__ float largest(float2 a) { return fmaxf(fabsf(a.x), fabsf(a.y)); }
+__device__ __forceinline__ float add_shuffled(float a, int o) { return a + __shfl_xor_sync(0xffffffffu, a, o); }
+__device__ __forceinline__ float2 add_shuffled(float2 a, int o) { return make_float2(add_shuffled(a.x, o), add_shuffled(a.y, o)); }
+
+// VE elements of a row: 16 bytes at once, or one element where alignment or the row's length do not allow that.  A lane's elements are
+// kept as pairs of floats (F), P per vector, or as single ones.
 template <typename T, int VE> struct Vec;
 template <> struct Vec<float, 4> {
-    static __device__ __forceinline__ void load(const float* p, float* v) { const float4 t = *(const float4*)p; v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w; }
-    static __device__ __forceinline__ void store(float* p, const float* v) { *(float4*)p = make_float4(v[0], v[1], v[2], v[3]); }
+    typedef float4 Raw; typedef float2 F;
+    static constexpr int P = 2;
+    static __device__ __forceinline__ void open(Raw t, float2* v) { v[0] = make_float2(t.x, t.y); v[1] = make_float2(t.z, t.w); }
+    static __device__ __forceinline__ Raw close(const float2* v) { return make_float4(v[0].x, v[0].y, v[1].x, v[1].y); }
 };
 template <> struct Vec<__nv_bfloat16, 8> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16* p, float* v)
+    typedef uint4 Raw; typedef float2 F;
+    static constexpr int P = 4;
+    static __device__ __forceinline__ void open(Raw t, float2* v)
     {
-        const uint4 t = *(const uint4*)p;
         const uint32_t w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+        for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xffff0000u));
     }
-    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* v)
+    static __device__ __forceinline__ Raw close(const float2* v)
     {
         uint32_t w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { const __nv_bfloat162 t = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]); w[k] = *(const uint32_t*)&t; }
-        *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int k = 0; k < 4; ++k) { const __nv_bfloat162 t = __floats2bfloat162_rn(v[k].x, v[k].y); w[k] = *(const uint32_t*)&t; }
+        return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
 template <> struct Vec<float, 1> {
-    static __device__ __forceinline__ void load(const float* p, float* v) { v[0] = *p; }
-    static __device__ __forceinline__ void store(float* p, const float* v) { *p = v[0]; }
+    typedef float Raw; typedef float F;
+    static constexpr int P = 1;
+    static __device__ __forceinline__ void open(Raw t, float* v) { v[0] = t; }
+    static __device__ __forceinline__ Raw close(const float* v) { return v[0]; }
 };
 template <> struct Vec<__nv_bfloat16, 1> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16* p, float* v) { v[0] = __bfloat162float(*p); }
-    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* v) { *p = __float2bfloat16_rn(v[0]); }
+    typedef __nv_bfloat16 Raw; typedef float F;
+    static constexpr int P = 1;
+    static __device__ __forceinline__ void open(Raw t, float* v) { v[0] = __bfloat162float(t); }
+    static __device__ __forceinline__ Raw close(const float* v) { return __float2bfloat16_rn(v[0]); }
 };
-template <typename T> __device__ __forceinline__ float as_stored(float v);
-template <> __device__ __forceinline__ float as_stored<float>(float v) { return v; }
-template <> __device__ __forceinline__ float as_stored<__nv_bfloat16>(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
+template <typename R> __device__ __forceinline__ R raw_zero() { R r; memset(&r, 0, sizeof(r)); return r; }
 
-// VE channel weights; p NULL: `fill`.
-template <int VE>
-__device__ __forceinline__ void load_weights(const float* p, int at, float fill, float* v)
+// The weights of VE channels; p NULL: `fill`.
+__device__ __forceinline__ void load_weights(const float* p, int at, float fill, float (&v)[1]) { v[0] = p ? __ldg(p + at) : fill; }
+template <int P>
+__device__ __forceinline__ void load_weights(const float* p, int at, float fill, float2 (&v)[P])
 {
-    if (p) {
-        if constexpr (VE == 1) v[0] = __ldg(p + at);
-        else
 #pragma unroll
-            for (int k = 0; k < VE; k += 4) {
-                const float4 t = __ldg((const float4*)(p + at + k));
-                v[k] = t.x; v[k + 1] = t.y; v[k + 2] = t.z; v[k + 3] = t.w;
-            }
-    } else {
-#pragma unroll
-        for (int k = 0; k < VE; ++k) v[k] = fill;
+    for (int k = 0; k < P; k += 2) {
+        const float4 t = p ? __ldg((const float4*)(p + at + 2 * k)) : make_float4(fill, fill, fill, fill);
+        v[k] = make_float2(t.x, t.y); v[k + 1] = make_float2(t.z, t.w);
     }
 }
 
@@ -89,9 +128,22 @@ __device__ __forceinline__ V reduce(V v, int group, V* slot)
     return reduce_lanes<Op>(t, 32);
 }
 
+// s / c by the reciprocal of c and a correction of the remainder: half a step, as the division, at a third of its instructions.
+__device__ __forceinline__ float over(float s, float c, float inv_c)
+{
+    const float q = s * inv_c;
+    return fabsf(q) < 1e30f ? fmaf(fmaf(-q, c, s), inv_c, q) : s / c;
+}
+// 1 / sqrt(v): the fast root (error below 2^-22) and one step of Newton's; its infinities and NaN stay.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v);
+    return v > 1e-37f && v < 1e37f ? fmaf(r, fmaf(-0.5f * v * r, r, 0.5f), r) : 1.f / sqrtf(v);
+}
+
 // One value of a row in 127 steps of the row's largest, `most` > 0, either way; exact: the real quotient 127 x / most, halves to even.
-// x * inv is off by less than 3 * 2^-24 of itself, so below 2^-15 absolutely: only next to a half is the quotient looked at again,
-// in products that 64 bits hold exactly.
+// r = x * inv is off by less than 2^-22 of itself (the inverse by 2^-23 and 2^-24, the product by 2^-24), so by less than 2^-15: only next
+// to a half is the quotient looked at again, in products that 64 bits hold exactly.
 __device__ __noinline__ int quantise_next_to_half(float x, float r, float most)
 {
     const float f = floorf(fabsf(r));
@@ -101,28 +153,32 @@ __device__ __noinline__ int quantise_next_to_half(float x, float r, float most)
     return x < 0.f ? -n : n;
 }
 constexpr float kRound = 12582912.f;    // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
+constexpr float kHalf = 0.5f - 0x1p-14f;
 template <int VE>
 __device__ __forceinline__ void quantise(const float* x, float inv, float most, uint32_t* q)
 {
+    const float r = x[0] * inv, t = r + kRound;
+    q[0] = __float_as_uint(t);
+    if (fabsf(r - (t - kRound)) > kHalf) q[0] = (uint32_t)quantise_next_to_half(x[0], r, most);
+}
+template <int VE>
+__device__ __forceinline__ void quantise(const float2* x, float inv, float most, uint32_t* q)
+{
     uint32_t b[VE];
     float far = 0.f;
+    const float2 inv2 = make_float2(inv, inv), round = make_float2(kRound, kRound), minus = make_float2(-1.f, -1.f);
 #pragma unroll
-    for (int k = 0; k < VE; ++k) {
-        const float r = x[k] * inv, t = r + kRound;
-        far = fmaxf(far, fabsf(r - (t - kRound)));
-        b[k] = __float_as_uint(t);
+    for (int k = 0; k < VE / 2; ++k) {
+        const float2 r = mul2(x[k], inv2), t = add2(r, round);
+        far = fmaxf(far, largest(add2(r, fma2(t, minus, round))));
+        b[2 * k] = __float_as_uint(t.x); b[2 * k + 1] = __float_as_uint(t.y);
     }
-    if (far > 0.5f - 0x1p-14f) {
+    if (far > kHalf) {
 #pragma unroll
-        for (int k = 0; k < VE; ++k) {
-            const float r = x[k] * inv, t = r + kRound;
-            if (fabsf(r - (t - kRound)) > 0.5f - 0x1p-14f) b[k] = (uint32_t)quantise_next_to_half(x[k], r, most);
-        }
+        for (int k = 0; k < VE; ++k) quantise<1>(k & 1 ? &x[k / 2].y : &x[k / 2].x, inv, most, b + k);
     }
-    if constexpr (VE == 1) q[0] = b[0];
-    else
 #pragma unroll
-        for (int k = 0; k < VE; k += 4) q[k / 4] = __byte_perm(__byte_perm(b[k], b[k + 1], 0x0040), __byte_perm(b[k + 2], b[k + 3], 0x0040), 0x5410);
+    for (int k = 0; k < VE; k += 4) q[k / 4] = __byte_perm(__byte_perm(b[k], b[k + 1], 0x0040), __byte_perm(b[k + 2], b[k + 3], 0x0040), 0x5410);
 }
 template <int VE>
 __device__ __forceinline__ void store_q(int8_t* p, const uint32_t* q)
@@ -131,20 +187,24 @@ __device__ __forceinline__ void store_q(int8_t* p, const uint32_t* q)
     else if constexpr (VE == 4) *(uint32_t*)p = q[0];
     else *p = (int8_t)q[0];
 }
-// What a row's largest bits say of it: its scale, its steps' inverse, and a power of two that lifts rows of the smallest numbers first (their
-// inverse would be infinite).  A row with an infinity or a NaN gets the scale NaN and zeros.
-struct RowScale { float scale, inv, most, lift; };
+// What a row's largest bits say of it: its steps' inverse, and a power of two that first moves rows of very small or very large numbers to
+// where that inverse is a normal number.  A row with an infinity or a NaN gets the scale NaN and zeros.
+struct RowScale { float inv, most, lift; };
 __device__ __forceinline__ RowScale row_scale(uint32_t bits)
 {
     RowScale s;
     s.most = __uint_as_float(bits);
     s.lift = 1.f;
-    s.scale = s.most / 127.f;
-    if (bits < 0x21800000u) { s.lift = 0x1p64f; s.most *= s.lift; }              // below 2^-60
-    s.inv = s.most > 0.f ? 127.f / s.most : 0.f;
-    if (bits >= 0x7f800000u) { s.scale = __uint_as_float(0x7fffffffu); s.inv = 0.f; s.lift = 0.f; s.most = 1.f; }
+    if (bits < 0x21800000u || bits >= 0x71800000u) {             // below 2^-60 (a row of zeros too), from 2^100 on
+        s.lift = bits >= 0x7f800000u ? 0.f : bits < 0x21800000u ? 0x1p64f : 0x1p-64f;
+        s.most = bits >= 0x7f800000u || bits == 0 ? 1.f : s.most * s.lift;
+    }
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(s.most));
+    s.inv = 127.f * r;
     return s;
 }
+__device__ __forceinline__ float scale_of(uint32_t bits) { return bits >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : __uint_as_float(bits) / 127.f; }
 
 // A row's place in q and scale: see dc_rows_args.
 __device__ __forceinline__ int64_t q_row(const dc_rows_args& a, int64_t row)
@@ -155,55 +215,66 @@ __device__ __forceinline__ int64_t q_row(const dc_rows_args& a, int64_t row)
 }
 
 // Rows in registers: NV vectors of VE elements per lane.  A row belongs to `group` lanes of a warp, which takes 32 / group rows at once, or
-// (BLOCK) to the CTA.  Lanes beyond the row's end hold zeros.
-template <typename T, int VE, int NV, bool BLOCK, bool NORM, bool QUANT>
-__global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rows(const dc_rows_args a, int group)
+// (BLOCK, its most threads) to the CTA.  Lanes beyond the row's end hold zeros (FULL: there are none).  The next rows' loads are in flight while
+// a row is worked on, but for CTAs of 1024 threads, whose registers have no room for them.
+template <typename T, int VE, int NV, int BLOCK, bool NORM, bool QUANT, bool FULL>
+__global__ void __launch_bounds__(BLOCK ? BLOCK : 256) k_rows(const dc_rows_args a, int group)
 {
+    typedef Vec<T, VE> V;
+    typedef typename V::F F;
+    constexpr int P = V::P;
+    constexpr bool AHEAD = BLOCK < 1024;
     __shared__ float red[BLOCK ? 6 * 32 : 1];
     const int lane = threadIdx.x & 31, sub = BLOCK ? threadIdx.x : lane & (group - 1), lanes = BLOCK ? blockDim.x : group;
     const int per_warp = BLOCK ? 1 : 32 / group;
     const int64_t first = BLOCK ? blockIdx.x : ((int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * per_warp;
     const int64_t step = BLOCK ? gridDim.x : (int64_t)gridDim.x * (blockDim.x >> 5) * per_warp;
     const int nvec = a.channels / VE;
-    const float c = (float)a.channels;
+    const float c = (float)a.channels, inv_c = 1.f / c;
     // weights of few channels per lane stay in registers; others come from L1 for every row
     constexpr bool KEEP = NORM && NV * VE <= 16;
-    float gk[KEEP ? NV * VE : 1], bk[KEEP ? NV * VE : 1];
+    F gk[KEEP ? NV : 1][P], bk[KEEP ? NV : 1][P];
     if (KEEP)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
-            if (i < nvec) { load_weights<VE>(a.gamma, i * VE, 1.f, gk + v * VE); load_weights<VE>(a.beta, i * VE, 0.f, bk + v * VE); }
+            if (FULL || i < nvec) { load_weights(a.gamma, i * VE, 1.f, gk[v]); load_weights(a.beta, i * VE, 0.f, bk[v]); }
         }
     dc_pdl_wait();
     dc_pdl_release();
-    int parity = 0;
-    for (int64_t base = first; base < a.rows; base += step, parity ^= 1) {
-        const int64_t row = BLOCK ? base : base + lane / group;
-        const bool on = row < a.rows;
-        float* const slot = red + (BLOCK ? parity * 96 : 0);
+    typename V::Raw next[NV];
+    auto fetch = [&](int64_t row) {
         const T* const x = (const T*)((const char*)a.x + (size_t)row * a.x_pitch);
-        float d[NV * VE];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
-            if (on && i < nvec) Vec<T, VE>::load(x + i * VE, d + v * VE);
-            else
-#pragma unroll
-                for (int k = 0; k < VE; ++k) d[v * VE + k] = 0.f;
+            next[v] = row < a.rows && (FULL || i < nvec) ? *(const typename V::Raw*)(x + i * VE) : raw_zero<typename V::Raw>();
         }
-        if (NORM) {
-            float s = 0.f;
+    };
+    int64_t row = BLOCK ? first : first + lane / group;
+    if (AHEAD) fetch(row);
+    int parity = 0;
+    for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
+        const bool on = row < a.rows;
+        float* const slot = red + (BLOCK ? parity * 96 : 0);
+        F d[NV * P];
+        if (!AHEAD) fetch(row);
 #pragma unroll
-            for (int k = 0; k < NV * VE; ++k) s += d[k];
-            const float mean = reduce<Sum, BLOCK>(s, group, slot) / c;
-            s = 0.f;
+        for (int v = 0; v < NV; ++v) V::open(next[v], d + v * P);
+        if (AHEAD) fetch(row + step);
+        if (NORM) {
+            F s = d[0];
+#pragma unroll
+            for (int k = 1; k < NV * P; ++k) s = add2(s, d[k]);
+            const float mean = over(reduce<Sum, (BLOCK > 0)>(sum_of(s), group, slot), c, inv_c);
+            const F minus = both<F>(-mean);
+            s = both<F>(0.f);
 #pragma unroll
             for (int v = 0; v < NV; ++v)
-                if (v * lanes + sub < nvec)
+                if (FULL || v * lanes + sub < nvec)
 #pragma unroll
-                    for (int k = 0; k < VE; ++k) { d[v * VE + k] -= mean; s += d[v * VE + k] * d[v * VE + k]; }
-            const float rstd = 1.f / sqrtf(reduce<Sum, BLOCK>(s, group, slot + 32) / c + a.eps);
+                    for (int k = v * P; k < v * P + P; ++k) { d[k] = add2(d[k], minus); s = fma2(d[k], d[k], s); }
+            const float rstd = inverse_root(over(reduce<Sum, (BLOCK > 0)>(sum_of(s), group, slot + 32), c, inv_c) + a.eps);
             if (on && sub == 0) {
                 if (a.mean) a.mean[row] = mean;
                 if (a.rstd) a.rstd[row] = rstd;
@@ -212,35 +283,35 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rows(const dc_rows_args 
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int i = v * lanes + sub;
-                if (i >= nvec) continue;
-                float g[VE], b[VE];
-                if (!KEEP) { load_weights<VE>(a.gamma, i * VE, 1.f, g); load_weights<VE>(a.beta, i * VE, 0.f, b); }
+                if (FULL || i < nvec) {
+                    F g[P], b[P];
+                    if (!KEEP) { load_weights(a.gamma, i * VE, 1.f, g); load_weights(a.beta, i * VE, 0.f, b); }
 #pragma unroll
-                for (int k = 0; k < VE; ++k) d[v * VE + k] = fmaf(d[v * VE + k] * rstd, KEEP ? gk[(v * VE + k) % (NV * VE)] : g[k], KEEP ? bk[v * VE + k] : b[k]);
-                if (on && a.y) Vec<T, VE>::store(y + i * VE, d + v * VE);
-                if (QUANT)
-#pragma unroll
-                    for (int k = 0; k < VE; ++k) d[v * VE + k] = as_stored<T>(d[v * VE + k]);
+                    for (int k = 0; k < P; ++k) d[v * P + k] = fma2(mul2(d[v * P + k], both<F>(rstd)), KEEP ? gk[KEEP ? v : 0][k] : g[k], KEEP ? bk[KEEP ? v : 0][k] : b[k]);
+                }
+                const typename V::Raw r = V::close(d + v * P);
+                if (on && a.y && (FULL || i < nvec)) *(typename V::Raw*)(y + i * VE) = r;
+                if (QUANT && sizeof(T) == 2) V::open(r, d + v * P);             // as the map holds it
             }
         }
         if (QUANT) {
             uint32_t m = 0;
 #pragma unroll
-            for (int k = 0; k < NV * VE; ++k) m = Most::of(m, __float_as_uint(d[k]) & 0x7fffffffu);
-            m = reduce<Most, BLOCK>(m, group, (uint32_t*)slot + 64);
+            for (int k = 0; k < NV * P; ++k) m = Most::of(m, size_bits(d[k]));
+            m = reduce<Most, (BLOCK > 0)>(m, group, (uint32_t*)slot + 64);
             const RowScale s = row_scale(m);
             const int64_t qr = q_row(a, row);
-            if (on && sub == 0) a.scale[qr] = s.scale;
+            if (on && sub == 0) a.scale[qr] = scale_of(m);
             if (s.lift != 1.f)
 #pragma unroll
-                for (int k = 0; k < NV * VE; ++k) d[k] = s.lift != 0.f ? d[k] * s.lift : 0.f;
+                for (int k = 0; k < NV * P; ++k) d[k] = s.lift != 0.f ? mul2(d[k], both<F>(s.lift)) : both<F>(0.f);
             int8_t* const q = a.q + (size_t)qr * a.q_pitch;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int i = v * lanes + sub;
                 uint32_t w[VE == 8 ? 2 : 1];
-                quantise<VE>(d + v * VE, s.inv, s.most, w);
-                if (on && i < nvec) store_q<VE>(q + i * VE, w);
+                quantise<VE>(d + v * P, s.inv, s.most, w);
+                if (on && (FULL || i < nvec)) store_q<VE>(q + i * VE, w);
             }
         }
     }
@@ -250,29 +321,30 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) k_rows(const dc_rows_args 
 template <typename T, bool NORM, bool QUANT>
 __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
 {
+    typedef Vec<T, 1> V;
     __shared__ float red[6 * 32];
     dc_pdl_wait();
     dc_pdl_release();
     int parity = 0;
-    const float c = (float)a.channels;
+    const float c = (float)a.channels, inv_c = 1.f / c;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, parity ^= 1) {
         float* const slot = red + parity * 96;
         const T* const x = (const T*)((const char*)a.x + (size_t)row * a.x_pitch);
         T* const y = (T*)((char*)a.y + (size_t)row * a.y_pitch);
         float mean = 0.f, rstd = 1.f;
-        auto value = [&](int i) {
-            float v;
-            Vec<T, 1>::load(x + i, &v);
-            if (!NORM) return v;
-            return fmaf((v - mean) * rstd, a.gamma ? __ldg(a.gamma + i) : 1.f, a.beta ? __ldg(a.beta + i) : 0.f);
+        auto at = [&](int i) { float v; V::open(x[i], &v); return v; };
+        auto value = [&](int i) -> T {                            // as the map holds it
+            float v = at(i);
+            if (NORM) v = fmaf((v - mean) * rstd, a.gamma ? __ldg(a.gamma + i) : 1.f, a.beta ? __ldg(a.beta + i) : 0.f);
+            return V::close(&v);
         };
         if (NORM) {
-            float s = 0.f, v;
-            for (int i = threadIdx.x; i < a.channels; i += blockDim.x) { Vec<T, 1>::load(x + i, &v); s += v; }
-            mean = reduce<Sum, true>(s, 32, slot) / c;
+            float s = 0.f;
+            for (int i = threadIdx.x; i < a.channels; i += blockDim.x) s += at(i);
+            mean = over(reduce<Sum, true>(s, 32, slot), c, inv_c);
             s = 0.f;
-            for (int i = threadIdx.x; i < a.channels; i += blockDim.x) { Vec<T, 1>::load(x + i, &v); s += (v - mean) * (v - mean); }
-            rstd = 1.f / sqrtf(reduce<Sum, true>(s, 32, slot + 32) / c + a.eps);
+            for (int i = threadIdx.x; i < a.channels; i += blockDim.x) { const float d = at(i) - mean; s = fmaf(d, d, s); }
+            rstd = inverse_root(over(reduce<Sum, true>(s, 32, slot + 32), c, inv_c) + a.eps);
             if (threadIdx.x == 0) {
                 if (a.mean) a.mean[row] = mean;
                 if (a.rstd) a.rstd[row] = rstd;
@@ -282,16 +354,19 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
         const int64_t qr = q_row(a, row);
         if (QUANT) {
             uint32_t m = 0;
-            for (int i = threadIdx.x; i < a.channels; i += blockDim.x) m = Most::of(m, __float_as_uint(as_stored<T>(value(i))) & 0x7fffffffu);
+            for (int i = threadIdx.x; i < a.channels; i += blockDim.x) { float v; V::open(value(i), &v); m = Most::of(m, size_bits(v)); }
             m = reduce<Most, true>(m, 32, (uint32_t*)slot + 64);
             s = row_scale(m);
-            if (threadIdx.x == 0) a.scale[qr] = s.scale;
+            if (threadIdx.x == 0) a.scale[qr] = scale_of(m);
         }
+#pragma unroll 1
         for (int i = threadIdx.x; i < a.channels; i += blockDim.x) {
-            const float v = value(i);
-            if (NORM && a.y) Vec<T, 1>::store(y + i, &v);
+            const T v = value(i);
+            if (NORM && a.y) y[i] = v;
             if (QUANT) {
-                const float t = s.lift != 0.f ? as_stored<T>(v) * s.lift : 0.f;
+                float t;
+                V::open(v, &t);
+                t = s.lift != 0.f ? t * s.lift : 0.f;
                 uint32_t w;
                 quantise<1>(&t, s.inv, s.most, &w);
                 a.q[(size_t)qr * a.q_pitch + i] = (int8_t)w;
@@ -309,108 +384,118 @@ struct dc_backward_args {
 };
 
 // Gradients.  The lanes of a group (or the CTA) keep the same channels through all their rows and add up those channels' sums in registers; at the
-// end a CTA joins its groups' sums in a fixed order and leaves them for k_join.
-template <typename T, int VE, int NV, bool BLOCK, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm_backward(const dc_backward_args a, int group)
+// end a CTA joins its warps' sums in a fixed order and leaves them for k_join.
+template <typename T, int VE, int NV, bool BLOCK, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backward_args a, int group)
 {
-    extern __shared__ float join[];     // [2][channels] (not BLOCK)
+    typedef Vec<T, VE> V;
+    typedef typename V::F F;
+    constexpr int P = V::P;
+    extern __shared__ float join[];     // [warps][2][channels] (not BLOCK)
     __shared__ float red[BLOCK ? 4 * 32 : 1];
     const int lane = threadIdx.x & 31, sub = BLOCK ? threadIdx.x : lane & (group - 1), lanes = BLOCK ? blockDim.x : group;
     const int per_warp = BLOCK ? 1 : 32 / group;
     const int64_t first = BLOCK ? blockIdx.x : ((int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * per_warp;
     const int64_t step = BLOCK ? gridDim.x : (int64_t)gridDim.x * (blockDim.x >> 5) * per_warp;
     const int nvec = a.channels / VE;
-    const float c = (float)a.channels;
-    float g[NV * VE], dg[NV * VE], db[NV * VE];
+    const float c = (float)a.channels, inv_c = 1.f / c;
+    F g[NV][P], dg[NV * P], db[NV * P];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int i = v * lanes + sub;
 #pragma unroll
-        for (int k = 0; k < VE; ++k) { g[v * VE + k] = 0.f; dg[v * VE + k] = 0.f; db[v * VE + k] = 0.f; }
-        if (i < nvec) load_weights<VE>(a.gamma, i * VE, 1.f, g + v * VE);
+        for (int k = 0; k < P; ++k) g[v][k] = dg[v * P + k] = db[v * P + k] = both<F>(0.f);
+        if (i < nvec) load_weights(a.gamma, i * VE, 1.f, g[v]);
     }
     dc_pdl_wait();
     dc_pdl_release();
-    int parity = 0;
-    for (int64_t base = first; base < a.rows; base += step, parity ^= 1) {
-        const int64_t row = BLOCK ? base : base + lane / group;
-        const bool on = row < a.rows;
+    typename V::Raw next_x[NV], next_dy[NV];
+    float next_mean, next_rstd;
+    auto fetch = [&](int64_t row) {
         const T* const x = (const T*)((const char*)a.x + (size_t)row * a.x_pitch);
         const T* const dy = (const T*)((const char*)a.dy + (size_t)row * a.dy_pitch);
-        float xh[NV * VE], d[NV * VE];
-        const float mean = on ? a.mean[row] : 0.f, rstd = on ? a.rstd[row] : 0.f;
+        const bool on = row < a.rows;
+        next_mean = on ? a.mean[row] : 0.f;
+        next_rstd = on ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
-            if (on && i < nvec) { Vec<T, VE>::load(x + i * VE, xh + v * VE); Vec<T, VE>::load(dy + i * VE, d + v * VE); }
-            else
-#pragma unroll
-                for (int k = 0; k < VE; ++k) { xh[v * VE + k] = mean; d[v * VE + k] = 0.f; }
+            next_x[v] = on && i < nvec ? *(const typename V::Raw*)(x + i * VE) : raw_zero<typename V::Raw>();
+            next_dy[v] = on && i < nvec ? *(const typename V::Raw*)(dy + i * VE) : raw_zero<typename V::Raw>();
         }
-        float s1 = 0.f, s2 = 0.f;
+    };
+    int64_t row = BLOCK ? first : first + lane / group;
+    fetch(row);
+    int parity = 0;
+    for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
+        const bool on = row < a.rows;
+        F xh[NV * P], d[NV * P];
+        const float mean = next_mean, rstd = next_rstd;
 #pragma unroll
-        for (int k = 0; k < NV * VE; ++k) {
-            xh[k] = (xh[k] - mean) * rstd;
-            dg[k] = fmaf(d[k], xh[k], dg[k]);
-            db[k] += d[k];
-            d[k] *= g[k];
-            s1 += d[k];
-            s2 = fmaf(d[k], xh[k], s2);
-        }
+        for (int v = 0; v < NV; ++v) { V::open(next_x[v], xh + v * P); V::open(next_dy[v], d + v * P); }
+        fetch(row + step);
+        F p1 = both<F>(0.f), p2 = p1;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (v * lanes + sub < nvec)                            // lanes beyond the row's end: zeros, whatever the mean and the scale are
+#pragma unroll
+                for (int k = v * P; k < v * P + P; ++k) {
+                    xh[k] = mul2(add2(xh[k], both<F>(-mean)), both<F>(rstd));
+                    dg[k] = fma2(d[k], xh[k], dg[k]);
+                    db[k] = add2(db[k], d[k]);
+                    d[k] = mul2(d[k], g[v][k - v * P]);
+                    p1 = add2(p1, d[k]);
+                    p2 = fma2(d[k], xh[k], p2);
+                }
         if (!a.dx) continue;
-        float* const slot = red + (BLOCK ? parity * 64 : 0);
+        float s1 = sum_of(p1), s2 = sum_of(p2);
         if (BLOCK) {                    // both sums behind one barrier
+            float* const slot = red + parity * 64;
             s1 = reduce_lanes<Sum>(s1, 32); s2 = reduce_lanes<Sum>(s2, 32);
             if (lane == 0) { slot[threadIdx.x >> 5] = s1; slot[32 + (threadIdx.x >> 5)] = s2; }
             __syncthreads();
             const int warps = blockDim.x >> 5;
             s1 = lane < warps ? slot[lane] : 0.f; s2 = lane < warps ? slot[32 + lane] : 0.f;
         }
-        s1 = reduce_lanes<Sum>(s1, BLOCK ? 32 : group) / c;
-        s2 = reduce_lanes<Sum>(s2, BLOCK ? 32 : group) / c;
+        s1 = reduce_lanes<Sum>(s1, BLOCK ? 32 : group) * -inv_c;
+        s2 = reduce_lanes<Sum>(s2, BLOCK ? 32 : group) * -inv_c;
         T* const dx = (T*)((char*)a.dx + (size_t)row * a.dx_pitch);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
 #pragma unroll
-            for (int k = 0; k < VE; ++k) d[v * VE + k] = (d[v * VE + k] - s1 - xh[v * VE + k] * s2) * rstd;
-            if (on && i < nvec) Vec<T, VE>::store(dx + i * VE, d + v * VE);
+            for (int k = v * P; k < v * P + P; ++k) d[k] = mul2(fma2(xh[k], both<F>(s2), add2(d[k], both<F>(s1))), both<F>(rstd));
+            if (on && i < nvec) *(typename V::Raw*)(dx + i * VE) = V::close(d + v * P);
         }
     }
     if (!a.partial) return;
     float* const out = a.partial + (size_t)blockIdx.x * 2 * a.channels;
-    if constexpr (BLOCK) {
+    float* const mine = BLOCK ? out : join + (threadIdx.x >> 5) * 2 * a.channels;
+    if (!BLOCK)
+        for (int o = group; o < 32; o <<= 1)                         // rows of one warp
+#pragma unroll
+            for (int k = 0; k < NV * P; ++k) { dg[k] = add_shuffled(dg[k], o); db[k] = add_shuffled(db[k], o); }
+    if (BLOCK || lane < group)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
-            if (i < nvec)
+            if (i < nvec) {
+                if constexpr (VE == 1) { mine[i] = dg[v]; mine[a.channels + i] = db[v]; }
+                else
 #pragma unroll
-                for (int k = 0; k < VE; ++k) { out[i * VE + k] = dg[v * VE + k]; out[a.channels + i * VE + k] = db[v * VE + k]; }
-        }
-    } else {
-    for (int o = group; o < 32; o <<= 1)                         // rows of one warp
-#pragma unroll
-        for (int k = 0; k < NV * VE; ++k) {
-            dg[k] += __shfl_xor_sync(0xffffffffu, dg[k], o);
-            db[k] += __shfl_xor_sync(0xffffffffu, db[k], o);
-        }
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) {           // warp after warp
-        if ((int)(threadIdx.x >> 5) == w && lane < group) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int i = v * lanes + sub;
-                if (i < nvec)
-#pragma unroll
-                    for (int k = 0; k < VE; ++k) {
-                        float* const p = join + i * VE + k;
-                        p[0] = w ? p[0] + dg[v * VE + k] : dg[v * VE + k];
-                        p[a.channels] = w ? p[a.channels] + db[v * VE + k] : db[v * VE + k];
+                    for (int k = 0; k < VE; k += 4) {
+                        const int j = v * P + k / 2;
+                        *(float4*)(mine + i * VE + k) = make_float4(dg[j].x, dg[j].y, dg[j + 1].x, dg[j + 1].y);
+                        *(float4*)(mine + a.channels + i * VE + k) = make_float4(db[j].x, db[j].y, db[j + 1].x, db[j + 1].y);
                     }
             }
         }
-        __syncthreads();
-    }
-    for (int i = threadIdx.x; i < 2 * a.channels; i += blockDim.x) out[i] = join[i];
+    if (BLOCK) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.channels; i += blockDim.x) {
+        float s = 0.f;
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += join[w * 2 * a.channels + i];
+        out[i] = s;
     }
 }
 
@@ -450,30 +535,49 @@ Split split_row(int nvec, int most)
     return best;
 }
 
+template <typename T, int VE, int NV, int BLOCK, bool NORM, bool QUANT, bool FULL>
+cudaError_t launch_rows_as(const dc_rows_args& a, int group, int threads, int64_t ctas, int num_sms, cudaStream_t stream)
+{
+    static int resident[33];            // CTAs of so many warps that an SM holds
+    int& fit = resident[threads / 32];
+    if (!fit) {
+        int n = 0;
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_rows<T, VE, NV, BLOCK, NORM, QUANT, FULL>, threads, 0);
+        if (e != cudaSuccess) return e;
+        fit = n > 0 ? n : 1;
+    }
+    const int64_t cap = (int64_t)num_sms * fit;
+    return dc_launch_pdl(k_rows<T, VE, NV, BLOCK, NORM, QUANT, FULL>, dim3((unsigned)(ctas < cap ? ctas : cap)), threads, 0, stream, a, group);
+}
+
 template <typename T, int VE, bool NORM, bool QUANT>
 cudaError_t launch_rows(const dc_rows_args& a, int num_sms, cudaStream_t stream)
 {
     const int nvec = a.channels / VE;
+#define DC_ROWS(NV, BLOCK, G, THREADS, CTAS)                                                                                                       return nvec == (NV) * ((BLOCK) ? (THREADS) : (G)) ? launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, true>(a, G, THREADS, CTAS, num_sms, stream)                                                            : launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, false>(a, G, THREADS, CTAS, num_sms, stream)
+    // few rows: a CTA for each, a vector per thread
+    if (nvec > 32 && nvec <= 1024 && a.rows <= 2 * num_sms) DC_ROWS(1, 1024, 32, dc_div_up(nvec, 32) * 32, a.rows);
     Split s = split_row(nvec, 4);
     if (s.group == 0 && nvec <= 32 * 8) s = {32, 8};
     if (s.group != 0) {
-        const int64_t per_cta = (int64_t)8 * (32 / s.group), want = (a.rows + per_cta - 1) / per_cta, cap = (int64_t)num_sms * 8;
-        const dim3 grid((unsigned)(want < cap ? want : cap));
+        const int64_t warps = (a.rows + 32 / s.group - 1) / (32 / s.group);
+        const int per_cta = warps >= 8 * (int64_t)num_sms ? 8 : warps >= 4 * (int64_t)num_sms ? 4 : warps >= 2 * (int64_t)num_sms ? 2 : 1;
+        const int64_t ctas = (warps + per_cta - 1) / per_cta;
         switch (s.nv) {
-        case 1: return dc_launch_pdl(k_rows<T, VE, 1, false, NORM, QUANT>, grid, 256, 0, stream, a, s.group);
-        case 2: return dc_launch_pdl(k_rows<T, VE, 2, false, NORM, QUANT>, grid, 256, 0, stream, a, s.group);
-        case 3: return dc_launch_pdl(k_rows<T, VE, 3, false, NORM, QUANT>, grid, 256, 0, stream, a, s.group);
-        case 4: return dc_launch_pdl(k_rows<T, VE, 4, false, NORM, QUANT>, grid, 256, 0, stream, a, s.group);
-        default: return dc_launch_pdl(k_rows<T, VE, 8, false, NORM, QUANT>, grid, 256, 0, stream, a, s.group);
+        case 1: DC_ROWS(1, 0, s.group, per_cta * 32, ctas);
+        case 2: DC_ROWS(2, 0, s.group, per_cta * 32, ctas);
+        case 3: DC_ROWS(3, 0, s.group, per_cta * 32, ctas);
+        case 4: DC_ROWS(4, 0, s.group, per_cta * 32, ctas);
+        default: DC_ROWS(8, 0, s.group, per_cta * 32, ctas);
         }
     }
     // a CTA per row: as many threads as leave each four vectors, up to 1024
     const int want = dc_div_up(dc_div_up(nvec, 4), 32) * 32, threads = want < 128 ? 128 : want > 1024 ? 1024 : want;
-    const int64_t cap = (int64_t)num_sms * (2048 / threads);
-    const dim3 grid((unsigned)(a.rows < cap ? a.rows : cap));
-    if (nvec <= threads * 4) return dc_launch_pdl(k_rows<T, VE, 4, true, NORM, QUANT>, grid, threads, 0, stream, a, 32);
-    if (VE < 8 && nvec <= threads * 8) return dc_launch_pdl(k_rows<T, VE, 8, true, NORM, QUANT>, grid, threads, 0, stream, a, 32);
-    return dc_launch_pdl(k_rows_long<T, NORM, QUANT>, grid, 1024, 0, stream, a);
+    if (threads <= 512) DC_ROWS(4, 512, 32, threads, a.rows);
+    if (nvec <= 4096) DC_ROWS(4, 1024, 32, threads, a.rows);
+    if constexpr (VE < 8) if (nvec <= 8192) DC_ROWS(8, 1024, 32, threads, a.rows);
+#undef DC_ROWS
+    return dc_launch_pdl(k_rows_long<T, NORM, QUANT>, dim3((unsigned)(a.rows < 2 * num_sms ? a.rows : 2 * num_sms)), 1024, 0, stream, a);
 }
 
 template <typename T, int VE>
@@ -483,30 +587,27 @@ cudaError_t launch_rows_kind(const dc_rows_args& a, bool norm, int num_sms, cuda
     return a.q ? launch_rows<T, VE, true, true>(a, num_sms, stream) : launch_rows<T, VE, true, false>(a, num_sms, stream);
 }
 
+// Rows of up to 256 channels (single elements at a time: 256) belong to a warp's lanes with 8 channels each, up to 512 with 16, longer ones to a CTA.
 template <typename T, int VE>
 cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t stream, int* ctas)
 {
-    const int nvec = a.channels / VE;
-    constexpr int MOST = 16 / VE;                                    // 16 channels per lane: their sums, values and weights stay in registers
-    const Split s = split_row(nvec, MOST);
-    const int most_ctas = 2 * num_sms < kBackwardCtas ? 2 * num_sms : kBackwardCtas;
+    const int nvec = a.channels / VE, most_ctas = 2 * num_sms < kBackwardCtas ? 2 * num_sms : kBackwardCtas;
+    constexpr int N8 = 8 / VE, N16 = 16 / VE, THREADS = 320;
+    Split s = split_row(nvec, N8);
+    const bool few = s.group != 0;
+    if (!few) s = split_row(nvec, N16);
     if (s.group != 0) {
-        constexpr int THREADS = 384;
         const int64_t per_cta = (int64_t)(THREADS / 32) * (32 / s.group), want = (a.rows + per_cta - 1) / per_cta;
         *ctas = (int)(want < 1 ? 1 : want < most_ctas ? want : most_ctas);
-        const size_t smem = (size_t)2 * a.channels * sizeof(float);
-#define DC_BWD(N) return dc_launch_pdl(k_norm_backward<T, VE, N, false, THREADS>, dim3((unsigned)*ctas), THREADS, smem, stream, a, s.group)
-        if (s.nv <= 1) DC_BWD(1);
-        if (s.nv <= 2) DC_BWD(MOST < 2 ? MOST : 2);
-        if (s.nv <= 4) DC_BWD(MOST < 4 ? MOST : 4);
-        if (s.nv <= 8) DC_BWD(MOST < 8 ? MOST : 8);
-        DC_BWD(MOST);
-#undef DC_BWD
+        const size_t smem = (size_t)(THREADS / 32) * 2 * a.channels * sizeof(float);
+        if (few) return dc_launch_pdl(k_norm_backward<T, VE, N8, false, THREADS, 2>, dim3((unsigned)*ctas), THREADS, smem, stream, a, s.group);
+        return dc_launch_pdl(k_norm_backward<T, VE, N16, false, THREADS, 1>, dim3((unsigned)*ctas), THREADS, smem, stream, a, s.group);
     }
     *ctas = (int)(a.rows < 1 ? 1 : a.rows < most_ctas ? a.rows : most_ctas);
-    const int want = dc_div_up(dc_div_up(nvec, MOST), 32) * 32;
-    if (want <= 512) return dc_launch_pdl(k_norm_backward<T, VE, MOST, true, 512>, dim3((unsigned)*ctas), want, 0, stream, a, 32);
-    return dc_launch_pdl(k_norm_backward<T, VE, MOST, true, 1024>, dim3((unsigned)*ctas), want, 0, stream, a, 32);
+    const int want = dc_div_up(dc_div_up(nvec, N8), 32) * 32;
+    if (want <= 512) return dc_launch_pdl(k_norm_backward<T, VE, N8, true, 512, 1>, dim3((unsigned)*ctas), want, 0, stream, a, 32);
+    if (want <= 1024) return dc_launch_pdl(k_norm_backward<T, VE, N8, true, 1024, 1>, dim3((unsigned)*ctas), want, 0, stream, a, 32);
+    return dc_launch_pdl(k_norm_backward<T, VE, N16, true, 1024, 1>, dim3((unsigned)*ctas), dc_div_up(dc_div_up(nvec, N16), 32) * 32, 0, stream, a, 32);
 }
 
 constexpr int kMostNormChannels = 16384;
