@@ -141,9 +141,12 @@ __device__ __forceinline__ float inverse_root(float v)
     return v > 1e-37f && v < 1e37f ? fmaf(r, fmaf(-0.5f * v * r, r, 0.5f), r) : 1.f / sqrtf(v);
 }
 
-// One value of a row in 127 steps of the row's largest, `most` > 0, either way; exact: the real quotient 127 x / most, halves to even.
-// r = x * inv is off by less than 2^-22 of itself (the inverse by 2^-23 and 2^-24, the product by 2^-24), so by less than 2^-15: only next
-// to a half is the quotient looked at again, in products that 64 bits hold exactly.
+// The values of a row in 127 steps of its largest, `most` > 0, either way; exact: the real quotient 127 x / most, halves to even.  inv: 1 / most, off by less
+// than 2^-22 of itself.
+// bfloat16: 127 x is exact, one step of Newton's makes the quotient the float next to the real one, and a real one that is not a half
+// is off it by a 2^-17th of itself at least: with x = i 2^a and most = j 2^b, i and j from 128 to 255, 254 x and an odd multiple of most
+// differ by 2^min(a, b) or not at all.  Halves are common there (0.1 % of a map), so nothing may branch on them.
+// float32: 127 x / most is off by less than 2^-15, so only next to a half it is looked at again, in products that 64 bits hold exactly.
 __device__ __noinline__ int quantise_next_to_half(float x, float r, float most)
 {
     const float f = floorf(fabsf(r));
@@ -152,30 +155,36 @@ __device__ __noinline__ int quantise_next_to_half(float x, float r, float most)
     if (d > 0.0 || (d == 0.0 && (n & 1))) ++n;
     return x < 0.f ? -n : n;
 }
-constexpr float kRound = 12582912.f;    // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
+constexpr float kRound = 12582912.f;    // 1.5 * 2^23: adding it leaves the nearest integer, of two the even one, in the low bits
 constexpr float kHalf = 0.5f - 0x1p-14f;
-template <int VE>
+template <typename F>
+__device__ __forceinline__ F quotient(F x, F inv, F most)        // 127 x / most for bfloat16 x
+{
+    const F n = mul2(x, both<F>(127.f)), q = mul2(n, inv);
+    return fma2(fma2(mul2(q, both<F>(-1.f)), most, n), inv, q);
+}
+template <typename T, int VE>
 __device__ __forceinline__ void quantise(const float* x, float inv, float most, uint32_t* q)
 {
-    const float r = x[0] * inv, t = r + kRound;
+    const float r = sizeof(T) == 2 ? quotient(x[0], inv, most) : x[0] * (127.f * inv), t = r + kRound;
     q[0] = __float_as_uint(t);
-    if (fabsf(r - (t - kRound)) > kHalf) q[0] = (uint32_t)quantise_next_to_half(x[0], r, most);
+    if (sizeof(T) == 4 && fabsf(r - (t - kRound)) > kHalf) q[0] = (uint32_t)quantise_next_to_half(x[0], r, most);
 }
-template <int VE>
+template <typename T, int VE>
 __device__ __forceinline__ void quantise(const float2* x, float inv, float most, uint32_t* q)
 {
     uint32_t b[VE];
     float far = 0.f;
-    const float2 inv2 = make_float2(inv, inv), round = make_float2(kRound, kRound), minus = make_float2(-1.f, -1.f);
+    const float2 inv2 = both<float2>(sizeof(T) == 2 ? inv : 127.f * inv), round = both<float2>(kRound), minus = both<float2>(-1.f);
 #pragma unroll
     for (int k = 0; k < VE / 2; ++k) {
-        const float2 r = mul2(x[k], inv2), t = add2(r, round);
-        far = fmaxf(far, largest(add2(r, fma2(t, minus, round))));
+        const float2 r = sizeof(T) == 2 ? quotient(x[k], inv2, both<float2>(most)) : mul2(x[k], inv2), t = add2(r, round);
+        if (sizeof(T) == 4) far = fmaxf(far, largest(add2(r, fma2(t, minus, round))));
         b[2 * k] = __float_as_uint(t.x); b[2 * k + 1] = __float_as_uint(t.y);
     }
-    if (far > kHalf) {
+    if (sizeof(T) == 4 && far > kHalf) {
 #pragma unroll
-        for (int k = 0; k < VE; ++k) quantise<1>(k & 1 ? &x[k / 2].y : &x[k / 2].x, inv, most, b + k);
+        for (int k = 0; k < VE; ++k) quantise<T, 1>(k & 1 ? &x[k / 2].y : &x[k / 2].x, inv, most, b + k);
     }
 #pragma unroll
     for (int k = 0; k < VE; k += 4) q[k / 4] = __byte_perm(__byte_perm(b[k], b[k + 1], 0x0040), __byte_perm(b[k + 2], b[k + 3], 0x0040), 0x5410);
@@ -199,9 +208,7 @@ __device__ __forceinline__ RowScale row_scale(uint32_t bits)
         s.lift = bits >= 0x7f800000u ? 0.f : bits < 0x21800000u ? 0x1p64f : 0x1p-64f;
         s.most = bits >= 0x7f800000u || bits == 0 ? 1.f : s.most * s.lift;
     }
-    float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(s.most));
-    s.inv = 127.f * r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(s.inv) : "f"(s.most));
     return s;
 }
 __device__ __forceinline__ float scale_of(uint32_t bits) { return bits >= 0x7f800000u ? __uint_as_float(0x7fffffffu) : __uint_as_float(bits) / 127.f; }
@@ -310,7 +317,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256) k_rows(const dc_rows_args
             for (int v = 0; v < NV; ++v) {
                 const int i = v * lanes + sub;
                 uint32_t w[VE == 8 ? 2 : 1];
-                quantise<VE>(d + v * P, s.inv, s.most, w);
+                quantise<T, VE>(d + v * P, s.inv, s.most, w);
                 if (on && (FULL || i < nvec)) store_q<VE>(q + i * VE, w);
             }
         }
@@ -368,7 +375,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
                 V::open(v, &t);
                 t = s.lift != 0.f ? t * s.lift : 0.f;
                 uint32_t w;
-                quantise<1>(&t, s.inv, s.most, &w);
+                quantise<T, 1>(&t, s.inv, s.most, &w);
                 a.q[(size_t)qr * a.q_pitch + i] = (int8_t)w;
             }
         }

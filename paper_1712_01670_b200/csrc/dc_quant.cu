@@ -27,7 +27,7 @@ __device__ int32_t g_status;                                  // the status word
 struct ProductArgs {
     dc_product_args p;
     int BN, NB, stages, stage_bytes, kchunks, k_last;         // columns per tile, column blocks; k_last: MMAs (32 values) of the last chunk
-    long long m_tiles;
+    int m_tiles;
     uint32_t idesc, tmem_cols;
     int wide;                                                 // out takes 16-byte stores
 };
@@ -70,6 +70,18 @@ __device__ __forceinline__ bool wait_at(uint32_t bar, uint32_t parity, Ctl* ctl,
     return mbar_wait_at(bar, parity, &ctl->abort_flag, &ctl->wait_ns, status);
 }
 
+// relu(acc sa scale + bias) of two columns, for one row: float32, two at once.
+__device__ __forceinline__ void finish2(uint32_t a0, uint32_t a1, float sa, float s0, float s1, float b0, float b1, float* f)
+{
+    asm("{\n\t.reg .b64 a, s, b, m;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 m, {%4, %4};\n\tmov.b64 s, {%5, %6};\n\tmov.b64 b, {%7, %8};\n\t"
+        "mul.rn.f32x2 a, a, m;\n\tfma.rn.f32x2 a, a, s, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(f[0]), "=f"(f[1]) : "f"((float)(int)a0), "f"((float)(int)a1), "f"(sa), "f"(s0), "f"(s1), "f"(b0), "f"(b1));
+}
+__device__ __forceinline__ float relu(float v)                // a NaN stays
+{
+    asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
+    return v;
+}
 template <typename T> struct Out;
 template <> struct Out<float> { static __device__ __forceinline__ uint32_t pack(float a, float) { return __float_as_uint(a); } };
 template <> struct Out<__nv_bfloat16> {
@@ -82,25 +94,28 @@ __device__ __forceinline__ void store_unit(char* row, int col, int n, uint4 v, i
 {
     constexpr int E = 16 / sizeof(T);
     if (wide && col + E <= n) { *(uint4*)(row + (size_t)col * sizeof(T)) = v; return; }
-    const T* const e = (const T*)&v;
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int k = 0; k < E; ++k)
-        if (col + k < n) ((T*)row)[col + k] = e[k];
+        if (col + k < n) {
+            if constexpr (sizeof(T) == 4) ((uint32_t*)row)[col + k] = w[k];
+            else ((uint16_t*)row)[col + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+        }
 }
 
 // The place of row r of a tile-ordered map in the map itself, or -1: beyond the map, in the gap behind a line of pixels, or reused.
-__device__ __forceinline__ int64_t out_row(const dc_product_args& p, int64_t tile, int r)
+__device__ __forceinline__ int64_t out_row(const dc_product_args& p, int tile, int r)
 {
-    const int64_t row = tile * kTileM + r;
+    const int row = tile * kTileM + r;
     if (row >= p.m) return -1;
-    if (p.masks && ((__ldcg(p.masks + tile * 4 + (r >> 5)) >> (r & 31)) & 1u)) return -1;
+    if (p.masks && ((__ldcg(p.masks + (size_t)tile * 4 + (r >> 5)) >> (r & 31)) & 1u)) return -1;
     if (p.padded == 0) return row;
-    const int64_t line = row / p.padded;
-    const int x = (int)(row - line * p.padded);
-    return x < p.width ? line * p.width + x : -1;
+    const int line = row / p.padded, x = row - line * p.padded;
+    return x < p.width ? (int64_t)line * p.width + x : -1;
 }
 
-template <bool PAIR, typename T>
+// LIST: a partial convolution's pixels (tile_list, masks, gaps behind lines).
+template <bool PAIR, bool LIST, typename T>
 __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const ProductArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -138,14 +153,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     const uint32_t tmem_base = ctl->tmem_base;
     dc_pdl_wait();
     dc_pdl_release();
-    const long long n_tiles = p.tile_list ? (long long)__ldcg(p.tile_count) : a.m_tiles;
-    const long long n_items = (n_tiles + M - 1) / M * a.NB;
+    const int n_tiles = LIST && p.tile_list ? __ldcg(p.tile_count) : a.m_tiles;
+    const int n_items = (n_tiles + M - 1) / M * a.NB;
     // tile `rank` of an item; an absent second tile repeats the first, and nothing of it is stored
-    auto tile_of = [&](long long item, bool* there) -> long long {
-        const long long idx = item / a.NB * M + rank;
+    auto tile_of = [&](int group, bool* there) -> int {
+        const int idx = group * M + rank;
         *there = idx < n_tiles;
-        const long long at = *there ? idx : idx - rank;
-        return p.tile_list ? (long long)__ldcg(p.tile_list + at) : at;
+        const int at = *there ? idx : idx - rank;
+        return LIST && p.tile_list ? __ldcg(p.tile_list + at) : at;
     };
     const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
 
@@ -156,8 +171,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
             RingPos r;
             r.start(ring0, (uint32_t)a.stages);
             bool ok = true, there;
-            for (long long item = first; item < n_items && ok; item += step) {
-                const int row = (int)(tile_of(item, &there) * kTileM), col = (int)(item % a.NB) * a.BN + rank * (a.BN / 2);
+            for (int item = first; item < n_items && ok; item += step) {
+                const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * a.BN + rank * (a.BN / 2);
                 for (int kc = 0; kc < a.kchunks; ++kc) {
                     ok = wait_at(empty0 + r.off, r.phase ^ 1u, ctl, status);
                     if (!ok) break;
@@ -186,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
             r.start(r0, (uint32_t)a.stages);
             uint32_t acc = 0, acc_ph = 0;
             bool ok = true;
-            for (long long item = first; item < n_items && ok; item += step) {
+            for (int item = first; item < n_items && ok; item += step) {
                 const uint32_t d = tmem_base + acc * (uint32_t)a.BN;
                 ok = wait_at(smem_u32(&ctl->tmem_empty[acc]), acc_ph ^ 1u, ctl, status);
                 tc_fence_after();
@@ -214,68 +229,74 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
         uint32_t acc = 0, acc_ph = 0;
         bool ok = true, there;
-        for (long long item = first; item < n_items; item += step) {
-            const long long tile = tile_of(item, &there);
-            const int n0 = (int)(item % a.NB) * a.BN;
+        for (int item = first; item < n_items; item += step) {
+            const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * a.BN;
             if (tid < a.BN) {
                 const int j = n0 + tid;
                 ctl->scale[acc][tid] = j < p.n ? __ldg(p.b_scale + j) : 0.f;
                 ctl->bias[acc][tid] = j < p.n && p.bias ? __ldg(p.bias + j) : 0.f;
             }
-            const int64_t mine = there ? out_row(p, tile, q * 32 + lane) : -1;
-            const int64_t at = tile * kTileM + q * 32 + lane;
+            const int64_t at = (int64_t)tile * kTileM + q * 32 + lane;
+            const int64_t mine = LIST ? (there ? out_row(p, tile, q * 32 + lane) : -1) : at;      // this lane's row of out
             float sa = at < p.m ? p.a_scale[at] : 0.f;
+            const int rows = LIST ? 32 : there ? (int)min((int64_t)32, p.m - (at - lane)) : 0;     // rows that exist (LIST: where mine says so)
+            char* to = (char*)p.out + (size_t)(at - lane + (lane >> 3)) * p.out_pitch;             // not LIST: row lane / 8 of the 32
             asm volatile("bar.sync 1, %0;" ::"n"(kEpiWarps * 32) : "memory");
             if (ok) ok = wait_at(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) sa = __uint_as_float(0x7fffffffu);       // a wait ran out: what is stored says so
             tc_fence_after();
             const uint32_t from = tmem_base + acc * (uint32_t)a.BN + ((uint32_t)(q * 32) << 16);
-            const unsigned rows = __ballot_sync(0xffffffffu, mine >= 0);
-            for (int c0 = half * CW; c0 < a.BN; c0 += 2 * CW) {
-                if (n0 + c0 >= p.n || rows == 0) break;
+            const int n_here = min(a.BN, p.n - n0);
+            bool held = true;                                 // the accumulator is still to be read
+            auto hand_back = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
+                    else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
+                }
+                held = false;
+            };
+            for (int c0 = half * CW; c0 < n_here; c0 += 2 * CW) {
+                uint32_t v[CW];
 #pragma unroll
-                for (int h = 0; h < CW / 32; ++h) {
-                    uint32_t v[32];
-                    tmem_ld32(from + c0 + h * 32, v);
-                    tmem_ld_wait();
-                    float f[32];
-                    const float4* const sc = (const float4*)&ctl->scale[acc][c0 + h * 32];
-                    const float4* const bi = (const float4*)&ctl->bias[acc][c0 + h * 32];
+                for (int h = 0; h < CW / 32; ++h) tmem_ld32(from + c0 + h * 32, v + h * 32);
+                tmem_ld_wait();
+                if (c0 + 2 * CW >= n_here) hand_back();
+                constexpr int E = 4 / (int)sizeof(T);         // columns per word
+                const float4* const sc = (const float4*)&ctl->scale[acc][c0];
+                const float4* const bi = (const float4*)&ctl->bias[acc][c0];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float4 s4 = sc[k], b4 = bi[k];
-                        f[4 * k] = fmaf((float)(int)v[4 * k] * sa, s4.x, b4.x);
-                        f[4 * k + 1] = fmaf((float)(int)v[4 * k + 1] * sa, s4.y, b4.y);
-                        f[4 * k + 2] = fmaf((float)(int)v[4 * k + 2] * sa, s4.z, b4.z);
-                        f[4 * k + 3] = fmaf((float)(int)v[4 * k + 3] * sa, s4.w, b4.w);
+                for (int u = 0; u < 8; ++u) {                 // units of 16 bytes
+                    float f[4 * E];
+#pragma unroll
+                    for (int k = 0; k < E; ++k) {
+                        const float4 s4 = sc[u * E + k], b4 = bi[u * E + k];
+                        const uint32_t* const w = v + (u * E + k) * 4;
+                        finish2(w[0], w[1], sa, s4.x, s4.y, b4.x, b4.y, f + 4 * k);
+                        finish2(w[2], w[3], sa, s4.z, s4.w, b4.z, b4.w, f + 4 * k + 2);
                     }
                     if (p.relu)
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) f[k] = f[k] < 0.f ? 0.f : f[k];      // a NaN stays
-                    constexpr int E = 4 / (int)sizeof(T), U = 8 / E;                      // columns per word, units of 16 bytes per 32 columns
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) w[k] = Out<T>::pack(f[(u * 4 + k) * E], f[(u * 4 + k) * E + E - 1]);
-                        sts128(stage + lane * 128 + (((h * U + u) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
-                    }
+                        for (int k = 0; k < 4 * E; ++k) f[k] = relu(f[k]);
+                    sts128(stage + lane * 128 + ((u ^ (lane & 7)) << 4), Out<T>::pack(f[0], f[E - 1]), Out<T>::pack(f[E], f[2 * E - 1]), Out<T>::pack(f[2 * E], f[3 * E - 1]),
+                           Out<T>::pack(f[3 * E], f[4 * E - 1]));
                 }
                 __syncwarp();
+                const int u = lane & 7, col = n0 + c0 + u * 4 * E;
+#pragma unroll
                 for (int it = 0; it < 8; ++it) {
-                    const int r = it * 4 + (lane >> 3), u = lane & 7;
-                    const int64_t to = __shfl_sync(0xffffffffu, mine, r);
-                    if (to >= 0) store_unit<T>((char*)p.out + (size_t)to * p.out_pitch, n0 + c0 + u * (16 / (int)sizeof(T)), p.n, lds128(stage + r * 128 + ((u ^ (r & 7)) << 4)), a.wide);
+                    const int r = it * 4 + (lane >> 3);
+                    const uint4 w = lds128(stage + r * 128 + ((u ^ (r & 7)) << 4));
+                    if (LIST) {
+                        const int64_t there_row = __shfl_sync(0xffffffffu, mine, r);
+                        if (there_row >= 0) store_unit<T>((char*)p.out + (size_t)there_row * p.out_pitch, col, p.n, w, a.wide);
+                    } else if (r < rows) store_unit<T>(to + (size_t)(it * 4) * p.out_pitch, col, p.n, w, a.wide);
                 }
                 __syncwarp();
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (PAIR) mbar_arrive_remote(lead_empty + 8u * acc);
-                else mbar_arrive(&ctl->tmem_empty[acc]);
-            }
+            if (held) hand_back();                            // a warp whose columns do not exist
             if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
         }
     }
@@ -315,11 +336,11 @@ bool encode_rows(CUtensorMap* tm, const void* base, size_t pitch, int64_t rows, 
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, typename T>
+template <bool PAIR, bool LIST, typename T>
 int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const ProductArgs& a, int ctas, int device, cudaStream_t stream)
 {
     static dc_once_per_device attr_set;
-    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product<PAIR, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product<PAIR, LIST, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -329,7 +350,7 @@ int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const Product
     cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmem; cfg.stream = stream;
     // g_dc_pdl off: see dc_launch_pdl
     cfg.attrs = g_dc_pdl ? attr : attr + 1; cfg.numAttrs = g_dc_pdl ? 2 : 1;
-    DC_CUDA(cudaLaunchKernelEx(&cfg, k_product<PAIR, T>, tmA, tmB, a));
+    DC_CUDA(cudaLaunchKernelEx(&cfg, k_product<PAIR, LIST, T>, tmA, tmB, a));
     return DC_OK;
 }
 
@@ -340,7 +361,7 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
     if (p.m <= 0) return DC_OK;
     ProductArgs a = {};
     a.p = p;
-    a.m_tiles = (p.m + kTileM - 1) / kTileM;
+    a.m_tiles = (int)((p.m + kTileM - 1) / kTileM);
     const long long tiles = p.tile_list ? p.max_tiles : a.m_tiles;
     // Pairs where their items of 256 x 256 fill the SMs; else the columns per tile that take the fewest turns, a tile counting its columns and the
     // quarter of a tile that it takes to fill and drain.
@@ -366,9 +387,13 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
     CUtensorMap tmA, tmB;
     if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
     const long long items = (pair ? (tiles + 1) / 2 : tiles) * a.NB, cap = pair ? num_sms / 2 : num_sms;
+    if (items >= 0x70000000) return DC_ERR_LIMIT;
     const int ctas = (int)(items < cap ? items : cap) * (pair ? 2 : 1);
-    if (dtype == DC_BF16) return pair ? launch_product<true, __nv_bfloat16>(tmA, tmB, a, ctas, device, stream) : launch_product<false, __nv_bfloat16>(tmA, tmB, a, ctas, device, stream);
-    return pair ? launch_product<true, float>(tmA, tmB, a, ctas, device, stream) : launch_product<false, float>(tmA, tmB, a, ctas, device, stream);
+#define DC_PRODUCT(PAIR, T) return p.padded ? launch_product<PAIR, true, T>(tmA, tmB, a, ctas, device, stream) : launch_product<PAIR, false, T>(tmA, tmB, a, ctas, device, stream)
+    if (dtype == DC_BF16) { if (pair) DC_PRODUCT(true, __nv_bfloat16); DC_PRODUCT(false, __nv_bfloat16); }
+    if (pair) DC_PRODUCT(true, float);
+    DC_PRODUCT(false, float);
+#undef DC_PRODUCT
 }
 
 constexpr int kMostTerms = 131071;
