@@ -48,7 +48,6 @@ template <> __device__ __forceinline__ float2 both<float2>(float a) { return mak
 __device__ __forceinline__ float sum_of(float a) { return a; }
 __device__ __forceinline__ float sum_of(float2 a) { return a.x + a.y; }
 __device__ __forceinline__ uint32_t size_bits(float a) { return __float_as_uint(a) & 0x7fffffffu; }
-__device__ __forceinline__ uint32_t size_bits(float2 a) { return max(size_bits(a.x), size_bits(a.y)); }
 __device__ __forceinline__ float largest(float2 a) { return fmaxf(fabsf(a.x), fabsf(a.y)); }
 __device__ __forceinline__ float add_shuffled(float a, int o) { return a + __shfl_xor_sync(0xffffffffu, a, o); }
 __device__ __forceinline__ float2 add_shuffled(float2 a, int o) { return make_float2(add_shuffled(a.x, o), add_shuffled(a.y, o)); }
@@ -91,6 +90,20 @@ template <> struct Vec<__nv_bfloat16, 1> {
     static __device__ __forceinline__ void open(Raw t, float* v) { v[0] = __bfloat162float(t); }
     static __device__ __forceinline__ Raw close(const float* v) { return __float2bfloat16_rn(v[0]); }
 };
+// The larger of m and the bits of a vector's sizes: two bfloat16 side by side, which most_of() joins.
+__device__ __forceinline__ uint32_t raw_most(uint32_t m, uint4 t)
+{
+    m = __vmaxu2(m, t.x & 0x7fff7fffu); m = __vmaxu2(m, t.y & 0x7fff7fffu);
+    m = __vmaxu2(m, t.z & 0x7fff7fffu); return __vmaxu2(m, t.w & 0x7fff7fffu);
+}
+__device__ __forceinline__ uint32_t raw_most(uint32_t m, float4 t)
+{
+    m = max(max(m, size_bits(t.x)), size_bits(t.y));
+    return max(max(m, size_bits(t.z)), size_bits(t.w));
+}
+__device__ __forceinline__ uint32_t raw_most(uint32_t m, float t) { return max(m, size_bits(t)); }
+__device__ __forceinline__ uint32_t raw_most(uint32_t m, __nv_bfloat16 t) { return max(m, (uint32_t)__bfloat16_as_ushort(t) & 0x7fffu); }
+template <typename T> __device__ __forceinline__ uint32_t most_of(uint32_t m) { return sizeof(T) == 2 ? max(m >> 16, m & 0xffffu) << 16 : m; }
 template <typename R> __device__ __forceinline__ R raw_zero() { R r; memset(&r, 0, sizeof(r)); return r; }
 
 // The weights of VE channels; p NULL: `fill`.
@@ -158,15 +171,15 @@ __device__ __noinline__ int quantise_next_to_half(float x, float r, float most)
 constexpr float kRound = 12582912.f;    // 1.5 * 2^23: adding it leaves the nearest integer, of two the even one, in the low bits
 constexpr float kHalf = 0.5f - 0x1p-14f;
 template <typename F>
-__device__ __forceinline__ F quotient(F x, F inv, F most)        // 127 x / most for bfloat16 x
+__device__ __forceinline__ F quotient(F x, F inv, F minus_most)        // 127 x / most for bfloat16 x
 {
     const F n = mul2(x, both<F>(127.f)), q = mul2(n, inv);
-    return fma2(fma2(mul2(q, both<F>(-1.f)), most, n), inv, q);
+    return fma2(fma2(q, minus_most, n), inv, q);
 }
 template <typename T, int VE>
 __device__ __forceinline__ void quantise(const float* x, float inv, float most, uint32_t* q)
 {
-    const float r = sizeof(T) == 2 ? quotient(x[0], inv, most) : x[0] * (127.f * inv), t = r + kRound;
+    const float r = sizeof(T) == 2 ? quotient(x[0], inv, -most) : x[0] * (127.f * inv), t = r + kRound;
     q[0] = __float_as_uint(t);
     if (sizeof(T) == 4 && fabsf(r - (t - kRound)) > kHalf) q[0] = (uint32_t)quantise_next_to_half(x[0], r, most);
 }
@@ -178,7 +191,7 @@ __device__ __forceinline__ void quantise(const float2* x, float inv, float most,
     const float2 inv2 = both<float2>(sizeof(T) == 2 ? inv : 127.f * inv), round = both<float2>(kRound), minus = both<float2>(-1.f);
 #pragma unroll
     for (int k = 0; k < VE / 2; ++k) {
-        const float2 r = sizeof(T) == 2 ? quotient(x[k], inv2, both<float2>(most)) : mul2(x[k], inv2), t = add2(r, round);
+        const float2 r = sizeof(T) == 2 ? quotient(x[k], inv2, both<float2>(-most)) : mul2(x[k], inv2), t = add2(r, round);
         if (sizeof(T) == 4) far = fmaxf(far, largest(add2(r, fma2(t, minus, round))));
         b[2 * k] = __float_as_uint(t.x); b[2 * k + 1] = __float_as_uint(t.y);
     }
@@ -265,9 +278,13 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256) k_rows(const dc_rows_args
         const bool on = row < a.rows;
         float* const slot = red + (BLOCK ? parity * 96 : 0);
         F d[NV * P];
+        uint32_t m = 0;
         if (!AHEAD) fetch(row);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) V::open(next[v], d + v * P);
+        for (int v = 0; v < NV; ++v) {
+            V::open(next[v], d + v * P);
+            if (QUANT && !NORM) m = raw_most(m, next[v]);
+        }
         if (AHEAD) fetch(row + step);
         if (NORM) {
             F s = d[0];
@@ -299,13 +316,11 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256) k_rows(const dc_rows_args
                 const typename V::Raw r = V::close(d + v * P);
                 if (on && a.y && (FULL || i < nvec)) *(typename V::Raw*)(y + i * VE) = r;
                 if (QUANT && sizeof(T) == 2) V::open(r, d + v * P);             // as the map holds it
+                if (QUANT) m = raw_most(m, r);
             }
         }
         if (QUANT) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int k = 0; k < NV * P; ++k) m = Most::of(m, size_bits(d[k]));
-            m = reduce<Most, (BLOCK > 0)>(m, group, (uint32_t*)slot + 64);
+            m = reduce<Most, (BLOCK > 0)>(most_of<T>(m), group, (uint32_t*)slot + 64);
             const RowScale s = row_scale(m);
             const int64_t qr = q_row(a, row);
             if (on && sub == 0) a.scale[qr] = scale_of(m);

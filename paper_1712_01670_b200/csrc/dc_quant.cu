@@ -7,7 +7,7 @@
 // added in float32 and rounded once, to the map's type.
 //
 // k_product: tcgen05.mma kind::i8 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, accumulators double
-// buffered in tensor memory, so that the eight warps that scale and store a tile work beside the MMAs of the next.  Large products run on
+// buffered in tensor memory, so that the sixteen warps that scale and store a tile work beside the MMAs of the next.  Large products run on
 // CTA pairs: 256 rows x 256 columns, each CTA loading its own 128 rows of a and half of b's, which is a third less traffic from L2 per
 // product than a CTA alone has.
 #include "dc_rows.cuh"
@@ -19,8 +19,8 @@ constexpr unsigned long long kWaitNs = 2000000000ull;        // every wait on th
 constexpr int kBytesK = 128;                                  // a stage: 128 values of K
 constexpr int kTileM = 128, kATile = kTileM * kBytesK;
 constexpr int kRing = 184 * 1024, kMaxStages = 7;
-constexpr int kEpiWarps = 8, kThreads = (2 + kEpiWarps) * 32;
-constexpr int kStage = 32 * 128;                              // a warp's 32 rows on their way out, 128 bytes each
+constexpr int kEpiWarps = 16, kThreads = (2 + kEpiWarps) * 32;
+constexpr int kStage = 32 * 64;                               // a warp's 32 rows on their way out, 64 bytes each
 
 __device__ int32_t g_status;                                  // the status word of launches without a cache
 
@@ -34,7 +34,6 @@ struct ProductArgs {
 
 struct Ctl {
     unsigned long long full[kMaxStages], empty[kMaxStages], tmem_full[2], tmem_empty[2];
-    alignas(16) float scale[2][256], bias[2][256];
     uint32_t tmem_base;
     volatile int abort_flag;
     unsigned long long wait_ns;
@@ -70,37 +69,53 @@ __device__ __forceinline__ bool wait_at(uint32_t bar, uint32_t parity, Ctl* ctl,
     return mbar_wait_at(bar, parity, &ctl->abort_flag, &ctl->wait_ns, status);
 }
 
-// relu(acc sa scale + bias) of two columns, for one row: float32, two at once.
-__device__ __forceinline__ void finish2(uint32_t a0, uint32_t a1, float sa, float s0, float s1, float b0, float b1, float* f)
+// acc sa scale + bias of two columns, for one row: float32, two at once.
+__device__ __forceinline__ float2 finish2(uint32_t a0, uint32_t a1, float sa, float2 s, float2 b)
 {
+    float2 f;
     asm("{\n\t.reg .b64 a, s, b, m;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 m, {%4, %4};\n\tmov.b64 s, {%5, %6};\n\tmov.b64 b, {%7, %8};\n\t"
         "mul.rn.f32x2 a, a, m;\n\tfma.rn.f32x2 a, a, s, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
-        : "=f"(f[0]), "=f"(f[1]) : "f"((float)(int)a0), "f"((float)(int)a1), "f"(sa), "f"(s0), "f"(s1), "f"(b0), "f"(b1));
+        : "=f"(f.x), "=f"(f.y) : "f"((float)(int)a0), "f"((float)(int)a1), "f"(sa), "f"(s.x), "f"(s.y), "f"(b.x), "f"(b.y));
+    return f;
 }
-__device__ __forceinline__ float relu(float v)                // a NaN stays
+// ReLU or nothing: low is zero or minus infinity; a NaN stays.
+__device__ __forceinline__ float at_least(float v, float low) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(low)); return r; }
+__device__ __forceinline__ uint32_t at_least_bf16(float2 a, float low)
 {
-    asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
-    return v;
+    const __nv_bfloat162 t = __floats2bfloat162_rn(a.x, a.y);
+    uint32_t r, lo = __float_as_uint(low);
+    lo |= lo >> 16;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(*(const uint32_t*)&t), "r"(lo));
+    return r;
 }
-template <typename T> struct Out;
-template <> struct Out<float> { static __device__ __forceinline__ uint32_t pack(float a, float) { return __float_as_uint(a); } };
-template <> struct Out<__nv_bfloat16> {
-    static __device__ __forceinline__ uint32_t pack(float a, float b) { const __nv_bfloat162 t = __floats2bfloat162_rn(a, b); return *(const uint32_t*)&t; }
-};
+// Sixteen rows x 32 columns of tensor memory: column group j (8 columns) in r[4 j ...]; a lane has columns 2 (lane % 4), + 1 of rows lane / 4
+// (r[4 j], r[4 j + 1]) and lane / 4 + 8.
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t* r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void stmatrix4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+// Two neighbouring columns' weights, from `col` on; beyond the last: zeros.
+__device__ __forceinline__ float2 two_of(const float* p, int col, int n, bool pairs)
+{
+    if (!p) return make_float2(0.f, 0.f);
+    if (pairs && col + 1 < n) return __ldg((const float2*)(p + col));
+    return make_float2(col < n ? __ldg(p + col) : 0.f, col + 1 < n ? __ldg(p + col + 1) : 0.f);
+}
 
-// Sixteen bytes of a row of out from column `col` on; n: the row's length.
-template <typename T>
+// Eight bfloat16 of a row of out from column `col` on; n: the row's length.
 __device__ __forceinline__ void store_unit(char* row, int col, int n, uint4 v, int wide)
 {
-    constexpr int E = 16 / sizeof(T);
-    if (wide && col + E <= n) { *(uint4*)(row + (size_t)col * sizeof(T)) = v; return; }
+    if (wide && col + 8 <= n) { *(uint4*)(row + (size_t)col * 2) = v; return; }
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int k = 0; k < E; ++k)
-        if (col + k < n) {
-            if constexpr (sizeof(T) == 4) ((uint32_t*)row)[col + k] = w[k];
-            else ((uint16_t*)row)[col + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
-        }
+    for (int k = 0; k < 8; ++k)
+        if (col + k < n) ((uint16_t*)row)[col + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
 }
 
 // The place of row r of a tile-ordered map in the map itself, or -1: beyond the map, in the gap behind a line of pixels, or reused.
@@ -221,30 +236,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         __syncwarp();
     } else {
         // ---------------- scales, bias, ReLU, rounding, store ----------------
-        // A warp has 32 rows (the quadrant of tensor memory that it may read) and chunks of 128 bytes of their columns: of two warps with the
-        // same rows, each every second chunk.  It turns them through shared memory, so that eight lanes store 128 bytes of a row.
-        const int q = warp & 3, half = (warp - 2) >> 2, tid = threadIdx.x - 64;
-        constexpr int CW = 128 / (int)sizeof(T);              // columns of a chunk
+        // A warp has 32 rows (the quadrant of tensor memory that it may read) and of their columns 32 at a time: of the four warps with the same
+        // rows each every fourth.  A lane holds two neighbouring columns of four rows in each group of eight columns, so that it needs the scales and
+        // biases of a quarter of the columns: with a row per lane every lane needed all of them, and reading those from shared memory took
+        // more of its bandwidth than the operands (25088 x 512 x 2048 to bf16: 42 us).  Float32 goes straight to out, four lanes to
+        // 32 bytes; bfloat16 through shared memory, four lanes to 64 bytes.
+        const int q = warp & 3, part = (warp - 2) >> 2;
+        const float low = p.relu ? 0.f : __uint_as_float(0xff800000u);
         const uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 2) * kStage;
+        const uint32_t to_stage = stage + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);   // + 512 per eight rows
         const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
+        const bool pairs = (((uintptr_t)p.b_scale | (uintptr_t)p.bias) & 7) == 0;
         uint32_t acc = 0, acc_ph = 0;
         bool ok = true, there;
         for (int item = first; item < n_items; item += step) {
             const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * a.BN;
-            if (tid < a.BN) {
-                const int j = n0 + tid;
-                ctl->scale[acc][tid] = j < p.n ? __ldg(p.b_scale + j) : 0.f;
-                ctl->bias[acc][tid] = j < p.n && p.bias ? __ldg(p.bias + j) : 0.f;
-            }
-            const int64_t at = (int64_t)tile * kTileM + q * 32 + lane;
-            const int64_t mine = LIST ? (there ? out_row(p, tile, q * 32 + lane) : -1) : at;      // this lane's row of out
-            float sa = at < p.m ? p.a_scale[at] : 0.f;
-            const int rows = LIST ? 32 : there ? (int)min((int64_t)32, p.m - (at - lane)) : 0;     // rows that exist (LIST: where mine says so)
-            char* to = (char*)p.out + (size_t)(at - lane + (lane >> 3)) * p.out_pitch;             // not LIST: row lane / 8 of the 32
-            asm volatile("bar.sync 1, %0;" ::"n"(kEpiWarps * 32) : "memory");
+            const int64_t row0 = (int64_t)tile * kTileM + q * 32;                                  // of a
+            const int rows = LIST ? 32 : there ? (int)max((int64_t)0, min((int64_t)32, p.m - row0)) : 0;   // that exist (LIST: where `mine` says so)
+            const int64_t mine = LIST ? (there ? out_row(p, tile, q * 32 + lane) : -1) : 0;        // row `lane` in out
+            float sa[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sa[k] = row0 + 8 * k + (lane >> 2) < p.m ? p.a_scale[row0 + 8 * k + (lane >> 2)] : 0.f;
             if (ok) ok = wait_at(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, status);
             ok = __all_sync(0xffffffffu, ok);
-            if (!ok) sa = __uint_as_float(0x7fffffffu);       // a wait ran out: what is stored says so
+            if (!ok) sa[0] = sa[1] = sa[2] = sa[3] = __uint_as_float(0x7fffffffu);                 // a wait ran out: what is stored says so
             tc_fence_after();
             const uint32_t from = tmem_base + acc * (uint32_t)a.BN + ((uint32_t)(q * 32) << 16);
             const int n_here = min(a.BN, p.n - n0);
@@ -258,43 +273,67 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
                 }
                 held = false;
             };
-            for (int c0 = half * CW; c0 < n_here; c0 += 2 * CW) {
-                uint32_t v[CW];
+            for (int c0 = part * 32; c0 < n_here; c0 += 4 * 32) {
+                uint32_t v[2][16];
+                tmem_ld_16x32(from + c0, v[0]);
+                tmem_ld_16x32(from + (16u << 16) + c0, v[1]);
+                float2 s[4], b[4];
 #pragma unroll
-                for (int h = 0; h < CW / 32; ++h) tmem_ld32(from + c0 + h * 32, v + h * 32);
+                for (int j = 0; j < 4; ++j) {
+                    const int col = n0 + c0 + 8 * j + 2 * (lane & 3);
+                    s[j] = two_of(p.b_scale, col, p.n, pairs); b[j] = two_of(p.bias, col, p.n, pairs);
+                }
                 tmem_ld_wait();
-                if (c0 + 2 * CW >= n_here) hand_back();
-                constexpr int E = 4 / (int)sizeof(T);         // columns per word
-                const float4* const sc = (const float4*)&ctl->scale[acc][c0];
-                const float4* const bi = (const float4*)&ctl->bias[acc][c0];
+                if (c0 + 4 * 32 >= n_here) hand_back();
+                const bool fast = !LIST && a.wide && rows == 32 && c0 + 32 <= n_here;
+                if constexpr (sizeof(T) == 4) {
+                    const int col = n0 + c0 + 2 * (lane & 3);
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {                 // units of 16 bytes
-                    float f[4 * E];
+                    for (int k = 0; k < 4; ++k) {             // rows lane / 4 + 8 k
+                        const int r = 8 * k + (lane >> 2);
+                        const int64_t to = LIST ? __shfl_sync(0xffffffffu, mine, r) : r < rows ? row0 + r : -1;
+                        float* const out = (float*)((char*)p.out + (size_t)to * p.out_pitch) + col;
 #pragma unroll
-                    for (int k = 0; k < E; ++k) {
-                        const float4 s4 = sc[u * E + k], b4 = bi[u * E + k];
-                        const uint32_t* const w = v + (u * E + k) * 4;
-                        finish2(w[0], w[1], sa, s4.x, s4.y, b4.x, b4.y, f + 4 * k);
-                        finish2(w[2], w[3], sa, s4.z, s4.w, b4.z, b4.w, f + 4 * k + 2);
+                        for (int j = 0; j < 4; ++j) {
+                            float2 f = finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]);
+                            f = make_float2(at_least(f.x, low), at_least(f.y, low));
+                            if (fast) *(float2*)(out + 8 * j) = f;
+                            else if (to >= 0) {
+                                if (a.wide && col + 8 * j + 1 < p.n) *(float2*)(out + 8 * j) = f;
+                                else {
+                                    if (col + 8 * j < p.n) out[8 * j] = f.x;
+                                    if (col + 8 * j + 1 < p.n) out[8 * j + 1] = f.y;
+                                }
+                            }
+                        }
                     }
-                    if (p.relu)
+                } else {
 #pragma unroll
-                        for (int k = 0; k < 4 * E; ++k) f[k] = relu(f[k]);
-                    sts128(stage + lane * 128 + ((u ^ (lane & 7)) << 4), Out<T>::pack(f[0], f[E - 1]), Out<T>::pack(f[E], f[2 * E - 1]), Out<T>::pack(f[2 * E], f[3 * E - 1]),
-                           Out<T>::pack(f[3 * E], f[4 * E - 1]));
-                }
-                __syncwarp();
-                const int u = lane & 7, col = n0 + c0 + u * 4 * E;
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t w[4];
 #pragma unroll
-                for (int it = 0; it < 8; ++it) {
-                    const int r = it * 4 + (lane >> 3);
-                    const uint4 w = lds128(stage + r * 128 + ((u ^ (r & 7)) << 4));
-                    if (LIST) {
-                        const int64_t there_row = __shfl_sync(0xffffffffu, mine, r);
-                        if (there_row >= 0) store_unit<T>((char*)p.out + (size_t)there_row * p.out_pitch, col, p.n, w, a.wide);
-                    } else if (r < rows) store_unit<T>(to + (size_t)(it * 4) * p.out_pitch, col, p.n, w, a.wide);
+                        for (int j = 0; j < 4; ++j)
+                            w[j] = at_least_bf16(finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]), low);
+                        stmatrix4(to_stage + k * 512, w[0], w[1], w[2], w[3]);
+                    }
+                    __syncwarp();
+                    const int u = lane & 3, col = n0 + c0 + u * 8;
+                    char* const out = (char*)p.out + (size_t)(row0 + (lane >> 2)) * p.out_pitch;   // not LIST
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) {
+                        const int r = it * 8 + (lane >> 2);
+                        const uint4 w = lds128(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
+                        if (LIST) {
+                            const int64_t to = __shfl_sync(0xffffffffu, mine, r);
+                            if (to >= 0) store_unit((char*)p.out + (size_t)to * p.out_pitch, col, p.n, w, a.wide);
+                        } else if (fast) {
+                            *(uint4*)(out + (size_t)(it * 8) * p.out_pitch + (size_t)col * 2) = w;
+                        } else if (r < rows) {
+                            store_unit(out + (size_t)(it * 8) * p.out_pitch, col, p.n, w, a.wide);
+                        }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
             if (held) hand_back();                            // a warp whose columns do not exist
             if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
