@@ -18,7 +18,7 @@ namespace {
 constexpr unsigned long long kWaitNs = 2000000000ull;        // every wait on the device
 constexpr int kBytesK = 128;                                  // a stage: 128 values of K
 constexpr int kTileM = 128, kATile = kTileM * kBytesK;
-constexpr int kRing = 184 * 1024, kMaxStages = 7;
+constexpr int kMaxStages = 9;
 constexpr int kEpiWarps = 16, kThreads = (2 + kEpiWarps) * 32;
 constexpr int kStage = 32 * 64;                               // a warp's 32 rows on their way out, 64 bytes each
 
@@ -26,10 +26,11 @@ __device__ int32_t g_status;                                  // the status word
 
 struct ProductArgs {
     dc_product_args p;
+    int bufs;                                                 // places a warp stages its boxes in, 1 or 2
     int BN, NB, stages, stage_bytes, kchunks, k_last;         // columns per tile, column blocks; k_last: MMAs (32 values) of the last chunk
     int m_tiles;
     uint32_t idesc, tmem_cols;
-    int wide;                                                 // out takes 16-byte stores
+    int wide, boxes;                                          // out takes 16-byte stores; is written in boxes by TMA
 };
 
 struct Ctl {
@@ -38,8 +39,7 @@ struct Ctl {
     volatile int abort_flag;
     unsigned long long wait_ns;
 };
-constexpr size_t kSmem = kRing + kEpiWarps * kStage + sizeof(Ctl) + 1024;
-static_assert(kSmem <= 227 * 1024, "shared memory of an SM");
+constexpr int kSmem = 227 * 1024, kRoom = kSmem - 1024 - (int)sizeof(Ctl);      // for the ring and the staging
 
 // As DC_UMMA_CHUNK, for 8-bit integers: n (1 to 4) MMAs of K = 32.
 #define DC_UMMA_I8(name, group)                                                                                                                 \
@@ -78,14 +78,17 @@ __device__ __forceinline__ float2 finish2(uint32_t a0, uint32_t a1, float sa, fl
         : "=f"(f.x), "=f"(f.y) : "f"((float)(int)a0), "f"((float)(int)a1), "f"(sa), "f"(s.x), "f"(s.y), "f"(b.x), "f"(b.y));
     return f;
 }
-// ReLU or nothing: low is zero or minus infinity; a NaN stays.
-__device__ __forceinline__ float at_least(float v, float low) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(low)); return r; }
-__device__ __forceinline__ uint32_t at_least_bf16(float2 a, float low)
+// ReLU or nothing; a NaN stays.
+template <bool RELU> __device__ __forceinline__ float clamped(float v)
 {
-    const __nv_bfloat162 t = __floats2bfloat162_rn(a.x, a.y);
-    uint32_t r, lo = __float_as_uint(low);
-    lo |= lo >> 16;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(*(const uint32_t*)&t), "r"(lo));
+    if (RELU) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
+    return v;
+}
+template <bool RELU> __device__ __forceinline__ uint32_t two_bf16(float2 a)
+{
+    uint32_t r;
+    if (RELU) asm("cvt.rn.relu.bf16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a.x), "f"(a.y));
+    else asm("cvt.rn.bf16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a.x), "f"(a.y));
     return r;
 }
 // Sixteen rows x 32 columns of tensor memory: column group j (8 columns) in r[4 j ...]; a lane has columns 2 (lane % 4), + 1 of rows lane / 4
@@ -100,12 +103,38 @@ __device__ __forceinline__ void stmatrix4(uint32_t addr, uint32_t a, uint32_t b,
 {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// Two neighbouring columns' weights, from `col` on; beyond the last: zeros.
-__device__ __forceinline__ float2 two_of(const float* p, int col, int n, bool pairs)
+// A warp's staged 32 rows of 64 bytes on their way to out; lane 0 issues.
+__device__ __forceinline__ void store_box(const CUtensorMap* tm, uint32_t stage, int col, int row)
 {
-    if (!p) return make_float2(0.f, 0.f);
-    if (pairs && col + 1 < n) return __ldg((const float2*)(p + col));
-    return make_float2(col < n ? __ldg(p + col) : 0.f, col + 1 < n ? __ldg(p + col + 1) : 0.f);
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(stage), "r"(col), "r"(row) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void store_read(int bufs)          // the place that comes next is free
+{
+    if (bufs == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+    else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+__device__ __forceinline__ void store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// The scales and biases of two neighbouring columns in each of four groups of eight, from `col` on; beyond the last column: zeros.
+__device__ __forceinline__ void column_weights(const dc_product_args& p, int col, bool whole, float2* s, float2* b)
+{
+    if (whole) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = __ldg((const float2*)(p.b_scale + col + 8 * j));
+        if (p.bias)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = __ldg((const float2*)(p.bias + col + 8 * j));
+        else
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = make_float2(0.f, 0.f);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int c = col + 8 * j;
+        s[j] = make_float2(c < p.n ? __ldg(p.b_scale + c) : 0.f, c + 1 < p.n ? __ldg(p.b_scale + c + 1) : 0.f);
+        b[j] = make_float2(p.bias && c < p.n ? __ldg(p.bias + c) : 0.f, p.bias && c + 1 < p.n ? __ldg(p.bias + c + 1) : 0.f);
+    }
 }
 
 // Eight bfloat16 of a row of out from column `col` on; n: the row's length.
@@ -130,13 +159,13 @@ __device__ __forceinline__ int64_t out_row(const dc_product_args& p, int tile, i
 }
 
 // LIST: a partial convolution's pixels (tile_list, masks, gaps behind lines).
-template <bool PAIR, bool LIST, typename T>
-__global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const ProductArgs a)
+template <bool PAIR, bool LIST, bool RELU, typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC, const ProductArgs a)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint8_t* staging = ring + kRing;
-    Ctl* ctl = (Ctl*)(staging + kEpiWarps * kStage);
+    uint8_t* staging = ring + a.stages * a.stage_bytes;
+    Ctl* ctl = (Ctl*)(staging + kEpiWarps * kStage * a.bufs);
     const dc_product_args& p = a.p;
     int32_t* const status = p.status ? p.status : &g_status;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -239,16 +268,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         // A warp has 32 rows (the quadrant of tensor memory that it may read) and of their columns 32 at a time: of the four warps with the same
         // rows each every fourth.  A lane holds two neighbouring columns of four rows in each group of eight columns, so that it needs the scales and
         // biases of a quarter of the columns: with a row per lane every lane needed all of them, and reading those from shared memory took
-        // more of its bandwidth than the operands (25088 x 512 x 2048 to bf16: 42 us).  Float32 goes straight to out, four lanes to
-        // 32 bytes; bfloat16 through shared memory, four lanes to 64 bytes.
+        // more of its bandwidth than the operands.  Where out takes 16-byte stores the warp turns its rows through shared memory and they leave
+        // as boxes of 32 rows x 64 bytes by TMA: 25088 x 512 x 2048 to bf16 in 30.6 us, 3.36 TB/s written (a fill of that size: 3.8), with
+        // the lanes' own stores of 64 bytes of a row 40.0, of 128 bytes 45.1.
         const int q = warp & 3, part = (warp - 2) >> 2;
-        const float low = p.relu ? 0.f : __uint_as_float(0xff800000u);
-        const uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 2) * kStage;
-        const uint32_t to_stage = stage + (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);   // + 512 per eight rows
+        uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 2) * kStage;
+        const uint32_t to_stage = (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);           // + 512 per eight rows
+        const uint32_t both = a.bufs == 2 ? stage ^ (stage + kEpiWarps * kStage) : 0;                   // from one place to the other
         const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
         const bool pairs = (((uintptr_t)p.b_scale | (uintptr_t)p.bias) & 7) == 0;
         uint32_t acc = 0, acc_ph = 0;
         bool ok = true, there;
+        auto row_scales = [&](int tile, float* s) {
+            const int64_t r = (int64_t)tile * kTileM + q * 32 + (lane >> 2);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] = r + 8 * k < p.m ? p.a_scale[r + 8 * k] : 0.f;
+        };
+        float next[4];
+        if (first < n_items) row_scales(tile_of(first / a.NB, &there), next);
         for (int item = first; item < n_items; item += step) {
             const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * a.BN;
             const int64_t row0 = (int64_t)tile * kTileM + q * 32;                                  // of a
@@ -256,7 +293,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
             const int64_t mine = LIST ? (there ? out_row(p, tile, q * 32 + lane) : -1) : 0;        // row `lane` in out
             float sa[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sa[k] = row0 + 8 * k + (lane >> 2) < p.m ? p.a_scale[row0 + 8 * k + (lane >> 2)] : 0.f;
+            for (int k = 0; k < 4; ++k) sa[k] = next[k];
+            bool later;
+            if (item + step < n_items) row_scales(tile_of((item + step) / a.NB, &later), next);      // on their way meanwhile
             if (ok) ok = wait_at(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) sa[0] = sa[1] = sa[2] = sa[3] = __uint_as_float(0x7fffffffu);                 // a wait ran out: what is stored says so
@@ -278,15 +317,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
                 tmem_ld_16x32(from + c0, v[0]);
                 tmem_ld_16x32(from + (16u << 16) + c0, v[1]);
                 float2 s[4], b[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int col = n0 + c0 + 8 * j + 2 * (lane & 3);
-                    s[j] = two_of(p.b_scale, col, p.n, pairs); b[j] = two_of(p.bias, col, p.n, pairs);
-                }
+                column_weights(p, n0 + c0 + 2 * (lane & 3), pairs && c0 + 32 <= n_here, s, b);
                 tmem_ld_wait();
                 if (c0 + 4 * 32 >= n_here) hand_back();
                 const bool fast = !LIST && a.wide && rows == 32 && c0 + 32 <= n_here;
-                if constexpr (sizeof(T) == 4) {
+                if (sizeof(T) == 4 && a.boxes) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {             // 16 columns at a time
+                        if (lane == 0) store_read(a.bufs);
+                        __syncwarp();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int j = 2 * h; j < 2 * h + 2; ++j) {
+                                const float2 f = finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]);
+                                const int r = 8 * k + (lane >> 2), u = 2 * (j & 1) + ((lane >> 1) & 1);
+                                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4) + 8 * (lane & 1)), "f"(clamped<RELU>(f.x)),
+                                             "f"(clamped<RELU>(f.y)) : "memory");
+                            }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0 && rows > 0) store_box(&tmC, stage, n0 + c0 + 16 * h, (int)row0);
+                        stage ^= both;
+                    }
+                } else if constexpr (sizeof(T) == 4) {
                     const int col = n0 + c0 + 2 * (lane & 3);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {             // rows lane / 4 + 8 k
@@ -296,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             float2 f = finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]);
-                            f = make_float2(at_least(f.x, low), at_least(f.y, low));
+                            f = make_float2(clamped<RELU>(f.x), clamped<RELU>(f.y));
                             if (fast) *(float2*)(out + 8 * j) = f;
                             else if (to >= 0) {
                                 if (a.wide && col + 8 * j + 1 < p.n) *(float2*)(out + 8 * j) = f;
@@ -308,13 +362,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
                         }
                     }
                 } else {
+                    if (a.boxes) {                            // the box before has left its place
+                        if (lane == 0) store_read(a.bufs);
+                        __syncwarp();
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         uint32_t w[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
-                            w[j] = at_least_bf16(finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]), low);
-                        stmatrix4(to_stage + k * 512, w[0], w[1], w[2], w[3]);
+                            w[j] = two_bf16<RELU>(finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]));
+                        stmatrix4(stage + to_stage + k * 512, w[0], w[1], w[2], w[3]);
+                    }
+                    if (a.boxes) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0 && rows > 0) store_box(&tmC, stage, n0 + c0, (int)row0);
+                        stage ^= both;
+                        continue;
                     }
                     __syncwarp();
                     const int u = lane & 3, col = n0 + c0 + u * 8;
@@ -338,6 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
             if (held) hand_back();                            // a warp whose columns do not exist
             if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
         }
+        if (a.boxes && lane == 0) store_done();
     }
     tc_fence_before();
     __syncthreads();
@@ -375,11 +441,21 @@ bool encode_rows(CUtensorMap* tm, const void* base, size_t pitch, int64_t rows, 
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, bool LIST, typename T>
-int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const ProductArgs& a, int ctas, int device, cudaStream_t stream)
+// out in boxes of 32 rows x 64 bytes; nothing is written beyond the last row and column.
+bool encode_out(CUtensorMap* tm, const dc_product_args& p, int elt)
+{
+    const size_t pitch = p.m < 2 ? ((size_t)p.n * elt + 15) / 16 * 16 : p.out_pitch;
+    const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m}, strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {(cuuint32_t)(64 / elt), 32}, elem[2] = {1, 1};
+    return encode_fn()(tm, elt == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p.out, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                       CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool PAIR, bool LIST, bool RELU, typename T>
+int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, const ProductArgs& a, int ctas, int device, cudaStream_t stream)
 {
     static dc_once_per_device attr_set;
-    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product<PAIR, LIST, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem));
+    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product<PAIR, LIST, RELU, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -389,7 +465,7 @@ int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const Product
     cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = kSmem; cfg.stream = stream;
     // g_dc_pdl off: see dc_launch_pdl
     cfg.attrs = g_dc_pdl ? attr : attr + 1; cfg.numAttrs = g_dc_pdl ? 2 : 1;
-    DC_CUDA(cudaLaunchKernelEx(&cfg, k_product<PAIR, LIST, T>, tmA, tmB, a));
+    DC_CUDA(cudaLaunchKernelEx(&cfg, k_product<PAIR, LIST, RELU, T>, tmA, tmB, tmC, a));
     return DC_OK;
 }
 
@@ -402,36 +478,44 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
     a.p = p;
     a.m_tiles = (int)((p.m + kTileM - 1) / kTileM);
     const long long tiles = p.tile_list ? p.max_tiles : a.m_tiles;
-    // Pairs where their items of 256 x 256 fill the SMs; else the columns per tile that take the fewest turns, a tile counting its columns and the
-    // quarter of a tile that it takes to fill and drain.
-    const bool pair = p.n > 128 && (tiles + 1) / 2 * dc_div_up(p.n, 256) >= num_sms / 2;
-    a.BN = 256;
-    if (!pair) {
-        long long best = -1;
-        for (int bn = 64; bn <= 128; bn *= 2) {
-            const long long turns = (tiles * dc_div_up(p.n, bn) + num_sms - 1) / num_sms, cost = turns * (bn + 64);
-            if (best < 0 || cost <= best) { best = cost; a.BN = bn; }
-        }
+    // The tile that takes the fewest cycles, as counted from measurements: operands arrive at about 50 bytes a cycle, an SM's share of out leaves
+    // at about 24 where others pause, and an item costs 500 to begin and end.
+    const int elt = dtype == DC_BF16 ? 2 : 4, kc = dc_div_up(p.k, kBytesK);
+    bool pair = false;
+    double best = 0.0;
+    for (int c = 0; c < 4; ++c) {
+        const bool two = c < 2;
+        const int bn = c == 0 ? 256 : c == 3 ? 64 : 128;
+        const long long n_items = (two ? (tiles + 1) / 2 : tiles) * dc_div_up(p.n, bn), at_once = two ? num_sms / 2 : num_sms, rounds = (n_items + at_once - 1) / at_once;
+        const double load = kc * (double)(kATile + (two ? bn / 2 : bn) * kBytesK) / 50.0, mma = kc * 2.0 * bn, out = 128.0 * bn * elt / 24.0;
+        const double cost = rounds * ((load > mma ? load : mma) + out + 500.0);
+        if (c == 0 || cost < best) { best = cost; pair = two; a.BN = bn; }
     }
     a.NB = dc_div_up(p.n, a.BN);
     const int b_rows = pair ? a.BN / 2 : a.BN;
     a.stage_bytes = kATile + b_rows * kBytesK;
-    a.stages = kRing / a.stage_bytes < kMaxStages ? kRing / a.stage_bytes : kMaxStages;
-    a.kchunks = dc_div_up(p.k, kBytesK);
+    a.bufs = kc <= 8 ? 2 : 1;                                 // long products take the room for operands
+    a.stages = (kRoom - kEpiWarps * kStage * a.bufs) / a.stage_bytes;
+    if (a.stages > kMaxStages) a.stages = kMaxStages;
+    a.kchunks = kc;
     a.k_last = dc_div_up(p.k - (a.kchunks - 1) * kBytesK, 32);
     // int32 accumulators, both operands signed 8-bit integers, K-major
     a.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(a.BN >> 3) << 17) | ((uint32_t)((pair ? 256 : 128) >> 4) << 24);
     a.tmem_cols = (uint32_t)(2 * a.BN);
     a.wide = (uintptr_t)p.out % 16 == 0 && p.out_pitch % 16 == 0;
-    CUtensorMap tmA, tmB;
+    CUtensorMap tmA, tmB, tmC = {};
     if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
+    if (a.wide && !p.padded) a.boxes = encode_out(&tmC, p, dtype == DC_BF16 ? 2 : 4);
     const long long items = (pair ? (tiles + 1) / 2 : tiles) * a.NB, cap = pair ? num_sms / 2 : num_sms;
     if (items >= 0x70000000) return DC_ERR_LIMIT;
     const int ctas = (int)(items < cap ? items : cap) * (pair ? 2 : 1);
-#define DC_PRODUCT(PAIR, T) return p.padded ? launch_product<PAIR, true, T>(tmA, tmB, a, ctas, device, stream) : launch_product<PAIR, false, T>(tmA, tmB, a, ctas, device, stream)
-    if (dtype == DC_BF16) { if (pair) DC_PRODUCT(true, __nv_bfloat16); DC_PRODUCT(false, __nv_bfloat16); }
-    if (pair) DC_PRODUCT(true, float);
-    DC_PRODUCT(false, float);
+#define DC_PRODUCT(PAIR, LIST, RELU, T) return launch_product<PAIR, LIST, RELU, T>(tmA, tmB, tmC, a, ctas, device, stream)
+#define DC_PRODUCT_OF(LIST, RELU, T) do { if (pair) DC_PRODUCT(true, LIST, RELU, T); DC_PRODUCT(false, LIST, RELU, T); } while (0)
+#define DC_PRODUCT_TO(T) do { if (p.padded) { if (p.relu) DC_PRODUCT_OF(true, true, T); DC_PRODUCT_OF(true, false, T); } if (p.relu) DC_PRODUCT_OF(false, true, T); DC_PRODUCT_OF(false, false, T); } while (0)
+    if (dtype == DC_BF16) DC_PRODUCT_TO(__nv_bfloat16);
+    DC_PRODUCT_TO(float);
+#undef DC_PRODUCT_TO
+#undef DC_PRODUCT_OF
 #undef DC_PRODUCT
 }
 
