@@ -273,20 +273,26 @@ def dc_search_blocks_noalloc(frame, prev, pitch, width, height, n_streams, block
 # layer normalisation and 8-bit rows: maps as torch tensors [..., channels]
 # --------------------------------------------------------------------------
 _DTYPES = {torch.float32: DC_FP32, torch.bfloat16: DC_BF16}
+_SIZES = {torch.float32: 4, torch.bfloat16: 2}
+_INT8 = {torch.int8: 1}
+# torch's current stream and device, asked for without an object or a context check: a short call costs about what its arguments do
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _rows(t, what, dtypes=_DTYPES):
+def _rows(t, what, sizes=_SIZES):
     """(address, pitch in bytes, rows, channels) of a map whose rows lie a constant stride apart."""
-    if t.dtype not in dtypes:
+    size = sizes.get(t.dtype)
+    if size is None:
         raise TypeError(f"{what}: unsupported type {t.dtype}")
     shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        rows, c = shape
+        if stride[1] == 1 or c < 2:
+            return t.data_ptr(), (stride[0] if rows > 1 else c) * size, rows, c
     if len(shape) < 1 or (shape[-1] > 1 and stride[-1] != 1):
         raise ValueError(f"{what}: a row's elements have to lie side by side")
-    c, size = shape[-1], t.element_size()
-    if len(shape) == 2:
-        return t.data_ptr(), (stride[0] if shape[0] > 1 else c) * size, shape[0], c
-    rows = 1
-    pitch = None
+    c, rows, pitch = shape[-1], 1, None
     for n, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
         if n == 0:
             return t.data_ptr(), c * size, 0, c
@@ -303,7 +309,7 @@ def _vector(t, n, what):
     """Address of a float32 vector of n values, or None."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what}: a contiguous float32 vector of {n} values is needed")
     return t.data_ptr()
 
@@ -311,22 +317,25 @@ def _vector(t, n, what):
 def _on_device(where, stream, tensors, *args):
     """One call of the library on the device that the tensors are on; stream: a cudaStream_t, or None for torch's current one there."""
     dev = tensors[0].get_device()
+    if dev < 0:
+        raise ValueError(f"{where}: all tensors have to be on one CUDA device")
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != dev):
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"{where}: all tensors have to be on one CUDA device")
-    st = torch.cuda.current_stream(dev).cuda_stream if stream is None else stream
-    fn = getattr(load(), where)
-    if dev == torch.cuda.current_device():
-        rc = fn(*args, st)
+    if stream is None:
+        stream = _raw_stream(dev)
+    fn = getattr(_lib or load(), where)
+    if dev == _raw_device():
+        rc = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, st)
+            rc = fn(*args, stream)
     if rc != DC_OK:
         raise DeepCacheError(rc, where)
 
 
 def _same_rows(a, b, what):
-    if a[2:] != b[2:]:
+    if a[3] != b[3] or a[2] != b[2]:
         raise ValueError(f"{what}: {b[2]} rows of {b[3]} where {a[2]} of {a[3]} are needed")
 
 
@@ -351,7 +360,7 @@ def _scratch(t, what):
         return None, 0
     if not t.is_contiguous():
         raise ValueError(f"{what}: has to be contiguous")
-    return t.data_ptr(), t.numel() * t.element_size()
+    return t.data_ptr(), t.nbytes
 
 
 def dc_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, workspace=None, stream=None):
@@ -370,9 +379,6 @@ def dc_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta
     _on_device("dc_layer_norm_backward", stream, (x, dy, gamma, mean, rstd, dx, dgamma, dbeta, workspace), dr[0], dr[1], xr[0], xr[1], _vector(gamma, xr[3], "gamma"),
                _vector(mean, xr[2], "mean"), _vector(rstd, xr[2], "rstd"), xr[2], xr[3], _DTYPES[x.dtype], ox[0], ox[1], _vector(dgamma, xr[3], "dgamma"),
                _vector(dbeta, xr[3], "dbeta"), wp, wn)
-
-
-_INT8 = (torch.int8,)
 
 
 def dc_quantize_rows(x, q, scale, stream=None):

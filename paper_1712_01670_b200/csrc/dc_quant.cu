@@ -415,6 +415,160 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
     }
 }
 
+// Few tiles: the reduction of 128 output channels x up to 128 rows split over a cluster of CTAs, as in dc_conv_cluster.cu.  What bounds such
+// products are the weights, each read once, so the weights are the side of 128 rows (tensor memory's lanes), the rows of x (16 to 128 of them) its columns, and the split
+// makes enough CTAs for the weights to stream at HBM's rate.  Each CTA takes its part of K; the int32 sums meet in distributed shared memory, where CTA r
+// finishes channels r * 128 / CS and on; they are exact, so the split changes no bit.  `early`: everything older than the kernel before is
+// complete (dc_linear_quantized: that kernel puts x into 8 bits), so the weights' loads start before the wait for it.
+// One row, 9216 -> 4096: 29 us with k_product's 64 CTAs that walk K alone.
+constexpr int kSplitThreads = 192, kSplitStages = 12;
+struct SplitArgs {
+    dc_product_args p;
+    int NT, CS, stages, stage_bytes, kchunks, k_last, m_tiles, early;     // NT: rows of x in a tile
+    uint32_t idesc, tmem_cols;
+};
+struct SplitCtl {
+    unsigned long long full[kSplitStages], empty[kSplitStages], done;
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    unsigned long long wait_ns;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const SplitArgs a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    int32_t* red = (int32_t*)(ring + (size_t)a.stages * a.stage_bytes);      // [CS][NT][128 / CS]: this CTA's channels, from every CTA
+    SplitCtl* ctl = (SplitCtl*)(red + 128 * a.NT);
+    const dc_product_args& p = a.p;
+    int32_t* const status = p.status ? p.status : &g_status;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank(), item = blockIdx.x / a.CS, mt = item % a.m_tiles, nt = item / a.m_tiles;
+    const int k0 = rank * a.kchunks / a.CS, nk = (rank + 1) * a.kchunks / a.CS - k0;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 2); mbar_init(&ctl->empty[i], 1); }   // weights and rows arrive apart
+        mbar_init(&ctl->done, 1);
+        ctl->abort_flag = 0;
+        ctl->wait_ns = kWaitNs;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(a.tmem_cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // waited for before another CTA's shared memory is written
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
+    const int ahead = nk < a.stages ? nk : a.stages;
+    auto load_weights = [&](int it, uint32_t off, uint32_t slot) {
+        mbar_expect_tx(full0 + off, (uint32_t)kATile);
+        tma_load_2d(slot, &tmW, (k0 + it) * kBytesK, nt * kTileM, full0 + off);
+    };
+    if (!a.early) { dc_pdl_wait(); dc_pdl_release(); }
+    if (warp == 0 && elect_one())
+        for (int it = 0; it < ahead; ++it) load_weights(it, 8u * it, ring0 + it * a.stage_bytes);
+    __syncwarp();
+    if (a.early) { dc_pdl_wait(); dc_pdl_release(); }
+
+    bool waited = false;                                                     // for the cluster
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        if (elect_one()) {
+            RingPos r;
+            r.start(ring0, (uint32_t)a.stages);
+            bool ok = true;
+            for (int it = 0; it < nk; ++it) {
+                if (it >= a.stages) {
+                    ok = mbar_wait_at(empty0 + r.off, r.phase ^ 1u, &ctl->abort_flag, &ctl->wait_ns, status);
+                    if (!ok) break;
+                    load_weights(it, r.off, r.data);
+                }
+                mbar_expect_tx(full0 + r.off, (uint32_t)(a.NT * kBytesK));
+                tma_load_2d(r.data + kATile, &tmX, (k0 + it) * kBytesK, mt * a.NT, full0 + r.off);
+                r.next(ring0, (uint32_t)a.stages, (uint32_t)a.stage_bytes);
+            }
+            if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        if (elect_one()) {
+            const uint64_t dconst = umma_desc(0, 1024, 2);
+            const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
+            RingPos r;
+            r.start(r0, (uint32_t)a.stages);
+            for (int it = 0; it < nk; ++it) {
+                if (!mbar_wait_at(full0 + r.off, r.phase, &ctl->abort_flag, &ctl->wait_ns, status)) break;
+                tc_fence_after();
+                umma_i8(tmem_base, r.data, r.data + (kATile >> 4), d_hi, a.idesc, it != 0, k0 + it + 1 < a.kchunks ? 4 : a.k_last);
+                if (it + a.stages < nk) umma_commit_at(empty0 + r.off);
+                if (it + 1 == nk) umma_commit(&ctl->done);
+                r.next(r0, (uint32_t)a.stages, slot);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- partial sums to the CTA that finishes the channel ----------------
+        const int q = warp & 3, m = q * 32 + lane, rows = 128 / a.CS, owner = m / rows;
+        const uint32_t dst = map_to_cta(red + (size_t)rank * a.NT * rows + (m - owner * rows), (uint32_t)owner);
+        bool ok = mbar_wait_at(smem_u32(&ctl->done), 0, &ctl->abort_flag, &ctl->wait_ns, status);
+        ok = __all_sync(0xffffffffu, ok);
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        waited = true;
+        if (ok) {
+            tc_fence_after();
+            const int there = (int)min((int64_t)a.NT, p.m - (int64_t)mt * a.NT);
+            for (int c = 0; c < a.NT && c < there; c += 16) {
+                uint32_t v[16];
+                asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                             : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                               "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                             : "r"(tmem_base + ((uint32_t)(q * 32) << 16) + c) : "memory");
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (c + k < there) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(dst + (uint32_t)((c + k) * rows * 4)), "r"(v[k]) : "memory");
+            }
+        }
+        tc_fence_before();
+    }
+    if (!waited) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    // a CTA that gave up has not sent its sums: every CTA of the cluster hears of it
+    if (ctl->abort_flag != 0)
+        for (int r = 0; r < a.CS; ++r)
+            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_to_cta((const void*)&ctl->abort_flag, (uint32_t)r)), "r"(1) : "memory");
+    cluster_sync_all();                      // this CTA's channels have arrived from every CTA
+    {
+        // ---------------- this CTA's channels: sums from all ranks, scales, bias, ReLU, rounding, store ----------------
+        const int rows = 128 / a.CS, there = (int)min((int64_t)a.NT, p.m - (int64_t)mt * a.NT);
+        const bool dead = ctl->abort_flag != 0;                              // what is stored says so
+        for (int u = threadIdx.x; u < rows * there; u += kSplitThreads) {
+            const int t = u / rows, ch = u - t * rows, j = nt * kTileM + rank * rows + ch;
+            if (j >= p.n) continue;
+            int32_t sum = 0;
+            for (int r = 0; r < a.CS; ++r) sum += red[((size_t)r * a.NT + t) * rows + ch];
+            const int64_t row = (int64_t)mt * a.NT + t;
+            const float sa = dead ? __uint_as_float(0x7fffffffu) : p.a_scale[row];
+            float f = fmaf((float)sum * sa, __ldg(p.b_scale + j), p.bias ? __ldg(p.bias + j) : 0.f);
+            if (p.relu) f = clamped<true>(f);
+            T* const out = (T*)((char*)p.out + (size_t)row * p.out_pitch) + j;
+            if constexpr (sizeof(T) == 4) *out = f;
+            else *out = __float2bfloat16_rn(f);
+        }
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(a.tmem_cols) : "memory");
+    }
+}
+
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeFn encode_fn()
@@ -469,6 +623,49 @@ int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtenso
     return DC_OK;
 }
 
+// How a product of few tiles is split, and the cycles that it takes (as dc_launch_product counts them).
+struct SplitPlan { int NT, CS; double cost; };
+SplitPlan split_plan(const dc_product_args& p, int kc, int num_sms)
+{
+    SplitPlan s;
+    s.NT = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
+    const long long tiles = (p.m + s.NT - 1) / s.NT * (long long)dc_div_up(p.n, kTileM);
+    s.CS = 1;
+    while (s.CS < 8 && 2 * s.CS <= kc && tiles * 2 * s.CS <= num_sms) s.CS *= 2;
+    const long long rounds = (tiles * s.CS + num_sms - 1) / num_sms;
+    s.cost = rounds * (dc_div_up(kc, s.CS) * (double)(kATile + s.NT * kBytesK) / 50.0 + 8.0 * s.NT + 1500.0);
+    return s;
+}
+
+template <typename T>
+int launch_split(const dc_product_args& p, const SplitPlan& s, int kc, int device, cudaStream_t stream)
+{
+    SplitArgs a = {};
+    a.p = p; a.NT = s.NT; a.CS = s.CS; a.kchunks = kc; a.k_last = dc_div_up(p.k - (kc - 1) * kBytesK, 32); a.early = p.early;
+    a.m_tiles = (int)((p.m + s.NT - 1) / s.NT);
+    a.stage_bytes = kATile + s.NT * kBytesK;
+    const int red = 128 * s.NT * 4, fixed = red + (int)sizeof(SplitCtl) + 1024, room = (227 * 1024 - fixed) / a.stage_bytes, most = dc_div_up(kc, s.CS);
+    a.stages = room < kSplitStages ? room : kSplitStages;
+    if (a.stages > most) a.stages = most;
+    a.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(s.NT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    a.tmem_cols = s.NT < 32 ? 32u : (uint32_t)s.NT;
+    CUtensorMap tmW, tmX;
+    if (!encode_rows(&tmW, p.b, p.b_pitch, p.n, p.k, kTileM) || !encode_rows(&tmX, p.a, p.a_pitch, p.m, p.k, s.NT)) return DC_ERR_CUDA;
+    static dc_once_per_device attr_set;
+    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product_split<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)s.CS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.m_tiles * dc_div_up(p.n, kTileM) * s.CS)); cfg.blockDim = dim3(kSplitThreads);
+    cfg.dynamicSmemBytes = (size_t)a.stages * a.stage_bytes + fixed; cfg.stream = stream;
+    cfg.attrs = attr; cfg.numAttrs = g_dc_pdl ? 2 : 1;
+    DC_CUDA(cudaLaunchKernelEx(&cfg, k_product_split<T>, tmW, tmX, a));
+    return DC_OK;
+}
+
 }  // namespace
 
 int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_sms, cudaStream_t stream)
@@ -490,6 +687,10 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
         const double load = kc * (double)(kATile + (two ? bn / 2 : bn) * kBytesK) / 50.0, mma = kc * 2.0 * bn, out = 128.0 * bn * elt / 24.0;
         const double cost = rounds * ((load > mma ? load : mma) + out + 500.0);
         if (c == 0 || cost < best) { best = cost; pair = two; a.BN = bn; }
+    }
+    if (!p.padded && p.n <= (1 << 20) && p.m <= (1 << 20)) {
+        const SplitPlan s = split_plan(p, kc, num_sms);
+        if (s.CS > 1 && s.cost < best) return dtype == DC_BF16 ? launch_split<__nv_bfloat16>(p, s, kc, device, stream) : launch_split<float>(p, s, kc, device, stream);
     }
     a.NB = dc_div_up(p.n, a.BN);
     const int b_rows = pair ? a.BN / 2 : a.BN;
@@ -577,7 +778,7 @@ int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, 
     if ((rc = dc_launch_rows(r, false, dtype, sms, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
     dc_product_args p = {};
     p.a = q; p.a_pitch = pitch; p.a_scale = scale; p.b = w_dev; p.b_pitch = w_pitch; p.b_scale = w_scale_dev; p.bias = bias_dev;
-    p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch;
+    p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch; p.early = 1;
     return dc_launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
 }
 

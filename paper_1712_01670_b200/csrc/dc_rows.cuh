@@ -26,6 +26,7 @@ struct dc_product_args {
     int64_t m; int n, k, relu;
     void* out; size_t out_pitch;
     int32_t* status;                    // device status word, or NULL
+    int early;                          // 1: the weights (b, b_scale, bias) are older than the kernel before, which waits for its own predecessor
     // A partial convolution's pixels (NULL, 0: every row): tiles of 128 rows of a, in images of `padded` rows per line of `width` pixels
     const int32_t *tile_list, *tile_count; const uint32_t* masks;
     int width, padded, max_tiles;
