@@ -65,7 +65,7 @@ typedef struct { int32_t x, y, w, h, sx, sy; } dc_region;
 
 typedef enum {
     DC_CONV = 0, DC_MAXPOOL = 1, DC_RELU = 2, DC_ADD = 3, DC_CONCAT = 4,
-    DC_RESIZE_AREA = 5, DC_LRN = 6, DC_FC = 7
+    DC_RESIZE_AREA = 5, DC_LRN = 6, DC_FC = 7, DC_LAYER_NORM = 8, DC_CONV_QUANT = 9
 } dc_layer_kind;
 
 /* One layer.  in0 / in1: index of the producing layer, -1 = the input frame
@@ -80,6 +80,13 @@ typedef enum {
  * DC_FC: fully connected; executable when kh, kw equal the input map's height and width (then it is the convolution
  *   whose kernel covers the whole map: weights [cout][kh][kw][cin], out 1 x 1, optional ReLU).  Table 2: nothing of
  *   its output is reusable.
+ * DC_LAYER_NORM: layer normalisation over the channels of each pixel (see dc_layer_norm; at most 16384 channels): weights_dev[i] = gamma [c],
+ *   bias_dev[i] = beta [c], either may be NULL (ones, zeros); epsilon 1e-5 unless dc_cache_set_norm_epsilon says otherwise.  Per pixel, so a
+ *   rectangle passes unchanged (Table 2, "others").
+ * DC_CONV_QUANT: a convolution in 8-bit integers with a scale for each pixel and each output channel (see dc_linear_quantized), optional ReLU,
+ *   weights [cout][kh][kw][cin] float32 as for DC_CONV, put into 8 bits at creation; at most 131071 terms.  Either pointwise (kh = kw = sh = sw = 1, no padding, out =
+ *   in): a pixel's scale depends on that pixel alone, so its output is cached and reused like any convolution's; or with a kernel that covers the whole input map
+ *   (out 1 x 1): a fully connected layer, one scale per stream, nothing of it reusable.
  * A layer table with an LRN or FC layer of another shape is accepted for region propagation, but such a cache
  * cannot run dc_infer_frame.
  * Limit: an executable cache takes DC_CONV and DC_FC kernels of at most 11 columns (kw <= 11; any kh);
@@ -140,7 +147,7 @@ typedef struct dc_cache dc_cache;      /* opaque, owned by the library */
 /* Builds a cache for one network and one frame geometry: validates, allocates the
  * key-frame buffer, two maps per convolution (current / cached), one per other layer,
  * region tables and tile lists, and converts the weights.  weights_dev[i] / bias_dev[i]
- * are float32 device arrays for DC_CONV layers and ignored (may be NULL) otherwise; they
+ * are float32 device arrays for DC_CONV, DC_CONV_QUANT and DC_LAYER_NORM layers and ignored (may be NULL) otherwise; they
  * are read during this call only.  cuda_stream is a cudaStream_t (NULL = default stream).
  * Synchronous.  Errors: DC_ERR_ARG, DC_ERR_CONFIG, DC_ERR_ALLOC, DC_ERR_CUDA. */
 int dc_cache_create(const dc_config* cfg, const dc_layer_desc* layers, int n_layers,
@@ -152,6 +159,9 @@ int dc_cache_destroy(dc_cache* cache);
 
 /* Empties the cache: the next dc_infer_frame is a full fresh frame (Section 5, expiry). */
 int dc_cache_reset(dc_cache* cache);
+
+/* The epsilon of a DC_LAYER_NORM layer (>= 0; 1e-5 at creation).  Empties the cache, as dc_cache_reset.  Errors: DC_ERR_ARG. */
+int dc_cache_set_norm_epsilon(dc_cache* cache, int layer, double eps);
 
 /* Device bytes held by the cache (cf. the memory overhead of Section 7.7). */
 int dc_cache_bytes(const dc_cache* cache, size_t* bytes);
@@ -184,7 +194,7 @@ int dc_match_blocks(dc_cache* cache, const uint8_t* frame_dev, size_t pitch_byte
 int dc_propagate_regions(dc_cache* cache, const dc_region* in_dev, const int32_t* n_in_dev,
                          int layer_begin, int layer_end, dc_region* out_dev, int32_t* n_out_dev);
 
-/* Section 5 "Reuse" for convolution layer `layer` (c_forward(top, bottom, c_blob, c_regions)
+/* Section 5 "Reuse" for convolution layer `layer` (DC_CONV, an executable DC_FC, DC_CONV_QUANT) (c_forward(top, bottom, c_blob, c_regions)
  * of Section 6): output pixels inside a rectangle are copied from prev_out_dev at the mapped
  * position, all others are convolved (+bias, +ReLU) from in_map_dev.
  *   in_map_dev    [S][Hi][Wi][cin]   complete input map (bottom blob)
@@ -254,7 +264,7 @@ int dc_cache_layer_regions(dc_cache* cache, int layer, dc_region** regions_dev, 
  * 0 a CUDA-core kernel (channel counts the tensor-core kernels cannot take) or any kernel of an fp32 cache, 1-10 a bf16 tensor-core
  * operand scheme (1, 2 tap by tap; 3, 4 input patch; 5, 6 column slabs; 7 column slabs on CTA pairs; 8, 9 tap by
  * tap on tiles made of 16 row pieces of 8 pixels taken across rows and streams, for small maps; 10 tap by tap with
- * the reduction split over a cluster of CTAs, for few tiles).  For inspection and tests.  Errors: DC_ERR_ARG. */
+ * the reduction split over a cluster of CTAs, for few tiles), 11 the 8-bit tensor-core product (DC_CONV_QUANT).  For inspection and tests.  Errors: DC_ERR_ARG. */
 int dc_cache_layer_conv_scheme(const dc_cache* cache, int layer, int32_t* scheme);
 
 /* Waits for the stream and returns the device status word: DC_OK, or what a kernel recorded since the

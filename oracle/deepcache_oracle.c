@@ -40,7 +40,7 @@ typedef struct {
 } orc_layer;
 
 enum { ORC_CONV = 0, ORC_MAXPOOL = 1, ORC_RELU = 2, ORC_ADD = 3, ORC_CONCAT = 4,
-       ORC_RESIZE_AREA = 5, ORC_LRN = 6, ORC_FC = 7 };
+       ORC_RESIZE_AREA = 5, ORC_LRN = 6, ORC_FC = 7, ORC_LAYER_NORM = 8, ORC_CONV_QUANT = 9 };
 
 #define ORC_INVALID UINT64_MAX
 
@@ -434,6 +434,9 @@ void orc_propagate_layer(const orc_layer* L, int in_h, int in_w,
         case ORC_FC:                       /* Table 2: (0, 0, 0, 0) */
             out[i] = EMPTY_REGION;
             break;
+        case ORC_CONV_QUANT:               /* over the whole map: fully connected; else pointwise: unchanged */
+            if (L->kh == in_h && L->kw == in_w && L->out_h == 1 && L->out_w == 1) { out[i] = EMPTY_REGION; break; }
+            /* fall through */
         default:                           /* Table 2, "Others": unchanged */
             out[i] = (in0[i].w > 0 && in0[i].h > 0) ? in0[i] : EMPTY_REGION;
             break;

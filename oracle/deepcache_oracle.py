@@ -24,7 +24,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _SRC = os.path.join(_HERE, "deepcache_oracle.c")
 _LIB = os.path.join(_HERE, "libdeepcache_oracle.so")
 
-KIND_CONV, KIND_MAXPOOL, KIND_RELU, KIND_ADD, KIND_CONCAT, KIND_RESIZE_AREA, KIND_LRN, KIND_FC = range(8)
+KIND_CONV, KIND_MAXPOOL, KIND_RELU, KIND_ADD, KIND_CONCAT, KIND_RESIZE_AREA, KIND_LRN, KIND_FC, KIND_LAYER_NORM, KIND_CONV_QUANT = range(10)
 SEARCH_ES, SEARCH_DS, SEARCH_TSS = 0, 1, 2
 QUANT_NONE, QUANT_BF16 = 0, 1
 
@@ -339,6 +339,38 @@ def fully_connected(x, layer, weight, bias, mode):
     return out
 
 
+def layer_norm(x, gamma, beta, eps, mode):
+    """Layer normalisation over the channels of each pixel of a stored map; gamma, beta may be None (ones, zeros)."""
+    x = np.asarray(x, np.float64)
+    d = x - x.mean(axis=-1, keepdims=True)
+    y = d / np.sqrt((d * d).mean(axis=-1, keepdims=True) + eps)
+    y = y * (1.0 if gamma is None else np.asarray(gamma, np.float64)) + (0.0 if beta is None else np.asarray(beta, np.float64))
+    return quant_array(y, mode)
+
+
+def quantise_rows(x):
+    """Rows in 127 steps of their largest value either way: (integers, scales).  Halves go to the even integer; a row of zeros has the
+    scale 0; the scale is stored in float32.  127 x is exact and the quotient is rounded once, so a half is seen as one."""
+    x = np.asarray(x, np.float64)
+    most = np.abs(x).max(axis=-1, keepdims=True)
+    q = np.rint(127.0 * x / np.where(most > 0, most, 1.0))
+    return q, (most[..., 0] / 127.0).astype(np.float32).astype(np.float64)
+
+
+def conv_quant(x, layer, weight, bias, mode, prev_out=None, regions=None):
+    """A convolution in 8-bit integers: pointwise with a scale per pixel, or over the whole map with one for the map, and a scale per output
+    channel; weight is the float32 one.  Reuse as for any convolution, the rest computed.  Returns (out, reused byte map)."""
+    x = np.asarray(x, np.float64)
+    cout = int(layer["cout"])
+    rows = x.reshape(1, 1, -1) if (layer["kh"], layer["kw"]) == x.shape[:2] and (layer["out_h"], layer["out_w"]) == (1, 1) else x
+    q, s = quantise_rows(rows)
+    wq, ws = quantise_rows(np.asarray(weight, np.float32).reshape(cout, -1))
+    y = np.einsum("hwk,ck->hwc", q, wq) * s[..., None] * ws + np.asarray(bias, np.float64)
+    if layer["relu"]:
+        y = np.maximum(y, 0.0)
+    return _copy_rectangles(quant_array(y, mode), prev_out, regions)
+
+
 def add(a, b, relu, mode):
     """Residual add (a multi-input layer of Table 2): element-wise sum, optional ReLU, storage rounding."""
     a = np.ascontiguousarray(a, np.float64)
@@ -370,15 +402,18 @@ class OracleCache:
 
     def __init__(self, width, height, layers, weights, biases, *, block=10, search_range=8,
                  search_kind=SEARCH_DS, psnr_db=20.0, expire_n=10, quant=QUANT_NONE, use_cache=True, skip_k=1,
-                 region_mode=0, cache_pool=False, lrn=(1e-4, 0.75, 1.0)):
+                 region_mode=0, cache_pool=False, lrn=(1e-4, 0.75, 1.0), norm_eps=1e-5):
         self.W, self.H = width, height
         self.layers = layers
         self.block, self.R, self.kind = block, search_range, search_kind
         self.T, self.N, self.quant, self.use_cache = psnr_db, expire_n, quant, use_cache
         self.skip_k, self.region_mode, self.cache_pool = skip_k, region_mode, cache_pool
         self.lrn = lrn                 # (alpha, beta, k) of every LRN layer
+        self.norm_eps = norm_eps       # of every layer normalisation
         # weights are stored at the storage precision (bf16 workloads round them once)
-        self.weights = [None if w is None else quant_array(w, quant) for w in weights]
+        # (layer normalisation keeps its own in float32, 8-bit convolutions take theirs from float32)
+        self.weights = [None if w is None else np.asarray(w, np.float32) if l["kind"] in (KIND_LAYER_NORM, KIND_CONV_QUANT) else quant_array(w, quant)
+                        for w, l in zip(weights, layers)]
         self.biases = [None if b is None else np.asarray(b, np.float64) for b in biases]
         self.reset()
 
@@ -436,6 +471,13 @@ class OracleCache:
                     out = lrn(x, l, *self.lrn, self.quant)
             elif k == KIND_CONCAT:
                 out = concat(x, maps[l["in1"]])
+            elif k == KIND_LAYER_NORM:
+                out = layer_norm(x, self.weights[i], self.biases[i], self.norm_eps, self.quant)
+            elif k == KIND_CONV_QUANT:
+                out, reused = conv_quant(x, l, self.weights[i], self.biases[i], self.quant, None if refresh else self.prev_maps[i],
+                                         None if refresh else per_layer_regions[i])
+                if (l["kh"], l["kw"]) != x.shape[:2]:
+                    info["reused"][i] = reused
             elif k == KIND_FC:
                 out = fully_connected(x, l, self.weights[i], self.biases[i], self.quant)
             else:
@@ -443,7 +485,7 @@ class OracleCache:
             maps.append(out)
         # the frame becomes the next key, the conv outputs the next values (Section 3)
         self.prev_frame = frame.copy()
-        kept = (KIND_CONV, KIND_MAXPOOL, KIND_LRN) if self.cache_pool else (KIND_CONV,)
+        kept = (KIND_CONV, KIND_CONV_QUANT, KIND_MAXPOOL, KIND_LRN) if self.cache_pool else (KIND_CONV, KIND_CONV_QUANT)
         self.prev_maps = [m if layers[i]["kind"] in kept else None for i, m in enumerate(maps)]
         self.frame_idx += 1
         info["maps"] = maps

@@ -16,7 +16,7 @@ DC_MAX_LAYERS = 128
 DC_OK = 0
 DC_ERR_ARG, DC_ERR_CONFIG, DC_ERR_ALLOC, DC_ERR_CUDA, DC_ERR_OVERFLOW, DC_ERR_TIMEOUT, DC_ERR_STATE, DC_ERR_LIMIT = range(-1, -9, -1)
 DC_NOALLOC_MAX_STREAMS = 64
-DC_CONV, DC_MAXPOOL, DC_RELU, DC_ADD, DC_CONCAT, DC_RESIZE_AREA, DC_LRN, DC_FC = range(8)
+DC_CONV, DC_MAXPOOL, DC_RELU, DC_ADD, DC_CONCAT, DC_RESIZE_AREA, DC_LRN, DC_FC, DC_LAYER_NORM, DC_CONV_QUANT = range(10)
 DC_SEARCH_EXHAUSTIVE, DC_SEARCH_DIAMOND, DC_SEARCH_THREE_STEP = 0, 1, 2
 DC_REGIONS_GLOBAL, DC_REGIONS_PER_BLOCK = 0, 1
 DC_FP32, DC_BF16 = 0, 1
@@ -49,7 +49,7 @@ class dc_frame_stats(C.Structure):
 
 REGION_DTYPE = np.dtype([(n, "<i4") for n in ("x", "y", "w", "h", "sx", "sy")])
 
-EXPORTS = ["dc_cache_create", "dc_cache_destroy", "dc_cache_reset", "dc_cache_bytes", "dc_cache_set_key",
+EXPORTS = ["dc_cache_create", "dc_cache_destroy", "dc_cache_reset", "dc_cache_set_norm_epsilon", "dc_cache_bytes", "dc_cache_set_key",
            "dc_match_blocks", "dc_propagate_regions", "dc_conv_partial", "dc_infer_frame", "dc_infer_frame_host",
            "dc_prefetch_frame_host", "dc_lookahead_frame",
            "dc_cache_layer_map", "dc_cache_layer_regions", "dc_cache_layer_conv_scheme", "dc_get_status", "dc_cache_launches",
@@ -79,6 +79,7 @@ def load():
         L.dc_cache_create.argtypes = [C.POINTER(dc_config), C.POINTER(dc_layer_desc), i, C.POINTER(vp), C.POINTER(vp), vp, C.POINTER(vp)]
         L.dc_cache_destroy.argtypes = [vp]
         L.dc_cache_reset.argtypes = [vp]
+        L.dc_cache_set_norm_epsilon.argtypes = [vp, i, C.c_double]
         L.dc_cache_bytes.argtypes = [vp, C.POINTER(sz)]
         L.dc_cache_set_key.argtypes = [vp, vp, sz]
         L.dc_match_blocks.argtypes = [vp, vp, sz, vp, vp, vp, vp, vp, vp]
@@ -164,6 +165,11 @@ def dc_cache_destroy(cache):
 
 def dc_cache_reset(cache):
     _check(load().dc_cache_reset(cache), "dc_cache_reset")
+
+
+def dc_cache_set_norm_epsilon(cache, layer: int, eps: float):
+    """The epsilon of a layer normalisation layer; empties the cache."""
+    _check(load().dc_cache_set_norm_epsilon(cache, layer, eps), "dc_cache_set_norm_epsilon")
 
 
 def dc_cache_bytes(cache) -> int:

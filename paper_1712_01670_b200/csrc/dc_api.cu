@@ -34,6 +34,7 @@ bool dc_layer_cached(const dc_cache* c, int layer)
 {
     const dc_layer_desc& d = c->L[layer].d;
     if (d.kind == DC_CONV) return true;
+    if (d.kind == DC_CONV_QUANT) return !dc_quant_whole(d, c->L[layer].in_h, c->L[layer].in_w);
     return (d.kind == DC_MAXPOOL || d.kind == DC_LRN) && c->cfg.cache_pool && ((size_t)d.cout * c->elt) % 16 == 0;
 }
 
@@ -101,7 +102,7 @@ int second_lists(dc_cache* c)
 bool layer_executable(const dc_layer_desc& L, int in_h, int in_w)
 {
     switch (L.kind) {
-    case DC_CONV: case DC_MAXPOOL: case DC_RELU: case DC_ADD: case DC_RESIZE_AREA: case DC_CONCAT: return true;
+    case DC_CONV: case DC_MAXPOOL: case DC_RELU: case DC_ADD: case DC_RESIZE_AREA: case DC_CONCAT: case DC_LAYER_NORM: case DC_CONV_QUANT: return true;
     case DC_LRN: return L.kh == 2 * L.ph + 1 && L.kw == L.kh && L.pw == L.ph;
     case DC_FC: return L.kh == in_h && L.kw == in_w && L.out_h == 1 && L.out_w == 1;
     default: return false;
@@ -122,7 +123,7 @@ int validate(const dc_config* cfg, const dc_layer_desc* layers, int n)
     const int elt = cfg->dtype == DC_BF16 ? 2 : 4;
     for (int i = 0; i < n; ++i) {
         const dc_layer_desc& L = layers[i];
-        if (L.kind < DC_CONV || L.kind > DC_FC) return DC_ERR_CONFIG;
+        if (L.kind < DC_CONV || L.kind > DC_CONV_QUANT) return DC_ERR_CONFIG;
         if (L.in0 < -1 || L.in0 >= i) return DC_ERR_CONFIG;
         int ih = L.in0 < 0 ? cfg->height : layers[L.in0].out_h;
         int iw = L.in0 < 0 ? cfg->width : layers[L.in0].out_w;
@@ -159,6 +160,15 @@ int validate(const dc_config* cfg, const dc_layer_desc* layers, int n)
             if (L.cin != ic) return DC_ERR_CONFIG;
             if (layer_executable(L, ih, iw) && (L.cout * elt) % 16 != 0) return DC_ERR_CONFIG;
             break;
+        case DC_CONV_QUANT: {
+            const bool pointwise = L.kh == 1 && L.kw == 1 && L.sh == 1 && L.sw == 1 && L.ph == 0 && L.pw == 0 && L.out_h == ih && L.out_w == iw;
+            if (L.cin != ic || (!pointwise && !dc_quant_whole(L, ih, iw)) || (L.cout * elt) % 16 != 0) return DC_ERR_CONFIG;
+            if ((long long)L.kh * L.kw * L.cin > 131071) return DC_ERR_CONFIG;
+            break;
+        }
+        case DC_LAYER_NORM:
+            if (ic > 16384) return DC_ERR_CONFIG;
+            [[fallthrough]];
         case DC_RELU:
             if (L.out_h != ih || L.out_w != iw || L.cout != ic) return DC_ERR_CONFIG;
             break;
@@ -228,7 +238,7 @@ int build(dc_cache* c, const dc_layer_desc* layers, const void* const* weights_d
     for (int i = 0; i < n; ++i) {
         dc_layer_rt& L = c->L[i];
         L.d = layers[i];
-        L.fuse_add = -1;
+        L.fuse_add = -1; L.norm_feeds = -1; L.norm_from = -1;
         // an executable fully-connected layer runs as the convolution that covers its input map; the device copy of the
         // layer table keeps DC_FC, so Table 2 still marks nothing of its output reusable and every tile is computed
         if (L.d.kind == DC_FC && c->executable) { L.d.kind = DC_CONV; L.d.sh = L.d.sw = 1; L.d.ph = L.d.pw = 0; }
@@ -240,6 +250,7 @@ int build(dc_cache* c, const dc_layer_desc* layers, const void* const* weights_d
         if ((L.d.kind == DC_ADD || L.d.kind == DC_CONCAT) && L.d.in1 < 0) need_input_map = true;
         L.map_bytes = (size_t)S * L.d.out_h * L.d.out_w * L.d.cout * c->elt;
         const bool cached = dc_layer_cached(c, i);
+        L.flat = L.d.kind == DC_CONV_QUANT && cached;                 // its rows in 8 bits lie as flat tiles count pixels
         const int copies = cached ? 2 : 1;
         for (int k = 0; k < copies; ++k) {
             DC_TRY(dev_alloc(c, (uint8_t**)&L.map[k], L.map_bytes));
@@ -269,6 +280,12 @@ int build(dc_cache* c, const dc_layer_desc* layers, const void* const* weights_d
             if (!weights_dev || !bias_dev || !weights_dev[i] || !bias_dev[i]) return DC_ERR_ARG;
             DC_TRY(dc_pack_weights(c, i, (const float*)weights_dev[i], (const float*)bias_dev[i]));
         }
+        if (L.d.kind == DC_CONV_QUANT) {
+            if (!weights_dev || !bias_dev || !weights_dev[i] || !bias_dev[i]) return DC_ERR_ARG;
+            DC_TRY(dc_build_quant(c, i, (const float*)weights_dev[i], (const float*)bias_dev[i]));
+        }
+        if (L.d.kind == DC_LAYER_NORM)
+            DC_TRY(dc_build_norm(c, i, weights_dev ? (const float*)weights_dev[i] : nullptr, bias_dev ? (const float*)bias_dev[i] : nullptr));
     }
     DC_CUDA(cudaMemcpyAsync(c->all_count, all_count, sizeof(int32_t) * 2 * n, cudaMemcpyHostToDevice, c->stream));
     DC_TRY(dev_alloc(c, &c->zero_masks, max_tiles * 4));
@@ -291,6 +308,13 @@ int build(dc_cache* c, const dc_layer_desc* layers, const void* const* weights_d
         if (d.kind != DC_ADD || d.in0 < 0 || d.in1 < 0 || d.in0 == d.in1) continue;
         dc_layer_rt& P = c->L[d.in0 > d.in1 ? d.in0 : d.in1];
         if (P.d.kind == DC_CONV && P.fuse_add < 0 && dc_conv_takes_add(c, d.in0 > d.in1 ? d.in0 : d.in1)) P.fuse_add = j;
+    }
+    // a layer norm writes the rows in 8 bits of the first pointwise 8-bit convolution that reads it
+    for (int j = 0; j < n && c->executable; ++j) {
+        const dc_layer_desc& d = c->L[j].d;
+        if (d.kind != DC_CONV_QUANT || !dc_layer_cached(c, j) || d.in0 < 0) continue;
+        dc_layer_rt& P = c->L[d.in0];
+        if (P.d.kind == DC_LAYER_NORM && P.norm_feeds < 0) { P.norm_feeds = j; c->L[j].norm_from = d.in0; }
     }
     // who reads the frame as a map, and who reads the resized frame
     c->fused_input = need_input_map; c->resize_feeds = -1;
@@ -334,6 +358,7 @@ void release(dc_cache* c)
     for (int i = 0; i < c->n_layers; ++i) {
         dc_layer_rt& L = c->L[i];
         cudaFree(L.map[0]); cudaFree(L.map[1]); cudaFree(L.weight); cudaFree(L.bias); cudaFree(L.weight_packed); cudaFree(L.weight_simt); cudaFree(L.weight_f32); cudaFree(L.in_padded); cudaFree(L.in_s2d); cudaFree(L.weight_halo);
+        cudaFree(L.w_scale); cudaFree(L.q_rows); cudaFree(L.q_scale);
         cudaFree(L.masks); cudaFree(L.dirty_list); cudaFree(L.all_list);
     }
     cudaGetLastError();
@@ -438,6 +463,13 @@ int dc_cache_reset(dc_cache* c)
     return DC_OK;
 }
 
+int dc_cache_set_norm_epsilon(dc_cache* c, int layer, double eps)
+{
+    if (!c || layer < 0 || layer >= c->n_layers || c->L[layer].d.kind != DC_LAYER_NORM || !(eps >= 0.0) || !(eps < 1e30)) return DC_ERR_ARG;
+    c->L[layer].eps = (float)eps;
+    return dc_cache_reset(c);
+}
+
 int dc_cache_bytes(const dc_cache* c, size_t* bytes)
 {
     if (!c || !bytes) return DC_ERR_ARG;
@@ -512,20 +544,24 @@ int dc_conv_partial(dc_cache* c, int layer, const void* in_map_dev, const void* 
                     const dc_region* regions_dev, const int32_t* n_regions_dev, void* out_map_dev)
 {
     if (!c || !in_map_dev || !out_map_dev || layer < 0 || layer >= c->n_layers) return DC_ERR_ARG;
-    if (!c->executable || c->L[layer].d.kind != DC_CONV) return DC_ERR_CONFIG;
+    if (!c->executable || (c->L[layer].d.kind != DC_CONV && c->L[layer].d.kind != DC_CONV_QUANT)) return DC_ERR_CONFIG;
     dc_layer_rt& L = c->L[layer];
+    const bool quant = L.d.kind == DC_CONV_QUANT, whole = quant && !dc_layer_cached(c, layer);
     const int tiles = dc_layer_tiles(c, L);
     const uintptr_t in_at = (uintptr_t)in_map_dev, out_at = (uintptr_t)out_map_dev;
     if (in_at % c->elt || out_at % c->elt) return DC_ERR_ARG;
     // the tensor-core kernels store vectors, and their loads take the map from a 16-byte boundary (copies of few-channel maps: from any)
-    if (dc_conv_bf16_supported(c, layer) && !dc_conv_any_element(c, layer, in_map_dev, out_map_dev) && (out_at % 16 || (in_at % 16 && L.d.cin % 16 == 0 && !L.s2d_s))) return DC_ERR_ARG;
+    if (!quant && dc_conv_bf16_supported(c, layer) && !dc_conv_any_element(c, layer, in_map_dev, out_map_dev) && (out_at % 16 || (in_at % 16 && L.d.cin % 16 == 0 && !L.s2d_s))) return DC_ERR_ARG;
     if (regions_dev || n_regions_dev) {
         if (!regions_dev || !n_regions_dev || !prev_out_dev || prev_out_dev == out_map_dev) return DC_ERR_ARG;
         if ((uintptr_t)prev_out_dev % 16 || out_at % 16) return DC_ERR_ARG;      // the reuse copy is a bulk copy
+        if (whole) return dc_launch_quant(c, layer, in_map_dev, false, out_map_dev, nullptr, nullptr, nullptr);     // Table 2: nothing is reusable
         DC_TRY(dc_launch_classify_copy(c, layer, regions_dev, n_regions_dev, prev_out_dev, out_map_dev, c->partial + 2, c->partial + 3,
                                        (unsigned long long*)c->partial));
+        if (quant) return dc_launch_quant(c, layer, in_map_dev, false, out_map_dev, L.dirty_list, c->partial + 2, L.masks);
         return dc_launch_conv(c, layer, in_map_dev, out_map_dev, L.dirty_list, c->partial + 2, L.masks, tiles);
     }
+    if (quant) return dc_launch_quant(c, layer, in_map_dev, false, out_map_dev, nullptr, nullptr, nullptr);
     return dc_launch_conv(c, layer, in_map_dev, out_map_dev, L.all_list, dc_all_count(c, layer), c->zero_masks, tiles);
 }
 
@@ -620,6 +656,20 @@ static int infer_frame(dc_cache* c, const uint8_t* frame_dev, size_t pitch, void
             break;
         }
         case DC_RELU: DC_TRY(dc_launch_relu(c, i, in)); break;
+        case DC_LAYER_NORM: DC_TRY(dc_launch_norm(c, i, in, L.map[0])); break;
+        case DC_CONV_QUANT: {
+            const bool filled = L.norm_from >= 0;
+            if (!dc_layer_cached(c, i)) { DC_TRY(dc_launch_quant(c, i, in, false, L.map[0], nullptr, nullptr, nullptr)); break; }
+            void* prev = L.map[L.cur]; void* out = L.map[L.cur ^ 1];
+            if (!refresh) {
+                if (!classified) DC_TRY(dc_launch_classify_copy(c, i, c->live + per_layer * i, c->alive + (size_t)i * S, prev, out, c->dirty_count + i, c->reuse_px + (size_t)i * S, nullptr));
+                DC_TRY(dc_launch_quant(c, i, in, filled, out, L.dirty_list, c->dirty_count + i, L.masks));
+            } else {
+                DC_TRY(dc_launch_quant(c, i, in, filled, out, nullptr, nullptr, nullptr));
+            }
+            L.cur ^= 1;
+            break;
+        }
         case DC_LRN: {
             if (!dc_layer_cached(c, i)) { DC_TRY(dc_launch_lrn(c, i, in, L.map[0], nullptr)); break; }
             void* prev = L.map[L.cur]; void* out = L.map[L.cur ^ 1];
@@ -800,6 +850,7 @@ int dc_cache_layer_conv_scheme(const dc_cache* c, int layer, int32_t* scheme)
 {
     if (!c || layer < 0 || layer >= c->n_layers || !scheme) return DC_ERR_ARG;
     const dc_layer_rt& L = c->L[layer];
+    if (L.d.kind == DC_CONV_QUANT && c->executable) { *scheme = 11; return DC_OK; }
     if (L.d.kind != DC_CONV || !c->executable) { *scheme = -1; return DC_OK; }
     if (!dc_conv_bf16_supported(c, layer)) { *scheme = 0; return DC_OK; }
     *scheme = L.tc_cs > 0 ? 10 : (L.tc_mt > 0 ? L.tc_mt : 1) + (L.flat ? 7 : 0);

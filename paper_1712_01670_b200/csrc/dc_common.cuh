@@ -71,6 +71,11 @@ struct dc_layer_rt {
     int32_t* all_list;              // conv: every tile (used by full frames)
     dc_tm_slot tm_a[4], tm_b;       // conv, bf16: tensor maps of the input (two bases, two channel groups) and of the weights
     int tm_next;                    // which of tm_a[] a new input base replaces
+    float eps;                      // layer norm: its epsilon; gamma in `weight`, beta in `bias` (NULL: ones, zeros)
+    int norm_feeds;                 // layer norm: the pointwise 8-bit convolution whose rows its kernel writes too, or -1
+    float* w_scale;                 // 8-bit convolution: a scale per output channel; its weights in `weight`, rows of dc_quant_pitch bytes
+    int8_t* q_rows; float* q_scale; // 8-bit convolution: its input in 8 bits; pointwise: lines of gpr * 8 pixels, as flat tiles count them
+    int norm_from;                  // 8-bit convolution: the layer norm that has filled them, or -1
 };
 
 // Everything one run of the matcher writes, and what the reuse step needs of region propagation.  Two sets exist so that both may already
@@ -254,8 +259,15 @@ int dc_launch_lrn(dc_cache* c, int layer, const void* in, void* out, const uint3
 int dc_launch_concat(dc_cache* c, int layer, const void* a, int ca, const void* b, int cb);
 int dc_launch_add(dc_cache* c, int layer, const void* a, const void* b, void* also);
 int dc_launch_relu(dc_cache* c, int layer, const void* a);
+// layer normalisation and 8-bit convolutions (dc_quant_layer.cu)
+int dc_build_norm(dc_cache* c, int layer, const float* gamma_dev, const float* beta_dev);
+int dc_build_quant(dc_cache* c, int layer, const float* w_dev, const float* b_dev);
+int dc_launch_norm(dc_cache* c, int layer, const void* in, void* out);
+int dc_launch_quant(dc_cache* c, int layer, const void* in, bool filled, void* out, const int32_t* tile_list, const int32_t* tile_count, const uint32_t* masks);
+// a DC_CONV_QUANT layer whose kernel covers its whole input map
+static inline bool dc_quant_whole(const dc_layer_desc& d, int in_h, int in_w) { return d.kh == in_h && d.kw == in_w && d.out_h == 1 && d.out_w == 1; }
 int dc_pack_weights(dc_cache* c, int layer, const float* w_dev, const float* b_dev);
-// true for layers that keep their last output as cached values: convolutions, and max pooling / LRN when cfg.cache_pool
+// true for layers that keep their last output as cached values: convolutions (8-bit ones where they are pointwise), and max pooling / LRN when cfg.cache_pool
 bool dc_layer_cached(const dc_cache* c, int layer);
 int dc_build_classify_table(dc_cache* c, dc_match_set& m);
 int dc_launch_classify_all(dc_cache* c, int cur);

@@ -234,6 +234,15 @@ __device__ __forceinline__ int64_t q_row(const dc_rows_args& a, int64_t row)
     return line * a.padded + (row - line * a.width);
 }
 
+// Is the row wanted?  (Reused pixels' are not.)
+__device__ __forceinline__ bool wanted(const dc_rows_args& a, int64_t row)
+{
+    if (row >= a.rows) return false;
+    if (!a.masks) return true;
+    const int64_t q = q_row(a, row);
+    return !((a.masks[q >> 5] >> (q & 31)) & 1u);
+}
+
 // Rows in registers: NV vectors of VE elements per lane.  A row belongs to `group` lanes of a warp, which takes 32 / group rows at once, or
 // (BLOCK, its most threads) to the CTA.  Lanes beyond the row's end hold zeros (FULL: there are none).  The next rows' loads are in flight while
 // a row is worked on, but for CTAs of 1024 threads, whose registers have no room for them.
@@ -263,23 +272,26 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256) k_rows(const dc_rows_args
     dc_pdl_wait();
     dc_pdl_release();
     typename V::Raw next[NV];
+    bool next_live;
     auto fetch = [&](int64_t row) {
         const T* const x = (const T*)((const char*)a.x + (size_t)row * a.x_pitch);
+        const bool live = QUANT && !NORM ? wanted(a, row) : row < a.rows;
+        next_live = live;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
-            next[v] = row < a.rows && (FULL || i < nvec) ? *(const typename V::Raw*)(x + i * VE) : raw_zero<typename V::Raw>();
+            next[v] = live && (FULL || i < nvec) ? *(const typename V::Raw*)(x + i * VE) : raw_zero<typename V::Raw>();
         }
     };
     int64_t row = BLOCK ? first : first + lane / group;
     if (AHEAD) fetch(row);
     int parity = 0;
     for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
-        const bool on = row < a.rows;
         float* const slot = red + (BLOCK ? parity * 96 : 0);
         F d[NV * P];
         uint32_t m = 0;
         if (!AHEAD) fetch(row);
+        const bool on = next_live;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             V::open(next[v], d + v * P);
@@ -350,6 +362,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
     int parity = 0;
     const float c = (float)a.channels, inv_c = 1.f / c;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, parity ^= 1) {
+        if (QUANT && !NORM && !wanted(a, row)) continue;
         float* const slot = red + parity * 96;
         const T* const x = (const T*)((const char*)a.x + (size_t)row * a.x_pitch);
         T* const y = (T*)((char*)a.y + (size_t)row * a.y_pitch);

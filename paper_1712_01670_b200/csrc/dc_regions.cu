@@ -45,7 +45,7 @@ __device__ __forceinline__ dc_region empty_region() { dc_region e = {0, 0, 0, 0,
 
 // A layer as propagation sees it, the fields of the horizontal axis and of the vertical one side by side.
 // axis[]: {c1, c2, sh, simple}.  The rule of a sliding window whose strides are powers of two (convolutions, pooling; LRN is one at stride 1,
-// ReLU one of a single pixel) is, on either axis, first = (x + c1) >> sh, last = (x + w + c2) >> sh.  simple: such a window on the layer
+// ReLU, layer norm and pointwise 8-bit convolutions ones of a single pixel) is, on either axis, first = (x + c1) >> sh, last = (x + w + c2) >> sh.  simple: such a window on the layer
 // before.
 // links: {in0, in1, kind, until}; kind: kWindow or the layer's; until: the last layer that reads this one's rectangle, kept (later than the
 // next one), and at least the last layer that reads the frame's.
@@ -712,7 +712,8 @@ int dc_build_propagate_table(dc_cache* c, const dc_layer_desc* layers)
         };
         if (d.kind == DC_CONV || d.kind == DC_MAXPOOL) window(d.kh, d.kw, d.sh, d.sw, d.ph, d.pw);
         else if (d.kind == DC_LRN) window(2 * d.ph + 1, 2 * d.ph + 1, 1, 1, d.ph, d.ph);
-        else if (d.kind == DC_RELU) window(1, 1, 1, 1, 0, 0);
+        else if (d.kind == DC_CONV_QUANT && dc_quant_whole(d, ih, iw)) e.links.z = DC_FC;      // nothing is reusable
+        else if (d.kind == DC_RELU || d.kind == DC_LAYER_NORM || d.kind == DC_CONV_QUANT) window(1, 1, 1, 1, 0, 0);
     }
     if (cudaMalloc(&c->prop_table, sizeof(PropLayer) * n) != cudaSuccess) { cudaGetLastError(); return DC_ERR_ALLOC; }
     c->bytes += sizeof(PropLayer) * n;

@@ -14,6 +14,7 @@ struct dc_rows_args {
     int8_t* q; size_t q_pitch; float* scale;   // or NULL
     // Pixels of maps of `width` columns, of which each image row begins at a multiple of `padded` rows of q and scale; 0: dense
     int width, padded;
+    const uint32_t* masks;              // of such pixels, those that are not wanted: a bit for each row of q, 128 to a tile; or NULL
 };
 // norm: false: the rows are quantised as they are.  *launches counts the kernels.
 int dc_launch_rows(const dc_rows_args& a, bool norm, int dtype, int num_sms, cudaStream_t stream);
@@ -27,7 +28,8 @@ struct dc_product_args {
     void* out; size_t out_pitch;
     int32_t* status;                    // device status word, or NULL
     int early;                          // 1: the weights (b, b_scale, bias) are older than the kernel before, which waits for its own predecessor
-    // A partial convolution's pixels (NULL, 0: every row): tiles of 128 rows of a, in images of `padded` rows per line of `width` pixels
+    // Pixels of maps (padded > 0; else every row): tiles of 128 rows of a, `padded` rows per line of `width` pixels; tile_list, masks: of a
+    // partial convolution, or NULL
     const int32_t *tile_list, *tile_count; const uint32_t* masks;
     int width, padded, max_tiles;
 };

@@ -88,6 +88,9 @@ class DeepCache:
     def reset(self):
         B.dc_cache_reset(self.handle)
 
+    def set_norm_epsilon(self, layer, eps):
+        B.dc_cache_set_norm_epsilon(self.handle, layer, eps)
+
     def set_key(self, frame):
         f, pitch = self._frame(frame)
         B.dc_cache_set_key(self.handle, f, pitch)

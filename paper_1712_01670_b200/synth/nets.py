@@ -13,7 +13,7 @@ from __future__ import annotations
 import numpy as np
 
 # Layer kind codes: an interface shared with the C header and the oracle.
-KIND_CONV, KIND_MAXPOOL, KIND_RELU, KIND_ADD, KIND_CONCAT, KIND_RESIZE_AREA, KIND_LRN, KIND_FC = range(8)
+KIND_CONV, KIND_MAXPOOL, KIND_RELU, KIND_ADD, KIND_CONCAT, KIND_RESIZE_AREA, KIND_LRN, KIND_FC, KIND_LAYER_NORM, KIND_CONV_QUANT = range(10)
 
 
 def _layer(kind, in0, out_h, out_w, cin, cout, k=1, s=1, p=0, relu=0, in1=-1, groups=1):
@@ -74,6 +74,21 @@ class NetBuilder:
         self.layers.append(l)
         return len(self.layers) - 1
 
+    def layer_norm(self, src: int) -> int:
+        """Layer normalisation over each pixel's channels (weights: gamma, beta)."""
+        h, w, c = self.shape(src)
+        self.layers.append(_layer(KIND_LAYER_NORM, src, h, w, c, c))
+        return len(self.layers) - 1
+
+    def conv_quant(self, src: int, cout: int, relu: int = 1, whole: bool = False) -> int:
+        """A 1 x 1 convolution in 8-bit integers, or (``whole``) a fully connected layer in 8-bit integers."""
+        h, w, c = self.shape(src)
+        l = _layer(KIND_CONV_QUANT, src, 1 if whole else h, 1 if whole else w, c, cout, relu=relu)
+        if whole:
+            l["kh"], l["kw"] = h, w
+        self.layers.append(l)
+        return len(self.layers) - 1
+
     def resize_area(self, src: int, oh: int, ow: int) -> int:
         h, w, c = self.shape(src)
         self.layers.append(_layer(KIND_RESIZE_AREA, src, oh, ow, c, c))
@@ -114,6 +129,25 @@ def inception_lrn_net(h=64, w=64):
     x = b.lrn(x, 2)
     x = b.maxpool(x, 4, 4)
     b.fc(x, 48)
+    return b.layers
+
+
+def norm_quant_net(h=64, w=64, width=32, blocks=2):
+    """Blocks of the kind that put layer normalisation in the place of local response normalisation: a convolution per channel, a
+    normalisation over the channels, a fourfold widening and a narrowing in 8-bit integers, and the block's input added; then a fully
+    connected head in 8-bit integers."""
+    b = NetBuilder(h, w)
+    x = b.conv(-1, width, 3, 1, 1)
+    for _ in range(blocks):
+        y = b.conv(x, width, 3, 1, 1, relu=0, groups=width)
+        y = b.layer_norm(y)
+        y = b.conv_quant(y, 4 * width)
+        y = b.conv_quant(y, width, relu=0)
+        x = b.add(y, x, relu=0)
+    x = b.maxpool(x, 2, 2)
+    x = b.layer_norm(x)
+    x = b.maxpool(x, 4, 4)
+    b.conv_quant(x, 48, relu=0, whole=True)
     return b.layers
 
 
@@ -164,7 +198,8 @@ def vgg16_trunk(h=224, w=224, src_h=None, src_w=None):
 
 
 def random_weights(layers, seed: int, *, std: float | None = None, bias_std: float = 0.05):
-    """He-normal (or fixed-``std``) weights for every conv and fully-connected layer; ``None`` elsewhere.
+    """He-normal (or fixed-``std``) weights for every conv and fully-connected layer, gamma and beta for layer
+    normalisation; ``None`` elsewhere.
 
     The last conv of a residual branch (a conv feeding an add with relu=0) is
     scaled by 0.5 so activations stay tame through deep residual stacks.
@@ -176,7 +211,11 @@ def random_weights(layers, seed: int, *, std: float | None = None, bias_std: flo
             feeds_add.add(l["in0"])
     weights, biases = [], []
     for i, l in enumerate(layers):
-        if l["kind"] not in (KIND_CONV, KIND_FC):
+        if l["kind"] == KIND_LAYER_NORM:                           # gamma, beta
+            weights.append((1.0 + rng.normal(0.0, 0.2, size=l["cout"])).astype(np.float32))
+            biases.append(rng.normal(0.0, 0.1, size=l["cout"]).astype(np.float32))
+            continue
+        if l["kind"] not in (KIND_CONV, KIND_FC, KIND_CONV_QUANT):
             weights.append(None)
             biases.append(None)
             continue
