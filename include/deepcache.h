@@ -343,7 +343,7 @@ int dc_layer_norm(const void* x_dev, size_t x_pitch, const float* gamma_dev, con
  *   mean_dev, rstd_dev    float32 [rows], as dc_layer_norm gave them
  *   dx_dev                the map's type, or NULL; may be dy_dev or x_dev with the same pitch
  *   dgamma_dev, dbeta_dev float32 [channels], or NULL; overwritten (zeros for zero rows)
- *   workspace_dev         dc_layer_norm_workspace bytes (4-byte aligned; not needed, and may be NULL, where both are NULL);
+ *   workspace_dev         dc_layer_norm_workspace bytes (16-byte aligned; not needed, and may be NULL, where both are NULL);
  *                         its content does not matter before or after the call; two calls that may overlap need one each
  * The sums of dgamma and dbeta are made in one order whatever the timing: equal calls give equal bits. */
 int dc_layer_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_dev, size_t x_pitch, const float* gamma_dev,
