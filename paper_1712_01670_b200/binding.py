@@ -278,81 +278,30 @@ def dc_search_blocks_noalloc(frame, prev, pitch, width, height, n_streams, block
 # --------------------------------------------------------------------------
 # layer normalisation and 8-bit rows: maps as torch tensors [..., channels]
 # --------------------------------------------------------------------------
-_DTYPES = {torch.float32: DC_FP32, torch.bfloat16: DC_BF16}
-_SIZES = {torch.float32: 4, torch.bfloat16: 2}
-_INT8 = {torch.int8: 1}
-# torch's current stream and device, asked for without an object or a context check: a short call costs about what its arguments do
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_native = None
 
 
-def _rows(t, what, sizes=_SIZES):
-    """(address, pitch in bytes, rows, channels) of a map whose rows lie a constant stride apart."""
-    size = sizes.get(t.dtype)
-    if size is None:
-        raise TypeError(f"{what}: unsupported type {t.dtype}")
-    shape, stride = t.shape, t.stride()
-    if len(shape) == 2:
-        rows, c = shape
-        if stride[1] == 1 or c < 2:
-            return t.data_ptr(), (stride[0] if rows > 1 else c) * size, rows, c
-    if len(shape) < 1 or (shape[-1] > 1 and stride[-1] != 1):
-        raise ValueError(f"{what}: a row's elements have to lie side by side")
-    c, rows, pitch = shape[-1], 1, None
-    for n, s in zip(reversed(shape[:-1]), reversed(stride[:-1])):
-        if n == 0:
-            return t.data_ptr(), c * size, 0, c
-        if n > 1:
-            if pitch is None:
-                pitch = s
-            elif s != pitch * rows:
-                raise ValueError(f"{what}: rows do not lie a constant stride apart")
-            rows *= n
-    return t.data_ptr(), (c if pitch is None else pitch) * size, rows, c
+def _tensors():
+    """The compiled marshalling of tensors (csrc/dc_torch.cpp)."""
+    global _native
+    if _native is None:
+        load()
+        try:
+            from . import _tensors as module
+        except ImportError as e:
+            raise ImportError(f"{e}: build it with `python -m paper_1712_01670_b200.build`") from e
+        _native = module
+    return _native
 
 
-def _vector(t, n, what):
-    """Address of a float32 vector of n values, or None."""
-    if t is None:
-        return None
-    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous float32 vector of {n} values is needed")
-    return t.data_ptr()
-
-
-def _on_device(where, stream, tensors, *args):
-    """One call of the library on the device that the tensors are on; stream: a cudaStream_t, or None for torch's current one there."""
-    dev = tensors[0].get_device()
-    if dev < 0:
-        raise ValueError(f"{where}: all tensors have to be on one CUDA device")
-    for t in tensors:
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"{where}: all tensors have to be on one CUDA device")
-    if stream is None:
-        stream = _raw_stream(dev)
-    fn = getattr(_lib or load(), where)
-    if dev == _raw_device():
-        rc = fn(*args, stream)
-    else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, stream)
-    if rc != DC_OK:
-        raise DeepCacheError(rc, where)
-
-
-def _same_rows(a, b, what):
-    if a[3] != b[3] or a[2] != b[2]:
-        raise ValueError(f"{what}: {b[2]} rows of {b[3]} where {a[2]} of {a[3]} are needed")
-
-
+# Below: x, y, dy, dx, out are maps [..., channels] of one type (float32, bfloat16) whose rows lie a constant stride apart, q, a, b, w 8-bit rows (int8,
+# a multiple of 16 bytes apart), everything else float32 vectors; None where it says so.  All on one CUDA device; stream: a cudaStream_t, or None for
+# torch's current one there.
 def dc_layer_norm(x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, stream=None):
-    """y = layer normalisation of x's rows; gamma, beta (or None), mean, rstd (or None): float32."""
-    xr, yr = _rows(x, "x"), _rows(y, "y")
-    _same_rows(xr, yr, "y")
-    if x.dtype != y.dtype:
-        raise TypeError("x and y differ in type")
-    _on_device("dc_layer_norm", stream, (x, y, gamma, beta, mean, rstd), xr[0], xr[1], _vector(gamma, xr[3], "gamma"), _vector(beta, xr[3], "beta"),
-               xr[2], xr[3], eps, _DTYPES[x.dtype], yr[0], yr[1], _vector(mean, xr[2], "mean"), _vector(rstd, xr[2], "rstd"))
+    """y = layer normalisation of x's rows; gamma, beta, mean, rstd may be None."""
+    rc = (_native or _tensors()).layer_norm(x, gamma, beta, y, mean, rstd, eps, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_layer_norm")
 
 
 def dc_layer_norm_workspace(channels: int) -> int:
@@ -361,67 +310,32 @@ def dc_layer_norm_workspace(channels: int) -> int:
     return v.value
 
 
-def _scratch(t, what):
-    if t is None:
-        return None, 0
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: has to be contiguous")
-    return t.data_ptr(), t.nbytes
-
-
 def dc_layer_norm_backward(dy, x, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, workspace=None, stream=None):
     """Gradients of dc_layer_norm; workspace: any tensor of dc_layer_norm_workspace(channels) bytes (for dgamma, dbeta)."""
-    xr, dr = _rows(x, "x"), _rows(dy, "dy")
-    _same_rows(xr, dr, "dy")
-    ox = (None, 0)
-    if dx is not None:
-        ox = _rows(dx, "dx")
-        _same_rows(xr, ox, "dx")
-    if x.dtype != dy.dtype or (dx is not None and dx.dtype != x.dtype):
-        raise TypeError("x, dy and dx differ in type")
-    if mean is None or rstd is None:
-        raise ValueError("mean and rstd are needed")
-    wp, wn = _scratch(workspace, "workspace")
-    _on_device("dc_layer_norm_backward", stream, (x, dy, gamma, mean, rstd, dx, dgamma, dbeta, workspace), dr[0], dr[1], xr[0], xr[1], _vector(gamma, xr[3], "gamma"),
-               _vector(mean, xr[2], "mean"), _vector(rstd, xr[2], "rstd"), xr[2], xr[3], _DTYPES[x.dtype], ox[0], ox[1], _vector(dgamma, xr[3], "dgamma"),
-               _vector(dbeta, xr[3], "dbeta"), wp, wn)
+    rc = (_native or _tensors()).layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_layer_norm_backward")
 
 
 def dc_quantize_rows(x, q, scale, stream=None):
-    """x's rows in 8 bits: q int8 (rows 16 bytes or a multiple apart), scale float32 [rows]."""
-    xr, qr = _rows(x, "x"), _rows(q, "q", _INT8)
-    _same_rows(xr, qr, "q")
-    _on_device("dc_quantize_rows", stream, (x, q, scale), xr[0], xr[1], xr[2], xr[3], _DTYPES[x.dtype], qr[0], _pitch8(qr), _vector(scale, xr[2], "scale"))
-
-
-def _pitch8(r):
-    """The pitch of 8-bit rows; a single row's is whatever the row needs."""
-    return r[1] if r[2] > 1 else -(-r[3] // 16) * 16
+    """x's rows in 8 bits: q, and a scale for each row."""
+    rc = (_native or _tensors()).quantize_rows(x, q, scale, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_quantize_rows")
 
 
 def dc_layer_norm_quantize(x, gamma, beta, q, scale, y=None, eps=1e-5, stream=None):
     """Layer normalisation straight into 8-bit rows (and y, if given)."""
-    xr, qr = _rows(x, "x"), _rows(q, "q", _INT8)
-    _same_rows(xr, qr, "q")
-    yr = (None, 0)
-    if y is not None:
-        yr = _rows(y, "y")
-        _same_rows(xr, yr, "y")
-        if y.dtype != x.dtype:
-            raise TypeError("x and y differ in type")
-    _on_device("dc_layer_norm_quantize", stream, (x, q, scale, gamma, beta, y), xr[0], xr[1], _vector(gamma, xr[3], "gamma"), _vector(beta, xr[3], "beta"), xr[2], xr[3], eps,
-               _DTYPES[x.dtype], yr[0], yr[1], qr[0], _pitch8(qr), _vector(scale, xr[2], "scale"))
+    rc = (_native or _tensors()).layer_norm_quantize(x, gamma, beta, q, scale, y, eps, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_layer_norm_quantize")
 
 
 def dc_matmul_quantized(a, a_scale, b, b_scale, bias, out, relu=False, stream=None):
-    """out = relu((a * a_scale) @ (b * b_scale).T + bias) for int8 rows a [m, k] and b [n, k]."""
-    ar, br, o = _rows(a, "a", _INT8), _rows(b, "b", _INT8), _rows(out, "out")
-    if br[3] != ar[3] or o[2] != ar[2] or o[3] != br[2]:
-        raise ValueError(f"a {tuple(a.shape)}, b {tuple(b.shape)} and out {tuple(out.shape)} do not fit together")
-    if a_scale is None or b_scale is None:
-        raise ValueError("both scales are needed")
-    _on_device("dc_matmul_quantized", stream, (a, b, a_scale, b_scale, bias, out), ar[0], _pitch8(ar), _vector(a_scale, ar[2], "a_scale"), br[0], _pitch8(br),
-               _vector(b_scale, br[2], "b_scale"), _vector(bias, br[2], "bias"), ar[2], br[2], ar[3], int(relu), _DTYPES[out.dtype], o[0], o[1])
+    """out = relu((a * a_scale) @ (b * b_scale).T + bias) for 8-bit rows a [m, k] and b [n, k]; bias may be None."""
+    rc = (_native or _tensors()).matmul_quantized(a, a_scale, b, b_scale, bias, out, relu, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_matmul_quantized")
 
 
 def dc_linear_workspace(rows: int, k: int) -> int:
@@ -432,13 +346,6 @@ def dc_linear_workspace(rows: int, k: int) -> int:
 
 def dc_linear_quantized(x, w, w_scale, bias, out, relu=False, workspace=None, stream=None):
     """out = relu(x @ (w * w_scale).T + bias) with x's rows put into 8 bits; workspace: any tensor of dc_linear_workspace(rows, k) bytes."""
-    xr, wr, o = _rows(x, "x"), _rows(w, "w", _INT8), _rows(out, "out")
-    if wr[3] != xr[3] or o[2] != xr[2] or o[3] != wr[2]:
-        raise ValueError(f"x {tuple(x.shape)}, w {tuple(w.shape)} and out {tuple(out.shape)} do not fit together")
-    if x.dtype != out.dtype:
-        raise TypeError("x and out differ in type")
-    if w_scale is None:
-        raise ValueError("w_scale is needed")
-    wp, wn = _scratch(workspace, "workspace")
-    _on_device("dc_linear_quantized", stream, (x, w, w_scale, bias, out, workspace), xr[0], xr[1], wr[0], _pitch8(wr), _vector(w_scale, wr[2], "w_scale"),
-               _vector(bias, wr[2], "bias"), xr[2], wr[2], xr[3], int(relu), _DTYPES[x.dtype], o[0], o[1], wp, wn)
+    rc = (_native or _tensors()).linear_quantized(x, w, w_scale, bias, out, relu, workspace, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_linear_quantized")

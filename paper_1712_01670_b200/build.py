@@ -1,4 +1,4 @@
-"""Builds ``libdeepcache.so`` in-tree with nvcc for sm_100a."""
+"""Builds ``libdeepcache.so`` in-tree with nvcc for sm_100a, and ``_tensors.so``, its binding to torch tensors, with the C++ compiler."""
 from __future__ import annotations
 
 import glob
@@ -9,6 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB = os.path.join(_HERE, "libdeepcache.so")
+TENSORS = os.path.join(_HERE, "_tensors.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
@@ -26,7 +27,33 @@ def stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def tensors_command():
+    """How ``_tensors.so`` is made: torch's own headers and libraries, libdeepcache found beside it."""
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    includes = [sysconfig.get_paths()["include"], INCLUDE, *cpp_extension.include_paths(), os.path.join(cuda, "include")]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+            *(f for i in includes for f in ("-isystem" if "torch" in i else "-I", i)), os.path.join(CSRC, "dc_torch.cpp"), "-o", TENSORS,
+            "-L", libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L", _HERE, "-ldeepcache", "-Wl,-rpath,$ORIGIN"]
+
+
+def build_tensors(force: bool = False) -> str:
+    deps = [os.path.join(CSRC, "dc_torch.cpp"), os.path.join(INCLUDE, "deepcache.h")]
+    if force or not os.path.exists(TENSORS) or any(os.path.getmtime(d) > os.path.getmtime(TENSORS) for d in deps):
+        subprocess.check_call(tensors_command())
+    return TENSORS
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_library(force, verbose)
+    build_tensors(force)
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

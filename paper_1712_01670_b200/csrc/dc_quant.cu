@@ -137,16 +137,6 @@ __device__ __forceinline__ void column_weights(const dc_product_args& p, int col
     }
 }
 
-// Eight bfloat16 of a row of out from column `col` on; n: the row's length.
-__device__ __forceinline__ void store_unit(char* row, int col, int n, uint4 v, int wide)
-{
-    if (wide && col + 8 <= n) { *(uint4*)(row + (size_t)col * 2) = v; return; }
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-        if (col + k < n) ((uint16_t*)row)[col + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
-}
-
 // The place of row r of a tile-ordered map in the map itself, or -1: beyond the map, in the gap behind a line of pixels, or reused.
 __device__ __forceinline__ int64_t out_row(const dc_product_args& p, int tile, int r)
 {
@@ -284,6 +274,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
 #pragma unroll
             for (int k = 0; k < 4; ++k) s[k] = r + 8 * k < p.m ? p.a_scale[r + 8 * k] : 0.f;
         };
+        auto stage_bf16 = [&](const uint32_t (&v)[2][16], const float* sa, const float2* s, const float2* b) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = two_bf16<RELU>(finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]));
+                stmatrix4(stage + to_stage + k * 512, w[0], w[1], w[2], w[3]);
+            }
+        };
+        auto stage_f32 = [&](const uint32_t (&v)[2][16], const float* sa, const float2* s, const float2* b, int h) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 2 * h; j < 2 * h + 2; ++j) {
+                    const float2 f = finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]);
+                    const int r = 8 * k + (lane >> 2), u = 2 * (j & 1) + ((lane >> 1) & 1);
+                    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4) + 8 * (lane & 1)), "f"(clamped<RELU>(f.x)),
+                                 "f"(clamped<RELU>(f.y)) : "memory");
+                }
+        };
         float next[4];
         if (first < n_items) row_scales(tile_of(first / a.NB, &there), next);
         for (int item = first; item < n_items; item += step) {
@@ -320,84 +330,56 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
                 column_weights(p, n0 + c0 + 2 * (lane & 3), pairs && c0 + 32 <= n_here, s, b);
                 tmem_ld_wait();
                 if (c0 + 4 * 32 >= n_here) hand_back();
-                const bool fast = !LIST && a.wide && rows == 32 && c0 + 32 <= n_here;
                 if (sizeof(T) == 4 && a.boxes) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {             // 16 columns at a time
                         if (lane == 0) store_read(a.bufs);
                         __syncwarp();
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-#pragma unroll
-                            for (int j = 2 * h; j < 2 * h + 2; ++j) {
-                                const float2 f = finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]);
-                                const int r = 8 * k + (lane >> 2), u = 2 * (j & 1) + ((lane >> 1) & 1);
-                                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4) + 8 * (lane & 1)), "f"(clamped<RELU>(f.x)),
-                                             "f"(clamped<RELU>(f.y)) : "memory");
-                            }
+                        stage_f32(v, sa, s, b, h);
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                         if (lane == 0 && rows > 0) store_box(&tmC, stage, n0 + c0 + 16 * h, (int)row0);
                         stage ^= both;
                     }
-                } else if constexpr (sizeof(T) == 4) {
-                    const int col = n0 + c0 + 2 * (lane & 3);
+                } else if (sizeof(T) == 2 && a.boxes) {
+                    if (lane == 0) store_read(a.bufs);        // the box before has left its place
+                    __syncwarp();
+                    stage_bf16(v, sa, s, b);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && rows > 0) store_box(&tmC, stage, n0 + c0, (int)row0);
+                    stage ^= both;
+                } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {             // rows lane / 4 + 8 k
-                        const int r = 8 * k + (lane >> 2);
-                        const int64_t to = LIST ? __shfl_sync(0xffffffffu, mine, r) : r < rows ? row0 + r : -1;
-                        float* const out = (float*)((char*)p.out + (size_t)to * p.out_pitch) + col;
+                    for (int h = 0; h < (sizeof(T) == 4 ? 2 : 1); ++h) {
+                        if constexpr (sizeof(T) == 2) stage_bf16(v, sa, s, b); else stage_f32(v, sa, s, b, h);
+                        __syncwarp();
+                        const int c1 = n0 + c0 + 16 * h;
+                        if (a.wide && c1 + 64 / (int)sizeof(T) <= p.n) {      // four lanes to 64 bytes
+                            const int u = lane & 3;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float2 f = finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]);
-                            f = make_float2(clamped<RELU>(f.x), clamped<RELU>(f.y));
-                            if (fast) *(float2*)(out + 8 * j) = f;
-                            else if (to >= 0) {
-                                if (a.wide && col + 8 * j + 1 < p.n) *(float2*)(out + 8 * j) = f;
-                                else {
-                                    if (col + 8 * j < p.n) out[8 * j] = f.x;
-                                    if (col + 8 * j + 1 < p.n) out[8 * j + 1] = f.y;
+                            for (int it = 0; it < 4; ++it) {
+                                const int r = it * 8 + (lane >> 2);
+                                const int64_t to = LIST ? __shfl_sync(0xffffffffu, mine, r) : r < rows ? row0 + r : -1;
+                                if (to >= 0) *(uint4*)((char*)p.out + (size_t)to * p.out_pitch + (size_t)c1 * sizeof(T) + u * 16) = lds128(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
+                            }
+                        } else {                              // an element per lane, side by side
+                            constexpr int PER = sizeof(T) == 4 ? 2 : 1;       // rows at once
+                            const int e = lane & (32 / PER - 1), u = e * (int)sizeof(T) >> 4;
+#pragma unroll 4
+                            for (int it = 0; it < 32 / PER; ++it) {
+                                const int r = it * PER + (PER == 2 ? lane >> 4 : 0);
+                                const int64_t to = LIST ? __shfl_sync(0xffffffffu, mine, r) : r < rows ? row0 + r : -1;
+                                const uint32_t at = stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4) + (e * (int)sizeof(T) & 15);
+                                if (to >= 0 && c1 + e < p.n) {
+                                    T* const out = (T*)((char*)p.out + (size_t)to * p.out_pitch) + c1 + e;
+                                    if constexpr (sizeof(T) == 4) { uint32_t w; asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory"); *(uint32_t*)out = w; }
+                                    else { uint16_t w; asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w) : "r"(at) : "memory"); *(uint16_t*)out = w; }
                                 }
                             }
                         }
-                    }
-                } else {
-                    if (a.boxes) {                            // the box before has left its place
-                        if (lane == 0) store_read(a.bufs);
                         __syncwarp();
                     }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            w[j] = two_bf16<RELU>(finish2(v[k >> 1][4 * j + 2 * (k & 1)], v[k >> 1][4 * j + 2 * (k & 1) + 1], sa[k], s[j], b[j]));
-                        stmatrix4(stage + to_stage + k * 512, w[0], w[1], w[2], w[3]);
-                    }
-                    if (a.boxes) {
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        __syncwarp();
-                        if (lane == 0 && rows > 0) store_box(&tmC, stage, n0 + c0, (int)row0);
-                        stage ^= both;
-                        continue;
-                    }
-                    __syncwarp();
-                    const int u = lane & 3, col = n0 + c0 + u * 8;
-                    char* const out = (char*)p.out + (size_t)(row0 + (lane >> 2)) * p.out_pitch;   // not LIST
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) {
-                        const int r = it * 8 + (lane >> 2);
-                        const uint4 w = lds128(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
-                        if (LIST) {
-                            const int64_t to = __shfl_sync(0xffffffffu, mine, r);
-                            if (to >= 0) store_unit((char*)p.out + (size_t)to * p.out_pitch, col, p.n, w, a.wide);
-                        } else if (fast) {
-                            *(uint4*)(out + (size_t)(it * 8) * p.out_pitch + (size_t)col * 2) = w;
-                        } else if (r < rows) {
-                            store_unit(out + (size_t)(it * 8) * p.out_pitch, col, p.n, w, a.wide);
-                        }
-                    }
-                    __syncwarp();
                 }
             }
             if (held) hand_back();                            // a warp whose columns do not exist
@@ -445,7 +427,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
     int32_t* const status = p.status ? p.status : &g_status;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank(), item = blockIdx.x / a.CS, mt = item % a.m_tiles, nt = item / a.m_tiles;
-    const int k0 = rank * a.kchunks / a.CS, nk = (rank + 1) * a.kchunks / a.CS - k0;
+    const int nk = (a.kchunks - rank + a.CS - 1) / a.CS;         // chunk it * CS + rank: a cluster reads whole stretches of a row at once
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 2); mbar_init(&ctl->empty[i], 1); }   // weights and rows arrive apart
@@ -469,7 +451,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
     const int ahead = nk < a.stages ? nk : a.stages;
     auto load_weights = [&](int it, uint32_t off, uint32_t slot) {
         mbar_expect_tx(full0 + off, (uint32_t)kATile);
-        tma_load_2d(slot, &tmW, (k0 + it) * kBytesK, nt * kTileM, full0 + off);
+        tma_load_2d(slot, &tmW, (it * a.CS + rank) * kBytesK, nt * kTileM, full0 + off);
     };
     if (!a.early) { dc_pdl_wait(); dc_pdl_release(); }
     if (warp == 0 && elect_one())
@@ -491,7 +473,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
                     load_weights(it, r.off, r.data);
                 }
                 mbar_expect_tx(full0 + r.off, (uint32_t)(a.NT * kBytesK));
-                tma_load_2d(r.data + kATile, &tmX, (k0 + it) * kBytesK, mt * a.NT, full0 + r.off);
+                tma_load_2d(r.data + kATile, &tmX, (it * a.CS + rank) * kBytesK, mt * a.NT, full0 + r.off);
                 r.next(ring0, (uint32_t)a.stages, (uint32_t)a.stage_bytes);
             }
             if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
@@ -507,7 +489,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
             for (int it = 0; it < nk; ++it) {
                 if (!mbar_wait_at(full0 + r.off, r.phase, &ctl->abort_flag, &ctl->wait_ns, status)) break;
                 tc_fence_after();
-                umma_i8(tmem_base, r.data, r.data + (kATile >> 4), d_hi, a.idesc, it != 0, k0 + it + 1 < a.kchunks ? 4 : a.k_last);
+                umma_i8(tmem_base, r.data, r.data + (kATile >> 4), d_hi, a.idesc, it != 0, it * a.CS + rank + 1 < a.kchunks ? 4 : a.k_last);
                 if (it + a.stages < nk) umma_commit_at(empty0 + r.off);
                 if (it + 1 == nk) umma_commit(&ctl->done);
                 r.next(r0, (uint32_t)a.stages, slot);
