@@ -402,7 +402,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
 // makes enough CTAs for the weights to stream at HBM's rate.  Each CTA takes its part of K; the int32 sums meet in distributed shared memory, where CTA r
 // finishes channels r * 128 / CS and on; they are exact, so the split changes no bit.  `early`: everything older than the kernel before is
 // complete (dc_linear_quantized: that kernel puts x into 8 bits), so the weights' loads start before the wait for it.
-// One row, 9216 -> 4096: 29 us with k_product's 64 CTAs that walk K alone.
+// With the rows put into 8 bits, us, in turns with k_product's 64 CTAs that walk K alone: 1 x 9216 x 4096 11.3 and 27.7, 32 x 25088 x 4096 23.1
+// and 45.9, 100 x 4096 x 1000 7.6 and 11.3; 196 x 1024 x 512 7.2 and 6.1.
 constexpr int kSplitThreads = 192, kSplitStages = 12;
 struct SplitArgs {
     dc_product_args p;
@@ -411,6 +412,7 @@ struct SplitArgs {
 };
 struct SplitCtl {
     unsigned long long full[kSplitStages], empty[kSplitStages], done;
+    alignas(16) float scale[128];
     uint32_t tmem_base;
     volatile int abort_flag;
     unsigned long long wait_ns;
@@ -421,8 +423,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    int32_t* red = (int32_t*)(ring + (size_t)a.stages * a.stage_bytes);      // [CS][NT][128 / CS]: this CTA's channels, from every CTA
-    SplitCtl* ctl = (SplitCtl*)(red + 128 * a.NT);
+    // [CS][NT / 4][128 / CS]: this CTA's channels, four rows' sums each, from every CTA; a warp's stores lie side by side
+    int4* red = (int4*)(ring + (size_t)a.stages * a.stage_bytes);
+    SplitCtl* ctl = (SplitCtl*)(red + 32 * a.NT);
     const dc_product_args& p = a.p;
     int32_t* const status = p.status ? p.status : &g_status;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -460,6 +463,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
     if (a.early) { dc_pdl_wait(); dc_pdl_release(); }
 
     bool waited = false;                                                     // for the cluster
+    // the channel that this thread finishes: the threads are a multiple of a CTA's channels
+    const int rows = 128 / a.CS, ch = threadIdx.x % rows, j = nt * kTileM + rank * rows + ch;
+    const float sb = j < p.n ? __ldg(p.b_scale + j) : 0.f, bias = j < p.n && p.bias ? __ldg(p.bias + j) : 0.f;
     if (warp == 0) {
         // ---------------- producer ----------------
         if (elect_one()) {
@@ -498,8 +504,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
         __syncwarp();
     } else {
         // ---------------- partial sums to the CTA that finishes the channel ----------------
-        const int q = warp & 3, m = q * 32 + lane, rows = 128 / a.CS, owner = m / rows;
-        const uint32_t dst = map_to_cta(red + (size_t)rank * a.NT * rows + (m - owner * rows), (uint32_t)owner);
+        const int q = warp & 3, m = q * 32 + lane, owner = m / rows;
+        if (m < a.NT) ctl->scale[m] = (int64_t)mt * a.NT + m < p.m ? p.a_scale[(int64_t)mt * a.NT + m] : 0.f;
+        const uint32_t dst = map_to_cta(red + rank * (a.NT / 4) * rows + m - owner * rows, (uint32_t)owner);
         bool ok = mbar_wait_at(smem_u32(&ctl->done), 0, &ctl->abort_flag, &ctl->wait_ns, status);
         ok = __all_sync(0xffffffffu, ok);
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -515,8 +522,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
                              : "r"(tmem_base + ((uint32_t)(q * 32) << 16) + c) : "memory");
                 tmem_ld_wait();
 #pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (c + k < there) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(dst + (uint32_t)((c + k) * rows * 4)), "r"(v[k]) : "memory");
+                for (int k = 0; k < 16; k += 4)
+                    if (c + k < there)
+                        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((c + k) / 4 * rows * 16)), "r"(v[k]), "r"(v[k + 1]), "r"(v[k + 2]), "r"(v[k + 3]) : "memory");
             }
         }
         tc_fence_before();
@@ -529,20 +537,25 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
     cluster_sync_all();                      // this CTA's channels have arrived from every CTA
     {
         // ---------------- this CTA's channels: sums from all ranks, scales, bias, ReLU, rounding, store ----------------
-        const int rows = 128 / a.CS, there = (int)min((int64_t)a.NT, p.m - (int64_t)mt * a.NT);
+        const int there = (int)min((int64_t)a.NT, p.m - (int64_t)mt * a.NT);
         const bool dead = ctl->abort_flag != 0;                              // what is stored says so
-        for (int u = threadIdx.x; u < rows * there; u += kSplitThreads) {
-            const int t = u / rows, ch = u - t * rows, j = nt * kTileM + rank * rows + ch;
-            if (j >= p.n) continue;
-            int32_t sum = 0;
-            for (int r = 0; r < a.CS; ++r) sum += red[((size_t)r * a.NT + t) * rows + ch];
-            const int64_t row = (int64_t)mt * a.NT + t;
-            const float sa = dead ? __uint_as_float(0x7fffffffu) : p.a_scale[row];
-            float f = fmaf((float)sum * sa, __ldg(p.b_scale + j), p.bias ? __ldg(p.bias + j) : 0.f);
-            if (p.relu) f = clamped<true>(f);
-            T* const out = (T*)((char*)p.out + (size_t)row * p.out_pitch) + j;
-            if constexpr (sizeof(T) == 4) *out = f;
-            else *out = __float2bfloat16_rn(f);
+        for (int t = threadIdx.x / rows * 4; t < there && j < p.n; t += kSplitThreads / rows * 4) {    // four rows of x
+            int4 sum = make_int4(0, 0, 0, 0);
+            for (int r = 0; r < a.CS; ++r) {
+                const int4 v = red[(r * (a.NT / 4) + t / 4) * rows + ch];
+                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+            }
+            const int32_t sums[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (t + k >= there) break;
+                const int64_t row = (int64_t)mt * a.NT + t + k;
+                float f = fmaf((float)sums[k] * (dead ? __uint_as_float(0x7fffffffu) : ctl->scale[t + k]), sb, bias);
+                if (p.relu) f = clamped<true>(f);
+                T* const out = (T*)((char*)p.out + (size_t)row * p.out_pitch) + j;
+                if constexpr (sizeof(T) == 4) *out = f;
+                else *out = __float2bfloat16_rn(f);
+            }
         }
     }
     if (warp == 1) {
@@ -605,18 +618,42 @@ int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtenso
     return DC_OK;
 }
 
+// Clusters of so many CTAs, each with an SM of its own, that the device holds at once.
+int clusters_at_once(int cs, int device)
+{
+    static int known[64][4];
+    const int at = cs == 1 ? 0 : cs == 2 ? 1 : cs == 4 ? 2 : 3;
+    if (device >= 0 && device < 64 && known[device][at]) return known[device][at];
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)cs); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = 200 * 1024; cfg.attrs = attr; cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(k_product_split<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k_product_split<float>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+    if (n < 1) n = 1;
+    if (device >= 0 && device < 64) known[device][at] = n;
+    return n;
+}
+
 // How a product of few tiles is split, and the cycles that it takes (as dc_launch_product counts them).
 struct SplitPlan { int NT, CS; double cost; };
-SplitPlan split_plan(const dc_product_args& p, int kc, int num_sms)
+SplitPlan split_plan(const dc_product_args& p, int kc, int device)
 {
-    SplitPlan s;
-    s.NT = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
-    const long long tiles = (p.m + s.NT - 1) / s.NT * (long long)dc_div_up(p.n, kTileM);
-    s.CS = 1;
-    while (s.CS < 8 && 2 * s.CS <= kc && tiles * 2 * s.CS <= num_sms) s.CS *= 2;
-    const long long rounds = (tiles * s.CS + num_sms - 1) / num_sms;
-    s.cost = rounds * (dc_div_up(kc, s.CS) * (double)(kATile + s.NT * kBytesK) / 50.0 + 8.0 * s.NT + 1500.0);
-    return s;
+    SplitPlan best = {};
+    const int NT = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
+    const long long tiles = (p.m + NT - 1) / NT * (long long)dc_div_up(p.n, kTileM);
+    for (int cs = 2; cs <= 8 && cs <= kc; cs *= 2) {
+        const int at_once = clusters_at_once(cs, device);
+        const long long rounds = (tiles + at_once - 1) / at_once;
+        // HBM's 3400 bytes a cycle shared by the CTAs; to send the sums, join and store them
+        const double load = (kATile + NT * kBytesK) / 50.0, hbm = kATile * (double)(tiles * cs < at_once * cs ? tiles * cs : at_once * cs) / 3400.0;
+        const double join = 2500.0 + NT * (cs == 8 ? 30.0 : cs == 4 ? 40.0 : 50.0);
+        const double cost = rounds * (dc_div_up(kc, cs) * (load > hbm ? load : hbm) + join);
+        if (rounds <= 2 && (best.CS == 0 || cost < best.cost)) best = {NT, cs, cost};
+    }
+    return best;
 }
 
 template <typename T>
@@ -671,7 +708,7 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
         if (c == 0 || cost < best) { best = cost; pair = two; a.BN = bn; }
     }
     if (!p.padded && p.n <= (1 << 20) && p.m <= (1 << 20)) {
-        const SplitPlan s = split_plan(p, kc, num_sms);
+        const SplitPlan s = split_plan(p, kc, device);
         if (s.CS > 1 && s.cost < best) return dtype == DC_BF16 ? launch_split<__nv_bfloat16>(p, s, kc, device, stream) : launch_split<float>(p, s, kc, device, stream);
     }
     a.NB = dc_div_up(p.n, a.BN);
