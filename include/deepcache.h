@@ -333,7 +333,8 @@ int dc_search_blocks_noalloc(const uint8_t* frame_dev, const uint8_t* prev_dev, 
  *   mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps), y = (x - mean) rstd gamma + beta
  *   gamma_dev, beta_dev   float32 [channels] or NULL (ones, zeros)
  *   mean_dev, rstd_dev    float32 [rows] or NULL: for dc_layer_norm_backward
- * y_dev may be x_dev with the same pitch.  eps >= 0.  A row with a NaN or an infinity becomes NaN, no other row changes.
+ * y_dev may be x_dev with the same pitch.  eps >= 0.  A row with a NaN or an infinity becomes NaN, no other row changes; sums and squares
+ * are float32, so rows of values beyond 1e18 or so have no meaningful result.
  * DC_ERR_LIMIT: more than 16384 channels. */
 int dc_layer_norm(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t rows, int32_t channels,
                   double eps, int32_t dtype, void* y_dev, size_t y_pitch, float* mean_dev, float* rstd_dev, void* cuda_stream);
@@ -367,7 +368,8 @@ int dc_layer_norm_quantize(const void* x_dev, size_t x_pitch, const float* gamma
 /* out[r][j] = relu(a_scale[r] b_scale[j] sum over k of a[r][k] b[j][k] + bias[j]): the product of two matrices of 8-bit rows.
  *   a_dev int8 [m][a_pitch], b_dev int8 [n][b_pitch] (weights: one row per output channel): 16-byte aligned, pitches multiples of 16;
  *   nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
- * The sums are exact (int32); scales, bias and ReLU are applied in float32, with one rounding to dtype.
+ * The sums are exact (int32); scales, bias and ReLU (which leaves a NaN) are applied in float32, with one rounding to dtype.  Every wait inside the
+ * kernels is bounded; should one run out (2 s), the results that it concerns are NaN.
  * DC_ERR_LIMIT: k > 131071 (a sum could pass 32 bits), m > 2^31 - 256, n > 2^28. */
 int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const int8_t* b_dev, size_t b_pitch,
                         const float* b_scale_dev, const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,

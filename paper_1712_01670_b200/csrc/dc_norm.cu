@@ -256,7 +256,7 @@ __device__ __forceinline__ bool wanted(const dc_rows_args& a, int64_t row)
 // (BLOCK, its most threads) to the CTA.  Lanes beyond the row's end hold zeros (FULL: there are none).  The next rows' loads are in flight while
 // a row is worked on, but for CTAs of 1024 threads, whose registers have no room for them.
 template <typename T, int VE, int NV, int BLOCK, bool NORM, bool QUANT, bool FULL>
-__global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : NORM && VE == 8 && NV <= 2 ? 3 : 2) k_rows(const dc_rows_args a, int group)
+__global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV <= 8 ? 3 : 2) : NORM && VE == 8 && NV <= 2 ? 3 : 2) k_rows(const dc_rows_args a, int group)
 {
     typedef Vec<T, VE> V;
     typedef typename V::F F;
@@ -623,9 +623,14 @@ cudaError_t launch_rows(const dc_rows_args& a, int num_sms, cudaStream_t stream)
         case 3: DC_ROWS(3, 0, s.group, per_cta * 32, ctas);
         case 4: DC_ROWS(4, 0, s.group, per_cta * 32, ctas);
         case 5: case 6: case 7: case 8: DC_ROWS(8, 0, s.group, per_cta * 32, ctas);
-        default: if constexpr (VE == 1) DC_ROWS(16, 0, s.group, per_cta * 32, ctas);
+        default:
+            if constexpr (VE == 1) {
+                if (s.nv <= 12) DC_ROWS(12, 0, s.group, per_cta * 32, ctas);
+                DC_ROWS(16, 0, s.group, per_cta * 32, ctas);
+            }
         }
     }
+    if constexpr (VE == 1) if (nvec <= 512 * 12) DC_ROWS(12, 512, 32, dc_div_up(dc_div_up(nvec, 12), 32) * 32, a.rows);
     // a CTA per row: as many threads as leave each four vectors, up to 1024
     const int want = dc_div_up(dc_div_up(nvec, 4), 32) * 32, threads = want < 128 ? 128 : want > 1024 ? 1024 : want;
     if (threads <= 512) DC_ROWS(4, 512, 32, threads, a.rows);
@@ -668,6 +673,7 @@ cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t
             if (full && s.nv == N8) return launch_backward_as<T, VE, N8, false, 320, 2, true>(a, s.group, num_sms, stream, ctas);
             return launch_backward_as<T, VE, N8, false, 320, 2, false>(a, s.group, num_sms, stream, ctas);
         }
+        if constexpr (VE == 1) if (s.nv <= 12) return launch_backward_as<T, VE, 12, false, 256, 2, false>(a, s.group, num_sms, stream, ctas);
         if (full && s.nv == N16) return launch_backward_as<T, VE, N16, false, T16, C16, true>(a, s.group, num_sms, stream, ctas);
         return launch_backward_as<T, VE, N16, false, T16, C16, false>(a, s.group, num_sms, stream, ctas);
     }

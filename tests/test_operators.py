@@ -602,6 +602,77 @@ def test_two_calls_at_once_on_two_streams():
 
 
 @gpu
+@pytest.mark.parametrize("m,k,n", [(1, 4096, 512), (20, 9216, 256), (300, 512, 300)])
+def test_weights_written_just_before_the_product(m, k, n):
+    """A product may start loading weights before the rows of x are ready, but not before what was enqueued in front of the call is done."""
+    x = make_map(m, k, torch.bfloat16, 1)
+    work, out = scratch(B.dc_linear_workspace(m, k)), torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    ws = [torch.randn(n, k, generator=gen(i), device="cuda") for i in range(4)]
+    big = torch.randn(64 << 20, device="cuda")
+    wq, sc = q_like(n, k), torch.empty(n, device="cuda")
+    want, got = [], []
+    for w in ws:
+        B.dc_quantize_rows(w, wq, sc)
+        torch.cuda.synchronize()
+        B.dc_linear_quantized(x, wq, sc, None, out, False, work)
+        torch.cuda.synchronize()
+        want.append(out.clone())
+    kept = [(q_like(n, k), torch.empty(n, device="cuda")) for _ in ws]
+    for w, (q, s) in zip(ws, kept):
+        B.dc_quantize_rows(w, q, s)
+    for _ in range(5):
+        for i, w in enumerate(ws):
+            big.mul_(1.0)                                               # something long in front
+            if i % 2:
+                B.dc_quantize_rows(w, wq, sc)
+            else:
+                wq.copy_(kept[i][0]), sc.copy_(kept[i][1])
+            o = torch.empty_like(out)
+            B.dc_linear_quantized(x, wq, sc, None, o, False, work)
+            got.append((i, o))
+    assert all(torch.equal(o, want[i]) for i, o in got)
+
+
+FIRST_CALL_IN_A_CAPTURE = """
+import torch
+from paper_1712_01670_b200 import binding as B
+x = torch.randn(40, 4096, device="cuda").bfloat16()
+w, s, out = torch.randint(-127, 128, (512, 4096), device="cuda").to(torch.int8), torch.rand(512, device="cuda"), torch.empty(40, 512, device="cuda").bfloat16()
+big, o2 = torch.randn(20000, 96, device="cuda"), torch.empty(20000, 64, device="cuda")
+w2 = torch.randint(-127, 128, (64, 96), device="cuda").to(torch.int8)
+work, work2 = torch.empty(1 << 20, dtype=torch.uint8, device="cuda"), torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+y, mean, rstd = torch.empty_like(big), torch.empty(20000, device="cuda"), torch.empty(20000, device="cuda")
+dg, db = torch.empty(96, device="cuda"), torch.empty(96, device="cuda")
+torch.cuda.synchronize()
+def run():
+    B.dc_linear_quantized(x, w, s, None, out, True, work)
+    B.dc_linear_quantized(big, w2, s[:64], None, o2, False, work2)
+    B.dc_layer_norm(big, None, None, y, mean, rstd)
+    B.dc_layer_norm_backward(big, big, None, mean, rstd, None, dg, db, work2)
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    run()
+g.replay()
+torch.cuda.synchronize()
+kept = [t.clone() for t in (out, o2, y, dg, db)]
+run()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(kept, (out, o2, y, dg, db)))
+print("the same")
+"""
+
+
+@gpu
+def test_the_first_call_of_a_process_inside_a_capture():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL_IN_A_CAPTURE], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "the same" in r.stdout, r.stdout + r.stderr
+
+
+@gpu
 def test_nothing_is_done_with_no_rows():
     x = torch.empty(0, 32, device="cuda")
     w, s = random_q(8, 32, 1)
@@ -673,6 +744,7 @@ ODD1 = C.c_void_p((1 << 20) + 1)
     ("dc_layer_norm_backward", dict(dtype=-1), B.DC_ERR_CONFIG),
     ("dc_layer_norm_backward", dict(rows=3, work=None), B.DC_ERR_ARG),
     ("dc_layer_norm_backward", dict(rows=3, bytes=296 * 8 * 64 - 1), B.DC_ERR_ARG),
+    ("dc_layer_norm_backward", dict(rows=3, work=C.c_void_p((1 << 20) + 8)), B.DC_ERR_ARG),
     ("dc_layer_norm_backward", dict(rows=3, mean=None), B.DC_ERR_ARG),
     ("dc_layer_norm_backward", dict(rows=3, rstd=None), B.DC_ERR_ARG),
     ("dc_layer_norm_backward", dict(rows=3, dy=None), B.DC_ERR_ARG),
