@@ -611,6 +611,10 @@ cudaError_t launch_rows(const dc_rows_args& a, int num_sms, cudaStream_t stream)
     if (nvec > 32 && nvec <= 1024 && a.rows <= 2 * num_sms) DC_ROWS(1, 1024, 32, dc_div_up(nvec, 32) * 32, a.rows);
     // Normalised: 16 channels per lane, whose weights stay in its registers (56 x 56 x 256, 32 streams, bf16: 19.3 us, 22.3 with 32).
     Split s = split_row(nvec, VE == 1 ? 8 : NORM ? 16 / VE : 4);
+    // Longer ones likewise, with a CTA to a row: 12000 x 2048 bf16 20.7 us, 26.5 with a warp; into 8 bits, with its third reduction, 12000 x 768 13.1 and
+    // 11.0, 6000 x 1536 11.3 and 15.0.
+    if constexpr (NORM && VE == 8)
+        if (s.group == 0 && nvec > (QUANT ? 96 : 64) && nvec <= 1024) DC_ROWS(2, 512, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
     if (s.group == 0) s = split_row(nvec, VE == 1 ? 16 : 4);
     if (s.group == 0 && nvec <= 32 * 8) s = {32, 8};
     if (s.group != 0) {
