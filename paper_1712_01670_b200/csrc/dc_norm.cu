@@ -106,14 +106,14 @@ __device__ __forceinline__ uint32_t raw_most(uint32_t m, __nv_bfloat16 t) { retu
 template <typename T> __device__ __forceinline__ uint32_t most_of(uint32_t m) { return sizeof(T) == 2 ? max(m >> 16, m & 0xffffu) << 16 : m; }
 template <typename R> __device__ __forceinline__ R raw_zero() { R r; memset(&r, 0, sizeof(r)); return r; }
 
-// The weights of VE channels; p NULL: `fill`.
-__device__ __forceinline__ void load_weights(const float* p, int at, float fill, float (&v)[1]) { v[0] = p ? __ldg(p + at) : fill; }
+// The weights of VE channels; p NULL: `fill`.  Read after the wait for the kernel before, which may have written them.
+__device__ __forceinline__ void load_weights(const float* p, int at, float fill, float (&v)[1]) { v[0] = p ? dc_ld(p + at) : fill; }
 template <int P>
 __device__ __forceinline__ void load_weights(const float* p, int at, float fill, float2 (&v)[P])
 {
 #pragma unroll
     for (int k = 0; k < P; k += 2) {
-        const float4 t = p ? __ldg((const float4*)(p + at + 2 * k)) : make_float4(fill, fill, fill, fill);
+        const float4 t = p ? dc_ld((const float4*)(p + at + 2 * k)) : make_float4(fill, fill, fill, fill);
         v[k] = make_float2(t.x, t.y); v[k + 1] = make_float2(t.z, t.w);
     }
 }
@@ -272,14 +272,14 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
     // weights of few channels per lane stay in registers; others come from L1 for every row
     constexpr bool KEEP = NORM && NV * VE <= 16;
     F gk[KEEP ? NV : 1][P], bk[KEEP ? NV : 1][P];
+    dc_pdl_wait();
+    dc_pdl_release();
     if (KEEP)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int i = v * lanes + sub;
             if (FULL || i < nvec) { load_weights(a.gamma, i * VE, 1.f, gk[v]); load_weights(a.beta, i * VE, 0.f, bk[v]); }
         }
-    dc_pdl_wait();
-    dc_pdl_release();
     typename V::Raw next[NV];
     bool next_live;
     // places advance by a step's rows: their products with the pitches are 64 bits wide
@@ -383,7 +383,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
         auto at = [&](int i) { float v; V::open(x[i], &v); return v; };
         auto value = [&](int i) -> T {                            // as the map holds it
             float v = at(i);
-            if (NORM) v = fmaf((v - mean) * rstd, a.gamma ? __ldg(a.gamma + i) : 1.f, a.beta ? __ldg(a.beta + i) : 0.f);
+            if (NORM) v = fmaf((v - mean) * rstd, a.gamma ? dc_ld(a.gamma + i) : 1.f, a.beta ? dc_ld(a.beta + i) : 0.f);
             return V::close(&v);
         };
         if (NORM) {
@@ -449,6 +449,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
     const int nvec = a.channels / VE;
     const float c = (float)a.channels, inv_c = 1.f / c;
     F g[NV][P], dg[NV * P], db[NV * P];
+    dc_pdl_wait();
+    dc_pdl_release();
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int i = v * lanes + sub;
@@ -456,8 +458,6 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
         for (int k = 0; k < P; ++k) g[v][k] = dg[v * P + k] = db[v * P + k] = both<F>(0.f);
         if (i < nvec) load_weights(a.gamma, i * VE, 1.f, g[v]);
     }
-    dc_pdl_wait();
-    dc_pdl_release();
     typename V::Raw next_x[NV], next_dy[NV];
     float next_mean, next_rstd;
     int64_t row = BLOCK ? first : first + lane / group;

@@ -115,15 +115,16 @@ __device__ __forceinline__ void store_read(int bufs)          // the place that 
     else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 __device__ __forceinline__ void store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// (dc_ld: the kernel before may have written them.)
 // The scales and biases of two neighbouring columns in each of four groups of eight, from `col` on; beyond the last column: zeros.
 __device__ __forceinline__ void column_weights(const dc_product_args& p, int col, bool whole, float2* s, float2* b)
 {
     if (whole) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] = __ldg((const float2*)(p.b_scale + col + 8 * j));
+        for (int j = 0; j < 4; ++j) s[j] = dc_ld((const float2*)(p.b_scale + col + 8 * j));
         if (p.bias)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[j] = __ldg((const float2*)(p.bias + col + 8 * j));
+            for (int j = 0; j < 4; ++j) b[j] = dc_ld((const float2*)(p.bias + col + 8 * j));
         else
 #pragma unroll
             for (int j = 0; j < 4; ++j) b[j] = make_float2(0.f, 0.f);
@@ -132,8 +133,8 @@ __device__ __forceinline__ void column_weights(const dc_product_args& p, int col
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int c = col + 8 * j;
-        s[j] = make_float2(c < p.n ? __ldg(p.b_scale + c) : 0.f, c + 1 < p.n ? __ldg(p.b_scale + c + 1) : 0.f);
-        b[j] = make_float2(p.bias && c < p.n ? __ldg(p.bias + c) : 0.f, p.bias && c + 1 < p.n ? __ldg(p.bias + c + 1) : 0.f);
+        s[j] = make_float2(c < p.n ? dc_ld(p.b_scale + c) : 0.f, c + 1 < p.n ? dc_ld(p.b_scale + c + 1) : 0.f);
+        b[j] = make_float2(p.bias && c < p.n ? dc_ld(p.bias + c) : 0.f, p.bias && c + 1 < p.n ? dc_ld(p.bias + c + 1) : 0.f);
     }
 }
 
@@ -465,7 +466,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
     bool waited = false;                                                     // for the cluster
     // the channel that this thread finishes: the threads are a multiple of a CTA's channels
     const int rows = 128 / a.CS, ch = threadIdx.x % rows, j = nt * kTileM + rank * rows + ch;
-    const float sb = j < p.n ? __ldg(p.b_scale + j) : 0.f, bias = j < p.n && p.bias ? __ldg(p.bias + j) : 0.f;
+    const float sb = j < p.n ? dc_ld(p.b_scale + j) : 0.f, bias = j < p.n && p.bias ? dc_ld(p.bias + j) : 0.f;
     if (warp == 0) {
         // ---------------- producer ----------------
         if (elect_one()) {

@@ -633,6 +633,54 @@ def test_weights_written_just_before_the_product(m, k, n):
     assert all(torch.equal(o, want[i]) for i, o in got)
 
 
+@gpu
+@pytest.mark.parametrize("c", [256, 100, 1024])
+def test_weights_that_the_kernel_before_writes(c):
+    """gamma, beta, scales and biases are read after the kernel in front is done: here it is the last one of the gradients, which lets its successor
+    start early."""
+    rows = 3000
+    x, dy = make_map(rows, c, torch.bfloat16, 1), make_map(rows, c, torch.bfloat16, 2)
+    _, mean, rstd, _ = norm64(x, None, None, 1e-5)
+    mean, rstd = mean.float(), rstd.float()
+    _, dg, db = run_backward(dy, x, None, mean, rstd)
+    y, q, s = torch.empty_like(x), q_like(rows, c), torch.empty(rows, device="cuda")
+    B.dc_layer_norm(x, dg, db, y)
+    B.dc_quantize_rows(y, q, s)
+    w, _ = random_q(c, c, 3)
+    out = torch.empty(rows, c, dtype=torch.bfloat16, device="cuda")
+    B.dc_matmul_quantized(q, s, w, db, dg, out)
+    few, want_few = q[:5], torch.empty(5, c, dtype=torch.bfloat16, device="cuda")
+    B.dc_matmul_quantized(few, s[:5], w, db, dg, want_few)
+    want_dx, _, _ = run_backward(dy, x, dg, mean, rstd)
+    torch.cuda.synchronize()
+    g, b, work = torch.empty(c, device="cuda"), torch.empty(c, device="cuda"), scratch(B.dc_layer_norm_workspace(c))
+    got = []
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):                                      # one right behind the other
+        for i in range(40):
+            g.fill_(-1.0), b.fill_(2.0)
+            B.dc_layer_norm_backward(dy, x, None, mean, rstd, None, g, b, work)
+            if i % 4 == 0:
+                o = torch.empty_like(y)
+                B.dc_layer_norm(x, g, b, o)
+                got.append((o, y))
+            elif i % 4 == 1:
+                o = torch.empty_like(out)
+                B.dc_matmul_quantized(q, s, w, b, g, o)
+                got.append((o, out))
+            elif i % 4 == 2:
+                o = torch.empty_like(want_few)
+                B.dc_matmul_quantized(few, s[:5], w, b, g, o)
+                got.append((o, want_few))
+            else:
+                o = torch.empty_like(want_dx)
+                B.dc_layer_norm_backward(dy, x, g, mean, rstd, o)
+                got.append((o, want_dx))
+    for _ in range(3):
+        graph.replay()
+    assert all(torch.equal(a, b) for a, b in got)
+
+
 FIRST_CALL_IN_A_CAPTURE = """
 import torch
 from paper_1712_01670_b200 import binding as B
