@@ -327,7 +327,8 @@ int dc_search_blocks_noalloc(const uint8_t* frame_dev, const uint8_t* prev_dev, 
  * and pitches are aligned to an element; 16-byte aligned ones, with rows of whole 16 bytes, are the fast case.  dtype is the map's
  * (DC_FP32, DC_BF16); sums, means and scales are float32 or wider.  Zero rows: DC_OK, nothing is done.  Nothing is allocated, and the work is enqueued on cuda_stream
  * (a cudaStream_t of the current device); the calls may be captured into a graph and may overlap, unless they share memory that one of them
- * writes.  Results do not depend on what runs beside them.  Errors: DC_ERR_ARG, DC_ERR_CONFIG (dtype), DC_ERR_LIMIT (sizes), DC_ERR_CUDA. */
+ * writes.  Results do not depend on what runs beside them.  Errors: DC_ERR_ARG, DC_ERR_CONFIG (dtype), DC_ERR_LIMIT (more than 0x7ff00000 rows, a
+ * pitch of 4 GB or more between rows, and what the call says), DC_ERR_CUDA. */
 
 /* Layer normalisation over the channels of each row:
  *   mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps), y = (x - mean) rstd gamma + beta
@@ -370,7 +371,7 @@ int dc_layer_norm_quantize(const void* x_dev, size_t x_pitch, const float* gamma
  *   nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
  * The sums are exact (int32); scales, bias and ReLU (which leaves a NaN) are applied in float32, with one rounding to dtype.  Every wait inside the
  * kernels is bounded; should one run out (2 s), the results that it concerns are NaN.
- * DC_ERR_LIMIT: k > 131071 (a sum could pass 32 bits), m > 2^31 - 256, n > 2^28. */
+ * DC_ERR_LIMIT: k > 131071 (a sum could pass 32 bits), n > 2^28. */
 int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const int8_t* b_dev, size_t b_pitch,
                         const float* b_scale_dev, const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
                         void* out_dev, size_t out_pitch, void* cuda_stream);

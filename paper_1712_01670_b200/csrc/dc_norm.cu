@@ -126,14 +126,18 @@ struct Most { static __device__ __forceinline__ uint32_t of(uint32_t a, uint32_t
 template <typename Op, typename V>
 __device__ __forceinline__ V reduce_lanes(V v, int group)
 {
-    for (int o = group >> 1; o > 0; o >>= 1) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)                             // steps beyond the group are passed over: no loop to count
+        if (o < group) v = Op::of(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 // The largest of a whole warp is one instruction.
 template <> __device__ __forceinline__ uint32_t reduce_lanes<Most, uint32_t>(uint32_t v, int group)
 {
     if (group == 32) return __reduce_max_sync(0xffffffffu, v);
-    for (int o = group >> 1; o > 0; o >>= 1) v = Most::of(v, __shfl_xor_sync(0xffffffffu, v, o));
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1)
+        if (o < group) v = Most::of(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 template <typename Op, bool BLOCK, typename V>
@@ -236,19 +240,21 @@ __device__ __forceinline__ RowScale row_scale(uint32_t bits)
 }
 
 // A row's place in q and scale: see dc_rows_args.
-__device__ __forceinline__ int64_t q_row(const dc_rows_args& a, int64_t row)
+__device__ __forceinline__ int q_row(const dc_rows_args& a, int row)
 {
     if (a.padded == 0) return row;
-    const int64_t line = row / a.width;
+    const int line = row / a.width;
     return line * a.padded + (row - line * a.width);
 }
+// Row `row` of a map: rows and pitches are below 2^32, so the place is one multiplication of 32 bits by 32.
+__device__ __forceinline__ char* row_at(const void* p, size_t pitch, int row) { return (char*)p + (uint64_t)(uint32_t)row * (uint32_t)pitch; }
 
 // Is the row wanted?  (Reused pixels' are not.)
-__device__ __forceinline__ bool wanted(const dc_rows_args& a, int64_t row)
+__device__ __forceinline__ bool wanted(const dc_rows_args& a, int row)
 {
-    if (row >= a.rows) return false;
+    if (row >= (int)a.rows) return false;
     if (!a.masks) return true;
-    const int64_t q = q_row(a, row);
+    const int q = q_row(a, row);
     return !((a.masks[q >> 5] >> (q & 31)) & 1u);
 }
 
@@ -264,9 +270,9 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
     constexpr bool AHEAD = BLOCK < 1024;
     __shared__ float red[BLOCK ? 6 * 32 : 1];
     const int lane = threadIdx.x & 31, sub = BLOCK ? threadIdx.x : lane & (group - 1), lanes = BLOCK ? blockDim.x : group;
-    const int per_warp = BLOCK ? 1 : 32 / group;
-    const int64_t first = BLOCK ? blockIdx.x : ((int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * per_warp;
-    const int64_t step = BLOCK ? gridDim.x : (int64_t)gridDim.x * (blockDim.x >> 5) * per_warp;
+    const int per_warp = BLOCK ? 1 : 32 / group, rows = (int)a.rows;
+    const int first = BLOCK ? blockIdx.x : (blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * per_warp;
+    const int step = BLOCK ? gridDim.x : gridDim.x * (blockDim.x >> 5) * per_warp;
     const int nvec = a.channels / VE;
     const float c = (float)a.channels, inv_c = 1.f / c;
     // weights of few channels per lane stay in registers; others come from L1 for every row
@@ -282,24 +288,22 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
         }
     typename V::Raw next[NV];
     bool next_live;
-    // places advance by a step's rows: their products with the pitches are 64 bits wide
-    int64_t row = BLOCK ? first : first + lane / group;
     constexpr int VB = VE * (int)sizeof(T);
-    const char* x_at = (const char*)a.x + (size_t)row * a.x_pitch + sub * VB;
-    char* y_at = NORM ? (char*)a.y + (size_t)row * a.y_pitch + sub * VB : nullptr;
-    int8_t* q_at = QUANT ? a.q + (size_t)row * a.q_pitch + sub * VE : nullptr;              // dense
-    const size_t x_step = (size_t)step * a.x_pitch, y_step = (size_t)step * a.y_pitch, q_step = (size_t)step * a.q_pitch;
     const int line = lanes * VB;
-    auto fetch = [&](int64_t r) {
-        const bool live = QUANT && !NORM ? wanted(a, r) : r < a.rows;
-        next_live = live;
+    // lanes beyond the row's end never load and keep their zeros; a row that is not there leaves the last one's values, and nothing of it is stored
 #pragma unroll
-        for (int v = 0; v < NV; ++v) next[v] = live && (FULL || v * lanes + sub < nvec) ? *(const typename V::Raw*)(x_at + v * line) : raw_zero<typename V::Raw>();
-        x_at += x_step;
+    for (int v = 0; v < NV; ++v) next[v] = raw_zero<typename V::Raw>();
+    auto fetch = [&](int r) {
+        next_live = NORM ? r < rows : wanted(a, r);
+        const char* const x = row_at(a.x, a.x_pitch, r) + sub * VB;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (next_live && (FULL || v * lanes + sub < nvec)) next[v] = *(const typename V::Raw*)(x + v * line);
     };
+    int row = BLOCK ? first : first + lane / group;
     if (AHEAD) fetch(row);
     int parity = 0;
-    for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
+    for (int base = first; base < rows; base += step, row += step, parity ^= 1) {
         float* const slot = red + (BLOCK ? parity * 96 : 0);
         F d[NV * P];
         uint32_t m = 0;
@@ -325,9 +329,10 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
                     for (int k = v * P; k < v * P + P; ++k) { d[k] = add2(d[k], minus); s = fma2(d[k], d[k], s); }
             const float rstd = inverse_root(over(reduce<Sum, (BLOCK > 0)>(sum_of(s), group, slot + 32), c, inv_c) + a.eps);
             if (on && sub == 0) {
-                if (a.mean) a.mean[row] = mean;
-                if (a.rstd) a.rstd[row] = rstd;
+                if (a.mean) a.mean[(uint32_t)row] = mean;
+                if (a.rstd) a.rstd[(uint32_t)row] = rstd;
             }
+            char* const y = NORM ? row_at(a.y, a.y_pitch, row) + sub * VB : nullptr;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int i = v * lanes + sub;
@@ -338,7 +343,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
                     for (int k = 0; k < P; ++k) d[v * P + k] = fma2(mul2(d[v * P + k], both<F>(rstd)), KEEP ? gk[KEEP ? v : 0][k] : g[k], KEEP ? bk[KEEP ? v : 0][k] : b[k]);
                 }
                 const typename V::Raw r = V::close(d + v * P);
-                if (on && a.y && (FULL || i < nvec)) *(typename V::Raw*)(y_at + v * line) = r;
+                if (on && a.y && (FULL || i < nvec)) *(typename V::Raw*)(y + v * line) = r;
                 if (QUANT && sizeof(T) == 2) V::open(r, d + v * P);             // as the map holds it
                 if (QUANT) m = raw_most(m, r);
             }
@@ -346,21 +351,19 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
         if (QUANT) {
             m = reduce<Most, (BLOCK > 0)>(most_of<T>(m), group, (uint32_t*)slot + 64);
             const RowScale s = row_scale(m);
-            const int64_t qr = q_row(a, row);
-            if (on && sub == 0) a.scale[qr] = s.scale;
+            const int qr = q_row(a, row);
+            if (on && sub == 0) a.scale[(uint32_t)qr] = s.scale;
             if (s.lift != 1.f)
 #pragma unroll
                 for (int k = 0; k < NV * P; ++k) d[k] = s.lift != 0.f ? mul2(d[k], both<F>(s.lift)) : both<F>(0.f);
-            int8_t* const q = a.padded ? a.q + (size_t)qr * a.q_pitch + sub * VE : q_at;
+            int8_t* const q = (int8_t*)row_at(a.q, a.q_pitch, qr) + sub * VE;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 uint32_t w[VE == 8 ? 2 : 1];
                 quantise<T, VE>(d + v * P, s.inv, s.most, w);
                 if (on && (FULL || v * lanes + sub < nvec)) store_q<VE>(q + v * lanes * VE, w);
             }
-            q_at += q_step;
         }
-        if (NORM) y_at += y_step;
     }
 }
 
@@ -374,11 +377,11 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
     dc_pdl_release();
     int parity = 0;
     const float c = (float)a.channels, inv_c = 1.f / c;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, parity ^= 1) {
+    for (int row = blockIdx.x; row < (int)a.rows; row += gridDim.x, parity ^= 1) {
         if (QUANT && !NORM && !wanted(a, row)) continue;
         float* const slot = red + parity * 96;
-        const T* const x = (const T*)((const char*)a.x + (size_t)row * a.x_pitch);
-        T* const y = (T*)((char*)a.y + (size_t)row * a.y_pitch);
+        const T* const x = (const T*)row_at(a.x, a.x_pitch, row);
+        T* const y = (T*)row_at(a.y, a.y_pitch, row);
         float mean = 0.f, rstd = 1.f;
         auto at = [&](int i) { float v; V::open(x[i], &v); return v; };
         auto value = [&](int i) -> T {                            // as the map holds it
@@ -399,7 +402,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
             }
         }
         RowScale s = {};
-        const int64_t qr = q_row(a, row);
+        const int qr = q_row(a, row);
         if (QUANT) {
             uint32_t m = 0;
             for (int i = threadIdx.x; i < a.channels; i += blockDim.x) { float v; V::open(value(i), &v); m = Most::of(m, size_bits(v)); }
@@ -445,7 +448,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lanes = group;
     const int team = BLOCK ? threadIdx.x / group : warp, sub = BLOCK ? threadIdx.x - team * group : lane & (group - 1);
     const int per_team = BLOCK ? 1 : 32 / group, teams = BLOCK ? blockDim.x / group : blockDim.x >> 5;
-    const int64_t first = ((int64_t)blockIdx.x * teams + team) * per_team, step = (int64_t)gridDim.x * teams * per_team;
+    const int first = (blockIdx.x * teams + team) * per_team, step = gridDim.x * teams * per_team, rows = (int)a.rows;
     const int nvec = a.channels / VE;
     const float c = (float)a.channels, inv_c = 1.f / c;
     F g[NV][P], dg[NV * P], db[NV * P];
@@ -460,28 +463,25 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
     }
     typename V::Raw next_x[NV], next_dy[NV];
     float next_mean, next_rstd;
-    int64_t row = BLOCK ? first : first + lane / group;
     constexpr int VB = VE * (int)sizeof(T);
-    const char *x_at = (const char*)a.x + (size_t)row * a.x_pitch + sub * VB, *dy_at = (const char*)a.dy + (size_t)row * a.dy_pitch + sub * VB;
-    char* dx_at = (char*)a.dx + (size_t)row * a.dx_pitch + sub * VB;
-    const size_t x_step = (size_t)step * a.x_pitch, dy_step = (size_t)step * a.dy_pitch, dx_step = (size_t)step * a.dx_pitch;
     const int line = lanes * VB;
-    auto fetch = [&](int64_t r) {
-        const bool on = r < a.rows;
-        next_mean = on ? a.mean[r] : 0.f;
-        next_rstd = on ? a.rstd[r] : 0.f;
+    // as in k_rows: lanes beyond the row's end keep zeros, a row that is not there the last one's values
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const bool there = on && (FULL || v * lanes + sub < nvec);
-            next_x[v] = there ? *(const typename V::Raw*)(x_at + v * line) : raw_zero<typename V::Raw>();
-            next_dy[v] = there ? *(const typename V::Raw*)(dy_at + v * line) : raw_zero<typename V::Raw>();
-        }
-        x_at += x_step; dy_at += dy_step;
+    for (int v = 0; v < NV; ++v) next_x[v] = next_dy[v] = raw_zero<typename V::Raw>();
+    next_mean = next_rstd = 0.f;
+    auto fetch = [&](int r) {
+        const bool live = r < rows;
+        const char *const x = row_at(a.x, a.x_pitch, r) + sub * VB, *const dy = row_at(a.dy, a.dy_pitch, r) + sub * VB;
+        if (live) { next_mean = a.mean[(uint32_t)r]; next_rstd = a.rstd[(uint32_t)r]; }
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+            if (live && (FULL || v * lanes + sub < nvec)) { next_x[v] = *(const typename V::Raw*)(x + v * line); next_dy[v] = *(const typename V::Raw*)(dy + v * line); }
     };
+    int row = BLOCK ? first : first + lane / group;
     fetch(row);
     int parity = 0;
-    for (int64_t base = first; base < a.rows; base += step, row += step, parity ^= 1) {
-        const bool on = row < a.rows;
+    for (int base = first; base < rows; base += step, row += step, parity ^= 1) {
+        const bool on = row < rows;
         F xh[NV * P], d[NV * P];
         const float mean = next_mean, rstd = next_rstd;
 #pragma unroll
@@ -494,8 +494,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
 #pragma unroll
                 for (int k = v * P; k < v * P + P; ++k) {
                     xh[k] = mul2(add2(xh[k], both<F>(-mean)), both<F>(rstd));
-                    dg[k] = fma2(d[k], xh[k], dg[k]);
-                    db[k] = add2(db[k], d[k]);
+                    if (on) { dg[k] = fma2(d[k], xh[k], dg[k]); db[k] = add2(db[k], d[k]); }
                     d[k] = mul2(d[k], g[v][k - v * P]);
                     p1 = add2(p1, d[k]);
                     p2 = fma2(d[k], xh[k], p2);
@@ -510,15 +509,18 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
             const int warps = group >> 5, at = team * warps + lane;
             s1 = lane < warps ? slot[at] : 0.f; s2 = lane < warps ? slot[32 + at] : 0.f;
         }
-        s1 = reduce_lanes<Sum>(s1, BLOCK ? 32 : group) * -inv_c;
-        s2 = reduce_lanes<Sum>(s2, BLOCK ? 32 : group) * -inv_c;
+        const int over_lanes = BLOCK ? 32 : group;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            if (o < over_lanes) { s1 += __shfl_xor_sync(0xffffffffu, s1, o); s2 += __shfl_xor_sync(0xffffffffu, s2, o); }
+        s1 *= -inv_c; s2 *= -inv_c;
+        char* const dx = row_at(a.dx, a.dx_pitch, row) + sub * VB;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
 #pragma unroll
             for (int k = v * P; k < v * P + P; ++k) d[k] = mul2(fma2(xh[k], both<F>(s2), add2(d[k], both<F>(s1))), both<F>(rstd));
-            if (on && (FULL || v * lanes + sub < nvec)) *(typename V::Raw*)(dx_at + v * line) = V::close(d + v * P);
+            if (on && (FULL || v * lanes + sub < nvec)) *(typename V::Raw*)(dx + v * line) = V::close(d + v * P);
         }
-        dx_at += dx_step;
     }
     if (!a.partial) return;
     float* const out = a.partial + (size_t)blockIdx.x * 2 * a.channels;
@@ -691,6 +693,7 @@ cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t
 }
 
 constexpr int kMostNormChannels = 16384;
+constexpr int64_t kMostRows = DC_MOST_ROWS;
 
 }  // namespace
 
@@ -716,6 +719,7 @@ int dc_launch_rows(const dc_rows_args& a, bool norm, int dtype, int num_sms, cud
 }
 
 // What every entry point asks of rows of a map.
+static bool rows_within(size_t a, size_t b, size_t c, int64_t rows) { return rows <= kMostRows && (rows < 2 || (a | b | c) <= 0xffffffffu); }
 static bool rows_ok(const void* p, size_t pitch, int64_t rows, int64_t columns, int elt)
 {
     return p && (uintptr_t)p % elt == 0 && pitch % elt == 0 && (rows < 2 || pitch >= (size_t)columns * elt);
@@ -732,7 +736,7 @@ static int norm_call(const void* x, size_t x_pitch, const float* gamma, const fl
     if (dtype != DC_FP32 && dtype != DC_BF16) return DC_ERR_CONFIG;
     const int elt = dtype == DC_BF16 ? 2 : 4;
     if (rows < 0 || channels < 1 || !(eps >= 0.0) || !(eps < 1e30)) return DC_ERR_ARG;
-    if (channels > kMostNormChannels) return DC_ERR_LIMIT;
+    if (channels > kMostNormChannels || !rows_within(x_pitch, y ? y_pitch : 0, want_q ? q_pitch : 0, rows)) return DC_ERR_LIMIT;
     if (!floats_ok(gamma) || !floats_ok(beta) || !floats_ok(mean) || !floats_ok(rstd)) return DC_ERR_ARG;
     if (rows == 0) return DC_OK;
     if (!rows_ok(x, x_pitch, rows, channels, elt) || ((want_y || y) && !rows_ok(y, y_pitch, rows, channels, elt))) return DC_ERR_ARG;
@@ -763,6 +767,7 @@ int dc_quantize_rows(const void* x_dev, size_t x_pitch, int64_t rows, int32_t ch
 {
     if (dtype != DC_FP32 && dtype != DC_BF16) return DC_ERR_CONFIG;
     if (rows < 0 || channels < 1) return DC_ERR_ARG;
+    if (!rows_within(x_pitch, q_pitch, 0, rows)) return DC_ERR_LIMIT;
     if (rows == 0) return DC_OK;
     if (!rows_ok(x_dev, x_pitch, rows, channels, dtype == DC_BF16 ? 2 : 4) || !quant_ok(q_dev, q_pitch, scale_dev, rows, channels)) return DC_ERR_ARG;
     dc_rows_args a = {};
@@ -786,7 +791,7 @@ int dc_layer_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_de
     if (dtype != DC_FP32 && dtype != DC_BF16) return DC_ERR_CONFIG;
     const int elt = dtype == DC_BF16 ? 2 : 4;
     if (rows < 0 || channels < 1) return DC_ERR_ARG;
-    if (channels > kMostNormChannels) return DC_ERR_LIMIT;
+    if (channels > kMostNormChannels || !rows_within(dy_pitch, x_pitch, dx_dev ? dx_pitch : 0, rows)) return DC_ERR_LIMIT;
     if (!floats_ok(gamma_dev) || !floats_ok(mean_dev) || !floats_ok(rstd_dev) || !floats_ok(dgamma_dev) || !floats_ok(dbeta_dev)) return DC_ERR_ARG;
     const bool weights = dgamma_dev || dbeta_dev;
     size_t need = 0;

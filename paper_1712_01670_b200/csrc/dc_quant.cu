@@ -741,7 +741,6 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
 }
 
 constexpr int kMostTerms = 131071;
-constexpr int64_t kMostRows = 0x7fffff00;
 
 // What both products ask of their operands.
 static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, const float* bias, int64_t m, int32_t n, int32_t k, int32_t dtype, const void* out, size_t out_pitch)
@@ -749,7 +748,7 @@ static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, 
     if (dtype != DC_FP32 && dtype != DC_BF16) return DC_ERR_CONFIG;
     const int elt = dtype == DC_BF16 ? 2 : 4;
     if (m < 0 || n < 1 || k < 1) return DC_ERR_ARG;
-    if (k > kMostTerms || m > kMostRows || n > (1 << 28)) return DC_ERR_LIMIT;
+    if (k > kMostTerms || m > DC_MOST_ROWS || n > (1 << 28)) return DC_ERR_LIMIT;
     if (m == 0) return DC_OK;
     if (!b || !b_scale || !out || (uintptr_t)b % 16 || b_pitch % 16 || (n > 1 && b_pitch < (size_t)k)) return DC_ERR_ARG;
     if ((uintptr_t)b_scale % 4 || (uintptr_t)bias % 4 || (uintptr_t)out % elt || out_pitch % elt || (m > 1 && out_pitch < (size_t)n * elt)) return DC_ERR_ARG;
@@ -787,6 +786,7 @@ int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, 
     const int elt = dtype == DC_BF16 ? 2 : 4;
     size_t need = 0;
     dc_linear_workspace(m, k, &need);
+    if (m > 1 && x_pitch > 0xffffffffu) return DC_ERR_LIMIT;
     if (!x_dev || (uintptr_t)x_dev % elt || x_pitch % elt || (m > 1 && x_pitch < (size_t)k * elt) || !workspace_dev || workspace_bytes < need) return DC_ERR_ARG;
     int device = 0, sms = 0;
     if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;

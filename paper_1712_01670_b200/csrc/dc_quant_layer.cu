@@ -26,6 +26,7 @@ int copy_floats(dc_cache* c, float** to, const float* from, size_t n)
 int dc_build_norm(dc_cache* c, int layer, const float* gamma, const float* beta)
 {
     dc_layer_rt& L = c->L[layer];
+    if ((size_t)c->S * L.d.out_h * L.d.out_w > (size_t)DC_MOST_ROWS) return DC_ERR_CONFIG;
     L.eps = 1e-5f;
     int rc = DC_OK;
     if (gamma) rc = copy_floats(c, (float**)&L.weight, gamma, L.d.cout);
@@ -40,7 +41,7 @@ int dc_build_quant(dc_cache* c, int layer, const float* w, const float* b)
     const int k = L.d.kh * L.d.kw * L.d.cin;
     const size_t pitch = dc_quant_pitch(k);
     const size_t rows = pointwise ? (size_t)c->S * L.d.out_h * L.gpr * DC_TILE_W : (size_t)c->S;
-    if (rows > 0x7fffff00u) return DC_ERR_CONFIG;
+    if (rows > (size_t)DC_MOST_ROWS || pitch > 0xffffffffu || (size_t)k * c->elt > 0xffffffffu) return DC_ERR_CONFIG;
     int rc = copy_floats(c, &L.bias, b, L.d.cout);
     if (rc == DC_OK) rc = layer_alloc(c, (int8_t**)&L.weight, pitch * L.d.cout);
     if (rc == DC_OK) rc = layer_alloc(c, &L.w_scale, (size_t)L.d.cout);

@@ -3,6 +3,9 @@
 #pragma once
 #include "dc_common.cuh"
 
+// Most rows of a call (the kernels count rows in 32 bits, a grid's step ahead).  Pitches are below 2^32 where there are two rows or more.
+#define DC_MOST_ROWS 0x7ff00000
+
 // Rows [rows][channels] to be normalised (norm), quantised (q) or both.  Pitches in bytes.
 struct dc_rows_args {
     const void* x; size_t x_pitch;

@@ -798,6 +798,11 @@ ODD1 = C.c_void_p((1 << 20) + 1)
     ("dc_layer_norm_backward", dict(rows=3, dy=None), B.DC_ERR_ARG),
     ("dc_layer_norm_backward", dict(rows=3, dxp=128), B.DC_ERR_ARG),
     ("dc_layer_norm_backward", dict(rows=3, dx=None, dgamma=None, dbeta=None, work=None), B.DC_OK),   # nothing wanted
+    ("dc_layer_norm", dict(rows=0x7ff00001), B.DC_ERR_LIMIT),
+    ("dc_layer_norm", dict(rows=2, yp=1 << 32), B.DC_ERR_LIMIT),
+    ("dc_layer_norm_backward", dict(rows=2, dyp=1 << 32), B.DC_ERR_LIMIT),
+    ("dc_quantize_rows", dict(rows=2, xp=1 << 40), B.DC_ERR_LIMIT),
+    ("dc_linear_quantized", dict(rows=2, xp=1 << 32), B.DC_ERR_LIMIT),
     ("dc_quantize_rows", dict(rows=-1), B.DC_ERR_ARG),
     ("dc_quantize_rows", dict(rows=2, q=None), B.DC_ERR_ARG),
     ("dc_quantize_rows", dict(rows=2, scale=None), B.DC_ERR_ARG),
