@@ -790,15 +790,17 @@ int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, 
     if (!x_dev || (uintptr_t)x_dev % elt || x_pitch % elt || (m > 1 && x_pitch < (size_t)k * elt) || !workspace_dev || workspace_bytes < need) return DC_ERR_ARG;
     int device = 0, sms = 0;
     if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
+    dc_product_args p = {};
+    p.b = w_dev; p.b_pitch = w_pitch; p.b_scale = w_scale_dev; p.bias = bias_dev;
+    p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch;
+    if (dc_few_pays(m, n, k)) return dc_launch_few(p, x_dev, x_pitch, dtype, device, sms, (cudaStream_t)cuda_stream);
     const size_t pitch = dc_quant_pitch(k);
     int8_t* const q = (int8_t*)(((uintptr_t)workspace_dev + 255) & ~(uintptr_t)255);
     float* const scale = (float*)(q + (size_t)m * pitch);
     dc_rows_args r = {};
     r.x = x_dev; r.x_pitch = x_pitch; r.rows = m; r.channels = k; r.q = q; r.q_pitch = pitch; r.scale = scale;
     if ((rc = dc_launch_rows(r, false, dtype, sms, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
-    dc_product_args p = {};
-    p.a = q; p.a_pitch = pitch; p.a_scale = scale; p.b = w_dev; p.b_pitch = w_pitch; p.b_scale = w_scale_dev; p.bias = bias_dev;
-    p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch; p.early = 1;
+    p.a = q; p.a_pitch = pitch; p.a_scale = scale; p.early = 1;
     return dc_launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
 }
 

@@ -83,6 +83,14 @@ int dc_launch_quant(dc_cache* c, int layer, const void* in, bool filled, void* o
     const int k = L.d.kh * L.d.kw * L.d.cin;
     dc_prof_scope ps(c, DC_ST_CONV);
     dc_product_args p = {};
+    p.a = L.q_rows; p.a_pitch = dc_quant_pitch(k); p.a_scale = L.q_scale; p.b = (const int8_t*)L.weight; p.b_pitch = p.a_pitch; p.b_scale = L.w_scale; p.bias = L.bias;
+    p.n = L.d.cout; p.k = k; p.relu = L.d.relu; p.out = out; p.out_pitch = (size_t)L.d.cout * c->elt; p.status = c->status;
+    p.early = 1;                                                                // weights are older than any frame
+    p.m = pointwise ? (int64_t)c->S * L.d.out_h * L.gpr * DC_TILE_W : (int64_t)c->S;
+    if (!pointwise && dc_few_pays(p.m, p.n, k)) {
+        c->launches += 1;
+        return dc_launch_few(p, in, (size_t)k * c->elt, c->cfg.dtype, c->device, c->num_sms, c->stream);
+    }
     if (!filled) {
         dc_rows_args a = {};
         a.x = in; a.x_pitch = (size_t)k * c->elt; a.channels = k;
@@ -94,10 +102,6 @@ int dc_launch_quant(dc_cache* c, int layer, const void* in, bool filled, void* o
         const int rc = dc_launch_rows(a, false, c->cfg.dtype, c->num_sms, c->stream);
         if (rc != DC_OK) return rc;
     }
-    p.a = L.q_rows; p.a_pitch = dc_quant_pitch(k); p.a_scale = L.q_scale; p.b = (const int8_t*)L.weight; p.b_pitch = p.a_pitch; p.b_scale = L.w_scale; p.bias = L.bias;
-    p.n = L.d.cout; p.k = k; p.relu = L.d.relu; p.out = out; p.out_pitch = (size_t)L.d.cout * c->elt; p.status = c->status;
-    p.early = 1;                                                                // weights are older than any frame
-    p.m = pointwise ? (int64_t)c->S * L.d.out_h * L.gpr * DC_TILE_W : (int64_t)c->S;
     if (pointwise && (tile_list || L.gpr * DC_TILE_W != L.d.out_w)) {
         p.width = L.d.out_w; p.padded = L.gpr * DC_TILE_W;
         p.tile_list = tile_list; p.tile_count = tile_count; p.masks = masks; p.max_tiles = tile_list ? dc_layer_tiles(c, L) : 0;

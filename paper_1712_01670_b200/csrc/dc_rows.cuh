@@ -38,6 +38,11 @@ struct dc_product_args {
 };
 int dc_launch_product(const dc_product_args& a, int dtype, int device, int num_sms, cudaStream_t stream);
 
+// The same for one row or a few short ones, given as the map has them (p.a and p.a_scale are not used), in one launch (dc_few.cu).
+#define DC_FEW_BYTES (200 * 1024)        // shared memory for them
+bool dc_few_pays(int64_t m, int n, int k);
+int dc_launch_few(const dc_product_args& p, const void* x, size_t x_pitch, int dtype, int device, int num_sms, cudaStream_t stream);
+
 static inline size_t dc_quant_pitch(int64_t k) { return (size_t)(k + 15) / 16 * 16; }
 // The device that is current, and its number of SMs (looked up once per device).
 int dc_current_device(int* device, int* num_sms);

@@ -499,6 +499,35 @@ def test_linear_has_the_bits_of_its_two_steps_and_keeps_what_is_not_finite_to_it
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", [(1, 1, 1), (1, 16, 3), (1, 17, 70), (1, 100, 50), (1, 1000, 300), (1, 4096, 4099), (1, 30001, 20), (2, 7, 5), (2, 512, 600), (2, 2049, 64),
+                                   (2, 100000, 8), (3, 64, 64), (3, 333, 77), (4, 1024, 256), (5, 130, 9), (7, 585, 40), (8, 512, 1000), (8, 5, 3)])
+def test_linear_of_one_row_and_of_a_few_short_ones(m, k, n, dtype):
+    t = TYPES[dtype]
+    x, _ = spread(make_map(m, k, t, m + k), k + 3 if k % 2 else k + 8, 5 if n % 2 else 0)
+    if m > 2:
+        x[1] = 0
+        x[2, k // 2] = float("nan")
+    if m > 4:
+        x[3] = (x[3].float() * 2.0 ** -130).to(t)
+        x[4] = (x[4].float() * 1e30).to(t)
+    w, ws = random_q(n, k, k)
+    bias = torch.randn(n, generator=gen(4), device="cuda") if n % 3 else None
+    for relu in (False, True):
+        out, buf = spread(torch.zeros(m, n, dtype=t, device="cuda"), n + 7, 1)
+        B.dc_linear_quantized(x, w, ws, bias, out, relu, scratch(B.dc_linear_workspace(m, k)))
+        q, s = quantise64(x)
+        good = torch.isfinite(x.float()).all(1)
+        want, bound = product64(q[good], s[good], w, ws, bias, relu)
+        T = half_step(t)
+        assert ((out[good].double() - want).abs() <= bound * (1 + T) + T * want.abs() + 1e-38).all()
+        assert torch.isnan(out[~good].float()).all()
+        rest = buf.clone()
+        rest[1:1 + m * (n + 7)].view(m, n + 7)[:, :n] = 77
+        assert (rest == 77).all()
+
+
+@gpu
 @pytest.mark.parametrize("k,n", [(20000, 33), (25088, 256), (70000, 16)])
 def test_linear_of_long_rows(k, n):
     for m in (1, 3, 33):
