@@ -207,6 +207,7 @@ struct dc_backward_args {
     int64_t rows; int channels;
     void* dx; size_t dx_pitch;          // or NULL
     float* partial;                     // [CTAs][2][channels], or NULL: no gradients of the weights
+    float *dgamma, *dbeta;              // a single CTA's sums go straight there (either may be NULL)
 };
 
 // Gradients.  A row belongs to `group` lanes of a warp, or (BLOCK) to `group` threads of whole warps, several such groups to a CTA.  They keep the same
@@ -324,7 +325,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_norm_backward(const dc_backwa
     for (int i = threadIdx.x; i < 2 * a.channels; i += blockDim.x) {
         float s = 0.f;
         for (int t = 0; t < teams; ++t) s += join[t * 2 * a.channels + i];
-        out[i] = s;
+        if (gridDim.x > 1) out[i] = s;
+        else if (i < a.channels) { if (a.dgamma) a.dgamma[i] = s; }
+        else if (a.dbeta) a.dbeta[i - a.channels] = s;
     }
 }
 
@@ -435,7 +438,10 @@ cudaError_t launch_backward_as(const dc_backward_args& a, int group, int num_sms
     const size_t smem = BLOCK && teams == 1 ? 0 : (size_t)teams * 2 * a.channels * sizeof(float);
     const int64_t per_cta = (int64_t)teams * (BLOCK ? 1 : 32 / group), want = (a.rows + per_cta - 1) / per_cta;
     const int most = CTAS * num_sms < kBackwardCtas ? CTAS * num_sms : kBackwardCtas;          // as many as are resident
-    *ctas = (int)(want < 1 ? 1 : want < most ? want : most);
+    // Up to three rows to a team: one CTA, which needs no second launch to join others' sums (20 x 100 bf16 3.3 us in a graph and 7.4 a pass, 4.3 and 9.7
+    // with one; from the fourth row on a turn's half microsecond adds up to more than the join).
+    const bool alone = want <= 3 && !(BLOCK && teams == 1);
+    *ctas = alone ? 1 : (int)(want < 2 ? 2 : want < most ? want : most);
     return dc_launch_pdl(k_norm_backward<T, VE, NV, BLOCK, THREADS, CTAS, FULL>, dim3((unsigned)*ctas), threads, smem, stream, a, group);
 }
 
@@ -580,7 +586,7 @@ int dc_layer_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_de
     if (!mean_dev || !rstd_dev || !rows_ok(dy_dev, dy_pitch, rows, channels, elt) || !rows_ok(x_dev, x_pitch, rows, channels, elt)) return DC_ERR_ARG;
     if (dx_dev && !rows_ok(dx_dev, dx_pitch, rows, channels, elt)) return DC_ERR_ARG;
     if (!dx_dev && !weights) return DC_OK;
-    dc_backward_args a = {dy_dev, dy_pitch, x_dev, x_pitch, gamma_dev, mean_dev, rstd_dev, rows, channels, dx_dev, dx_pitch, weights ? (float*)workspace_dev : nullptr};
+    dc_backward_args a = {dy_dev, dy_pitch, x_dev, x_pitch, gamma_dev, mean_dev, rstd_dev, rows, channels, dx_dev, dx_pitch, weights ? (float*)workspace_dev : nullptr, dgamma_dev, dbeta_dev};
     int device = 0, sms = 0, ctas = 0;
     const int rc = dc_current_device(&device, &sms);
     if (rc != DC_OK) return rc;
@@ -589,7 +595,7 @@ int dc_layer_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_de
                      (uintptr_t)gamma_dev % 16 == 0;
     if (dtype == DC_BF16) DC_CUDA(vec ? (launch_backward<__nv_bfloat16, 8>(a, sms, stream, &ctas)) : (launch_backward<__nv_bfloat16, 1>(a, sms, stream, &ctas)));
     else DC_CUDA(vec ? (launch_backward<float, 4>(a, sms, stream, &ctas)) : (launch_backward<float, 1>(a, sms, stream, &ctas)));
-    if (weights)
+    if (weights && ctas != 1)
         DC_CUDA(dc_launch_pdl(k_join, dim3((unsigned)dc_div_up(2 * channels, 32)), 1024, 0, stream, (const float*)workspace_dev, ctas, (int)channels, dgamma_dev, dbeta_dev));
     return DC_OK;
 }
