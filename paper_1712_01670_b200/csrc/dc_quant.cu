@@ -115,8 +115,8 @@ __device__ __forceinline__ void store_read(int bufs)          // the place that 
     else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 __device__ __forceinline__ void store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-// (dc_ld: the kernel before may have written them.)
-// The scales and biases of two neighbouring columns in each of four groups of eight, from `col` on; beyond the last column: zeros.
+// The scales and biases of two neighbouring columns in each of four groups of eight, from `col` on; beyond the last column: zeros.  (dc_ld: the
+// kernel before may have written them.)
 __device__ __forceinline__ void column_weights(const dc_product_args& p, int col, bool whole, float2* s, float2* b)
 {
     if (whole) {
@@ -260,8 +260,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
         // rows each every fourth.  A lane holds two neighbouring columns of four rows in each group of eight columns, so that it needs the scales and
         // biases of a quarter of the columns: with a row per lane every lane needed all of them, and reading those from shared memory took
         // more of its bandwidth than the operands.  Where out takes 16-byte stores the warp turns its rows through shared memory and they leave
-        // as boxes of 32 rows x 64 bytes by TMA: 25088 x 512 x 2048 to bf16 in 30.6 us, 3.36 TB/s written (a fill of that size: 3.8), with
-        // the lanes' own stores of 64 bytes of a row 40.0, of 128 bytes 45.1.
+        // as boxes of 32 rows x 64 bytes by TMA: 25088 x 512 x 2048 to bf16 in 28.6 us, 3.6 TB/s written (to float32 41, 5.0); before the
+        // instructions were cut 30.6, and then with the lanes' own stores of 64 bytes of a row 40.0, of 128 bytes 45.1.
         const int q = warp & 3, part = (warp - 2) >> 2;
         uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 2) * kStage;
         const uint32_t to_stage = (lane & 7) * 64 + (((lane >> 3) ^ ((lane >> 1) & 3)) << 4);           // + 512 per eight rows
@@ -591,7 +591,7 @@ bool encode_rows(CUtensorMap* tm, const void* base, size_t pitch, int64_t rows, 
                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// out in boxes of 32 rows x 64 bytes; nothing is written beyond the last row and column.
+// out in boxes of 32 rows x 64 bytes; rows of whole 16 bytes, beyond which nothing is written, nor beyond the last row.
 bool encode_out(CUtensorMap* tm, const dc_product_args& p, int elt)
 {
     const size_t pitch = p.m < 2 ? ((size_t)p.n * elt + 15) / 16 * 16 : p.out_pitch;
@@ -726,7 +726,8 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
     a.wide = (uintptr_t)p.out % 16 == 0 && p.out_pitch % 16 == 0;
     CUtensorMap tmA, tmB, tmC = {};
     if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
-    if (a.wide && !p.padded) a.boxes = encode_out(&tmC, p, dtype == DC_BF16 ? 2 : 4);
+    // (a box is cut at whole 16 bytes, not at the row's last column)
+    if (a.wide && !p.padded && (size_t)p.n * elt % 16 == 0) a.boxes = encode_out(&tmC, p, dtype == DC_BF16 ? 2 : 4);
     const long long items = (pair ? (tiles + 1) / 2 : tiles) * a.NB, cap = pair ? num_sms / 2 : num_sms;
     if (items >= 0x70000000) return DC_ERR_LIMIT;
     const int ctas = (int)(items < cap ? items : cap) * (pair ? 2 : 1);

@@ -455,7 +455,7 @@ def test_product_of_the_longest_rows_and_the_largest_values(m):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("m,k,n,pitch,offset", [(20, 100, 40, 48, 0), (20, 100, 40, 41, 3), (150, 256, 250, 250, 1), (150, 256, 250, 301, 0), (1, 200, 33, 33, 1), (6, 200, 300, 333, 0)])
+@pytest.mark.parametrize("m,k,n,pitch,offset", [(20, 100, 40, 48, 0), (150, 256, 250, 256, 0), (150, 64, 33, 40, 0), (300, 512, 1001, 1008, 0), (20, 100, 40, 41, 3), (150, 256, 250, 250, 1), (150, 256, 250, 301, 0), (1, 200, 33, 33, 1), (6, 200, 300, 333, 0)])
 def test_product_into_strided_and_shifted_rows(m, k, n, pitch, offset, dtype):
     a, sa = random_q(m, k, 1, pitch=(k + 15) // 16 * 16 + 32)
     b, sb = random_q(n, k, 2, pitch=(k + 15) // 16 * 16 + 16)
