@@ -2,7 +2,7 @@
 //
 // What bounds such a layer is its weights, each read once, and the launch; it needs no tensor core.  Every CTA puts the rows into 8 bits itself, into
 // shared memory (about a microsecond, beside a launch and a wait of its own), while its first weights are on their way to L2.  A channel's
-// weights belong to `group` lanes of a warp, 16 values to a lane and step, four steps in flight; a step is one 16-byte load and four dp4a per
+// weights belong to `group` lanes of a warp, 16 values to a lane and step, four or eight steps in flight; a step is one 16-byte load and four dp4a per
 // row of x.  The sums are exact, so they are the same as the other kernels'.
 // us in a graph (us a pass from the host), so and with dc_norm.cu's and dc_quant.cu's kernels: 1 x 1024 x 256 3.2 (3.3) and 3.9 (5.7), 1 x 4096 x 1000
 // 4.2 (4.2) and 5.0 (5.7), 1 x 4096 x 4096 5.4 and 6.6, 1 x 9216 x 4096 11.7 and 11.3; 2 x 2048 x 4096 5.2 (5.0) and 5.2 (6.1), 2 x 4096 x 4096
@@ -108,12 +108,13 @@ __global__ void __launch_bounds__(kFewThreads) k_product_few(const FewArgs a)
         int sum[M];
 #pragma unroll
         for (int r = 0; r < M; ++r) sum[r] = 0;
-        for (int u0 = sub; u0 < a.units; u0 += 4 * group) {
-            int4 w[4];
+        constexpr int U = M == 1 ? 8 : 4;                         // steps in flight
+        for (int u0 = sub; u0 < a.units; u0 += U * group) {
+            int4 w[U];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = u0 + e * group < a.units ? unit_of(row, u0 + e * group, k) : make_int4(0, 0, 0, 0);
+            for (int e = 0; e < U; ++e) w[e] = u0 + e * group < a.units ? unit_of(row, u0 + e * group, k) : make_int4(0, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < U; ++e) {
                 if (u0 + e * group >= a.units) break;
 #pragma unroll
                 for (int r = 0; r < M; ++r) {
