@@ -238,7 +238,9 @@ def test_layers_that_read_the_frame_and_each_other(dtype):
     x = b.add(b.add(a, c), d)
     x = b.conv_quant(x, 40)
     x = b.layer_norm(x)
-    b.conv_quant(x, 16, whole=True)
+    x = b.conv_quant(x, 16, whole=True)
+    x = b.conv_quant(x, 24)                                        # a map of one pixel
+    b.layer_norm(x)
     check_frames(b.layers, 52, 60, 2, dtype, frames_of(52, 60, 4, 2, 3))
 
 
@@ -303,6 +305,33 @@ def test_whole_map_layers_ignore_rectangles():
             assert_near(dc.conv_partial(q, inp, *args), want, bound, "whole map")
     finally:
         dc.close()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [B.DC_FP32, B.DC_BF16])
+def test_frames_from_the_host_have_the_bits_of_those_on_the_device(dtype):
+    """dc_infer_frame_host, with the next frame announced, on a table whose last layer is an 8-bit convolution."""
+    h, w, S = 48, 52, 2
+    b = nets.NetBuilder(h, w)
+    x = b.conv(-1, 32, 3, 1, 1)
+    x = b.layer_norm(x)
+    b.conv_quant(x, 16)
+    weights, biases = nets.random_weights(b.layers, 5)
+    frames = frames_of(h, w, 6, S, 8)
+    a, c = (DeepCache(w, h, b.layers, weights, biases, n_streams=S, block=8, search_range=8, dtype=dtype, expire_n=4) for _ in range(2))
+    try:
+        t = torch.bfloat16 if dtype == B.DC_BF16 else torch.float32
+        pinned = [torch.as_tensor(f).pin_memory() for f in frames]
+        out = torch.empty(a.out_shape(-1), dtype=t).pin_memory()
+        for i, f in enumerate(pinned):
+            want = a.infer_frame(f.cuda())
+            if i + 1 < len(pinned):
+                B.dc_prefetch_frame_host(c.handle, pinned[i + 1].data_ptr(), w * 3)
+            B.dc_infer_frame_host(c.handle, f.data_ptr(), w * 3, out.data_ptr())
+            assert torch.equal(out.cuda(), want), f"frame {i}"
+        assert a.status() == c.status() == B.DC_OK
+    finally:
+        a.close(), c.close()
 
 
 @gpu

@@ -82,7 +82,7 @@ def check_norm(x, gamma, beta, eps=1e-5, y=None):
 
 
 NORM_SHAPES = [(1, 1), (1, 7), (3, 8), (5, 16), (33, 24), (130, 48), (257, 96), (64, 100), (1000, 256), (31, 257), (77, 512), (19, 513), (9, 1000), (50, 1024),
-               (49, 2048), (6, 2049), (5, 4096), (3, 4100), (3, 8192), (2, 8193), (2, 16384), (700, 64), (40000, 32)]
+               (49, 2048), (6, 2049), (5, 4096), (3, 4100), (3, 8192), (2, 8193), (2, 16384), (700, 64), (40000, 32), (70001, 1), (50000, 3), (30000, 17)]
 
 
 @gpu
@@ -114,6 +114,26 @@ def test_norm_of_strided_and_shifted_rows(rows, c, pitch, offset, dtype):
     rest = buf.clone()
     rest[offset:offset + rows * pitch].view(rows, pitch)[:, :c] = 77
     assert (rest == 77).all(), "something beside the rows was written"
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_between_maps_of_different_strides_and_a_part_of_the_statistics(dtype):
+    rows, c = 90, 128
+    x = make_map(rows, c, TYPES[dtype], 1)
+    want, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.dc_layer_norm(x, None, None, want, mean, rstd)
+    for pitch, offset in ((136, 0), (129, 0), (128, 3)):
+        y, _ = spread(torch.zeros_like(x), pitch, offset)
+        m, r = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        check_norm(x, None, None, y=y)
+        B.dc_layer_norm(x, None, None, y, m)
+        B.dc_layer_norm(x, None, None, y, None, r)
+        xs, _ = spread(x, pitch, offset)
+        z = torch.empty_like(x)
+        check_norm(xs, None, None, y=z)
+        if pitch % 8 == 0 and offset == 0:
+            assert torch.equal(y, want) and torch.equal(z, want) and torch.equal(m, mean) and torch.equal(r, rstd)
 
 
 @gpu
@@ -253,9 +273,11 @@ def test_backward_of_strided_rows_and_of_a_part_of_the_gradients(dtype):
     B.dc_layer_norm_backward(dy, x, gamma, mean, rstd, dgamma=g2, workspace=work)
     B.dc_layer_norm_backward(dy, x, gamma, mean, rstd, dbeta=b2, workspace=work)
     assert torch.equal(g2, dg) and torch.equal(b2, db)
-    inplace = dy.clone()
-    B.dc_layer_norm_backward(inplace, x, gamma, mean, rstd, dx=inplace)
-    assert torch.equal(inplace, dx)
+    for k in (0, 1):                                                   # in place: the bits of the same call with an output of its own
+        inplace = [dy.clone(), x.clone()]
+        B.dc_layer_norm_backward(inplace[0], inplace[1], gamma, mean, rstd, dx=only)
+        B.dc_layer_norm_backward(inplace[0], inplace[1], gamma, mean, rstd, dx=inplace[k])
+        assert torch.equal(inplace[k], only) and torch.equal(inplace[1 - k], (x, dy)[k])
 
 
 @gpu
@@ -427,7 +449,7 @@ def check_product(a, sa, b, sb, bias, relu, dtype, out=None):
 
 PRODUCTS = [(1, 1, 1), (1, 16, 8), (1, 300, 77), (1, 4096, 1000), (2, 64, 64), (3, 1000, 130), (7, 128, 256), (8, 2048, 513), (9, 96, 40), (16, 512, 1024), (31, 4096, 200),
             (33, 160, 96), (64, 9216, 512), (100, 31, 33), (127, 129, 127), (128, 128, 128), (129, 257, 65), (200, 384, 1536), (256, 64, 1000), (300, 700, 17), (1000, 256, 64),
-            (5000, 48, 24), (4096, 512, 2048), (4100, 520, 2050), (21952, 64, 256), (40000, 16, 8)]
+            (5000, 48, 24), (1, 64, 100000), (5, 48, 65537), (100352, 16, 8), (17, 131, 4097), (4096, 512, 2048), (4100, 520, 2050), (21952, 64, 256), (40000, 16, 8)]
 
 
 @gpu
