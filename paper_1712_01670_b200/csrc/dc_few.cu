@@ -5,7 +5,7 @@
 // weights belong to `group` lanes of a warp, 16 values to a lane and step, four or eight steps in flight; a step is one 16-byte load and four dp4a per
 // row of x.  The sums are exact, so they are the same as the other kernels'.
 // us in a graph (us a pass from the host), so and with dc_norm.cu's and dc_quant.cu's kernels: 1 x 1024 x 256 3.2 (3.3) and 3.9 (5.7), 1 x 4096 x 1000
-// 4.2 (4.2) and 5.0 (5.7), 1 x 4096 x 4096 5.4 and 6.6, 1 x 9216 x 4096 11.7 and 11.3; 2 x 2048 x 4096 5.2 (5.0) and 5.2 (6.1), 2 x 4096 x 4096
+// 4.2 (4.2) and 5.0 (5.7), 1 x 4096 x 4096 5.3 and 6.6, 1 x 9216 x 4096 11.5 and 11.7, 1 x 16384 x 4096 16.2 and 15.8; 2 x 2048 x 4096 5.2 (5.0) and 5.2 (6.1), 2 x 4096 x 4096
 // 6.7 and 6.7; 4 x 1024 x 256 4.1 (4.2) and 4.0 (5.7), 4 x 4096 x 1000 6.2 and 5.3, 8 x 1024 x 256 4.9 (5.0) and 4.3 (5.8).
 #include "dc_quantise.cuh"
 
@@ -163,12 +163,12 @@ int launch_rows(const FewArgs& a, int threads, size_t per_row, int device, int n
 
 }  // namespace
 
-// Up to 24 MB of weights for one row, 12 for two, 1 for more, whose values are at most 4096 in all: see the figures above.
+// Up to 40 MB of weights for one row, 12 for two, 1 for more, whose values are at most 4096 in all: see the figures above.
 bool dc_few_pays(int64_t m, int n, int k)
 {
     const double weights = (double)n * (double)dc_quant_pitch(k);
     if (dc_quant_pitch(k) * (size_t)(m < 2 ? 1 : 2) > DC_FEW_BYTES) return false;
-    return m == 1 ? weights <= 24e6 : m == 2 ? weights <= 12e6 : m <= 8 && m * k <= 4096 && weights <= 1e6;
+    return m == 1 ? weights <= 40e6 : m == 2 ? weights <= 12e6 : m <= 8 && m * k <= 4096 && weights <= 1e6;
 }
 
 int dc_launch_few(const dc_product_args& p, const void* x, size_t x_pitch, int dtype, int device, int num_sms, cudaStream_t stream)
