@@ -178,6 +178,16 @@ struct dc_once_per_device {
         done[dev] = true;
         return true;
     }
+    // For calls that threads make at the same time without a cache of their own: none passes before the opt-in has been made.
+    template <typename F>
+    cudaError_t ensure(int dev, F opt_in)
+    {
+        const bool kept = dev >= 0 && dev < 64;
+        if (kept && __atomic_load_n(&done[dev], __ATOMIC_ACQUIRE)) return cudaSuccess;
+        const cudaError_t e = opt_in();
+        if (kept && e == cudaSuccess) __atomic_store_n(&done[dev], true, __ATOMIC_RELEASE);
+        return e;
+    }
 };
 
 // Programmatic dependent launch: a kernel launched with dc_launch_pdl may become resident while the previous kernel of

@@ -146,7 +146,7 @@ template <typename T, int VE, int M>
 int launch(const FewArgs& a, int threads, size_t smem, int device, int num_sms, cudaStream_t stream)
 {
     static dc_once_per_device attr_set;
-    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product_few<T, VE, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, DC_FEW_BYTES));
+    DC_CUDA(attr_set.ensure(device, [] { return cudaFuncSetAttribute(k_product_few<T, VE, M>, cudaFuncAttributeMaxDynamicSharedMemorySize, DC_FEW_BYTES); }));
     const int per_cta = threads / 32 * (32 / a.group), want = dc_div_up(a.p.n, per_cta), fit = (int)(DC_FEW_BYTES / (smem + 1024)), cap = num_sms * (fit < 2 ? 1 : 2 * (kFewThreads / threads));
     DC_CUDA(dc_launch_pdl(k_product_few<T, VE, M>, dim3((unsigned)(want < cap ? want : cap)), threads, smem, stream, a));
     return DC_OK;

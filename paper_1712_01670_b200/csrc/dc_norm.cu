@@ -8,6 +8,8 @@
 // registers, by a group of 1 to 32 lanes or by a CTA, and everything that it needs (the mean, the squares around it, the largest value) is
 // reduced among those.  Sums are float32 whatever the map's type; the squares are taken around the mean, not from a sum of squares,
 // which loses what a row with a large mean has left.
+#include <atomic>
+
 #include "dc_quantise.cuh"
 
 namespace {
@@ -51,7 +53,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
     const int nvec = a.channels / VE;
     const float c = (float)a.channels, inv_c = 1.f / c;
     // weights of few channels per lane stay in registers; others come from L1 for every row
-    constexpr bool KEEP = NORM && NV * VE <= 16;
+    constexpr bool KEEP = NORM && NV * VE <= 24;
     F gk[KEEP ? NV : 1][P], bk[KEEP ? NV : 1][P];
     dc_pdl_wait();
     dc_pdl_release();
@@ -370,13 +372,13 @@ Split split_row(int nvec, int most)
 template <typename T, int VE, int NV, int BLOCK, bool NORM, bool QUANT, bool FULL>
 cudaError_t launch_rows_as(const dc_rows_args& a, int group, int threads, int64_t ctas, int num_sms, cudaStream_t stream)
 {
-    static int resident[33];            // CTAs of so many warps that an SM holds
-    int& fit = resident[threads / 32];
+    static std::atomic<int> resident[33];            // CTAs of so many warps that an SM holds
+    int fit = resident[threads / 32].load(std::memory_order_relaxed);
     if (!fit) {
         int n = 0;
         const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, k_rows<T, VE, NV, BLOCK, NORM, QUANT, FULL>, threads, 0);
         if (e != cudaSuccess) return e;
-        fit = n > 0 ? n : 1;
+        resident[threads / 32].store(fit = n > 0 ? n : 1, std::memory_order_relaxed);
     }
     const int64_t cap = (int64_t)num_sms * fit;
     return dc_launch_pdl(k_rows<T, VE, NV, BLOCK, NORM, QUANT, FULL>, dim3((unsigned)(ctas < cap ? ctas : cap)), threads, 0, stream, a, group);
@@ -389,12 +391,12 @@ cudaError_t launch_rows(const dc_rows_args& a, int num_sms, cudaStream_t stream)
 #define DC_ROWS(NV, BLOCK, G, THREADS, CTAS)                                                                                                       return nvec == (NV) * ((BLOCK) ? (THREADS) : (G)) ? launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, true>(a, G, THREADS, CTAS, num_sms, stream)                                                            : launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, false>(a, G, THREADS, CTAS, num_sms, stream)
     // few rows: a CTA for each, a vector per thread
     if (nvec > 32 && nvec <= 1024 && a.rows <= 2 * num_sms) DC_ROWS(1, 1024, 32, dc_div_up(nvec, 32) * 32, a.rows);
-    // Normalised: 16 channels per lane, whose weights stay in its registers (56 x 56 x 256, 32 streams, bf16: 19.3 us, 22.3 with 32).
-    Split s = split_row(nvec, VE == 1 ? 8 : NORM ? 16 / VE : 4);
-    // Longer ones likewise, with a CTA to a row: 12000 x 2048 bf16 20.7 us, 26.5 with a warp; into 8 bits, with its third reduction, 12000 x 768 13.1 and
-    // 11.0, 6000 x 1536 11.3 and 15.0.
+    // Normalised: 16 channels per lane, whose weights stay in its registers (56 x 56 x 256, 32 streams, bf16: 19.3 us, 22.3 with 32), or 24 of bfloat16
+    // where that leaves fewer places idle: 25088 x 384 into 8 bits 10.8 us and 13.8, x 768 17.6 and 21.0 (its weights from L1 before).
+    Split s = split_row(nvec, VE == 1 ? 8 : NORM && VE == 8 ? 3 : 4);
+    // Longer ones likewise, with a CTA to a row: 12000 x 2048 bf16 20.7 us, 26.5 with a warp; into 8 bits 6000 x 1536 11.3 and 15.0.
     if constexpr (NORM && VE == 8)
-        if (s.group == 0 && nvec > (QUANT ? 96 : 64) && nvec <= 1024) DC_ROWS(2, 512, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
+        if (s.group == 0 && nvec <= 1024) DC_ROWS(2, 512, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
     if (s.group == 0) s = split_row(nvec, VE == 1 ? 16 : 4);
     if (s.group == 0 && nvec <= 32 * 8) s = {32, 8};
     if (s.group != 0) {
@@ -442,6 +444,14 @@ cudaError_t launch_backward_as(const dc_backward_args& a, int group, int num_sms
     // with one; from the fourth row on a turn's half microsecond adds up to more than the join).
     const bool alone = want <= 3 && !(BLOCK && teams == 1);
     *ctas = alone ? 1 : (int)(want < 2 ? 2 : want < most ? want : most);
+    if (smem > 48 * 1024 - 1024) {
+        static dc_once_per_device attr_set;
+        int device;
+        cudaError_t e = cudaGetDevice(&device);
+        if (e == cudaSuccess)
+            e = attr_set.ensure(device, [] { return cudaFuncSetAttribute(k_norm_backward<T, VE, NV, BLOCK, THREADS, CTAS, FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize, 128 * 1024); });
+        if (e != cudaSuccess) return e;
+    }
     return dc_launch_pdl(k_norm_backward<T, VE, NV, BLOCK, THREADS, CTAS, FULL>, dim3((unsigned)*ctas), threads, smem, stream, a, group);
 }
 
@@ -451,7 +461,16 @@ template <typename T, int VE>
 cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t stream, int* ctas)
 {
     const int nvec = a.channels / VE;
-    constexpr int N8 = 8 / VE, N16 = 16 / VE, T16 = VE == 8 ? 256 : 384, C16 = VE == 8 ? 2 : 1;
+    constexpr int N8 = 8 / VE, N16 = 16 / VE, T16 = VE == 8 ? 256 : 384, C16 = VE == 8 ? 2 : 1, T24 = VE == 8 ? 384 : 512;
+    if constexpr (VE > 1) {
+        // Three vectors where two leave more places idle: bf16 50000 x 384 24.9 us and 28.4, 25000 x 768 25.2 and 32.9 (as teams of 96 threads), f32
+        // 50000 x 192 22.8 and 26.1, 25000 x 384 23.0 and 25.1.  Their one large CTA starts later: bf16 100 x 384 5.1 us and 4.6, 1000 x 768 6.2 either way.
+        const Split t = split_row(nvec, 3);
+        if (t.nv == 3 && a.rows > 1000) {
+            if (nvec == t.group * 3) return launch_backward_as<T, VE, 3, false, T24, 1, true>(a, t.group, num_sms, stream, ctas);
+            return launch_backward_as<T, VE, 3, false, T24, 1, false>(a, t.group, num_sms, stream, ctas);
+        }
+    }
     Split s = split_row(nvec, VE == 8 ? N16 : N8);
     if (s.group == 0) s = split_row(nvec, N16);
     if (s.group != 0) {
@@ -464,6 +483,22 @@ cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t
         if (full && s.nv == N16) return launch_backward_as<T, VE, N16, false, T16, C16, true>(a, s.group, num_sms, stream, ctas);
         return launch_backward_as<T, VE, N16, false, T16, C16, false>(a, s.group, num_sms, stream, ctas);
     }
+    // Of large maps, longer rows too have two vectors per thread, or three where that takes no more places: bf16 20000 x 1024 26.9 us and 33.5 with one,
+    // 5000 x 4096 29.7 and 34.6, 14000 x 1536 28.7 and 29.8 with two, f32 12000 x 768 22.7 and 25.5 with two; of small ones more threads: bf16
+    // 2000 x 1024 7.5 and 7.4, f32 1500 x 1024 8.4 and 7.2.
+    if constexpr (VE > 1)
+        if (a.rows * a.channels > 1 << 21) {
+            const int two = dc_div_up(dc_div_up(nvec, 2), 32) * 32, three = dc_div_up(dc_div_up(nvec, 3), 32) * 32;
+            if (three <= T24 && 3 * three <= 2 * two) {
+                if (nvec == three * 3) return launch_backward_as<T, VE, 3, true, T24, 1, true>(a, three, num_sms, stream, ctas);
+                return launch_backward_as<T, VE, 3, true, T24, 1, false>(a, three, num_sms, stream, ctas);
+            }
+            if constexpr (VE == 8)
+                if (two <= 512) {
+                    if (nvec == two * 2) return launch_backward_as<T, VE, 2, true, 512, 1, true>(a, two, num_sms, stream, ctas);
+                    return launch_backward_as<T, VE, 2, true, 512, 1, false>(a, two, num_sms, stream, ctas);
+                }
+        }
     const int want = dc_div_up(dc_div_up(nvec, N8), 32) * 32;
     if (want <= 512) {
         if (want * N8 == nvec) return launch_backward_as<T, VE, N8, true, 512, 1, true>(a, want, num_sms, stream, ctas);
@@ -480,11 +515,13 @@ constexpr int64_t kMostRows = DC_MOST_ROWS;
 
 int dc_current_device(int* device, int* num_sms)
 {
-    static int sms[64];
+    static std::atomic<int> sms[64];
     DC_CUDA(cudaGetDevice(device));
     if (*device < 0 || *device >= 64) { DC_CUDA(cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, *device)); return DC_OK; }
-    if (!sms[*device]) DC_CUDA(cudaDeviceGetAttribute(&sms[*device], cudaDevAttrMultiProcessorCount, *device));
-    *num_sms = sms[*device];
+    *num_sms = sms[*device].load(std::memory_order_relaxed);
+    if (*num_sms) return DC_OK;
+    DC_CUDA(cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, *device));
+    sms[*device].store(*num_sms, std::memory_order_relaxed);
     return DC_OK;
 }
 

@@ -605,7 +605,7 @@ template <bool PAIR, bool LIST, bool RELU, typename T>
 int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, const ProductArgs& a, int ctas, int device, cudaStream_t stream)
 {
     static dc_once_per_device attr_set;
-    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product<PAIR, LIST, RELU, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    DC_CUDA(attr_set.ensure(device, [] { return cudaFuncSetAttribute(k_product<PAIR, LIST, RELU, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); }));
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -672,7 +672,7 @@ int launch_split(const dc_product_args& p, const SplitPlan& s, int kc, int devic
     CUtensorMap tmW, tmX;
     if (!encode_rows(&tmW, p.b, p.b_pitch, p.n, p.k, kTileM) || !encode_rows(&tmX, p.a, p.a_pitch, p.m, p.k, s.NT)) return DC_ERR_CUDA;
     static dc_once_per_device attr_set;
-    if (attr_set.first(device)) DC_CUDA(cudaFuncSetAttribute(k_product_split<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+    DC_CUDA(attr_set.ensure(device, [] { return cudaFuncSetAttribute(k_product_split<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024); }));
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)s.CS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;

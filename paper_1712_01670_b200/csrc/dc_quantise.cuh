@@ -81,12 +81,15 @@ template <> struct Vec<__nv_bfloat16, 1> {
     static __device__ __forceinline__ void open(Raw t, float* v) { v[0] = __bfloat162float(t); }
     static __device__ __forceinline__ Raw close(const float* v) { return __float2bfloat16_rn(v[0]); }
 };
-// The larger of m and the bits of a vector's sizes: two bfloat16 side by side, which most_of() joins.
-__device__ __forceinline__ uint32_t raw_most(uint32_t m, uint4 t)
+// The larger of m and the bits of a vector's sizes: two bfloat16 side by side, which most_of() joins.  One instruction for two elements; the
+// sign that it leaves is cut off at the end, and a NaN stays one.  (With a mask and an integer maximum: 13.4 us, not 13.1, for 25088 rows of 512.)
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b)
 {
-    m = __vmaxu2(m, t.x & 0x7fff7fffu); m = __vmaxu2(m, t.y & 0x7fff7fffu);
-    m = __vmaxu2(m, t.z & 0x7fff7fffu); return __vmaxu2(m, t.w & 0x7fff7fffu);
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
+__device__ __forceinline__ uint32_t raw_most(uint32_t m, uint4 t) { return larger2(larger2(larger2(larger2(m, t.x), t.y), t.z), t.w) & 0x7fff7fffu; }
 __device__ __forceinline__ uint32_t raw_most(uint32_t m, float4 t)
 {
     m = max(max(m, size_bits(t.x)), size_bits(t.y));

@@ -252,6 +252,35 @@ def test_backward_of_many_rows_is_the_same_every_time(rows, c):
         assert all(torch.equal(a, b) for a, b in zip(first, again))
 
 
+# three vectors per lane (whole and with places to spare), two or three per thread of longer rows, small and large maps
+@gpu
+@pytest.mark.parametrize("dtype,rows,c", [("bf16", 1001, 24), ("bf16", 1500, 136), ("bf16", 3000, 192), ("bf16", 1111, 384), ("bf16", 2000, 552), ("bf16", 2751, 768),
+                                          ("bf16", 2101, 1000), ("bf16", 2055, 1024), ("bf16", 1400, 1536), ("bf16", 1499, 1480), ("bf16", 400, 8192), ("bf16", 300, 8184),
+                                          ("f32", 1001, 12), ("f32", 3000, 96), ("f32", 1300, 92), ("f32", 1999, 384), ("f32", 2800, 768), ("f32", 2999, 760),
+                                          ("f32", 2222, 1024), ("f32", 600, 6144), ("f32", 400, 6136)])
+def test_backward_of_large_maps(dtype, rows, c):
+    g = gen(5 * rows + c)
+    x, dy = make_map(rows, c, TYPES[dtype], rows + c), torch.randn(rows, c, generator=g, device="cuda").to(TYPES[dtype])
+    gamma = torch.randn(c, generator=g, device="cuda")
+    mean, rstd, *first = check_backward(dy, x, gamma)
+    again = run_backward(dy, x, gamma, mean, rstd)
+    assert all(torch.equal(p, q) for p, q in zip(first, again))
+
+
+@gpu
+@pytest.mark.parametrize("c", [24, 48, 136, 192, 384, 520, 640, 768])
+def test_norm_and_quantise_of_three_vectors_per_lane(c):
+    rows = 1207
+    g = gen(c)
+    x = make_map(rows, c, torch.bfloat16, c)
+    gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+    y = check_norm(x, gamma, beta)
+    q, scale, q2, scale2 = q_like(rows, c), torch.empty(rows, device="cuda"), q_like(rows, c), torch.empty(rows, device="cuda")
+    B.dc_layer_norm_quantize(x, gamma, beta, q, scale)
+    B.dc_quantize_rows(y, q2, scale2)
+    assert torch.equal(q, q2) and torch.equal(scale, scale2)
+
+
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_backward_of_strided_rows_and_of_a_part_of_the_gradients(dtype):
