@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
     const int nvec = a.channels / VE;
     const float c = (float)a.channels, inv_c = 1.f / c;
     // weights of few channels per lane stay in registers; others come from L1 for every row
-    constexpr bool KEEP = NORM && NV * VE <= 24;
+    constexpr bool KEEP = NORM && NV * VE <= (VE == 8 && BLOCK == 0 ? 32 : 16);
     F gk[KEEP ? NV : 1][P], bk[KEEP ? NV : 1][P];
     dc_pdl_wait();
     dc_pdl_release();
@@ -394,9 +394,11 @@ cudaError_t launch_rows(const dc_rows_args& a, int num_sms, cudaStream_t stream)
     // Normalised: 16 channels per lane, whose weights stay in its registers (56 x 56 x 256, 32 streams, bf16: 19.3 us, 22.3 with 32), or 24 of bfloat16
     // where that leaves fewer places idle: 25088 x 384 into 8 bits 10.8 us and 13.8, x 768 17.6 and 21.0 (its weights from L1 before).
     Split s = split_row(nvec, VE == 1 ? 8 : NORM && VE == 8 ? 3 : 4);
-    // Longer ones likewise, with a CTA to a row: 12000 x 2048 bf16 20.7 us, 26.5 with a warp; into 8 bits 6000 x 1536 11.3 and 15.0.
+    // Longer ones likewise, with a CTA to a row: 12000 x 2048 bf16 20.7 us, 26.5 with a warp; into 8 bits 6000 x 1536 11.3 and 15.0.  Four vectors for
+    // every lane of a warp need no barriers and just fit: 25088 x 1024 into 8 bits 21.7 us and 24.7, 25000 x 1024 19.2 and 20.4; with places idle
+    // (25088 x 1000 26.6 and 25.5) or fewer than four rows to a resident warp (5000 x 1024 5.4 and 5.2) the CTA is better.
     if constexpr (NORM && VE == 8)
-        if (s.group == 0 && nvec <= 1024) DC_ROWS(2, 512, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
+        if (s.group == 0 && nvec <= 1024 && !(nvec == 4 * 32 && a.rows >= 64 * num_sms)) DC_ROWS(2, 512, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
     if (s.group == 0) s = split_row(nvec, VE == 1 ? 16 : 4);
     if (s.group == 0 && nvec <= 32 * 8) s = {32, 8};
     if (s.group != 0) {

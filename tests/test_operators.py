@@ -268,9 +268,8 @@ def test_backward_of_large_maps(dtype, rows, c):
 
 
 @gpu
-@pytest.mark.parametrize("c", [24, 48, 136, 192, 384, 520, 640, 768])
-def test_norm_and_quantise_of_three_vectors_per_lane(c):
-    rows = 1207
+@pytest.mark.parametrize("rows,c", [(1207, 24), (1207, 48), (1207, 136), (1207, 192), (1207, 384), (1207, 520), (1207, 640), (1207, 768), (9601, 1024), (6001, 1024), (9601, 1000)])
+def test_norm_and_quantise_of_three_and_four_vectors_per_lane(rows, c):
     g = gen(c)
     x = make_map(rows, c, torch.bfloat16, c)
     gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
