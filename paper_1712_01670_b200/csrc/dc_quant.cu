@@ -10,6 +10,8 @@
 // buffered in tensor memory, so that the sixteen warps that scale and store a tile work beside the MMAs of the next.  Large products run on
 // CTA pairs: 256 rows x 256 columns, each CTA loading its own 128 rows of a and half of b's, which is a third less traffic from L2 per
 // product than a CTA alone has.
+#include <atomic>
+
 #include "dc_rows.cuh"
 #include "dc_tcgen05.cuh"
 
@@ -569,11 +571,12 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
                              CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 EncodeFn encode_fn()
 {
-    static EncodeFn fn = nullptr;
+    static std::atomic<EncodeFn> known;
+    EncodeFn fn = known.load(std::memory_order_relaxed);
     if (!fn) {
         void* p = nullptr;
         cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) fn = (EncodeFn)p;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) known.store(fn = (EncodeFn)p, std::memory_order_relaxed);
         cudaGetLastError();
     }
     return fn;
@@ -622,9 +625,10 @@ int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtenso
 // Clusters of so many CTAs, each with an SM of its own, that the device holds at once.
 int clusters_at_once(int cs, int device)
 {
-    static int known[64][4];
+    static std::atomic<int> known[64][4];
     const int at = cs == 1 ? 0 : cs == 2 ? 1 : cs == 4 ? 2 : 3;
-    if (device >= 0 && device < 64 && known[device][at]) return known[device][at];
+    if (device >= 0 && device < 64)
+        if (const int n = known[device][at].load(std::memory_order_relaxed)) return n;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
@@ -634,7 +638,7 @@ int clusters_at_once(int cs, int device)
     if (cudaFuncSetAttribute(k_product_split<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess ||
         cudaOccupancyMaxActiveClusters(&n, k_product_split<float>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
     if (n < 1) n = 1;
-    if (device >= 0 && device < 64) known[device][at] = n;
+    if (device >= 0 && device < 64) known[device][at].store(n, std::memory_order_relaxed);
     return n;
 }
 

@@ -789,6 +789,51 @@ print("the same")
 """
 
 
+FIRST_CALLS_OF_THREADS = """
+import threading
+import torch
+from paper_1712_01670_b200 import binding as B
+N = 6
+x = torch.randn(2100, 768, device="cuda").bfloat16()
+w, s = torch.randint(-127, 128, (512, 768), device="cuda").to(torch.int8), torch.rand(512, device="cuda")
+mean, rstd = x.float().mean(1), 1 / x.float().std(1)
+bufs = [[torch.empty(n, dtype=torch.uint8, device="cuda") for n in (1 << 22, B.dc_layer_norm_workspace(768))] +
+        [torch.empty(m, 512, device="cuda").bfloat16() for m in (1, 30, 2100)] + [torch.empty_like(x), torch.empty(768, device="cuda"), torch.empty(768, device="cuda")] for _ in range(N)]
+streams = [torch.cuda.Stream() for _ in range(N)]
+torch.cuda.synchronize()
+gate, failed = threading.Barrier(N), []
+def run(i):
+    try:
+        work, partial, one, few, many, dx, dg, db = bufs[i]
+        gate.wait()
+        with torch.cuda.stream(streams[i]):
+            B.dc_linear_quantized(x[:1], w, s, None, one, True, work)
+            B.dc_linear_quantized(x[:30], w, s, None, few, True, work)
+            B.dc_linear_quantized(x, w, s, None, many, True, work)
+            B.dc_layer_norm_backward(x, x, None, mean, rstd, dx, dg, db, partial)
+    except Exception as e:
+        failed.append(repr(e))
+threads = [threading.Thread(target=run, args=(i,)) for i in range(N)]
+for t in threads: t.start()
+for t in threads: t.join()
+torch.cuda.synchronize()
+assert not failed, failed
+assert all(torch.equal(p, q) for b in bufs[1:] for p, q in zip(bufs[0][2:], b[2:]))
+assert torch.equal(bufs[0][4][:1], bufs[0][2]) and torch.equal(bufs[0][4][:30], bufs[0][3])
+print("the same")
+"""
+
+
+@gpu
+def test_the_first_calls_of_a_process_from_several_threads():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS_OF_THREADS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "the same" in r.stdout, r.stdout + r.stderr
+
+
 @gpu
 def test_the_first_call_of_a_process_inside_a_capture():
     import os
