@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
     dc_pdl_release();
     int parity = 0;
     const float c = (float)a.channels, inv_c = 1.f / c;
-    for (int row = blockIdx.x; row < (int)a.rows; row += gridDim.x, parity ^= 1) {
+    for (int row = blockIdx.x; row < (int)a.rows; row += gridDim.x) {
         if (QUANT && !NORM && !wanted(a, row)) continue;
         float* const slot = red + parity * 96;
         const T* const x = (const T*)row_at(a.x, a.x_pitch, row);
@@ -200,6 +200,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
                 a.q[(size_t)qr * a.q_pitch + i] = (int8_t)w;
             }
         }
+        parity ^= 1;                    // rows that are passed over reduce nothing and take no turn: two neighbouring reductions would meet in one slot
     }
 }
 

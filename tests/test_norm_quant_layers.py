@@ -290,6 +290,43 @@ def test_partial_convolution_with_a_callers_rectangles(h, w, cin, cout, S, dtype
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [B.DC_FP32, B.DC_BF16])
+def test_partial_convolution_of_rows_longer_than_registers(dtype):
+    """Rows of more channels than a CTA holds, read one by one, behind 4 lines of a caller's rectangles each: of the rows that a CTA takes
+    (296 apart on 148 SMs, which is 4 lines of 74 pixels) every second one is reused.  A row's largest value is reduced in a slot of shared memory that the
+    CTA's next row but one uses again."""
+    t = torch.bfloat16 if dtype == B.DC_BF16 else torch.float32
+    h, w, cin, cout, S = 20, 74, 8200, 16, 2
+    b = nets.NetBuilder(h, w)
+    q = b.conv_quant(b.conv(-1, cin, 1), cout)
+    weights, biases = nets.random_weights(b.layers, 3)
+    dc = DeepCache(w, h, b.layers, weights, biases, n_streams=S, block=8, dtype=dtype, max_regions=4)
+    try:
+        g = torch.Generator(device="cuda")
+        g.manual_seed(8)
+        inp = torch.empty(S * h * w * cin + 1, dtype=t, device="cuda")[1:].view(S, h, w, cin)      # not 16-byte aligned: single elements
+        inp.copy_(torch.randn(S, h, w, cin, generator=g, device="cuda") * torch.exp(2 * torch.randn(S, h, w, 1, generator=g, device="cuda")))
+        prev = torch.randn(S, h, w, cout, generator=g, device="cuda").to(t)
+        regs = torch.zeros(S, 4, 6, dtype=torch.int32, device="cuda")
+        for k, y in enumerate((4, 12)):
+            regs[:, k] = torch.tensor((0, y, w, 4, 0, y), dtype=torch.int32)
+        n = torch.full((S,), 2, dtype=torch.int32, device="cuda")
+        fresh = torch.ones(S, h, w, dtype=torch.bool, device="cuda")
+        fresh[:, 4:8] = fresh[:, 12:16] = False
+        want, bound = quant_layer64(inp, b.layers[q], weights[q], biases[q])
+        first = None
+        for _ in range(10):
+            got = dc.conv_partial(q, inp, prev, regs, n)
+            assert_near(got[fresh], want[fresh], bound[fresh], "computed pixels")
+            assert torch.equal(got[~fresh], prev[~fresh])
+            first = got.clone() if first is None else first
+            assert torch.equal(got, first)
+        assert dc.status() == B.DC_OK
+    finally:
+        dc.close()
+
+
+@gpu
 def test_whole_map_layers_ignore_rectangles():
     b = nets.NetBuilder(6, 5)
     q = b.conv_quant(-1, 32, relu=0, whole=True)
