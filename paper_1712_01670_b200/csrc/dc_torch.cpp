@@ -1,7 +1,7 @@
 // Torch tensors to the entry points of libdeepcache that take a caller's own maps (dc_layer_norm and on): the module _tensors, which
 // binding.py wraps.  These calls are short - a few microseconds on the GPU - and the same marshalling in Python and ctypes took longer than
 // that (a normalisation into 8 bits and the product behind it, 196 x 384 x 1536: 15.3 us a pass, 6.1 so; gradients of 196 x 1024: 15.7
-// and 9.1).  Argument marshalling only: addresses, pitches, types, the device and its current stream.
+// and 9.2).  Argument marshalling only: addresses, pitches, types, the device and its current stream.  As in ctypes, the GIL is not held during the call itself.
 #include <Python.h>
 
 #include <c10/cuda/CUDAGuard.h>
@@ -104,6 +104,12 @@ int truth(PyObject* o)
     if (v < 0) throw Refused{nullptr, ""};
     return v;
 }
+// The GIL is not held during the library's call: a launch waits where the stream's queue is full, and what the stream waits for may be another
+// Python thread.  Everything that may run Python comes before it.  (0.1 us a call: 196 x 1024 gradients 9.2 us a pass, 8.9 with the GIL held.)
+struct WithoutGil {
+    PyThreadState* const state = PyEval_SaveThread();
+    ~WithoutGil() { PyEval_RestoreThread(state); }
+};
 int32_t channels_of(const Rows& r) { return r.channels > INT32_MAX ? INT32_MAX : (int32_t)r.channels; }
 
 int layer_norm(PyObject* const* o)       // x, gamma, beta, y, mean, rstd, eps, stream
@@ -114,8 +120,10 @@ int layer_norm(PyObject* const* o)       // x, gamma, beta, y, mean, rstd, eps, 
     same(xr, yr, "y");
     const float *g = vector_of(gamma, xr.channels, "gamma"), *b = vector_of(beta, xr.channels, "beta");
     float *m = vector_of(mean, xr.rows, "mean"), *r = vector_of(rstd, xr.rows, "rstd");
+    const double eps = number(o[6]);
     const Place p("dc_layer_norm", {x, y, gamma, beta, mean, rstd}, o[7]);
-    return dc_layer_norm(xr.at, xr.pitch, g, b, xr.rows, channels_of(xr), number(o[6]), xr.dtype, yr.at, yr.pitch, m, r, p.stream);
+    const WithoutGil call;
+    return dc_layer_norm(xr.at, xr.pitch, g, b, xr.rows, channels_of(xr), eps, xr.dtype, yr.at, yr.pitch, m, r, p.stream);
 }
 
 int layer_norm_backward(PyObject* const* o)      // dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream
@@ -130,6 +138,7 @@ int layer_norm_backward(PyObject* const* o)      // dy, x, gamma, mean, rstd, dx
     const float *g = vector_of(gamma, xr.channels, "gamma"), *m = vector_of(mean, xr.rows, "mean", false), *r = vector_of(rstd, xr.rows, "rstd", false);
     float *dg = vector_of(dgamma, xr.channels, "dgamma"), *db = vector_of(dbeta, xr.channels, "dbeta");
     const Place p("dc_layer_norm_backward", {x, dy, gamma, mean, rstd, dx, dgamma, dbeta, work}, o[9]);
+    const WithoutGil call;
     return dc_layer_norm_backward(dr.at, dr.pitch, xr.at, xr.pitch, g, m, r, xr.rows, channels_of(xr), xr.dtype, ox.at, ox.pitch, dg, db, work ? work->data_ptr() : nullptr,
                                   work ? work->nbytes() : 0, p.stream);
 }
@@ -141,6 +150,7 @@ int quantize_rows(PyObject* const* o)    // x, q, scale, stream
     same(xr, qr, "q", false);
     float* s = vector_of(scale, xr.rows, "scale");
     const Place p("dc_quantize_rows", {x, q, scale}, o[3]);
+    const WithoutGil call;
     return dc_quantize_rows(xr.at, xr.pitch, xr.rows, channels_of(xr), xr.dtype, (int8_t*)qr.at, qr.pitch, s, p.stream);
 }
 
@@ -154,8 +164,10 @@ int layer_norm_quantize(PyObject* const* o)      // x, gamma, beta, q, scale, y,
     if (y) { yr = rows_of(*y, "y"); same(xr, yr, "y"); }
     const float *g = vector_of(gamma, xr.channels, "gamma"), *b = vector_of(beta, xr.channels, "beta");
     float* s = vector_of(scale, xr.rows, "scale");
+    const double eps = number(o[6]);
     const Place p("dc_layer_norm_quantize", {x, q, scale, gamma, beta, y}, o[7]);
-    return dc_layer_norm_quantize(xr.at, xr.pitch, g, b, xr.rows, channels_of(xr), number(o[6]), xr.dtype, yr.at, yr.pitch, (int8_t*)qr.at, qr.pitch, s, p.stream);
+    const WithoutGil call;
+    return dc_layer_norm_quantize(xr.at, xr.pitch, g, b, xr.rows, channels_of(xr), eps, xr.dtype, yr.at, yr.pitch, (int8_t*)qr.at, qr.pitch, s, p.stream);
 }
 
 void fit(const Rows& a, const Rows& b, const Rows& out)
@@ -173,8 +185,10 @@ int matmul_quantized(PyObject* const* o)         // a, a_scale, b, b_scale, bias
     const Rows ar = rows_of(*a, "a", true), br = rows_of(*b, "b", true), r = rows_of(*out, "out");
     fit(ar, br, r);
     const float *sa = vector_of(as, ar.rows, "a_scale", false), *sb = vector_of(bs, br.rows, "b_scale", false), *c = vector_of(bias, br.rows, "bias");
+    const int relu = truth(o[6]);
     const Place p("dc_matmul_quantized", {a, b, as, bs, bias, out}, o[7]);
-    return dc_matmul_quantized((const int8_t*)ar.at, ar.pitch, sa, (const int8_t*)br.at, br.pitch, sb, c, ar.rows, (int32_t)br.rows, channels_of(ar), truth(o[6]), r.dtype, r.at, r.pitch,
+    const WithoutGil call;
+    return dc_matmul_quantized((const int8_t*)ar.at, ar.pitch, sa, (const int8_t*)br.at, br.pitch, sb, c, ar.rows, (int32_t)br.rows, channels_of(ar), relu, r.dtype, r.at, r.pitch,
                                p.stream);
 }
 
@@ -187,8 +201,10 @@ int linear_quantized(PyObject* const* o)         // x, w, w_scale, bias, out, re
     if (xr.dtype != r.dtype) throw Refused{PyExc_TypeError, "x and out differ in type"};
     if (work && !work->is_contiguous()) throw Refused{PyExc_ValueError, "workspace: has to be contiguous"};
     const float *sw = vector_of(ws, wr.rows, "w_scale", false), *c = vector_of(bias, wr.rows, "bias");
+    const int relu = truth(o[5]);
     const Place p("dc_linear_quantized", {x, w, ws, bias, out, work}, o[7]);
-    return dc_linear_quantized(xr.at, xr.pitch, (const int8_t*)wr.at, wr.pitch, sw, c, xr.rows, (int32_t)wr.rows, channels_of(xr), truth(o[5]), xr.dtype, r.at, r.pitch,
+    const WithoutGil call;
+    return dc_linear_quantized(xr.at, xr.pitch, (const int8_t*)wr.at, wr.pitch, sw, c, xr.rows, (int32_t)wr.rows, channels_of(xr), relu, xr.dtype, r.at, r.pitch,
                                work ? work->data_ptr() : nullptr, work ? work->nbytes() : 0, p.stream);
 }
 

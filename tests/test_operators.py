@@ -845,6 +845,48 @@ def test_the_first_call_of_a_process_inside_a_capture():
 
 
 @gpu
+def test_other_python_threads_run_during_a_call():
+    """With no forced switches between threads, another thread can only have run between two calls if a call gave it the interpreter."""
+    import sys
+    import threading
+    import time
+    rows, c = 40, 64
+    x = make_map(rows, c, torch.float32, 1)
+    y, dx, q, s, out, work = torch.empty_like(x), torch.empty_like(x), q_like(rows, c), torch.empty(rows, device="cuda"), torch.empty(rows, 8, device="cuda"), scratch(1 << 20)
+    w, ws = random_q(8, c, 2)
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    calls = [lambda: B.dc_layer_norm(x, None, None, y), lambda: B.dc_layer_norm_backward(x, x, None, mean, rstd, dx), lambda: B.dc_quantize_rows(x, q, s),
+             lambda: B.dc_layer_norm_quantize(x, None, None, q, s), lambda: B.dc_matmul_quantized(q, s, w, ws, None, out),
+             lambda: B.dc_linear_quantized(x, w, ws, None, out, False, work)]
+    turns, stop, before = [0], [], sys.getswitchinterval()
+
+    def other():
+        while not stop:
+            turns[0] += 1
+            time.sleep(0)                                              # hands the interpreter back
+
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    sys.setswitchinterval(100.0)
+    thread = threading.Thread(target=other)
+    try:
+        thread.start()
+        seen = []
+        for call in calls:
+            t = turns[0]
+            for _ in range(1000):
+                call()
+            seen.append(turns[0] - t)
+    finally:
+        stop.append(1)
+        sys.setswitchinterval(before)
+        thread.join()
+    torch.cuda.synchronize()
+    assert min(seen) > 0, seen
+
+
+@gpu
 def test_nothing_is_done_with_no_rows():
     x = torch.empty(0, 32, device="cuda")
     w, s = random_q(8, 32, 1)
