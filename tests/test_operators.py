@@ -834,6 +834,72 @@ def test_the_first_calls_of_a_process_from_several_threads():
     assert r.returncode == 0 and "the same" in r.stdout, r.stdout + r.stderr
 
 
+FIRST_C_CALLS_OF_THREADS = """
+import ctypes as C
+import threading
+import time
+import torch
+from paper_1712_01670_b200 import binding as B
+N, K, M = 6, 768, 2100
+L = B.load()
+xs = [torch.randn(M, K, device="cuda"), torch.randn(M, K, device="cuda").bfloat16()]
+w, s = torch.randint(-127, 128, (512, K), device="cuda").to(torch.int8), torch.rand(512, device="cuda")
+stats = [(x.float().mean(1), 1 / x.float().std(1)) for x in xs]
+def buffers():
+    per_type = [[torch.empty(m, 512, device="cuda").to(x.dtype) for m in (1, 30, 300, M) for relu in (0, 1)] + [torch.empty_like(x), torch.empty(K, device="cuda"), torch.empty(K, device="cuda")] for x in xs]
+    return [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (1 << 22, B.dc_layer_norm_workspace(K))], per_type
+def calls_of(bufs, stream):                    # arguments made beforehand: a thread only calls
+    (work, partial), per_type = bufs
+    st, got = stream.cuda_stream, []
+    for dtype, x, (mean, rstd), outs in zip((B.DC_FP32, B.DC_BF16), xs, stats, per_type):
+        pitch, out_pitch = K * x.element_size(), 512 * x.element_size()
+        for i, m in enumerate((1, 30, 300, M)):
+            for relu in (0, 1):
+                got.append((L.dc_linear_quantized, (x.data_ptr(), pitch, w.data_ptr(), K, s.data_ptr(), None, m, 512, K, relu, dtype, outs[2 * i + relu].data_ptr(), out_pitch,
+                                                    work.data_ptr(), 1 << 22, st)))
+        got.append((L.dc_layer_norm_backward, (x.data_ptr(), pitch, x.data_ptr(), pitch, None, mean.data_ptr(), rstd.data_ptr(), M, K, dtype, outs[8].data_ptr(), pitch,
+                                               outs[9].data_ptr(), outs[10].data_ptr(), partial.data_ptr(), partial.numel(), st)))
+    return got
+bufs = [buffers() for _ in range(N)]
+streams = [torch.cuda.Stream() for _ in range(N)]
+todo = [calls_of(b, t) for b, t in zip(bufs, streams)]
+torch.cuda.synchronize()
+gate, at, codes = threading.Barrier(N), [[] for _ in range(N)], [[] for _ in range(N)]
+def run(i):
+    for f, a in todo[i]:
+        gate.wait()
+        t = time.perf_counter_ns()
+        codes[i].append(f(*a))
+        at[i].append((t, time.perf_counter_ns()))
+threads = [threading.Thread(target=run, args=(i,)) for i in range(N)]
+for t in threads: t.start()
+for t in threads: t.join()
+torch.cuda.synchronize()
+assert all(c == [0] * len(todo[0]) for c in codes), codes
+at_once = sum(any(p is not q and max(p[0], q[0]) < min(p[1], q[1]) for p in spans for q in spans) for spans in zip(*at))
+assert at_once > len(todo[0]) // 2, f"of {len(todo[0])} calls only {at_once} were made by two threads at once"
+outs = [[t for p in b[1] for t in p] for b in bufs]
+assert all(torch.equal(p, q) for o in outs[1:] for p, q in zip(outs[0], o))
+again = [t.clone() for t in outs[0]]
+for f, a in todo[0]:
+    assert f(*a) == 0
+torch.cuda.synchronize()
+assert all(torch.equal(p, q) for p, q in zip(again, outs[0]))
+print("the same")
+"""
+
+
+@gpu
+def test_the_first_c_calls_of_a_process_overlap():
+    """Through the C ABI, which holds no lock: the first calls of several threads are in the library at the same time, all succeed and agree."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_C_CALLS_OF_THREADS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "the same" in r.stdout, r.stdout + r.stderr
+
+
 @gpu
 def test_the_first_call_of_a_process_inside_a_capture():
     import os
