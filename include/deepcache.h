@@ -327,7 +327,8 @@ int dc_search_blocks_noalloc(const uint8_t* frame_dev, const uint8_t* prev_dev, 
  * and pitches are aligned to an element; 16-byte aligned ones, with rows of whole 16 bytes, are the fast case.  dtype is the map's
  * (DC_FP32, DC_BF16); sums, means and scales are float32 or wider.  Zero rows: DC_OK, nothing is done.  Nothing is allocated, and the work is enqueued on cuda_stream
  * (a cudaStream_t of the current device); the calls may be captured into a graph and may overlap, unless they share memory that one of them
- * writes.  Results do not depend on what runs beside them.  Errors: DC_ERR_ARG, DC_ERR_CONFIG (dtype), DC_ERR_LIMIT (more than 0x7ff00000 rows, a
+ * writes.  Results do not depend on what runs beside them.  What a call writes lies apart from what it reads and from what else it writes, but for what the
+ * call says.  Errors: DC_ERR_ARG, DC_ERR_CONFIG (dtype), DC_ERR_LIMIT (more than 0x7ff00000 rows, a
  * pitch of 4 GB or more between rows, and what the call says), DC_ERR_CUDA. */
 
 /* Layer normalisation over the channels of each row:
@@ -361,7 +362,8 @@ int dc_layer_norm_workspace(int32_t channels, size_t* bytes);
 int dc_quantize_rows(const void* x_dev, size_t x_pitch, int64_t rows, int32_t channels, int32_t dtype,
                      int8_t* q_dev, size_t q_pitch, float* scale_dev, void* cuda_stream);
 
-/* dc_layer_norm and dc_quantize_rows of its output in one pass: the same bits as the two calls one after the other.  y_dev may be NULL. */
+/* dc_layer_norm and dc_quantize_rows of its output in one pass: the same bits as the two calls one after the other.  y_dev may be NULL, or x_dev with the same
+ * pitch. */
 int dc_layer_norm_quantize(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t rows, int32_t channels,
                            double eps, int32_t dtype, void* y_dev, size_t y_pitch, int8_t* q_dev, size_t q_pitch, float* scale_dev,
                            void* cuda_stream);
@@ -377,8 +379,8 @@ int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scal
                         void* out_dev, size_t out_pitch, void* cuda_stream);
 
 /* A whole layer: the rows of x [m][k] (dtype) into 8 bits, then the product with weights w: the same bits as dc_quantize_rows and
- * dc_matmul_quantized.  workspace_dev: dc_linear_workspace bytes, any alignment; its content does not matter before or after the call; two calls that may overlap
- * need one each. */
+ * dc_matmul_quantized.  out_dev may lie over x_dev, with any pitch.  workspace_dev: dc_linear_workspace bytes, any alignment, apart from all else; its content does
+ * not matter before or after the call; two calls that may overlap need one each. */
 int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, size_t w_pitch, const float* w_scale_dev,
                         const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
                         void* out_dev, size_t out_pitch, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);

@@ -760,6 +760,16 @@ static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, 
     return DC_OK;
 }
 
+// Do the rows of two maps share no memory?  (false too where that is not seen at once: stretches that cross, of different pitches.)
+static bool rows_apart(uintptr_t a, size_t a_pitch, size_t a_row, uintptr_t b, size_t b_pitch, size_t b_row, int64_t rows)
+{
+    const size_t before = (size_t)(rows - 1);
+    if (b >= a + before * a_pitch + a_row || a >= b + before * b_pitch + b_row) return true;
+    if (a_pitch != b_pitch || rows < 2) return false;
+    const size_t d = b >= a ? (b - a) % a_pitch : (a_pitch - (a - b) % a_pitch) % a_pitch;      // columns of one buffer
+    return d >= a_row && d + b_row <= a_pitch;
+}
+
 extern "C" {
 
 int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const int8_t* b_dev, size_t b_pitch, const float* b_scale_dev, const float* bias_dev,
@@ -798,7 +808,8 @@ int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, 
     dc_product_args p = {};
     p.b = w_dev; p.b_pitch = w_pitch; p.b_scale = w_scale_dev; p.bias = bias_dev;
     p.m = m; p.n = n; p.k = k; p.relu = relu; p.out = out_dev; p.out_pitch = out_pitch;
-    if (dc_few_pays(m, n, k)) return dc_launch_few(p, x_dev, x_pitch, dtype, device, sms, (cudaStream_t)cuda_stream);
+    // one launch writes out while other CTAs still read x: where they may share memory, x is put into the workspace first
+    if (dc_few_pays(m, n, k) && rows_apart((uintptr_t)x_dev, x_pitch, (size_t)k * elt, (uintptr_t)out_dev, out_pitch, (size_t)n * elt, m)) return dc_launch_few(p, x_dev, x_pitch, dtype, device, sms, (cudaStream_t)cuda_stream);
     const size_t pitch = dc_quant_pitch(k);
     int8_t* const q = (int8_t*)(((uintptr_t)workspace_dev + 255) & ~(uintptr_t)255);
     float* const scale = (float*)(q + (size_t)m * pitch);

@@ -578,6 +578,33 @@ def test_linear_of_one_row_and_of_a_few_short_ones(m, k, n, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", [(1, 1024, 1024), (1, 4096, 4096), (1, 512, 9000), (1, 9000, 64), (2, 2048, 2048), (4, 1024, 256), (8, 512, 512), (64, 512, 512)])
+def test_linear_over_its_own_input(m, k, n, dtype):
+    """out over x, at its start, beginning in its middle and one element in front of it: the bits of an output apart."""
+    t = TYPES[dtype]
+    wide = max(k, n)
+    wq, ws = random_q(n, k, 5)
+    bias = torch.randn(n, generator=gen(6), device="cuda")
+    work = scratch(B.dc_linear_workspace(m, k))
+    data = make_map(m, k, t, m + n)
+    want = torch.empty(m, n, dtype=t, device="cuda")
+    B.dc_linear_quantized(data, wq, ws, bias, want, True, work)
+    buf = torch.empty(3 * m * wide + 64, dtype=t, device="cuda")
+    x = buf[m * wide:2 * m * wide].view(m, wide)[:, :k]
+    for offset in (0, wide // 2, -1, wide - n, -m * wide + 8):
+        for _ in range(5):
+            x.copy_(data)
+            out = buf[m * wide + offset:2 * m * wide + offset].view(m, wide)[:, :n]
+            B.dc_linear_quantized(x, wq, ws, bias, out, True, work)
+            assert torch.equal(out, want), offset
+    x, out = buf[:m * (k + n)].view(m, k + n).split([k, n], 1)         # columns of one buffer: apart
+    x.copy_(data)
+    B.dc_linear_quantized(x, wq, ws, bias, out, True, work)
+    assert torch.equal(out, want) and torch.equal(x, data)
+
+
+@gpu
 @pytest.mark.parametrize("k,n", [(20000, 33), (25088, 256), (70000, 16)])
 def test_linear_of_long_rows(k, n):
     for m in (1, 3, 33):
