@@ -362,8 +362,9 @@ int dc_layer_norm_workspace(int32_t channels, size_t* bytes);
 int dc_quantize_rows(const void* x_dev, size_t x_pitch, int64_t rows, int32_t channels, int32_t dtype,
                      int8_t* q_dev, size_t q_pitch, float* scale_dev, void* cuda_stream);
 
-/* dc_layer_norm and dc_quantize_rows of its output in one pass: the same bits as the two calls one after the other.  y_dev may be NULL, or x_dev with the same
- * pitch. */
+/* dc_layer_norm and dc_quantize_rows of its output in one pass.  y_dev may be NULL, or x_dev with the same pitch.  The same bits as the two calls one after
+ * the other, if y_dev and y_pitch are multiples of 16 in both or in neither (NULL counts as a multiple): rows that are not 16-byte aligned are added
+ * up in another order, so the last bit of a mean may differ, and with it a value's rounding to the map's type. */
 int dc_layer_norm_quantize(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t rows, int32_t channels,
                            double eps, int32_t dtype, void* y_dev, size_t y_pitch, int8_t* q_dev, size_t q_pitch, float* scale_dev,
                            void* cuda_stream);

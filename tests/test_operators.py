@@ -448,6 +448,29 @@ def test_norm_and_quantise_in_one_pass_has_the_bits_of_two(rows, c, dtype):
     assert torch.equal(q, q1) and torch.equal(q, q2) and torch.equal(bits(scale), bits(s1)) and torch.equal(bits(scale), bits(s2))
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(900, 64), (400, 512), (50, 2048), (700, 1000)])
+def test_norm_and_quantise_with_an_output_that_is_not_aligned(rows, c, dtype):
+    """The bits of the two calls where the map between them is aligned in both or in neither; else each within its bound, and its steps exact."""
+    t, g = TYPES[dtype], gen(c)
+    x = make_map(rows, c, t, rows)
+    gamma, beta = torch.randn(c, generator=g, device="cuda"), torch.randn(c, generator=g, device="cuda")
+    outs = [spread(torch.zeros_like(x), pitch, offset)[0] for pitch, offset in ((c, 0), (c + 1, 0), (c, 1), (c + 8, 3))]
+    done = []
+    for y in outs:
+        check_norm(x, gamma, beta, y=y)
+        q, s, q1, s1, y1 = q_like(rows, c), torch.empty(rows, device="cuda"), q_like(rows, c), torch.empty(rows, device="cuda"), spread(torch.zeros_like(x), y.stride(0), y.storage_offset())[0]
+        B.dc_quantize_rows(y, q, s)
+        B.dc_layer_norm_quantize(x, gamma, beta, q1, s1, y1)
+        wq, ws = quantise64(y)
+        assert torch.equal(y, y1) and torch.equal(q, q1) and torch.equal(s, s1) and torch.equal(q, wq) and torch.equal(s, ws)
+        done.append((q, s))
+    q, s = q_like(rows, c), torch.empty(rows, device="cuda")
+    B.dc_layer_norm_quantize(x, gamma, beta, q, s)
+    assert torch.equal(q, done[0][0]) and torch.equal(s, done[0][1])
+
+
 # ---------------------------------------------------------------------------
 # products
 # ---------------------------------------------------------------------------
