@@ -329,7 +329,8 @@ int dc_search_blocks_noalloc(const uint8_t* frame_dev, const uint8_t* prev_dev, 
  * (a cudaStream_t of the current device); the calls may be captured into a graph and may overlap, unless they share memory that one of them
  * writes.  Results do not depend on what runs beside them.  What a call writes lies apart from what it reads and from what else it writes, but for what the
  * call says.  Errors: DC_ERR_ARG, DC_ERR_CONFIG (dtype), DC_ERR_LIMIT (more than 0x7ff00000 rows, a
- * pitch of 4 GB or more between rows, and what the call says), DC_ERR_CUDA. */
+ * pitch of 4 GB or more between rows - of operands in 8 bits 1 TB, of out_dev any - and what the call says), DC_ERR_CUDA.  With a single row its pitch is
+ * not looked at, but for its alignment. */
 
 /* Layer normalisation over the channels of each row:
  *   mean = sum x / C, rstd = 1 / sqrt(sum (x - mean)^2 / C + eps), y = (x - mean) rstd gamma + beta

@@ -587,7 +587,7 @@ bool encode_rows(CUtensorMap* tm, const void* base, size_t pitch, int64_t rows, 
 {
     EncodeFn enc = encode_fn();
     if (!enc) return false;
-    if (rows < 2 && pitch < dc_quant_pitch(k)) pitch = dc_quant_pitch(k);      // a single row's pitch is anything
+    if (rows < 2) pitch = dc_quant_pitch(k);                                   // a single row's is anything
     const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
     const cuuint32_t box[2] = {(cuuint32_t)kBytesK, (cuuint32_t)box_rows}, elem[2] = {1, 1};
     return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -746,6 +746,7 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
 }
 
 constexpr int kMostTerms = 131071;
+constexpr size_t kMostPitch = ((size_t)1 << 40) - 16;          // of operands: what a tensor map takes
 
 // What both products ask of their operands.
 static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, const float* bias, int64_t m, int32_t n, int32_t k, int32_t dtype, const void* out, size_t out_pitch)
@@ -753,7 +754,7 @@ static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, 
     if (dtype != DC_FP32 && dtype != DC_BF16) return DC_ERR_CONFIG;
     const int elt = dtype == DC_BF16 ? 2 : 4;
     if (m < 0 || n < 1 || k < 1) return DC_ERR_ARG;
-    if (k > kMostTerms || m > DC_MOST_ROWS || n > (1 << 28)) return DC_ERR_LIMIT;
+    if (k > kMostTerms || m > DC_MOST_ROWS || n > (1 << 28) || (n > 1 && b_pitch > kMostPitch)) return DC_ERR_LIMIT;
     if (m == 0) return DC_OK;
     if (!b || !b_scale || !out || (uintptr_t)b % 16 || b_pitch % 16 || (n > 1 && b_pitch < (size_t)k)) return DC_ERR_ARG;
     if ((uintptr_t)b_scale % 4 || (uintptr_t)bias % 4 || (uintptr_t)out % elt || out_pitch % elt || (m > 1 && out_pitch < (size_t)n * elt)) return DC_ERR_ARG;
@@ -777,6 +778,7 @@ int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scal
 {
     int rc = product_check(b_dev, b_pitch, b_scale_dev, bias_dev, m, n, k, dtype, out_dev, out_pitch);
     if (rc != DC_OK || m == 0) return rc;
+    if (m > 1 && a_pitch > kMostPitch) return DC_ERR_LIMIT;
     if (!a_dev || !a_scale_dev || (uintptr_t)a_dev % 16 || a_pitch % 16 || (m > 1 && a_pitch < (size_t)k) || (uintptr_t)a_scale_dev % 4) return DC_ERR_ARG;
     int device = 0, sms = 0;
     if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;

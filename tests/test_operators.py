@@ -540,6 +540,43 @@ def test_product_into_strided_and_shifted_rows(m, k, n, pitch, offset, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("pitch", [0, 16, 1 << 32, 1 << 41, (1 << 63) - 16])
+def test_a_single_row_has_any_pitch(pitch):
+    L, st = B.load(), torch.cuda.current_stream().cuda_stream
+    for m, k, n in ((1, 300, 5), (1, 300, 1), (200, 300, 1), (1, 4096, 40000)):
+        (a, sa), (b, sb) = random_q(m, k, 1), random_q(n, k, 2)
+        want, got = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+        B.dc_matmul_quantized(a, sa, b, sb, None, want)
+        assert L.dc_matmul_quantized(a.data_ptr(), pitch if m == 1 else a.stride(0), sa.data_ptr(), b.data_ptr(), pitch if n == 1 else b.stride(0), sb.data_ptr(), None,
+                                     m, n, k, 0, B.DC_FP32, got.data_ptr(), pitch if m == 1 else 4 * n, st) == B.DC_OK
+        assert torch.equal(got, want)
+    x, y, want, q, wq, s, ws = *(torch.empty(1, 300, device="cuda") for _ in range(3)), q_like(1, 300), q_like(1, 300), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    x.copy_(make_map(1, 300, torch.float32, 4))
+    B.dc_layer_norm(x, None, None, want)
+    B.dc_quantize_rows(x, wq, ws)
+    assert L.dc_layer_norm(x.data_ptr(), pitch, None, None, 1, 300, 1e-5, B.DC_FP32, y.data_ptr(), pitch, None, None, st) == B.DC_OK
+    assert L.dc_quantize_rows(x.data_ptr(), pitch, 1, 300, B.DC_FP32, q.data_ptr(), pitch, s.data_ptr(), st) == B.DC_OK
+    assert torch.equal(y, want) and torch.equal(q, wq) and torch.equal(s, ws)
+
+
+@gpu
+def test_product_of_rows_far_apart():
+    """Rows of either side and of the output more than 4 GB apart."""
+    k, pitch = 96, (1 << 32) + 16
+    buf = torch.empty(2 * pitch + 4 * k, dtype=torch.int8, device="cuda")
+    far = buf.as_strided((3, k), (pitch, 1))
+    near, sn = random_q(3, k, 1)
+    far.copy_(near)
+    for rows in (40, 300):
+        other, so = random_q(rows, k, 2)
+        for a, sa, b, sb, c in ((far, sn, other, so, near), (other, so, far, sn, other)):
+            assert torch.equal(check_product(a, sa, b, sb, None, False, torch.float32), check_product(c, sa, near if b is far else b, sb, None, False, torch.float32))
+    out = torch.empty(2 * (pitch // 4) + 64, device="cuda").as_strided((3, 64), (pitch // 4, 1))
+    b, sb = random_q(64, k, 3)
+    check_product(near, sn, b, sb, None, True, torch.float32, out=out)
+
+
+@gpu
 @pytest.mark.parametrize("m", [1, 6, 64, 700])
 @pytest.mark.parametrize("relu", [False, True])
 def test_linear_has_the_bits_of_its_two_steps_and_keeps_what_is_not_finite_to_its_row(m, relu):
@@ -1115,6 +1152,12 @@ ODD1 = C.c_void_p((1 << 20) + 1)
 ])
 def test_refusals(name, kw, status):
     assert call(name, **kw) == status
+
+
+@pytest.mark.parametrize("name,kw", [("dc_matmul_quantized", dict(rows=2, qp=1 << 40)), ("dc_matmul_quantized", dict(rows=2, wp=1 << 40)), ("dc_matmul_quantized", dict(rows=1, wp=1 << 60)),
+                                     ("dc_linear_quantized", dict(rows=1, wp=1 << 40))])
+def test_operands_too_far_apart_are_refused(name, kw):
+    assert call(name, **kw) == B.DC_ERR_LIMIT
 
 
 def test_workspaces():
