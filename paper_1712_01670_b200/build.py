@@ -40,6 +40,19 @@ def tensors_command():
             "-L", libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L", _HERE, "-ldeepcache", "-Wl,-rpath,$ORIGIN"]
 
 
+def tensors_lack() -> str:
+    """What ``_tensors.so`` needs beside nvcc and is not there, or an empty text."""
+    import importlib.util
+    import shutil
+    import sysconfig
+    if importlib.util.find_spec("torch") is None:
+        return "torch"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python's headers"
+    cxx = os.environ.get("CXX", "g++")
+    return "" if shutil.which(cxx) else f"the C++ compiler {cxx}"
+
+
 def build_tensors(force: bool = False) -> str:
     deps = [os.path.join(CSRC, "dc_torch.cpp"), os.path.join(INCLUDE, "deepcache.h")]
     if force or not os.path.exists(TENSORS) or any(os.path.getmtime(d) > os.path.getmtime(TENSORS) for d in deps):
@@ -48,8 +61,14 @@ def build_tensors(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    """Both libraries.  The C library needs nvcc alone; where what the binding to torch tensors needs is not there, it is left out and that is
+    said, and its calls say so in their turn."""
     build_library(force, verbose)
-    build_tensors(force)
+    lack = tensors_lack()
+    if lack:
+        print(f"{os.path.basename(TENSORS)} is not built: {lack} is missing")
+    else:
+        build_tensors(force)
     return LIB
 
 

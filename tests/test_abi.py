@@ -2,6 +2,7 @@
 import ctypes
 import os
 import re
+import sys
 
 import pytest
 
@@ -60,3 +61,21 @@ def test_engine_refuses_to_run_without_cuda():
     from paper_1712_01670_b200.synth import configs
     with pytest.raises(RuntimeError):
         DeepCache.from_workload(configs.WORKLOADS[1]())
+
+
+def test_the_c_library_builds_without_a_cxx_compiler(monkeypatch, tmp_path, capsys):
+    """What the binding to torch tensors needs beside nvcc is no condition of the C library; its absence is said."""
+    monkeypatch.setattr(build, "TENSORS", str(tmp_path / "_tensors.so"))
+    monkeypatch.setenv("CXX", str(tmp_path / "no-such-compiler"))
+    assert build.build() == build.LIB and os.path.exists(build.LIB)
+    assert "no-such-compiler is missing" in capsys.readouterr().out and not os.path.exists(build.TENSORS)
+
+
+def test_the_c_library_builds_without_torch(monkeypatch, tmp_path, capsys):
+    import importlib.util
+    found = importlib.util.find_spec
+    monkeypatch.setattr(build, "TENSORS", str(tmp_path / "_tensors.so"))
+    monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: None if name == "torch" else found(name, *a))
+    monkeypatch.setitem(sys.modules, "torch", None)                   # an import of it fails
+    assert build.build() == build.LIB
+    assert "torch is missing" in capsys.readouterr().out
