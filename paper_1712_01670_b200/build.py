@@ -27,6 +27,13 @@ def stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _torch_and_python() -> str:
+    """What ``_tensors.so`` is made for.  It holds this text itself, so that it is made anew when one of the two changes."""
+    import sys
+    import torch
+    return f"_tensors for torch {torch.__version__}, python {sys.version_info.major}.{sys.version_info.minor}"
+
+
 def tensors_command():
     """How ``_tensors.so`` is made: torch's own headers and libraries, libdeepcache found beside it."""
     import sysconfig
@@ -36,8 +43,19 @@ def tensors_command():
     includes = [sysconfig.get_paths()["include"], INCLUDE, *cpp_extension.include_paths(), os.path.join(cuda, "include")]
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     return [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+            f'-DDC_BUILT_FOR="{_torch_and_python()}"',
             *(f for i in includes for f in ("-isystem" if "torch" in i else "-I", i)), os.path.join(CSRC, "dc_torch.cpp"), "-o", TENSORS,
             "-L", libs, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L", _HERE, "-ldeepcache", "-Wl,-rpath,$ORIGIN"]
+
+
+def tensors_stale() -> bool:
+    if not os.path.exists(TENSORS):
+        return True
+    t = os.path.getmtime(TENSORS)
+    if any(os.path.getmtime(d) > t for d in (os.path.join(CSRC, "dc_torch.cpp"), os.path.join(INCLUDE, "deepcache.h"))):
+        return True
+    with open(TENSORS, "rb") as f:
+        return _torch_and_python().encode() + b"\0" not in f.read()
 
 
 def tensors_lack() -> str:
@@ -54,8 +72,7 @@ def tensors_lack() -> str:
 
 
 def build_tensors(force: bool = False) -> str:
-    deps = [os.path.join(CSRC, "dc_torch.cpp"), os.path.join(INCLUDE, "deepcache.h")]
-    if force or not os.path.exists(TENSORS) or any(os.path.getmtime(d) > os.path.getmtime(TENSORS) for d in deps):
+    if force or tensors_stale():
         subprocess.check_call(tensors_command())
     return TENSORS
 

@@ -228,7 +228,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 #define DC_ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {DC_ENTRY(layer_norm, 8), DC_ENTRY(layer_norm_backward, 10), DC_ENTRY(quantize_rows, 4), DC_ENTRY(layer_norm_quantize, 8),
                           DC_ENTRY(matmul_quantized, 8), DC_ENTRY(linear_quantized, 8), {nullptr, nullptr, 0, nullptr}};
-PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_tensors", "Torch tensors to libdeepcache's entry points on maps of the caller's own.", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_tensors", "Torch tensors to libdeepcache's entry points on maps of the caller's own.  " DC_BUILT_FOR, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 

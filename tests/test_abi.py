@@ -79,3 +79,12 @@ def test_the_c_library_builds_without_torch(monkeypatch, tmp_path, capsys):
     monkeypatch.setitem(sys.modules, "torch", None)                   # an import of it fails
     assert build.build() == build.LIB
     assert "torch is missing" in capsys.readouterr().out
+
+
+def test_the_binding_to_tensors_is_made_anew_for_another_torch(monkeypatch):
+    import torch
+    build.build()
+    assert not build.tensors_stale()
+    monkeypatch.setattr(torch, "__version__", torch.__version__ + ".1")
+    assert build.tensors_stale()
+    assert any(torch.__version__ in a for a in build.tensors_command())
