@@ -385,48 +385,64 @@ cudaError_t launch_rows_as(const dc_rows_args& a, int group, int threads, int64_
     return dc_launch_pdl(k_rows<T, VE, NV, BLOCK, NORM, QUANT, FULL>, dim3((unsigned)(ctas < cap ? ctas : cap)), threads, 0, stream, a, group);
 }
 
+// PART: rows that leave places idle come here too.
+template <typename T, int VE, int NV, int BLOCK, bool NORM, bool QUANT, bool PART>
+cudaError_t launch_rows_of(const dc_rows_args& a, int group, int threads, int64_t ctas, int num_sms, cudaStream_t stream)
+{
+    if constexpr (PART)
+        if (a.channels / VE != NV * (BLOCK ? threads : group)) return launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, false>(a, group, threads, ctas, num_sms, stream);
+    return launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, true>(a, group, threads, ctas, num_sms, stream);
+}
+
 template <typename T, int VE, bool NORM, bool QUANT>
 cudaError_t launch_rows(const dc_rows_args& a, int num_sms, cudaStream_t stream)
 {
     const int nvec = a.channels / VE;
-#define DC_ROWS(NV, BLOCK, G, THREADS, CTAS)                                                                                                       return nvec == (NV) * ((BLOCK) ? (THREADS) : (G)) ? launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, true>(a, G, THREADS, CTAS, num_sms, stream)                                                            : launch_rows_as<T, VE, NV, BLOCK, NORM, QUANT, false>(a, G, THREADS, CTAS, num_sms, stream)
+    constexpr bool NORM8 = NORM && VE == 8;
+#define DC_ROWS(NV, BLOCK, PART, G, THREADS, CTAS) return launch_rows_of<T, VE, NV, BLOCK, NORM, QUANT, (PART)>(a, G, THREADS, CTAS, num_sms, stream)
     // few rows: a CTA for each, a vector per thread
-    if (nvec > 32 && nvec <= 1024 && a.rows <= 2 * num_sms) DC_ROWS(1, 1024, 32, dc_div_up(nvec, 32) * 32, a.rows);
+    if (nvec > 32 && nvec <= 1024 && a.rows <= 2 * num_sms) DC_ROWS(1, 1024, true, 32, dc_div_up(nvec, 32) * 32, a.rows);
     // Normalised: 16 channels per lane, whose weights stay in its registers (56 x 56 x 256, 32 streams, bf16: 19.3 us, 22.3 with 32), or 24 of bfloat16
     // where that leaves fewer places idle: 25088 x 384 into 8 bits 10.8 us and 13.8, x 768 17.6 and 21.0 (its weights from L1 before).
-    Split s = split_row(nvec, VE == 1 ? 8 : NORM && VE == 8 ? 3 : 4);
+    constexpr int MOST = VE == 1 ? 8 : NORM8 ? 3 : 4;
+    Split s = split_row(nvec, MOST);
     // Longer ones likewise, with a CTA to a row: 12000 x 2048 bf16 20.7 us, 26.5 with a warp; into 8 bits 6000 x 1536 11.3 and 15.0.  Four vectors for
     // every lane of a warp need no barriers and just fit: 25088 x 1024 into 8 bits 21.7 us and 24.7, 25000 x 1024 19.2 and 20.4; with places idle
     // (25088 x 1000 26.6 and 25.5) or fewer than four rows to a resident warp (5000 x 1024 5.4 and 5.2) the CTA is better.
-    if constexpr (NORM && VE == 8)
-        if (s.group == 0 && nvec <= 1024 && !(nvec == 4 * 32 && a.rows >= 64 * num_sms)) DC_ROWS(2, 512, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
+    if constexpr (NORM8)
+        if (s.group == 0 && nvec <= 1024 && !(nvec == 4 * 32 && a.rows >= 64 * num_sms)) DC_ROWS(2, 512, true, 32, dc_div_up(dc_div_up(nvec, 2), 32) * 32, a.rows);
     if (s.group == 0) s = split_row(nvec, VE == 1 ? 16 : 4);
-    if (s.group == 0 && nvec <= 32 * 8) s = {32, 8};
+    if constexpr (VE > 1 && !NORM8) if (s.group == 0 && nvec <= 32 * 8) s = {32, 8};
     if (s.group != 0) {
         const int64_t warps = (a.rows + 32 / s.group - 1) / (32 / s.group);
         const int per_cta = warps >= 8 * (int64_t)num_sms ? 8 : warps >= 4 * (int64_t)num_sms ? 4 : warps >= 2 * (int64_t)num_sms ? 2 : 1;
         const int64_t ctas = (warps + per_cta - 1) / per_cta;
+        // With places idle no count is split_row's choice whose double is within its limit: half the lanes then have as few places in all.
         switch (s.nv) {
-        case 1: DC_ROWS(1, 0, s.group, per_cta * 32, ctas);
-        case 2: DC_ROWS(2, 0, s.group, per_cta * 32, ctas);
-        case 3: DC_ROWS(3, 0, s.group, per_cta * 32, ctas);
-        case 4: DC_ROWS(4, 0, s.group, per_cta * 32, ctas);
-        case 5: case 6: case 7: case 8: DC_ROWS(8, 0, s.group, per_cta * 32, ctas);
-        default:
-            if constexpr (VE == 1) {
-                if (s.nv <= 12) DC_ROWS(12, 0, s.group, per_cta * 32, ctas);
-                DC_ROWS(16, 0, s.group, per_cta * 32, ctas);
-            }
+        case 1: DC_ROWS(1, 0, false, s.group, per_cta * 32, ctas);
+        case 2: DC_ROWS(2, 0, 2 * 2 > MOST, s.group, per_cta * 32, ctas);
+        case 3: DC_ROWS(3, 0, 2 * 3 > MOST, s.group, per_cta * 32, ctas);
+        case 4: DC_ROWS(4, 0, 2 * 4 > MOST && !NORM8, s.group, per_cta * 32, ctas);        // (NORM8: see above)
         }
+        if constexpr (VE == 1) {
+            if (s.nv > 12) DC_ROWS(16, 0, true, s.group, per_cta * 32, ctas);
+            if (s.nv > 8) DC_ROWS(12, 0, true, s.group, per_cta * 32, ctas);
+        }
+        if constexpr (!NORM8) DC_ROWS(8, 0, true, s.group, per_cta * 32, ctas);
     }
-    if constexpr (VE == 1) if (nvec <= 512 * 12) DC_ROWS(12, 512, 32, dc_div_up(dc_div_up(nvec, 12), 32) * 32, a.rows);
-    // a CTA per row: as many threads as leave each four vectors, up to 1024
-    const int want = dc_div_up(dc_div_up(nvec, 4), 32) * 32, threads = want < 128 ? 128 : want > 1024 ? 1024 : want;
-    if (threads <= 512) DC_ROWS(4, 512, 32, threads, a.rows);
-    if (nvec <= 4096) DC_ROWS(4, 1024, 32, threads, a.rows);
-    if constexpr (VE < 8) if (nvec <= 8192) DC_ROWS(8, 1024, 32, threads, a.rows);
+    // a CTA per row: as many threads as leave each four vectors (single elements: 12), up to 1024; normalised rows end at kMostNormChannels
+    if constexpr (VE == 1) {
+        if (nvec <= 512 * 12) DC_ROWS(12, 512, true, 32, dc_div_up(dc_div_up(nvec, 12), 32) * 32, a.rows);
+        if (nvec <= 8192) DC_ROWS(8, 1024, true, 32, 1024, a.rows);
+    } else {
+        const int want = dc_div_up(dc_div_up(nvec, 4), 32) * 32, threads = want < 128 ? 128 : want > 1024 ? 1024 : want;
+        if (threads <= 512) DC_ROWS(4, 512, true, 32, threads, a.rows);
+        if constexpr (!NORM8) if (nvec <= 4096) DC_ROWS(4, 1024, true, 32, threads, a.rows);
+        if constexpr (VE == 4 && !NORM) if (nvec <= 8192) DC_ROWS(8, 1024, true, 32, threads, a.rows);
+    }
 #undef DC_ROWS
-    return dc_launch_pdl(k_rows_long<T, NORM, QUANT>, dim3((unsigned)(a.rows < 2 * num_sms ? a.rows : 2 * num_sms)), 1024, 0, stream, a);
+    if constexpr (NORM && VE > 1) return cudaErrorInvalidValue;       // (no row is that long)
+    else return dc_launch_pdl(k_rows_long<T, NORM, QUANT>, dim3((unsigned)(a.rows < 2 * num_sms ? a.rows : 2 * num_sms)), 1024, 0, stream, a);
 }
 
 template <typename T, int VE>
@@ -479,8 +495,9 @@ cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t
     if (s.group != 0) {
         const bool full = nvec == s.group * s.nv;
         if (s.nv <= N8) {
-            if (full && s.nv == N8) return launch_backward_as<T, VE, N8, false, 320, 2, true>(a, s.group, num_sms, stream, ctas);
-            return launch_backward_as<T, VE, N8, false, 320, 2, false>(a, s.group, num_sms, stream, ctas);
+            if constexpr (N8 > 1)                                 // (a single vector per lane leaves no place idle)
+                if (!full || s.nv != N8) return launch_backward_as<T, VE, N8, false, 320, 2, false>(a, s.group, num_sms, stream, ctas);
+            return launch_backward_as<T, VE, N8, false, 320, 2, true>(a, s.group, num_sms, stream, ctas);
         }
         if constexpr (VE == 1) if (s.nv <= 12) return launch_backward_as<T, VE, 12, false, 256, 2, false>(a, s.group, num_sms, stream, ctas);
         if (full && s.nv == N16) return launch_backward_as<T, VE, N16, false, T16, C16, true>(a, s.group, num_sms, stream, ctas);
