@@ -163,12 +163,14 @@ int launch_rows(const FewArgs& a, int threads, size_t per_row, int device, int n
 
 }  // namespace
 
-// Up to 40 MB of weights for one row, 12 for two, 1 for more, whose values are at most 4096 in all: see the figures above.
+// Up to 52 MB of weights for one row, 12 for two, 1 for more, whose values are at most 4096 in all.  bf16, us in a graph, so and with the two launches: one row of
+// 4096 channels out 9.3 and 11.1 at 34 MB, 11.3 and 12.3 at 42, 12.0 and 12.4 at 46, 13.0 and 13.2 at 50, 13.9 and 13.6 at 55, 14.4 and 14.3 at 59, 16.3 and 15.6 at 67, 23.8 and 21.0 at 103;
+// longer rows meet there too (16384 x 3584, 59 MB, 14.9 and 14.6), shorter ones later (4096 x 16384, 67 MB, 13.9 and 21.7); two rows 6.2 and 7.2 at 10 MB, 8.4 and 8.0 at 14.
 bool dc_few_pays(int64_t m, int n, int k)
 {
     const double weights = (double)n * (double)dc_quant_pitch(k);
     if (dc_quant_pitch(k) * (size_t)(m < 2 ? 1 : 2) > DC_FEW_BYTES) return false;
-    return m == 1 ? weights <= 40e6 : m == 2 ? weights <= 12e6 : m <= 8 && m * k <= 4096 && weights <= 1e6;
+    return m == 1 ? weights <= 52e6 : m == 2 ? weights <= 12e6 : m <= 8 && m * k <= 4096 && weights <= 1e6;
 }
 
 int dc_launch_few(const dc_product_args& p, const void* x, size_t x_pitch, int dtype, int device, int num_sms, cudaStream_t stream)

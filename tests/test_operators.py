@@ -638,6 +638,19 @@ def test_linear_of_one_row_and_of_a_few_short_ones(m, k, n, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("m,k,n", [(1, 12688, 4098), (1, 12704, 4094), (1, 12704, 4090), (2, 2928, 4098), (2, 2944, 4077)])
+def test_linear_on_either_side_of_the_single_launch(m, k, n):
+    """Weights just above and just below what the single launch takes: the bits of the two steps."""
+    x = make_map(m, k, torch.bfloat16, 2)
+    wq, ws = random_q(n, k, 3)
+    q, s, want, got = q_like(m, k), torch.empty(m, device="cuda"), torch.empty(m, n, dtype=torch.bfloat16, device="cuda"), torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    B.dc_quantize_rows(x, q, s)
+    B.dc_matmul_quantized(q, s, wq, ws, None, want)
+    B.dc_linear_quantized(x, wq, ws, None, got, False, scratch(B.dc_linear_workspace(m, k)))
+    assert torch.equal(got, want)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,k,n", [(1, 1024, 1024), (1, 4096, 4096), (1, 512, 9000), (1, 9000, 64), (2, 2048, 2048), (4, 1024, 256), (8, 512, 512), (64, 512, 512)])
 def test_linear_over_its_own_input(m, k, n, dtype):
