@@ -246,6 +246,49 @@ def test_layers_that_read_the_frame_and_each_other(dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [B.DC_FP32, B.DC_BF16])
+def test_layers_that_read_the_resized_frame(dtype):
+    """A normalisation and an 8-bit convolution that read the frame behind an area resize, with an ordinary convolution beside them."""
+    b = nets.NetBuilder(80, 96)
+    r = b.resize_area(-1, 40, 48)
+    n = b.layer_norm(r)
+    x = b.add(b.conv_quant(n, 24), b.conv_quant(r, 24, relu=0))
+    x = b.add(x, b.conv(r, 24, 3, 1, 1))
+    b.conv_quant(b.layer_norm(x), 16)
+    g = rng(6)
+    big = np.kron(g.integers(0, 256, size=(2, 30, 34, 3)), np.ones((1, 4, 4, 1))).astype(np.uint8)
+    frames = [big[:, 4 * t:4 * t + 80, 8 * t:8 * t + 96].copy() for t in range(4)]
+    layers, weights, biases = b.layers, *nets.random_weights(b.layers, 5)
+    dc = DeepCache(96, 80, layers, weights, biases, n_streams=2, block=8, search_range=8, dtype=dtype, expire_n=4)
+    prev, reused_any = {}, 0.0
+    try:
+        for t, f in enumerate(frames):
+            _, stats = dc.infer_frame(torch.as_tensor(f).cuda(), want_stats=True)
+            maps = [dc.layer_map(i) for i in range(len(layers))]
+            for i, l in enumerate(layers):
+                what = f"frame {t} layer {i}"
+                if l["kind"] == nets.KIND_LAYER_NORM:
+                    assert_near(maps[i], *norm_layer64(maps[l["in0"]], weights[i], biases[i], 1e-5), what)
+                elif l["kind"] == nets.KIND_CONV_QUANT:
+                    want, bound = quant_layer64(maps[l["in0"]], l, weights[i], biases[i])
+                    fresh = torch.ones(2, l["out_h"], l["out_w"], dtype=torch.bool, device="cuda")
+                    if not stats[0].refreshed:
+                        regs, n_regs = dc.layer_regions(i)
+                        for s in range(2):
+                            for x0, y0, rw, rh, sx, sy in regs[s, :int(n_regs[s])].cpu().tolist():
+                                if rw > 0:
+                                    assert torch.equal(maps[i][s, y0:y0 + rh, x0:x0 + rw], prev[i][s, sy:sy + rh, sx:sx + rw]), what
+                                    fresh[s, y0:y0 + rh, x0:x0 + rw] = False
+                    reused_any += 1 - float(fresh.double().mean())
+                    assert_near(maps[i][fresh], want[fresh], bound[fresh], what)
+            prev = dict(enumerate(maps))
+            assert dc.status() == B.DC_OK
+        assert reused_any > 0, "no pixel was reused: the test's frames do not match"
+    finally:
+        dc.close()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [B.DC_FP32, B.DC_BF16])
 @pytest.mark.parametrize("h,w,cin,cout,S", [(33, 45, 24, 40, 2), (16, 24, 64, 256, 4), (7, 7, 512, 128, 3)])
 def test_partial_convolution_with_a_callers_rectangles(h, w, cin, cout, S, dtype):
     """dc_conv_partial on an 8-bit layer: a caller's maps and rectangles, a whole map, and a bad rectangle."""
