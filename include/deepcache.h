@@ -373,7 +373,8 @@ int dc_layer_norm_quantize(const void* x_dev, size_t x_pitch, const float* gamma
 /* out[r][j] = relu(a_scale[r] b_scale[j] sum over k of a[r][k] b[j][k] + bias[j]): the product of two matrices of 8-bit rows.
  *   a_dev int8 [m][a_pitch], b_dev int8 [n][b_pitch] (weights: one row per output channel): 16-byte aligned, pitches multiples of 16;
  *   nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
- * The sums are exact (int32); scales, bias and ReLU (which leaves a NaN) are applied in float32, with one rounding to dtype.  Every wait inside the
+ * The sums are exact (int32); a_scale, b_scale, bias and ReLU (which leaves a NaN) are applied in float32, in this order, with one rounding to dtype: a
+ * sum that a_scale takes beyond float32's range stays infinite, whatever b_scale is.  Every wait inside the
  * kernels is bounded; should one run out (2 s), the results that it concerns are NaN.
  * DC_ERR_LIMIT: k > 131071 (a sum could pass 32 bits), n > 2^28. */
 int dc_matmul_quantized(const int8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const int8_t* b_dev, size_t b_pitch,

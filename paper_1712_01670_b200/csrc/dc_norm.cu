@@ -519,6 +519,7 @@ cudaError_t launch_backward(const dc_backward_args& a, int num_sms, cudaStream_t
                     return launch_backward_as<T, VE, 2, true, 512, 1, false>(a, two, num_sms, stream, ctas);
                 }
         }
+    // Beyond 512 threads there are 64 registers for each, too few for a row ahead and the sums: 40 to 230 bytes a thread spill up to 8192 channels, 810 to 910 beyond.
     const int want = dc_div_up(dc_div_up(nvec, N8), 32) * 32;
     if (want <= 512) {
         if (want * N8 == nvec) return launch_backward_as<T, VE, N8, true, 512, 1, true>(a, want, num_sms, stream, ctas);

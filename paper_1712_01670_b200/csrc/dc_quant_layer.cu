@@ -3,7 +3,8 @@
 // A pointwise 8-bit convolution is a partial convolution like any other: its pixels in rectangles come from the cached map, tiles without a
 // pixel left are not in the list, and of the others only the rest is computed.  Its input's rows in 8 bits lie in lines of a multiple of
 // eight pixels, so that a flat tile (16 groups of 8 pixels of one line) is 128 rows one behind another whatever the map's width, and one box
-// of a TMA load.  Rows of reused pixels are not put into 8 bits.
+// of a TMA load.  Rows of reused pixels are not put into 8 bits, but where the layer normalisation in front writes the rows: it normalises every pixel and puts every one
+// into 8 bits.
 #include "dc_rows.cuh"
 
 namespace {

@@ -146,8 +146,8 @@ __device__ __forceinline__ V reduce(V v, int group, V* slot)
     return reduce_lanes<Op>(t, 32);
 }
 
-// s / c by the reciprocal of c and a correction of the remainder: half a step, as the division, at a third of its instructions.  (An
-// infinite s gives NaN.)
+// s / c by the reciprocal of c and one correction by the remainder, which a fused multiply-add has exactly (Markstein 1990): half a step, as the division, at a
+// third of its instructions.  (An infinite s gives NaN.)
 __device__ __forceinline__ float over(float s, float c, float inv_c)
 {
     const float q = s * inv_c;

@@ -19,7 +19,7 @@ struct dc_rows_args {
     int width, padded;
     const uint32_t* masks;              // of such pixels, those that are not wanted: a bit for each row of q, 128 to a tile; or NULL
 };
-// norm: false: the rows are quantised as they are.  *launches counts the kernels.
+// norm: false: the rows are quantised as they are.  One kernel.
 int dc_launch_rows(const dc_rows_args& a, bool norm, int dtype, int num_sms, cudaStream_t stream);
 
 // out[r][j] = relu(a_scale[r] * b_scale[j] * sum_k a[r][k] b[j][k] + bias[j])
