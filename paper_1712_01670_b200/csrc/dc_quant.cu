@@ -408,6 +408,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
 // With the rows put into 8 bits, us, in turns with k_product's 64 CTAs that walk K alone: 1 x 9216 x 4096 11.3 and 27.7, 32 x 25088 x 4096 23.1
 // and 45.9, 100 x 4096 x 1000 7.6 and 11.3; 196 x 1024 x 512 7.2 and 6.1.
 constexpr int kSplitThreads = 192, kSplitStages = 12;
+// A CTA of it waits for its cluster, and tensor memory is given out without a limit on the wait.  So it may not share an SM with a kernel of another stream that takes all 512
+// columns and waits for other CTAs too (the convolutions on CTA pairs, which leave up to 48 KB of shared memory): each could hold what the other's
+// cluster is waiting for.  It takes at least this much; what fits beside it then, and it itself twice or three times, have columns for all.
+constexpr size_t kSplitLeast = 64 * 1024;
 struct SplitArgs {
     dc_product_args p;
     int NT, CS, stages, stage_bytes, kchunks, k_last, m_tiles, early;     // NT: rows of x in a tile
@@ -684,7 +688,8 @@ int launch_split(const dc_product_args& p, const SplitPlan& s, int kc, int devic
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.m_tiles * dc_div_up(p.n, kTileM) * s.CS)); cfg.blockDim = dim3(kSplitThreads);
-    cfg.dynamicSmemBytes = (size_t)a.stages * a.stage_bytes + fixed; cfg.stream = stream;
+    const size_t smem = (size_t)a.stages * a.stage_bytes + fixed;
+    cfg.dynamicSmemBytes = smem > kSplitLeast ? smem : kSplitLeast; cfg.stream = stream;
     cfg.attrs = attr; cfg.numAttrs = g_dc_pdl ? 2 : 1;
     DC_CUDA(cudaLaunchKernelEx(&cfg, k_product_split<T>, tmW, tmX, a));
     return DC_OK;

@@ -436,3 +436,50 @@ def test_epsilon_is_set_and_empties_the_cache():
                 dc.set_norm_epsilon(layer, eps)
     finally:
         dc.close()
+
+
+@gpu
+def test_products_beside_an_inference_on_cta_pairs(monkeypatch):
+    """Few rows, short reductions, on another stream than an inference whose convolutions run on CTA pairs with all of tensor memory and whose next frame is
+    matched meanwhile (they then leave the most shared memory free): both end, with the results that they have alone."""
+    monkeypatch.setenv("DC_CONV_SCHEME", "7")
+    h, w, S = 480, 640, 5                                           # blocks of 4: enough of them for the overlapped pass
+    b = nets.NetBuilder(h, w)
+    x = b.resize_area(-1, 56, 56)
+    x = b.conv(x, 64, 3, 1, 1)
+    pairs = [b.conv(x, 256, 3, 1, 1)]
+    pairs.append(b.conv(pairs[0], 256, 3, 1, 1))
+    weights, biases = nets.random_weights(b.layers, 4)
+    frames = [torch.as_tensor(f).cuda() for f in frames_of(h, w, 6, S, 2)]
+    m, k, n = 8, 512, 4096
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    a, wq = (torch.randint(-127, 128, (r, k), generator=g, device="cuda", dtype=torch.int32).to(torch.int8) for r in (m, n))
+    sa, sw = torch.rand(m, generator=g, device="cuda"), torch.rand(n, generator=g, device="cuda")
+    want, out = (torch.empty(m, n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    B.dc_matmul_quantized(a, sa, wq, sw, None, want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+
+    def run(beside):
+        dc = DeepCache(w, h, b.layers, weights, biases, n_streams=S, block=4, search_range=4, dtype=B.DC_BF16, expire_n=3)
+        try:
+            assert [B.dc_cache_layer_conv_scheme(dc.handle, i) for i in pairs] == [7, 7]
+            outs = []
+            for rounds in range(4):
+                for t, f in enumerate(frames):
+                    outs.append(dc.infer_frame(f))
+                    B.dc_lookahead_frame(dc.handle, frames[(t + 1) % len(frames)], w * 3)
+                    if beside:
+                        with torch.cuda.stream(side):
+                            for _ in range(40):
+                                B.dc_matmul_quantized(a, sa, wq, sw, None, out)
+            torch.cuda.synchronize()
+            assert dc.status() == B.DC_OK
+            return outs
+        finally:
+            dc.close()
+
+    alone, beside = run(False), run(True)
+    assert all(torch.equal(p, q) for p, q in zip(alone, beside))
+    assert torch.equal(out, want)
