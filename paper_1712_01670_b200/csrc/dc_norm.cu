@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : 256, BLOCK ? 1 : VE == 1 ? (NV
                     F g[P], b[P];
                     if (!KEEP) { load_weights(a.gamma, i * VE, 1.f, g); load_weights(a.beta, i * VE, 0.f, b); }
 #pragma unroll
-                    for (int k = 0; k < P; ++k) d[v * P + k] = fma2(mul2(d[v * P + k], both<F>(rstd)), KEEP ? gk[KEEP ? v : 0][k] : g[k], KEEP ? bk[KEEP ? v : 0][k] : b[k]);
+                    for (int k = 0; k < P; ++k) d[v * P + k] = fma2(rounded(d[v * P + k], both<F>(rstd)), KEEP ? gk[KEEP ? v : 0][k] : g[k], KEEP ? bk[KEEP ? v : 0][k] : b[k]);
                 }
                 const typename V::Raw r = V::close(d + v * P);
                 if (on && a.y && (FULL || i < nvec)) *(typename V::Raw*)(y + v * line) = r;
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(1024) k_rows_long(const dc_rows_args a)
         auto at = [&](int i) { float v; V::open(x[i], &v); return v; };
         auto value = [&](int i) -> T {                            // as the map holds it
             float v = at(i);
-            if (NORM) v = fmaf((v - mean) * rstd, a.gamma ? dc_ld(a.gamma + i) : 1.f, a.beta ? dc_ld(a.beta + i) : 0.f);
+            if (NORM) v = fmaf(rounded(v - mean, rstd), a.gamma ? dc_ld(a.gamma + i) : 1.f, a.beta ? dc_ld(a.beta + i) : 0.f);
             return V::close(&v);
         };
         if (NORM) {

@@ -33,6 +33,10 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 __device__ __forceinline__ float add2(float a, float b) { return a + b; }
 __device__ __forceinline__ float mul2(float a, float b) { return a * b; }
 __device__ __forceinline__ float fma2(float a, float b, float c) { return fmaf(a, b, c); }
+// A product that is rounded whatever follows it.  The compiler may join a * b with an addition, and where gamma is absent, and so 1, fmaf(a * b, 1, beta) is one: a
+// row's values would have other bits in one kernel than in another.
+__device__ __forceinline__ float rounded(float a, float b) { return __fmul_rn(a, b); }
+__device__ __forceinline__ float2 rounded(float2 a, float2 b) { return mul2(a, b); }
 template <typename F> __device__ __forceinline__ F both(float a);
 template <> __device__ __forceinline__ float both<float>(float a) { return a; }
 template <> __device__ __forceinline__ float2 both<float2>(float a) { return make_float2(a, a); }

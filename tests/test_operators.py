@@ -471,6 +471,27 @@ def test_norm_and_quantise_with_an_output_that_is_not_aligned(rows, c, dtype):
     assert torch.equal(q, done[0][0]) and torch.equal(s, done[0][1])
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,c", [(400, 17), (300, 64), (200, 250), (200, 511), (100, 1001), (100, 2048), (60, 5001), (60, 7001), (30, 9001), (20, 16383)])
+def test_norm_and_quantise_has_the_bits_of_two_with_any_weights(rows, c, dtype):
+    """Rows of every kind of kernel, whole vectors and single elements, with either weight or none."""
+    t, g = TYPES[dtype], gen(c)
+    x, _ = spread(make_map(rows, c, t, 5), c + (3 if c % 2 else 8), c % 2)
+    for gamma in (None, torch.randn(c, generator=g, device="cuda")):
+        for beta in (None, torch.randn(c, generator=g, device="cuda")):
+            y, y1, q, q1, q2 = torch.empty(rows, c, dtype=t, device="cuda"), torch.empty(rows, c, dtype=t, device="cuda"), q_like(rows, c), q_like(rows, c), q_like(rows, c)
+            s, s1, s2 = (torch.empty(rows, device="cuda") for _ in range(3))
+            check_norm(x, gamma, beta, y=y)
+            B.dc_quantize_rows(y, q, s)
+            B.dc_layer_norm_quantize(x, gamma, beta, q1, s1, y1)
+            wq, ws = quantise64(y1)
+            assert torch.equal(y, y1) and torch.equal(q, q1) and torch.equal(s, s1) and torch.equal(q1, wq) and torch.equal(s1, ws)
+            B.dc_layer_norm_quantize(x, gamma, beta, q2, s2)
+            if c % 8 == 0 or c * y.element_size() % 16:                # (the map is aligned alike: rows of whole 16 bytes, or single elements either way)
+                assert torch.equal(q, q2) and torch.equal(s, s2)
+
+
 # ---------------------------------------------------------------------------
 # products
 # ---------------------------------------------------------------------------
