@@ -389,6 +389,72 @@ int dc_linear_quantized(const void* x_dev, size_t x_pitch, const int8_t* w_dev, 
                         void* out_dev, size_t out_pitch, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
 int dc_linear_workspace(int64_t m, int32_t k, size_t* bytes);
 
+/* ---- group normalisation with an activation ----
+ * What the section above says of maps, rows, pitches, streams, what a call writes and errors holds here and below.  The rows of a map are those of `maps` images
+ * (streams) of `pixels` pixels each, one image behind another; channels are in `groups` groups of neighbouring ones (channels a multiple of groups). */
+typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_SILU = 2 } dc_activation;     /* z, max(z, 0), z / (1 + e^-z) */
+
+/* Over the pixels of an image and the channels of a group:
+ *   mean = sum x / N, rstd = 1 / sqrt(sum (x - mean)^2 / N + eps), z = (x - mean) rstd gamma + beta, y = activation(z)
+ *   gamma_dev, beta_dev   float32 [channels] or NULL (ones, zeros)
+ *   mean_dev, rstd_dev    float32 [maps][groups] or NULL: for dc_group_norm_backward
+ *   workspace_dev         dc_group_norm_workspace bytes, any alignment, apart from all else; its content does not matter before or after the call;
+ *                         two calls that may overlap need one each.  Not needed for no rows.
+ * y_dev may be x_dev with the same pitch.  eps >= 0.  A group of an image with a NaN or an infinity becomes NaN (with ReLU too), no other one changes; sums and squares are float32,
+ * so values beyond 1e18 or so have no meaningful result.  Equal calls give equal bits; one whose pointers or pitches are aligned otherwise adds up in another order.
+ * DC_ERR_CONFIG: activation; DC_ERR_LIMIT: more than 16384 channels, maps * groups beyond 2^27 or so many small images that a grid cannot hold them. */
+int dc_group_norm(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t maps, int64_t pixels, int32_t channels,
+                  int32_t groups, double eps, int32_t activation, int32_t dtype, void* y_dev, size_t y_pitch, float* mean_dev, float* rstd_dev,
+                  void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+int dc_group_norm_workspace(int64_t maps, int64_t pixels, int32_t channels, int32_t groups, size_t* bytes);
+
+/* Its gradients, for the gradient dy of y, with xh = (x - mean) rstd, dz = dy activation'(z) and g = dz gamma:
+ *   dx = rstd (g - mean(g) - xh mean(g xh)) with means over an image's group,  dgamma = sum over rows of dz xh,  dbeta = sum over rows of dz
+ *   mean_dev, rstd_dev    float32 [maps][groups], as dc_group_norm gave them
+ *   dx_dev                the map's type, or NULL; may be dy_dev or x_dev with the same pitch
+ *   dgamma_dev, dbeta_dev float32 [channels], or NULL; overwritten (zeros for no rows)
+ *   workspace_dev         dc_group_norm_workspace bytes, as above
+ * z is computed again, with the forward pass's roundings: ReLU's gradient is dy exactly where that pass has kept z > 0, if it was given this mean and rstd. */
+int dc_group_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev,
+                           const float* mean_dev, const float* rstd_dev, int64_t maps, int64_t pixels, int32_t channels, int32_t groups,
+                           int32_t activation, int32_t dtype, void* dx_dev, size_t dx_pitch, float* dgamma_dev, float* dbeta_dev,
+                           void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+
+/* ---- rows in 8-bit floating point, a scale for each block of 128 ----
+ * Values are e4m3 (four bits of exponent, three of mantissa, up to 448, no infinities); 128 neighbours of a row share a scale. */
+
+/* x [rows][channels] in 8 bits, as it lies (q) and turned (qt, for products that sum over rows), either or both:
+ *   block_rows    1: a scale for 128 values of a row (activations, gradients); 128: for 128 rows x 128 values (weights)
+ *   q_dev [rows][q_pitch], scale_dev float32 [ceil(rows / block_rows)][ceil(channels / 128)]; both NULL: not wanted
+ *   qt_dev [channels][qt_pitch], scale_t_dev float32 [ceil(channels / block_rows)][ceil(rows / 128)]: the same of x turned; both NULL: not wanted
+ * The scale is the smallest power of two, and not below 2^-126, that takes the block's largest value to 448 or below: x / scale is exact, and q is the value next to it
+ * (halves to even).  A block of zeros has the scale 0.  A block with a NaN or an infinity gets the scale NaN and zeros.
+ * q_dev, qt_dev: 16-byte aligned, pitches multiples of 16; what lies between a row's end and the next row is not written.  DC_ERR_CONFIG: block_rows. */
+int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t channels, int32_t dtype, int32_t block_rows,
+                       uint8_t* q_dev, size_t q_pitch, float* scale_dev, uint8_t* qt_dev, size_t qt_pitch, float* scale_t_dev, void* cuda_stream);
+
+/* out[r][j] = relu(sum over blocks i of s(r, j, i) (sum over k of block i of a[r][k] b[j][k]) + bias[j]),  s(r, j, i) = a_scale[r][i] b_scale[j'][i]
+ *   a_dev e4m3 [m][a_pitch], a_scale_dev float32 [m][ceil(k / 128)]
+ *   b_dev e4m3 [n][b_pitch], b_scale_dev float32 [ceil(n / b_block_rows)][ceil(k / 128)], b_block_rows 128 (weights: j' = j / 128) or 1 (j' = j)
+ *   both 16-byte aligned, pitches multiples of 16; nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
+ * Any scales: float32, not only those of dc_quantize_blocks.  A block's products are added up on the tensor cores in float32 (error below 2^-20 of the sum of their sizes), scaled
+ * (a scale by a scale first where b's is for 128 rows, else the sum by b's and then by a's) and added to the blocks before in float32, with one rounding to dtype behind bias and ReLU
+ * (which leaves a NaN).  The order of the blocks' sum depends on m, n, k and the device alone.  Every wait inside the kernels is bounded; should one run out (2 s), the results that it
+ * concerns are NaN.
+ * The gradients of out = x wT: dx = dy w is this product with dc_quantize_blocks' dy and the turned weights, dw = dyT x that of both turned (b_block_rows 1).
+ * DC_ERR_LIMIT: n > 2^28.  DC_ERR_CONFIG: b_block_rows. */
+int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const uint8_t* b_dev, size_t b_pitch, const float* b_scale_dev,
+                     int32_t b_block_rows, const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
+                     void* out_dev, size_t out_pitch, void* cuda_stream);
+
+/* A whole layer: the rows of x [m][k] (dtype) into 8 bits (block_rows 1), then the product with weights w.  out_dev may lie over x_dev, with any pitch.
+ * workspace_dev: dc_linear_blocks_workspace bytes, any alignment, apart from all else; its content does not matter before or after the call; two calls that may
+ * overlap need one each. */
+int dc_linear_blocks(const void* x_dev, size_t x_pitch, const uint8_t* w_dev, size_t w_pitch, const float* w_scale_dev, int32_t w_block_rows,
+                     const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
+                     void* out_dev, size_t out_pitch, void* workspace_dev, size_t workspace_bytes, void* cuda_stream);
+int dc_linear_blocks_workspace(int64_t m, int32_t k, size_t* bytes);
+
 const char* dc_strerror(int status);
 
 #ifdef __cplusplus

@@ -20,6 +20,7 @@ DC_CONV, DC_MAXPOOL, DC_RELU, DC_ADD, DC_CONCAT, DC_RESIZE_AREA, DC_LRN, DC_FC, 
 DC_SEARCH_EXHAUSTIVE, DC_SEARCH_DIAMOND, DC_SEARCH_THREE_STEP = 0, 1, 2
 DC_REGIONS_GLOBAL, DC_REGIONS_PER_BLOCK = 0, 1
 DC_FP32, DC_BF16 = 0, 1
+DC_ACT_NONE, DC_ACT_RELU, DC_ACT_SILU = 0, 1, 2
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdeepcache.so")
 
@@ -55,7 +56,9 @@ EXPORTS = ["dc_cache_create", "dc_cache_destroy", "dc_cache_reset", "dc_cache_se
            "dc_cache_layer_map", "dc_cache_layer_regions", "dc_cache_layer_conv_scheme", "dc_get_status", "dc_cache_launches",
            "dc_cache_set_profiling", "dc_cache_profile", "dc_cache_counters", "dc_search_blocks_noalloc",
            "dc_layer_norm", "dc_layer_norm_backward", "dc_layer_norm_workspace", "dc_quantize_rows", "dc_layer_norm_quantize",
-           "dc_matmul_quantized", "dc_linear_quantized", "dc_linear_workspace", "dc_strerror"]
+           "dc_matmul_quantized", "dc_linear_quantized", "dc_linear_workspace",
+           "dc_group_norm", "dc_group_norm_backward", "dc_group_norm_workspace", "dc_quantize_blocks", "dc_matmul_blocks", "dc_linear_blocks",
+           "dc_linear_blocks_workspace", "dc_strerror"]
 PROFILE_STAGES = ["search", "verify", "merge", "propagate", "classify_copy", "conv", "input", "pointwise", "key_update"]
 
 _lib = None
@@ -108,6 +111,13 @@ def load():
         L.dc_matmul_quantized.argtypes = [vp, sz, vp, vp, sz, vp, vp, i64, i32, i32, i32, i32, vp, sz, vp]
         L.dc_linear_quantized.argtypes = [vp, sz, vp, sz, vp, vp, i64, i32, i32, i32, i32, vp, sz, vp, sz, vp]
         L.dc_linear_workspace.argtypes = [i64, i32, C.POINTER(sz)]
+        L.dc_group_norm.argtypes = [vp, sz, vp, vp, i64, i64, i32, i32, f64, i32, i32, vp, sz, vp, vp, vp, sz, vp]
+        L.dc_group_norm_backward.argtypes = [vp, sz, vp, sz, vp, vp, vp, vp, i64, i64, i32, i32, i32, i32, vp, sz, vp, vp, vp, sz, vp]
+        L.dc_group_norm_workspace.argtypes = [i64, i64, i32, i32, C.POINTER(sz)]
+        L.dc_quantize_blocks.argtypes = [vp, sz, i64, i32, i32, i32, vp, sz, vp, vp, sz, vp, vp]
+        L.dc_matmul_blocks.argtypes = [vp, sz, vp, vp, sz, vp, i32, vp, i64, i32, i32, i32, i32, vp, sz, vp]
+        L.dc_linear_blocks.argtypes = [vp, sz, vp, sz, vp, i32, vp, i64, i32, i32, i32, i32, vp, sz, vp, sz, vp]
+        L.dc_linear_blocks_workspace.argtypes = [i64, i32, C.POINTER(sz)]
         L.dc_strerror.argtypes = [i]
         L.dc_strerror.restype = C.c_char_p
         for name in EXPORTS[:-1]:
@@ -349,3 +359,58 @@ def dc_linear_quantized(x, w, w_scale, bias, out, relu=False, workspace=None, st
     rc = (_native or _tensors()).linear_quantized(x, w, w_scale, bias, out, relu, workspace, stream)
     if rc:
         raise DeepCacheError(rc, "dc_linear_quantized")
+
+
+# --------------------------------------------------------------------------
+# group normalisation with an activation: maps [maps, ..., channels], the first dimension counting images (streams); mean, rstd: float32 [maps, groups];
+# workspace: any tensor of dc_group_norm_workspace bytes
+# --------------------------------------------------------------------------
+def dc_group_norm_workspace(maps: int, pixels: int, channels: int, groups: int) -> int:
+    v = C.c_size_t()
+    _check(load().dc_group_norm_workspace(maps, pixels, channels, groups, C.byref(v)), "dc_group_norm_workspace")
+    return v.value
+
+
+def dc_group_norm(x, groups, gamma, beta, y, mean=None, rstd=None, activation=DC_ACT_NONE, eps=1e-5, workspace=None, stream=None):
+    """y = activation(group normalisation of x); gamma, beta, mean, rstd may be None."""
+    rc = (_native or _tensors()).group_norm(x, groups, gamma, beta, y, mean, rstd, activation, eps, workspace, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_group_norm")
+
+
+def dc_group_norm_backward(dy, x, groups, gamma, beta, mean, rstd, dx=None, dgamma=None, dbeta=None, activation=DC_ACT_NONE, workspace=None, stream=None):
+    """Gradients of dc_group_norm, from dy, the gradient of its output."""
+    rc = (_native or _tensors()).group_norm_backward(dy, x, groups, gamma, beta, mean, rstd, dx, dgamma, dbeta, activation, workspace, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_group_norm_backward")
+
+
+# --------------------------------------------------------------------------
+# 8-bit floating point with a scale for each block of 128: q, q_t, a, b, w are two-dimensional torch.float8_e4m3fn (or uint8 that holds its bits), rows a
+# multiple of 16 bytes apart; scales contiguous float32 tables.  b_scale and w_scale have a row for 128 rows of b, or for each.
+# --------------------------------------------------------------------------
+def dc_quantize_blocks(x, q=None, scale=None, q_t=None, scale_t=None, block_rows=1, stream=None):
+    """x [rows, channels] in 8 bits: q, scale [ceil(rows / block_rows), ceil(channels / 128)]; and turned, q_t [channels, rows], scale_t."""
+    rc = (_native or _tensors()).quantize_blocks(x, q, scale, q_t, scale_t, block_rows, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_quantize_blocks")
+
+
+def dc_matmul_blocks(a, a_scale, b, b_scale, bias, out, relu=False, stream=None):
+    """out = relu((a with its scales) @ (b with its scales).T + bias) for a [m, k], b [n, k]; bias may be None."""
+    rc = (_native or _tensors()).matmul_blocks(a, a_scale, b, b_scale, bias, out, relu, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_matmul_blocks")
+
+
+def dc_linear_blocks_workspace(rows: int, k: int) -> int:
+    v = C.c_size_t()
+    _check(load().dc_linear_blocks_workspace(rows, k, C.byref(v)), "dc_linear_blocks_workspace")
+    return v.value
+
+
+def dc_linear_blocks(x, w, w_scale, bias, out, relu=False, workspace=None, stream=None):
+    """out = relu(x @ (w with its scales).T + bias) with x's rows put into 8 bits; workspace: any tensor of dc_linear_blocks_workspace(rows, k) bytes."""
+    rc = (_native or _tensors()).linear_blocks(x, w, w_scale, bias, out, relu, workspace, stream)
+    if rc:
+        raise DeepCacheError(rc, "dc_linear_blocks")

@@ -1,0 +1,688 @@
+// Rows in 8-bit floating point (e4m3) with a scale for each block of 128 values, and their products.
+//
+//   scale = the smallest power of two with max |x| <= 448 scale,  q = e4m3(x / scale)
+//   out[r][j] = relu(sum_i a_scale[r][i] b_scale[j'][i] sum_{k in block i} a[r][k] b[j][k] + bias[j])
+//
+// k_quantize_blocks: memory bounds it: a tile of 128 x 128 values is read once, into registers, and leaves as rows, turned, or both.
+//
+// k_blocks: tcgen05.mma kind::f8f6f4 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, which are one block.  A block's sums leave
+// tensor memory as soon as they are there, are scaled and added up in the registers of eight warps, beside the MMAs of the next block (two accumulators in turns).
+#include "dc_product.cuh"
+#include "dc_quantise.cuh"
+
+namespace {
+
+__device__ int32_t g_blocks_status;                           // the status word of these launches
+
+// ---------------------------------------------------------------------------
+// rows in 8 bits
+// ---------------------------------------------------------------------------
+struct BlocksArgs {
+    const void* x; size_t x_pitch;
+    int rows, channels, kb, rb;                               // kb, rb: blocks of 128 columns, of 128 rows
+    uint8_t* q; size_t q_pitch; float* scale;                 // or NULL
+    uint8_t* qt; size_t qt_pitch; float* scale_t;             // or NULL
+    int block_rows;
+};
+
+// What the bits of a block's largest size say: its scale and 1 / scale, both powers of two, so x / scale is exact.  448 = 1.75 * 2^8: with most = 1.f * 2^e the scale is
+// 2^(e - 8), or twice that where 1.f > 1.75.
+struct BlockScale { float scale, inv; bool bad; };
+__device__ __forceinline__ BlockScale block_scale(uint32_t bits)
+{
+    BlockScale s;
+    s.bad = bits >= 0x7f800000u;
+    const int e = max((int)((bits + 0x1fffffu) >> 23) - 8, 1);
+    s.scale = s.bad ? __uint_as_float(0x7fffffffu) : bits == 0 ? 0.f : __uint_as_float((uint32_t)e << 23);
+    s.inv = __uint_as_float((uint32_t)(254 - e) << 23);
+    return s;
+}
+// Two floats as e4m3, the first one in the low byte.
+__device__ __forceinline__ uint32_t two_e4m3(float2 v)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+
+// Eight values of a row.
+template <typename T> struct Eight;
+template <> struct Eight<__nv_bfloat16> {
+    uint4 raw;
+    __device__ __forceinline__ void zero() { raw = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const char* p) { raw = *(const uint4*)p; }
+    __device__ __forceinline__ void put(int k, __nv_bfloat16 v)
+    {
+        uint32_t* const w = &raw.x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i == k >> 1) w[i] |= (uint32_t)__bfloat16_as_ushort(v) << (16 * (k & 1));
+    }
+    __device__ __forceinline__ void open(float2* v) const { Vec<__nv_bfloat16, 8>::open(raw, v); }
+};
+template <> struct Eight<float> {
+    float4 raw[2];
+    __device__ __forceinline__ void zero() { raw[0] = raw[1] = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void load(const char* p) { raw[0] = *(const float4*)p; raw[1] = *(const float4*)(p + 16); }
+    __device__ __forceinline__ void put(int k, float v)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i == k) (&raw[i >> 2].x)[i & 3] = v;
+    }
+    __device__ __forceinline__ void open(float2* v) const { Vec<float, 4>::open(raw[0], v); Vec<float, 4>::open(raw[1], v + 2); }
+};
+
+__device__ __forceinline__ void store_bytes(uint8_t* p, uint2 w, int there)       // the first `there` of eight
+{
+    if (there >= 8) { *(uint2*)p = w; return; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < there) p[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+}
+
+// A CTA has 128 x 128 values, a thread eight columns of eight rows.  WIDE: rows are aligned to 16 bytes.  TURN: x turned is wanted.
+template <typename T, bool WIDE, bool TURN>
+__global__ void __launch_bounds__(256) k_quantize_blocks(const BlocksArgs a)
+{
+    __shared__ uint32_t most_of_column[16][128];
+    __shared__ float inv_of_column[128];                      // 1 / scale; negative: a NaN or an infinity
+    __shared__ uint32_t most_of_tile;
+    __shared__ uint2 turned[128 * 16];                        // [column][rows / 8], the eights of a column in another order for each eight columns: no bank conflicts
+    const int tile_c = blockIdx.x % a.kb, tile_r = blockIdx.x / a.kb;
+    const int part = threadIdx.x & 15, team = threadIdx.x >> 4, lane = threadIdx.x & 31;
+    const int col = tile_c * 128 + part * 8, row0 = tile_r * 128 + team * 8, columns = min(8, a.channels - col);
+    dc_pdl_wait();
+    dc_pdl_release();
+    if (threadIdx.x == 0) most_of_tile = 0;
+    Eight<T> v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i].zero();
+        if (row0 + i < a.rows && columns > 0) {
+            const char* const x = (const char*)a.x + (size_t)(row0 + i) * a.x_pitch + (size_t)col * sizeof(T);
+            if (WIDE && columns == 8) v[i].load(x);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < columns) v[i].put(k, ((const T*)x)[k]);
+        }
+    }
+    uint32_t most[8], down[8];                                // of the rows, of the columns
+#pragma unroll
+    for (int k = 0; k < 8; ++k) down[k] = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float2 f[4];
+        v[i].open(f);
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t x = size_bits(f[k].x), y = size_bits(f[k].y);
+            m = max(m, max(x, y));
+            if (TURN) { down[2 * k] = max(down[2 * k], x); down[2 * k + 1] = max(down[2 * k + 1], y); }
+        }
+        most[i] = __reduce_max_sync(0xffffu << (lane & 16), m);
+    }
+    if (a.block_rows > 1) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, most[i]);
+        __syncthreads();
+        if (part == 0) atomicMax(&most_of_tile, m);           // the same whatever the order
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most[i] = most_of_tile;
+        if (threadIdx.x == 0) {
+            const float s = block_scale(most[0]).scale;
+            if (a.q) a.scale[(size_t)tile_r * a.kb + tile_c] = s;
+            if (TURN) a.scale_t[(size_t)tile_c * a.rb + tile_r] = s;
+        }
+    }
+    if (a.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const BlockScale s = block_scale(most[i]);
+            float2 f[4];
+            v[i].open(f);
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = s.bad ? 0u : two_e4m3(mul2(f[k], both<float2>(s.inv)));
+            if (row0 + i < a.rows) {
+                if (columns > 0) store_bytes(a.q + (size_t)(row0 + i) * a.q_pitch + col, make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16), columns);
+                if (a.block_rows == 1 && part == 0) a.scale[(size_t)(row0 + i) * a.kb + tile_c] = s.scale;
+            }
+        }
+    }
+    if (TURN) {
+        if (a.block_rows == 1) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) most_of_column[team][part * 8 + k] = down[k];
+            __syncthreads();
+            if (threadIdx.x < 128) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int t = 0; t < 16; ++t) m = max(m, most_of_column[t][threadIdx.x]);
+                const BlockScale s = block_scale(m);
+                inv_of_column[threadIdx.x] = s.bad ? -1.f : s.inv;
+                const int c = tile_c * 128 + threadIdx.x;
+                if (c < a.channels) a.scale_t[(size_t)c * a.rb + tile_r] = s.scale;
+            }
+        } else if (threadIdx.x < 128) {
+            const BlockScale s = block_scale(most[0]);
+            inv_of_column[threadIdx.x] = s.bad ? -1.f : s.inv;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {                      // two columns of eight rows
+            const float i0 = inv_of_column[part * 8 + k], i1 = inv_of_column[part * 8 + k + 1];
+            uint32_t lo[2] = {0, 0}, hi[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float2 f[4];
+                v[i].open(f);
+                const uint32_t t = two_e4m3(mul2(f[k / 2], make_float2(i0, i1)));
+                lo[i >> 2] |= (t & 0xffu) << (8 * (i & 3));
+                hi[i >> 2] |= (t >> 8) << (8 * (i & 3));
+            }
+            const int c = part * 8 + k, at = team ^ part;
+            turned[c * 16 + at] = i0 < 0.f ? make_uint2(0, 0) : make_uint2(lo[0], lo[1]);
+            turned[(c + 1) * 16 + at] = i1 < 0.f ? make_uint2(0, 0) : make_uint2(hi[0], hi[1]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {                      // 16 lanes to a column's 128 bytes
+            const int c = it * 16 + (threadIdx.x >> 4), r = tile_r * 128 + part * 8;
+            if (tile_c * 128 + c < a.channels && r < a.rows)
+                store_bytes(a.qt + (size_t)(tile_c * 128 + c) * a.qt_pitch + r, turned[c * 16 + (part ^ (c >> 3 & 15))], a.rows - r);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// products
+// ---------------------------------------------------------------------------
+struct BlocksProduct {
+    const uint8_t* a; size_t a_pitch; const float* a_scale;
+    const uint8_t* b; size_t b_pitch; const float* b_scale;
+    const float* bias;                                        // or NULL
+    int64_t m; int n, k, relu, b_block_rows;
+    void* out; size_t out_pitch;
+};
+struct BlocksTiles {
+    BlocksProduct p;
+    int NB, m_tiles, stages, stage_bytes, kb, k_last;         // column tiles; blocks of K; MMAs (32 values) of the last one
+    uint32_t idesc;
+    int wide, boxes;                                          // out takes 16-byte stores; is written in boxes by TMA
+};
+
+constexpr int kAddWarps = 8, kBlocksThreads = (4 + kAddWarps) * 32;
+constexpr int kBlocksMostStages = 8, kScaleSlots = 4;
+constexpr int kBox = 32 * 64;                                 // a warp's 32 rows on their way out, 64 bytes each; two of them
+struct BlocksCtl {
+    unsigned long long full[kBlocksMostStages], empty[kBlocksMostStages], tmem_full[2], tmem_empty[2], scale_full[kScaleSlots], scale_empty[kScaleSlots];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    unsigned long long wait_ns;
+};
+constexpr int kBlocksSmem = 227 * 1024;
+constexpr int kScaleBytes = kScaleSlots * (2 * 128 + 256) * 4;
+constexpr int kBlocksRoom = kBlocksSmem - 1024 - (int)sizeof(BlocksCtl) - kScaleBytes - kAddWarps * 2 * kBox;
+
+#define DC_UMMA_F8(name, group)                                                                                                                 \
+    __device__ __forceinline__ void name(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, int n)                            \
+    {                                                                                                                                           \
+        _Pragma("unroll") for (int k = 0; k < 4; ++k)                                                                                           \
+            if (k < n)                                                                                                                          \
+                asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t" \
+                             "tcgen05.mma." group ".kind::f8f6f4 [%0], da, db, %4, p;\n\t}"                                                     \
+                             ::"r"(d), "r"(a_lo + 2u * k), "r"(b_lo + 2u * k), "r"(hi), "r"(idesc), "r"(k) : "memory");                          \
+    }
+DC_UMMA_F8(umma_f8, "cta_group::1")
+DC_UMMA_F8(umma_f8_pair, "cta_group::2")
+#undef DC_UMMA_F8
+
+__device__ __forceinline__ bool blocks_wait(uint32_t bar, uint32_t parity, BlocksCtl* ctl)
+{
+    return mbar_wait_at(bar, parity, &ctl->abort_flag, &ctl->wait_ns, &g_blocks_status);
+}
+
+// BN: columns of a tile.  EACH: b has a scale for each row and block, not for 128 rows.
+template <bool PAIR, int BN, bool EACH, typename T>
+__global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC, const BlocksTiles a)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint8_t* const staging = ring + a.stages * a.stage_bytes;
+    float* const row_scale = (float*)(staging + kAddWarps * 2 * kBox);       // [slots][2][128]: of the rows, for either 128 columns
+    float* const col_scale = row_scale + kScaleSlots * 256;                  // [slots][256]: EACH
+    BlocksCtl* const ctl = (BlocksCtl*)(col_scale + kScaleSlots * 256);
+    const BlocksProduct& p = a.p;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+    constexpr int M = PAIR ? 2 : 1;                           // row tiles of an item
+    constexpr uint32_t kColumns = 2 * BN;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], kAddWarps * M); }
+        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 1); mbar_init(&ctl->scale_empty[i], kAddWarps); }
+        ctl->abort_flag = 0;
+        ctl->wait_ns = kWaitNs;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmB) : "memory");
+    }
+    if (warp == 1) {
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kColumns) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kColumns) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                             // both CTAs' barriers exist before either is signalled from outside
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    dc_pdl_wait();
+    dc_pdl_release();
+    const int n_items = (a.m_tiles + M - 1) / M * a.NB;
+    // row tile `rank` of an item; an absent second tile repeats the first, and nothing of it is stored
+    auto tile_of = [&](int group, bool* there) -> int {
+        const int idx = group * M + rank;
+        *there = idx < a.m_tiles;
+        return *there ? idx : idx - rank;
+    };
+    const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
+
+    if (warp < 4) {
+        if (BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 0) {
+            // ---------------- producer ----------------
+            if (elect_one()) {
+                const uint32_t lead_full = PAIR ? map_to_cta(&ctl->full[0], 0) : full0;
+                RingPos r;
+                r.start(ring0, (uint32_t)a.stages);
+                bool ok = true, there;
+                for (int item = first; item < n_items && ok; item += step) {
+                    const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * BN + rank * (BN / 2);
+                    for (int kc = 0; kc < a.kb; ++kc) {
+                        ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
+                        if (!ok) break;
+                        if (PAIR) {
+                            if (rank == 0) mbar_expect_tx(full0 + r.off, 2u * (uint32_t)a.stage_bytes);
+                            load_pair(r.data, &tmA, kc * kBytesK, row, lead_full + r.off);
+                            load_pair(r.data + kATile, &tmB, kc * kBytesK, col, lead_full + r.off);
+                        } else {
+                            mbar_expect_tx(full0 + r.off, (uint32_t)a.stage_bytes);
+                            tma_load_2d(r.data, &tmA, kc * kBytesK, row, full0 + r.off);
+                            tma_load_2d(r.data + kATile, &tmB, kc * kBytesK, col, full0 + r.off);
+                        }
+                        r.next(ring0, (uint32_t)a.stages, (uint32_t)a.stage_bytes);
+                    }
+                }
+                // on an abort: give the copies already issued a bounded chance to land before the CTA exits
+                if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
+            }
+            __syncwarp();
+        } else if (warp == 1) {
+            // ---------------- MMA issuer (of a pair: the leader's, for both CTAs) ----------------
+            if (rank == 0 && elect_one()) {
+                const uint64_t dconst = umma_desc(0, 1024, 2);
+                const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
+                RingPos r;
+                r.start(r0, (uint32_t)a.stages);
+                uint32_t acc = 0, acc_ph = 0;
+                bool ok = true;
+                for (int item = first; item < n_items && ok; item += step)
+                    for (int kc = 0; kc < a.kb; ++kc) {
+                        ok = blocks_wait(smem_u32(&ctl->tmem_empty[acc]), acc_ph ^ 1u, ctl) && blocks_wait(full0 + r.off, r.phase, ctl);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int n = kc + 1 < a.kb ? 4 : a.k_last;
+                        const uint32_t d = tmem_base + acc * (uint32_t)BN;
+                        if (PAIR) {
+                            umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                            commit_pair(empty0 + r.off);
+                            commit_pair(smem_u32(&ctl->tmem_full[acc]));
+                        } else {
+                            umma_f8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                            umma_commit_at(empty0 + r.off);
+                            umma_commit(&ctl->tmem_full[acc]);
+                        }
+                        r.next(r0, (uint32_t)a.stages, slot);
+                        if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+                    }
+            }
+            __syncwarp();
+        } else if (warp == 2) {
+            // ---------------- scales ----------------
+            // A lane has four rows (and of EACH's columns eight at most).
+            uint32_t slot = 0, phase = 0;
+            bool ok = true, there;
+            for (int item = first; item < n_items && ok; item += step) {
+                const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN;
+                for (int kc = 0; kc < a.kb && ok; ++kc) {
+                    float s[4], c[EACH ? BN / 32 : 2];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t r = (int64_t)tile * kTileM + 32 * i + lane;
+                        s[i] = r < p.m ? p.a_scale[r * a.kb + kc] : 0.f;
+                    }
+                    if (EACH)
+#pragma unroll
+                        for (int i = 0; i < BN / 32; ++i) { const int j = n0 + 32 * i + lane; c[i] = j < p.n ? p.b_scale[(size_t)j * a.kb + kc] : 0.f; }
+                    else
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) { const int j = n0 + 128 * h; c[h] = (h == 0 || BN > 128) && j < p.n ? p.b_scale[(size_t)(j / 128) * a.kb + kc] : 0.f; }
+                    ok = blocks_wait(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (EACH) row_scale[slot * 256 + 32 * i + lane] = s[i];
+                        else
+#pragma unroll
+                            for (int h = 0; h < (BN > 128 ? 2 : 1); ++h) row_scale[slot * 256 + h * 128 + 32 * i + lane] = s[i] * c[h];
+                    }
+                    if (EACH)
+#pragma unroll
+                        for (int i = 0; i < BN / 32; ++i) col_scale[slot * 256 + 32 * i + lane] = c[i];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl->scale_full[slot]);
+                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1u; }
+                }
+            }
+        }
+    } else {
+        // ---------------- sums of the blocks; bias, ReLU, rounding, store ----------------
+        // A warp has 32 rows, one to a lane (the quadrant of tensor memory that it may read), and half of the columns.
+        if (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        constexpr int MINE = BN / 2;
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 4) * 2 * kBox;
+        const uint32_t both_places = stage ^ (stage + kBox);
+        const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
+        const float* const my_scale = row_scale + (!EACH && BN > 128 ? half * 128 : 0) + q * 32 + lane;
+        uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0;
+        bool ok = true, there;
+        for (int item = first; item < n_items; item += step) {
+            const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN + half * MINE;
+            const int64_t row0 = (int64_t)tile * kTileM + q * 32;
+            const int rows = there ? (int)max((int64_t)0, min((int64_t)32, p.m - row0)) : 0;
+            float2 sum[MINE / 2];
+#pragma unroll
+            for (int i = 0; i < MINE / 2; ++i) sum[i] = make_float2(0.f, 0.f);
+            for (int kc = 0; kc < a.kb; ++kc) {
+                if (ok) ok = blocks_wait(smem_u32(&ctl->scale_full[slot]), phase, ctl) && blocks_wait(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const float2 s = both<float2>(my_scale[slot * 256]);
+                const uint32_t from = tmem_base + acc * (uint32_t)BN + (uint32_t)(half * MINE) + ((uint32_t)(q * 32) << 16);
+#pragma unroll
+                for (int c = 0; c < MINE; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(from + c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        float2 t[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) t[h] = make_float2(__uint_as_float(v[2 * (i + h)]), __uint_as_float(v[2 * (i + h) + 1]));
+                        if (EACH) {
+                            const float4 b = *(const float4*)(col_scale + slot * 256 + half * MINE + c + 2 * i);
+                            t[0] = mul2(t[0], make_float2(b.x, b.y));
+                            t[1] = mul2(t[1], make_float2(b.z, b.w));
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) sum[c / 2 + i + h] = fma2(t[h], s, sum[c / 2 + i + h]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
+                    else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
+                    mbar_arrive(&ctl->scale_empty[slot]);
+                }
+                if (++slot == kScaleSlots) { slot = 0; phase ^= 1u; }
+                if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+            }
+            if (!ok)                                          // a wait ran out: what is stored says so
+#pragma unroll
+                for (int i = 0; i < MINE / 2; ++i) sum[i] = make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
+            constexpr int PER = 64 / (int)sizeof(T);          // columns of a box
+#pragma unroll
+            for (int c = 0; c < MINE; c += PER) {
+                const int c1 = n0 + c;
+                if (c1 >= p.n) break;
+                if (a.boxes) { if (lane == 0) store_read(2); }
+                __syncwarp();
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < PER / 2; ++i) {
+                    float2 f = sum[c / 2 + i];
+                    const int j = c1 + 2 * i;
+                    if (p.bias) f = add2(f, make_float2(j < p.n ? dc_ld(p.bias + j) : 0.f, j + 1 < p.n ? dc_ld(p.bias + j + 1) : 0.f));
+                    if constexpr (sizeof(T) == 2) w[i] = p.relu ? two_bf16<true>(f) : two_bf16<false>(f);
+                    else {
+                        w[2 * i] = __float_as_uint(p.relu ? clamped<true>(f.x) : f.x);
+                        w[2 * i + 1] = __float_as_uint(p.relu ? clamped<true>(f.y) : f.y);
+                    }
+                }
+                // a lane's row of 64 bytes, its 16 bytes in another order for each two rows: no bank conflicts
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sts128(stage + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4), w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+                if (a.boxes) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && rows > 0) store_box(&tmC, stage, c1, (int)row0);
+                    stage ^= both_places;
+                    continue;
+                }
+                __syncwarp();
+                if (a.wide && c1 + PER <= p.n) {              // four lanes to 64 bytes
+                    const int u = lane & 3;
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) {
+                        const int r = it * 8 + (lane >> 2);
+                        if (r < rows) *(uint4*)((char*)p.out + (size_t)(row0 + r) * p.out_pitch + (size_t)c1 * sizeof(T) + u * 16) = lds128(stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
+                    }
+                } else {                                      // an element per lane, side by side
+                    constexpr int AT_ONCE = 32 / PER;         // rows
+                    const int e = lane & (PER - 1), u = e * (int)sizeof(T) >> 4;
+#pragma unroll 4
+                    for (int it = 0; it < 32 / AT_ONCE; ++it) {
+                        const int r = it * AT_ONCE + lane / PER;
+                        const uint32_t at = stage + r * 64 + ((u ^ ((r >> 1) & 3)) << 4) + (e * (int)sizeof(T) & 15);
+                        if (r < rows && c1 + e < p.n) {
+                            T* const out = (T*)((char*)p.out + (size_t)(row0 + r) * p.out_pitch) + c1 + e;
+                            if constexpr (sizeof(T) == 4) { uint32_t x; asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory"); *(uint32_t*)out = x; }
+                            else { uint16_t x; asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at) : "memory"); *(uint16_t*)out = x; }
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        if (a.boxes && lane == 0) store_done();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_all();                             // neither CTA frees tensor memory or leaves while the other may still use it
+    if (warp == 1) {
+        tc_fence_after();
+        if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kColumns) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kColumns) : "memory");
+    }
+}
+
+template <bool PAIR, int BN, bool EACH, typename T>
+int launch_blocks(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, const BlocksTiles& a, int ctas, int device, cudaStream_t stream)
+{
+    static dc_once_per_device attr_set;
+    DC_CUDA(attr_set.ensure(device, [] {
+        // the warps that add up take registers that the others give back: 128 * 56 + 256 * 224 = 384 * 168 in all
+        cudaFuncAttributes at;
+        cudaError_t e = cudaFuncGetAttributes(&at, k_blocks<PAIR, BN, EACH, T>);
+        if (e == cudaSuccess && BN == 256 && at.numRegs < 168) return cudaErrorInvalidKernelImage;
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(k_blocks<PAIR, BN, EACH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem);
+    }));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PAIR ? 2 : 1; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)ctas); cfg.blockDim = dim3(kBlocksThreads); cfg.dynamicSmemBytes = kBlocksSmem; cfg.stream = stream;
+    cfg.attrs = g_dc_pdl ? attr : attr + 1; cfg.numAttrs = g_dc_pdl ? 2 : 1;
+    DC_CUDA(cudaLaunchKernelEx(&cfg, k_blocks<PAIR, BN, EACH, T>, tmA, tmB, tmC, a));
+    return DC_OK;
+}
+
+int launch_product(const BlocksProduct& p, int dtype, int device, int num_sms, cudaStream_t stream)
+{
+    BlocksTiles a = {};
+    a.p = p;
+    a.m_tiles = (int)((p.m + kTileM - 1) / kTileM);
+    const int elt = dtype == DC_BF16 ? 2 : 4;
+    a.kb = dc_div_up(p.k, kBytesK);
+    bool pair = false;
+    int BN = 64;
+    double best = 0.0;
+    for (int c = 0; c < 4; ++c) {
+        const bool two = c < 2;
+        const int bn = c == 0 ? 256 : c == 3 ? 64 : 128;
+        const long long n_items = (two ? (a.m_tiles + 1) / 2 : a.m_tiles) * (long long)dc_div_up(p.n, bn), at_once = two ? num_sms / 2 : num_sms, rounds = (n_items + at_once - 1) / at_once;
+        const double load = a.kb * (double)(kATile + (two ? bn / 2 : bn) * kBytesK) / 50.0, mma = a.kb * 2.0 * bn, out = 128.0 * bn * elt / 24.0;
+        const double cost = rounds * ((load > mma ? load : mma) + out + 500.0);
+        if (c == 0 || cost < best) { best = cost; pair = two; BN = bn; }
+    }
+    a.NB = dc_div_up(p.n, BN);
+    const int b_rows = pair ? BN / 2 : BN;
+    a.stage_bytes = kATile + b_rows * kBytesK;
+    a.stages = kBlocksRoom / a.stage_bytes;
+    if (a.stages > kBlocksMostStages) a.stages = kBlocksMostStages;
+    a.k_last = dc_div_up(p.k - (a.kb - 1) * kBytesK, 32);
+    // float32 accumulators, both operands e4m3, K-major
+    a.idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((pair ? 256 : 128) >> 4) << 24);
+    a.wide = (uintptr_t)p.out % 16 == 0 && p.out_pitch % 16 == 0;
+    CUtensorMap tmA, tmB, tmC = {};
+    if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
+    if (a.wide && (size_t)p.n * elt % 16 == 0) a.boxes = encode_out(&tmC, p.out, p.out_pitch, p.m, p.n, elt);
+    const long long items = (pair ? (a.m_tiles + 1) / 2 : a.m_tiles) * (long long)a.NB, cap = pair ? num_sms / 2 : num_sms;
+    if (items >= 0x70000000) return DC_ERR_LIMIT;
+    const int ctas = (int)(items < cap ? items : cap) * (pair ? 2 : 1);
+#define DC_BLOCKS(PAIR, BN, EACH, T) return launch_blocks<PAIR, BN, EACH, T>(tmA, tmB, tmC, a, ctas, device, stream)
+#define DC_BLOCKS_OF(EACH, T) do { if (pair && BN == 256) DC_BLOCKS(true, 256, EACH, T); if (pair) DC_BLOCKS(true, 128, EACH, T); if (BN == 128) DC_BLOCKS(false, 128, EACH, T); DC_BLOCKS(false, 64, EACH, T); } while (0)
+#define DC_BLOCKS_TO(T) do { if (p.b_block_rows == 1) DC_BLOCKS_OF(true, T); DC_BLOCKS_OF(false, T); } while (0)
+    if (dtype == DC_BF16) DC_BLOCKS_TO(__nv_bfloat16);
+    DC_BLOCKS_TO(float);
+#undef DC_BLOCKS_TO
+#undef DC_BLOCKS_OF
+#undef DC_BLOCKS
+}
+
+template <typename T>
+cudaError_t launch_quantize(const BlocksArgs& a, bool wide, cudaStream_t stream)
+{
+    const dim3 grid((unsigned)((int64_t)a.kb * a.rb));
+    if (a.qt) return wide ? dc_launch_pdl(k_quantize_blocks<T, true, true>, grid, 256, 0, stream, a) : dc_launch_pdl(k_quantize_blocks<T, false, true>, grid, 256, 0, stream, a);
+    return wide ? dc_launch_pdl(k_quantize_blocks<T, true, false>, grid, 256, 0, stream, a) : dc_launch_pdl(k_quantize_blocks<T, false, false>, grid, 256, 0, stream, a);
+}
+
+int quantize(BlocksArgs& a, int dtype, cudaStream_t stream)
+{
+    a.kb = dc_div_up(a.channels, 128); a.rb = (int)(((int64_t)a.rows + 127) / 128);
+    if ((int64_t)a.kb * a.rb > 0x7fffffff) return DC_ERR_LIMIT;
+    const bool wide = (uintptr_t)a.x % 16 == 0 && (a.rows < 2 || a.x_pitch % 16 == 0);
+    DC_CUDA(dtype == DC_BF16 ? launch_quantize<__nv_bfloat16>(a, wide, stream) : launch_quantize<float>(a, wide, stream));
+    return DC_OK;
+}
+
+bool floats_ok(const float* p) { return (uintptr_t)p % sizeof(float) == 0; }
+bool bytes_ok(const uint8_t* q, size_t pitch, const float* scale, int64_t rows, int64_t columns)
+{
+    return q && scale && floats_ok(scale) && (uintptr_t)q % 16 == 0 && pitch % 16 == 0 && (rows < 2 || pitch >= (size_t)columns);
+}
+// What both products ask of their operands.
+int product_check(const uint8_t* b, size_t b_pitch, const float* b_scale, int32_t b_block_rows, const float* bias, int64_t m, int32_t n, int32_t k, int32_t dtype, const void* out, size_t out_pitch)
+{
+    if ((dtype != DC_FP32 && dtype != DC_BF16) || (b_block_rows != 1 && b_block_rows != 128)) return DC_ERR_CONFIG;
+    const int elt = dtype == DC_BF16 ? 2 : 4;
+    if (m < 0 || n < 1 || k < 1) return DC_ERR_ARG;
+    if (m > DC_MOST_ROWS || n > (1 << 28) || (n > 1 && b_pitch > kMostPitch)) return DC_ERR_LIMIT;
+    if (m == 0) return DC_OK;
+    if (!bytes_ok(b, b_pitch, b_scale, n, k) || !out) return DC_ERR_ARG;
+    if (!floats_ok(bias) || (uintptr_t)out % elt || out_pitch % elt || (m > 1 && out_pitch < (size_t)n * elt)) return DC_ERR_ARG;
+    return DC_OK;
+}
+size_t blocks_pitch(int64_t k) { return (size_t)(k + 15) / 16 * 16; }
+
+}  // namespace
+
+extern "C" {
+
+int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t channels, int32_t dtype, int32_t block_rows, uint8_t* q_dev, size_t q_pitch, float* scale_dev,
+                       uint8_t* qt_dev, size_t qt_pitch, float* scale_t_dev, void* cuda_stream)
+{
+    if ((dtype != DC_FP32 && dtype != DC_BF16) || (block_rows != 1 && block_rows != 128)) return DC_ERR_CONFIG;
+    const int elt = dtype == DC_BF16 ? 2 : 4;
+    if (rows < 0 || channels < 1 || !q_dev != !scale_dev || !qt_dev != !scale_t_dev) return DC_ERR_ARG;
+    if (rows > DC_MOST_ROWS || (rows > 1 && x_pitch > 0xffffffffu) || (q_dev && rows > 1 && q_pitch > kMostPitch) || (qt_dev && channels > 1 && qt_pitch > kMostPitch)) return DC_ERR_LIMIT;
+    if (rows == 0 || (!q_dev && !qt_dev)) return DC_OK;
+    if (!x_dev || (uintptr_t)x_dev % elt || x_pitch % elt || (rows > 1 && x_pitch < (size_t)channels * elt)) return DC_ERR_ARG;
+    if ((q_dev && !bytes_ok(q_dev, q_pitch, scale_dev, rows, channels)) || (qt_dev && !bytes_ok(qt_dev, qt_pitch, scale_t_dev, channels, rows))) return DC_ERR_ARG;
+    BlocksArgs a = {};
+    a.x = x_dev; a.x_pitch = x_pitch; a.rows = (int)rows; a.channels = channels; a.block_rows = block_rows;
+    a.q = q_dev; a.q_pitch = q_pitch; a.scale = scale_dev; a.qt = qt_dev; a.qt_pitch = qt_pitch; a.scale_t = scale_t_dev;
+    return quantize(a, dtype, (cudaStream_t)cuda_stream);
+}
+
+int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const uint8_t* b_dev, size_t b_pitch, const float* b_scale_dev, int32_t b_block_rows,
+                     const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype, void* out_dev, size_t out_pitch, void* cuda_stream)
+{
+    int rc = product_check(b_dev, b_pitch, b_scale_dev, b_block_rows, bias_dev, m, n, k, dtype, out_dev, out_pitch);
+    if (rc != DC_OK || m == 0) return rc;
+    if (m > 1 && a_pitch > kMostPitch) return DC_ERR_LIMIT;
+    if (!bytes_ok(a_dev, a_pitch, a_scale_dev, m, k)) return DC_ERR_ARG;
+    int device = 0, sms = 0;
+    if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
+    const BlocksProduct p = {a_dev, a_pitch, a_scale_dev, b_dev, b_pitch, b_scale_dev, bias_dev, m, n, k, relu, b_block_rows, out_dev, out_pitch};
+    return launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
+}
+
+int dc_linear_blocks_workspace(int64_t m, int32_t k, size_t* bytes)
+{
+    if (m < 0 || k < 1 || !bytes) return DC_ERR_ARG;
+    *bytes = (size_t)m * (blocks_pitch(k) + sizeof(float) * dc_div_up(k, 128)) + 256;
+    return DC_OK;
+}
+
+int dc_linear_blocks(const void* x_dev, size_t x_pitch, const uint8_t* w_dev, size_t w_pitch, const float* w_scale_dev, int32_t w_block_rows, const float* bias_dev, int64_t m, int32_t n,
+                     int32_t k, int32_t relu, int32_t dtype, void* out_dev, size_t out_pitch, void* workspace_dev, size_t workspace_bytes, void* cuda_stream)
+{
+    int rc = product_check(w_dev, w_pitch, w_scale_dev, w_block_rows, bias_dev, m, n, k, dtype, out_dev, out_pitch);
+    if (rc != DC_OK || m == 0) return rc;
+    const int elt = dtype == DC_BF16 ? 2 : 4;
+    size_t need = 0;
+    dc_linear_blocks_workspace(m, k, &need);
+    if (m > 1 && x_pitch > 0xffffffffu) return DC_ERR_LIMIT;
+    if (!x_dev || (uintptr_t)x_dev % elt || x_pitch % elt || (m > 1 && x_pitch < (size_t)k * elt) || !workspace_dev || workspace_bytes < need) return DC_ERR_ARG;
+    int device = 0, sms = 0;
+    if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
+    const size_t pitch = blocks_pitch(k);
+    uint8_t* const q = (uint8_t*)(((uintptr_t)workspace_dev + 255) & ~(uintptr_t)255);
+    float* const scale = (float*)(q + (size_t)m * pitch);
+    BlocksArgs a = {};
+    a.x = x_dev; a.x_pitch = x_pitch; a.rows = (int)m; a.channels = k; a.block_rows = 1; a.q = q; a.q_pitch = pitch; a.scale = scale;
+    if ((rc = quantize(a, dtype, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
+    const BlocksProduct p = {q, pitch, scale, w_dev, w_pitch, w_scale_dev, bias_dev, m, n, k, relu, w_block_rows, out_dev, out_pitch};
+    return launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

@@ -12,14 +12,10 @@
 // product than a CTA alone has.
 #include <atomic>
 
-#include "dc_rows.cuh"
-#include "dc_tcgen05.cuh"
+#include "dc_product.cuh"
 
 namespace {
 
-constexpr unsigned long long kWaitNs = 2000000000ull;        // every wait on the device
-constexpr int kBytesK = 128;                                  // a stage: 128 values of K
-constexpr int kTileM = 128, kATile = kTileM * kBytesK;
 constexpr int kMaxStages = 9;
 constexpr int kEpiWarps = 16, kThreads = (2 + kEpiWarps) * 32;
 constexpr int kStage = 32 * 64;                               // a warp's 32 rows on their way out, 64 bytes each
@@ -57,15 +53,6 @@ DC_UMMA_I8(umma_i8, "cta_group::1")
 DC_UMMA_I8(umma_i8_pair, "cta_group::2")
 #undef DC_UMMA_I8
 
-__device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* tm, int c0, int c1, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1) : "memory");
-}
-__device__ __forceinline__ void commit_pair(uint32_t bar)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
 __device__ __forceinline__ bool wait_at(uint32_t bar, uint32_t parity, Ctl* ctl, int32_t* status)
 {
     return mbar_wait_at(bar, parity, &ctl->abort_flag, &ctl->wait_ns, status);
@@ -80,19 +67,6 @@ __device__ __forceinline__ float2 finish2(uint32_t a0, uint32_t a1, float sa, fl
         : "=f"(f.x), "=f"(f.y) : "f"((float)(int)a0), "f"((float)(int)a1), "f"(sa), "f"(s.x), "f"(s.y), "f"(b.x), "f"(b.y));
     return f;
 }
-// ReLU or nothing; a NaN stays.
-template <bool RELU> __device__ __forceinline__ float clamped(float v)
-{
-    if (RELU) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v));
-    return v;
-}
-template <bool RELU> __device__ __forceinline__ uint32_t two_bf16(float2 a)
-{
-    uint32_t r;
-    if (RELU) asm("cvt.rn.relu.bf16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a.x), "f"(a.y));
-    else asm("cvt.rn.bf16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a.x), "f"(a.y));
-    return r;
-}
 // Sixteen rows x 32 columns of tensor memory: column group j (8 columns) in r[4 j ...]; a lane has columns 2 (lane % 4), + 1 of rows lane / 4
 // (r[4 j], r[4 j + 1]) and lane / 4 + 8.
 __device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t* r)
@@ -105,18 +79,6 @@ __device__ __forceinline__ void stmatrix4(uint32_t addr, uint32_t a, uint32_t b,
 {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// A warp's staged 32 rows of 64 bytes on their way to out; lane 0 issues.
-__device__ __forceinline__ void store_box(const CUtensorMap* tm, uint32_t stage, int col, int row)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(stage), "r"(col), "r"(row) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-__device__ __forceinline__ void store_read(int bufs)          // the place that comes next is free
-{
-    if (bufs == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-    else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-}
-__device__ __forceinline__ void store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // The scales and biases of two neighbouring columns in each of four groups of eight, from `col` on; beyond the last column: zeros.  (dc_ld: the
 // kernel before may have written them.)
 __device__ __forceinline__ void column_weights(const dc_product_args& p, int col, bool whole, float2* s, float2* b)
@@ -571,43 +533,6 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_product_split(const __grid
     }
 }
 
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encode_fn()
-{
-    static std::atomic<EncodeFn> known;
-    EncodeFn fn = known.load(std::memory_order_relaxed);
-    if (!fn) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess) known.store(fn = (EncodeFn)p, std::memory_order_relaxed);
-        cudaGetLastError();
-    }
-    return fn;
-}
-
-// Rows of 8-bit values in boxes of box_rows x 128 bytes; zeros beyond the last row and the last value.
-bool encode_rows(CUtensorMap* tm, const void* base, size_t pitch, int64_t rows, int k, int box_rows)
-{
-    EncodeFn enc = encode_fn();
-    if (!enc) return false;
-    if (rows < 2) pitch = dc_quant_pitch(k);                                   // a single row's is anything
-    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {(cuuint32_t)kBytesK, (cuuint32_t)box_rows}, elem[2] = {1, 1};
-    return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, (void*)base, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// out in boxes of 32 rows x 64 bytes; rows of whole 16 bytes, beyond which nothing is written, nor beyond the last row.
-bool encode_out(CUtensorMap* tm, const dc_product_args& p, int elt)
-{
-    const size_t pitch = p.m < 2 ? ((size_t)p.n * elt + 15) / 16 * 16 : p.out_pitch;
-    const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m}, strides[1] = {(cuuint64_t)pitch};
-    const cuuint32_t box[2] = {(cuuint32_t)(64 / elt), 32}, elem[2] = {1, 1};
-    return encode_fn()(tm, elt == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p.out, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
-                       CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <bool PAIR, bool LIST, bool RELU, typename T>
 int launch_product(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, const ProductArgs& a, int ctas, int device, cudaStream_t stream)
 {
@@ -736,7 +661,7 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
     CUtensorMap tmA, tmB, tmC = {};
     if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
     // (a box is cut at whole 16 bytes, not at the row's last column)
-    if (a.wide && !p.padded && (size_t)p.n * elt % 16 == 0) a.boxes = encode_out(&tmC, p, dtype == DC_BF16 ? 2 : 4);
+    if (a.wide && !p.padded && (size_t)p.n * elt % 16 == 0) a.boxes = encode_out(&tmC, p.out, p.out_pitch, p.m, p.n, elt);
     const long long items = (pair ? (tiles + 1) / 2 : tiles) * a.NB, cap = pair ? num_sms / 2 : num_sms;
     if (items >= 0x70000000) return DC_ERR_LIMIT;
     const int ctas = (int)(items < cap ? items : cap) * (pair ? 2 : 1);
@@ -751,7 +676,6 @@ int dc_launch_product(const dc_product_args& p, int dtype, int device, int num_s
 }
 
 constexpr int kMostTerms = 131071;
-constexpr size_t kMostPitch = ((size_t)1 << 40) - 16;          // of operands: what a tensor map takes
 
 // What both products ask of their operands.
 static int product_check(const int8_t* b, size_t b_pitch, const float* b_scale, const float* bias, int64_t m, int32_t n, int32_t k, int32_t dtype, const void* out, size_t out_pitch)

@@ -208,6 +208,150 @@ int linear_quantized(PyObject* const* o)         // x, w, w_scale, bias, out, re
                                work ? work->data_ptr() : nullptr, work ? work->nbytes() : 0, p.stream);
 }
 
+// ---- group normalisation, 8-bit floating point ----
+// [maps, ..., channels]: the first dimension counts images, the last one channels.
+int64_t maps_of(const at::Tensor& t, const char* what)
+{
+    if (t.dim() < 2) throw Refused{PyExc_ValueError, std::string(what) + ": [maps, ..., channels] is needed"};
+    return t.size(0);
+}
+int64_t pixels_of(const at::Tensor& t)
+{
+    int64_t n = 1;
+    for (int64_t d = 1; d < t.dim() - 1; ++d) n *= t.size(d);
+    return n;
+}
+int32_t count(PyObject* o, const char* what)
+{
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Refused{nullptr, ""};
+    if (v < INT32_MIN || v > INT32_MAX) throw Refused{PyExc_ValueError, std::string(what) + " is out of range"};
+    return (int32_t)v;
+}
+int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Rows of e4m3.
+Rows bytes_of(const at::Tensor& t, const char* what)
+{
+    if (t.scalar_type() != at::kFloat8_e4m3fn && t.scalar_type() != at::kByte)
+        throw Refused{PyExc_TypeError, std::string(what) + ": unsupported type " + c10::toString(t.scalar_type()) + " (float8_e4m3fn, or uint8 that holds its bits)"};
+    if (t.dim() != 2) throw Refused{PyExc_ValueError, std::string(what) + ": two dimensions are needed"};
+    Rows r;
+    r.rows = t.size(0); r.channels = t.size(1); r.at = t.data_ptr();
+    if (r.channels > 1 && t.stride(1) != 1) throw Refused{PyExc_ValueError, std::string(what) + ": a row's elements have to lie side by side"};
+    r.pitch = r.rows > 1 ? (size_t)t.stride(0) : (size_t)((r.channels + 15) / 16 * 16);
+    return r;
+}
+float* table_of(const at::Tensor* t, int64_t rows, int64_t columns, const char* what)
+{
+    if (!t) return nullptr;
+    if (t->scalar_type() != at::kFloat || t->dim() != 2 || t->size(0) != rows || t->size(1) != columns || !t->is_contiguous())
+        throw Refused{PyExc_ValueError, std::string(what) + ": a contiguous float32 tensor [" + std::to_string(rows) + ", " + std::to_string(columns) + "] is needed"};
+    return (float*)t->data_ptr();
+}
+// Scales of b: for 128 of its rows, or for each.  (The same for a single row.)
+int32_t block_rows_of(const at::Tensor* t, int64_t rows, int64_t blocks, const char* what, float** at)
+{
+    if (!t) throw Refused{PyExc_ValueError, std::string(what) + " is needed"};
+    const bool each = t->dim() == 2 && t->size(0) == rows && rows != ceil_of(rows, 128);
+    *at = table_of(t, each ? rows : ceil_of(rows, 128), blocks, what);
+    return each ? 1 : 128;
+}
+void whole(const at::Tensor* work)
+{
+    if (work && !work->is_contiguous()) throw Refused{PyExc_ValueError, "workspace: has to be contiguous"};
+}
+
+int group_norm(PyObject* const* o)       // x, groups, gamma, beta, y, mean, rstd, activation, eps, workspace, stream
+{
+    const at::Tensor *x = tensor(o[0], "x"), *gamma = tensor(o[2], "gamma", true), *beta = tensor(o[3], "beta", true), *y = tensor(o[4], "y"), *mean = tensor(o[5], "mean", true),
+                     *rstd = tensor(o[6], "rstd", true), *work = tensor(o[9], "workspace", true);
+    const int32_t groups = count(o[1], "groups"), activation = count(o[7], "activation");
+    const Rows xr = rows_of(*x, "x"), yr = rows_of(*y, "y");
+    same(xr, yr, "y");
+    const int64_t maps = maps_of(*x, "x"), pixels = pixels_of(*x);
+    const float *g = vector_of(gamma, xr.channels, "gamma"), *b = vector_of(beta, xr.channels, "beta");
+    float *m = vector_of(mean, maps * groups, "mean"), *r = vector_of(rstd, maps * groups, "rstd");
+    whole(work);
+    const double eps = number(o[8]);
+    const Place p("dc_group_norm", {x, y, gamma, beta, mean, rstd, work}, o[10]);
+    const WithoutGil call;
+    return dc_group_norm(xr.at, xr.pitch, g, b, maps, pixels, channels_of(xr), groups, eps, activation, xr.dtype, yr.at, yr.pitch, m, r, work ? work->data_ptr() : nullptr,
+                         work ? work->nbytes() : 0, p.stream);
+}
+
+int group_norm_backward(PyObject* const* o)      // dy, x, groups, gamma, beta, mean, rstd, dx, dgamma, dbeta, activation, workspace, stream
+{
+    const at::Tensor *dy = tensor(o[0], "dy"), *x = tensor(o[1], "x"), *gamma = tensor(o[3], "gamma", true), *beta = tensor(o[4], "beta", true), *mean = tensor(o[5], "mean", true),
+                     *rstd = tensor(o[6], "rstd", true), *dx = tensor(o[7], "dx", true), *dgamma = tensor(o[8], "dgamma", true), *dbeta = tensor(o[9], "dbeta", true),
+                     *work = tensor(o[11], "workspace", true);
+    const int32_t groups = count(o[2], "groups"), activation = count(o[10], "activation");
+    const Rows xr = rows_of(*x, "x"), dr = rows_of(*dy, "dy");
+    same(xr, dr, "dy");
+    Rows ox;
+    if (dx) { ox = rows_of(*dx, "dx"); same(xr, ox, "dx"); }
+    const int64_t maps = maps_of(*x, "x"), pixels = pixels_of(*x);
+    const float *g = vector_of(gamma, xr.channels, "gamma"), *b = vector_of(beta, xr.channels, "beta"), *m = vector_of(mean, maps * groups, "mean", false),
+                *r = vector_of(rstd, maps * groups, "rstd", false);
+    float *dg = vector_of(dgamma, xr.channels, "dgamma"), *db = vector_of(dbeta, xr.channels, "dbeta");
+    whole(work);
+    const Place p("dc_group_norm_backward", {x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, work}, o[12]);
+    const WithoutGil call;
+    return dc_group_norm_backward(dr.at, dr.pitch, xr.at, xr.pitch, g, b, m, r, maps, pixels, channels_of(xr), groups, activation, xr.dtype, ox.at, ox.pitch, dg, db,
+                                  work ? work->data_ptr() : nullptr, work ? work->nbytes() : 0, p.stream);
+}
+
+int quantize_blocks(PyObject* const* o)  // x, q, scale, q_t, scale_t, block_rows, stream
+{
+    const at::Tensor *x = tensor(o[0], "x"), *q = tensor(o[1], "q", true), *scale = tensor(o[2], "scale", true), *qt = tensor(o[3], "q_t", true), *scale_t = tensor(o[4], "scale_t", true);
+    const int32_t block = count(o[5], "block_rows");
+    const Rows xr = rows_of(*x, "x");
+    const int64_t by = block == 128 ? 128 : 1;
+    Rows qr, tr;
+    if (q) { qr = bytes_of(*q, "q"); same(xr, qr, "q", false); }
+    if (qt) {
+        tr = bytes_of(*qt, "q_t");
+        if (tr.rows != xr.channels || tr.channels != xr.rows)
+            throw Refused{PyExc_ValueError, "q_t: [" + std::to_string(xr.channels) + ", " + std::to_string(xr.rows) + "] is needed"};
+    }
+    float *s = table_of(scale, ceil_of(xr.rows, by), ceil_of(xr.channels, 128), "scale"), *st = table_of(scale_t, ceil_of(xr.channels, by), ceil_of(xr.rows, 128), "scale_t");
+    const Place p("dc_quantize_blocks", {x, q, scale, qt, scale_t}, o[6]);
+    const WithoutGil call;
+    return dc_quantize_blocks(xr.at, xr.pitch, xr.rows, channels_of(xr), xr.dtype, block, (uint8_t*)qr.at, qr.pitch, s, (uint8_t*)tr.at, tr.pitch, st, p.stream);
+}
+
+int matmul_blocks(PyObject* const* o)    // a, a_scale, b, b_scale, bias, out, relu, stream
+{
+    const at::Tensor *a = tensor(o[0], "a"), *as = tensor(o[1], "a_scale"), *b = tensor(o[2], "b"), *bs = tensor(o[3], "b_scale"), *bias = tensor(o[4], "bias", true), *out = tensor(o[5], "out");
+    const Rows ar = bytes_of(*a, "a"), br = bytes_of(*b, "b"), r = rows_of(*out, "out");
+    fit(ar, br, r);
+    const int64_t blocks = ceil_of(ar.channels, 128);
+    float* sb;
+    const float *sa = table_of(as, ar.rows, blocks, "a_scale"), *c = vector_of(bias, br.rows, "bias");
+    const int32_t by = block_rows_of(bs, br.rows, blocks, "b_scale", &sb);
+    const int relu = truth(o[6]);
+    const Place p("dc_matmul_blocks", {a, b, as, bs, bias, out}, o[7]);
+    const WithoutGil call;
+    return dc_matmul_blocks((const uint8_t*)ar.at, ar.pitch, sa, (const uint8_t*)br.at, br.pitch, sb, by, c, ar.rows, (int32_t)br.rows, channels_of(ar), relu, r.dtype, r.at, r.pitch, p.stream);
+}
+
+int linear_blocks(PyObject* const* o)    // x, w, w_scale, bias, out, relu, workspace, stream
+{
+    const at::Tensor *x = tensor(o[0], "x"), *w = tensor(o[1], "w"), *ws = tensor(o[2], "w_scale"), *bias = tensor(o[3], "bias", true), *out = tensor(o[4], "out"),
+                     *work = tensor(o[6], "workspace", true);
+    const Rows xr = rows_of(*x, "x"), wr = bytes_of(*w, "w"), r = rows_of(*out, "out");
+    fit(xr, wr, r);
+    if (xr.dtype != r.dtype) throw Refused{PyExc_TypeError, "x and out differ in type"};
+    whole(work);
+    float* sw;
+    const int32_t by = block_rows_of(ws, wr.rows, ceil_of(wr.channels, 128), "w_scale", &sw);
+    const float* c = vector_of(bias, wr.rows, "bias");
+    const int relu = truth(o[5]);
+    const Place p("dc_linear_blocks", {x, w, ws, bias, out, work}, o[7]);
+    const WithoutGil call;
+    return dc_linear_blocks(xr.at, xr.pitch, (const uint8_t*)wr.at, wr.pitch, sw, by, c, xr.rows, (int32_t)wr.rows, channels_of(xr), relu, xr.dtype, r.at, r.pitch,
+                            work ? work->data_ptr() : nullptr, work ? work->nbytes() : 0, p.stream);
+}
+
 // Every function returns the call's status; nothing is thrown into Python.
 template <int (*CALL)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
@@ -227,7 +371,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n)
 
 #define DC_ENTRY(name, n) {#name, (PyCFunction)(void (*)(void))entry<name, n>, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {DC_ENTRY(layer_norm, 8), DC_ENTRY(layer_norm_backward, 10), DC_ENTRY(quantize_rows, 4), DC_ENTRY(layer_norm_quantize, 8),
-                          DC_ENTRY(matmul_quantized, 8), DC_ENTRY(linear_quantized, 8), {nullptr, nullptr, 0, nullptr}};
+                          DC_ENTRY(matmul_quantized, 8), DC_ENTRY(linear_quantized, 8),
+                          DC_ENTRY(group_norm, 11), DC_ENTRY(group_norm_backward, 13), DC_ENTRY(quantize_blocks, 7), DC_ENTRY(matmul_blocks, 8), DC_ENTRY(linear_blocks, 8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_tensors", "Torch tensors to libdeepcache's entry points on maps of the caller's own.  " DC_BUILT_FOR, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
