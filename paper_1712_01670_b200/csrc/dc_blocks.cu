@@ -213,11 +213,12 @@ struct BlocksTiles {
     BlocksProduct p;
     int NB, m_tiles, stages, stage_bytes, kb, k_last;         // column tiles; blocks of K; MMAs (32 values) of the last one
     uint32_t idesc;
+    int bufs;                                                 // places a warp stages its boxes in, 1 or 2
     int wide, boxes;                                          // out takes 16-byte stores; is written in boxes by TMA
 };
 
 constexpr int kAddWarps = 8, kBlocksThreads = (4 + kAddWarps) * 32;
-constexpr int kBlocksMostStages = 8, kScaleSlots = 4;
+constexpr int kBlocksMostStages = 8, kScaleSlots = 3;         // a slot: the scales of four blocks of K
 constexpr int kBox = 32 * 64;                                 // a warp's 32 rows on their way out, 64 bytes each; two of them
 struct BlocksCtl {
     unsigned long long full[kBlocksMostStages], empty[kBlocksMostStages], tmem_full[2], tmem_empty[2], scale_full[kScaleSlots], scale_empty[kScaleSlots];
@@ -226,8 +227,8 @@ struct BlocksCtl {
     unsigned long long wait_ns;
 };
 constexpr int kBlocksSmem = 227 * 1024;
-constexpr int kScaleBytes = kScaleSlots * (2 * 128 + 256) * 4;
-constexpr int kBlocksRoom = kBlocksSmem - 1024 - (int)sizeof(BlocksCtl) - kScaleBytes - kAddWarps * 2 * kBox;
+constexpr int kRowScales = 128 * 4, kScaleBytes = kScaleSlots * (kRowScales + 8) * 4, kEachBytes = kScaleSlots * (kRowScales + 4 * 256) * 4;
+constexpr int kBlocksRoom = kBlocksSmem - 1024 - (int)sizeof(BlocksCtl);
 
 #define DC_UMMA_F8(name, group)                                                                                                                 \
     __device__ __forceinline__ void name(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, int n)                            \
@@ -242,9 +243,69 @@ DC_UMMA_F8(umma_f8, "cta_group::1")
 DC_UMMA_F8(umma_f8_pair, "cta_group::2")
 #undef DC_UMMA_F8
 
+// A bounded wait, of one thread or (WARP) of a whole warp.  What bounds the loops that wait is the instructions from one block of K to the next, so a wait that is over
+// at once is a look, a vote and nothing else; the clock is looked at after 256 looks.
+template <bool WARP>
 __device__ __forceinline__ bool blocks_wait(uint32_t bar, uint32_t parity, BlocksCtl* ctl)
 {
-    return mbar_wait_at(bar, parity, &ctl->abort_flag, &ctl->wait_ns, &g_blocks_status);
+    unsigned long long t0 = 0;
+#pragma unroll 1
+    for (uint32_t spin = 0;; ++spin) {
+        bool done = mbar_try(bar, parity);
+        if (WARP) done = __all_sync(0xffffffffu, done);
+        if (done) return true;
+        if ((spin & 255u) == 255u) {
+            const unsigned long long t = now_ns();
+            if (spin == 255u) t0 = t;
+            bool over = ctl->abort_flag != 0 || t - t0 > ctl->wait_ns;
+            if (WARP) over = __any_sync(0xffffffffu, over);
+            if (over) {
+                ctl->abort_flag = 1;
+                atomicExch(&g_blocks_status, (int)DC_ERR_TIMEOUT);
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ float4 lds_floats(uint32_t at)
+{
+    const uint4 v = lds128(at);
+    return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+}
+// Two floats in one 64-bit register, as packed arithmetic has them: as pairs of 32-bit registers the sums were moved about, an instruction for each product.
+__device__ __forceinline__ uint64_t pair_of(uint32_t a, uint32_t b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float2 floats_of(uint64_t v)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
+__device__ __forceinline__ void add_product(uint64_t& sum, uint64_t a, uint64_t b) { asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(sum) : "l"(a), "l"(b)); }
+__device__ __forceinline__ uint64_t product(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ void lds_pairs(uint32_t at, uint64_t* v) { asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at)); }
+// N floats from global into shared memory; zeros where there are none (`any`: an address that is).
+template <int N>
+__device__ __forceinline__ void copy_floats(uint32_t dst, const float* src, const float* any, bool there)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(there ? src : any), "r"(there ? 4 * N : 0), "n"(4 * N) : "memory");
+}
+// The wait for a load of 32 columns, which names them: nothing that reads them comes before it.
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t* r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
+                   "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]),
+                   "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]) :: "memory");
 }
 
 // BN: columns of a tile.  EACH: b has a scale for each row and block, not for 128 rows.
@@ -254,9 +315,10 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* const staging = ring + a.stages * a.stage_bytes;
-    float* const row_scale = (float*)(staging + kAddWarps * 2 * kBox);       // [slots][2][128]: of the rows, for either 128 columns
-    float* const col_scale = row_scale + kScaleSlots * 256;                  // [slots][256]: EACH
-    BlocksCtl* const ctl = (BlocksCtl*)(col_scale + kScaleSlots * 256);
+    float* const row_scale = (float*)(staging + kAddWarps * a.bufs * kBox);  // [slots][128 rows][4 blocks]
+    float* const col_scale = row_scale + kScaleSlots * kRowScales;           // EACH: [slots][4 blocks][256 columns]; else [slots][2][4 blocks]: of either 128 columns
+    constexpr int kCols = EACH ? 4 * 256 : 8;
+    BlocksCtl* const ctl = (BlocksCtl*)(col_scale + kScaleSlots * kCols);
     const BlocksProduct& p = a.p;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
@@ -266,7 +328,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], kAddWarps * M); }
-        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 1); mbar_init(&ctl->scale_empty[i], kAddWarps); }
+        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 32); mbar_init(&ctl->scale_empty[i], kAddWarps); }
         ctl->abort_flag = 0;
         ctl->wait_ns = kWaitNs;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -310,7 +372,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 for (int item = first; item < n_items && ok; item += step) {
                     const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * BN + rank * (BN / 2);
                     for (int kc = 0; kc < a.kb; ++kc) {
-                        ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
+                        ok = blocks_wait<false>(empty0 + r.off, r.phase ^ 1u, ctl);
                         if (!ok) break;
                         if (PAIR) {
                             if (rank == 0) mbar_expect_tx(full0 + r.off, 2u * (uint32_t)a.stage_bytes);
@@ -328,74 +390,81 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
             }
             __syncwarp();
-        } else if (warp == 1) {
-            // ---------------- MMA issuer (of a pair: the leader's, for both CTAs) ----------------
+        } else if (warp < 3) {
+            // ---------------- MMA issuers (of a pair: the leader's, for both CTAs) ----------------
+            // Each block of K has an accumulator of its own, so two warps issue in turns: two waits, four MMAs and two commits take one warp 1000 cycles, a block's
+            // MMAs 512.
             if (rank == 0 && elect_one()) {
                 const uint64_t dconst = umma_desc(0, 1024, 2);
                 const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
+                const uint32_t mine = (uint32_t)warp - 1u, d = tmem_base + mine * (uint32_t)BN;
+                const uint32_t my_empty = smem_u32(&ctl->tmem_empty[mine]), my_full = smem_u32(&ctl->tmem_full[mine]);
                 RingPos r;
                 r.start(r0, (uint32_t)a.stages);
-                uint32_t acc = 0, acc_ph = 0;
+                uint32_t turn = 0, acc_ph = 1;
                 bool ok = true;
                 for (int item = first; item < n_items && ok; item += step)
-                    for (int kc = 0; kc < a.kb; ++kc) {
-                        ok = blocks_wait(smem_u32(&ctl->tmem_empty[acc]), acc_ph ^ 1u, ctl) && blocks_wait(full0 + r.off, r.phase, ctl);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const int n = kc + 1 < a.kb ? 4 : a.k_last;
-                        const uint32_t d = tmem_base + acc * (uint32_t)BN;
-                        if (PAIR) {
-                            umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
-                            commit_pair(empty0 + r.off);
-                            commit_pair(smem_u32(&ctl->tmem_full[acc]));
-                        } else {
-                            umma_f8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
-                            umma_commit_at(empty0 + r.off);
-                            umma_commit(&ctl->tmem_full[acc]);
+                    for (int kc = 0; kc < a.kb; ++kc, turn ^= 1u) {
+                        if (turn == mine) {
+                            ok = blocks_wait<false>(my_empty, acc_ph, ctl) && blocks_wait<false>(full0 + r.off, r.phase, ctl);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const int n = kc + 1 < a.kb ? 4 : a.k_last;
+                            if (PAIR) {
+                                umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                                commit_pair(my_full);
+                                commit_pair(empty0 + r.off);
+                            } else {
+                                umma_f8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                                umma_commit_at(my_full);
+                                umma_commit_at(empty0 + r.off);
+                            }
+                            acc_ph ^= 1u;
                         }
                         r.next(r0, (uint32_t)a.stages, slot);
-                        if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
                     }
             }
             __syncwarp();
-        } else if (warp == 2) {
+        } else {
             // ---------------- scales ----------------
-            // A lane has four rows (and of EACH's columns eight at most).
+            // Copied four blocks at a time, straight into shared memory, several slots ahead.  A row's scales lie side by side: 16 bytes to a copy where they are
+            // aligned.  A lane has four rows, and of EACH's columns eight at most.
             uint32_t slot = 0, phase = 0;
             bool ok = true, there;
+            const bool quads = a.kb % 4 == 0 && ((uintptr_t)p.a_scale | (uintptr_t)p.b_scale) % 16 == 0;
             for (int item = first; item < n_items && ok; item += step) {
                 const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN;
-                for (int kc = 0; kc < a.kb && ok; ++kc) {
-                    float s[4], c[EACH ? BN / 32 : 2];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int64_t r = (int64_t)tile * kTileM + 32 * i + lane;
-                        s[i] = r < p.m ? p.a_scale[r * a.kb + kc] : 0.f;
-                    }
-                    if (EACH)
-#pragma unroll
-                        for (int i = 0; i < BN / 32; ++i) { const int j = n0 + 32 * i + lane; c[i] = j < p.n ? p.b_scale[(size_t)j * a.kb + kc] : 0.f; }
-                    else
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) { const int j = n0 + 128 * h; c[h] = (h == 0 || BN > 128) && j < p.n ? p.b_scale[(size_t)(j / 128) * a.kb + kc] : 0.f; }
-                    ok = blocks_wait(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl);
-                    ok = __all_sync(0xffffffffu, ok);
+                const float* const rows = p.a_scale + ((size_t)tile * kTileM + lane) * a.kb;
+                const int n_rows = (int)min((int64_t)kTileM, p.m - (int64_t)tile * kTileM) - lane;
+                const int j0 = EACH ? n0 + lane : n0 / 128 + lane, n_cols = EACH ? p.n - j0 : lane < 2 ? (p.n + 127) / 128 - j0 : 0;
+                const float* const cols = p.b_scale + (size_t)j0 * a.kb;
+                for (int kc = 0; kc < a.kb; kc += 4) {
+                    ok = blocks_wait<true>(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl);
                     if (!ok) break;
+                    const uint32_t rows_at = smem_u32(row_scale + slot * kRowScales) + 16 * lane, cols_at = smem_u32(col_scale + slot * kCols);
+                    if (quads) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (EACH) row_scale[slot * 256 + 32 * i + lane] = s[i];
-                        else
+                        for (int i = 0; i < 4; ++i) copy_floats<4>(rows_at + i * 512, rows + (size_t)(32 * i) * a.kb + kc, p.a_scale, 32 * i < n_rows);
+                        if (!EACH && lane < 2) copy_floats<4>(cols_at + 16 * lane, cols + kc, p.b_scale, n_cols > 0);
+                    } else
 #pragma unroll
-                            for (int h = 0; h < (BN > 128 ? 2 : 1); ++h) row_scale[slot * 256 + h * 128 + 32 * i + lane] = s[i] * c[h];
-                    }
+                        for (int u = 0; u < 4; ++u) {
+                            const bool on = kc + u < a.kb;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) copy_floats<1>(rows_at + i * 512 + 4 * u, rows + (size_t)(32 * i) * a.kb + kc + u, p.a_scale, on && 32 * i < n_rows);
+                            if (!EACH && lane < 2) copy_floats<1>(cols_at + 16 * lane + 4 * u, cols + kc + u, p.b_scale, on && n_cols > 0);
+                        }
                     if (EACH)
 #pragma unroll
-                        for (int i = 0; i < BN / 32; ++i) col_scale[slot * 256 + 32 * i + lane] = c[i];
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&ctl->scale_full[slot]);
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int i = 0; i < BN / 32; ++i)
+                                copy_floats<1>(cols_at + u * 1024 + i * 128 + 4 * lane, cols + (size_t)(32 * i) * a.kb + kc + u, p.b_scale, kc + u < a.kb && 32 * i < n_cols);
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&ctl->scale_full[slot])) : "memory");
                     if (++slot == kScaleSlots) { slot = 0; phase ^= 1u; }
                 }
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
         }
     } else {
         // ---------------- sums of the blocks; bias, ReLU, rounding, store ----------------
@@ -403,69 +472,93 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
         if (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         constexpr int MINE = BN / 2;
         const int q = warp & 3, half = (warp - 4) >> 2;
-        uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 4) * 2 * kBox;
-        const uint32_t both_places = stage ^ (stage + kBox);
+        uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 4) * kBox;
+        const uint32_t both_places = a.bufs == 2 ? stage ^ (stage + kAddWarps * kBox) : 0;       // from one place to the other
         const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
-        const float* const my_scale = row_scale + (!EACH && BN > 128 ? half * 128 : 0) + q * 32 + lane;
+        const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + lane) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? half * MINE : BN > 128 ? half * 4 : 0) * 4;
         uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0;
         bool ok = true, there;
+        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]), from0 = tmem_base + (uint32_t)(half * MINE) + ((uint32_t)(q * 32) << 16);
+        uint32_t v[2][32];
+        // the next block's sums are there: the first of them on their way
+        auto begin = [&]() {
+            ok = ok && blocks_wait<true>(tmem_full0 + 8u * acc, acc_ph, ctl);
+            if (!ok) return;
+            tc_fence_after();
+            tmem_ld32(from0 + acc * (uint32_t)BN, v[0]);
+        };
+        if (first < n_items) begin();
         for (int item = first; item < n_items; item += step) {
             const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN + half * MINE;
             const int64_t row0 = (int64_t)tile * kTileM + q * 32;
             const int rows = there ? (int)max((int64_t)0, min((int64_t)32, p.m - row0)) : 0;
-            float2 sum[MINE / 2];
+            float4 scales = make_float4(0.f, 0.f, 0.f, 0.f);  // four blocks'
+            uint64_t sum[MINE / 2];
 #pragma unroll
-            for (int i = 0; i < MINE / 2; ++i) sum[i] = make_float2(0.f, 0.f);
-            for (int kc = 0; kc < a.kb; ++kc) {
-                if (ok) ok = blocks_wait(smem_u32(&ctl->scale_full[slot]), phase, ctl) && blocks_wait(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
-                const float2 s = both<float2>(my_scale[slot * 256]);
-                const uint32_t from = tmem_base + acc * (uint32_t)BN + (uint32_t)(half * MINE) + ((uint32_t)(q * 32) << 16);
-#pragma unroll
-                for (int c = 0; c < MINE; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(from + c, v);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        float2 t[2];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) t[h] = make_float2(__uint_as_float(v[2 * (i + h)]), __uint_as_float(v[2 * (i + h) + 1]));
-                        if (EACH) {
-                            const float4 b = *(const float4*)(col_scale + slot * 256 + half * MINE + c + 2 * i);
-                            t[0] = mul2(t[0], make_float2(b.x, b.y));
-                            t[1] = mul2(t[1], make_float2(b.z, b.w));
-                        }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) sum[c / 2 + i + h] = fma2(t[h], s, sum[c / 2 + i + h]);
+            for (int i = 0; i < MINE / 2; ++i) sum[i] = 0;
+            for (int kc = 0; kc < a.kb && ok; ++kc) {
+                const int u = kc & 3;
+                if (u == 0) {
+                    ok = ok && blocks_wait<true>(smem_u32(&ctl->scale_full[slot]), phase, ctl);
+                    scales = lds_floats(my_rows + slot * (kRowScales * 4));
+                    if (!EACH) {
+                        const float4 b = lds_floats(my_cols + slot * (kCols * 4));
+                        scales = make_float4(scales.x * b.x, scales.y * b.y, scales.z * b.z, scales.w * b.w);
                     }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
-                    else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
-                    mbar_arrive(&ctl->scale_empty[slot]);
+                const uint32_t s1 = __float_as_uint(u == 0 ? scales.x : u == 1 ? scales.y : u == 2 ? scales.z : scales.w);
+                const uint64_t s = pair_of(s1, s1);
+                const uint32_t from = from0 + acc * (uint32_t)BN;
+#pragma unroll
+                for (int c = 0; c < MINE / 32; ++c) {
+                    uint32_t* const now = v[c & 1];
+                    tmem_ld_wait32(now);
+                    if (c + 1 < MINE / 32) tmem_ld32(from + 32 * (c + 1), v[(c + 1) & 1]);      // on its way meanwhile
+                    else {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
+                            else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
+                        }
+                        if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+                        // (with an odd number of loads the next one's place is the one that is being read)
+                        if (MINE / 32 % 2 == 0 && (kc + 1 < a.kb || item + step < n_items)) begin();
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        uint64_t t[2] = {pair_of(now[2 * i], now[2 * i + 1]), pair_of(now[2 * i + 2], now[2 * i + 3])};
+                        if (EACH) {
+                            uint64_t b[2];
+                            lds_pairs(my_cols + slot * (kCols * 4) + (uint32_t)(u * 256 + 32 * c + 2 * i) * 4, b);
+                            t[0] = product(t[0], b[0]);
+                            t[1] = product(t[1], b[1]);
+                        }
+                        add_product(sum[16 * c + i], t[0], s);
+                        add_product(sum[16 * c + i + 1], t[1], s);
+                    }
                 }
-                if (++slot == kScaleSlots) { slot = 0; phase ^= 1u; }
-                if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+                if (MINE / 32 % 2 != 0 && (kc + 1 < a.kb || item + step < n_items)) begin();
+                if (u == 3 || kc + 1 == a.kb) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_relaxed(&ctl->scale_empty[slot]);       // (the scales have long been read: sums were made of them)
+                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1u; }
+                }
             }
             if (!ok)                                          // a wait ran out: what is stored says so
 #pragma unroll
-                for (int i = 0; i < MINE / 2; ++i) sum[i] = make_float2(__uint_as_float(0x7fffffffu), __uint_as_float(0x7fffffffu));
+                for (int i = 0; i < MINE / 2; ++i) sum[i] = 0x7fffffff7fffffffull;
             constexpr int PER = 64 / (int)sizeof(T);          // columns of a box
 #pragma unroll
             for (int c = 0; c < MINE; c += PER) {
                 const int c1 = n0 + c;
                 if (c1 >= p.n) break;
-                if (a.boxes) { if (lane == 0) store_read(2); }
+                if (a.boxes) { if (lane == 0) store_read(a.bufs); }
                 __syncwarp();
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < PER / 2; ++i) {
-                    float2 f = sum[c / 2 + i];
+                    float2 f = floats_of(sum[c / 2 + i]);
                     const int j = c1 + 2 * i;
                     if (p.bias) f = add2(f, make_float2(j < p.n ? dc_ld(p.bias + j) : 0.f, j + 1 < p.n ? dc_ld(p.bias + j + 1) : 0.f));
                     if constexpr (sizeof(T) == 2) w[i] = p.relu ? two_bf16<true>(f) : two_bf16<false>(f);
@@ -565,7 +658,8 @@ int launch_product(const BlocksProduct& p, int dtype, int device, int num_sms, c
     a.NB = dc_div_up(p.n, BN);
     const int b_rows = pair ? BN / 2 : BN;
     a.stage_bytes = kATile + b_rows * kBytesK;
-    a.stages = kBlocksRoom / a.stage_bytes;
+    a.bufs = a.kb <= 8 ? 2 : 1;                               // long products take the room for operands
+    a.stages = (kBlocksRoom - kAddWarps * kBox * a.bufs - (p.b_block_rows == 1 ? kEachBytes : kScaleBytes)) / a.stage_bytes;
     if (a.stages > kBlocksMostStages) a.stages = kBlocksMostStages;
     a.k_last = dc_div_up(p.k - (a.kb - 1) * kBytesK, 32);
     // float32 accumulators, both operands e4m3, K-major
