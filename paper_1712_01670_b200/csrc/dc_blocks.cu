@@ -3,7 +3,7 @@
 //   scale = the smallest power of two with max |x| <= 448 scale,  q = e4m3(x / scale)
 //   out[r][j] = relu(sum_i a_scale[r][i] b_scale[j'][i] sum_{k in block i} a[r][k] b[j][k] + bias[j])
 //
-// k_quantize_blocks: memory bounds it: a tile of 128 x 128 values is read once, into registers, and leaves as rows, turned, or both.
+// k_quantize_row_blocks, k_quantize_tile: memory bounds them: a value is read once and leaves in its row, turned, or both.
 //
 // k_blocks: tcgen05.mma kind::f8f6f4 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, which are one block.  A block's sums leave
 // tensor memory as soon as they are there, are scaled and added up in the registers of eight warps, beside the MMAs of the next block (two accumulators in turns).
@@ -59,6 +59,8 @@ template <> struct Eight<__nv_bfloat16> {
             if (i == k >> 1) w[i] |= (uint32_t)__bfloat16_as_ushort(v) << (16 * (k & 1));
     }
     __device__ __forceinline__ void open(float2* v) const { Vec<__nv_bfloat16, 8>::open(raw, v); }
+    __device__ __forceinline__ uint32_t most() const { return most_of<__nv_bfloat16>(raw_most(0u, raw)); }        // the bits of the largest size; above infinity's: a NaN
+    __device__ __forceinline__ void keep(uint4* p) const { p[0] = raw; }
 };
 template <> struct Eight<float> {
     float4 raw[2];
@@ -71,6 +73,8 @@ template <> struct Eight<float> {
             if (i == k) (&raw[i >> 2].x)[i & 3] = v;
     }
     __device__ __forceinline__ void open(float2* v) const { Vec<float, 4>::open(raw[0], v); Vec<float, 4>::open(raw[1], v + 2); }
+    __device__ __forceinline__ uint32_t most() const { return raw_most(raw_most(0u, raw[0]), raw[1]); }
+    __device__ __forceinline__ void keep(uint4* p) const { ((float4*)p)[0] = raw[0]; ((float4*)p)[1] = raw[1]; }
 };
 
 __device__ __forceinline__ void store_bytes(uint8_t* p, uint2 w, int there)       // the first `there` of eight
@@ -80,122 +84,170 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, uint2 w, int there)     
     for (int i = 0; i < 8; ++i)
         if (i < there) p[i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
 }
-
-// A CTA has 128 x 128 values, a thread eight columns of eight rows.  WIDE: rows are aligned to 16 bytes.  TURN: x turned is wanted.
-template <typename T, bool WIDE, bool TURN>
-__global__ void __launch_bounds__(256) k_quantize_blocks(const BlocksArgs a)
+__device__ __forceinline__ void store_bytes(uint8_t* p, uint4 w, int there)       // of sixteen
 {
-    __shared__ uint32_t most_of_column[16][128];
-    __shared__ float inv_of_column[128];                      // 1 / scale; negative: a NaN or an infinity
-    __shared__ uint32_t most_of_tile;
-    __shared__ uint2 turned[128 * 16];                        // [column][rows / 8], the eights of a column in another order for each eight columns: no bank conflicts
-    const int tile_c = blockIdx.x % a.kb, tile_r = blockIdx.x / a.kb;
-    const int part = threadIdx.x & 15, team = threadIdx.x >> 4, lane = threadIdx.x & 31;
-    const int col = tile_c * 128 + part * 8, row0 = tile_r * 128 + team * 8, columns = min(8, a.channels - col);
+    if (there >= 16) { *(uint4*)p = w; return; }
+    if (there > 0) store_bytes(p, make_uint2(w.x, w.y), there);
+    if (there > 8) store_bytes(p + 8, make_uint2(w.z, w.w), there - 8);
+}
+// Eight columns of a row, `there` of which exist.  WIDE: rows are aligned to 16 bytes.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load_eight(Eight<T>& v, const char* x, int there)
+{
+    v.zero();
+    if (WIDE && there >= 8) v.load(x);
+    else
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (k < there) v.put(k, ((const T*)x)[k]);
+}
+template <typename T>
+__device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale& s)
+{
+    float2 f[4];
+    v.open(f);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = s.bad ? 0u : two_e4m3(mul2(f[k], both<float2>(s.inv)));
+    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+}
+
+// Rows alone: sixteen lanes to a block, four blocks of a lane in flight.  by_kb: see divided().
+__device__ __forceinline__ uint32_t divided(uint32_t n, uint2 by) { return by.x ? __umulhi(n, by.x) >> by.y : n; }
+
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a, uint2 by_kb, uint32_t items)
+{
+    const int part = threadIdx.x & 15, lane = threadIdx.x & 31;
     dc_pdl_wait();
     dc_pdl_release();
-    if (threadIdx.x == 0) most_of_tile = 0;
-    Eight<T> v[8];
+    const uint32_t first = blockIdx.x * 64u + (threadIdx.x >> 4);
+    Eight<T> v[4];
+    uint32_t row[4], block[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i].zero();
-        if (row0 + i < a.rows && columns > 0) {
-            const char* const x = (const char*)a.x + (size_t)(row0 + i) * a.x_pitch + (size_t)col * sizeof(T);
-            if (WIDE && columns == 8) v[i].load(x);
-            else
+    for (int u = 0; u < 4; ++u) {
+        const uint32_t item = first + 16u * u;
+        row[u] = divided(item, by_kb);
+        block[u] = item - row[u] * (uint32_t)a.kb;
+        const int col = (int)block[u] * 128 + part * 8;
+        load_eight<WIDE>(v[u], (const char*)a.x + (size_t)row[u] * a.x_pitch + (size_t)col * sizeof(T), item < items ? a.channels - col : 0);
+    }
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < columns) v[i].put(k, ((const T*)x)[k]);
+    for (int u = 0; u < 4; ++u) {
+        const uint32_t m = __reduce_max_sync(0xffffu << (lane & 16), v[u].most());
+        if (first + 16u * u >= items) continue;
+        const BlockScale s = block_scale(m);
+        const int col = (int)block[u] * 128 + part * 8;
+        if (col < a.channels) store_bytes(a.q + (size_t)row[u] * a.q_pitch + col, eight_e4m3(v[u], s), a.channels - col);
+        if (part == 0) a.scale[(size_t)row[u] * a.kb + block[u]] = s.scale;
+    }
+}
+
+// Turned, or with a scale for 128 x 128 values: a CTA has such a tile, read once.  A thread has eight columns of eight rows, which it puts into 8 bits on their way to shared memory;
+// and then a column (bfloat16: two) of 64 (32) rows, which it reads from there twice, for the largest value and for the values.  WHOLE: one scale for the tile.
+template <typename T, bool WIDE, bool WHOLE>
+__global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
+{
+    constexpr int PER = 4 / (int)sizeof(T), TEAMS = 2 * PER, ROWS = 128 / TEAMS;       // columns of a thread, threads to a column, rows of each
+    extern __shared__ uint4 tile4[];                          // [128][128] of the map's type
+    __shared__ uint32_t most_of[TEAMS][128];
+    __shared__ uint32_t most_of_tile;
+    const int tile_c = blockIdx.x % a.kb, tile_r = blockIdx.x / a.kb, lane = threadIdx.x & 31;
+    const int part = threadIdx.x & 15, team = threadIdx.x >> 4, col = tile_c * 128 + part * 8, there = a.channels - col;
+    dc_pdl_wait();
+    dc_pdl_release();
+    if (WHOLE) {
+        if (threadIdx.x == 0) most_of_tile = 0;
+        __syncthreads();
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i0 = 0; i0 < 8; i0 += 4) {
+        Eight<T> v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = tile_r * 128 + (i0 + i) * 16 + team;
+            load_eight<WIDE>(v[i], (const char*)a.x + (size_t)row * a.x_pitch + (size_t)col * sizeof(T), row < a.rows ? there : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (i0 + i) * 16 + team, row = tile_r * 128 + r;
+            if (WHOLE || a.qt) v[i].keep(tile4 + (r * 16 + part) * (sizeof(T) / 2));
+            const uint32_t m = v[i].most();
+            if (WHOLE) most = max(most, m);
+            else if (a.q) {
+                const BlockScale s = block_scale(__reduce_max_sync(0xffffu << (lane & 16), m));
+                if (row < a.rows) {
+                    if (there > 0) store_bytes(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v[i], s), there);
+                    if (part == 0) a.scale[(size_t)row * a.kb + tile_c] = s.scale;
+                }
+            }
         }
     }
-    uint32_t most[8], down[8];                                // of the rows, of the columns
-#pragma unroll
-    for (int k = 0; k < 8; ++k) down[k] = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        float2 f[4];
-        v[i].open(f);
-        uint32_t m = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t x = size_bits(f[k].x), y = size_bits(f[k].y);
-            m = max(m, max(x, y));
-            if (TURN) { down[2 * k] = max(down[2 * k], x); down[2 * k + 1] = max(down[2 * k + 1], y); }
-        }
-        most[i] = __reduce_max_sync(0xffffu << (lane & 16), m);
-    }
-    if (a.block_rows > 1) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, most[i]);
+    BlockScale s;
+    if (WHOLE) {
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) atomicMax(&most_of_tile, most);        // the same whatever the order
         __syncthreads();
-        if (part == 0) atomicMax(&most_of_tile, m);           // the same whatever the order
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most[i] = most_of_tile;
+        s = block_scale(most_of_tile);
         if (threadIdx.x == 0) {
-            const float s = block_scale(most[0]).scale;
-            if (a.q) a.scale[(size_t)tile_r * a.kb + tile_c] = s;
-            if (TURN) a.scale_t[(size_t)tile_c * a.rb + tile_r] = s;
+            if (a.q) a.scale[(size_t)tile_r * a.kb + tile_c] = s.scale;
+            if (a.qt) a.scale_t[(size_t)tile_c * a.rb + tile_r] = s.scale;
+        }
+        if (a.q && there > 0)
+#pragma unroll 2
+            for (int i = 0; i < 8; ++i) {
+                const int r = i * 16 + team, row = tile_r * 128 + r;
+                if (row >= a.rows) break;
+                Eight<T> v;
+                v.load((const char*)(tile4 + (r * 16 + part) * (sizeof(T) / 2)));
+                store_bytes(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v, s), there);
+            }
+    } else __syncthreads();
+    if (!a.qt) return;
+    const int c = threadIdx.x % (128 / PER) * PER, turn = threadIdx.x / (128 / PER), row0 = tile_r * 128 + turn * ROWS;
+    const uint32_t* const word = (const uint32_t*)((const char*)tile4 + ((size_t)turn * ROWS * 128 + c) * sizeof(T));
+    constexpr int LINE = 128 / PER;                           // words of a row
+    BlockScale t[PER];
+    if (WHOLE)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) t[k] = s;
+    else {
+        uint32_t m = 0;
+#pragma unroll 8
+        for (int r = 0; r < ROWS; ++r) m = PER == 2 ? larger2(m, word[r * LINE]) & 0x7fff7fffu : max(m, word[r * LINE] & 0x7fffffffu);
+        if (PER == 2) { most_of[turn][c] = m << 16; most_of[turn][c + 1] = m & 0xffff0000u; } else most_of[turn][c] = m;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            uint32_t all = 0;
+#pragma unroll
+            for (int i = 0; i < TEAMS; ++i) all = max(all, most_of[i][c + k]);
+            t[k] = block_scale(all);
+            if (turn == 0 && tile_c * 128 + c + k < a.channels) a.scale_t[(size_t)(tile_c * 128 + c + k) * a.rb + tile_r] = t[k].scale;
         }
     }
-    if (a.q) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const BlockScale s = block_scale(most[i]);
-            float2 f[4];
-            v[i].open(f);
+    for (int g = 0; g < ROWS; g += 16) {                      // sixteen rows: 16 bytes of a column
+        uint32_t out[PER][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = s.bad ? 0u : two_e4m3(mul2(f[k], both<float2>(s.inv)));
-            if (row0 + i < a.rows) {
-                if (columns > 0) store_bytes(a.q + (size_t)(row0 + i) * a.q_pitch + col, make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16), columns);
-                if (a.block_rows == 1 && part == 0) a.scale[(size_t)(row0 + i) * a.kb + tile_c] = s.scale;
+            for (int i = 0; i < 4; ++i) w[i] = word[(g + 4 * q + i) * LINE];
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                float f[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(PER == 2 ? (k ? w[i] & 0xffff0000u : w[i] << 16) : w[i]);
+                const float2 inv = both<float2>(t[k].inv);
+                out[k][q] = t[k].bad ? 0u : two_e4m3(mul2(make_float2(f[0], f[1]), inv)) | two_e4m3(mul2(make_float2(f[2], f[3]), inv)) << 16;
             }
         }
-    }
-    if (TURN) {
-        if (a.block_rows == 1) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) most_of_column[team][part * 8 + k] = down[k];
-            __syncthreads();
-            if (threadIdx.x < 128) {
-                uint32_t m = 0;
-#pragma unroll
-                for (int t = 0; t < 16; ++t) m = max(m, most_of_column[t][threadIdx.x]);
-                const BlockScale s = block_scale(m);
-                inv_of_column[threadIdx.x] = s.bad ? -1.f : s.inv;
-                const int c = tile_c * 128 + threadIdx.x;
-                if (c < a.channels) a.scale_t[(size_t)c * a.rb + tile_r] = s.scale;
-            }
-        } else if (threadIdx.x < 128) {
-            const BlockScale s = block_scale(most[0]);
-            inv_of_column[threadIdx.x] = s.bad ? -1.f : s.inv;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < 8; k += 2) {                      // two columns of eight rows
-            const float i0 = inv_of_column[part * 8 + k], i1 = inv_of_column[part * 8 + k + 1];
-            uint32_t lo[2] = {0, 0}, hi[2] = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float2 f[4];
-                v[i].open(f);
-                const uint32_t t = two_e4m3(mul2(f[k / 2], make_float2(i0, i1)));
-                lo[i >> 2] |= (t & 0xffu) << (8 * (i & 3));
-                hi[i >> 2] |= (t >> 8) << (8 * (i & 3));
-            }
-            const int c = part * 8 + k, at = team ^ part;
-            turned[c * 16 + at] = i0 < 0.f ? make_uint2(0, 0) : make_uint2(lo[0], lo[1]);
-            turned[(c + 1) * 16 + at] = i1 < 0.f ? make_uint2(0, 0) : make_uint2(hi[0], hi[1]);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int it = 0; it < 8; ++it) {                      // 16 lanes to a column's 128 bytes
-            const int c = it * 16 + (threadIdx.x >> 4), r = tile_r * 128 + part * 8;
-            if (tile_c * 128 + c < a.channels && r < a.rows)
-                store_bytes(a.qt + (size_t)(tile_c * 128 + c) * a.qt_pitch + r, turned[c * 16 + (part ^ (c >> 3 & 15))], a.rows - r);
-        }
+        for (int k = 0; k < PER; ++k)
+            if (tile_c * 128 + c + k < a.channels)
+                store_bytes(a.qt + (size_t)(tile_c * 128 + c + k) * a.qt_pitch + row0 + g, make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]), a.rows - row0 - g);
     }
 }
 
@@ -681,21 +733,38 @@ int launch_product(const BlocksProduct& p, int dtype, int device, int num_sms, c
 #undef DC_BLOCKS
 }
 
-template <typename T>
-cudaError_t launch_quantize(const BlocksArgs& a, bool wide, cudaStream_t stream)
+template <typename T, bool WIDE>
+int launch_quantize(const BlocksArgs& a, int device, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)((int64_t)a.kb * a.rb));
-    if (a.qt) return wide ? dc_launch_pdl(k_quantize_blocks<T, true, true>, grid, 256, 0, stream, a) : dc_launch_pdl(k_quantize_blocks<T, false, true>, grid, 256, 0, stream, a);
-    return wide ? dc_launch_pdl(k_quantize_blocks<T, true, false>, grid, 256, 0, stream, a) : dc_launch_pdl(k_quantize_blocks<T, false, false>, grid, 256, 0, stream, a);
+    if (!a.qt && a.block_rows == 1) {
+        const int64_t items = (int64_t)a.rows * a.kb;
+        if (items < 0x7fffffff) {
+            // n / kb = n * by.x >> (32 + by.y) for n < 2^31, by.x the next whole number above 2^(32 + by.y) / kb, 2^by.y < kb
+            uint2 by = make_uint2(0, 0);
+            if (a.kb > 1) {
+                while ((2 << by.y) < a.kb) ++by.y;
+                by.x = (uint32_t)((((uint64_t)1 << (32 + by.y)) + a.kb - 1) / a.kb);
+            }
+            DC_CUDA(dc_launch_pdl(k_quantize_row_blocks<T, WIDE>, dim3((unsigned)((items + 63) / 64)), 256, 0, stream, a, by, (uint32_t)items));
+            return DC_OK;
+        }
+    }
+    const int64_t tiles = (int64_t)a.kb * a.rb;
+    if (tiles > 0x7fffffff) return DC_ERR_LIMIT;
+    const size_t smem = 128 * 128 * sizeof(T);
+    auto* const kernel = a.block_rows > 1 ? k_quantize_tile<T, WIDE, true> : k_quantize_tile<T, WIDE, false>;
+    static dc_once_per_device set[2];
+    DC_CUDA(set[a.block_rows > 1].ensure(device, [=] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); }));
+    DC_CUDA(dc_launch_pdl(kernel, dim3((unsigned)tiles), 256, smem, stream, a));
+    return DC_OK;
 }
 
-int quantize(BlocksArgs& a, int dtype, cudaStream_t stream)
+int quantize(BlocksArgs& a, int dtype, int device, cudaStream_t stream)
 {
     a.kb = dc_div_up(a.channels, 128); a.rb = (int)(((int64_t)a.rows + 127) / 128);
-    if ((int64_t)a.kb * a.rb > 0x7fffffff) return DC_ERR_LIMIT;
     const bool wide = (uintptr_t)a.x % 16 == 0 && (a.rows < 2 || a.x_pitch % 16 == 0);
-    DC_CUDA(dtype == DC_BF16 ? launch_quantize<__nv_bfloat16>(a, wide, stream) : launch_quantize<float>(a, wide, stream));
-    return DC_OK;
+    if (dtype == DC_BF16) return wide ? launch_quantize<__nv_bfloat16, true>(a, device, stream) : launch_quantize<__nv_bfloat16, false>(a, device, stream);
+    return wide ? launch_quantize<float, true>(a, device, stream) : launch_quantize<float, false>(a, device, stream);
 }
 
 bool floats_ok(const float* p) { return (uintptr_t)p % sizeof(float) == 0; }
@@ -734,7 +803,9 @@ int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t 
     BlocksArgs a = {};
     a.x = x_dev; a.x_pitch = x_pitch; a.rows = (int)rows; a.channels = channels; a.block_rows = block_rows;
     a.q = q_dev; a.q_pitch = q_pitch; a.scale = scale_dev; a.qt = qt_dev; a.qt_pitch = qt_pitch; a.scale_t = scale_t_dev;
-    return quantize(a, dtype, (cudaStream_t)cuda_stream);
+    int device = 0, sms = 0;
+    const int rc = dc_current_device(&device, &sms);
+    return rc != DC_OK ? rc : quantize(a, dtype, device, (cudaStream_t)cuda_stream);
 }
 
 int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const uint8_t* b_dev, size_t b_pitch, const float* b_scale_dev, int32_t b_block_rows,
@@ -774,7 +845,7 @@ int dc_linear_blocks(const void* x_dev, size_t x_pitch, const uint8_t* w_dev, si
     float* const scale = (float*)(q + (size_t)m * pitch);
     BlocksArgs a = {};
     a.x = x_dev; a.x_pitch = x_pitch; a.rows = (int)m; a.channels = k; a.block_rows = 1; a.q = q; a.q_pitch = pitch; a.scale = scale;
-    if ((rc = quantize(a, dtype, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
+    if ((rc = quantize(a, dtype, device, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
     const BlocksProduct p = {q, pitch, scale, w_dev, w_pitch, w_scale_dev, bias_dev, m, n, k, relu, w_block_rows, out_dev, out_pitch};
     return launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
 }

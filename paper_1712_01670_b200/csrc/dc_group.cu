@@ -28,6 +28,7 @@ struct GroupArgs {
     float eps;
     int maps, pixels, channels, groups, per;        // per: channels of a group
     int width, slices, gs, pieces, piece_items;     // columns of a slice; slices of a map; groups of a slice; slices of a group; columns of a group (with pieces)
+    int by_width, by_per;                           // slices of at most 16 columns: 65536 / width and / per, rounded up; else 0
     int chunks, rows_per;                           // CTAs to the rows of a slice, and the rows of each
     float2* part;                                   // [maps][chunks * pieces][groups]: mean and squares, or the two sums of a group's gradients
     float* sums;                                    // [maps][chunks][2][channels]: sums of dz and of dz xh; or NULL: not wanted
@@ -57,27 +58,78 @@ __device__ __forceinline__ Place place_of(const GroupArgs& a)
 __device__ __forceinline__ char* row_at(const void* p, size_t pitch, int64_t row) { return (char*)p + (uint64_t)row * pitch; }
 
 // 1 / (1 + e^-z)
-__device__ __forceinline__ float sigmoid(float z)
+__device__ __forceinline__ float one_and_exp(float z)
+{
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    return 1.f + e;
+}
+__device__ __forceinline__ float reciprocal(float v)
 {
     float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-z)));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-template <int ACT> __device__ __forceinline__ float act(float z)
+// Of four values: an exponential each and, JOINT, one reciprocal for all, 1 / a = bcd / abcd (the unit for both gives 16 results a cycle); where abcd is beyond a number's
+// range, or none, each has its own.  Not JOINT: a value's result depends on no other.
+template <bool JOINT>
+__device__ __forceinline__ void sigmoids(const float2* z, float2* p)
 {
-    if (ACT == DC_ACT_RELU) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(z));
-    if (ACT == DC_ACT_SILU) z *= sigmoid(z);
-    return z;
+    const float2 a = make_float2(one_and_exp(z[0].x), one_and_exp(z[0].y)), c = make_float2(one_and_exp(z[1].x), one_and_exp(z[1].y));
+    if (JOINT) {
+        const float ab = a.x * a.y, cd = c.x * c.y, t = ab * cd;
+        if (t < 1e37f) {
+            const float r = reciprocal(t);
+            p[0] = mul2(both<float2>(r * cd), make_float2(a.y, a.x));
+            p[1] = mul2(both<float2>(r * ab), make_float2(c.y, c.x));
+            return;
+        }
+    }
+    p[0] = make_float2(reciprocal(a.x), reciprocal(a.y));
+    p[1] = make_float2(reciprocal(c.x), reciprocal(c.y));
 }
-template <int ACT> __device__ __forceinline__ float2 act(float2 z) { return make_float2(act<ACT>(z.x), act<ACT>(z.y)); }
-// dy act'(z)
-template <int ACT> __device__ __forceinline__ float act_back(float dy, float z)
+template <bool JOINT> __device__ __forceinline__ void sigmoids(const float* z, float* p) { p[0] = reciprocal(one_and_exp(z[0])); }
+
+__device__ __forceinline__ float positive(float z) { asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(z)); return z; }
+__device__ __forceinline__ float2 positive(float2 z) { return make_float2(positive(z.x), positive(z.y)); }
+__device__ __forceinline__ float where_positive(float dy, float z) { return z > 0.f ? dy : z != z ? z : 0.f; }
+__device__ __forceinline__ float2 where_positive(float2 dy, float2 z) { return make_float2(where_positive(dy.x, z.x), where_positive(dy.y, z.y)); }
+// act(z), and dy act'(z), of a column's values, in place
+template <int ACT, bool JOINT, int P, typename F>
+__device__ __forceinline__ void activate(F (&z)[P])
 {
-    if (ACT == DC_ACT_RELU) return z > 0.f ? dy : z != z ? z : 0.f;
-    if (ACT == DC_ACT_SILU) { const float p = sigmoid(z); return dy * (p * fmaf(z, 1.f - p, 1.f)); }
-    return dy;
+    constexpr int STEP = P > 1 ? 2 : 1;
+#pragma unroll
+    for (int k = 0; k < P; k += STEP) {
+        if (ACT == DC_ACT_SILU) {
+            F p[STEP];
+            sigmoids<JOINT>(z + k, p);
+#pragma unroll
+            for (int h = 0; h < STEP; ++h) z[k + h] = mul2(z[k + h], p[h]);
+        } else if (ACT == DC_ACT_RELU)
+#pragma unroll
+            for (int h = 0; h < STEP; ++h) z[k + h] = positive(z[k + h]);
+    }
 }
-template <int ACT> __device__ __forceinline__ float2 act_back(float2 dy, float2 z) { return make_float2(act_back<ACT>(dy.x, z.x), act_back<ACT>(dy.y, z.y)); }
+template <int ACT, bool JOINT, int P, typename F>
+__device__ __forceinline__ void activate_back(F (&dy)[P], const F (&z)[P])
+{
+    constexpr int STEP = P > 1 ? 2 : 1;
+#pragma unroll
+    for (int k = 0; k < P; k += STEP) {
+        if (ACT == DC_ACT_SILU) {
+            F p[STEP];
+            sigmoids<JOINT>(z + k, p);
+#pragma unroll
+            for (int h = 0; h < STEP; ++h) {
+                const F zp = mul2(z[k + h], p[h]);                               // p (1 + z (1 - p)) = p + zp - zp p
+                dy[k + h] = mul2(dy[k + h], fma2(mul2(zp, both<F>(-1.f)), p[h], add2(p[h], zp)));
+            }
+        } else if (ACT == DC_ACT_RELU)
+#pragma unroll
+            for (int h = 0; h < STEP; ++h) dy[k + h] = where_positive(dy[k + h], z[k + h]);
+    }
+}
 
 __device__ __forceinline__ float lane_of(float v, int) { return v; }
 __device__ __forceinline__ float lane_of(float2 v, int k) { return k ? v.y : v.x; }
@@ -197,6 +249,12 @@ template <typename T, int VE, bool ONE> struct Column {
     __device__ __forceinline__ void weights(const GroupArgs& a, const Place& p, int col)
     {
         const int c = (p.col0 + col) * VE;
+        if constexpr (VE > 1)
+            if ((((uintptr_t)a.gamma | (uintptr_t)a.beta) & 15) == 0) {
+                load_weights(a.gamma, c, 1.f, g);
+                load_weights(a.beta, c, 0.f, b);
+                return;
+            }
 #pragma unroll
         for (int k = 0; k < P; ++k) {
             g[k] = two<F>(a.gamma ? dc_ld(a.gamma + c + (VE > 1 ? 2 * k : 0)) : 1.f, VE > 1 ? (a.gamma ? dc_ld(a.gamma + c + 2 * k + 1) : 1.f) : 0.f);
@@ -210,7 +268,10 @@ template <typename T, int VE, bool ONE> struct Column {
         for (int k = 0; k < (ONE ? 1 : P); ++k) {
             float2 v[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[h] = read(a.pieces > 1 ? 0 : (col * VE + (ONE || VE == 1 ? 0 : 2 * k + h)) / a.per);
+            for (int h = 0; h < 2; ++h) {
+                const int channel = col * VE + (ONE || VE == 1 ? 0 : 2 * k + h);
+                v[h] = read(a.by_per ? channel * a.by_per >> 16 : a.pieces > 1 ? 0 : channel / a.per);
+            }
             first[k] = two<F>(v[0].x, v[1].x);
             second[k] = two<F>(v[0].y, v[1].y);
         }
@@ -248,7 +309,8 @@ __global__ void __launch_bounds__(kThreads) k_group_apply(const GroupArgs a)
             F d[P];
             V::open(raw[u], d);
 #pragma unroll
-            for (int k = 0; k < P; ++k) d[k] = act<ACT>(affine(hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), c.g[k], c.b[k]));
+            for (int k = 0; k < P; ++k) d[k] = affine(hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), c.g[k], c.b[k]);
+            activate<ACT, ONE>(d);
             *(typename V::Raw*)(y + (size_t)(r + u * turns) * a.y_pitch) = V::close(d);
         }
     }
@@ -288,15 +350,14 @@ __global__ void __launch_bounds__(kThreads) k_group_back_sums(const GroupArgs a)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 if (r + u * turns >= p.rows) break;
-                F d[P], e[P];
+                F d[P], e[P], z[P];
                 V::open(rx[u], d);
                 V::open(rd[u], e);
 #pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    const F xh = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), dz = act_back<ACT>(e[k], affine(xh, c.g[k], c.b[k]));
-                    d1[k] = add2(d1[k], dz);
-                    d2[k] = fma2(dz, xh, d2[k]);
-                }
+                for (int k = 0; k < P; ++k) { d[k] = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(d[k], c.g[k], c.b[k]); }
+                activate_back<ACT, ONE>(e, z);
+#pragma unroll
+                for (int k = 0; k < P; ++k) { d1[k] = add2(d1[k], e[k]); d2[k] = fma2(e[k], d[k], d2[k]); }
             }
         }
 #pragma unroll
@@ -369,17 +430,306 @@ __global__ void __launch_bounds__(kThreads) k_group_back_apply(const GroupArgs a
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (r + u * turns >= p.rows) break;
-            F d[P], e[P];
+            F d[P], e[P], z[P];
             V::open(rx[u], d);
             V::open(rd[u], e);
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int at = ONE ? 0 : k;
-                const F xh = hat(d[k], mean[at], rstd[at]), dz = act_back<ACT>(e[k], affine(xh, c.g[k], c.b[k]));
-                d[k] = mul2(fma2(xh, m2[at], add2(mul2(dz, c.g[k]), m1[at])), rstd[at]);
-            }
+            for (int k = 0; k < P; ++k) { d[k] = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(d[k], c.g[k], c.b[k]); }
+            activate_back<ACT, ONE>(e, z);
+#pragma unroll
+            for (int k = 0; k < P; ++k) d[k] = mul2(fma2(d[k], m2[ONE ? 0 : k], add2(mul2(e[k], c.g[k]), m1[ONE ? 0 : k])), rstd[ONE ? 0 : k]);
             *(typename V::Raw*)(dx + (size_t)(r + u * turns) * a.y_pitch) = V::close(d);
         }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// A slice of a map in the shared memory of a cluster: read once
+// ---------------------------------------------------------------------------
+constexpr int kMostResident = 256;                            // threads
+constexpr int kMostCluster = 8, kMostGroups = 64;             // CTAs to a slice; groups of one
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Nothing is sent before every CTA of the cluster runs.
+__device__ __forceinline__ void cluster_started(bool cluster) { if (cluster) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait(bool cluster) { if (cluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// To the same place in CTA `rank` of the cluster.
+__device__ __forceinline__ void send(const float2* at, int rank, float2 v)
+{
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(at)), "r"(rank));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
+}
+// What threads of one column have to add up: within a warp first, where its lanes hold whole rows of columns.  Returns the rows of partial sums that are left.
+template <int N, typename F>
+__device__ __forceinline__ int fold(F (&v)[N], int cols, int turns)
+{
+    if (cols & (cols - 1)) return turns;
+    for (int o = cols; o < 32; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = add_shuffled(v[k], o);
+    return (int)blockDim.x >> 5;
+}
+// ... and which of them this thread leaves, or none.
+__device__ __forceinline__ int fold_row(int cols, int turn, int turns)
+{
+    if (cols & (cols - 1)) return turn < turns ? turn : -1;
+    return (threadIdx.x & 31) < cols ? (int)(threadIdx.x >> 5) : -1;
+}
+// A thread's place: `turns` rows of columns at once (at most 256 threads and 16 columns: one multiplication).
+__device__ __forceinline__ void seat(const GroupArgs& a, int& col, int& turn, int& turns)
+{
+    turns = (int)blockDim.x * a.by_width >> 16;
+    turn = (int)threadIdx.x * a.by_width >> 16;
+    col = (int)threadIdx.x - turn * a.width;
+}
+// Rows of partial sums added up: a thread to each of `wide` places.
+__device__ __forceinline__ float rows_of_sums(const float* part, int left, int wide, int i)
+{
+    float t = 0.f;
+    for (int k = 0; k < left; ++k) t += part[k * wide + i];
+    return t;
+}
+
+__device__ __forceinline__ Place resident_place(const GroupArgs& a)
+{
+    Place p;
+    p.chunk = blockIdx.x; p.map = blockIdx.z; p.piece = 0; p.ngroups = a.gs; p.cols = a.width;
+    p.group0 = blockIdx.y * a.gs; p.col0 = blockIdx.y * a.width; p.row0 = p.chunk * a.rows_per; p.rows = rows_of(a, p.chunk);
+    return p;
+}
+
+// A CTA has rows_per rows of a slice; its cluster has the slice.  Each thread copies its own values into shared memory and reads them twice from there.  Distances are
+// taken from the group's first value in the CTA's first row, so that threads' sums just add up.
+template <typename T, int VE, bool ONE, int ACT>
+__global__ void __launch_bounds__(kMostResident) k_group_resident(const GroupArgs a)
+{
+    typedef Vec<T, VE> V;
+    typedef typename V::F F;
+    constexpr int P = V::P, IT = ONE ? 1 : VE, N = ONE ? 1 : P;
+    extern __shared__ uint4 kept[];                           // [rows_per][columns], then the partial sums
+    __shared__ float2 exchange[kMostCluster][kMostGroups], fin[kMostGroups];
+    cluster_started(a.chunks > 1);
+    dc_pdl_wait();
+    dc_pdl_release();
+    const Place p = resident_place(a);
+    int col, turn, turns;
+    seat(a, col, turn, turns);
+    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
+    const size_t at = (size_t)(p.col0 + col) * 16;
+    const char* const x = row_at(a.x, a.x_pitch, row0) + at;
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(kept) + 16u * threadIdx.x, line = 16u * turns * p.cols;
+    if (turn < turns) {
+        uint32_t to = mine;
+        for (int r = turn; r < p.rows; r += turns, to += line) copy16(to, x + (size_t)r * a.x_pitch);
+    }
+    float* const part = (float*)(kept + (size_t)a.rows_per * p.cols);     // [rows of partial sums][sums, squares][items]
+    const int items = p.cols * IT;
+    Column<T, VE, ONE> c;
+    c.weights(a, p, col);
+    F s[2 * N], first[N], unused[N];
+    if (p.rows > 0)
+        c.groups(a, p, col, first, unused, [&](int g) {
+            float v;
+            Vec<T, 1>::open(((const T*)row_at(a.x, a.x_pitch, row0))[(p.group0 + g) * a.per], &v);
+            return make_float2(-v, 0.f);
+        });
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) s[k] = both<F>(0.f);
+    copies_done();
+    if (turn < turns) {
+        const uint4* k4 = kept + threadIdx.x;
+#pragma unroll 4
+        for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols) {
+            F d[P];
+            V::open(*(const typename V::Raw*)k4, d);
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                const int i = ONE ? 0 : k;
+                const F t = add2(d[k], first[i]);
+                s[i] = add2(s[i], t);
+                s[N + i] = fma2(t, t, s[N + i]);
+            }
+        }
+    }
+    const int left = fold(s, p.cols, turns), to = fold_row(p.cols, turn, turns);
+    if (to >= 0)
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            part[to * 2 * items + col * IT + i] = ONE ? sum_of(s[0]) : lane_of(s[ONE ? 0 : i / 2], i & 1);
+            part[(to * 2 + 1) * items + col * IT + i] = ONE ? sum_of(s[N]) : lane_of(s[N + (ONE ? 0 : i / 2)], i & 1);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * items; i += blockDim.x) part[i] = rows_of_sums(part, left, 2 * items, i);       // (its own column alone)
+    __syncthreads();
+    cluster_wait(a.chunks > 1);
+    const int of = ONE && a.gs == p.cols ? 1 : items / p.ngroups;
+    for (int g = threadIdx.x >> 5; g < p.ngroups; g += blockDim.x >> 5) {
+        float sum = 0.f, squares = 0.f;
+        for (int i = g * of + (threadIdx.x & 31); i < (g + 1) * of; i += 32) { sum += part[i]; squares += part[items + i]; }
+        if (of > 1) { sum = reduce_lanes<Sum>(sum, 32); squares = reduce_lanes<Sum>(squares, 32); }
+        else { sum = __shfl_sync(0xffffffffu, sum, 0); squares = __shfl_sync(0xffffffffu, squares, 0); }
+        const float n = (float)p.rows * (float)a.per;
+        float2 r = make_float2(0.f, 0.f);
+        if (p.rows > 0) {
+            float v;
+            Vec<T, 1>::open(((const T*)row_at(a.x, a.x_pitch, row0))[(p.group0 + g) * a.per], &v);
+            const float m = sum / n;
+            r = make_float2(m + v, fmaxf(fmaf(-m, sum, squares), 0.f) + (sum - sum));
+        }
+        const int rank = threadIdx.x & 31;
+        if (rank < a.chunks) send(&exchange[p.chunk][g], rank, r);
+    }
+    if (a.chunks > 1) cluster_sync(); else __syncthreads();
+    if (threadIdx.x < p.ngroups) {
+        const int g = threadIdx.x;
+        const float total = (float)a.pixels * (float)a.per;
+        float mean = 0.f, squares = 0.f;
+        for (int k = 0; k < a.chunks; ++k) mean = fmaf((float)rows_of(a, k) * (float)a.per, exchange[k][g].x, mean);
+        mean /= total;
+        for (int k = 0; k < a.chunks; ++k) {
+            const float2 v = exchange[k][g];
+            const float w = (float)rows_of(a, k) * (float)a.per, d = v.x - mean;
+            if (w > 0.f) squares += fmaf(w * d, d, v.y);
+        }
+        const float rstd = inverse_root(squares / total + a.eps);
+        fin[g] = make_float2(-mean, rstd);
+        if (p.chunk == 0) {
+            if (a.mean) a.mean[(size_t)p.map * a.groups + p.group0 + g] = mean;
+            if (a.rstd) a.rstd[(size_t)p.map * a.groups + p.group0 + g] = rstd;
+        }
+    }
+    __syncthreads();
+    if (turn >= turns) return;
+    F mean[N], rstd[N];
+    c.groups(a, p, col, mean, rstd, [&](int g) { return fin[g]; });
+    char* y = row_at(a.y, a.y_pitch, row0 + turn) + at;
+    const uint4* k4 = kept + threadIdx.x;
+#pragma unroll 4
+    for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols, y += turns * a.y_pitch) {
+        F d[P];
+        V::open(*(const typename V::Raw*)k4, d);
+#pragma unroll
+        for (int k = 0; k < P; ++k) d[k] = affine(hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), c.g[k], c.b[k]);
+        activate<ACT, ONE>(d);
+        *(typename V::Raw*)y = V::close(d);
+    }
+}
+
+// The gradients likewise: x and dy are kept (behind a ReLU dy or zero, which is as exact).  SiLU's derivative is worked out twice: 32 maps of 56 x 56 x 256 bf16 55 us; with dz
+// kept as floats, which leaves an SM two CTAs in the place of four, 61.
+template <typename T, int VE, bool ONE, int ACT>
+__global__ void __launch_bounds__(kMostResident, ONE ? 4 : 2) k_group_back_resident(const GroupArgs a)
+{
+    typedef Vec<T, VE> V;
+    typedef typename V::F F;
+    constexpr int P = V::P, N = ONE ? 1 : P;
+    extern __shared__ uint4 kept[];                           // [2][rows_per][columns], then the partial sums
+    __shared__ float2 exchange[kMostCluster][kMostGroups], fin[kMostGroups];
+    cluster_started(a.chunks > 1);
+    dc_pdl_wait();
+    dc_pdl_release();
+    const Place p = resident_place(a);
+    const int wide = p.cols * VE;
+    int col, turn, turns;
+    seat(a, col, turn, turns);
+    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
+    const size_t at = (size_t)(p.col0 + col) * 16;
+    const char *const x = row_at(a.x, a.x_pitch, row0) + at, *const dy = row_at(a.dy, a.dy_pitch, row0) + at;
+    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(kept) + 16u * threadIdx.x, line = 16u * turns * p.cols, other = 16u * a.rows_per * p.cols;
+    if (turn < turns) {
+        uint32_t to = mine;
+        for (int r = turn; r < p.rows; r += turns, to += line) { copy16(to, x + (size_t)r * a.x_pitch); copy16(to + other, dy + (size_t)r * a.dy_pitch); }
+    }
+    float* const part = (float*)(kept + 2 * (size_t)a.rows_per * p.cols);     // [rows of partial sums][2][channels]
+    Column<T, VE, ONE> c;
+    c.weights(a, p, col);
+    F mean[N], rstd[N], s[2 * P];
+    const size_t of_map = (size_t)p.map * a.groups + p.group0;
+    c.groups(a, p, col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of_map + g), dc_ld(a.rstd + of_map + g)); });
+#pragma unroll
+    for (int k = 0; k < 2 * P; ++k) s[k] = both<F>(0.f);
+    copies_done();
+    const size_t half = (size_t)a.rows_per * p.cols;
+    if (turn < turns) {
+        uint4* k4 = kept + threadIdx.x;
+#pragma unroll 2
+        for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols) {
+            F d[P], e[P], z[P];
+            V::open(*(const typename V::Raw*)k4, d);
+            V::open(*(const typename V::Raw*)(k4 + half), e);
+#pragma unroll
+            for (int k = 0; k < P; ++k) { d[k] = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(d[k], c.g[k], c.b[k]); }
+            activate_back<ACT, ONE>(e, z);
+#pragma unroll
+            for (int k = 0; k < P; ++k) { s[k] = add2(s[k], e[k]); s[P + k] = fma2(e[k], d[k], s[P + k]); }
+            if (ACT == DC_ACT_RELU) *(typename V::Raw*)(k4 + half) = V::close(e);           // dy or zero: as exact as it came
+        }
+    }
+    const int left = fold(s, p.cols, turns), to = fold_row(p.cols, turn, turns);
+    if (to >= 0)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+            part[to * 2 * wide + col * VE + i] = lane_of(s[i / 2], i & 1);
+            part[(to * 2 + 1) * wide + col * VE + i] = lane_of(s[P + i / 2], i & 1);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * wide; i += blockDim.x) {
+        const float t = rows_of_sums(part, left, 2 * wide, i);
+        part[i] = t;                                          // (its own column alone)
+        if (a.sums) a.sums[((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + (i < wide ? p.col0 * VE + i : a.channels + p.col0 * VE + i - wide)] = t;
+    }
+    __syncthreads();
+    cluster_wait(a.chunks > 1);
+    const int of = wide / p.ngroups;
+    for (int g = threadIdx.x >> 5; g < p.ngroups; g += blockDim.x >> 5) {
+        float t1 = 0.f, t2 = 0.f;
+        for (int i = g * of + (threadIdx.x & 31); i < (g + 1) * of; i += 32) {
+            const float w = a.gamma ? dc_ld(a.gamma + p.col0 * VE + i) : 1.f;
+            t1 = fmaf(w, part[i], t1); t2 = fmaf(w, part[wide + i], t2);
+        }
+        t1 = reduce_lanes<Sum>(t1, 32); t2 = reduce_lanes<Sum>(t2, 32);
+        const int rank = threadIdx.x & 31;
+        if (rank < a.chunks) send(&exchange[p.chunk][g], rank, make_float2(t1, t2));
+    }
+    if (a.chunks > 1) cluster_sync(); else __syncthreads();
+    if (!a.y) return;
+    if (threadIdx.x < p.ngroups) {
+        float t1 = 0.f, t2 = 0.f;
+        for (int k = 0; k < a.chunks; ++k) { t1 += exchange[k][threadIdx.x].x; t2 += exchange[k][threadIdx.x].y; }
+        const float total = (float)a.pixels * (float)a.per;
+        fin[threadIdx.x] = make_float2(-t1 / total, -t2 / total);
+    }
+    __syncthreads();
+    if (turn >= turns) return;
+    F m1[N], m2[N];
+    c.groups(a, p, col, m1, m2, [&](int g) { return fin[g]; });
+    char* dx = row_at(a.y, a.y_pitch, row0 + turn) + at;
+    const uint4* k4 = kept + threadIdx.x;
+#pragma unroll 2
+    for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols, dx += turns * a.y_pitch) {
+        F d[P], e[P], z[P];
+        V::open(*(const typename V::Raw*)k4, d);
+        V::open(*(const typename V::Raw*)(k4 + half), e);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const int i = ONE ? 0 : k;
+            d[k] = hat(d[k], mean[i], rstd[i]);
+            z[k] = affine(d[k], c.g[k], c.b[k]);
+        }
+        if (ACT == DC_ACT_SILU) activate_back<ACT, ONE>(e, z);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const int i = ONE ? 0 : k;
+            d[k] = mul2(fma2(d[k], m2[i], add2(mul2(e[k], c.g[k]), m1[i])), rstd[i]);
+        }
+        *(typename V::Raw*)dx = V::close(d);
     }
 }
 
@@ -408,7 +758,8 @@ __global__ void __launch_bounds__(1024) k_group_join(const float* sums, int coun
 int most_chunks(int64_t maps, int64_t pixels)
 {
     int64_t c = (pixels + 15) / 16;
-    const int64_t room = maps > 0 ? (4096 + maps - 1) / maps : 1;
+    int64_t room = maps > 0 ? (4096 + maps - 1) / maps : 1;
+    if (room < kMostCluster) room = kMostCluster;
     if (c > room) c = room;
     return (int)(c > kMostChunks ? kMostChunks : c < 1 ? 1 : c);
 }
@@ -442,9 +793,71 @@ bool plan_columns(GroupArgs& a, int ve)
     return true;
 }
 
-template <typename T, int VE, bool ONE, int ACT>
-cudaError_t launch_group(const GroupArgs& a, bool back, cudaStream_t stream)
+// A slice in the shared memory of a cluster, if it fits: columns of 64 bytes a row (fewer where it does not), CTAs of up to 56 KB, four to an SM, so that some load while others compute
+// and store, or as many as a cluster has, or larger ones; 256 threads, or 128 where those would have fewer than four vectors each.  32 maps of 56 x 56 x 256 bf16, SiLU, us: forward 28.9
+// (columns of 32 bytes 34.2, of 128 34.6; 25 KB 30.5, 100 KB 40), gradients 55.1 (60.5, 61; 100 KB and more 80).
+constexpr int kWantKept = 56 * 1024, kMostKept = 200 * 1024;
+bool plan_resident(GroupArgs& a, int ve, int planes, int num_sms, int* block, size_t* smem)
 {
+    const int least = a.per / gcd(a.per, ve), unit = least * ve / a.per, bytes = 16 * planes;
+    if (a.channels % ve || a.groups % unit || least > 16 || a.maps > 65535) return false;
+    const int units = a.groups / unit;
+    int best = 0;
+    for (int j = 1; j <= units && j * least <= 16; ++j) {
+        if (units % j || j * unit > kMostGroups) continue;
+        if ((int64_t)a.pixels * j * least * bytes > (int64_t)kMostCluster * kMostKept) break;
+        best = j;
+        if (j * least >= 4) break;
+    }
+    if (!best) return false;
+    a.pieces = 1; a.gs = best * unit; a.width = best * least; a.slices = units / best;
+    const int64_t slice = (int64_t)a.pixels * a.width * bytes;
+    int turns = kMostResident / a.width;
+    a.by_width = dc_div_up(65536, a.width); a.by_per = dc_div_up(65536, a.per);
+    int cs = 1;
+    while (cs < kMostCluster && (slice > (int64_t)cs * kWantKept || ((int64_t)a.maps * a.slices * cs < num_sms && a.pixels >= 4 * cs * turns))) cs *= 2;
+    if (cs > most_chunks(a.maps, a.pixels)) return false;
+    a.rows_per = dc_div_up(a.pixels, cs);
+    a.chunks = cs;
+    const int threads = (int64_t)a.rows_per * a.width >= 4 * kMostResident ? kMostResident : kMostResident / 2;
+    turns = threads / a.width;
+    const int left = a.width & (a.width - 1) ? turns : threads / 32;
+    *block = threads;
+    *smem = (size_t)a.rows_per * a.width * bytes + (size_t)left * 2 * a.width * ve * sizeof(float);
+    return *smem <= (size_t)kMostKept + 16 * 1024;
+}
+
+template <typename T, int VE, bool ONE, int ACT>
+cudaError_t launch_resident(const GroupArgs& a, bool back, int block, size_t smem, int device, cudaStream_t stream)
+{
+    auto* const kernel = back ? k_group_back_resident<T, VE, ONE, ACT> : k_group_resident<T, VE, ONE, ACT>;
+    static dc_once_per_device set[2];
+    const cudaError_t e = set[back].ensure(device, [=] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostKept + 16 * 1024); });
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.chunks; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.chunks, (unsigned)a.slices, (unsigned)a.maps); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cfg.attrs = attr; cfg.numAttrs = g_dc_pdl ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+template <typename T, int VE, bool ONE, int ACT>
+cudaError_t launch_group(GroupArgs& a, bool back, int device, int num_sms, cudaStream_t stream)
+{
+    if constexpr (VE > 1) {
+        GroupArgs r = a;
+        size_t smem = 0;
+        int block = 0;
+        const int planes = back ? 2 : 1;                      // 16 bytes that are kept of a column's row: x, and dy
+        if (plan_resident(r, VE, planes, num_sms, &block, &smem)) {
+            a.chunks = r.chunks;                              // (for the join of the sums)
+            return launch_resident<T, VE, ONE, ACT>(r, back, block, smem, device, stream);
+        }
+    }
     const dim3 grid((unsigned)((int64_t)a.maps * a.slices * a.chunks));
     if (!back) {
         const cudaError_t e = dc_launch_pdl(k_group_stats<T, VE, ONE>, grid, kThreads, 0, stream, a);
@@ -454,13 +867,13 @@ cudaError_t launch_group(const GroupArgs& a, bool back, cudaStream_t stream)
     return e != cudaSuccess || !a.y ? e : dc_launch_pdl(k_group_back_apply<T, VE, ONE, ACT>, grid, kThreads, 0, stream, a);
 }
 template <typename T, int VE>
-cudaError_t launch_group_as(const GroupArgs& a, bool back, int activation, cudaStream_t stream)
+cudaError_t launch_group_as(GroupArgs& a, bool back, int activation, int device, int num_sms, cudaStream_t stream)
 {
 #define DC_GROUP(ONE) \
     switch (activation) { \
-    case DC_ACT_RELU: return launch_group<T, VE, ONE, DC_ACT_RELU>(a, back, stream); \
-    case DC_ACT_SILU: return launch_group<T, VE, ONE, DC_ACT_SILU>(a, back, stream); \
-    default: return launch_group<T, VE, ONE, DC_ACT_NONE>(a, back, stream); \
+    case DC_ACT_RELU: return launch_group<T, VE, ONE, DC_ACT_RELU>(a, back, device, num_sms, stream); \
+    case DC_ACT_SILU: return launch_group<T, VE, ONE, DC_ACT_SILU>(a, back, device, num_sms, stream); \
+    default: return launch_group<T, VE, ONE, DC_ACT_NONE>(a, back, device, num_sms, stream); \
     }
     if constexpr (VE > 1)
         if (a.per % VE) { DC_GROUP(false) }
@@ -471,6 +884,9 @@ cudaError_t launch_group_as(const GroupArgs& a, bool back, int activation, cudaS
 int launch(GroupArgs& a, bool back, int activation, int dtype, cudaStream_t stream)
 {
     const int elt = dtype == DC_BF16 ? 2 : 4, ve = 16 / elt;
+    int device = 0, sms = 0;
+    const int rc = dc_current_device(&device, &sms);
+    if (rc != DC_OK) return rc;
     auto aligned = [](const void* p, size_t pitch) { return (uintptr_t)p % 16 == 0 && pitch % 16 == 0; };
     const bool rows = (int64_t)a.maps * a.pixels > 1;
     const bool vec = aligned(a.x, rows ? a.x_pitch : 0) && (!a.y || aligned(a.y, rows ? a.y_pitch : 0)) && (!back || aligned(a.dy, rows ? a.dy_pitch : 0)) && plan_columns(a, ve);
@@ -481,8 +897,8 @@ int launch(GroupArgs& a, bool back, int activation, int dtype, cudaStream_t stre
     a.rows_per = dc_div_up(a.pixels, a.chunks);
     a.chunks = dc_div_up(a.pixels, a.rows_per);
     if ((int64_t)a.maps * a.slices * a.chunks > 0x7fffffff) return DC_ERR_LIMIT;
-    if (dtype == DC_BF16) DC_CUDA(vec ? (launch_group_as<__nv_bfloat16, 8>(a, back, activation, stream)) : (launch_group_as<__nv_bfloat16, 1>(a, back, activation, stream)));
-    else DC_CUDA(vec ? (launch_group_as<float, 4>(a, back, activation, stream)) : (launch_group_as<float, 1>(a, back, activation, stream)));
+    if (dtype == DC_BF16) DC_CUDA(vec ? (launch_group_as<__nv_bfloat16, 8>(a, back, activation, device, sms, stream)) : (launch_group_as<__nv_bfloat16, 1>(a, back, activation, device, sms, stream)));
+    else DC_CUDA(vec ? (launch_group_as<float, 4>(a, back, activation, device, sms, stream)) : (launch_group_as<float, 1>(a, back, activation, device, sms, stream)));
     return DC_OK;
 }
 
