@@ -6,7 +6,7 @@
 // k_quantize_row_blocks, k_quantize_tile: memory bounds them: a value is read once and leaves in its row, turned, or both.
 //
 // k_blocks: tcgen05.mma kind::f8f6f4 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, which are one block.  A block's sums leave
-// tensor memory as soon as they are there, are scaled and added up in the registers of eight warps, beside the MMAs of the next block (two accumulators in turns).
+// tensor memory as soon as they are there, are scaled and added up in the registers of eight warps, beside the MMAs of the next blocks (two to four accumulators in turns).
 #include "dc_product.cuh"
 #include "dc_quantise.cuh"
 
@@ -273,7 +273,7 @@ constexpr int kAddWarps = 8, kBlocksThreads = (4 + kAddWarps) * 32;
 constexpr int kBlocksMostStages = 8, kScaleSlots = 3;         // a slot: the scales of four blocks of K
 constexpr int kBox = 32 * 64;                                 // a warp's 32 rows on their way out, 64 bytes each; two of them
 struct BlocksCtl {
-    unsigned long long full[kBlocksMostStages], empty[kBlocksMostStages], tmem_full[2], tmem_empty[2], scale_full[kScaleSlots], scale_empty[kScaleSlots];
+    unsigned long long full[kBlocksMostStages], empty[kBlocksMostStages], tmem_full[4], tmem_empty[4], scale_full[kScaleSlots], scale_empty[kScaleSlots];
     uint32_t tmem_base;
     volatile int abort_flag;
     unsigned long long wait_ns;
@@ -297,8 +297,8 @@ DC_UMMA_F8(umma_f8_pair, "cta_group::2")
 
 // A bounded wait, of one thread or (WARP) of a whole warp.  What bounds the loops that wait is the instructions from one block of K to the next, so a wait that is over
 // at once is a look, a vote and nothing else; the clock is looked at after 256 looks.
-template <bool WARP>
-__device__ __forceinline__ bool blocks_wait(uint32_t bar, uint32_t parity, BlocksCtl* ctl)
+template <bool WARP, typename CTL>
+__device__ __forceinline__ bool blocks_wait(uint32_t bar, uint32_t parity, CTL* ctl)
 {
     unsigned long long t0 = 0;
 #pragma unroll 1
@@ -360,6 +360,19 @@ __device__ __forceinline__ void tmem_ld_wait32(uint32_t* r)
                    "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]) :: "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait16(uint32_t* r)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
+                   "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+
 // BN: columns of a tile.  EACH: b has a scale for each row and block, not for 128 rows.
 template <bool PAIR, int BN, bool EACH, typename T>
 __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC, const BlocksTiles a)
@@ -375,11 +388,11 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
     constexpr int M = PAIR ? 2 : 1;                           // row tiles of an item
-    constexpr uint32_t kColumns = 2 * BN;
+    constexpr uint32_t ACCS = BN > 128 ? 2 : 4, kColumns = ACCS * BN;         // accumulators
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], kAddWarps * M); }
+        for (int i = 0; i < (int)ACCS; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], kAddWarps * M); }
         for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 32); mbar_init(&ctl->scale_empty[i], kAddWarps); }
         ctl->abort_flag = 0;
         ctl->wait_ns = kWaitNs;
@@ -449,31 +462,31 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             if (rank == 0 && elect_one()) {
                 const uint64_t dconst = umma_desc(0, 1024, 2);
                 const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
-                const uint32_t mine = (uint32_t)warp - 1u, d = tmem_base + mine * (uint32_t)BN;
-                const uint32_t my_empty = smem_u32(&ctl->tmem_empty[mine]), my_full = smem_u32(&ctl->tmem_full[mine]);
+                const uint32_t mine = (uint32_t)warp - 1u, tmem_empty0 = smem_u32(&ctl->tmem_empty[0]), tmem_full0 = smem_u32(&ctl->tmem_full[0]);
                 RingPos r;
                 r.start(r0, (uint32_t)a.stages);
-                uint32_t turn = 0, acc_ph = 1;
+                uint32_t acc = 0, acc_ph = 1;
                 bool ok = true;
                 for (int item = first; item < n_items && ok; item += step)
-                    for (int kc = 0; kc < a.kb; ++kc, turn ^= 1u) {
-                        if (turn == mine) {
-                            ok = blocks_wait<false>(my_empty, acc_ph, ctl) && blocks_wait<false>(full0 + r.off, r.phase, ctl);
+                    for (int kc = 0; kc < a.kb; ++kc) {
+                        if ((acc & 1u) == mine) {
+                            ok = blocks_wait<false>(full0 + r.off, r.phase, ctl) && blocks_wait<false>(tmem_empty0 + 8u * acc, acc_ph, ctl);
                             if (!ok) break;
                             tc_fence_after();
                             const int n = kc + 1 < a.kb ? 4 : a.k_last;
+                            const uint32_t d = tmem_base + acc * (uint32_t)BN;
                             if (PAIR) {
                                 umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
-                                commit_pair(my_full);
+                                commit_pair(tmem_full0 + 8u * acc);
                                 commit_pair(empty0 + r.off);
                             } else {
                                 umma_f8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
-                                umma_commit_at(my_full);
+                                umma_commit_at(tmem_full0 + 8u * acc);
                                 umma_commit_at(empty0 + r.off);
                             }
-                            acc_ph ^= 1u;
                         }
                         r.next(r0, (uint32_t)a.stages, slot);
+                        if (++acc == ACCS) { acc = 0; acc_ph ^= 1u; }
                     }
             }
             __syncwarp();
@@ -573,7 +586,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                             if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
                             else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
                         }
-                        if (++acc == 2u) { acc = 0; acc_ph ^= 1u; }
+                        if (++acc == ACCS) { acc = 0; acc_ph ^= 1u; }
                         // (with an odd number of loads the next one's place is the one that is being read)
                         if (MINE / 32 % 2 == 0 && (kc + 1 < a.kb || item + step < n_items)) begin();
                     }
@@ -666,6 +679,289 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     }
 }
 
+// ---------------------------------------------------------------------------
+// products of few rows
+// ---------------------------------------------------------------------------
+// What bounds them are the weights, each read once: they are the side of 128 rows (tensor memory's lanes), the rows of a (16 to 128 of them) its columns, and the blocks of K are dealt to a
+// cluster of CTAs, enough of them for the weights to stream at HBM's rate.  Each CTA scales and adds up its own blocks in registers; the partial sums meet in distributed shared
+// memory, where CTA r finishes channels r * 128 / CS and on, in the order of the ranks.  `early`: everything older than the kernel before is complete (dc_linear_blocks: that kernel
+// puts x into 8 bits), so the weights' loads start before the wait for it.
+constexpr int kSplitThreads = 192, kSplitStages = 12, kSplitScales = 32 * 1024;
+// A CTA of it waits for its cluster, and tensor memory is given out without a limit on the wait: it takes at least this much shared memory for each 128 columns, so that what fits beside
+// it has columns too (as the split product of integers, dc_quant.cu).
+constexpr size_t kSplitLeast = 64 * 1024;
+struct BlocksSplit {
+    BlocksProduct p;
+    int CS, stages, kb, k_last, m_tiles, early;
+    uint32_t idesc;
+};
+struct BlocksSplitCtl {
+    unsigned long long full[kSplitStages], empty[kSplitStages], tmem_full[2], tmem_empty[2];
+    uint32_t tmem_base;
+    volatile int abort_flag;
+    unsigned long long wait_ns;
+};
+
+template <int NT, bool EACH, typename T>
+__global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const BlocksSplit a)
+{
+    constexpr uint32_t kStageBytes = kATile + NT * kBytesK, kColumns = 2 * NT < 32 ? 32 : 2 * NT;
+    constexpr int LD = NT < 32 ? 16 : 32;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* const ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    // [CS][NT / 4][128 / CS]: this CTA's channels, four rows' sums each, from every CTA; a warp's stores lie side by side
+    float4* const red = (float4*)(ring + (size_t)a.stages * kStageBytes);
+    BlocksSplitCtl* const ctl = (BlocksSplitCtl*)(red + 32 * NT);
+    float* const scale = (float*)(ctl + 1);                   // [this CTA's blocks][NT]: of the rows, without EACH times the weights'
+    const BlocksProduct& p = a.p;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const int rank = (int)cluster_rank(), item = blockIdx.x / a.CS, mt = item % a.m_tiles, nt = item / a.m_tiles;
+    const int nk = (a.kb - rank + a.CS - 1) / a.CS;           // block it * CS + rank: a cluster reads whole stretches of a row at once
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 2); mbar_init(&ctl->empty[i], 1); }   // weights and rows arrive apart
+        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], 4); }
+        ctl->abort_flag = 0;
+        ctl->wait_ns = kWaitNs;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(kColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // waited for before another CTA's shared memory is written
+    tc_fence_after();
+    const uint32_t tmem_base = ctl->tmem_base;
+    const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
+    const int ahead = nk < a.stages ? nk : a.stages;
+    auto load_weights = [&](int it, uint32_t off, uint32_t slot) {
+        mbar_expect_tx(full0 + off, (uint32_t)kATile);
+        tma_load_2d(slot, &tmW, (it * a.CS + rank) * kBytesK, nt * kTileM, full0 + off);
+    };
+    if (!a.early) { dc_pdl_wait(); dc_pdl_release(); }
+    if (warp == 0 && elect_one())
+        for (int it = 0; it < ahead; ++it) load_weights(it, 8u * it, ring0 + it * kStageBytes);
+    __syncwarp();
+    if (a.early) { dc_pdl_wait(); dc_pdl_release(); }
+
+    bool waited = false;                                                     // for the cluster
+    // the channel that this thread finishes: the threads are a multiple of a CTA's channels
+    const int rows = 128 / a.CS, ch = threadIdx.x % rows, j = nt * kTileM + rank * rows + ch;
+    const float bias = j < p.n && p.bias ? dc_ld(p.bias + j) : 0.f;
+    if (warp == 0) {
+        // ---------------- producer ----------------
+        if (elect_one()) {
+            RingPos r;
+            r.start(ring0, (uint32_t)a.stages);
+            bool ok = true;
+            for (int it = 0; it < nk; ++it) {
+                if (it >= a.stages) {
+                    ok = blocks_wait<false>(empty0 + r.off, r.phase ^ 1u, ctl);
+                    if (!ok) break;
+                    load_weights(it, r.off, r.data);
+                }
+                mbar_expect_tx(full0 + r.off, (uint32_t)(NT * kBytesK));
+                tma_load_2d(r.data + kATile, &tmX, (it * a.CS + rank) * kBytesK, mt * NT, full0 + r.off);
+                r.next(ring0, (uint32_t)a.stages, kStageBytes);
+            }
+            if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------- MMA issuer ----------------
+        if (elect_one()) {
+            const uint64_t dconst = umma_desc(0, 1024, 2);
+            const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4);
+            RingPos r;
+            r.start(r0, (uint32_t)a.stages);
+            uint32_t acc = 0, acc_ph = 1;
+            for (int it = 0; it < nk; ++it) {
+                if (!blocks_wait<false>(full0 + r.off, r.phase, ctl) || !blocks_wait<false>(smem_u32(&ctl->tmem_empty[acc]), acc_ph, ctl)) break;
+                tc_fence_after();
+                umma_f8(tmem_base + acc * NT, r.data, r.data + (kATile >> 4), d_hi, a.idesc, it * a.CS + rank + 1 < a.kb ? 4 : a.k_last);
+                umma_commit_at(smem_u32(&ctl->tmem_full[acc]));
+                umma_commit_at(empty0 + r.off);
+                r.next(r0, (uint32_t)a.stages, kStageBytes >> 4);
+                acc ^= 1u;
+                acc_ph ^= acc == 0;
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---------------- sums of this CTA's blocks, and their way to the CTA that finishes the channel ----------------
+        const int q = warp & 3, m = q * 32 + lane, owner = m / rows;
+        for (int i = threadIdx.x - 64; i < nk * NT; i += 128) {
+            const int64_t row = (int64_t)mt * NT + i % NT;
+            const int at = i / NT * a.CS + rank;
+            float s = row < p.m ? p.a_scale[row * a.kb + at] : 0.f;
+            if (!EACH) s *= dc_ld(p.b_scale + (size_t)nt * a.kb + at);
+            scale[i] = s;
+        }
+        const float* const weight_scale = p.b_scale + (size_t)min(nt * kTileM + m, p.n - 1) * a.kb + rank;      // EACH: of this lane's channel
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        uint64_t sum[NT / 2];
+#pragma unroll
+        for (int i = 0; i < NT / 2; ++i) sum[i] = 0;
+        uint32_t acc = 0, acc_ph = 0;
+        const uint32_t scale0 = smem_u32(scale);
+        bool ok = true;
+        float next = EACH && nk > 0 ? weight_scale[0] : 1.f;
+        for (int it = 0; it < nk; ++it) {
+            const uint32_t sw = __float_as_uint(next);
+            if (EACH && it + 1 < nk) next = weight_scale[(size_t)(it + 1) * a.CS];
+            ok = blocks_wait<true>(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t from = tmem_base + acc * NT + ((uint32_t)(q * 32) << 16);
+#pragma unroll
+            for (int c = 0; c < NT; c += LD) {
+                uint32_t v[LD];
+                if constexpr (LD == 32) { tmem_ld32(from + c, v); tmem_ld_wait32(v); }
+                else { tmem_ld16(from + c, v); tmem_ld_wait16(v); }
+#pragma unroll
+                for (int i = 0; i < LD / 2; i += 2) {
+                    uint64_t s[2], t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
+                    lds_pairs(scale0 + (uint32_t)(it * NT + c + 2 * i) * 4, s);
+                    if (EACH) { t[0] = product(t[0], pair_of(sw, sw)); t[1] = product(t[1], pair_of(sw, sw)); }
+                    add_product(sum[c / 2 + i], t[0], s[0]);
+                    add_product(sum[c / 2 + i + 1], t[1], s[1]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
+            acc ^= 1u;
+            acc_ph ^= acc == 0;
+        }
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        waited = true;
+        if (ok) {
+            const uint32_t dst = map_to_cta(red + rank * (NT / 4) * rows + m - owner * rows, (uint32_t)owner);
+            const int there = (int)min((int64_t)NT, p.m - (int64_t)mt * NT);
+#pragma unroll
+            for (int c = 0; c < NT; c += 4)
+                if (c < there) {
+                    const float2 x = floats_of(sum[c / 2]), y = floats_of(sum[c / 2 + 1]);
+                    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)(c / 4 * rows * 16)), "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y) : "memory");
+                }
+        }
+    }
+    if (!waited) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    // a CTA that gave up has not sent its sums: every CTA of the cluster hears of it
+    if (ctl->abort_flag != 0)
+        for (int r = 0; r < a.CS; ++r)
+            asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_to_cta((const void*)&ctl->abort_flag, (uint32_t)r)), "r"(1) : "memory");
+    cluster_sync_all();                      // this CTA's channels have arrived from every CTA
+    {
+        // ---------------- this CTA's channels: sums from all ranks, bias, ReLU, rounding, store ----------------
+        const int there = (int)min((int64_t)NT, p.m - (int64_t)mt * NT);
+        const float dead = ctl->abort_flag != 0 ? __uint_as_float(0x7fffffffu) : 0.f;        // what is stored says so
+        for (int t = threadIdx.x / rows * 4; t < there && j < p.n; t += kSplitThreads / rows * 4) {    // four rows of a
+            float4 sum = make_float4(dead, dead, dead, dead);
+            for (int r = 0; r < a.CS; ++r) {
+                const float4 v = red[(r * (NT / 4) + t / 4) * rows + ch];
+                sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+            }
+            const float sums[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (t + k >= there) break;
+                float f = sums[k] + bias;
+                if (p.relu) f = clamped<true>(f);
+                T* const out = (T*)((char*)p.out + (size_t)((int64_t)mt * NT + t + k) * p.out_pitch) + j;
+                if constexpr (sizeof(T) == 4) *out = f;
+                else *out = __float2bfloat16_rn(f);
+            }
+        }
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kColumns) : "memory");
+    }
+}
+
+// Clusters of so many CTAs, each with an SM of its own, that the device holds at once.
+int clusters_at_once(int cs, int device)
+{
+    static std::atomic<int> known[64][4];
+    const int at = cs == 1 ? 0 : cs == 2 ? 1 : cs == 4 ? 2 : 3;
+    if (device >= 0 && device < 64)
+        if (const int n = known[device][at].load(std::memory_order_relaxed)) return n;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)cs); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = 200 * 1024; cfg.attrs = attr; cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(k_blocks_split<16, false, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, k_blocks_split<16, false, float>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
+    if (n < 1) n = 1;
+    if (device >= 0 && device < 64) known[device][at].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+// How a product of few tiles is split, and the cycles that it takes (as launch_product counts them).
+struct SplitPlan { int NT, CS; double cost; };
+SplitPlan split_plan(const BlocksProduct& p, int kb, int device)
+{
+    SplitPlan best = {};
+    const int NT = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
+    const long long tiles = (p.m + NT - 1) / NT * (long long)dc_div_up(p.n, kTileM);
+    for (int cs = 2; cs <= 8 && cs <= kb; cs *= 2) {
+        if ((size_t)dc_div_up(kb, cs) * NT * sizeof(float) > (size_t)kSplitScales) continue;
+        const int at_once = clusters_at_once(cs, device);
+        const long long rounds = (tiles + at_once - 1) / at_once;
+        // HBM's 3400 bytes a cycle shared by the CTAs; a block's way through tensor memory; to send the sums, join and store them
+        const double load = (kATile + NT * kBytesK) / 50.0, hbm = kATile * (double)(tiles * cs < at_once * cs ? tiles * cs : at_once * cs) / 3400.0, add = 400.0 + 4.0 * NT;
+        const double join = 2500.0 + NT * (cs == 8 ? 30.0 : cs == 4 ? 40.0 : 50.0);
+        const double step = load > hbm ? (load > add ? load : add) : (hbm > add ? hbm : add), cost = rounds * (dc_div_up(kb, cs) * step + join);
+        if (rounds <= 2 && (best.CS == 0 || cost < best.cost)) best = {NT, cs, cost};
+    }
+    return best;
+}
+
+template <int NT, bool EACH, typename T>
+int launch_split_as(const BlocksProduct& p, const SplitPlan& s, int kb, int early, int device, cudaStream_t stream)
+{
+    BlocksSplit a = {};
+    a.p = p; a.CS = s.CS; a.kb = kb; a.k_last = dc_div_up(p.k - (kb - 1) * kBytesK, 32); a.early = early;
+    a.m_tiles = (int)((p.m + NT - 1) / NT);
+    const int stage = kATile + NT * kBytesK, most = dc_div_up(kb, s.CS), fixed = 128 * NT * 4 + (int)sizeof(BlocksSplitCtl) + 1024 + most * NT * 4, room = (kBlocksSmem - fixed) / stage;
+    a.stages = room < kSplitStages ? room : kSplitStages;
+    if (a.stages > most) a.stages = most;
+    a.idesc = (1u << 4) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+    CUtensorMap tmW, tmX;
+    if (!encode_rows(&tmW, p.b, p.b_pitch, p.n, p.k, kTileM) || !encode_rows(&tmX, p.a, p.a_pitch, p.m, p.k, NT)) return DC_ERR_CUDA;
+    static dc_once_per_device attr_set;
+    DC_CUDA(attr_set.ensure(device, [] { return cudaFuncSetAttribute(k_blocks_split<NT, EACH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem); }));
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)s.CS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.m_tiles * dc_div_up(p.n, kTileM) * s.CS)); cfg.blockDim = dim3(kSplitThreads);
+    const size_t smem = (size_t)a.stages * stage + fixed, least = kSplitLeast * (NT > 64 ? 2 : 1);
+    cfg.dynamicSmemBytes = smem > least ? smem : least; cfg.stream = stream;
+    cfg.attrs = attr; cfg.numAttrs = g_dc_pdl ? 2 : 1;
+    DC_CUDA(cudaLaunchKernelEx(&cfg, k_blocks_split<NT, EACH, T>, tmW, tmX, a));
+    return DC_OK;
+}
+template <bool EACH, typename T>
+int launch_split(const BlocksProduct& p, const SplitPlan& s, int kb, int early, int device, cudaStream_t stream)
+{
+    switch (s.NT) {
+    case 16: return launch_split_as<16, EACH, T>(p, s, kb, early, device, stream);
+    case 32: return launch_split_as<32, EACH, T>(p, s, kb, early, device, stream);
+    case 64: return launch_split_as<64, EACH, T>(p, s, kb, early, device, stream);
+    default: return launch_split_as<128, EACH, T>(p, s, kb, early, device, stream);
+    }
+}
+
 template <bool PAIR, int BN, bool EACH, typename T>
 int launch_blocks(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC, const BlocksTiles& a, int ctas, int device, cudaStream_t stream)
 {
@@ -689,7 +985,8 @@ int launch_blocks(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensor
     return DC_OK;
 }
 
-int launch_product(const BlocksProduct& p, int dtype, int device, int num_sms, cudaStream_t stream)
+// early: b, its scales and bias are older than the kernel before, which waits for its own predecessor.
+int launch_product(const BlocksProduct& p, int dtype, bool early, int device, int num_sms, cudaStream_t stream)
 {
     BlocksTiles a = {};
     a.p = p;
@@ -703,9 +1000,16 @@ int launch_product(const BlocksProduct& p, int dtype, int device, int num_sms, c
         const bool two = c < 2;
         const int bn = c == 0 ? 256 : c == 3 ? 64 : 128;
         const long long n_items = (two ? (a.m_tiles + 1) / 2 : a.m_tiles) * (long long)dc_div_up(p.n, bn), at_once = two ? num_sms / 2 : num_sms, rounds = (n_items + at_once - 1) / at_once;
-        const double load = a.kb * (double)(kATile + (two ? bn / 2 : bn) * kBytesK) / 50.0, mma = a.kb * 2.0 * bn, out = 128.0 * bn * elt / 24.0;
+        const double load = a.kb * (double)(kATile + (two ? bn / 2 : bn) * kBytesK) / 50.0, mma = a.kb * (500.0 + 2.0 * bn), out = 128.0 * bn * elt / 24.0;
         const double cost = rounds * ((load > mma ? load : mma) + out + 500.0);
         if (c == 0 || cost < best) { best = cost; pair = two; BN = bn; }
+    }
+    if (p.n <= (1 << 20) && p.m <= (1 << 20)) {
+        const SplitPlan s = split_plan(p, a.kb, device);
+        if (s.CS > 1 && s.cost < best) {
+            if (p.b_block_rows == 1) return dtype == DC_BF16 ? launch_split<true, __nv_bfloat16>(p, s, a.kb, early, device, stream) : launch_split<true, float>(p, s, a.kb, early, device, stream);
+            return dtype == DC_BF16 ? launch_split<false, __nv_bfloat16>(p, s, a.kb, early, device, stream) : launch_split<false, float>(p, s, a.kb, early, device, stream);
+        }
     }
     a.NB = dc_div_up(p.n, BN);
     const int b_rows = pair ? BN / 2 : BN;
@@ -818,7 +1122,7 @@ int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_
     int device = 0, sms = 0;
     if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
     const BlocksProduct p = {a_dev, a_pitch, a_scale_dev, b_dev, b_pitch, b_scale_dev, bias_dev, m, n, k, relu, b_block_rows, out_dev, out_pitch};
-    return launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
+    return launch_product(p, dtype, false, device, sms, (cudaStream_t)cuda_stream);
 }
 
 int dc_linear_blocks_workspace(int64_t m, int32_t k, size_t* bytes)
@@ -847,7 +1151,7 @@ int dc_linear_blocks(const void* x_dev, size_t x_pitch, const uint8_t* w_dev, si
     a.x = x_dev; a.x_pitch = x_pitch; a.rows = (int)m; a.channels = k; a.block_rows = 1; a.q = q; a.q_pitch = pitch; a.scale = scale;
     if ((rc = quantize(a, dtype, device, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
     const BlocksProduct p = {q, pitch, scale, w_dev, w_pitch, w_scale_dev, bias_dev, m, n, k, relu, w_block_rows, out_dev, out_pitch};
-    return launch_product(p, dtype, device, sms, (cudaStream_t)cuda_stream);
+    return launch_product(p, dtype, true, device, sms, (cudaStream_t)cuda_stream);
 }
 
 }  // extern "C"
