@@ -269,7 +269,7 @@ struct BlocksTiles {
     int wide, boxes;                                          // out takes 16-byte stores; is written in boxes by TMA
 };
 
-constexpr int kAddWarps = 8, kBlocksThreads = (4 + kAddWarps) * 32;
+constexpr int kAddWarps = 16, kFirstAdder = 3, kBlocksThreads = (kFirstAdder + kAddWarps) * 32;
 constexpr int kBlocksMostStages = 8, kScaleSlots = 3;         // a slot: the scales of four blocks of K
 constexpr int kBox = 32 * 64;                                 // a warp's 32 rows on their way out, 64 bytes each; two of them
 struct BlocksCtl {
@@ -387,13 +387,13 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     const BlocksProduct& p = a.p;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
-    constexpr int M = PAIR ? 2 : 1;                           // row tiles of an item
+    constexpr int M = PAIR ? 2 : 1, PARTS = BN < 128 ? 2 : 4; // row tiles of an item; warps that share a row's columns
     constexpr uint32_t ACCS = BN > 128 ? 2 : 4, kColumns = ACCS * BN;         // accumulators
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], 1); }
-        for (int i = 0; i < (int)ACCS; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], kAddWarps * M); }
-        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 32); mbar_init(&ctl->scale_empty[i], kAddWarps); }
+        for (int i = 0; i < (int)ACCS; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], 4 * PARTS * M); }
+        for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 32); mbar_init(&ctl->scale_empty[i], 4 * PARTS); }
         ctl->abort_flag = 0;
         ctl->wait_ns = kWaitNs;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -425,8 +425,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     };
     const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
 
-    if (warp < 4) {
-        if (BN == 256) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp < kFirstAdder) {
         if (warp == 0) {
             // ---------------- producer ----------------
             if (elect_one()) {
@@ -455,35 +454,31 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
             }
             __syncwarp();
-        } else if (warp < 3) {
-            // ---------------- MMA issuers (of a pair: the leader's, for both CTAs) ----------------
-            // Each block of K has an accumulator of its own, so two warps issue in turns: two waits, four MMAs and two commits take one warp 1000 cycles, a block's
-            // MMAs 512.
+        } else if (warp == 1) {
+            // ---------------- MMA issuer (of a pair: the leader's, for both CTAs) ----------------
             if (rank == 0 && elect_one()) {
                 const uint64_t dconst = umma_desc(0, 1024, 2);
                 const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
-                const uint32_t mine = (uint32_t)warp - 1u, tmem_empty0 = smem_u32(&ctl->tmem_empty[0]), tmem_full0 = smem_u32(&ctl->tmem_full[0]);
+                const uint32_t tmem_empty0 = smem_u32(&ctl->tmem_empty[0]), tmem_full0 = smem_u32(&ctl->tmem_full[0]);
                 RingPos r;
                 r.start(r0, (uint32_t)a.stages);
                 uint32_t acc = 0, acc_ph = 1;
                 bool ok = true;
                 for (int item = first; item < n_items && ok; item += step)
                     for (int kc = 0; kc < a.kb; ++kc) {
-                        if ((acc & 1u) == mine) {
-                            ok = blocks_wait<false>(full0 + r.off, r.phase, ctl) && blocks_wait<false>(tmem_empty0 + 8u * acc, acc_ph, ctl);
-                            if (!ok) break;
-                            tc_fence_after();
-                            const int n = kc + 1 < a.kb ? 4 : a.k_last;
-                            const uint32_t d = tmem_base + acc * (uint32_t)BN;
-                            if (PAIR) {
-                                umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
-                                commit_pair(tmem_full0 + 8u * acc);
-                                commit_pair(empty0 + r.off);
-                            } else {
-                                umma_f8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
-                                umma_commit_at(tmem_full0 + 8u * acc);
-                                umma_commit_at(empty0 + r.off);
-                            }
+                        ok = blocks_wait<false>(full0 + r.off, r.phase, ctl) && blocks_wait<false>(tmem_empty0 + 8u * acc, acc_ph, ctl);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int n = kc + 1 < a.kb ? 4 : a.k_last;
+                        const uint32_t d = tmem_base + acc * (uint32_t)BN;
+                        if (PAIR) {
+                            umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                            commit_pair(tmem_full0 + 8u * acc);
+                            commit_pair(empty0 + r.off);
+                        } else {
+                            umma_f8(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                            umma_commit_at(tmem_full0 + 8u * acc);
+                            umma_commit_at(empty0 + r.off);
                         }
                         r.next(r0, (uint32_t)a.stages, slot);
                         if (++acc == ACCS) { acc = 0; acc_ph ^= 1u; }
@@ -531,30 +526,20 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
         }
-    } else {
+    } else if (warp < kFirstAdder + 4 * PARTS) {
         // ---------------- sums of the blocks; bias, ReLU, rounding, store ----------------
-        // A warp has 32 rows, one to a lane (the quadrant of tensor memory that it may read), and half of the columns.
-        if (BN == 256) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-        constexpr int MINE = BN / 2;
-        const int q = warp & 3, half = (warp - 4) >> 2;
-        uint32_t stage = smem_u32(staging) + (uint32_t)(warp - 4) * kBox;
+        // A warp has 32 rows, one to a lane (the quadrant of tensor memory that it may read), and a quarter of the columns (of 64: half, so that they make a box; the rest has nothing to do).
+        constexpr int MINE = BN / PARTS;
+        const int q = warp & 3, part = (warp - kFirstAdder) >> 2;
+        uint32_t stage = smem_u32(staging) + (uint32_t)(warp - kFirstAdder) * kBox;
         const uint32_t both_places = a.bufs == 2 ? stage ^ (stage + kAddWarps * kBox) : 0;       // from one place to the other
         const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
-        const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + lane) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? half * MINE : BN > 128 ? half * 4 : 0) * 4;
+        const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + lane) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? part * MINE : BN > 128 ? part / 2 * 4 : 0) * 4;
         uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0;
         bool ok = true, there;
-        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]), from0 = tmem_base + (uint32_t)(half * MINE) + ((uint32_t)(q * 32) << 16);
-        uint32_t v[2][32];
-        // the next block's sums are there: the first of them on their way
-        auto begin = [&]() {
-            ok = ok && blocks_wait<true>(tmem_full0 + 8u * acc, acc_ph, ctl);
-            if (!ok) return;
-            tc_fence_after();
-            tmem_ld32(from0 + acc * (uint32_t)BN, v[0]);
-        };
-        if (first < n_items) begin();
+        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]), from0 = tmem_base + (uint32_t)(part * MINE) + ((uint32_t)(q * 32) << 16);
         for (int item = first; item < n_items; item += step) {
-            const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN + half * MINE;
+            const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN + part * MINE;
             const int64_t row0 = (int64_t)tile * kTileM + q * 32;
             const int rows = there ? (int)max((int64_t)0, min((int64_t)32, p.m - row0)) : 0;
             float4 scales = make_float4(0.f, 0.f, 0.f, 0.f);  // four blocks'
@@ -564,7 +549,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             for (int kc = 0; kc < a.kb && ok; ++kc) {
                 const int u = kc & 3;
                 if (u == 0) {
-                    ok = ok && blocks_wait<true>(smem_u32(&ctl->scale_full[slot]), phase, ctl);
+                    ok = blocks_wait<true>(smem_u32(&ctl->scale_full[slot]), phase, ctl);
                     scales = lds_floats(my_rows + slot * (kRowScales * 4));
                     if (!EACH) {
                         const float4 b = lds_floats(my_cols + slot * (kCols * 4));
@@ -573,13 +558,16 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 }
                 const uint32_t s1 = __float_as_uint(u == 0 ? scales.x : u == 1 ? scales.y : u == 2 ? scales.z : scales.w);
                 const uint64_t s = pair_of(s1, s1);
+                ok = ok && blocks_wait<true>(tmem_full0 + 8u * acc, acc_ph, ctl);
+                if (!ok) break;
+                tc_fence_after();
                 const uint32_t from = from0 + acc * (uint32_t)BN;
 #pragma unroll
-                for (int c = 0; c < MINE / 32; ++c) {
-                    uint32_t* const now = v[c & 1];
-                    tmem_ld_wait32(now);
-                    if (c + 1 < MINE / 32) tmem_ld32(from + 32 * (c + 1), v[(c + 1) & 1]);      // on its way meanwhile
-                    else {
+                for (int c = 0; c < MINE; c += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(from + c, v);
+                    tmem_ld_wait16(v);
+                    if (c + 16 == MINE) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) {
@@ -587,23 +575,20 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                             else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
                         }
                         if (++acc == ACCS) { acc = 0; acc_ph ^= 1u; }
-                        // (with an odd number of loads the next one's place is the one that is being read)
-                        if (MINE / 32 % 2 == 0 && (kc + 1 < a.kb || item + step < n_items)) begin();
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        uint64_t t[2] = {pair_of(now[2 * i], now[2 * i + 1]), pair_of(now[2 * i + 2], now[2 * i + 3])};
+                    for (int i = 0; i < 8; i += 2) {
+                        uint64_t t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
                         if (EACH) {
                             uint64_t b[2];
-                            lds_pairs(my_cols + slot * (kCols * 4) + (uint32_t)(u * 256 + 32 * c + 2 * i) * 4, b);
+                            lds_pairs(my_cols + slot * (kCols * 4) + (uint32_t)(u * 256 + c + 2 * i) * 4, b);
                             t[0] = product(t[0], b[0]);
                             t[1] = product(t[1], b[1]);
                         }
-                        add_product(sum[16 * c + i], t[0], s);
-                        add_product(sum[16 * c + i + 1], t[1], s);
+                        add_product(sum[c / 2 + i], t[0], s);
+                        add_product(sum[c / 2 + i + 1], t[1], s);
                     }
                 }
-                if (MINE / 32 % 2 != 0 && (kc + 1 < a.kb || item + step < n_items)) begin();
                 if (u == 3 || kc + 1 == a.kb) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive_relaxed(&ctl->scale_empty[slot]);       // (the scales have long been read: sums were made of them)
@@ -967,11 +952,7 @@ int launch_blocks(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensor
 {
     static dc_once_per_device attr_set;
     DC_CUDA(attr_set.ensure(device, [] {
-        // the warps that add up take registers that the others give back: 128 * 56 + 256 * 224 = 384 * 168 in all
-        cudaFuncAttributes at;
-        cudaError_t e = cudaFuncGetAttributes(&at, k_blocks<PAIR, BN, EACH, T>);
-        if (e == cudaSuccess && BN == 256 && at.numRegs < 168) return cudaErrorInvalidKernelImage;
-        return e != cudaSuccess ? e : cudaFuncSetAttribute(k_blocks<PAIR, BN, EACH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem);
+        return cudaFuncSetAttribute(k_blocks<PAIR, BN, EACH, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem);
     }));
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
