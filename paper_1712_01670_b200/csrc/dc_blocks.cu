@@ -295,29 +295,52 @@ DC_UMMA_F8(umma_f8, "cta_group::1")
 DC_UMMA_F8(umma_f8_pair, "cta_group::2")
 #undef DC_UMMA_F8
 
-// A bounded wait, of one thread or (WARP) of a whole warp.  What bounds the loops that wait is the instructions from one block of K to the next, so a wait that is over
-// at once is a look, a vote and nothing else; the clock is looked at after 256 looks.
-template <bool WARP, typename CTL>
+// Bounded waits, of one thread and of a whole warp.  What bounds the loops that wait is the instructions, and most of all the branches, from one block of K to the next: a wait that is over
+// at once is a look (of a warp: and a vote) and nothing else; the clock is looked at after 256 more.
+template <typename CTL>
+__device__ __forceinline__ bool blocks_late(CTL* ctl, uint32_t spin, unsigned long long& t0)
+{
+    if ((spin & 255u) != 255u) return false;
+    const unsigned long long t = now_ns();
+    if (spin == 255u) t0 = t;
+    if (ctl->abort_flag == 0 && t - t0 <= ctl->wait_ns) return false;
+    ctl->abort_flag = 1;
+    atomicExch(&g_blocks_status, (int)DC_ERR_TIMEOUT);
+    return true;
+}
+template <typename CTL>
 __device__ __forceinline__ bool blocks_wait(uint32_t bar, uint32_t parity, CTL* ctl)
 {
     unsigned long long t0 = 0;
 #pragma unroll 1
-    for (uint32_t spin = 0;; ++spin) {
-        bool done = mbar_try(bar, parity);
-        if (WARP) done = __all_sync(0xffffffffu, done);
-        if (done) return true;
-        if ((spin & 255u) == 255u) {
-            const unsigned long long t = now_ns();
-            if (spin == 255u) t0 = t;
-            bool over = ctl->abort_flag != 0 || t - t0 > ctl->wait_ns;
-            if (WARP) over = __any_sync(0xffffffffu, over);
-            if (over) {
-                ctl->abort_flag = 1;
-                atomicExch(&g_blocks_status, (int)DC_ERR_TIMEOUT);
-                return false;
-            }
-        }
-    }
+    for (uint32_t spin = 0; !mbar_try(bar, parity); ++spin)
+        if (blocks_late(ctl, spin, t0)) return false;
+    return true;
+}
+__device__ __forceinline__ uint32_t look(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p, q;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tvote.sync.all.pred q, p, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done;
+}
+// `dead`: a wait has run out; nothing is waited for any more.
+template <typename CTL>
+__device__ __forceinline__ void blocks_wait_warp(uint32_t bar, uint32_t parity, CTL* ctl, uint32_t& dead)
+{
+    if (__builtin_expect(look(bar, parity), 1)) return;
+    unsigned long long t0 = 0;
+#pragma unroll 1
+    for (uint32_t spin = 0; !dead && !look(bar, parity); ++spin) dead = __any_sync(0xffffffffu, blocks_late(ctl, spin, t0));
+}
+// An arrival of lane 0, without a branch.
+__device__ __forceinline__ void arrive_first(uint32_t bar, int lane)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(lane) : "memory");
+}
+__device__ __forceinline__ void arrive_first_remote(uint32_t bar, int lane)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t}" ::"r"(bar), "r"(lane) : "memory");
 }
 __device__ __forceinline__ float4 lds_floats(uint32_t at)
 {
@@ -436,7 +459,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 for (int item = first; item < n_items && ok; item += step) {
                     const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * BN + rank * (BN / 2);
                     for (int kc = 0; kc < a.kb; ++kc) {
-                        ok = blocks_wait<false>(empty0 + r.off, r.phase ^ 1u, ctl);
+                        ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
                         if (!ok) break;
                         if (PAIR) {
                             if (rank == 0) mbar_expect_tx(full0 + r.off, 2u * (uint32_t)a.stage_bytes);
@@ -466,7 +489,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 bool ok = true;
                 for (int item = first; item < n_items && ok; item += step)
                     for (int kc = 0; kc < a.kb; ++kc) {
-                        ok = blocks_wait<false>(full0 + r.off, r.phase, ctl) && blocks_wait<false>(tmem_empty0 + 8u * acc, acc_ph, ctl);
+                        ok = blocks_wait(full0 + r.off, r.phase, ctl) && blocks_wait(tmem_empty0 + 8u * acc, acc_ph, ctl);
                         if (!ok) break;
                         tc_fence_after();
                         const int n = kc + 1 < a.kb ? 4 : a.k_last;
@@ -490,17 +513,18 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             // Copied four blocks at a time, straight into shared memory, several slots ahead.  A row's scales lie side by side: 16 bytes to a copy where they are
             // aligned.  A lane has four rows, and of EACH's columns eight at most.
             uint32_t slot = 0, phase = 0;
-            bool ok = true, there;
+            uint32_t dead = 0;
+            bool there;
             const bool quads = a.kb % 4 == 0 && ((uintptr_t)p.a_scale | (uintptr_t)p.b_scale) % 16 == 0;
-            for (int item = first; item < n_items && ok; item += step) {
+            for (int item = first; item < n_items && !dead; item += step) {
                 const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN;
                 const float* const rows = p.a_scale + ((size_t)tile * kTileM + lane) * a.kb;
                 const int n_rows = (int)min((int64_t)kTileM, p.m - (int64_t)tile * kTileM) - lane;
                 const int j0 = EACH ? n0 + lane : n0 / 128 + lane, n_cols = EACH ? p.n - j0 : lane < 2 ? (p.n + 127) / 128 - j0 : 0;
                 const float* const cols = p.b_scale + (size_t)j0 * a.kb;
                 for (int kc = 0; kc < a.kb; kc += 4) {
-                    ok = blocks_wait<true>(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl);
-                    if (!ok) break;
+                    blocks_wait_warp(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl, dead);
+                    if (dead) break;
                     const uint32_t rows_at = smem_u32(row_scale + slot * kRowScales) + 16 * lane, cols_at = smem_u32(col_scale + slot * kCols);
                     if (quads) {
 #pragma unroll
@@ -535,67 +559,64 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
         const uint32_t both_places = a.bufs == 2 ? stage ^ (stage + kAddWarps * kBox) : 0;       // from one place to the other
         const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
         const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + lane) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? part * MINE : BN > 128 ? part / 2 * 4 : 0) * 4;
-        uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0;
-        bool ok = true, there;
-        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]), from0 = tmem_base + (uint32_t)(part * MINE) + ((uint32_t)(q * 32) << 16);
+        uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0, dead = 0;
+        bool there;
+        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]), tmem_empty0 = smem_u32(&ctl->tmem_empty[0]), from0 = tmem_base + (uint32_t)(part * MINE) + ((uint32_t)(q * 32) << 16);
+        const uint32_t scale_full0 = smem_u32(&ctl->scale_full[0]), scale_empty0 = smem_u32(&ctl->scale_empty[0]);
         for (int item = first; item < n_items; item += step) {
             const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN + part * MINE;
             const int64_t row0 = (int64_t)tile * kTileM + q * 32;
             const int rows = there ? (int)max((int64_t)0, min((int64_t)32, p.m - row0)) : 0;
-            float4 scales = make_float4(0.f, 0.f, 0.f, 0.f);  // four blocks'
             uint64_t sum[MINE / 2];
 #pragma unroll
             for (int i = 0; i < MINE / 2; ++i) sum[i] = 0;
-            for (int kc = 0; kc < a.kb && ok; ++kc) {
-                const int u = kc & 3;
-                if (u == 0) {
-                    ok = blocks_wait<true>(smem_u32(&ctl->scale_full[slot]), phase, ctl);
-                    scales = lds_floats(my_rows + slot * (kRowScales * 4));
-                    if (!EACH) {
-                        const float4 b = lds_floats(my_cols + slot * (kCols * 4));
-                        scales = make_float4(scales.x * b.x, scales.y * b.y, scales.z * b.z, scales.w * b.w);
-                    }
-                }
-                const uint32_t s1 = __float_as_uint(u == 0 ? scales.x : u == 1 ? scales.y : u == 2 ? scales.z : scales.w);
-                const uint64_t s = pair_of(s1, s1);
-                ok = ok && blocks_wait<true>(tmem_full0 + 8u * acc, acc_ph, ctl);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t from = from0 + acc * (uint32_t)BN;
+            for (int k0 = 0; k0 < a.kb; k0 += 4) {
+                blocks_wait_warp(scale_full0 + 8u * slot, phase, ctl, dead);
+                const float4 r = lds_floats(my_rows + slot * (kRowScales * 4)), b = EACH ? make_float4(1.f, 1.f, 1.f, 1.f) : lds_floats(my_cols + slot * (kCols * 4));
+                float s0 = r.x * b.x, s1 = r.y * b.y, s2 = r.z * b.z;
+                const float s3 = r.w * b.w;
+                uint32_t cols = my_cols + slot * (kCols * 4);
+                const int here = min(4, a.kb - k0);
+#pragma unroll 1
+                for (int u = 0; u < here; ++u, cols += 1024) {
+                    const uint64_t s = pair_of(__float_as_uint(s0), __float_as_uint(s0));
+                    s0 = s1; s1 = s2; s2 = s3;
+                    blocks_wait_warp(tmem_full0 + 8u * acc, acc_ph, ctl, dead);
+                    tc_fence_after();
+                    const uint32_t from = from0 + acc * (uint32_t)BN;
 #pragma unroll
-                for (int c = 0; c < MINE; c += 16) {
-                    uint32_t v[16];
-                    tmem_ld16(from + c, v);
-                    tmem_ld_wait16(v);
-                    if (c + 16 == MINE) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
-                            else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
+                    for (int c = 0; c < MINE; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld16(from + c, v);
+                        tmem_ld_wait16(v);
+                        if (c + 16 == MINE) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (PAIR) arrive_first_remote(lead_empty + 8u * acc, lane);
+                            else arrive_first(tmem_empty0 + 8u * acc, lane);
                         }
-                        if (++acc == ACCS) { acc = 0; acc_ph ^= 1u; }
-                    }
 #pragma unroll
-                    for (int i = 0; i < 8; i += 2) {
-                        uint64_t t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
-                        if (EACH) {
-                            uint64_t b[2];
-                            lds_pairs(my_cols + slot * (kCols * 4) + (uint32_t)(u * 256 + c + 2 * i) * 4, b);
-                            t[0] = product(t[0], b[0]);
-                            t[1] = product(t[1], b[1]);
+                        for (int i = 0; i < 8; i += 2) {
+                            uint64_t t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
+                            if (EACH) {
+                                uint64_t w[2];
+                                lds_pairs(cols + (uint32_t)(c + 2 * i) * 4, w);
+                                t[0] = product(t[0], w[0]);
+                                t[1] = product(t[1], w[1]);
+                            }
+                            add_product(sum[c / 2 + i], t[0], s);
+                            add_product(sum[c / 2 + i + 1], t[1], s);
                         }
-                        add_product(sum[c / 2 + i], t[0], s);
-                        add_product(sum[c / 2 + i + 1], t[1], s);
                     }
+                    acc = (acc + 1u) & (ACCS - 1u);
+                    acc_ph ^= acc == 0u;
                 }
-                if (u == 3 || kc + 1 == a.kb) {
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_relaxed(&ctl->scale_empty[slot]);       // (the scales have long been read: sums were made of them)
-                    if (++slot == kScaleSlots) { slot = 0; phase ^= 1u; }
-                }
+                __syncwarp();
+                arrive_first(scale_empty0 + 8u * slot, lane);               // (the scales have been read: sums were made of them)
+                slot = slot + 1u == kScaleSlots ? 0u : slot + 1u;
+                phase ^= slot == 0u;
             }
-            if (!ok)                                          // a wait ran out: what is stored says so
+            if (dead)                                         // a wait ran out: what is stored says so
 #pragma unroll
                 for (int i = 0; i < MINE / 2; ++i) sum[i] = 0x7fffffff7fffffffull;
             constexpr int PER = 64 / (int)sizeof(T);          // columns of a box
@@ -745,7 +766,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
             bool ok = true;
             for (int it = 0; it < nk; ++it) {
                 if (it >= a.stages) {
-                    ok = blocks_wait<false>(empty0 + r.off, r.phase ^ 1u, ctl);
+                    ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
                     if (!ok) break;
                     load_weights(it, r.off, r.data);
                 }
@@ -765,7 +786,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
             r.start(r0, (uint32_t)a.stages);
             uint32_t acc = 0, acc_ph = 1;
             for (int it = 0; it < nk; ++it) {
-                if (!blocks_wait<false>(full0 + r.off, r.phase, ctl) || !blocks_wait<false>(smem_u32(&ctl->tmem_empty[acc]), acc_ph, ctl)) break;
+                if (!blocks_wait(full0 + r.off, r.phase, ctl) || !blocks_wait(smem_u32(&ctl->tmem_empty[acc]), acc_ph, ctl)) break;
                 tc_fence_after();
                 umma_f8(tmem_base + acc * NT, r.data, r.data + (kATile >> 4), d_hi, a.idesc, it * a.CS + rank + 1 < a.kb ? 4 : a.k_last);
                 umma_commit_at(smem_u32(&ctl->tmem_full[acc]));
@@ -793,13 +814,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
         for (int i = 0; i < NT / 2; ++i) sum[i] = 0;
         uint32_t acc = 0, acc_ph = 0;
         const uint32_t scale0 = smem_u32(scale);
-        bool ok = true;
+        uint32_t dead = 0;
         float next = EACH && nk > 0 ? weight_scale[0] : 1.f;
         for (int it = 0; it < nk; ++it) {
             const uint32_t sw = __float_as_uint(next);
             if (EACH && it + 1 < nk) next = weight_scale[(size_t)(it + 1) * a.CS];
-            ok = blocks_wait<true>(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl);
-            if (!ok) break;
+            blocks_wait_warp(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, dead);
+            if (dead) break;
             tc_fence_after();
             const uint32_t from = tmem_base + acc * NT + ((uint32_t)(q * 32) << 16);
 #pragma unroll
@@ -818,13 +839,13 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
+            arrive_first(smem_u32(&ctl->tmem_empty[acc]), lane);
             acc ^= 1u;
             acc_ph ^= acc == 0;
         }
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
         waited = true;
-        if (ok) {
+        if (!dead) {
             const uint32_t dst = map_to_cta(red + rank * (NT / 4) * rows + m - owner * rows, (uint32_t)owner);
             const int there = (int)min((int64_t)NT, p.m - (int64_t)mt * NT);
 #pragma unroll
