@@ -692,7 +692,8 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
 // cluster of CTAs, enough of them for the weights to stream at HBM's rate.  Each CTA scales and adds up its own blocks in registers; the partial sums meet in distributed shared
 // memory, where CTA r finishes channels r * 128 / CS and on, in the order of the ranks.  `early`: everything older than the kernel before is complete (dc_linear_blocks: that kernel
 // puts x into 8 bits), so the weights' loads start before the wait for it.
-constexpr int kSplitThreads = 192, kSplitStages = 12, kSplitScales = 32 * 1024;
+constexpr int kSplitStages = 12, kSplitScales = 32 * 1024;
+template <int NT> struct SplitAdders { static constexpr int N = NT < 64 ? 4 : 8; };   // warps that add up: of wide tiles two to the same 32 channels, with half of the columns each
 // A CTA of it waits for its cluster, and tensor memory is given out without a limit on the wait: it takes at least this much shared memory for each 128 columns, so that what fits beside
 // it has columns too (as the split product of integers, dc_quant.cu).
 constexpr size_t kSplitLeast = 64 * 1024;
@@ -709,10 +710,10 @@ struct BlocksSplitCtl {
 };
 
 template <int NT, bool EACH, typename T>
-__global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const BlocksSplit a)
+__global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_split(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const BlocksSplit a)
 {
     constexpr uint32_t kStageBytes = kATile + NT * kBytesK, kColumns = 2 * NT < 32 ? 32 : 2 * NT;
-    constexpr int LD = NT < 32 ? 16 : 32;
+    constexpr int LD = NT < 32 ? 16 : 32, ADDERS = SplitAdders<NT>::N, kThreads = 64 + 32 * ADDERS, MINE = NT / (ADDERS / 4);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     // [CS][NT / 4][128 / CS]: this CTA's channels, four rows' sums each, from every CTA; a warp's stores lie side by side
@@ -726,7 +727,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 2); mbar_init(&ctl->empty[i], 1); }   // weights and rows arrive apart
-        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], 4); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], ADDERS); }
         ctl->abort_flag = 0;
         ctl->wait_ns = kWaitNs;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -799,8 +800,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
         __syncwarp();
     } else {
         // ---------------- sums of this CTA's blocks, and their way to the CTA that finishes the channel ----------------
-        const int q = warp & 3, m = q * 32 + lane, owner = m / rows;
-        for (int i = threadIdx.x - 64; i < nk * NT; i += 128) {
+        const int q = warp & 3, m = q * 32 + lane, owner = m / rows, col0 = (warp - 2) / 4 * MINE;
+        for (int i = threadIdx.x - 64; i < nk * NT; i += 32 * ADDERS) {
             const int64_t row = (int64_t)mt * NT + i % NT;
             const int at = i / NT * a.CS + rank;
             float s = row < p.m ? p.a_scale[row * a.kb + at] : 0.f;
@@ -808,12 +809,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
             scale[i] = s;
         }
         const float* const weight_scale = p.b_scale + (size_t)min(nt * kTileM + m, p.n - 1) * a.kb + rank;      // EACH: of this lane's channel
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        uint64_t sum[NT / 2];
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * ADDERS) : "memory");
+        uint64_t sum[MINE / 2];
 #pragma unroll
-        for (int i = 0; i < NT / 2; ++i) sum[i] = 0;
+        for (int i = 0; i < MINE / 2; ++i) sum[i] = 0;
         uint32_t acc = 0, acc_ph = 0;
-        const uint32_t scale0 = smem_u32(scale);
+        const uint32_t scale0 = smem_u32(scale + col0);
         uint32_t dead = 0;
         float next = EACH && nk > 0 ? weight_scale[0] : 1.f;
         for (int it = 0; it < nk; ++it) {
@@ -822,9 +823,9 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
             blocks_wait_warp(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, dead);
             if (dead) break;
             tc_fence_after();
-            const uint32_t from = tmem_base + acc * NT + ((uint32_t)(q * 32) << 16);
+            const uint32_t from = tmem_base + acc * NT + col0 + ((uint32_t)(q * 32) << 16);
 #pragma unroll
-            for (int c = 0; c < NT; c += LD) {
+            for (int c = 0; c < MINE; c += LD) {
                 uint32_t v[LD];
                 if constexpr (LD == 32) { tmem_ld32(from + c, v); tmem_ld_wait32(v); }
                 else { tmem_ld16(from + c, v); tmem_ld_wait16(v); }
@@ -849,10 +850,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
             const uint32_t dst = map_to_cta(red + rank * (NT / 4) * rows + m - owner * rows, (uint32_t)owner);
             const int there = (int)min((int64_t)NT, p.m - (int64_t)mt * NT);
 #pragma unroll
-            for (int c = 0; c < NT; c += 4)
-                if (c < there) {
+            for (int c = 0; c < MINE; c += 4)
+                if (col0 + c < there) {
                     const float2 x = floats_of(sum[c / 2]), y = floats_of(sum[c / 2 + 1]);
-                    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)(c / 4 * rows * 16)), "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y) : "memory");
+                    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)((col0 + c) / 4 * rows * 16)), "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y) : "memory");
                 }
         }
     }
@@ -866,7 +867,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) k_blocks_split(const __grid_
         // ---------------- this CTA's channels: sums from all ranks, bias, ReLU, rounding, store ----------------
         const int there = (int)min((int64_t)NT, p.m - (int64_t)mt * NT);
         const float dead = ctl->abort_flag != 0 ? __uint_as_float(0x7fffffffu) : 0.f;        // what is stored says so
-        for (int t = threadIdx.x / rows * 4; t < there && j < p.n; t += kSplitThreads / rows * 4) {    // four rows of a
+        for (int t = threadIdx.x / rows * 4; t < there && j < p.n; t += kThreads / rows * 4) {    // four rows of a
             float4 sum = make_float4(dead, dead, dead, dead);
             for (int r = 0; r < a.CS; ++r) {
                 const float4 v = red[(r * (NT / 4) + t / 4) * rows + ch];
@@ -901,7 +902,7 @@ int clusters_at_once(int cs, int device)
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)cs); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = 200 * 1024; cfg.attrs = attr; cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)cs); cfg.blockDim = dim3(192); cfg.dynamicSmemBytes = 200 * 1024; cfg.attrs = attr; cfg.numAttrs = 1;
     int n = 0;
     if (cudaFuncSetAttribute(k_blocks_split<16, false, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem) != cudaSuccess ||
         cudaOccupancyMaxActiveClusters(&n, k_blocks_split<16, false, float>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
@@ -950,7 +951,7 @@ int launch_split_as(const BlocksProduct& p, const SplitPlan& s, int kb, int earl
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.m_tiles * dc_div_up(p.n, kTileM) * s.CS)); cfg.blockDim = dim3(kSplitThreads);
+    cfg.gridDim = dim3((unsigned)(a.m_tiles * dc_div_up(p.n, kTileM) * s.CS)); cfg.blockDim = dim3(64 + 32 * SplitAdders<NT>::N);
     const size_t smem = (size_t)a.stages * stage + fixed, least = kSplitLeast * (NT > 64 ? 2 : 1);
     cfg.dynamicSmemBytes = smem > least ? smem : least; cfg.stream = stream;
     cfg.attrs = attr; cfg.numAttrs = g_dc_pdl ? 2 : 1;
@@ -998,12 +999,14 @@ int launch_product(const BlocksProduct& p, int dtype, bool early, int device, in
     bool pair = false;
     int BN = 64;
     double best = 0.0;
+    // The tile that takes the fewest cycles, as counted from measurements: a block of K takes so many (what bounds it is its way from the MMAs to the sums and back), an SM's share of out leaves
+    // at about 24 bytes a cycle where others pause, and an item costs 500 to begin and end.
+    static constexpr double kStep[4][2] = {{1040.0, 1690.0}, {635.0, 800.0}, {635.0, 780.0}, {480.0, 540.0}};     // scales for 128 rows of b, for each
     for (int c = 0; c < 4; ++c) {
         const bool two = c < 2;
         const int bn = c == 0 ? 256 : c == 3 ? 64 : 128;
         const long long n_items = (two ? (a.m_tiles + 1) / 2 : a.m_tiles) * (long long)dc_div_up(p.n, bn), at_once = two ? num_sms / 2 : num_sms, rounds = (n_items + at_once - 1) / at_once;
-        const double load = a.kb * (double)(kATile + (two ? bn / 2 : bn) * kBytesK) / 50.0, mma = a.kb * (500.0 + 2.0 * bn), out = 128.0 * bn * elt / 24.0;
-        const double cost = rounds * ((load > mma ? load : mma) + out + 500.0);
+        const double cost = rounds * (a.kb * kStep[c][p.b_block_rows == 1] + 128.0 * bn * elt / 24.0 + 500.0);
         if (c == 0 || cost < best) { best = cost; pair = two; BN = bn; }
     }
     if (p.n <= (1 << 20) && p.m <= (1 << 20)) {

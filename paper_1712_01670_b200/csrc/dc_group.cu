@@ -493,6 +493,7 @@ __device__ __forceinline__ void seat(const GroupArgs& a, int& col, int& turn, in
 __device__ __forceinline__ float rows_of_sums(const float* part, int left, int wide, int i)
 {
     float t = 0.f;
+#pragma unroll 8
     for (int k = 0; k < left; ++k) t += part[k * wide + i];
     return t;
 }
