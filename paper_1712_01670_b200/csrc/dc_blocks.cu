@@ -90,16 +90,22 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, uint4 w, int there)     
     if (there > 0) store_bytes(p, make_uint2(w.x, w.y), there);
     if (there > 8) store_bytes(p + 8, make_uint2(w.z, w.w), there - 8);
 }
-// Eight columns of a row, `there` of which exist.  WIDE: rows are aligned to 16 bytes.
+// Eight columns of a row, `there` of which exist.  WIDE: rows are aligned to 16 bytes and of whole eights, so all of them or none.
 template <bool WIDE, typename T>
 __device__ __forceinline__ void load_eight(Eight<T>& v, const char* x, int there)
 {
     v.zero();
-    if (WIDE && there >= 8) v.load(x);
+    if (WIDE) { if (there > 0) v.load(x); }
     else
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (k < there) v.put(k, ((const T*)x)[k]);
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_eight(uint8_t* q, uint2 w, int there)
+{
+    if (WIDE) { if (there > 0) *(uint2*)q = w; }
+    else if (there > 0) store_bytes(q, w, there);
 }
 template <typename T>
 __device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale& s)
@@ -108,8 +114,9 @@ __device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale&
     v.open(f);
     uint32_t w[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = s.bad ? 0u : two_e4m3(mul2(f[k], both<float2>(s.inv)));
-    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    for (int k = 0; k < 4; ++k) w[k] = two_e4m3(mul2(f[k], both<float2>(s.inv)));
+    const uint32_t kept = s.bad ? 0u : 0xffffffffu;
+    return make_uint2(__byte_perm(w[0], w[1], 0x5410) & kept, __byte_perm(w[2], w[3], 0x5410) & kept);
 }
 
 // Rows alone: sixteen lanes to a block, four blocks of a lane in flight.  by_kb: see divided().
@@ -138,7 +145,7 @@ __global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a,
         if (first + 16u * u >= items) continue;
         const BlockScale s = block_scale(m);
         const int col = (int)block[u] * 128 + part * 8;
-        if (col < a.channels) store_bytes(a.q + (size_t)row[u] * a.q_pitch + col, eight_e4m3(v[u], s), a.channels - col);
+        store_eight<WIDE>(a.q + (size_t)row[u] * a.q_pitch + col, eight_e4m3(v[u], s), a.channels - col);
         if (part == 0) a.scale[(size_t)row[u] * a.kb + block[u]] = s.scale;
     }
 }
@@ -178,7 +185,7 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
             else if (a.q) {
                 const BlockScale s = block_scale(__reduce_max_sync(0xffffu << (lane & 16), m));
                 if (row < a.rows) {
-                    if (there > 0) store_bytes(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v[i], s), there);
+                    store_eight<WIDE>(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v[i], s), there);
                     if (part == 0) a.scale[(size_t)row * a.kb + tile_c] = s.scale;
                 }
             }
@@ -201,13 +208,14 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
                 if (row >= a.rows) break;
                 Eight<T> v;
                 v.load((const char*)(tile4 + (r * 16 + part) * (sizeof(T) / 2)));
-                store_bytes(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v, s), there);
+                store_eight<WIDE>(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v, s), there);
             }
     } else __syncthreads();
     if (!a.qt) return;
     const int c = threadIdx.x % (128 / PER) * PER, turn = threadIdx.x / (128 / PER), row0 = tile_r * 128 + turn * ROWS;
     const uint32_t* const word = (const uint32_t*)((const char*)tile4 + ((size_t)turn * ROWS * 128 + c) * sizeof(T));
     constexpr int LINE = 128 / PER;                           // words of a row
+    const bool whole = tile_r * 128 + 128 <= a.rows && tile_c * 128 + 128 <= a.channels;
     BlockScale t[PER];
     if (WHOLE)
 #pragma unroll
@@ -241,13 +249,14 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(PER == 2 ? (k ? w[i] & 0xffff0000u : w[i] << 16) : w[i]);
                 const float2 inv = both<float2>(t[k].inv);
-                out[k][q] = t[k].bad ? 0u : two_e4m3(mul2(make_float2(f[0], f[1]), inv)) | two_e4m3(mul2(make_float2(f[2], f[3]), inv)) << 16;
+                out[k][q] = __byte_perm(two_e4m3(mul2(make_float2(f[0], f[1]), inv)), two_e4m3(mul2(make_float2(f[2], f[3]), inv)), 0x5410) & (t[k].bad ? 0u : 0xffffffffu);
             }
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k)
-            if (tile_c * 128 + c + k < a.channels)
-                store_bytes(a.qt + (size_t)(tile_c * 128 + c + k) * a.qt_pitch + row0 + g, make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]), a.rows - row0 - g);
+            if (whole || tile_c * 128 + c + k < a.channels)
+                if (whole) *(uint4*)(a.qt + (size_t)(tile_c * 128 + c + k) * a.qt_pitch + row0 + g) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
+                else store_bytes(a.qt + (size_t)(tile_c * 128 + c + k) * a.qt_pitch + row0 + g, make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]), a.rows - row0 - g);
     }
 }
 
@@ -1071,7 +1080,7 @@ int launch_quantize(const BlocksArgs& a, int device, cudaStream_t stream)
 int quantize(BlocksArgs& a, int dtype, int device, cudaStream_t stream)
 {
     a.kb = dc_div_up(a.channels, 128); a.rb = (int)(((int64_t)a.rows + 127) / 128);
-    const bool wide = (uintptr_t)a.x % 16 == 0 && (a.rows < 2 || a.x_pitch % 16 == 0);
+    const bool wide = (uintptr_t)a.x % 16 == 0 && (a.rows < 2 || a.x_pitch % 16 == 0) && a.channels % 8 == 0;
     if (dtype == DC_BF16) return wide ? launch_quantize<__nv_bfloat16, true>(a, device, stream) : launch_quantize<__nv_bfloat16, false>(a, device, stream);
     return wide ? launch_quantize<float, true>(a, device, stream) : launch_quantize<float, false>(a, device, stream);
 }
