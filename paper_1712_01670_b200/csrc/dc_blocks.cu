@@ -119,7 +119,7 @@ __device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale&
     return make_uint2(__byte_perm(w[0], w[1], 0x5410) & kept, __byte_perm(w[2], w[3], 0x5410) & kept);
 }
 
-// Rows alone: sixteen lanes to a block, four blocks of a lane in flight.  by_kb: see divided().
+// Rows alone: sixteen lanes to a block of each of four rows, all four in flight.  by_kb: see divided().
 __device__ __forceinline__ uint32_t divided(uint32_t n, uint2 by) { return by.x ? __umulhi(n, by.x) >> by.y : n; }
 
 template <typename T, bool WIDE>
@@ -128,36 +128,34 @@ __global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a,
     const int part = threadIdx.x & 15, lane = threadIdx.x & 31;
     dc_pdl_wait();
     dc_pdl_release();
-    const uint32_t first = blockIdx.x * 64u + (threadIdx.x >> 4);
+    const uint32_t item = blockIdx.x * 16u + (threadIdx.x >> 4), fours = divided(item, by_kb), block = item - fours * (uint32_t)a.kb;
+    const int row0 = (int)fours * 4, rows = item < items ? min(4, a.rows - row0) : 0, col = (int)block * 128 + part * 8, there = a.channels - col;
+    const char* x = (const char*)a.x + (size_t)row0 * a.x_pitch + (size_t)col * sizeof(T);
     Eight<T> v[4];
-    uint32_t row[4], block[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const uint32_t item = first + 16u * u;
-        row[u] = divided(item, by_kb);
-        block[u] = item - row[u] * (uint32_t)a.kb;
-        const int col = (int)block[u] * 128 + part * 8;
-        load_eight<WIDE>(v[u], (const char*)a.x + (size_t)row[u] * a.x_pitch + (size_t)col * sizeof(T), item < items ? a.channels - col : 0);
-    }
+    for (int u = 0; u < 4; ++u, x += a.x_pitch) load_eight<WIDE>(v[u], x, u < rows ? there : 0);
+    BlockScale s[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const uint32_t m = __reduce_max_sync(0xffffu << (lane & 16), v[u].most());
-        if (first + 16u * u >= items) continue;
-        const BlockScale s = block_scale(m);
-        const int col = (int)block[u] * 128 + part * 8;
-        store_eight<WIDE>(a.q + (size_t)row[u] * a.q_pitch + col, eight_e4m3(v[u], s), a.channels - col);
-        if (part == 0) a.scale[(size_t)row[u] * a.kb + block[u]] = s.scale;
+    for (int u = 0; u < 4; ++u) s[u] = block_scale(__reduce_max_sync(0xffffu << (lane & 16), v[u].most()));
+    uint8_t* q = a.q + (size_t)row0 * a.q_pitch + col;
+    if (there > 0)
+#pragma unroll
+        for (int u = 0; u < 4; ++u, q += a.q_pitch)
+            if (u < rows) store_eight<WIDE>(q, eight_e4m3(v[u], s[u]), there);
+    if (part < rows) {                                        // a lane to each row's scale
+        const float t = part == 0 ? s[0].scale : part == 1 ? s[1].scale : part == 2 ? s[2].scale : s[3].scale;
+        a.scale[(size_t)(row0 + part) * a.kb + block] = t;
     }
 }
 
 // Turned, or with a scale for 128 x 128 values: a CTA has such a tile, read once.  A thread has eight columns of eight rows, which it puts into 8 bits on their way to shared memory;
-// and then a column (bfloat16: two) of 64 (32) rows, which it reads from there twice, for the largest value and for the values.  WHOLE: one scale for the tile.
+// and then a column (bfloat16: two) of 64 (32) rows, which it reads from there.  WHOLE: one scale for the tile.
 template <typename T, bool WIDE, bool WHOLE>
 __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
 {
     constexpr int PER = 4 / (int)sizeof(T), TEAMS = 2 * PER, ROWS = 128 / TEAMS;       // columns of a thread, threads to a column, rows of each
     extern __shared__ uint4 tile4[];                          // [128][128] of the map's type
-    __shared__ uint32_t most_of[TEAMS][128];
+    __shared__ alignas(8) uint32_t most_of[TEAMS][128];
     __shared__ uint32_t most_of_tile;
     const int tile_c = blockIdx.x % a.kb, tile_r = blockIdx.x / a.kb, lane = threadIdx.x & 31;
     const int part = threadIdx.x & 15, team = threadIdx.x >> 4, col = tile_c * 128 + part * 8, there = a.channels - col;
@@ -213,18 +211,24 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
     } else __syncthreads();
     if (!a.qt) return;
     const int c = threadIdx.x % (128 / PER) * PER, turn = threadIdx.x / (128 / PER), row0 = tile_r * 128 + turn * ROWS;
-    const uint32_t* const word = (const uint32_t*)((const char*)tile4 + ((size_t)turn * ROWS * 128 + c) * sizeof(T));
     constexpr int LINE = 128 / PER;                           // words of a row
+    const uint32_t* const word = (const uint32_t*)((const char*)tile4 + ((size_t)turn * ROWS * 128 + c) * sizeof(T));
     const bool whole = tile_r * 128 + 128 <= a.rows && tile_c * 128 + 128 <= a.channels;
+    uint32_t w[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) w[r] = word[r * LINE];
     BlockScale t[PER];
     if (WHOLE)
 #pragma unroll
         for (int k = 0; k < PER; ++k) t[k] = s;
     else {
-        uint32_t m = 0;
-#pragma unroll 8
-        for (int r = 0; r < ROWS; ++r) m = PER == 2 ? larger2(m, word[r * LINE]) & 0x7fff7fffu : max(m, word[r * LINE] & 0x7fffffffu);
-        if (PER == 2) { most_of[turn][c] = m << 16; most_of[turn][c + 1] = m & 0xffff0000u; } else most_of[turn][c] = m;
+        uint32_t m[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) m[r & 3] = PER == 2 ? larger2(m[r & 3], w[r]) : max(m[r & 3], w[r] & 0x7fffffffu);
+        if (PER == 2) {
+            const uint32_t all = larger2(larger2(m[0], m[1]), larger2(m[2], m[3])) & 0x7fff7fffu;
+            *(uint2*)&most_of[turn][c] = make_uint2(all << 16, all & 0xffff0000u);
+        } else most_of[turn][c] = max(max(m[0], m[1]), max(m[2], m[3]));
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
@@ -236,27 +240,24 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
         }
     }
 #pragma unroll
-    for (int g = 0; g < ROWS; g += 16) {                      // sixteen rows: 16 bytes of a column
-        uint32_t out[PER][4];
+    for (int k = 0; k < PER; ++k) {
+        const float2 inv = both<float2>(t[k].inv);
+        const uint32_t kept = t[k].bad ? 0u : 0xffffffffu;
+        const int column = tile_c * 128 + c + k;
+        uint8_t* const out = a.qt + (size_t)column * a.qt_pitch + row0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint32_t w[4];
+        for (int g = 0; g < ROWS; g += 16) {                  // sixteen rows: 16 bytes of a column
+            uint32_t o[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = word[(g + 4 * q + i) * LINE];
-#pragma unroll
-            for (int k = 0; k < PER; ++k) {
+            for (int q = 0; q < 4; ++q) {
                 float f[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(PER == 2 ? (k ? w[i] & 0xffff0000u : w[i] << 16) : w[i]);
-                const float2 inv = both<float2>(t[k].inv);
-                out[k][q] = __byte_perm(two_e4m3(mul2(make_float2(f[0], f[1]), inv)), two_e4m3(mul2(make_float2(f[2], f[3]), inv)), 0x5410) & (t[k].bad ? 0u : 0xffffffffu);
+                for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(PER == 2 ? (k ? w[g + 4 * q + i] & 0xffff0000u : w[g + 4 * q + i] << 16) : w[g + 4 * q + i]);
+                o[q] = __byte_perm(two_e4m3(mul2(make_float2(f[0], f[1]), inv)), two_e4m3(mul2(make_float2(f[2], f[3]), inv)), 0x5410) & kept;
             }
+            if (whole) *(uint4*)(out + g) = make_uint4(o[0], o[1], o[2], o[3]);
+            else if (column < a.channels) store_bytes(out + g, make_uint4(o[0], o[1], o[2], o[3]), a.rows - row0 - g);
         }
-#pragma unroll
-        for (int k = 0; k < PER; ++k)
-            if (whole || tile_c * 128 + c + k < a.channels)
-                if (whole) *(uint4*)(a.qt + (size_t)(tile_c * 128 + c + k) * a.qt_pitch + row0 + g) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
-                else store_bytes(a.qt + (size_t)(tile_c * 128 + c + k) * a.qt_pitch + row0 + g, make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]), a.rows - row0 - g);
     }
 }
 
@@ -1055,7 +1056,7 @@ template <typename T, bool WIDE>
 int launch_quantize(const BlocksArgs& a, int device, cudaStream_t stream)
 {
     if (!a.qt && a.block_rows == 1) {
-        const int64_t items = (int64_t)a.rows * a.kb;
+        const int64_t items = ((int64_t)a.rows + 3) / 4 * a.kb;
         if (items < 0x7fffffff) {
             // n / kb = n * by.x >> (32 + by.y) for n < 2^31, by.x the next whole number above 2^(32 + by.y) / kb, 2^by.y < kb
             uint2 by = make_uint2(0, 0);
@@ -1063,7 +1064,7 @@ int launch_quantize(const BlocksArgs& a, int device, cudaStream_t stream)
                 while ((2 << by.y) < a.kb) ++by.y;
                 by.x = (uint32_t)((((uint64_t)1 << (32 + by.y)) + a.kb - 1) / a.kb);
             }
-            DC_CUDA(dc_launch_pdl(k_quantize_row_blocks<T, WIDE>, dim3((unsigned)((items + 63) / 64)), 256, 0, stream, a, by, (uint32_t)items));
+            DC_CUDA(dc_launch_pdl(k_quantize_row_blocks<T, WIDE>, dim3((unsigned)((items + 15) / 16)), 256, 0, stream, a, by, (uint32_t)items));
             return DC_OK;
         }
     }
