@@ -123,11 +123,9 @@ __device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale&
 __device__ __forceinline__ uint32_t divided(uint32_t n, uint2 by) { return by.x ? __umulhi(n, by.x) >> by.y : n; }
 
 template <typename T, bool WIDE>
-__global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a, uint2 by_kb, uint32_t items)
+__device__ __forceinline__ void row_blocks(const BlocksArgs& a, uint2 by_kb, uint32_t items)
 {
     const int part = threadIdx.x & 15, lane = threadIdx.x & 31;
-    dc_pdl_wait();
-    dc_pdl_release();
     const uint32_t item = blockIdx.x * 16u + (threadIdx.x >> 4), fours = divided(item, by_kb), block = item - fours * (uint32_t)a.kb;
     const int row0 = (int)fours * 4, rows = item < items ? min(4, a.rows - row0) : 0, col = (int)block * 128 + part * 8, there = a.channels - col;
     const char* x = (const char*)a.x + (size_t)row0 * a.x_pitch + (size_t)col * sizeof(T);
@@ -145,6 +143,74 @@ __global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a,
     if (part < rows) {                                        // a lane to each row's scale
         const float t = part == 0 ? s[0].scale : part == 1 ? s[1].scale : part == 2 ? s[2].scale : s[3].scale;
         a.scale[(size_t)(row0 + part) * a.kb + block] = t;
+    }
+}
+
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a, uint2 by_kb, uint32_t items)
+{
+    dc_pdl_wait();
+    dc_pdl_release();
+    row_blocks<T, WIDE>(a, by_kb, items);
+}
+
+// Turned, of few tiles: 128 rows x 32 columns to a CTA, four times as many as whole tiles; the rows, if they are wanted too, are put into 8 bits by the first row_ctas CTAs, which read x once
+// more.  Both ways, us, so and as whole tiles: 196 x 1024 bf16 2.0 and 4.5, 1000 x 333 f32 3.1 and 6.6, 40000 x 96 bf16 8.3 and 9.7, 6000 x 1001 14.7 and 15.2, 12544 x 512 f32 13.3 and 13.5,
+// 25088 x 512 bf16 22.0 and 16.8.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(256) k_quantize_columns(const BlocksArgs a, uint2 by_kb, uint32_t items, int row_ctas)
+{
+    constexpr int PER = 4 / (int)sizeof(T), TEAMS = 256 * PER / 32, ROWS = 128 / TEAMS, LINE = 32 / PER;       // columns of a thread, threads to a column, rows of each, words of a row
+    __shared__ uint4 tile4[128 * 32 * sizeof(T) / 16];
+    __shared__ alignas(8) uint32_t most_of[TEAMS][32];
+    dc_pdl_wait();
+    dc_pdl_release();
+    if ((int)blockIdx.x < row_ctas) { row_blocks<T, WIDE>(a, by_kb, items); return; }
+    const int quarters = (a.channels + 31) / 32, tile = (int)blockIdx.x - row_ctas, tile_r = tile / quarters, col0 = (tile - tile_r * quarters) * 32;
+    {
+        const int part = threadIdx.x & 3, col = col0 + part * 8, there = a.channels - col;
+        Eight<T> v[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = tile_r * 128 + i * 64 + (threadIdx.x >> 2);
+            load_eight<WIDE>(v[i], (const char*)a.x + (size_t)row * a.x_pitch + (size_t)col * sizeof(T), row < a.rows ? there : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i].keep(tile4 + ((i * 64 + (threadIdx.x >> 2)) * 4 + part) * (sizeof(T) / 2));
+    }
+    __syncthreads();
+    const int c = threadIdx.x % LINE * PER, turn = threadIdx.x / LINE, row0 = tile_r * 128 + turn * ROWS;
+    const uint32_t* const word = (const uint32_t*)tile4 + turn * ROWS * LINE + threadIdx.x % LINE;
+    uint32_t w[ROWS], m = 0;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) w[r] = word[r * LINE];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) m = PER == 2 ? larger2(m, w[r]) : max(m, w[r] & 0x7fffffffu);
+    if (PER == 2) { m &= 0x7fff7fffu; *(uint2*)&most_of[turn][c] = make_uint2(m << 16, m & 0xffff0000u); }
+    else most_of[turn][c] = m;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        uint32_t all = 0;
+#pragma unroll
+        for (int i = 0; i < TEAMS; ++i) all = max(all, most_of[i][c + k]);
+        const BlockScale t = block_scale(all);
+        const int column = col0 + c + k;
+        if (column >= a.channels) break;
+        if (turn == 0) a.scale_t[(size_t)column * a.rb + tile_r] = t.scale;
+        const uint32_t kept = t.bad ? 0u : 0xffffffffu;
+        uint32_t o[ROWS / 4];
+#pragma unroll
+        for (int q = 0; q < ROWS / 4; ++q) {
+            float f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(PER == 2 ? (k ? w[4 * q + i] & 0xffff0000u : w[4 * q + i] << 16) : w[4 * q + i]);
+            o[q] = __byte_perm(two_e4m3(mul2(make_float2(f[0], f[1]), both<float2>(t.inv))), two_e4m3(mul2(make_float2(f[2], f[3]), both<float2>(t.inv))), 0x5410) & kept;
+        }
+        uint8_t* const out = a.qt + (size_t)column * a.qt_pitch + row0;
+        if (row0 >= a.rows) break;
+        if constexpr (ROWS == 16) store_bytes(out, make_uint4(o[0], o[1], o[2], o[3]), a.rows - row0);
+        else store_bytes(out, make_uint2(o[0], o[1]), a.rows - row0);
     }
 }
 
@@ -279,7 +345,7 @@ struct BlocksTiles {
     int wide, boxes;                                          // out takes 16-byte stores; is written in boxes by TMA
 };
 
-constexpr int kAddWarps = 16, kFirstAdder = 3, kBlocksThreads = (kFirstAdder + kAddWarps) * 32;
+constexpr int kAddWarps = 16, kFirstAdder = 4, kBlocksThreads = (kFirstAdder + kAddWarps) * 32;
 constexpr int kBlocksMostStages = 8, kScaleSlots = 3;         // a slot: the scales of four blocks of K
 constexpr int kBox = 32 * 64;                                 // a warp's 32 rows on their way out, 64 bytes each; two of them
 struct BlocksCtl {
@@ -384,26 +450,16 @@ __device__ __forceinline__ void copy_floats(uint32_t dst, const float* src, cons
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(there ? src : any), "r"(there ? 4 * N : 0), "n"(4 * N) : "memory");
 }
-// The wait for a load of 32 columns, which names them: nothing that reads them comes before it.
-__device__ __forceinline__ void tmem_ld_wait32(uint32_t* r)
+// Columns of tensor memory, loaded and waited for in one statement: nothing that reads them comes before they are there.
+__device__ __forceinline__ void tmem_read16(uint32_t taddr, uint32_t* r)
 {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
-                   "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]),
-                   "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]) :: "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
 }
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r)
+__device__ __forceinline__ void tmem_read32(uint32_t taddr, uint32_t* r)
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait16(uint32_t* r)
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
-                   "+r"(r[14]), "+r"(r[15]) :: "memory");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(taddr) : "memory");
 }
 
 // BN: columns of a tile.  EACH: b has a scale for each row and block, not for 128 rows.
@@ -421,11 +477,13 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
     constexpr int M = PAIR ? 2 : 1, PARTS = BN < 128 ? 2 : 4; // row tiles of an item; warps that share a row's columns
-    constexpr uint32_t ACCS = BN > 128 ? 2 : 4, kColumns = ACCS * BN;         // accumulators
+    // Tiles of 256 columns are two halves with accumulators, barriers and an issuer of their own.
+    constexpr int HALVES = BN > 128 ? 2 : 1, BH = BN / HALVES;
+    constexpr uint32_t ACCS = HALVES == 2 ? 2 : 4, kColumns = 4 * BH;         // accumulators of a half
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], 1); }
-        for (int i = 0; i < (int)ACCS; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], 4 * PARTS * M); }
+        for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 1); mbar_init(&ctl->empty[i], HALVES); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], 4 * PARTS / HALVES * M); }
         for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 32); mbar_init(&ctl->scale_empty[i], 4 * PARTS); }
         ctl->abort_flag = 0;
         ctl->wait_ns = kWaitNs;
@@ -467,7 +525,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 r.start(ring0, (uint32_t)a.stages);
                 bool ok = true, there;
                 for (int item = first; item < n_items && ok; item += step) {
-                    const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * BN + rank * (BN / 2);
+                    const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * BN + rank * (BH / 2);
                     for (int kc = 0; kc < a.kb; ++kc) {
                         ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
                         if (!ok) break;
@@ -475,6 +533,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                             if (rank == 0) mbar_expect_tx(full0 + r.off, 2u * (uint32_t)a.stage_bytes);
                             load_pair(r.data, &tmA, kc * kBytesK, row, lead_full + r.off);
                             load_pair(r.data + kATile, &tmB, kc * kBytesK, col, lead_full + r.off);
+                            if (HALVES == 2) load_pair(r.data + kATile + BH / 2 * kBytesK, &tmB, kc * kBytesK, col + BH, lead_full + r.off);
                         } else {
                             mbar_expect_tx(full0 + r.off, (uint32_t)a.stage_bytes);
                             tma_load_2d(r.data, &tmA, kc * kBytesK, row, full0 + r.off);
@@ -487,15 +546,18 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
             }
             __syncwarp();
-        } else if (warp == 1) {
-            // ---------------- MMA issuer (of a pair: the leader's, for both CTAs) ----------------
+        } else if (warp <= HALVES) {
+            // ---------------- MMA issuers (of a pair: the leader's, for both CTAs) ----------------
+            // What bounds a block of K is its round: MMAs, their completion's way to the adders, the reads, the release's way back, the issue.  Halves with rounds of their own take as many columns at
+            // once as one issuer's, but their MMAs half as long: 8192 x 4096 x 4096 121 to 125 us, 127 as one; 25088 x 512 x 2048 40.4 and 43.
             if (rank == 0 && elect_one()) {
                 const uint64_t dconst = umma_desc(0, 1024, 2);
                 const uint32_t d_hi = (uint32_t)(dconst >> 32), r0 = (uint32_t)dconst + (ring0 >> 4), slot = (uint32_t)a.stage_bytes >> 4;
-                const uint32_t tmem_empty0 = smem_u32(&ctl->tmem_empty[0]), tmem_full0 = smem_u32(&ctl->tmem_full[0]);
+                const uint32_t tmem_empty0 = smem_u32(&ctl->tmem_empty[0]) + 16u * ((uint32_t)warp - 1u), tmem_full0 = smem_u32(&ctl->tmem_full[0]) + 16u * ((uint32_t)warp - 1u);
                 RingPos r;
                 r.start(r0, (uint32_t)a.stages);
                 uint32_t acc = 0, acc_ph = 1;
+                const uint32_t half = (uint32_t)warp - 1u, b_at = (kATile + half * (uint32_t)(BH / 2 * kBytesK)) >> 4;
                 bool ok = true;
                 for (int item = first; item < n_items && ok; item += step)
                     for (int kc = 0; kc < a.kb; ++kc) {
@@ -503,9 +565,9 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                         if (!ok) break;
                         tc_fence_after();
                         const int n = kc + 1 < a.kb ? 4 : a.k_last;
-                        const uint32_t d = tmem_base + acc * (uint32_t)BN;
+                        const uint32_t d = tmem_base + (half * ACCS + acc) * (uint32_t)BH;
                         if (PAIR) {
-                            umma_f8_pair(d, r.data, r.data + (kATile >> 4), d_hi, a.idesc, n);
+                            umma_f8_pair(d, r.data, r.data + b_at, d_hi, a.idesc, n);
                             commit_pair(tmem_full0 + 8u * acc);
                             commit_pair(empty0 + r.off);
                         } else {
@@ -518,7 +580,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                     }
             }
             __syncwarp();
-        } else {
+        } else if (warp == 3) {
             // ---------------- scales ----------------
             // Copied four blocks at a time, straight into shared memory, several slots ahead.  A row's scales lie side by side: 16 bytes to a copy where they are
             // aligned.  A lane has four rows, and of EACH's columns eight at most.
@@ -567,11 +629,12 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
         const int q = warp & 3, part = (warp - kFirstAdder) >> 2;
         uint32_t stage = smem_u32(staging) + (uint32_t)(warp - kFirstAdder) * kBox;
         const uint32_t both_places = a.bufs == 2 ? stage ^ (stage + kAddWarps * kBox) : 0;       // from one place to the other
-        const uint32_t lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) : 0;
+        const uint32_t half = HALVES == 2 ? part / 2 : 0, lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) + 16u * half : 0;
         const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + lane) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? part * MINE : BN > 128 ? part / 2 * 4 : 0) * 4;
         uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0, dead = 0;
         bool there;
-        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]), tmem_empty0 = smem_u32(&ctl->tmem_empty[0]), from0 = tmem_base + (uint32_t)(part * MINE) + ((uint32_t)(q * 32) << 16);
+        const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]) + 16u * half, tmem_empty0 = smem_u32(&ctl->tmem_empty[0]);
+        const uint32_t from0 = tmem_base + half * ACCS * (uint32_t)BH + (uint32_t)(part * MINE) % (uint32_t)BH + ((uint32_t)(q * 32) << 16);
         const uint32_t scale_full0 = smem_u32(&ctl->scale_full[0]), scale_empty0 = smem_u32(&ctl->scale_empty[0]);
         for (int item = first; item < n_items; item += step) {
             const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN + part * MINE;
@@ -593,12 +656,11 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                     s0 = s1; s1 = s2; s2 = s3;
                     blocks_wait_warp(tmem_full0 + 8u * acc, acc_ph, ctl, dead);
                     tc_fence_after();
-                    const uint32_t from = from0 + acc * (uint32_t)BN;
+                    const uint32_t from = from0 + acc * (uint32_t)BH;
 #pragma unroll
                     for (int c = 0; c < MINE; c += 16) {
                         uint32_t v[16];
-                        tmem_ld16(from + c, v);
-                        tmem_ld_wait16(v);
+                        tmem_read16(from + c, v);
                         if (c + 16 == MINE) {
                             tc_fence_before();
                             __syncwarp();
@@ -837,8 +899,8 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
 #pragma unroll
             for (int c = 0; c < MINE; c += LD) {
                 uint32_t v[LD];
-                if constexpr (LD == 32) { tmem_ld32(from + c, v); tmem_ld_wait32(v); }
-                else { tmem_ld16(from + c, v); tmem_ld_wait16(v); }
+                if constexpr (LD == 32) tmem_read32(from + c, v);
+                else tmem_read16(from + c, v);
 #pragma unroll
                 for (int i = 0; i < LD / 2; i += 2) {
                     uint64_t s[2], t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
@@ -1034,10 +1096,10 @@ int launch_product(const BlocksProduct& p, int dtype, bool early, int device, in
     if (a.stages > kBlocksMostStages) a.stages = kBlocksMostStages;
     a.k_last = dc_div_up(p.k - (a.kb - 1) * kBytesK, 32);
     // float32 accumulators, both operands e4m3, K-major
-    a.idesc = (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((pair ? 256 : 128) >> 4) << 24);
+    a.idesc = (1u << 4) | ((uint32_t)((BN > 128 ? 128 : BN) >> 3) << 17) | ((uint32_t)((pair ? 256 : 128) >> 4) << 24);
     a.wide = (uintptr_t)p.out % 16 == 0 && p.out_pitch % 16 == 0;
     CUtensorMap tmA, tmB, tmC = {};
-    if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, b_rows)) return DC_ERR_CUDA;
+    if (!encode_rows(&tmA, p.a, p.a_pitch, p.m, p.k, kTileM) || !encode_rows(&tmB, p.b, p.b_pitch, p.n, p.k, BN > 128 ? b_rows / 2 : b_rows)) return DC_ERR_CUDA;
     if (a.wide && (size_t)p.n * elt % 16 == 0) a.boxes = encode_out(&tmC, p.out, p.out_pitch, p.m, p.n, elt);
     const long long items = (pair ? (a.m_tiles + 1) / 2 : a.m_tiles) * (long long)a.NB, cap = pair ? num_sms / 2 : num_sms;
     if (items >= 0x70000000) return DC_ERR_LIMIT;
@@ -1053,20 +1115,23 @@ int launch_product(const BlocksProduct& p, int dtype, bool early, int device, in
 }
 
 template <typename T, bool WIDE>
-int launch_quantize(const BlocksArgs& a, int device, cudaStream_t stream)
+int launch_quantize(const BlocksArgs& a, int device, int num_sms, cudaStream_t stream)
 {
-    if (!a.qt && a.block_rows == 1) {
-        const int64_t items = ((int64_t)a.rows + 3) / 4 * a.kb;
-        if (items < 0x7fffffff) {
-            // n / kb = n * by.x >> (32 + by.y) for n < 2^31, by.x the next whole number above 2^(32 + by.y) / kb, 2^by.y < kb
-            uint2 by = make_uint2(0, 0);
-            if (a.kb > 1) {
-                while ((2 << by.y) < a.kb) ++by.y;
-                by.x = (uint32_t)((((uint64_t)1 << (32 + by.y)) + a.kb - 1) / a.kb);
-            }
-            DC_CUDA(dc_launch_pdl(k_quantize_row_blocks<T, WIDE>, dim3((unsigned)((items + 15) / 16)), 256, 0, stream, a, by, (uint32_t)items));
-            return DC_OK;
-        }
+    const int64_t items = ((int64_t)a.rows + 3) / 4 * a.kb;
+    // n / kb = n * by.x >> (32 + by.y) for n < 2^31, by.x the next whole number above 2^(32 + by.y) / kb, 2^by.y < kb
+    uint2 by = make_uint2(0, 0);
+    if (a.kb > 1) {
+        while ((2 << by.y) < a.kb) ++by.y;
+        by.x = (uint32_t)((((uint64_t)1 << (32 + by.y)) + a.kb - 1) / a.kb);
+    }
+    if (!a.qt && a.block_rows == 1 && items < 0x7fffffff) {
+        DC_CUDA(dc_launch_pdl(k_quantize_row_blocks<T, WIDE>, dim3((unsigned)((items + 15) / 16)), 256, 0, stream, a, by, (uint32_t)items));
+        return DC_OK;
+    }
+    if (a.qt && a.block_rows == 1 && 2 * (int64_t)a.kb * a.rb < 5 * (int64_t)num_sms) {
+        const int rows = a.q ? (int)((items + 15) / 16) : 0;
+        DC_CUDA(dc_launch_pdl(k_quantize_columns<T, WIDE>, dim3((unsigned)(rows + a.rb * dc_div_up(a.channels, 32))), 256, 0, stream, a, by, (uint32_t)items, rows));
+        return DC_OK;
     }
     const int64_t tiles = (int64_t)a.kb * a.rb;
     if (tiles > 0x7fffffff) return DC_ERR_LIMIT;
@@ -1078,12 +1143,12 @@ int launch_quantize(const BlocksArgs& a, int device, cudaStream_t stream)
     return DC_OK;
 }
 
-int quantize(BlocksArgs& a, int dtype, int device, cudaStream_t stream)
+int quantize(BlocksArgs& a, int dtype, int device, int num_sms, cudaStream_t stream)
 {
     a.kb = dc_div_up(a.channels, 128); a.rb = (int)(((int64_t)a.rows + 127) / 128);
     const bool wide = (uintptr_t)a.x % 16 == 0 && (a.rows < 2 || a.x_pitch % 16 == 0) && a.channels % 8 == 0;
-    if (dtype == DC_BF16) return wide ? launch_quantize<__nv_bfloat16, true>(a, device, stream) : launch_quantize<__nv_bfloat16, false>(a, device, stream);
-    return wide ? launch_quantize<float, true>(a, device, stream) : launch_quantize<float, false>(a, device, stream);
+    if (dtype == DC_BF16) return wide ? launch_quantize<__nv_bfloat16, true>(a, device, num_sms, stream) : launch_quantize<__nv_bfloat16, false>(a, device, num_sms, stream);
+    return wide ? launch_quantize<float, true>(a, device, num_sms, stream) : launch_quantize<float, false>(a, device, num_sms, stream);
 }
 
 bool floats_ok(const float* p) { return (uintptr_t)p % sizeof(float) == 0; }
@@ -1124,7 +1189,7 @@ int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t 
     a.q = q_dev; a.q_pitch = q_pitch; a.scale = scale_dev; a.qt = qt_dev; a.qt_pitch = qt_pitch; a.scale_t = scale_t_dev;
     int device = 0, sms = 0;
     const int rc = dc_current_device(&device, &sms);
-    return rc != DC_OK ? rc : quantize(a, dtype, device, (cudaStream_t)cuda_stream);
+    return rc != DC_OK ? rc : quantize(a, dtype, device, sms, (cudaStream_t)cuda_stream);
 }
 
 int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const uint8_t* b_dev, size_t b_pitch, const float* b_scale_dev, int32_t b_block_rows,
@@ -1164,7 +1229,7 @@ int dc_linear_blocks(const void* x_dev, size_t x_pitch, const uint8_t* w_dev, si
     float* const scale = (float*)(q + (size_t)m * pitch);
     BlocksArgs a = {};
     a.x = x_dev; a.x_pitch = x_pitch; a.rows = (int)m; a.channels = k; a.block_rows = 1; a.q = q; a.q_pitch = pitch; a.scale = scale;
-    if ((rc = quantize(a, dtype, device, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
+    if ((rc = quantize(a, dtype, device, sms, (cudaStream_t)cuda_stream)) != DC_OK) return rc;
     const BlocksProduct p = {q, pitch, scale, w_dev, w_pitch, w_scale_dev, bias_dev, m, n, k, relu, w_block_rows, out_dev, out_pitch};
     return launch_product(p, dtype, true, device, sms, (cudaStream_t)cuda_stream);
 }

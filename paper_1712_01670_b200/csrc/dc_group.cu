@@ -32,6 +32,8 @@ struct GroupArgs {
     int chunks, rows_per;                           // CTAs to the rows of a slice, and the rows of each
     float2* part;                                   // [maps][chunks * pieces][groups]: mean and squares, or the two sums of a group's gradients
     float* sums;                                    // [maps][chunks][2][channels]: sums of dz and of dz xh; or NULL: not wanted
+    bool joined;                                    // (host) they have been
+    float *dgamma, *dbeta;                          // of a single map that clusters hold whole: written at once
 };
 
 // The columns of a CTA.
@@ -466,6 +468,12 @@ __device__ __forceinline__ void send(const float2* at, int rank, float2 v)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(at)), "r"(rank));
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
 }
+__device__ __forceinline__ void send(const float* at, int rank, float v)
+{
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(at)), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
+}
 // What threads of one column have to add up: within a warp first, where its lanes hold whole rows of columns.  Returns the rows of partial sums that are left.
 template <int N, typename F>
 __device__ __forceinline__ int fold(F (&v)[N], int cols, int turns)
@@ -680,14 +688,16 @@ __global__ void __launch_bounds__(kMostResident, ONE ? 4 : 2) k_group_back_resid
             part[to * 2 * wide + col * VE + i] = lane_of(s[i / 2], i & 1);
             part[(to * 2 + 1) * wide + col * VE + i] = lane_of(s[P + i / 2], i & 1);
         }
+    float* const sums_of_all = part + (size_t)left * 2 * wide;               // [chunks][2][channels]: of a single map, in the first CTA
     __syncthreads();
+    cluster_wait(a.chunks > 1);
     for (int i = threadIdx.x; i < 2 * wide; i += blockDim.x) {
         const float t = rows_of_sums(part, left, 2 * wide, i);
         part[i] = t;                                          // (its own column alone)
-        if (a.sums) a.sums[((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + (i < wide ? p.col0 * VE + i : a.channels + p.col0 * VE + i - wide)] = t;
+        if (a.dgamma || a.dbeta) send(sums_of_all + p.chunk * 2 * wide + i, 0, t);
+        else if (a.sums) a.sums[((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + (i < wide ? p.col0 * VE + i : a.channels + p.col0 * VE + i - wide)] = t;
     }
     __syncthreads();
-    cluster_wait(a.chunks > 1);
     const int of = wide / p.ngroups;
     for (int g = threadIdx.x >> 5; g < p.ngroups; g += blockDim.x >> 5) {
         float t1 = 0.f, t2 = 0.f;
@@ -700,6 +710,13 @@ __global__ void __launch_bounds__(kMostResident, ONE ? 4 : 2) k_group_back_resid
         if (rank < a.chunks) send(&exchange[p.chunk][g], rank, make_float2(t1, t2));
     }
     if (a.chunks > 1) cluster_sync(); else __syncthreads();
+    if ((a.dgamma || a.dbeta) && p.chunk == 0)
+        for (int i = threadIdx.x; i < 2 * wide; i += blockDim.x) {
+            const float t = rows_of_sums(sums_of_all, a.chunks, 2 * wide, i);
+            const int ch = p.col0 * VE + (i < wide ? i : i - wide);
+            if (i < wide) { if (a.dbeta) a.dbeta[ch] = t; }
+            else if (a.dgamma) a.dgamma[ch] = t;
+        }
     if (!a.y) return;
     if (threadIdx.x < p.ngroups) {
         float t1 = 0.f, t2 = 0.f;
@@ -824,7 +841,7 @@ bool plan_resident(GroupArgs& a, int ve, int planes, int num_sms, int* block, si
     turns = threads / a.width;
     const int left = a.width & (a.width - 1) ? turns : threads / 32;
     *block = threads;
-    *smem = (size_t)a.rows_per * a.width * bytes + (size_t)left * 2 * a.width * ve * sizeof(float);
+    *smem = (size_t)a.rows_per * a.width * bytes + (size_t)(left + (a.dgamma || a.dbeta ? cs : 0)) * 2 * a.width * ve * sizeof(float);
     return *smem <= (size_t)kMostKept + 16 * 1024;
 }
 
@@ -854,7 +871,9 @@ cudaError_t launch_group(GroupArgs& a, bool back, int device, int num_sms, cudaS
         size_t smem = 0;
         int block = 0;
         const int planes = back ? 2 : 1;                      // 16 bytes that are kept of a column's row: x, and dy
+        if (a.maps > 1) r.dgamma = r.dbeta = nullptr;
         if (plan_resident(r, VE, planes, num_sms, &block, &smem)) {
+            a.joined = r.dgamma || r.dbeta;
             a.chunks = r.chunks;                              // (for the join of the sums)
             return launch_resident<T, VE, ONE, ACT>(r, back, block, smem, device, stream);
         }
@@ -979,9 +998,10 @@ int dc_group_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_de
     a.mean = (float*)mean_dev; a.rstd = (float*)rstd_dev;
     a.maps = (int)maps; a.pixels = (int)pixels; a.channels = channels; a.groups = groups; a.per = channels / groups;
     a.part = (float2*)(((uintptr_t)workspace_dev + 255) & ~(uintptr_t)255);
+    a.dgamma = dgamma_dev; a.dbeta = dbeta_dev;
     a.sums = weights ? (float*)((char*)a.part + part_bytes(maps, most_chunks(maps, pixels), channels, groups)) : nullptr;
     if ((rc = launch(a, true, activation, dtype, stream)) != DC_OK) return rc;
-    if (weights)
+    if (weights && !a.joined)
         DC_CUDA(dc_launch_pdl(k_group_join, dim3((unsigned)dc_div_up(2 * channels, 32)), 1024, 0, stream, (const float*)a.sums, a.maps * a.chunks, (int)channels, dgamma_dev, dbeta_dev));
     return DC_OK;
 }
