@@ -8,9 +8,8 @@
 // A slice is the columns of a map that a CTA works on: some whole groups, or a piece of one that is wider than a CTA.  A thread has one column (16 bytes of
 // each of its rows, or one element where rows are not aligned to 16 bytes) and so one set of weights and of sums.
 //
-// Sums of squares: each thread takes its values' distances from the first of them, which is one of the n values themselves, so the squares around it are at most n
-// times those around the mean, whatever the mean is; threads', CTAs' and chunks' means and squares are then joined by
-// M2 = sum M2_i + sum n_i (mean_i - mean)^2, in a fixed order: equal calls give equal bits.
+// Sums of squares: a CTA takes its values' distances from one of them (the group's first in its first row), so that no distance is beyond the group's range, whatever the mean is, and
+// threads' sums just add up; CTAs' means and squares are then joined by M2 = sum M2_i + sum n_i (mean_i - mean)^2, in a fixed order: equal calls give equal bits.
 #include <atomic>
 
 #include "dc_quantise.cuh"
@@ -18,7 +17,7 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostChunks = 64;
+constexpr int kMostChunks = 128;
 
 struct GroupArgs {
     const void *x, *dy; void* y;                    // y: the output, or dx
@@ -28,7 +27,7 @@ struct GroupArgs {
     float eps;
     int maps, pixels, channels, groups, per;        // per: channels of a group
     int width, slices, gs, pieces, piece_items;     // columns of a slice; slices of a map; groups of a slice; slices of a group; columns of a group (with pieces)
-    int by_width, by_per;                           // slices of at most 16 columns: 65536 / width and / per, rounded up; else 0
+    int by_width, by_per;                           // slices of at most 64 columns: 65536 / width and (groups of at most 128 channels) / per, rounded up; else 0
     int chunks, rows_per;                           // CTAs to the rows of a slice, and the rows of each
     float2* part;                                   // [maps][chunks * pieces][groups]: mean and squares, or the two sums of a group's gradients
     float* sums;                                    // [maps][chunks][2][channels]: sums of dz and of dz xh; or NULL: not wanted
@@ -144,110 +143,26 @@ template <typename F> __device__ __forceinline__ F hat(F x, F minus_mean, F rstd
 __device__ __forceinline__ float affine(float xh, float g, float b) { return __fadd_rn(__fmul_rn(xh, g), b); }
 __device__ __forceinline__ float2 affine(float2 xh, float2 g, float2 b) { return add2(mul2(xh, g), b); }
 
-// Means and squares of the items of a group, joined by a warp: item i has n(i) values; all lanes get the result.
-template <typename N, typename M, typename Q>
-__device__ __forceinline__ float2 join_items(int items, N n, M mean, Q squares, float total)
+// Nothing is sent to another CTA of a cluster before every one of them runs.
+__device__ __forceinline__ void cluster_started(bool cluster) { if (cluster) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait(bool cluster) { if (cluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// A thread's place: `turns` rows of columns at once.
+struct Seat { int col, turn, turns; };
+__device__ __forceinline__ Seat seat_of(const GroupArgs& a, const Place& p)
 {
-    const int lane = threadIdx.x & 31;
-    float s = 0.f;
-    for (int i = lane; i < items; i += 32) s = fmaf(n(i), mean(i), s);
-    s = reduce_lanes<Sum>(s, 32);
-    const float m = total > 0.f ? s / total : 0.f;
-    float q = 0.f;
-    for (int i = lane; i < items; i += 32) {
-        const float w = n(i), d = mean(i) - m;
-        q += w > 0.f ? fmaf(w * d, d, squares(i)) : 0.f;
-    }
-    return make_float2(m, reduce_lanes<Sum>(q, 32));
+    Seat s;
+    if (a.by_width) { s.turns = (int)blockDim.x * a.by_width >> 16; s.turn = (int)threadIdx.x * a.by_width >> 16; }
+    else { s.turns = (int)blockDim.x / p.cols; s.turn = (int)threadIdx.x / p.cols; }
+    s.col = (int)threadIdx.x - s.turn * p.cols;
+    return s;
 }
 
-// Chunks' statistics of a map (k_group_apply's input), of a thread's columns.  ONE: a column's channels belong to one group.
-template <typename T, int VE, bool ONE>
-__global__ void __launch_bounds__(kThreads) k_group_stats(const GroupArgs a)
-{
-    typedef Vec<T, VE> V;
-    typedef typename V::F F;
-    constexpr int P = V::P, IT = ONE ? 1 : VE;       // items (channels or whole columns) of a column
-    __shared__ float pm[kThreads * IT], pq[kThreads * IT];
-    dc_pdl_wait();
-    dc_pdl_release();
-    const Place p = place_of(a);
-    const int turns = kThreads / p.cols, col = threadIdx.x % p.cols, turn = threadIdx.x / p.cols;
-    if (turn < turns) {
-        const char* const x = row_at(a.x, a.x_pitch, (int64_t)p.map * a.pixels + p.row0) + (size_t)(p.col0 + col) * VE * sizeof(T);
-        F s[ONE ? 1 : P], q[ONE ? 1 : P], shift[ONE ? 1 : P];
-#pragma unroll
-        for (int k = 0; k < (ONE ? 1 : P); ++k) s[k] = q[k] = shift[k] = both<F>(0.f);
-        int n = 0;
-        for (int r = turn; r < p.rows; r += 4 * turns) {
-            typename V::Raw raw[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) raw[u] = r + u * turns < p.rows ? *(const typename V::Raw*)(x + (size_t)(r + u * turns) * a.x_pitch) : raw_zero<typename V::Raw>();
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (r + u * turns >= p.rows) break;
-                F d[P];
-                V::open(raw[u], d);
-                if (n++ == 0)
-#pragma unroll
-                    for (int k = 0; k < (ONE ? 1 : P); ++k) shift[k] = ONE ? both<F>(-lane_of(d[0], 0)) : mul2(d[k], both<F>(-1.f));
-#pragma unroll
-                for (int k = 0; k < P; ++k) {
-                    const int at = ONE ? 0 : k;
-                    const F t = add2(d[k], shift[at]);
-                    s[at] = add2(s[at], t);
-                    q[at] = fma2(t, t, q[at]);
-                }
-            }
-        }
-        // the thread's items: mean and squares around it
-        const float count = (float)(n * (ONE ? VE : 1));
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            const float ss = ONE ? sum_of(s[0]) : lane_of(s[ONE ? 0 : i / 2], i & 1), qq = ONE ? sum_of(q[0]) : lane_of(q[ONE ? 0 : i / 2], i & 1);
-            const float m = n ? ss / count : 0.f;
-            const int at = turn * p.cols * IT + col * IT + i;
-            pm[at] = m - lane_of(shift[ONE ? 0 : i / 2], i & 1);
-            pq[at] = fmaxf(fmaf(-m, ss, qq), 0.f) + (ss - ss);           // (a NaN or an infinity stays one)
-        }
-    }
-    __syncthreads();
-    const int items = p.cols * IT, of = a.pieces > 1 ? items : items / p.ngroups;
-    for (int g = threadIdx.x >> 5; g < p.ngroups; g += kThreads / 32) {
-        auto at = [&](int i) { return i / of * items + g * of + i % of; };
-        auto n = [&](int i) { const int t = i / of; return (float)((p.rows > t ? (p.rows - t + turns - 1) / turns : 0) * (ONE ? VE : 1)); };
-        const float2 r = join_items(turns * of, n, [&](int i) { return pm[at(i)]; }, [&](int i) { return pq[at(i)]; }, (float)p.rows * of * (ONE ? VE : 1));
-        if ((threadIdx.x & 31) == 0) a.part[((size_t)p.map * a.chunks * a.pieces + p.chunk * a.pieces + p.piece) * a.groups + p.group0 + g] = r;
-    }
-}
-
-// A slice's groups' mean and rstd, from the chunks'.
-template <int VE>
-__device__ __forceinline__ void join_chunks(const GroupArgs& a, const Place& p, float2* fin)
-{
-    for (int g = threadIdx.x >> 5; g < p.ngroups; g += kThreads / 32) {
-        const float2* const part = a.part + (size_t)p.map * a.chunks * a.pieces * a.groups + p.group0 + g;
-        auto at = [&](int i) { return __ldcg(part + (size_t)i * a.groups); };
-        auto n = [&](int i) { return (float)rows_of(a, i / a.pieces) * (float)(a.pieces > 1 ? cols_of(a, i % a.pieces) * VE : a.per); };
-        const float total = (float)a.pixels * (float)a.per;
-        const float2 r = join_items(a.chunks * a.pieces, n, [&](int i) { return at(i).x; }, [&](int i) { return at(i).y; }, total);
-        const float rstd = inverse_root(r.y / total + a.eps);
-        if ((threadIdx.x & 31) == 0) {
-            fin[g] = make_float2(r.x, rstd);
-            if (p.chunk == 0 && p.piece == 0) {
-                if (a.mean) a.mean[(size_t)p.map * a.groups + p.group0 + g] = r.x;
-                if (a.rstd) a.rstd[(size_t)p.map * a.groups + p.group0 + g] = rstd;
-            }
-        }
-    }
-    __syncthreads();
-}
-
-// What a thread keeps of its column: the weights, and its groups' numbers (fin: of the slice's groups).
+// What a thread keeps of its column: the weights, and its groups' numbers.
 template <typename T, int VE, bool ONE> struct Column {
     typedef typename Vec<T, VE>::F F;
-    static constexpr int P = Vec<T, VE>::P;
-    F g[P], b[P], first[ONE ? 1 : P], second[ONE ? 1 : P];
+    static constexpr int P = Vec<T, VE>::P, N = ONE ? 1 : P;
+    F g[P], b[P];
     __device__ __forceinline__ void weights(const GroupArgs& a, const Place& p, int col)
     {
         const int c = (p.col0 + col) * VE;
@@ -263,11 +178,12 @@ template <typename T, int VE, bool ONE> struct Column {
             b[k] = two<F>(a.beta ? dc_ld(a.beta + c + (VE > 1 ? 2 * k : 0)) : 0.f, VE > 1 ? (a.beta ? dc_ld(a.beta + c + 2 * k + 1) : 0.f) : 0.f);
         }
     }
+    // Two numbers of each of its groups; read(group of the slice).
     template <typename R>
-    __device__ __forceinline__ void groups(const GroupArgs& a, const Place& p, int col, F* first, F* second, R read) const
+    static __device__ __forceinline__ void groups(const GroupArgs& a, int col, F* first, F* second, R read)
     {
 #pragma unroll
-        for (int k = 0; k < (ONE ? 1 : P); ++k) {
+        for (int k = 0; k < N; ++k) {
             float2 v[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -280,222 +196,22 @@ template <typename T, int VE, bool ONE> struct Column {
     }
 };
 
-template <typename T, int VE, bool ONE, int ACT>
-__global__ void __launch_bounds__(kThreads) k_group_apply(const GroupArgs a)
-{
-    typedef Vec<T, VE> V;
-    typedef typename V::F F;
-    constexpr int P = V::P;
-    __shared__ float2 fin[kThreads * (ONE ? 1 : VE)];
-    dc_pdl_wait();
-    dc_pdl_release();
-    const Place p = place_of(a);
-    join_chunks<VE>(a, p, fin);
-    const int turns = kThreads / p.cols, col = threadIdx.x % p.cols, turn = threadIdx.x / p.cols;
-    if (turn >= turns) return;
-    Column<T, VE, ONE> c;
-    F mean[ONE ? 1 : P], rstd[ONE ? 1 : P];
-    c.weights(a, p, col);
-    c.groups(a, p, col, mean, rstd, [&](int g) { return make_float2(-fin[g].x, fin[g].y); });
-    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
-    const size_t at = (size_t)(p.col0 + col) * VE * sizeof(T);
-    const char* const x = row_at(a.x, a.x_pitch, row0) + at;
-    char* const y = row_at(a.y, a.y_pitch, row0) + at;
-    for (int r = turn; r < p.rows; r += 4 * turns) {
-        typename V::Raw raw[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) raw[u] = r + u * turns < p.rows ? *(const typename V::Raw*)(x + (size_t)(r + u * turns) * a.x_pitch) : raw_zero<typename V::Raw>();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (r + u * turns >= p.rows) break;
-            F d[P];
-            V::open(raw[u], d);
-#pragma unroll
-            for (int k = 0; k < P; ++k) d[k] = affine(hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), c.g[k], c.b[k]);
-            activate<ACT, ONE>(d);
-            *(typename V::Raw*)(y + (size_t)(r + u * turns) * a.y_pitch) = V::close(d);
-        }
-    }
-}
-
-// Gradients, first pass: a chunk's sums of dz and dz xh of each channel, and of each group with gamma.
-template <typename T, int VE, bool ONE, int ACT>
-__global__ void __launch_bounds__(kThreads) k_group_back_sums(const GroupArgs a)
-{
-    typedef Vec<T, VE> V;
-    typedef typename V::F F;
-    constexpr int P = V::P;
-    __shared__ float s1[kThreads * VE], s2[kThreads * VE];
-    dc_pdl_wait();
-    dc_pdl_release();
-    const Place p = place_of(a);
-    const int turns = kThreads / p.cols, col = threadIdx.x % p.cols, turn = threadIdx.x / p.cols, wide = p.cols * VE;
-    if (turn < turns) {
-        Column<T, VE, ONE> c;
-        F mean[ONE ? 1 : P], rstd[ONE ? 1 : P], d1[P], d2[P];
-        c.weights(a, p, col);
-        const size_t of = (size_t)p.map * a.groups + p.group0;
-        c.groups(a, p, col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of + g), dc_ld(a.rstd + of + g)); });
-#pragma unroll
-        for (int k = 0; k < P; ++k) d1[k] = d2[k] = both<F>(0.f);
-        const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
-        const size_t at = (size_t)(p.col0 + col) * VE * sizeof(T);
-        const char *const x = row_at(a.x, a.x_pitch, row0) + at, *const dy = row_at(a.dy, a.dy_pitch, row0) + at;
-        for (int r = turn; r < p.rows; r += 2 * turns) {
-            typename V::Raw rx[2], rd[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bool there = r + u * turns < p.rows;
-                rx[u] = there ? *(const typename V::Raw*)(x + (size_t)(r + u * turns) * a.x_pitch) : raw_zero<typename V::Raw>();
-                rd[u] = there ? *(const typename V::Raw*)(dy + (size_t)(r + u * turns) * a.dy_pitch) : raw_zero<typename V::Raw>();
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (r + u * turns >= p.rows) break;
-                F d[P], e[P], z[P];
-                V::open(rx[u], d);
-                V::open(rd[u], e);
-#pragma unroll
-                for (int k = 0; k < P; ++k) { d[k] = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(d[k], c.g[k], c.b[k]); }
-                activate_back<ACT, ONE>(e, z);
-#pragma unroll
-                for (int k = 0; k < P; ++k) { d1[k] = add2(d1[k], e[k]); d2[k] = fma2(e[k], d[k], d2[k]); }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < VE; ++i) { s1[turn * wide + col * VE + i] = lane_of(d1[i / 2 % P], i & 1); s2[turn * wide + col * VE + i] = lane_of(d2[i / 2 % P], i & 1); }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < wide; i += kThreads) {
-        float t1 = 0.f, t2 = 0.f;
-        for (int t = 0; t < turns; ++t) { t1 += s1[t * wide + i]; t2 += s2[t * wide + i]; }
-        s1[i] = t1; s2[i] = t2;
-        const int ch = p.col0 * VE + i;
-        if (a.sums) {
-            float* const out = a.sums + ((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + ch;
-            out[0] = t1; out[a.channels] = t2;
-        }
-    }
-    __syncthreads();
-    const int of = wide / p.ngroups;
-    for (int g = threadIdx.x >> 5; g < p.ngroups; g += kThreads / 32) {
-        float t1 = 0.f, t2 = 0.f;
-        for (int i = g * of + (threadIdx.x & 31); i < (g + 1) * of; i += 32) {
-            const float w = a.gamma ? dc_ld(a.gamma + p.col0 * VE + i) : 1.f;
-            t1 = fmaf(w, s1[i], t1); t2 = fmaf(w, s2[i], t2);
-        }
-        t1 = reduce_lanes<Sum>(t1, 32); t2 = reduce_lanes<Sum>(t2, 32);
-        if ((threadIdx.x & 31) == 0) a.part[((size_t)p.map * a.chunks * a.pieces + p.chunk * a.pieces + p.piece) * a.groups + p.group0 + g] = make_float2(t1, t2);
-    }
-}
-
-// Second pass: dx.
-template <typename T, int VE, bool ONE, int ACT>
-__global__ void __launch_bounds__(kThreads) k_group_back_apply(const GroupArgs a)
-{
-    typedef Vec<T, VE> V;
-    typedef typename V::F F;
-    constexpr int P = V::P;
-    __shared__ float2 fin[kThreads * (ONE ? 1 : VE)];
-    dc_pdl_wait();
-    dc_pdl_release();
-    const Place p = place_of(a);
-    for (int g = threadIdx.x >> 5; g < p.ngroups; g += kThreads / 32) {
-        const float2* const part = a.part + (size_t)p.map * a.chunks * a.pieces * a.groups + p.group0 + g;
-        float t1 = 0.f, t2 = 0.f;
-        for (int i = threadIdx.x & 31; i < a.chunks * a.pieces; i += 32) { const float2 v = __ldcg(part + (size_t)i * a.groups); t1 += v.x; t2 += v.y; }
-        t1 = reduce_lanes<Sum>(t1, 32); t2 = reduce_lanes<Sum>(t2, 32);
-        const float total = (float)a.pixels * (float)a.per;
-        if ((threadIdx.x & 31) == 0) fin[g] = make_float2(-t1 / total, -t2 / total);
-    }
-    __syncthreads();
-    const int turns = kThreads / p.cols, col = threadIdx.x % p.cols, turn = threadIdx.x / p.cols;
-    if (turn >= turns) return;
-    Column<T, VE, ONE> c;
-    F mean[ONE ? 1 : P], rstd[ONE ? 1 : P], m1[ONE ? 1 : P], m2[ONE ? 1 : P];
-    c.weights(a, p, col);
-    const size_t of = (size_t)p.map * a.groups + p.group0;
-    c.groups(a, p, col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of + g), dc_ld(a.rstd + of + g)); });
-    c.groups(a, p, col, m1, m2, [&](int g) { return fin[g]; });
-    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
-    const size_t at = (size_t)(p.col0 + col) * VE * sizeof(T);
-    const char *const x = row_at(a.x, a.x_pitch, row0) + at, *const dy = row_at(a.dy, a.dy_pitch, row0) + at;
-    char* const dx = row_at(a.y, a.y_pitch, row0) + at;
-    for (int r = turn; r < p.rows; r += 2 * turns) {
-        typename V::Raw rx[2], rd[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const bool there = r + u * turns < p.rows;
-            rx[u] = there ? *(const typename V::Raw*)(x + (size_t)(r + u * turns) * a.x_pitch) : raw_zero<typename V::Raw>();
-            rd[u] = there ? *(const typename V::Raw*)(dy + (size_t)(r + u * turns) * a.dy_pitch) : raw_zero<typename V::Raw>();
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            if (r + u * turns >= p.rows) break;
-            F d[P], e[P], z[P];
-            V::open(rx[u], d);
-            V::open(rd[u], e);
-#pragma unroll
-            for (int k = 0; k < P; ++k) { d[k] = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(d[k], c.g[k], c.b[k]); }
-            activate_back<ACT, ONE>(e, z);
-#pragma unroll
-            for (int k = 0; k < P; ++k) d[k] = mul2(fma2(d[k], m2[ONE ? 0 : k], add2(mul2(e[k], c.g[k]), m1[ONE ? 0 : k])), rstd[ONE ? 0 : k]);
-            *(typename V::Raw*)(dx + (size_t)(r + u * turns) * a.y_pitch) = V::close(d);
-        }
-    }
-}
-
-// ---------------------------------------------------------------------------
-// A slice of a map in the shared memory of a cluster: read once
-// ---------------------------------------------------------------------------
-constexpr int kMostResident = 256;                            // threads
-constexpr int kMostCluster = 8, kMostGroups = 64;             // CTAs to a slice; groups of one
-
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// Nothing is sent before every CTA of the cluster runs.
-__device__ __forceinline__ void cluster_started(bool cluster) { if (cluster) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait(bool cluster) { if (cluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// To the same place in CTA `rank` of the cluster.
-__device__ __forceinline__ void send(const float2* at, int rank, float2 v)
-{
-    uint32_t to;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(at)), "r"(rank));
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
-}
-__device__ __forceinline__ void send(const float* at, int rank, float v)
-{
-    uint32_t to;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(at)), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
-}
 // What threads of one column have to add up: within a warp first, where its lanes hold whole rows of columns.  Returns the rows of partial sums that are left.
+__device__ __forceinline__ bool folds(int cols) { return cols <= 32 && !(cols & (cols - 1)); }
 template <int N, typename F>
 __device__ __forceinline__ int fold(F (&v)[N], int cols, int turns)
 {
-    if (cols & (cols - 1)) return turns;
+    if (!folds(cols)) return turns;
     for (int o = cols; o < 32; o <<= 1)
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = add_shuffled(v[k], o);
     return (int)blockDim.x >> 5;
 }
 // ... and which of them this thread leaves, or none.
-__device__ __forceinline__ int fold_row(int cols, int turn, int turns)
+__device__ __forceinline__ int fold_row(const Seat& s, int cols)
 {
-    if (cols & (cols - 1)) return turn < turns ? turn : -1;
+    if (!folds(cols)) return s.turn < s.turns ? s.turn : -1;
     return (threadIdx.x & 31) < cols ? (int)(threadIdx.x >> 5) : -1;
-}
-// A thread's place: `turns` rows of columns at once (at most 256 threads and 16 columns: one multiplication).
-__device__ __forceinline__ void seat(const GroupArgs& a, int& col, int& turn, int& turns)
-{
-    turns = (int)blockDim.x * a.by_width >> 16;
-    turn = (int)threadIdx.x * a.by_width >> 16;
-    col = (int)threadIdx.x - turn * a.width;
 }
 // Rows of partial sums added up: a thread to each of `wide` places.
 __device__ __forceinline__ float rows_of_sums(const float* part, int left, int wide, int i)
@@ -505,7 +221,363 @@ __device__ __forceinline__ float rows_of_sums(const float* part, int left, int w
     for (int k = 0; k < left; ++k) t += part[k * wide + i];
     return t;
 }
+// Lanes to a group of so many items: a power of two.
+__device__ __forceinline__ int lanes_to(int items) { return items >= 32 ? 32 : 1 << (31 - __clz(items)); }
 
+// The value that a group's distances are taken from: its first channel in the CTA's first row.
+template <typename T>
+__device__ __forceinline__ float first_of(const GroupArgs& a, const Place& p, int64_t row0, int g)
+{
+    float v;
+    Vec<T, 1>::open(((const T*)row_at(a.x, a.x_pitch, row0))[(p.group0 + g) * a.per], &v);
+    return v;
+}
+
+// Statistics of a CTA's rows: s holds each thread's sums of distances and of their squares.  out(group, {mean, squares around it}, lane of the group, lanes)
+template <typename T, int VE, bool ONE, int N2, typename F, typename Out>
+__device__ __forceinline__ void finish_stats(const GroupArgs& a, const Place& p, const Seat& seat, int64_t row0, F (&s)[N2], float* part, bool cluster, Out out)
+{
+    constexpr int IT = ONE ? 1 : VE, N = N2 / 2;
+    const int items = p.cols * IT, left = fold(s, p.cols, seat.turns), to = fold_row(seat, p.cols);
+    if (to >= 0)
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            part[to * 2 * items + seat.col * IT + i] = ONE ? sum_of(s[0]) : lane_of(s[ONE ? 0 : i / 2], i & 1);
+            part[(to * 2 + 1) * items + seat.col * IT + i] = ONE ? sum_of(s[N]) : lane_of(s[N + (ONE ? 0 : i / 2)], i & 1);
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * items; i += blockDim.x) part[i] = rows_of_sums(part, left, 2 * items, i);       // (its own column alone)
+    __syncthreads();
+    cluster_wait(cluster);
+    const int of = items / p.ngroups, lanes = lanes_to(of), sub = threadIdx.x & (lanes - 1);
+    for (int base = 0; base < p.ngroups; base += blockDim.x / lanes) {
+        const int g = base + threadIdx.x / lanes;
+        float sum = 0.f, squares = 0.f;
+        if (g < p.ngroups)
+            for (int i = g * of + sub; i < (g + 1) * of; i += lanes) { sum += part[i]; squares += part[items + i]; }
+        sum = reduce_lanes<Sum>(sum, lanes); squares = reduce_lanes<Sum>(squares, lanes);
+        if (g >= p.ngroups) continue;
+        float2 r = make_float2(0.f, 0.f);
+        if (p.rows > 0) {
+            const float m = sum / ((float)p.rows * (float)(of * (ONE ? VE : 1)));
+            r = make_float2(m + first_of<T>(a, p, row0, g), fmaxf(fmaf(-m, sum, squares), 0.f) + (sum - sum));       // (a NaN or an infinity stays one)
+        }
+        out(g, r, sub, lanes);
+    }
+}
+
+// Means and squares of a group's parts, joined in their order: n(i) values in part i.  {-mean, rstd}
+template <typename N, typename V>
+__device__ __forceinline__ float2 join_parts(int parts, float total, float eps, int sub, int lanes, N n, V value)
+{
+    float s = 0.f, q = 0.f;
+#pragma unroll 4
+    for (int i = sub; i < parts; i += lanes) s = fmaf(n(i), value(i).x, s);
+    const float mean = reduce_lanes<Sum>(s, lanes) / total;
+#pragma unroll 4
+    for (int i = sub; i < parts; i += lanes) {
+        const float w = n(i);
+        const float2 v = value(i);
+        const float d = v.x - mean;
+        q += w > 0.f ? fmaf(w * d, d, v.y) : 0.f;
+    }
+    return make_float2(-mean, inverse_root(reduce_lanes<Sum>(q, lanes) / total + eps));
+}
+
+// Gradients, first half: s holds each thread's sums of dz and of dz xh.  total(place, sum) of each channel; out(group, the two sums with gamma, lane, lanes).
+template <int VE, int P2, typename F, typename Total, typename Out>
+__device__ __forceinline__ void finish_sums(const GroupArgs& a, const Place& p, const Seat& seat, F (&s)[P2], float* part, bool cluster, Total total, Out out)
+{
+    constexpr int P = P2 / 2;
+    const int wide = p.cols * VE, left = fold(s, p.cols, seat.turns), to = fold_row(seat, p.cols);
+    if (to >= 0)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+            part[to * 2 * wide + seat.col * VE + i] = lane_of(s[i / 2 % P], i & 1);
+            part[(to * 2 + 1) * wide + seat.col * VE + i] = lane_of(s[P + i / 2 % P], i & 1);
+        }
+    __syncthreads();
+    cluster_wait(cluster);
+    for (int i = threadIdx.x; i < 2 * wide; i += blockDim.x) {
+        const float t = rows_of_sums(part, left, 2 * wide, i);
+        part[i] = t;                                          // (its own column alone)
+        total(i, t);
+    }
+    __syncthreads();
+    const int of = wide / p.ngroups, lanes = lanes_to(of), sub = threadIdx.x & (lanes - 1);
+    for (int base = 0; base < p.ngroups; base += blockDim.x / lanes) {
+        const int g = base + threadIdx.x / lanes;
+        float t1 = 0.f, t2 = 0.f;
+        if (g < p.ngroups)
+            for (int i = g * of + sub; i < (g + 1) * of; i += lanes) {
+                const float w = a.gamma ? dc_ld(a.gamma + p.col0 * VE + i) : 1.f;
+                t1 = fmaf(w, part[i], t1); t2 = fmaf(w, part[wide + i], t2);
+            }
+        t1 = reduce_lanes<Sum>(t1, lanes); t2 = reduce_lanes<Sum>(t2, lanes);
+        if (g < p.ngroups) out(g, make_float2(t1, t2), sub, lanes);
+    }
+}
+
+// A row's share of a thread, and what is done to it.
+template <typename T, int VE, bool ONE> struct Work {
+    typedef Vec<T, VE> V;
+    typedef typename V::F F;
+    typedef typename V::Raw Raw;
+    static constexpr int P = V::P, N = ONE ? 1 : P;
+    static __device__ __forceinline__ void stats(Raw raw, const F* first, F* s)
+    {
+        F d[P];
+        V::open(raw, d);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const int i = ONE ? 0 : k;
+            const F t = add2(d[k], first[i]);
+            s[i] = add2(s[i], t);
+            s[N + i] = fma2(t, t, s[N + i]);
+        }
+    }
+    template <int ACT>
+    static __device__ __forceinline__ Raw apply(Raw raw, const Column<T, VE, ONE>& c, const F* mean, const F* rstd)
+    {
+        F d[P];
+        V::open(raw, d);
+#pragma unroll
+        for (int k = 0; k < P; ++k) d[k] = affine(hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), c.g[k], c.b[k]);
+        activate<ACT, ONE>(d);
+        return V::close(d);
+    }
+    template <int ACT>
+    static __device__ __forceinline__ void back(Raw x, Raw dy, const Column<T, VE, ONE>& c, const F* mean, const F* rstd, F (&xh)[P], F (&dz)[P])
+    {
+        F z[P];
+        V::open(x, xh);
+        V::open(dy, dz);
+#pragma unroll
+        for (int k = 0; k < P; ++k) { xh[k] = hat(xh[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(xh[k], c.g[k], c.b[k]); }
+        activate_back<ACT, ONE>(dz, z);
+    }
+    template <int ACT>
+    static __device__ __forceinline__ void sums(Raw x, Raw dy, const Column<T, VE, ONE>& c, const F* mean, const F* rstd, F* s, Raw* masked)
+    {
+        F xh[P], dz[P];
+        back<ACT>(x, dy, c, mean, rstd, xh, dz);
+#pragma unroll
+        for (int k = 0; k < P; ++k) { s[k] = add2(s[k], dz[k]); s[P + k] = fma2(dz[k], xh[k], s[P + k]); }
+        if (ACT == DC_ACT_RELU && masked) *masked = V::close(dz);      // dy or zero: as exact as it came
+    }
+    // ACT: DC_ACT_NONE where dy is dz already
+    template <int ACT>
+    static __device__ __forceinline__ Raw gradient(Raw x, Raw dy, const Column<T, VE, ONE>& c, const F* mean, const F* rstd, const F* m1, const F* m2)
+    {
+        F xh[P], dz[P];
+        back<ACT>(x, dy, c, mean, rstd, xh, dz);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const int i = ONE ? 0 : k;
+            xh[k] = mul2(fma2(xh[k], m2[i], add2(mul2(dz[k], c.g[k]), m1[i])), rstd[i]);
+        }
+        return V::close(xh);
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Two launches: a map's rows in up to 128 chunks, sums first, the map after
+// ---------------------------------------------------------------------------
+// f(row, raw) of a thread's rows, four loads in flight.
+template <int U, typename Raw, typename F>
+__device__ __forceinline__ void each_row(const Place& p, const Seat& s, const char* x, size_t x_pitch, F f)
+{
+    for (int r = s.turn; r < p.rows; r += U * s.turns) {
+        Raw raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = r + u * s.turns < p.rows ? *(const Raw*)(x + (size_t)(r + u * s.turns) * x_pitch) : raw_zero<Raw>();
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (r + u * s.turns < p.rows) f(r + u * s.turns, raw[u]);
+    }
+}
+template <int U, typename Raw, typename F>
+__device__ __forceinline__ void each_two(const Place& p, const Seat& s, const char* x, size_t x_pitch, const char* dy, size_t dy_pitch, F f)
+{
+    for (int r = s.turn; r < p.rows; r += U * s.turns) {
+        Raw rx[U], rd[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool there = r + u * s.turns < p.rows;
+            rx[u] = there ? *(const Raw*)(x + (size_t)(r + u * s.turns) * x_pitch) : raw_zero<Raw>();
+            rd[u] = there ? *(const Raw*)(dy + (size_t)(r + u * s.turns) * dy_pitch) : raw_zero<Raw>();
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (r + u * s.turns < p.rows) f(r + u * s.turns, rx[u], rd[u]);
+    }
+}
+
+template <typename T, int VE, bool ONE>
+__global__ void __launch_bounds__(kThreads) k_group_stats(const GroupArgs a)
+{
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    __shared__ float part[2 * kThreads * (ONE ? 1 : VE)];
+    dc_pdl_wait();
+    dc_pdl_release();
+    const Place p = place_of(a);
+    const Seat seat = seat_of(a, p);
+    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
+    F s[2 * W::N], first[W::N], unused[W::N];
+    Column<T, VE, ONE>::groups(a, seat.col, first, unused, [&](int g) { return make_float2(-first_of<T>(a, p, row0, g), 0.f); });
+#pragma unroll
+    for (int k = 0; k < 2 * W::N; ++k) s[k] = both<F>(0.f);
+    if (seat.turn < seat.turns)
+        each_row<4, typename W::Raw>(p, seat, row_at(a.x, a.x_pitch, row0) + (size_t)(p.col0 + seat.col) * VE * sizeof(T), a.x_pitch, [&](int, typename W::Raw raw) { W::stats(raw, first, s); });
+    finish_stats<T, VE, ONE>(a, p, seat, row0, s, part, false, [&](int g, float2 r, int sub, int) {
+        if (sub == 0) a.part[((size_t)p.map * a.chunks * a.pieces + p.chunk * a.pieces + p.piece) * a.groups + p.group0 + g] = r;
+    });
+}
+
+// join(group of the slice, whether there is one, lane, lanes): a slice's groups, as many lanes to each as there are parts to join, but so few that all groups go at once.
+template <typename J>
+__device__ __forceinline__ void each_group(const GroupArgs& a, const Place& p, J join)
+{
+    int lanes = lanes_to(a.chunks * a.pieces);
+    while (lanes > 1 && lanes * p.ngroups > (int)blockDim.x) lanes >>= 1;
+    const int sub = threadIdx.x & (lanes - 1);
+    for (int base = 0; base < p.ngroups; base += blockDim.x / lanes) {
+        const int g = base + threadIdx.x / lanes;
+        join(min(g, p.ngroups - 1), g < p.ngroups, sub, lanes);
+    }
+    __syncthreads();
+}
+// The values of part i of a group.
+template <int VE>
+__device__ __forceinline__ float part_size(const GroupArgs& a, int i)
+{
+    if (a.pieces == 1) return (float)rows_of(a, i) * (float)a.per;
+    const int chunk = i / a.pieces;
+    return (float)rows_of(a, chunk) * (float)(cols_of(a, i - chunk * a.pieces) * VE);
+}
+
+template <typename T, int VE, bool ONE, int ACT>
+__global__ void __launch_bounds__(kThreads) k_group_apply(const GroupArgs a)
+{
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    __shared__ float2 fin[kThreads * (ONE ? 1 : VE)];
+    dc_pdl_wait();
+    dc_pdl_release();
+    const Place p = place_of(a);
+    const Seat seat = seat_of(a, p);
+    Column<T, VE, ONE> c;
+    c.weights(a, p, seat.col);
+    each_group(a, p, [&](int g, bool on, int sub, int lanes) {
+        const float2* const part = a.part + (size_t)p.map * a.chunks * a.pieces * a.groups + p.group0 + g;
+        const float2 r = join_parts(a.chunks * a.pieces, (float)a.pixels * (float)a.per, a.eps, sub, lanes, [&](int i) { return part_size<VE>(a, i); },
+                                    [&](int i) { return dc_ld(part + (size_t)i * a.groups); });
+        if (!on || sub) return;
+        fin[g] = r;
+        if (p.chunk == 0 && p.piece == 0) {
+            if (a.mean) a.mean[(size_t)p.map * a.groups + p.group0 + g] = -r.x;
+            if (a.rstd) a.rstd[(size_t)p.map * a.groups + p.group0 + g] = r.y;
+        }
+    });
+    if (seat.turn >= seat.turns) return;
+    F mean[W::N], rstd[W::N];
+    c.groups(a, seat.col, mean, rstd, [&](int g) { return fin[g]; });
+    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
+    const size_t at = (size_t)(p.col0 + seat.col) * VE * sizeof(T);
+    char* const y = row_at(a.y, a.y_pitch, row0) + at;
+    each_row<4, typename W::Raw>(p, seat, row_at(a.x, a.x_pitch, row0) + at, a.x_pitch,
+                                 [&](int r, typename W::Raw raw) { *(typename W::Raw*)(y + (size_t)r * a.y_pitch) = W::template apply<ACT>(raw, c, mean, rstd); });
+}
+
+template <typename T, int VE, bool ONE, int ACT>
+__global__ void __launch_bounds__(kThreads) k_group_back_sums(const GroupArgs a)
+{
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    __shared__ float part[2 * kThreads * VE];
+    dc_pdl_wait();
+    dc_pdl_release();
+    const Place p = place_of(a);
+    const Seat seat = seat_of(a, p);
+    Column<T, VE, ONE> c;
+    F mean[W::N], rstd[W::N], s[2 * W::P];
+    c.weights(a, p, seat.col);
+    const size_t of = (size_t)p.map * a.groups + p.group0;
+    c.groups(a, seat.col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of + g), dc_ld(a.rstd + of + g)); });
+#pragma unroll
+    for (int k = 0; k < 2 * W::P; ++k) s[k] = both<F>(0.f);
+    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
+    const size_t at = (size_t)(p.col0 + seat.col) * VE * sizeof(T);
+    if (seat.turn < seat.turns)
+        each_two<2, typename W::Raw>(p, seat, row_at(a.x, a.x_pitch, row0) + at, a.x_pitch, row_at(a.dy, a.dy_pitch, row0) + at, a.dy_pitch,
+                                     [&](int, typename W::Raw x, typename W::Raw dy) { W::template sums<ACT>(x, dy, c, mean, rstd, s, nullptr); });
+    const int wide = p.cols * VE;
+    finish_sums<VE>(a, p, seat, s, part, false,
+        [&](int i, float t) { if (a.sums) a.sums[((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + (i < wide ? p.col0 * VE + i : a.channels + p.col0 * VE + i - wide)] = t; },
+        [&](int g, float2 r, int sub, int) {
+            if (sub == 0) a.part[((size_t)p.map * a.chunks * a.pieces + p.chunk * a.pieces + p.piece) * a.groups + p.group0 + g] = r;
+        });
+}
+
+template <typename T, int VE, bool ONE, int ACT>
+__global__ void __launch_bounds__(kThreads) k_group_back_apply(const GroupArgs a)
+{
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    __shared__ float2 fin[kThreads * (ONE ? 1 : VE)];
+    dc_pdl_wait();
+    dc_pdl_release();
+    const Place p = place_of(a);
+    const Seat seat = seat_of(a, p);
+    Column<T, VE, ONE> c;
+    c.weights(a, p, seat.col);
+    each_group(a, p, [&](int g, bool on, int sub, int lanes) {
+        const float2* const part = a.part + (size_t)p.map * a.chunks * a.pieces * a.groups + p.group0 + g;
+        float t1 = 0.f, t2 = 0.f;
+        for (int i = sub; i < a.chunks * a.pieces; i += lanes) { const float2 v = dc_ld(part + (size_t)i * a.groups); t1 += v.x; t2 += v.y; }
+        t1 = reduce_lanes<Sum>(t1, lanes); t2 = reduce_lanes<Sum>(t2, lanes);
+        const float total = (float)a.pixels * (float)a.per;
+        if (on && sub == 0) fin[g] = make_float2(-t1 / total, -t2 / total);
+    });
+    if (seat.turn >= seat.turns) return;
+    F mean[W::N], rstd[W::N], m1[W::N], m2[W::N];
+    const size_t of = (size_t)p.map * a.groups + p.group0;
+    c.groups(a, seat.col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of + g), dc_ld(a.rstd + of + g)); });
+    c.groups(a, seat.col, m1, m2, [&](int g) { return fin[g]; });
+    const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
+    const size_t at = (size_t)(p.col0 + seat.col) * VE * sizeof(T);
+    char* const dx = row_at(a.y, a.y_pitch, row0) + at;
+    each_two<2, typename W::Raw>(p, seat, row_at(a.x, a.x_pitch, row0) + at, a.x_pitch, row_at(a.dy, a.dy_pitch, row0) + at, a.dy_pitch,
+                                 [&](int r, typename W::Raw x, typename W::Raw dy) { *(typename W::Raw*)(dx + (size_t)r * a.y_pitch) = W::template gradient<ACT>(x, dy, c, mean, rstd, m1, m2); });
+}
+
+// ---------------------------------------------------------------------------
+// One launch: a slice of a map in the shared memory of a cluster, read once
+// ---------------------------------------------------------------------------
+constexpr int kMostResident = 256;                            // threads
+constexpr int kMostCluster = 8, kMostGroups = 64, kMostColumns = 64;       // CTAs to a slice; groups, columns of one
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// To the same place in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t place_in(const void* at, int rank)
+{
+    uint32_t to;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(at)), "r"(rank));
+    return to;
+}
+__device__ __forceinline__ void send(const float2* at, int rank, float2 v)
+{
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(place_in(at, rank)), "f"(v.x), "f"(v.y) : "memory");
+}
+__device__ __forceinline__ void send(const float* at, int rank, float v)
+{
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(place_in(at, rank)), "f"(v) : "memory");
+}
 __device__ __forceinline__ Place resident_place(const GroupArgs& a)
 {
     Place p;
@@ -513,122 +585,80 @@ __device__ __forceinline__ Place resident_place(const GroupArgs& a)
     p.group0 = blockIdx.y * a.gs; p.col0 = blockIdx.y * a.width; p.row0 = p.chunk * a.rows_per; p.rows = rows_of(a, p.chunk);
     return p;
 }
+// A thread's own values of a map into shared memory, one behind another for the threads; they are there once copies_done() has passed.
+template <typename Raw>
+__device__ __forceinline__ void keep_rows(const Place& p, const Seat& s, const char* x, size_t pitch, Raw* kept)
+{
+    if (s.turn >= s.turns) return;
+    Raw* to = kept + threadIdx.x;
+    const int line = s.turns * p.cols;
+    x += (size_t)s.turn * pitch;
+    const size_t step = (size_t)s.turns * pitch;
+    if constexpr (sizeof(Raw) == 16) {
+        uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+        for (int r = s.turn; r < p.rows; r += s.turns, at += 16u * line, x += step) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(x) : "memory");
+    } else {
+#pragma unroll 8
+        for (int r = s.turn; r < p.rows; r += s.turns, to += line, x += step) *to = *(const Raw*)x;
+    }
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__host__ __device__ constexpr size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
-// A CTA has rows_per rows of a slice; its cluster has the slice.  Each thread copies its own values into shared memory and reads them twice from there.  Distances are
-// taken from the group's first value in the CTA's first row, so that threads' sums just add up.
+// A CTA has rows_per rows of a slice; its cluster has the slice.  Each thread copies its own values into shared memory and reads them twice from there.
 template <typename T, int VE, bool ONE, int ACT>
 __global__ void __launch_bounds__(kMostResident) k_group_resident(const GroupArgs a)
 {
-    typedef Vec<T, VE> V;
-    typedef typename V::F F;
-    constexpr int P = V::P, IT = ONE ? 1 : VE, N = ONE ? 1 : P;
-    extern __shared__ uint4 kept[];                           // [rows_per][columns], then the partial sums
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    typedef typename W::Raw Raw;
+    extern __shared__ uint4 shared4[];                        // [rows_per][columns], then the partial sums
     __shared__ float2 exchange[kMostCluster][kMostGroups], fin[kMostGroups];
-    cluster_started(a.chunks > 1);
+    const bool cluster = a.chunks > 1;
+    cluster_started(cluster);
     dc_pdl_wait();
     dc_pdl_release();
     const Place p = resident_place(a);
-    int col, turn, turns;
-    seat(a, col, turn, turns);
+    const Seat seat = seat_of(a, p);
     const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
-    const size_t at = (size_t)(p.col0 + col) * 16;
-    const char* const x = row_at(a.x, a.x_pitch, row0) + at;
-    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(kept) + 16u * threadIdx.x, line = 16u * turns * p.cols;
-    if (turn < turns) {
-        uint32_t to = mine;
-        for (int r = turn; r < p.rows; r += turns, to += line) copy16(to, x + (size_t)r * a.x_pitch);
-    }
-    float* const part = (float*)(kept + (size_t)a.rows_per * p.cols);     // [rows of partial sums][sums, squares][items]
-    const int items = p.cols * IT;
+    const size_t at = (size_t)(p.col0 + seat.col) * VE * sizeof(T);
+    Raw* const kept = (Raw*)shared4;
+    keep_rows(p, seat, row_at(a.x, a.x_pitch, row0) + at, a.x_pitch, kept);
+    float* const part = (float*)((char*)shared4 + up16((size_t)a.rows_per * p.cols * sizeof(Raw)));      // [rows of partial sums][sums, squares][items]
     Column<T, VE, ONE> c;
-    c.weights(a, p, col);
-    F s[2 * N], first[N], unused[N];
-    if (p.rows > 0)
-        c.groups(a, p, col, first, unused, [&](int g) {
-            float v;
-            Vec<T, 1>::open(((const T*)row_at(a.x, a.x_pitch, row0))[(p.group0 + g) * a.per], &v);
-            return make_float2(-v, 0.f);
-        });
+    c.weights(a, p, seat.col);
+    F s[2 * W::N], first[W::N], unused[W::N];
+    if (p.rows > 0) c.groups(a, seat.col, first, unused, [&](int g) { return make_float2(-first_of<T>(a, p, row0, g), 0.f); });
 #pragma unroll
-    for (int k = 0; k < 2 * N; ++k) s[k] = both<F>(0.f);
+    for (int k = 0; k < 2 * W::N; ++k) s[k] = both<F>(0.f);
     copies_done();
-    if (turn < turns) {
-        const uint4* k4 = kept + threadIdx.x;
+    const int line = seat.turns * p.cols;
+    if (seat.turn < seat.turns) {
+        const Raw* k4 = kept + threadIdx.x;
 #pragma unroll 4
-        for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols) {
-            F d[P];
-            V::open(*(const typename V::Raw*)k4, d);
-#pragma unroll
-            for (int k = 0; k < P; ++k) {
-                const int i = ONE ? 0 : k;
-                const F t = add2(d[k], first[i]);
-                s[i] = add2(s[i], t);
-                s[N + i] = fma2(t, t, s[N + i]);
-            }
-        }
+        for (int r = seat.turn; r < p.rows; r += seat.turns, k4 += line) W::stats(*k4, first, s);
     }
-    const int left = fold(s, p.cols, turns), to = fold_row(p.cols, turn, turns);
-    if (to >= 0)
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            part[to * 2 * items + col * IT + i] = ONE ? sum_of(s[0]) : lane_of(s[ONE ? 0 : i / 2], i & 1);
-            part[(to * 2 + 1) * items + col * IT + i] = ONE ? sum_of(s[N]) : lane_of(s[N + (ONE ? 0 : i / 2)], i & 1);
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * items; i += blockDim.x) part[i] = rows_of_sums(part, left, 2 * items, i);       // (its own column alone)
-    __syncthreads();
-    cluster_wait(a.chunks > 1);
-    const int of = ONE && a.gs == p.cols ? 1 : items / p.ngroups;
-    for (int g = threadIdx.x >> 5; g < p.ngroups; g += blockDim.x >> 5) {
-        float sum = 0.f, squares = 0.f;
-        for (int i = g * of + (threadIdx.x & 31); i < (g + 1) * of; i += 32) { sum += part[i]; squares += part[items + i]; }
-        if (of > 1) { sum = reduce_lanes<Sum>(sum, 32); squares = reduce_lanes<Sum>(squares, 32); }
-        else { sum = __shfl_sync(0xffffffffu, sum, 0); squares = __shfl_sync(0xffffffffu, squares, 0); }
-        const float n = (float)p.rows * (float)a.per;
-        float2 r = make_float2(0.f, 0.f);
-        if (p.rows > 0) {
-            float v;
-            Vec<T, 1>::open(((const T*)row_at(a.x, a.x_pitch, row0))[(p.group0 + g) * a.per], &v);
-            const float m = sum / n;
-            r = make_float2(m + v, fmaxf(fmaf(-m, sum, squares), 0.f) + (sum - sum));
-        }
-        const int rank = threadIdx.x & 31;
-        if (rank < a.chunks) send(&exchange[p.chunk][g], rank, r);
-    }
-    if (a.chunks > 1) cluster_sync(); else __syncthreads();
+    finish_stats<T, VE, ONE>(a, p, seat, row0, s, part, cluster, [&](int g, float2 r, int sub, int lanes) {
+        for (int rank = sub; rank < a.chunks; rank += lanes) send(&exchange[p.chunk][g], rank, r);
+    });
+    if (cluster) cluster_sync(); else __syncthreads();
     if (threadIdx.x < p.ngroups) {
         const int g = threadIdx.x;
-        const float total = (float)a.pixels * (float)a.per;
-        float mean = 0.f, squares = 0.f;
-        for (int k = 0; k < a.chunks; ++k) mean = fmaf((float)rows_of(a, k) * (float)a.per, exchange[k][g].x, mean);
-        mean /= total;
-        for (int k = 0; k < a.chunks; ++k) {
-            const float2 v = exchange[k][g];
-            const float w = (float)rows_of(a, k) * (float)a.per, d = v.x - mean;
-            if (w > 0.f) squares += fmaf(w * d, d, v.y);
-        }
-        const float rstd = inverse_root(squares / total + a.eps);
-        fin[g] = make_float2(-mean, rstd);
+        const float2 r = join_parts(a.chunks, (float)a.pixels * (float)a.per, a.eps, 0, 1, [&](int i) { return (float)rows_of(a, i) * (float)a.per; }, [&](int i) { return exchange[i][g]; });
+        fin[g] = r;
         if (p.chunk == 0) {
-            if (a.mean) a.mean[(size_t)p.map * a.groups + p.group0 + g] = mean;
-            if (a.rstd) a.rstd[(size_t)p.map * a.groups + p.group0 + g] = rstd;
+            if (a.mean) a.mean[(size_t)p.map * a.groups + p.group0 + g] = -r.x;
+            if (a.rstd) a.rstd[(size_t)p.map * a.groups + p.group0 + g] = r.y;
         }
     }
     __syncthreads();
-    if (turn >= turns) return;
-    F mean[N], rstd[N];
-    c.groups(a, p, col, mean, rstd, [&](int g) { return fin[g]; });
-    char* y = row_at(a.y, a.y_pitch, row0 + turn) + at;
-    const uint4* k4 = kept + threadIdx.x;
+    if (seat.turn >= seat.turns) return;
+    F mean[W::N], rstd[W::N];
+    c.groups(a, seat.col, mean, rstd, [&](int g) { return fin[g]; });
+    char* y = row_at(a.y, a.y_pitch, row0 + seat.turn) + at;
+    const Raw* k4 = kept + threadIdx.x;
 #pragma unroll 4
-    for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols, y += turns * a.y_pitch) {
-        F d[P];
-        V::open(*(const typename V::Raw*)k4, d);
-#pragma unroll
-        for (int k = 0; k < P; ++k) d[k] = affine(hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]), c.g[k], c.b[k]);
-        activate<ACT, ONE>(d);
-        *(typename V::Raw*)y = V::close(d);
-    }
+    for (int r = seat.turn; r < p.rows; r += seat.turns, k4 += line, y += seat.turns * a.y_pitch) *(Raw*)y = W::template apply<ACT>(*k4, c, mean, rstd);
 }
 
 // The gradients likewise: x and dy are kept (behind a ReLU dy or zero, which is as exact).  SiLU's derivative is worked out twice: 32 maps of 56 x 56 x 256 bf16 55 us; with dz
@@ -636,80 +666,49 @@ __global__ void __launch_bounds__(kMostResident) k_group_resident(const GroupArg
 template <typename T, int VE, bool ONE, int ACT>
 __global__ void __launch_bounds__(kMostResident, ONE ? 4 : 2) k_group_back_resident(const GroupArgs a)
 {
-    typedef Vec<T, VE> V;
-    typedef typename V::F F;
-    constexpr int P = V::P, N = ONE ? 1 : P;
-    extern __shared__ uint4 kept[];                           // [2][rows_per][columns], then the partial sums
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    typedef typename W::Raw Raw;
+    extern __shared__ uint4 shared4[];                        // [2][rows_per][columns], then the partial sums
     __shared__ float2 exchange[kMostCluster][kMostGroups], fin[kMostGroups];
-    cluster_started(a.chunks > 1);
+    const bool cluster = a.chunks > 1;
+    cluster_started(cluster);
     dc_pdl_wait();
     dc_pdl_release();
     const Place p = resident_place(a);
-    const int wide = p.cols * VE;
-    int col, turn, turns;
-    seat(a, col, turn, turns);
+    const Seat seat = seat_of(a, p);
+    const int wide = p.cols * VE, line = seat.turns * p.cols;
     const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
-    const size_t at = (size_t)(p.col0 + col) * 16;
-    const char *const x = row_at(a.x, a.x_pitch, row0) + at, *const dy = row_at(a.dy, a.dy_pitch, row0) + at;
-    const uint32_t mine = (uint32_t)__cvta_generic_to_shared(kept) + 16u * threadIdx.x, line = 16u * turns * p.cols, other = 16u * a.rows_per * p.cols;
-    if (turn < turns) {
-        uint32_t to = mine;
-        for (int r = turn; r < p.rows; r += turns, to += line) { copy16(to, x + (size_t)r * a.x_pitch); copy16(to + other, dy + (size_t)r * a.dy_pitch); }
-    }
-    float* const part = (float*)(kept + 2 * (size_t)a.rows_per * p.cols);     // [rows of partial sums][2][channels]
+    const size_t at = (size_t)(p.col0 + seat.col) * VE * sizeof(T), half = up16((size_t)a.rows_per * p.cols * sizeof(Raw));
+    Raw *const kept = (Raw*)shared4, *const kept_dy = (Raw*)((char*)shared4 + half);
+    keep_rows(p, seat, row_at(a.x, a.x_pitch, row0) + at, a.x_pitch, kept);
+    keep_rows(p, seat, row_at(a.dy, a.dy_pitch, row0) + at, a.dy_pitch, kept_dy);
+    float* const part = (float*)((char*)shared4 + 2 * half);             // [rows of partial sums][2][channels]
     Column<T, VE, ONE> c;
-    c.weights(a, p, col);
-    F mean[N], rstd[N], s[2 * P];
+    c.weights(a, p, seat.col);
+    F mean[W::N], rstd[W::N], s[2 * W::P];
     const size_t of_map = (size_t)p.map * a.groups + p.group0;
-    c.groups(a, p, col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of_map + g), dc_ld(a.rstd + of_map + g)); });
+    c.groups(a, seat.col, mean, rstd, [&](int g) { return make_float2(-dc_ld(a.mean + of_map + g), dc_ld(a.rstd + of_map + g)); });
 #pragma unroll
-    for (int k = 0; k < 2 * P; ++k) s[k] = both<F>(0.f);
+    for (int k = 0; k < 2 * W::P; ++k) s[k] = both<F>(0.f);
     copies_done();
-    const size_t half = (size_t)a.rows_per * p.cols;
-    if (turn < turns) {
-        uint4* k4 = kept + threadIdx.x;
+    if (seat.turn < seat.turns) {
+        const Raw* x = kept + threadIdx.x;
+        Raw* dy = kept_dy + threadIdx.x;
 #pragma unroll 2
-        for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols) {
-            F d[P], e[P], z[P];
-            V::open(*(const typename V::Raw*)k4, d);
-            V::open(*(const typename V::Raw*)(k4 + half), e);
-#pragma unroll
-            for (int k = 0; k < P; ++k) { d[k] = hat(d[k], mean[ONE ? 0 : k], rstd[ONE ? 0 : k]); z[k] = affine(d[k], c.g[k], c.b[k]); }
-            activate_back<ACT, ONE>(e, z);
-#pragma unroll
-            for (int k = 0; k < P; ++k) { s[k] = add2(s[k], e[k]); s[P + k] = fma2(e[k], d[k], s[P + k]); }
-            if (ACT == DC_ACT_RELU) *(typename V::Raw*)(k4 + half) = V::close(e);           // dy or zero: as exact as it came
-        }
+        for (int r = seat.turn; r < p.rows; r += seat.turns, x += line, dy += line) W::template sums<ACT>(*x, *dy, c, mean, rstd, s, dy);
     }
-    const int left = fold(s, p.cols, turns), to = fold_row(p.cols, turn, turns);
-    if (to >= 0)
-#pragma unroll
-        for (int i = 0; i < VE; ++i) {
-            part[to * 2 * wide + col * VE + i] = lane_of(s[i / 2], i & 1);
-            part[(to * 2 + 1) * wide + col * VE + i] = lane_of(s[P + i / 2], i & 1);
-        }
-    float* const sums_of_all = part + (size_t)left * 2 * wide;               // [chunks][2][channels]: of a single map, in the first CTA
-    __syncthreads();
-    cluster_wait(a.chunks > 1);
-    for (int i = threadIdx.x; i < 2 * wide; i += blockDim.x) {
-        const float t = rows_of_sums(part, left, 2 * wide, i);
-        part[i] = t;                                          // (its own column alone)
-        if (a.dgamma || a.dbeta) send(sums_of_all + p.chunk * 2 * wide + i, 0, t);
-        else if (a.sums) a.sums[((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + (i < wide ? p.col0 * VE + i : a.channels + p.col0 * VE + i - wide)] = t;
-    }
-    __syncthreads();
-    const int of = wide / p.ngroups;
-    for (int g = threadIdx.x >> 5; g < p.ngroups; g += blockDim.x >> 5) {
-        float t1 = 0.f, t2 = 0.f;
-        for (int i = g * of + (threadIdx.x & 31); i < (g + 1) * of; i += 32) {
-            const float w = a.gamma ? dc_ld(a.gamma + p.col0 * VE + i) : 1.f;
-            t1 = fmaf(w, part[i], t1); t2 = fmaf(w, part[wide + i], t2);
-        }
-        t1 = reduce_lanes<Sum>(t1, 32); t2 = reduce_lanes<Sum>(t2, 32);
-        const int rank = threadIdx.x & 31;
-        if (rank < a.chunks) send(&exchange[p.chunk][g], rank, make_float2(t1, t2));
-    }
-    if (a.chunks > 1) cluster_sync(); else __syncthreads();
+    const int left = folds(p.cols) ? (int)blockDim.x >> 5 : seat.turns;
+    float* const sums_of_all = part + (size_t)left * 2 * wide;           // [chunks][2][channels]: of a single map, in the first CTA
+    finish_sums<VE>(a, p, seat, s, part, cluster,
+        [&](int i, float t) {
+            if (a.dgamma || a.dbeta) send(sums_of_all + p.chunk * 2 * wide + i, 0, t);
+            else if (a.sums) a.sums[((size_t)p.map * a.chunks + p.chunk) * 2 * a.channels + (i < wide ? p.col0 * VE + i : a.channels + p.col0 * VE + i - wide)] = t;
+        },
+        [&](int g, float2 r, int sub, int lanes) {
+            for (int rank = sub; rank < a.chunks; rank += lanes) send(&exchange[p.chunk][g], rank, r);
+        });
+    if (cluster) cluster_sync(); else __syncthreads();
     if ((a.dgamma || a.dbeta) && p.chunk == 0)
         for (int i = threadIdx.x; i < 2 * wide; i += blockDim.x) {
             const float t = rows_of_sums(sums_of_all, a.chunks, 2 * wide, i);
@@ -725,30 +724,14 @@ __global__ void __launch_bounds__(kMostResident, ONE ? 4 : 2) k_group_back_resid
         fin[threadIdx.x] = make_float2(-t1 / total, -t2 / total);
     }
     __syncthreads();
-    if (turn >= turns) return;
-    F m1[N], m2[N];
-    c.groups(a, p, col, m1, m2, [&](int g) { return fin[g]; });
-    char* dx = row_at(a.y, a.y_pitch, row0 + turn) + at;
-    const uint4* k4 = kept + threadIdx.x;
+    if (seat.turn >= seat.turns) return;
+    F m1[W::N], m2[W::N];
+    c.groups(a, seat.col, m1, m2, [&](int g) { return fin[g]; });
+    char* dx = row_at(a.y, a.y_pitch, row0 + seat.turn) + at;
+    const Raw *x = kept + threadIdx.x, *dy = kept_dy + threadIdx.x;
+    constexpr int LEFT = ACT == DC_ACT_RELU ? DC_ACT_NONE : ACT;         // of the activation, behind the first half
 #pragma unroll 2
-    for (int r = turn; r < p.rows; r += turns, k4 += turns * p.cols, dx += turns * a.y_pitch) {
-        F d[P], e[P], z[P];
-        V::open(*(const typename V::Raw*)k4, d);
-        V::open(*(const typename V::Raw*)(k4 + half), e);
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int i = ONE ? 0 : k;
-            d[k] = hat(d[k], mean[i], rstd[i]);
-            z[k] = affine(d[k], c.g[k], c.b[k]);
-        }
-        if (ACT == DC_ACT_SILU) activate_back<ACT, ONE>(e, z);
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int i = ONE ? 0 : k;
-            d[k] = mul2(fma2(d[k], m2[i], add2(mul2(e[k], c.g[k]), m1[i])), rstd[i]);
-        }
-        *(typename V::Raw*)dx = V::close(d);
-    }
+    for (int r = seat.turn; r < p.rows; r += seat.turns, x += line, dy += line, dx += seat.turns * a.y_pitch) *(Raw*)dx = W::template gradient<LEFT>(*x, *dy, c, mean, rstd, m1, m2);
 }
 
 // dgamma and dbeta: the sums of all maps and chunks, 32 threads per column, in a fixed order.
@@ -786,7 +769,7 @@ int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return 
 size_t part_bytes(int64_t maps, int chunks, int channels, int groups) { return ((size_t)maps * chunks * ((size_t)groups + channels / kThreads + 1) * sizeof(float2) + 255) / 256 * 256; }
 
 // Columns of VE channels: whole groups to a slice, as many as a CTA has threads for; or a wide group in pieces.  False: VE does not go.
-bool plan_columns(GroupArgs& a, int ve)
+bool plan_columns(GroupArgs& a, int ve, int elt)
 {
     const int least = a.per / gcd(a.per, ve);                  // columns that whole groups take at least
     a.pieces = 1;
@@ -806,42 +789,47 @@ bool plan_columns(GroupArgs& a, int ve)
     const int units = a.groups / unit;
     int best = 1;
     for (int j = 1; j <= units; ++j)
-        if (units % j == 0 && j * least <= kThreads && (j == 1 || (j - 1) * least * ve < 64)) best = j;   // columns of 64 channels or so
+        if (units % j == 0 && j * least <= kThreads && best * least * ve * elt < 64) best = j;             // 64 bytes of a row or more
     a.gs = best * unit; a.width = best * least; a.slices = units / best;
+    if (a.width <= kMostColumns) {
+        a.by_width = dc_div_up(65536, a.width);
+        a.by_per = a.per <= 128 ? dc_div_up(65536, a.per) : 0;
+    }
     return true;
 }
 
 // A slice in the shared memory of a cluster, if it fits: columns of 64 bytes a row (fewer where it does not), CTAs of up to 56 KB, four to an SM, so that some load while others compute
 // and store, or as many as a cluster has, or larger ones; 256 threads, or 128 where those would have fewer than four vectors each.  32 maps of 56 x 56 x 256 bf16, SiLU, us: forward 28.9
-// (columns of 32 bytes 34.2, of 128 34.6; 25 KB 30.5, 100 KB 40), gradients 55.1 (60.5, 61; 100 KB and more 80).
-constexpr int kWantKept = 56 * 1024, kMostKept = 200 * 1024;
-bool plan_resident(GroupArgs& a, int ve, int planes, int num_sms, int* block, size_t* smem)
+// (columns of 32 bytes 34.2, of 128 34.6; 25 KB 30.5, 100 KB 40), gradients 55.1 (60.5, 61; 100 KB and more 80).  Large CTAs that do not even fill the SMs leave the map to two launches
+// with more of them: 16629 x 32, one map, 12.6 us and 9.1; 9273 x 32 8.6 and 8.0, 8 x 12544 x 64 16.7 and 21.4, 7241 x 320 10.7 and 16.8.
+constexpr int kWantKept = 56 * 1024, kMostKept = 200 * 1024, kFewKept = 120 * 1024;
+bool plan_resident(GroupArgs& a, int ve, int elt, int planes, int num_sms, int* block, size_t* smem)
 {
-    const int least = a.per / gcd(a.per, ve), unit = least * ve / a.per, bytes = 16 * planes;
-    if (a.channels % ve || a.groups % unit || least > 16 || a.maps > 65535) return false;
+    const int least = a.per / gcd(a.per, ve), unit = least * ve / a.per, column = ve * elt, bytes = column * planes;
+    if (a.channels % ve || a.groups % unit || least > kMostColumns || a.maps > 65535) return false;
     const int units = a.groups / unit;
     int best = 0;
-    for (int j = 1; j <= units && j * least <= 16; ++j) {
+    for (int j = 1; j <= units && j * least <= kMostColumns; ++j) {
         if (units % j || j * unit > kMostGroups) continue;
         if ((int64_t)a.pixels * j * least * bytes > (int64_t)kMostCluster * kMostKept) break;
         best = j;
-        if (j * least >= 4) break;
+        if (j * least * column >= 64) break;
     }
-    if (!best) return false;
+    if (!best || (int64_t)units / best > 65535) return false;
     a.pieces = 1; a.gs = best * unit; a.width = best * least; a.slices = units / best;
     const int64_t slice = (int64_t)a.pixels * a.width * bytes;
     int turns = kMostResident / a.width;
-    a.by_width = dc_div_up(65536, a.width); a.by_per = dc_div_up(65536, a.per);
+    a.by_width = dc_div_up(65536, a.width); a.by_per = a.per <= 128 ? dc_div_up(65536, a.per) : 0;
     int cs = 1;
     while (cs < kMostCluster && (slice > (int64_t)cs * kWantKept || ((int64_t)a.maps * a.slices * cs < num_sms && a.pixels >= 4 * cs * turns))) cs *= 2;
-    if (cs > most_chunks(a.maps, a.pixels)) return false;
+    if (cs > most_chunks(a.maps, a.pixels) || (slice > (int64_t)cs * kFewKept * planes && (int64_t)a.maps * a.slices * cs < num_sms)) return false;
     a.rows_per = dc_div_up(a.pixels, cs);
     a.chunks = cs;
     const int threads = (int64_t)a.rows_per * a.width >= 4 * kMostResident ? kMostResident : kMostResident / 2;
     turns = threads / a.width;
-    const int left = a.width & (a.width - 1) ? turns : threads / 32;
+    const int left = a.width > 32 || a.width & (a.width - 1) ? turns : threads / 32;
     *block = threads;
-    *smem = (size_t)a.rows_per * a.width * bytes + (size_t)(left + (a.dgamma || a.dbeta ? cs : 0)) * 2 * a.width * ve * sizeof(float);
+    *smem = planes * up16((size_t)a.rows_per * a.width * column) + (size_t)(left + (a.dgamma || a.dbeta ? cs : 0)) * 2 * a.width * ve * sizeof(float);
     return *smem <= (size_t)kMostKept + 16 * 1024;
 }
 
@@ -866,17 +854,14 @@ cudaError_t launch_resident(const GroupArgs& a, bool back, int block, size_t sme
 template <typename T, int VE, bool ONE, int ACT>
 cudaError_t launch_group(GroupArgs& a, bool back, int device, int num_sms, cudaStream_t stream)
 {
-    if constexpr (VE > 1) {
-        GroupArgs r = a;
-        size_t smem = 0;
-        int block = 0;
-        const int planes = back ? 2 : 1;                      // 16 bytes that are kept of a column's row: x, and dy
-        if (a.maps > 1) r.dgamma = r.dbeta = nullptr;
-        if (plan_resident(r, VE, planes, num_sms, &block, &smem)) {
-            a.joined = r.dgamma || r.dbeta;
-            a.chunks = r.chunks;                              // (for the join of the sums)
-            return launch_resident<T, VE, ONE, ACT>(r, back, block, smem, device, stream);
-        }
+    GroupArgs r = a;
+    size_t smem = 0;
+    int block = 0;
+    if (a.maps > 1) r.dgamma = r.dbeta = nullptr;
+    if (plan_resident(r, VE, (int)sizeof(T), back ? 2 : 1, num_sms, &block, &smem)) {      // kept: x, and dy
+        a.joined = r.dgamma || r.dbeta;
+        a.chunks = r.chunks;                                  // (for the join of the sums)
+        return launch_resident<T, VE, ONE, ACT>(r, back, block, smem, device, stream);
     }
     const dim3 grid((unsigned)((int64_t)a.maps * a.slices * a.chunks));
     if (!back) {
@@ -909,8 +894,8 @@ int launch(GroupArgs& a, bool back, int activation, int dtype, cudaStream_t stre
     if (rc != DC_OK) return rc;
     auto aligned = [](const void* p, size_t pitch) { return (uintptr_t)p % 16 == 0 && pitch % 16 == 0; };
     const bool rows = (int64_t)a.maps * a.pixels > 1;
-    const bool vec = aligned(a.x, rows ? a.x_pitch : 0) && (!a.y || aligned(a.y, rows ? a.y_pitch : 0)) && (!back || aligned(a.dy, rows ? a.dy_pitch : 0)) && plan_columns(a, ve);
-    if (!vec) plan_columns(a, 1);
+    const bool vec = aligned(a.x, rows ? a.x_pitch : 0) && (!a.y || aligned(a.y, rows ? a.y_pitch : 0)) && (!back || aligned(a.dy, rows ? a.dy_pitch : 0)) && plan_columns(a, ve, elt);
+    if (!vec) plan_columns(a, 1, elt);
     const int most = most_chunks(a.maps, a.pixels), turns = kThreads / a.width;
     a.chunks = dc_div_up(a.pixels, 4 * turns);
     if (a.chunks > most) a.chunks = most;
