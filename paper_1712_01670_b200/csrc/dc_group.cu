@@ -6,7 +6,7 @@
 // What bounds them: memory, one read and one write of the map (two reads and a write for the gradients).
 //
 // A slice is the columns of a map that a CTA works on: some whole groups, or a piece of one that is wider than a CTA.  A thread has one column (16 bytes of
-// each of its rows, or one element where rows are not aligned to 16 bytes) and so one set of weights and of sums.
+// each of its rows, or two elements or one where rows are not aligned to 16 bytes) and so one set of weights and of sums.
 //
 // Sums of squares: a CTA takes its values' distances from one of them (the group's first in its first row), so that no distance is beyond the group's range, whatever the mean is, and
 // threads' sums just add up; CTAs' means and squares are then joined by M2 = sum M2_i + sum n_i (mean_i - mean)^2, in a fixed order: equal calls give equal bits.
@@ -15,6 +15,20 @@
 #include "dc_quantise.cuh"
 
 namespace {
+
+// Two elements of a row, where it does not lie on 16 bytes.
+template <> struct Vec<float, 2> {
+    typedef float2 Raw; typedef float2 F;
+    static constexpr int P = 1;
+    static __device__ __forceinline__ void open(Raw t, float2* v) { v[0] = t; }
+    static __device__ __forceinline__ Raw close(const float2* v) { return v[0]; }
+};
+template <> struct Vec<__nv_bfloat16, 2> {
+    typedef uint32_t Raw; typedef float2 F;
+    static constexpr int P = 1;
+    static __device__ __forceinline__ void open(Raw t, float2* v) { v[0] = make_float2(__uint_as_float(t << 16), __uint_as_float(t & 0xffff0000u)); }
+    static __device__ __forceinline__ Raw close(const float2* v) { const __nv_bfloat162 t = __floats2bfloat162_rn(v[0].x, v[0].y); return *(const uint32_t*)&t; }
+};
 
 constexpr int kThreads = 256;
 constexpr int kMostChunks = 128;
@@ -71,25 +85,27 @@ __device__ __forceinline__ float reciprocal(float v)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// Of four values: an exponential each and, JOINT, one reciprocal for all, 1 / a = bcd / abcd (the unit for both gives 16 results a cycle); where abcd is beyond a number's
+// Of four values (or two): an exponential each and, JOINT, one reciprocal for all, 1 / a = bcd / abcd (the unit for both gives 16 results a cycle); where abcd is beyond a number's
 // range, or none, each has its own.  Not JOINT: a value's result depends on no other.
-template <bool JOINT>
+template <bool JOINT, int STEP>
 __device__ __forceinline__ void sigmoids(const float2* z, float2* p)
 {
-    const float2 a = make_float2(one_and_exp(z[0].x), one_and_exp(z[0].y)), c = make_float2(one_and_exp(z[1].x), one_and_exp(z[1].y));
+    float2 a[STEP];
+#pragma unroll
+    for (int h = 0; h < STEP; ++h) a[h] = make_float2(one_and_exp(z[h].x), one_and_exp(z[h].y));
     if (JOINT) {
-        const float ab = a.x * a.y, cd = c.x * c.y, t = ab * cd;
+        const float ab = a[0].x * a[0].y, cd = STEP > 1 ? a[STEP - 1].x * a[STEP - 1].y : 1.f, t = ab * cd;
         if (t < 1e37f) {
             const float r = reciprocal(t);
-            p[0] = mul2(both<float2>(r * cd), make_float2(a.y, a.x));
-            p[1] = mul2(both<float2>(r * ab), make_float2(c.y, c.x));
+            p[0] = mul2(both<float2>(STEP > 1 ? r * cd : r), make_float2(a[0].y, a[0].x));
+            if (STEP > 1) p[STEP - 1] = mul2(both<float2>(r * ab), make_float2(a[STEP - 1].y, a[STEP - 1].x));
             return;
         }
     }
-    p[0] = make_float2(reciprocal(a.x), reciprocal(a.y));
-    p[1] = make_float2(reciprocal(c.x), reciprocal(c.y));
+#pragma unroll
+    for (int h = 0; h < STEP; ++h) p[h] = make_float2(reciprocal(a[h].x), reciprocal(a[h].y));
 }
-template <bool JOINT> __device__ __forceinline__ void sigmoids(const float* z, float* p) { p[0] = reciprocal(one_and_exp(z[0])); }
+template <bool JOINT, int STEP> __device__ __forceinline__ void sigmoids(const float* z, float* p) { p[0] = reciprocal(one_and_exp(z[0])); }
 
 __device__ __forceinline__ float positive(float z) { asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(z)); return z; }
 __device__ __forceinline__ float2 positive(float2 z) { return make_float2(positive(z.x), positive(z.y)); }
@@ -104,7 +120,7 @@ __device__ __forceinline__ void activate(F (&z)[P])
     for (int k = 0; k < P; k += STEP) {
         if (ACT == DC_ACT_SILU) {
             F p[STEP];
-            sigmoids<JOINT>(z + k, p);
+            sigmoids<JOINT, STEP>(z + k, p);
 #pragma unroll
             for (int h = 0; h < STEP; ++h) z[k + h] = mul2(z[k + h], p[h]);
         } else if (ACT == DC_ACT_RELU)
@@ -120,7 +136,7 @@ __device__ __forceinline__ void activate_back(F (&dy)[P], const F (&z)[P])
     for (int k = 0; k < P; k += STEP) {
         if (ACT == DC_ACT_SILU) {
             F p[STEP];
-            sigmoids<JOINT>(z + k, p);
+            sigmoids<JOINT, STEP>(z + k, p);
 #pragma unroll
             for (int h = 0; h < STEP; ++h) {
                 const F zp = mul2(z[k + h], p[h]);                               // p (1 + z (1 - p)) = p + zp - zp p
@@ -166,7 +182,7 @@ template <typename T, int VE, bool ONE> struct Column {
     __device__ __forceinline__ void weights(const GroupArgs& a, const Place& p, int col)
     {
         const int c = (p.col0 + col) * VE;
-        if constexpr (VE > 1)
+        if constexpr (VE > 2)
             if ((((uintptr_t)a.gamma | (uintptr_t)a.beta) & 15) == 0) {
                 load_weights(a.gamma, c, 1.f, g);
                 load_weights(a.beta, c, 0.f, b);
@@ -594,9 +610,11 @@ __device__ __forceinline__ void keep_rows(const Place& p, const Seat& s, const c
     const int line = s.turns * p.cols;
     x += (size_t)s.turn * pitch;
     const size_t step = (size_t)s.turns * pitch;
-    if constexpr (sizeof(Raw) == 16) {
+    if constexpr (sizeof(Raw) >= 4) {
         uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
-        for (int r = s.turn; r < p.rows; r += s.turns, at += 16u * line, x += step) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(x) : "memory");
+        for (int r = s.turn; r < p.rows; r += s.turns, at += (uint32_t)sizeof(Raw) * line, x += step)
+            if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(x) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(x), "n"((int)sizeof(Raw)) : "memory");
     } else {
 #pragma unroll 8
         for (int r = s.turn; r < p.rows; r += s.turns, to += line, x += step) *to = *(const Raw*)x;
@@ -880,7 +898,7 @@ cudaError_t launch_group_as(GroupArgs& a, bool back, int activation, int device,
     case DC_ACT_SILU: return launch_group<T, VE, ONE, DC_ACT_SILU>(a, back, device, num_sms, stream); \
     default: return launch_group<T, VE, ONE, DC_ACT_NONE>(a, back, device, num_sms, stream); \
     }
-    if constexpr (VE > 1)
+    if constexpr (VE > 2)
         if (a.per % VE) { DC_GROUP(false) }
     DC_GROUP(true)
 #undef DC_GROUP
@@ -892,18 +910,30 @@ int launch(GroupArgs& a, bool back, int activation, int dtype, cudaStream_t stre
     int device = 0, sms = 0;
     const int rc = dc_current_device(&device, &sms);
     if (rc != DC_OK) return rc;
-    auto aligned = [](const void* p, size_t pitch) { return (uintptr_t)p % 16 == 0 && pitch % 16 == 0; };
     const bool rows = (int64_t)a.maps * a.pixels > 1;
-    const bool vec = aligned(a.x, rows ? a.x_pitch : 0) && (!a.y || aligned(a.y, rows ? a.y_pitch : 0)) && (!back || aligned(a.dy, rows ? a.dy_pitch : 0)) && plan_columns(a, ve, elt);
-    if (!vec) plan_columns(a, 1, elt);
+    auto aligned = [&](size_t by) {
+        auto one = [&](const void* p, size_t pitch) { return (uintptr_t)p % by == 0 && (!rows || pitch % by == 0); };
+        return one(a.x, a.x_pitch) && (!a.y || one(a.y, a.y_pitch)) && (!back || one(a.dy, a.dy_pitch));
+    };
+    // 16 bytes of a row to a thread, or two elements of one group, or one
+    const int at_once = aligned(16) && plan_columns(a, ve, elt) ? ve : aligned(2 * elt) && a.per % 2 == 0 && plan_columns(a, 2, elt) ? 2 : 1;
+    if (at_once == 1) plan_columns(a, 1, elt);
     const int most = most_chunks(a.maps, a.pixels), turns = kThreads / a.width;
-    a.chunks = dc_div_up(a.pixels, 4 * turns);
+    // Eight CTAs to an SM with 16 rows to a thread or more (what a CTA does but once would outweigh the work of more), or two with four or more; at most 64.
+    const int64_t units = (int64_t)a.maps * a.slices;
+    auto of = [&](int rows, int per_sm) { const int64_t c = dc_div_up(a.pixels, rows * turns), w = (per_sm * (int64_t)sms + units - 1) / units; return (int)(c < w ? c : w); };
+    a.chunks = of(4, 2) > of(16, 8) ? of(4, 2) : of(16, 8);
+    if (a.chunks < dc_div_up(a.pixels, 64 * turns)) a.chunks = dc_div_up(a.pixels, 64 * turns);
     if (a.chunks > most) a.chunks = most;
     a.rows_per = dc_div_up(a.pixels, a.chunks);
     a.chunks = dc_div_up(a.pixels, a.rows_per);
     if ((int64_t)a.maps * a.slices * a.chunks > 0x7fffffff) return DC_ERR_LIMIT;
-    if (dtype == DC_BF16) DC_CUDA(vec ? (launch_group_as<__nv_bfloat16, 8>(a, back, activation, device, sms, stream)) : (launch_group_as<__nv_bfloat16, 1>(a, back, activation, device, sms, stream)));
-    else DC_CUDA(vec ? (launch_group_as<float, 4>(a, back, activation, device, sms, stream)) : (launch_group_as<float, 1>(a, back, activation, device, sms, stream)));
+#define DC_GROUP(T, VE) DC_CUDA((launch_group_as<T, VE>(a, back, activation, device, sms, stream)))
+    if (dtype == DC_BF16) { if (at_once == 8) DC_GROUP(__nv_bfloat16, 8); else if (at_once == 2) DC_GROUP(__nv_bfloat16, 2); else DC_GROUP(__nv_bfloat16, 1); }
+    else if (at_once == 4) DC_GROUP(float, 4);
+    else if (at_once == 2) DC_GROUP(float, 2);
+    else DC_GROUP(float, 1);
+#undef DC_GROUP
     return DC_OK;
 }
 
