@@ -401,7 +401,8 @@ typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_SILU = 2 } dc_activation
  *   workspace_dev         dc_group_norm_workspace bytes, any alignment, apart from all else; its content does not matter before or after the call;
  *                         two calls that may overlap need one each.  Not needed for no rows.
  * y_dev may be x_dev with the same pitch.  eps >= 0.  A group of an image with a NaN or an infinity becomes NaN (with ReLU too), no other one changes; sums and squares are float32,
- * so values beyond 1e18 or so have no meaningful result.  Equal calls give equal bits; one whose pointers or pitches are aligned otherwise adds up in another order.
+ * so values beyond 1e18 or so have no meaningful result.  Equal calls give equal bits; one whose
+ * pointers or pitches are aligned otherwise, on a device of another size too, adds up in another order.
  * DC_ERR_CONFIG: activation; DC_ERR_LIMIT: more than 16384 channels, maps * groups beyond 2^27 or so many small images that a grid cannot hold them. */
 int dc_group_norm(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t maps, int64_t pixels, int32_t channels,
                   int32_t groups, double eps, int32_t activation, int32_t dtype, void* y_dev, size_t y_pitch, float* mean_dev, float* rstd_dev,
@@ -429,7 +430,8 @@ int dc_group_norm_backward(const void* dy_dev, size_t dy_pitch, const void* x_de
  *   qt_dev [channels][qt_pitch], scale_t_dev float32 [ceil(channels / block_rows)][ceil(rows / 128)]: the same of x turned; both NULL: not wanted
  * The scale is the smallest power of two, and not below 2^-126, that takes the block's largest value to 448 or below: x / scale is exact, and q is the value next to it
  * (halves to even).  A block of zeros has the scale 0.  A block with a NaN or an infinity gets the scale NaN and zeros.
- * q_dev, qt_dev: 16-byte aligned, pitches multiples of 16; what lies between a row's end and the next row is not written.  DC_ERR_CONFIG: block_rows. */
+ * q_dev, qt_dev: 16-byte aligned, pitches multiples of 16; what lies between a row's end and the next row is not written.  DC_ERR_CONFIG: block_rows;
+ * DC_ERR_LIMIT: more than 2^28 channels, or so many blocks that a grid cannot hold them. */
 int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t channels, int32_t dtype, int32_t block_rows,
                        uint8_t* q_dev, size_t q_pitch, float* scale_dev, uint8_t* qt_dev, size_t qt_pitch, float* scale_t_dev, void* cuda_stream);
 
@@ -442,7 +444,7 @@ int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t 
  * (which leaves a NaN).  The order of the blocks' sum depends on m, n, k and the device alone.  Every wait inside the kernels is bounded; should one run out (2 s), the results that it
  * concerns are NaN.
  * The gradients of out = x wT: dx = dy w is this product with dc_quantize_blocks' dy and the turned weights, dw = dyT x that of both turned (b_block_rows 1).
- * DC_ERR_LIMIT: n > 2^28.  DC_ERR_CONFIG: b_block_rows. */
+ * DC_ERR_LIMIT: n or k > 2^28.  DC_ERR_CONFIG: b_block_rows. */
 int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_dev, const uint8_t* b_dev, size_t b_pitch, const float* b_scale_dev,
                      int32_t b_block_rows, const float* bias_dev, int64_t m, int32_t n, int32_t k, int32_t relu, int32_t dtype,
                      void* out_dev, size_t out_pitch, void* cuda_stream);

@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(kThreads) k_group_back_apply(const GroupArgs a
 // ---------------------------------------------------------------------------
 // One launch: a slice of a map in the shared memory of a cluster, read once
 // ---------------------------------------------------------------------------
-constexpr int kMostResident = 256;                            // threads
+constexpr int kMostResident = 512;                            // threads
 constexpr int kMostCluster = 8, kMostGroups = 64, kMostColumns = 64;       // CTAs to a slice; groups, columns of one
 
 __device__ __forceinline__ void cluster_sync()
@@ -625,7 +625,7 @@ __host__ __device__ constexpr size_t up16(size_t n) { return (n + 15) / 16 * 16;
 
 // A CTA has rows_per rows of a slice; its cluster has the slice.  Each thread copies its own values into shared memory and reads them twice from there.
 template <typename T, int VE, bool ONE, int ACT>
-__global__ void __launch_bounds__(kMostResident) k_group_resident(const GroupArgs a)
+__global__ void __launch_bounds__(kMostResident, ONE ? 2 : 1) k_group_resident(const GroupArgs a)
 {
     typedef Work<T, VE, ONE> W;
     typedef typename W::F F;
@@ -682,7 +682,7 @@ __global__ void __launch_bounds__(kMostResident) k_group_resident(const GroupArg
 // The gradients likewise: x and dy are kept (behind a ReLU dy or zero, which is as exact).  SiLU's derivative is worked out twice: 32 maps of 56 x 56 x 256 bf16 55 us; with dz
 // kept as floats, which leaves an SM two CTAs in the place of four, 61.
 template <typename T, int VE, bool ONE, int ACT>
-__global__ void __launch_bounds__(kMostResident, ONE ? 4 : 2) k_group_back_resident(const GroupArgs a)
+__global__ void __launch_bounds__(kMostResident, ONE ? 2 : 1) k_group_back_resident(const GroupArgs a)
 {
     typedef Work<T, VE, ONE> W;
     typedef typename W::F F;
@@ -816,11 +816,11 @@ bool plan_columns(GroupArgs& a, int ve, int elt)
     return true;
 }
 
-// A slice in the shared memory of a cluster, if it fits: columns of 64 bytes a row (fewer where it does not), CTAs of up to 56 KB, four to an SM, so that some load while others compute
-// and store, or as many as a cluster has, or larger ones; 256 threads, or 128 where those would have fewer than four vectors each.  32 maps of 56 x 56 x 256 bf16, SiLU, us: forward 28.9
-// (columns of 32 bytes 34.2, of 128 34.6; 25 KB 30.5, 100 KB 40), gradients 55.1 (60.5, 61; 100 KB and more 80).  Large CTAs that do not even fill the SMs leave the map to two launches
-// with more of them: 16629 x 32, one map, 12.6 us and 9.1; 9273 x 32 8.6 and 8.0, 8 x 12544 x 64 16.7 and 21.4, 7241 x 320 10.7 and 16.8.
-constexpr int kWantKept = 56 * 1024, kMostKept = 200 * 1024, kFewKept = 120 * 1024;
+// A slice in the shared memory of a cluster, if it fits: columns of 64 bytes a row, CTAs of up to 56 KB, four to an SM, so that some load while others compute
+// and store, or as many as a cluster has, or larger ones; 256 threads, 128 where those would have fewer than four vectors each, 512 in CTAs of more than 110 KB (8 x 12544 x 250 in 5 groups 57 us and 72).  32 maps of 56 x 56 x 256 bf16, SiLU, us: forward 28.9
+// (columns of 32 bytes 34.2, of 128 34.6; 25 KB 30.5, 100 KB 40), gradients 55.1 (60.5, 61; 100 KB and more 80).  What does not fit, and large CTAs that do not even fill the SMs, are left to two launches
+// with more of them: 4 x 50176 x 64, gradients, 45 us, with columns of 32 bytes 73; 16629 x 32, one map, 12.6 us and 9.1; 9273 x 32 8.6 and 8.0, 8 x 12544 x 64 16.7 and 21.4, 7241 x 320 10.7 and 16.8.
+constexpr int kWantKept = 56 * 1024, kMostKept = 200 * 1024, kFewKept = 120 * 1024, kLargeKept = 110 * 1024;
 bool plan_resident(GroupArgs& a, int ve, int elt, int planes, int num_sms, int* block, size_t* smem)
 {
     const int least = a.per / gcd(a.per, ve), unit = least * ve / a.per, column = ve * elt, bytes = column * planes;
@@ -829,21 +829,22 @@ bool plan_resident(GroupArgs& a, int ve, int elt, int planes, int num_sms, int* 
     int best = 0;
     for (int j = 1; j <= units && j * least <= kMostColumns; ++j) {
         if (units % j || j * unit > kMostGroups) continue;
-        if ((int64_t)a.pixels * j * least * bytes > (int64_t)kMostCluster * kMostKept) break;
+        if ((int64_t)a.pixels * j * least * bytes > (int64_t)kMostCluster * kMostKept) return false;
         best = j;
         if (j * least * column >= 64) break;
     }
     if (!best || (int64_t)units / best > 65535) return false;
     a.pieces = 1; a.gs = best * unit; a.width = best * least; a.slices = units / best;
     const int64_t slice = (int64_t)a.pixels * a.width * bytes;
-    int turns = kMostResident / a.width;
+    int turns = 256 / a.width;
     a.by_width = dc_div_up(65536, a.width); a.by_per = a.per <= 128 ? dc_div_up(65536, a.per) : 0;
     int cs = 1;
     while (cs < kMostCluster && (slice > (int64_t)cs * kWantKept || ((int64_t)a.maps * a.slices * cs < num_sms && a.pixels >= 4 * cs * turns))) cs *= 2;
     if (cs > most_chunks(a.maps, a.pixels) || (slice > (int64_t)cs * kFewKept * planes && (int64_t)a.maps * a.slices * cs < num_sms)) return false;
     a.rows_per = dc_div_up(a.pixels, cs);
     a.chunks = cs;
-    const int threads = (int64_t)a.rows_per * a.width >= 4 * kMostResident ? kMostResident : kMostResident / 2;
+    const int64_t columns = (int64_t)a.rows_per * a.width;
+    const int threads = columns * bytes > kLargeKept ? 512 : columns >= 4 * 256 ? 256 : 128;
     turns = threads / a.width;
     const int left = a.width > 32 || a.width & (a.width - 1) ? turns : threads / 32;
     *block = threads;

@@ -159,6 +159,13 @@ def test_quantize_strided_rows(pitch, offset, extra, dtype):
         assert (whole[:, k:] == 0x7F).all()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k", [(6000, 1000), (47000, 128), (400, 17000), (130, 40000), (100000, 8), (6001, 1003)])
+def test_quantize_of_many_tiles(rows, k, dtype):
+    check_quantize(make(rows, k, TYPES[dtype], 5))
+
+
 # ---------------------------------------------------------------------------
 # products
 # ---------------------------------------------------------------------------
@@ -208,7 +215,7 @@ def check_product(a, sa, b, sb, bias, relu, dtype, out=None):
 
 PRODUCTS = [(1, 1, 1), (1, 8, 16), (1, 1000, 128), (1, 300, 4096), (2, 129, 129), (3, 64, 333), (7, 4096, 127), (8, 200, 1024), (16, 256, 512), (17, 1000, 1000), (32, 520, 4100), (33, 128, 31),
             (64, 130, 640), (100, 1000, 256), (127, 127, 127), (128, 128, 128), (129, 257, 257), (200, 512, 384), (256, 256, 2048), (300, 333, 77), (513, 1024, 200), (1000, 777, 333),
-            (777, 333, 1000), (2500, 256, 64), (4000, 50, 40), (1500, 1500, 1500), (5000, 640, 300)]
+            (777, 333, 1000), (2500, 256, 64), (4000, 50, 40), (1500, 1500, 1500), (5000, 640, 300), (40, 40, 40000), (20000, 64, 640), (3000, 3000, 130), (300, 5000, 1280)]
 
 
 @gpu
@@ -266,6 +273,33 @@ def test_scales_of_any_size(m):
     out = torch.full((m, 140), 77.0, device="cuda")
     B.dc_matmul_blocks(a, torch.zeros_like(sa), b, sb, None, out)
     assert (out == 0).all()
+
+
+@gpu
+def test_products_beside_each_other_and_other_kernels():
+    """Large and split products, layers and integer products on four streams at once: each takes tensor memory, and none changes another's bits."""
+    calls = []
+    for i, (m, n, k) in enumerate([(2000, 1500, 900), (40, 3000, 4096), (100, 2000, 3000), (1, 4000, 2048)]):
+        a, b = random_rows(m, k, i), random_rows(n, k, i + 9)
+        sa, sb = random_scales(m, up(k), i), random_scales(up(n), up(k), i)
+        calls.append(lambda out, a=a, b=b, sa=sa, sb=sb: B.dc_matmul_blocks(a, sa, b, sb, None, out))
+        calls[-1].shape = (m, n)
+    g = gen(3)
+    a8, b8 = (torch.randint(-127, 128, (r, 2048), generator=g, device="cuda", dtype=torch.int8) for r in (64, 3000))
+    s64, s3k = torch.rand(64, generator=g, device="cuda"), torch.rand(3000, generator=g, device="cuda")
+    calls.append(lambda out: B.dc_matmul_quantized(a8, s64, b8, s3k, None, out))
+    calls[-1].shape = (64, 3000)
+    want = [torch.empty(c.shape, device="cuda") for c in calls]
+    for c, o in zip(calls, want):
+        c(o)
+    torch.cuda.synchronize()
+    got, streams = [torch.full_like(o, 7.0) for o in want], [torch.cuda.Stream() for _ in range(4)]
+    for _ in range(12):
+        for i, (c, o) in enumerate(zip(calls, got)):
+            with torch.cuda.stream(streams[i % 4]):
+                c(o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
 @gpu
@@ -432,6 +466,7 @@ def test_refusals_of_the_c_abi():
     at = (C.addressof(buf) + 255) & ~255
     n = C.c_size_t()
     assert lib.dc_linear_blocks_workspace(1, 1, None) == B.DC_ERR_ARG and lib.dc_linear_blocks_workspace(-1, 1, C.byref(n)) == B.DC_ERR_ARG
+    assert lib.dc_linear_blocks_workspace(2, (1 << 28) + 1, C.byref(n)) == B.DC_ERR_LIMIT and lib.dc_linear_blocks_workspace(1 << 31, 8, C.byref(n)) == B.DC_ERR_LIMIT
     assert lib.dc_linear_blocks_workspace(2, 0, C.byref(n)) == B.DC_ERR_ARG and lib.dc_linear_blocks_workspace(2, 32, C.byref(n)) == B.DC_OK
     room = n.value
 
@@ -444,6 +479,7 @@ def test_refusals_of_the_c_abi():
     assert quantize(q=at + 8) == B.DC_ERR_ARG and quantize(q_pitch=40) == B.DC_ERR_ARG and quantize(q_pitch=16) == B.DC_ERR_ARG and quantize(s=at + 2) == B.DC_ERR_ARG
     assert quantize(qt=at + 4, qt_pitch=16, st=at) == B.DC_ERR_ARG and quantize(qt=at, qt_pitch=8, st=at) == B.DC_ERR_ARG
     assert quantize(rows=1 << 31) == B.DC_ERR_LIMIT and quantize(x_pitch=1 << 32) == B.DC_ERR_LIMIT and quantize(q_pitch=1 << 40) == B.DC_ERR_LIMIT
+    assert quantize(c=(1 << 28) + 1, rows=1) == B.DC_ERR_LIMIT
     assert quantize(q=None, s=None) == B.DC_OK and quantize(rows=0) == B.DC_OK
 
     def product(a=at, a_pitch=32, sa=at, b=at, b_pitch=32, sb=at, block=128, bias=None, m=2, n=4, k=32, dtype=B.DC_FP32, out=at, out_pitch=16):
@@ -455,6 +491,7 @@ def test_refusals_of_the_c_abi():
     for call in (product, layer):
         assert call(dtype=2) == B.DC_ERR_CONFIG and call(block=64) == B.DC_ERR_CONFIG
         assert call(m=-1) == B.DC_ERR_ARG and call(n=0) == B.DC_ERR_ARG and call(k=0) == B.DC_ERR_ARG and call(m=0) == B.DC_OK
+        assert call(k=(1 << 28) + 1) == B.DC_ERR_LIMIT
         assert call(n=(1 << 28) + 1) == B.DC_ERR_LIMIT and call(m=1 << 31) == B.DC_ERR_LIMIT and call(b_pitch=1 << 40) == B.DC_ERR_LIMIT
         assert call(b=None) == B.DC_ERR_ARG and call(b=at + 8) == B.DC_ERR_ARG and call(b_pitch=24) == B.DC_ERR_ARG and call(b_pitch=16) == B.DC_ERR_ARG
         assert call(sb=None) == B.DC_ERR_ARG and call(sb=at + 2) == B.DC_ERR_ARG and call(bias=at + 1) == B.DC_ERR_ARG

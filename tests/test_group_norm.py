@@ -113,7 +113,8 @@ def check_norm(x, groups, gamma, beta, act="none", eps=EPS, y=None):
 
 SHAPES = [(1, 1, 1, 1), (2, 1, 8, 8), (1, 3, 8, 1), (2, 5, 12, 4), (3, 49, 64, 32), (2, 100, 96, 32), (1, 49, 2048, 32), (4, 729, 260, 20), (2, 3025, 96, 32), (2, 200, 4096, 1),
           (1, 7, 16384, 2), (1, 33, 4098, 2), (5, 3, 257, 1), (3, 1000, 40, 5), (64, 2, 32, 4), (1, 20000, 16, 4), (2, 64, 24, 1), (40, 196, 64, 8), (1, 2500, 512, 32), (7, 31, 7, 7),
-          (2, 900, 128, 32), (1, 16, 1032, 3), (3, 257, 48, 2), (1000, 1, 16, 2), (1, 1, 16384, 1), (2, 50, 640, 5)]
+          (2, 900, 128, 32), (1, 16, 1032, 3), (3, 257, 48, 2), (1000, 1, 16, 2), (1, 1, 16384, 1), (2, 50, 640, 5), (70000, 1, 8, 2), (66000, 3, 6, 3), (2, 6000, 250, 5), (1, 17000, 32, 32), (2, 3000, 672, 32), (1, 3000, 130, 1),
+          (3, 400, 66, 11), (2, 12000, 64, 32), (1, 30000, 64, 8), (4, 90, 96, 96)]
 
 
 @gpu
