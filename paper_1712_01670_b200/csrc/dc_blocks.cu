@@ -95,6 +95,13 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, uint4 w, int there)     
     if (there > 0) store_bytes(p, make_uint2(w.x, w.y), there);
     if (there > 8) store_bytes(p + 8, make_uint2(w.z, w.w), there - 8);
 }
+// The largest among sixteen lanes.  (A reduction of half a warp runs once for each half, behind branches.)
+__device__ __forceinline__ uint32_t most_of_half(uint32_t m, int lane)
+{
+    const bool upper = lane & 16;
+    const uint32_t a = __reduce_max_sync(0xffffffffu, upper ? 0u : m), b = __reduce_max_sync(0xffffffffu, upper ? m : 0u);
+    return upper ? b : a;
+}
 // Eight columns of a row, `there` of which exist.  WIDE: rows are aligned to 16 bytes and of whole eights, so all of them or none.
 template <bool WIDE, typename T>
 __device__ __forceinline__ void load_eight(Eight<T>& v, const char* x, int there)
@@ -139,7 +146,7 @@ __device__ __forceinline__ void row_blocks(const BlocksArgs& a, uint2 by_kb, uin
     for (int u = 0; u < 4; ++u, x += a.x_pitch) load_eight<WIDE>(v[u], x, u < rows ? there : 0);
     BlockScale s[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) s[u] = block_scale(__reduce_max_sync(0xffffu << (lane & 16), v[u].most()));
+    for (int u = 0; u < 4; ++u) s[u] = block_scale(most_of_half(v[u].most(), lane));
     uint8_t* q = a.q + (size_t)row0 * a.q_pitch + col;
     if (there > 0)
 #pragma unroll
@@ -252,7 +259,7 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
             const uint32_t m = v[i].most();
             if (WHOLE) most = max(most, m);
             else if (a.q) {
-                const BlockScale s = block_scale(__reduce_max_sync(0xffffu << (lane & 16), m));
+                const BlockScale s = block_scale(most_of_half(m, lane));
                 if (row < a.rows) {
                     store_eight<WIDE>(a.q + (size_t)row * a.q_pitch + col, eight_e4m3(v[i], s), there);
                     if (part == 0) a.scale[(size_t)row * a.kb + tile_c] = s.scale;
