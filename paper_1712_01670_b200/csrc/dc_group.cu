@@ -72,12 +72,18 @@ __device__ __forceinline__ Place place_of(const GroupArgs& a)
 }
 __device__ __forceinline__ char* row_at(const void* p, size_t pitch, int64_t row) { return (char*)p + (uint64_t)row * pitch; }
 
-// 1 / (1 + e^-z)
-__device__ __forceinline__ float one_and_exp(float z)
+// 1 + e^-z, and 1 / that
+__device__ __forceinline__ float exp2_of(float v)
 {
     float e;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
-    return 1.f + e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
+    return e;
+}
+__device__ __forceinline__ float one_and_exp(float z) { return 1.f + exp2_of(z * -1.4426950408889634f); }
+__device__ __forceinline__ float2 one_and_exp(float2 z)
+{
+    z = mul2(z, both<float2>(-1.4426950408889634f));
+    return add2(make_float2(exp2_of(z.x), exp2_of(z.y)), both<float2>(1.f));
 }
 __device__ __forceinline__ float reciprocal(float v)
 {
@@ -92,7 +98,7 @@ __device__ __forceinline__ void sigmoids(const float2* z, float2* p)
 {
     float2 a[STEP];
 #pragma unroll
-    for (int h = 0; h < STEP; ++h) a[h] = make_float2(one_and_exp(z[h].x), one_and_exp(z[h].y));
+    for (int h = 0; h < STEP; ++h) a[h] = one_and_exp(z[h]);
     if (JOINT) {
         const float ab = a[0].x * a[0].y, cd = STEP > 1 ? a[STEP - 1].x * a[STEP - 1].y : 1.f, t = ab * cd;
         if (t < 1e37f) {
@@ -139,8 +145,9 @@ __device__ __forceinline__ void activate_back(F (&dy)[P], const F (&z)[P])
             sigmoids<JOINT, STEP>(z + k, p);
 #pragma unroll
             for (int h = 0; h < STEP; ++h) {
-                const F zp = mul2(z[k + h], p[h]);                               // p (1 + z (1 - p)) = p + zp - zp p
-                dy[k + h] = mul2(dy[k + h], fma2(mul2(zp, both<F>(-1.f)), p[h], add2(p[h], zp)));
+                // p (1 + z (1 - p))
+                const F zp = mul2(z[k + h], p[h]), rest = fma2(p[h], both<F>(-1.f), both<F>(1.f));
+                dy[k + h] = mul2(dy[k + h], fma2(zp, rest, p[h]));
             }
         } else if (ACT == DC_ACT_RELU)
 #pragma unroll
