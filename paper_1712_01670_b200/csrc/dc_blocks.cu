@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
 // memory, where CTA r finishes channels r * 128 / CS and on, in the order of the ranks.  `early`: everything older than the kernel before is complete (dc_linear_blocks: that kernel
 // puts x into 8 bits), so the weights' loads start before the wait for it.
 constexpr int kSplitStages = 12, kSplitScales = 32 * 1024;
-template <int NT> struct SplitAdders { static constexpr int N = NT < 64 ? 4 : 8; };   // warps that add up: of wide tiles two to the same 32 channels, with half of the columns each
+template <int NT> struct SplitAdders { static constexpr int N = NT < 64 ? 4 : NT < 128 ? 8 : 16; };   // warps that add up: of wide tiles two to the same 32 channels, with half of the columns each
 // A CTA of it waits for its cluster, and tensor memory is given out without a limit on the wait: it takes at least this much shared memory for each 128 columns, so that what fits beside
 // it has columns too (as the split product of integers, dc_quant.cu).
 constexpr size_t kSplitLeast = 64 * 1024;
@@ -787,7 +787,7 @@ struct BlocksSplit {
     uint32_t idesc;
 };
 struct BlocksSplitCtl {
-    unsigned long long full[kSplitStages], empty[kSplitStages], tmem_full[2], tmem_empty[2];
+    unsigned long long full[kSplitStages], empty[kSplitStages], tmem_full[4], tmem_empty[4];
     uint32_t tmem_base;
     volatile int abort_flag;
     unsigned long long wait_ns;
@@ -796,7 +796,7 @@ struct BlocksSplitCtl {
 template <int NT, bool EACH, typename T>
 __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_split(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const BlocksSplit a)
 {
-    constexpr uint32_t kStageBytes = kATile + NT * kBytesK, kColumns = 2 * NT < 32 ? 32 : 2 * NT;
+    constexpr uint32_t kStageBytes = kATile + NT * kBytesK, ACCS = 4, kColumns = ACCS * NT;          // accumulators
     constexpr int LD = NT < 32 ? 16 : 32, ADDERS = SplitAdders<NT>::N, kThreads = 64 + 32 * ADDERS, MINE = NT / (ADDERS / 4);
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const ring = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -811,7 +811,7 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 2); mbar_init(&ctl->empty[i], 1); }   // weights and rows arrive apart
-        for (int i = 0; i < 2; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], ADDERS); }
+        for (int i = 0; i < (int)ACCS; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], ADDERS); }
         ctl->abort_flag = 0;
         ctl->wait_ns = kWaitNs;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -877,7 +877,7 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
                 umma_commit_at(smem_u32(&ctl->tmem_full[acc]));
                 umma_commit_at(empty0 + r.off);
                 r.next(r0, (uint32_t)a.stages, kStageBytes >> 4);
-                acc ^= 1u;
+                acc = (acc + 1u) & (ACCS - 1u);
                 acc_ph ^= acc == 0;
             }
         }
@@ -925,7 +925,7 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
             tc_fence_before();
             __syncwarp();
             arrive_first(smem_u32(&ctl->tmem_empty[acc]), lane);
-            acc ^= 1u;
+            acc = (acc + 1u) & (ACCS - 1u);
             acc_ph ^= acc == 0;
         }
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -1036,7 +1036,7 @@ int launch_split_as(const BlocksProduct& p, const SplitPlan& s, int kb, int earl
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.m_tiles * dc_div_up(p.n, kTileM) * s.CS)); cfg.blockDim = dim3(64 + 32 * SplitAdders<NT>::N);
-    const size_t smem = (size_t)a.stages * stage + fixed, least = kSplitLeast * (NT > 64 ? 2 : 1);
+    const size_t smem = (size_t)a.stages * stage + fixed, least = NT > 64 ? kBlocksSmem : kSplitLeast * (NT > 32 ? 2 : 1);
     cfg.dynamicSmemBytes = smem > least ? smem : least; cfg.stream = stream;
     cfg.attrs = attr; cfg.numAttrs = g_dc_pdl ? 2 : 1;
     DC_CUDA(cudaLaunchKernelEx(&cfg, k_blocks_split<NT, EACH, T>, tmW, tmX, a));
