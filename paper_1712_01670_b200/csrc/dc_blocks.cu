@@ -426,6 +426,11 @@ __device__ __forceinline__ void arrive_first(uint32_t bar, int lane)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(lane) : "memory");
 }
+// ... after which what the warp has read from shared memory may be written over.
+__device__ __forceinline__ void arrive_read(uint32_t bar, int lane)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"(lane) : "memory");
+}
 __device__ __forceinline__ void arrive_first_remote(uint32_t bar, int lane)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n\t}" ::"r"(bar), "r"(lane) : "memory");
@@ -474,6 +479,28 @@ __device__ __forceinline__ void tmem_read32(uint32_t taddr, uint32_t* r)
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(taddr) : "memory");
 }
 
+// 32 rows x 16 columns in fragments: a lane has columns 8 j + 2 (lane % 4) and the next one of rows lane / 4 + 8 i, i < 4, in r[8 (i / 2) + 4 j + 2 (i % 2)] and the next one.  Four columns' scales
+// to a lane, then, in the place of sixteen: shared memory hands out 128 bytes a cycle, also of one value to all lanes of a warp.  4000 x 4096 x 2000 with a scale for each row 51.9 us, with a row to a lane 61.8.
+__device__ __forceinline__ void tmem_read_fragments(uint32_t taddr, uint32_t* r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%16];\n\ttcgen05.ld.sync.aligned.16x256b.x2.b32 {%8, %9, %10, %11, %12, %13, %14, %15}, [%17];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr), "r"(taddr + (16u << 16)) : "memory");
+}
+__device__ __forceinline__ float lds_float(uint32_t at)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint64_t lds_pair(uint32_t at)
+{
+    uint64_t v;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(at));
+    return v;
+}
+
 // BN: columns of a tile.  EACH: b has a scale for each row and block, not for 128 rows.
 template <bool PAIR, int BN, bool EACH, typename T>
 __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmC, const BlocksTiles a)
@@ -488,6 +515,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     const BlocksProduct& p = a.p;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)cluster_rank() : 0, first = PAIR ? blockIdx.x >> 1 : blockIdx.x, step = PAIR ? gridDim.x >> 1 : gridDim.x;
+    constexpr bool FRAG = EACH && BN > 128;                   // (with 32 columns to a warp a row to a lane is as fast or faster: 4000 x 4096 x 2000 57.5 us and 59)
     constexpr int M = PAIR ? 2 : 1, PARTS = BN < 128 ? 2 : 4; // row tiles of an item; warps that share a row's columns
     // Tiles of 256 columns are two halves with accumulators, barriers and an issuer of their own.
     constexpr int HALVES = BN > 128 ? 2 : 1, BH = BN / HALVES;
@@ -636,13 +664,13 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
         }
     } else if (warp < kFirstAdder + 4 * PARTS) {
         // ---------------- sums of the blocks; bias, ReLU, rounding, store ----------------
-        // A warp has 32 rows, one to a lane (the quadrant of tensor memory that it may read), and a quarter of the columns (of 64: half, so that they make a box; the rest has nothing to do).
+        // A warp has 32 rows (the quadrant of tensor memory that it may read), one to a lane or, FRAG, in fragments, and a quarter of the columns (of 64: half, so that they make a box; the rest has nothing to do).
         constexpr int MINE = BN / PARTS;
         const int q = warp & 3, part = (warp - kFirstAdder) >> 2;
         uint32_t stage = smem_u32(staging) + (uint32_t)(warp - kFirstAdder) * kBox;
         const uint32_t both_places = a.bufs == 2 ? stage ^ (stage + kAddWarps * kBox) : 0;       // from one place to the other
         const uint32_t half = HALVES == 2 ? part / 2 : 0, lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) + 16u * half : 0;
-        const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + lane) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? part * MINE : BN > 128 ? part / 2 * 4 : 0) * 4;
+        const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + (FRAG ? lane >> 2 : lane)) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? part * MINE + (FRAG ? 2 * (lane & 3) : 0) : BN > 128 ? part / 2 * 4 : 0) * 4;
         uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0, dead = 0;
         bool there;
         const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]) + 16u * half, tmem_empty0 = smem_u32(&ctl->tmem_empty[0]);
@@ -657,46 +685,64 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             for (int i = 0; i < MINE / 2; ++i) sum[i] = 0;
             for (int k0 = 0; k0 < a.kb; k0 += 4) {
                 blocks_wait_warp(scale_full0 + 8u * slot, phase, ctl, dead);
-                const float4 r = lds_floats(my_rows + slot * (kRowScales * 4)), b = EACH ? make_float4(1.f, 1.f, 1.f, 1.f) : lds_floats(my_cols + slot * (kCols * 4));
-                float s0 = r.x * b.x, s1 = r.y * b.y, s2 = r.z * b.z;
-                const float s3 = r.w * b.w;
-                uint32_t cols = my_cols + slot * (kCols * 4);
+                float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+                if (!FRAG) {
+                    const float4 r = lds_floats(my_rows + slot * (kRowScales * 4)), b = EACH ? make_float4(1.f, 1.f, 1.f, 1.f) : lds_floats(my_cols + slot * (kCols * 4));
+                    s0 = r.x * b.x; s1 = r.y * b.y; s2 = r.z * b.z; s3 = r.w * b.w;
+                }
+                uint32_t cols = my_cols + slot * (kCols * 4), rows_at = my_rows + slot * (kRowScales * 4);
                 const int here = min(4, a.kb - k0);
 #pragma unroll 1
-                for (int u = 0; u < here; ++u, cols += 1024) {
-                    const uint64_t s = pair_of(__float_as_uint(s0), __float_as_uint(s0));
-                    s0 = s1; s1 = s2; s2 = s3;
+                for (int u = 0; u < here; ++u, cols += 1024, rows_at += 4) {
+                    uint64_t s[FRAG ? 4 : 1];
+                    if constexpr (FRAG) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { const uint32_t t = __float_as_uint(lds_float(rows_at + i * 128)); s[i] = pair_of(t, t); }
+                    } else {
+                        s[0] = pair_of(__float_as_uint(s0), __float_as_uint(s0));
+                        s0 = s1; s1 = s2; s2 = s3;
+                    }
                     blocks_wait_warp(tmem_full0 + 8u * acc, acc_ph, ctl, dead);
                     tc_fence_after();
                     const uint32_t from = from0 + acc * (uint32_t)BH;
 #pragma unroll
                     for (int c = 0; c < MINE; c += 16) {
                         uint32_t v[16];
-                        tmem_read16(from + c, v);
+                        uint64_t of_cols[2];
+                        if constexpr (FRAG) {
+                            of_cols[0] = lds_pair(cols + (uint32_t)c * 4);   // (under way while tensor memory is read)
+                            of_cols[1] = lds_pair(cols + (uint32_t)c * 4 + 32);
+                            tmem_read_fragments(from + c, v);
+                        } else tmem_read16(from + c, v);
                         if (c + 16 == MINE) {
                             tc_fence_before();
                             __syncwarp();
                             if (PAIR) arrive_first_remote(lead_empty + 8u * acc, lane);
                             else arrive_first(tmem_empty0 + 8u * acc, lane);
                         }
+                        if constexpr (FRAG) {
 #pragma unroll
-                        for (int i = 0; i < 8; i += 2) {
-                            uint64_t t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
-                            if (EACH) {
-                                uint64_t w[2];
-                                lds_pairs(cols + (uint32_t)(c + 2 * i) * 4, w);
-                                t[0] = product(t[0], w[0]);
-                                t[1] = product(t[1], w[1]);
+                            for (int i = 0; i < 8; ++i)
+                                add_product(sum[c / 2 + i], product(pair_of(v[2 * i], v[2 * i + 1]), of_cols[i >> 1 & 1]), s[2 * (i >> 2) + (i & 1)]);
+                        } else
+#pragma unroll
+                            for (int i = 0; i < 8; i += 2) {
+                                uint64_t t[2] = {pair_of(v[2 * i], v[2 * i + 1]), pair_of(v[2 * i + 2], v[2 * i + 3])};
+                                if (EACH) {
+                                    uint64_t w[2];
+                                    lds_pairs(cols + (uint32_t)(c + 2 * i) * 4, w);
+                                    t[0] = product(t[0], w[0]);
+                                    t[1] = product(t[1], w[1]);
+                                }
+                                add_product(sum[c / 2 + i], t[0], s[0]);
+                                add_product(sum[c / 2 + i + 1], t[1], s[0]);
                             }
-                            add_product(sum[c / 2 + i], t[0], s);
-                            add_product(sum[c / 2 + i + 1], t[1], s);
-                        }
                     }
                     acc = (acc + 1u) & (ACCS - 1u);
                     acc_ph ^= acc == 0u;
                 }
                 __syncwarp();
-                arrive_first(scale_empty0 + 8u * slot, lane);               // (the scales have been read: sums were made of them)
+                arrive_read(scale_empty0 + 8u * slot, lane);
                 slot = slot + 1u == kScaleSlots ? 0u : slot + 1u;
                 phase ^= slot == 0u;
             }
@@ -710,21 +756,39 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 if (c1 >= p.n) break;
                 if (a.boxes) { if (lane == 0) store_read(a.bufs); }
                 __syncwarp();
-                uint32_t w[16];
+                // 32 rows of 64 bytes, the 16 bytes of a row in another order for each two rows: no bank conflicts
+                if constexpr (FRAG) {
+                    const uint32_t at = stage + (lane >> 2) * 64, mix = lane >> 3 & 3;
 #pragma unroll
-                for (int i = 0; i < PER / 2; ++i) {
-                    float2 f = floats_of(sum[c / 2 + i]);
-                    const int j = c1 + 2 * i;
-                    if (p.bias) f = add2(f, make_float2(j < p.n ? dc_ld(p.bias + j) : 0.f, j + 1 < p.n ? dc_ld(p.bias + j + 1) : 0.f));
-                    if constexpr (sizeof(T) == 2) w[i] = p.relu ? two_bf16<true>(f) : two_bf16<false>(f);
-                    else {
-                        w[2 * i] = __float_as_uint(p.relu ? clamped<true>(f.x) : f.x);
-                        w[2 * i + 1] = __float_as_uint(p.relu ? clamped<true>(f.y) : f.y);
+                    for (int j = 0; j < PER / 8; ++j) {
+                        const int j1 = c1 + 8 * j + 2 * (lane & 3);
+                        const float2 bias = make_float2(p.bias && j1 < p.n ? dc_ld(p.bias + j1) : 0.f, p.bias && j1 + 1 < p.n ? dc_ld(p.bias + j1 + 1) : 0.f);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {         // row lane / 4 + 8 i
+                            const float2 f = add2(floats_of(sum[(c + 8 * j) / 16 * 8 + 4 * (i >> 1) + 2 * (j & 1) + (i & 1)]), bias);
+                            if constexpr (sizeof(T) == 2)
+                                asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + i * 512 + ((j ^ mix) << 4) + 4 * (lane & 3)), "r"(p.relu ? two_bf16<true>(f) : two_bf16<false>(f)) : "memory");
+                            else
+                                asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at + i * 512 + (((2 * j + (lane >> 1 & 1)) ^ mix) << 4) + 8 * (lane & 1)),
+                                             "f"(p.relu ? clamped<true>(f.x) : f.x), "f"(p.relu ? clamped<true>(f.y) : f.y) : "memory");
+                        }
                     }
-                }
-                // a lane's row of 64 bytes, its 16 bytes in another order for each two rows: no bank conflicts
+                } else {
+                    uint32_t w[16];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) sts128(stage + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4), w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+                    for (int i = 0; i < PER / 2; ++i) {
+                        float2 f = floats_of(sum[c / 2 + i]);
+                        const int j = c1 + 2 * i;
+                        if (p.bias) f = add2(f, make_float2(j < p.n ? dc_ld(p.bias + j) : 0.f, j + 1 < p.n ? dc_ld(p.bias + j + 1) : 0.f));
+                        if constexpr (sizeof(T) == 2) w[i] = p.relu ? two_bf16<true>(f) : two_bf16<false>(f);
+                        else {
+                            w[2 * i] = __float_as_uint(p.relu ? clamped<true>(f.x) : f.x);
+                            w[2 * i + 1] = __float_as_uint(p.relu ? clamped<true>(f.y) : f.y);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) sts128(stage + lane * 64 + ((u ^ ((lane >> 1) & 3)) << 4), w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+                }
                 if (a.boxes) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
@@ -777,7 +841,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
 // memory, where CTA r finishes channels r * 128 / CS and on, in the order of the ranks.  `early`: everything older than the kernel before is complete (dc_linear_blocks: that kernel
 // puts x into 8 bits), so the weights' loads start before the wait for it.
 constexpr int kSplitStages = 12, kSplitScales = 32 * 1024;
-template <int NT> struct SplitAdders { static constexpr int N = NT < 64 ? 4 : NT < 128 ? 8 : 16; };   // warps that add up: of wide tiles two to the same 32 channels, with half of the columns each
+template <int NT> struct SplitAdders { static constexpr int N = NT < 64 ? 4 : NT < 128 ? 8 : 16; };   // warps that add up: of wide tiles two or four to the same 32 channels, with a share of the columns each
 // A CTA of it waits for its cluster, and tensor memory is given out without a limit on the wait: it takes at least this much shared memory for each 128 columns, so that what fits beside
 // it has columns too (as the split product of integers, dc_quant.cu).
 constexpr size_t kSplitLeast = 64 * 1024;
@@ -1085,7 +1149,7 @@ int launch_product(const BlocksProduct& p, int dtype, bool early, int device, in
     double best = 0.0;
     // The tile that takes the fewest cycles, as counted from measurements: a block of K takes so many (what bounds it is its way from the MMAs to the sums and back), an SM's share of out leaves
     // at about 24 bytes a cycle where others pause, and an item costs 500 to begin and end.
-    static constexpr double kStep[4][2] = {{1040.0, 1690.0}, {635.0, 800.0}, {635.0, 780.0}, {480.0, 540.0}};     // scales for 128 rows of b, for each
+    static constexpr double kStep[4][2] = {{1040.0, 1540.0}, {635.0, 800.0}, {635.0, 780.0}, {480.0, 540.0}};     // scales for 128 rows of b, for each
     for (int c = 0; c < 4; ++c) {
         const bool two = c < 2;
         const int bn = c == 0 ? 256 : c == 3 ? 64 : 128;

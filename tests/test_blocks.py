@@ -246,6 +246,61 @@ def test_product_into_strided_rows(m, pitch, offset, dtype):
 
 @gpu
 @pytest.mark.parametrize("each", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k,pitch,offset", [(600, 1008, 0), (40, 1003, 0), (600, 1000, 1), (129, 1008, 8)])
+def test_product_of_wide_tiles_into_strided_rows(k, pitch, offset, dtype, each):
+    m, n = 4600, 1000
+    a, b = random_rows(m, k, 1), random_rows(n, k, 2)
+    sa, sb = random_scales(m, up(k), 3), random_scales(n if each else up(n), up(k), 4)
+    buf = torch.full((m * pitch + offset + 64,), 77.0, dtype=TYPES[dtype], device="cuda")
+    out = buf[offset:offset + m * pitch].view(m, pitch)[:, :n]
+    check_product(a, sa, b, sb, torch.randn(n + 1, generator=gen(5), device="cuda")[1:] if offset != 8 else None, offset != 0, dtype, out)
+    out.fill_(77.0)
+    assert (buf == 77.0).all(), "something beside the rows was written"
+
+
+def far(rows, columns, pitch, dtype):
+    """Rows `pitch` elements apart, the last ones behind 2^32 bytes and (of 8-bit values) elements."""
+    t = torch.empty(rows * pitch, dtype=dtype, device="cuda").view(rows, pitch)[:, :columns]
+    assert (rows - 1) * pitch * t.element_size() > 1 << 32
+    return t
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_behind_four_gigabytes(dtype):
+    rows, k, t = 1300, 264, TYPES[dtype]
+    near = make(rows, k, t, 3)
+    x, q, qt = far(rows, k, 1 << 21, t), far(rows, k, 1 << 22, torch.uint8), far(k, rows, 1 << 24, torch.uint8)
+    x.copy_(near)
+    for block in (1, 128):
+        want = [bytes_like(rows, k), bytes_like(k, rows)]
+        got = [torch.empty(up(rows, block), up(k), device="cuda"), torch.empty(up(k, block), up(rows), device="cuda")]
+        scales = [torch.empty_like(v) for v in got]
+        B.dc_quantize_blocks(near, want[0], scales[0], want[1], scales[1], block)
+        B.dc_quantize_blocks(x, q, got[0], qt, got[1], block)
+        assert torch.equal(q, bits(want[0])) and torch.equal(qt, bits(want[1])) and torch.equal(got[0], scales[0]) and torch.equal(got[1], scales[1])
+    del qt
+
+
+@gpu
+@pytest.mark.parametrize("each", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(1300, 1030), (20, 1030)])
+def test_products_of_rows_behind_four_gigabytes(m, n, dtype, each):
+    k, t = 300, TYPES[dtype]
+    a, b = random_rows(m, k, 1), random_rows(n, k, 2)
+    sa, sb = random_scales(m, up(k), 3), random_scales(n if each else up(n), up(k), 4)
+    want = torch.empty(m, n, dtype=t, device="cuda")
+    B.dc_matmul_blocks(a, sa, b, sb, None, want)
+    far_a, far_b, out = far(m, k, 1 << 28 if m < 100 else 1 << 22, torch.uint8), far(n, k, 1 << 23, torch.uint8), far(m, n, 1 << 27 if m < 100 else 1 << 21, t)
+    far_a.copy_(a.view(torch.uint8)), far_b.copy_(b.view(torch.uint8))
+    B.dc_matmul_blocks(far_a, sa, far_b, sb, None, out)
+    assert torch.equal(out, want)
+
+
+@gpu
+@pytest.mark.parametrize("each", [False, True])
 @pytest.mark.parametrize("m,n,k", [(1, 200, 300), (20, 200, 300), (300, 600, 300)])
 def test_nan_values_and_scales_reach_their_rows_alone(m, n, k, each):
     a, b = random_rows(m, k, 1), random_rows(n, k, 2)

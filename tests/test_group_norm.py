@@ -352,6 +352,34 @@ def test_relu_backward_keeps_what_the_forward_pass_kept():
 # streams, graphs, refusals
 # ---------------------------------------------------------------------------
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("maps,pixels,c,groups", [(2, 600, 64, 8), (1, 1200, 40, 8), (4, 300, 33, 3), (2, 700, 4096, 2)])
+def test_rows_behind_four_gigabytes(maps, pixels, c, groups, dtype):
+    t, pitch = TYPES[dtype], 1 << 21
+    def far():
+        m = torch.empty(maps * pixels * pitch, dtype=t, device="cuda").view(maps, pixels, pitch)[:, :, :c]
+        assert (maps * pixels - 1) * pitch * m.element_size() > 1 << 32
+        return m
+    gamma, beta = weights(c, 3)
+    x, dy = make(maps, pixels, c, t, 4), make(maps, pixels, c, t, 5)
+    y, dx, numbers = torch.empty_like(x), torch.empty_like(x), [torch.empty(2, maps, groups, device="cuda") for _ in range(2)]
+    gradients = [torch.empty(2, c, device="cuda") for _ in range(2)]
+    work = scratch(maps, pixels, c, groups)
+    B.dc_group_norm(x, groups, gamma, beta, y, *numbers[0], ACTS["silu"], EPS, work)
+    B.dc_group_norm_backward(dy, x, groups, gamma, beta, *numbers[0], dx, *gradients[0], ACTS["silu"], work)
+    far_x, far_dy, far_y, far_dx = far(), far(), far(), far()
+    far_x.copy_(x), far_dy.copy_(dy)
+    B.dc_group_norm(far_x, groups, gamma, beta, far_y, *numbers[1], ACTS["silu"], EPS, work)
+    B.dc_group_norm_backward(far_dy, far_x, groups, gamma, beta, *numbers[1], far_dx, *gradients[1], ACTS["silu"], work)
+    # (rows of 33 elements lie on fewer bytes than those 2^21 apart: sums in another order there)
+    if c % 8 == 0:
+        assert torch.equal(far_y, y) and torch.equal(far_dx, dx) and torch.equal(numbers[0], numbers[1]) and torch.equal(gradients[0], gradients[1])
+    else:
+        check_norm(far_x, groups, gamma, beta, "silu")
+        check_backward(far_dy, far_x, groups, gamma, beta, "silu")
+
+
+@gpu
 def test_equal_calls_give_equal_bits_on_streams_and_in_graphs():
     maps, pixels, c, groups = 4, 900, 96, 32
     gamma, beta = weights(c, 3)
