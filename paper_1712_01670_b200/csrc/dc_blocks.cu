@@ -8,7 +8,7 @@
 //
 // Products: tcgen05.mma kind::f8f6f4 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, which are one block.  A block's sums leave
 // tensor memory as soon as they are there, are scaled and added up in the registers of sixteen warps, beside the MMAs of the next blocks (two to four accumulators in turns).  The scales
-// are any floats, so they cannot be left to the MMA, which takes powers of two.  8192 x 4096 x 4096 to bf16 121 to 127 us, 2.2 PFLOP/s at 1.6 GHz: tensor pipe 59 % busy, instruction issue 59 %;
+// are any floats, so they cannot be left to the MMA, which takes powers of two.  8192 x 4096 x 4096 to bf16 121 to 127 us, 2.2 PFLOP/s at 1.6 GHz: tensor pipe 56 % busy, instruction issue 63 %;
 // the same product of 8-bit integers, whose sums stay in tensor memory, 82.
 //   k_blocks        256 x 256 (CTA pairs) to 128 x 64 tiles
 //   k_blocks_split  few tiles: the blocks of K dealt to a cluster
@@ -131,6 +131,25 @@ __device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale&
     return make_uint2(__byte_perm(w[0], w[1], 0x5410) & kept, __byte_perm(w[2], w[3], 0x5410) & kept);
 }
 
+// A tile of 128 x 128 of a map whose rows are not aligned, into shared memory: an element to a lane, side by side.  (Eight neighbours to a lane, element by element, spread each of a warp's loads over
+// 512 or 1024 bytes: 25087 x 513 bf16 24.8 us, so 29.9; 4096 x 9219 with a scale for 128 rows 45.5 and 54.8.)
+template <typename T>
+__device__ __forceinline__ void stage_tile(const BlocksArgs& a, int row0, int col0, T* tile)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int r0 = threadIdx.x >> 5; r0 < 128; r0 += 32) {     // four rows of a warp at once
+        T v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int row = row0 + r0 + i / 4 * 8, col = col0 + i % 4 * 32 + lane;
+            v[i] = row < a.rows && col < a.channels ? ((const T*)((const char*)a.x + (size_t)row * a.x_pitch))[col] : T(0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tile[(r0 + i / 4 * 8) * 128 + i % 4 * 32 + lane] = v[i];
+    }
+}
+
 // Rows alone: sixteen lanes to a block of each of four rows, all four in flight.  by_kb: see divided().
 __device__ __forceinline__ uint32_t divided(uint32_t n, uint2 by) { return by.x ? __umulhi(n, by.x) >> by.y : n; }
 
@@ -167,7 +186,7 @@ __global__ void __launch_bounds__(256) k_quantize_row_blocks(const BlocksArgs a,
 }
 
 // Turned, of few tiles: 128 rows x 32 columns to a CTA, four times as many as whole tiles; the rows, if they are wanted too, are put into 8 bits by the first row_ctas CTAs, which read x once
-// more.  Both ways, us, so and as whole tiles: 196 x 1024 bf16 2.0 and 4.5, 1000 x 333 f32 3.1 and 6.6, 40000 x 96 bf16 8.3 and 9.7, 6000 x 1001 14.7 and 15.2, 12544 x 512 f32 13.3 and 13.5,
+// more.  Both ways, us, so and as whole tiles: 196 x 1024 bf16 2.0 and 4.5, 1000 x 333 f32 3.1 and 6.6, 40000 x 96 bf16 8.3 and 9.7, 6000 x 1001 14.7 and 13.4, 12544 x 512 f32 13.3 and 13.5,
 // 25088 x 512 bf16 22.0 and 16.8.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(256) k_quantize_columns(const BlocksArgs a, uint2 by_kb, uint32_t items, int row_ctas)
@@ -243,6 +262,10 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
         if (threadIdx.x == 0) most_of_tile = 0;
         __syncthreads();
     }
+    if (!WIDE) {
+        stage_tile(a, tile_r * 128, tile_c * 128, (T*)tile4);
+        __syncthreads();
+    }
     uint32_t most = 0;
 #pragma unroll
     for (int i0 = 0; i0 < 8; i0 += 4) {
@@ -250,12 +273,13 @@ __global__ void __launch_bounds__(256) k_quantize_tile(const BlocksArgs a)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = tile_r * 128 + (i0 + i) * 16 + team;
-            load_eight<WIDE>(v[i], (const char*)a.x + (size_t)row * a.x_pitch + (size_t)col * sizeof(T), row < a.rows ? there : 0);
+            if (!WIDE) v[i].load((const char*)(tile4 + (((i0 + i) * 16 + team) * 16 + part) * (sizeof(T) / 2)));
+            else load_eight<WIDE>(v[i], (const char*)a.x + (size_t)row * a.x_pitch + (size_t)col * sizeof(T), row < a.rows ? there : 0);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = (i0 + i) * 16 + team, row = tile_r * 128 + r;
-            if (WHOLE || a.qt) v[i].keep(tile4 + (r * 16 + part) * (sizeof(T) / 2));
+            if (WIDE && (WHOLE || a.qt)) v[i].keep(tile4 + (r * 16 + part) * (sizeof(T) / 2));
             const uint32_t m = v[i].most();
             if (WHOLE) most = max(most, m);
             else if (a.q) {
