@@ -8,8 +8,8 @@
 // A slice is the columns of a map that a CTA works on: some whole groups, or a piece of one that is wider than a CTA.  A thread has one column (16 bytes of
 // each of its rows, or two elements or one where rows are not aligned to 16 bytes) and so one set of weights and of sums.
 //
-// Sums of squares: a CTA takes its values' distances from one of them (the group's first in its first row), so that no distance is beyond the group's range, whatever the mean is, and
-// threads' sums just add up; CTAs' means and squares are then joined by M2 = sum M2_i + sum n_i (mean_i - mean)^2, in a fixed order: equal calls give equal bits.
+// Sums of squares: a CTA takes its values' distances from a number within 2 sigma of their mean (statistics()), so that no more than 4/5 of the squares are taken off again as the mean's own,
+// and threads' sums just add up; CTAs' means and squares are then joined by M2 = sum M2_i + sum n_i (mean_i - mean)^2, in a fixed order: equal calls give equal bits.
 #include <atomic>
 
 #include "dc_quantise.cuh"
@@ -43,7 +43,7 @@ struct GroupArgs {
     int width, slices, gs, pieces, piece_items;     // columns of a slice; slices of a map; groups of a slice; slices of a group; columns of a group (with pieces)
     int by_width, by_per;                           // slices of at most 64 columns: 65536 / width and (groups of at most 128 channels) / per, rounded up; else 0
     int chunks, rows_per;                           // CTAs to the rows of a slice, and the rows of each
-    float2* part;                                   // [maps][chunks * pieces][groups]: mean and squares, or the two sums of a group's gradients
+    float2* part;                                   // [maps][chunks * pieces][groups]: minus the mean, and squares, or the two sums of a group's gradients
     float* sums;                                    // [maps][chunks][2][channels]: sums of dz and of dz xh; or NULL: not wanted
     bool joined;                                    // (host) they have been
     float *dgamma, *dbeta;                          // of a single map that clusters hold whole: written at once
@@ -247,64 +247,22 @@ __device__ __forceinline__ float rows_of_sums(const float* part, int left, int w
 // Lanes to a group of so many items: a power of two.
 __device__ __forceinline__ int lanes_to(int items) { return items >= 32 ? 32 : 1 << (31 - __clz(items)); }
 
-// The value that a group's distances are taken from: its first channel in the CTA's first row.
-template <typename T>
-__device__ __forceinline__ float first_of(const GroupArgs& a, const Place& p, int64_t row0, int g)
-{
-    float v;
-    Vec<T, 1>::open(((const T*)row_at(a.x, a.x_pitch, row0))[(p.group0 + g) * a.per], &v);
-    return v;
-}
-
-// Statistics of a CTA's rows: s holds each thread's sums of distances and of their squares.  out(group, {mean, squares around it}, lane of the group, lanes)
-template <typename T, int VE, bool ONE, int N2, typename F, typename Out>
-__device__ __forceinline__ void finish_stats(const GroupArgs& a, const Place& p, const Seat& seat, int64_t row0, F (&s)[N2], float* part, bool cluster, Out out)
-{
-    constexpr int IT = ONE ? 1 : VE, N = N2 / 2;
-    const int items = p.cols * IT, left = fold(s, p.cols, seat.turns), to = fold_row(seat, p.cols);
-    if (to >= 0)
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            part[to * 2 * items + seat.col * IT + i] = ONE ? sum_of(s[0]) : lane_of(s[ONE ? 0 : i / 2], i & 1);
-            part[(to * 2 + 1) * items + seat.col * IT + i] = ONE ? sum_of(s[N]) : lane_of(s[N + (ONE ? 0 : i / 2)], i & 1);
-        }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * items; i += blockDim.x) part[i] = rows_of_sums(part, left, 2 * items, i);       // (its own column alone)
-    __syncthreads();
-    cluster_wait(cluster);
-    const int of = items / p.ngroups, lanes = lanes_to(of), sub = threadIdx.x & (lanes - 1);
-    for (int base = 0; base < p.ngroups; base += blockDim.x / lanes) {
-        const int g = base + threadIdx.x / lanes;
-        float sum = 0.f, squares = 0.f;
-        if (g < p.ngroups)
-            for (int i = g * of + sub; i < (g + 1) * of; i += lanes) { sum += part[i]; squares += part[items + i]; }
-        sum = reduce_lanes<Sum>(sum, lanes); squares = reduce_lanes<Sum>(squares, lanes);
-        if (g >= p.ngroups) continue;
-        float2 r = make_float2(0.f, 0.f);
-        if (p.rows > 0) {
-            const float m = sum / ((float)p.rows * (float)(of * (ONE ? VE : 1)));
-            r = make_float2(m + first_of<T>(a, p, row0, g), fmaxf(fmaf(-m, sum, squares), 0.f) + (sum - sum));       // (a NaN or an infinity stays one)
-        }
-        out(g, r, sub, lanes);
-    }
-}
-
-// Means and squares of a group's parts, joined in their order: n(i) values in part i.  {-mean, rstd}
+// Means (minus them) and squares of a group's parts, joined in their order: n(i) values in part i.  {-mean, rstd}
 template <typename N, typename V>
 __device__ __forceinline__ float2 join_parts(int parts, float total, float eps, int sub, int lanes, N n, V value)
 {
     float s = 0.f, q = 0.f;
 #pragma unroll 4
     for (int i = sub; i < parts; i += lanes) s = fmaf(n(i), value(i).x, s);
-    const float mean = reduce_lanes<Sum>(s, lanes) / total;
+    const float minus_mean = reduce_lanes<Sum>(s, lanes) / total;
 #pragma unroll 4
     for (int i = sub; i < parts; i += lanes) {
         const float w = n(i);
         const float2 v = value(i);
-        const float d = v.x - mean;
+        const float d = v.x - minus_mean;
         q += w > 0.f ? fmaf(w * d, d, v.y) : 0.f;
     }
-    return make_float2(-mean, inverse_root(reduce_lanes<Sum>(q, lanes) / total + eps));
+    return make_float2(minus_mean, inverse_root(reduce_lanes<Sum>(q, lanes) / total + eps));
 }
 
 // Gradients, first half: s holds each thread's sums of dz and of dz xh.  total(place, sum) of each channel; out(group, the two sums with gamma, lane, lanes).
@@ -403,6 +361,74 @@ template <typename T, int VE, bool ONE> struct Work {
     }
 };
 
+// What a group's distances are taken from at first: the mean of eight of its values (of equal ones: that value), in as many of the CTA's first rows as it takes.
+template <typename T>
+__device__ __forceinline__ float first_of(const GroupArgs& a, const Place& p, int64_t row0, int g)
+{
+    const char* const x = row_at(a.x, a.x_pitch, row0) + (size_t)(p.group0 + g) * a.per * sizeof(T);
+    float v[8];
+    int row = 0, channel = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        Vec<T, 1>::open(((const T*)(x + (size_t)min(row, p.rows - 1) * a.x_pitch))[channel], v + k);
+        if (++channel == a.per) { channel = 0; ++row; }
+    }
+#pragma unroll
+    for (int n = 4; n > 0; n /= 2)
+#pragma unroll
+        for (int k = 0; k < n; ++k) v[k] += v[k + n];
+    return v[0] * 0.125f;
+}
+
+// Statistics of a CTA's rows: found[group] = {-mean, squares around it}.  rows(first, s) adds the distances of a thread's values from `first` and their squares to s.
+// The squares around the mean are what is left of those around `first`, and next to nothing is where that lies far from the rest: a single value 1000 sigma away as `first` of 25000 took
+// 5 digits from them.  So where it turns out to lie more than 2 sigma from the mean, the rows are gone through once more with the mean in its place.  (The mean of eight normal values lies within
+// 2 sigma but for one group of 10^8; with one or two values in its place 4 x 50176 x 64 in 32 groups took 27.3 us, 24.1 so.)
+template <typename T, int VE, bool ONE, typename Rows>
+__device__ __forceinline__ void statistics(const GroupArgs& a, const Place& p, const Seat& seat, int64_t row0, float* part, float2* found, Rows rows)
+{
+    typedef Work<T, VE, ONE> W;
+    typedef typename W::F F;
+    constexpr int IT = ONE ? 1 : VE, N = W::N;
+    const int items = p.cols * IT, of = items / p.ngroups, lanes = lanes_to(of), sub = threadIdx.x & (lanes - 1);
+    const float n = (float)p.rows * (float)(of * (ONE ? VE : 1));
+    for (int g = threadIdx.x; g < p.ngroups; g += blockDim.x) found[g].x = p.rows > 0 ? -first_of<T>(a, p, row0, g) : 0.f;
+    __syncthreads();
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+        F s[2 * N], first[N], unused[N];                      // (minus what distances are taken from)
+        Column<T, VE, ONE>::groups(a, seat.col, first, unused, [&](int g) { return make_float2(found[g].x, 0.f); });
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) s[k] = both<F>(0.f);
+        rows(first, s);
+        const int left = fold(s, p.cols, seat.turns), to = fold_row(seat, p.cols);
+        if (to >= 0)
+#pragma unroll
+            for (int i = 0; i < IT; ++i) {
+                part[to * 2 * items + seat.col * IT + i] = ONE ? sum_of(s[0]) : lane_of(s[ONE ? 0 : i / 2], i & 1);
+                part[(to * 2 + 1) * items + seat.col * IT + i] = ONE ? sum_of(s[N]) : lane_of(s[N + (ONE ? 0 : i / 2)], i & 1);
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * items; i += blockDim.x) part[i] = rows_of_sums(part, left, 2 * items, i);       // (its own column alone)
+        __syncthreads();
+        bool far = false;
+        for (int base = 0; base < p.ngroups; base += blockDim.x / lanes) {
+            const int g = base + threadIdx.x / lanes;
+            float sum = 0.f, squares = 0.f;
+            if (g < p.ngroups)
+                for (int i = g * of + sub; i < (g + 1) * of; i += lanes) { sum += part[i]; squares += part[items + i]; }
+            sum = reduce_lanes<Sum>(sum, lanes); squares = reduce_lanes<Sum>(squares, lanes);
+            if (g >= p.ngroups || sub) continue;
+            if (p.rows > 0) {
+                const float m = sum / n, around = fmaf(-m, sum, squares);
+                found[g] = make_float2(found[g].x - m, fmaxf(around, 0.f) + (sum - sum));       // (a NaN or an infinity stays one)
+                far |= m * sum > 4.f * around;
+            } else found[g].y = 0.f;
+        }
+        if (!__syncthreads_or(far) || again) return;          // found is there for all
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Two launches: a map's rows in up to 128 chunks, sums first, the map after
 // ---------------------------------------------------------------------------
@@ -436,26 +462,24 @@ __device__ __forceinline__ void each_two(const Place& p, const Seat& s, const ch
     }
 }
 
+// (CTAs to an SM: as many as the grid is made for, but where a thread has sums of eight groups.)
 template <typename T, int VE, bool ONE>
-__global__ void __launch_bounds__(kThreads) k_group_stats(const GroupArgs a)
+__global__ void __launch_bounds__(kThreads, ONE && VE <= 4 ? 6 : ONE || VE <= 4 ? 5 : 4) k_group_stats(const GroupArgs a)
 {
     typedef Work<T, VE, ONE> W;
     typedef typename W::F F;
     __shared__ float part[2 * kThreads * (ONE ? 1 : VE)];
+    __shared__ float2 found[kThreads * (ONE ? 1 : VE)];
     dc_pdl_wait();
     dc_pdl_release();
     const Place p = place_of(a);
     const Seat seat = seat_of(a, p);
     const int64_t row0 = (int64_t)p.map * a.pixels + p.row0;
-    F s[2 * W::N], first[W::N], unused[W::N];
-    Column<T, VE, ONE>::groups(a, seat.col, first, unused, [&](int g) { return make_float2(-first_of<T>(a, p, row0, g), 0.f); });
-#pragma unroll
-    for (int k = 0; k < 2 * W::N; ++k) s[k] = both<F>(0.f);
-    if (seat.turn < seat.turns)
-        each_row<4, typename W::Raw>(p, seat, row_at(a.x, a.x_pitch, row0) + (size_t)(p.col0 + seat.col) * VE * sizeof(T), a.x_pitch, [&](int, typename W::Raw raw) { W::stats(raw, first, s); });
-    finish_stats<T, VE, ONE>(a, p, seat, row0, s, part, false, [&](int g, float2 r, int sub, int) {
-        if (sub == 0) a.part[((size_t)p.map * a.chunks * a.pieces + p.chunk * a.pieces + p.piece) * a.groups + p.group0 + g] = r;
+    const char* const x = row_at(a.x, a.x_pitch, row0) + (size_t)(p.col0 + seat.col) * VE * sizeof(T);
+    statistics<T, VE, ONE>(a, p, seat, row0, part, found, [&](const F* first, F* s) {
+        if (seat.turn < seat.turns) each_row<4, typename W::Raw>(p, seat, x, a.x_pitch, [&](int, typename W::Raw raw) { W::stats(raw, first, s); });
     });
+    for (int g = threadIdx.x; g < p.ngroups; g += kThreads) a.part[((size_t)p.map * a.chunks * a.pieces + p.chunk * a.pieces + p.piece) * a.groups + p.group0 + g] = found[g];
 }
 
 // join(group of the slice, whether there is one, lane, lanes): a slice's groups, as many lanes to each as there are parts to join, but so few that all groups go at once.
@@ -630,9 +654,10 @@ __device__ __forceinline__ void keep_rows(const Place& p, const Seat& s, const c
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __host__ __device__ constexpr size_t up16(size_t n) { return (n + 15) / 16 * 16; }
 
-// A CTA has rows_per rows of a slice; its cluster has the slice.  Each thread copies its own values into shared memory and reads them twice from there.
+// A CTA has rows_per rows of a slice; its cluster has the slice.  Each thread copies its own values into shared memory and reads them twice from there (three times at most: statistics()).
+// Registers: 64 at most, so that four CTAs of 256 threads fit an SM; 80, and three, where a thread has sums of eight groups.
 template <typename T, int VE, bool ONE, int ACT>
-__global__ void __launch_bounds__(kMostResident, ONE ? 2 : 1) k_group_resident(const GroupArgs a)
+__global__ void __launch_bounds__(ONE || VE <= 4 ? kMostResident : 768, ONE || VE <= 4 ? 2 : 1) k_group_resident(const GroupArgs a)
 {
     typedef Work<T, VE, ONE> W;
     typedef typename W::F F;
@@ -652,20 +677,16 @@ __global__ void __launch_bounds__(kMostResident, ONE ? 2 : 1) k_group_resident(c
     float* const part = (float*)((char*)shared4 + up16((size_t)a.rows_per * p.cols * sizeof(Raw)));      // [rows of partial sums][sums, squares][items]
     Column<T, VE, ONE> c;
     c.weights(a, p, seat.col);
-    F s[2 * W::N], first[W::N], unused[W::N];
-    if (p.rows > 0) c.groups(a, seat.col, first, unused, [&](int g) { return make_float2(-first_of<T>(a, p, row0, g), 0.f); });
-#pragma unroll
-    for (int k = 0; k < 2 * W::N; ++k) s[k] = both<F>(0.f);
-    copies_done();
     const int line = seat.turns * p.cols;
-    if (seat.turn < seat.turns) {
+    statistics<T, VE, ONE>(a, p, seat, row0, part, fin, [&](const F* first, F* s) {
+        copies_done();
+        if (seat.turn >= seat.turns) return;
         const Raw* k4 = kept + threadIdx.x;
 #pragma unroll 4
         for (int r = seat.turn; r < p.rows; r += seat.turns, k4 += line) W::stats(*k4, first, s);
-    }
-    finish_stats<T, VE, ONE>(a, p, seat, row0, s, part, cluster, [&](int g, float2 r, int sub, int lanes) {
-        for (int rank = sub; rank < a.chunks; rank += lanes) send(&exchange[p.chunk][g], rank, r);
     });
+    cluster_wait(cluster);
+    for (int rank = threadIdx.x / kMostGroups, g = threadIdx.x % kMostGroups; rank < a.chunks && g < p.ngroups; rank += blockDim.x / kMostGroups) send(&exchange[p.chunk][g], rank, fin[g]);
     if (cluster) cluster_sync(); else __syncthreads();
     if (threadIdx.x < p.ngroups) {
         const int g = threadIdx.x;

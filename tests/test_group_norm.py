@@ -213,6 +213,64 @@ def test_maps_of_more_dimensions_and_none():
 
 
 # ---------------------------------------------------------------------------
+# maps with a value far from all others
+# ---------------------------------------------------------------------------
+def check_statistics(x, groups):
+    """Mean and rstd, off by what float32 sums of positive numbers are off by, whatever the values are.
+
+    Distances are taken from some value c, and so that the mean is no farther from c than 2 sigma of the rows that are added up together, or from the mean itself: of Q, the squares
+    of distances, at most 4/5 are taken off as the mean's.  Q is off by DEPTH u of itself, a sum of N distances by DEPTH u sqrt(N Q), so what is left, M >= Q/5, by
+    DEPTH u (1 + 2 sqrt(4/5)) Q <= 14 DEPTH u M.  Where parts are joined, their means are off by DEPTH u sqrt(Q_i / N_i) and two roundings, which moves M by
+    2 DEPTH u sqrt(5) M + 4 u sqrt(M N (var + mean^2)) at most.  Some roundings of sums that are there already: 16 u."""
+    maps, pixels, c = x.shape
+    v = split(x, groups)
+    wmean = v.mean((1, 3))
+    var = (v - wmean[:, None, :, None]).square().mean((1, 3))
+    wrstd = (var + EPS).rsqrt()
+    y, mean, rstd = torch.empty(maps, pixels, c, dtype=x.dtype, device="cuda"), torch.empty(maps, groups, device="cuda"), torch.empty(maps, groups, device="cuda")
+    B.dc_group_norm(x, groups, None, None, y, mean, rstd, ACTS["none"], EPS, scratch(maps, pixels, c, groups))
+    root = (var + wmean.square()).sqrt()
+    dm = DEPTH * U * (5 * var).sqrt() + 16 * U * root
+    dv = ((14 + 2 * 5 ** 0.5) * DEPTH + 16) * U + 4 * U * root / var.sqrt()
+    dr = 0.5 * dv * (1 + 2 * dv) + 8 * U
+    assert dv.max() < 4e-4, "the bound says nothing"
+    assert ((mean.double() - wmean).abs() <= dm).all()
+    off = ((rstd.double() - wrstd).abs() / wrstd - dr).max()
+    assert off <= 0, f"rstd off by {off:.3e} of itself more than the bound"
+    z = (x.double() - wide(wmean, c)) * wide(wrstd, c)
+    T = torch.finfo(x.dtype).eps / 2
+    over = (y.double() - z).abs() - ((wide(wrstd * dm, c) + z.abs() * (wide(dr, c) + 4 * U) + 2 * U * z.abs()) * (1 + T) + T * z.abs())
+    assert over.max() <= 0, f"off by {over.max():.3e} more than the bound"
+
+
+# one launch and two, whole vectors to a group and not, rows of two elements and of one, groups wider than a CTA
+FAR = [(1, 3136, 64, 8), (4, 3136, 256, 32), (3, 900, 24, 8), (2, 3025, 96, 32), (1, 20000, 16, 4), (1, 30000, 64, 8), (2, 700, 4096, 2), (2, 4000, 66, 11), (2, 4000, 33, 3), (2, 6000, 250, 5),
+       (40, 196, 64, 8)]
+
+
+@gpu
+@pytest.mark.parametrize("where", ["first", "any", "row", "channel"])
+@pytest.mark.parametrize("far", [30.0, 1e3, 3e4])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("maps,pixels,c,groups", FAR)
+def test_norm_with_values_far_from_the_rest(maps, pixels, c, groups, dtype, far, where):
+    """A group's first value, any one, its first row or its first channel `far` standard deviations away."""
+    g = gen(pixels + c)
+    x = torch.randn(maps, pixels, c, generator=g, device="cuda")
+    v = x.view(maps, pixels, groups, c // groups)
+    if where == "first":
+        v[:, 0, :, 0] += far
+    elif where == "any":
+        at = torch.randint(0, pixels, (maps,), generator=g, device="cuda")
+        v[torch.arange(maps, device="cuda"), at, :, (c // groups) // 2] -= far
+    elif where == "row":
+        v[:, 0] += far
+    else:
+        v[..., 0] += far
+    check_statistics(x.to(TYPES[dtype]), groups)
+
+
+# ---------------------------------------------------------------------------
 # gradients
 # ---------------------------------------------------------------------------
 def gradients64(dy, x, groups, gamma, beta, mean, rstd, act):
