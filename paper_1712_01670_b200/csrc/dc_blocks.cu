@@ -17,8 +17,6 @@
 
 namespace {
 
-__device__ int32_t g_blocks_status;                           // the status word of these launches
-
 // ---------------------------------------------------------------------------
 // rows in 8 bits
 // ---------------------------------------------------------------------------
@@ -373,12 +371,17 @@ struct BlocksProduct {
     int64_t m; int n, k, relu, b_block_rows;
     void* out; size_t out_pitch;
 };
+struct BlocksLimits {
+    unsigned long long wait_ns;                               // of every wait
+    uint32_t loads;                                           // blocks of K that a CTA loads before it stops: 0xffffffff, but where a test makes the waits run out
+};
 struct BlocksTiles {
     BlocksProduct p;
     int NB, m_tiles, stages, stage_bytes, kb, k_last;         // column tiles; blocks of K; MMAs (32 values) of the last one
     uint32_t idesc;
     int bufs;                                                 // places a warp stages its boxes in, 1 or 2
     int wide, boxes;                                          // out takes 16-byte stores; is written in boxes by TMA
+    BlocksLimits limits;
 };
 
 constexpr int kAddWarps = 16, kFirstAdder = 4, kBlocksThreads = (kFirstAdder + kAddWarps) * 32;
@@ -417,7 +420,6 @@ __device__ __forceinline__ bool blocks_late(CTL* ctl, uint32_t spin, unsigned lo
     if (spin == 255u) t0 = t;
     if (ctl->abort_flag == 0 && t - t0 <= ctl->wait_ns) return false;
     ctl->abort_flag = 1;
-    atomicExch(&g_blocks_status, (int)DC_ERR_TIMEOUT);
     return true;
 }
 template <typename CTL>
@@ -436,15 +438,19 @@ __device__ __forceinline__ uint32_t look(uint32_t bar, uint32_t parity)
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done;
 }
-// `dead`: a wait has run out; nothing is waited for any more.
+// True: it has run out.
 template <typename CTL>
-__device__ __forceinline__ void blocks_wait_warp(uint32_t bar, uint32_t parity, CTL* ctl, uint32_t& dead)
+__device__ __forceinline__ bool blocks_run_out(uint32_t bar, uint32_t parity, CTL* ctl)
 {
-    if (__builtin_expect(look(bar, parity), 1)) return;
+    if (__builtin_expect(look(bar, parity), 1)) return false;
     unsigned long long t0 = 0;
 #pragma unroll 1
-    for (uint32_t spin = 0; !dead && !look(bar, parity); ++spin) dead = __any_sync(0xffffffffu, blocks_late(ctl, spin, t0));
+    for (uint32_t spin = 0; !look(bar, parity); ++spin)
+        if (__any_sync(0xffffffffu, blocks_late(ctl, spin, t0))) return true;
+    return false;
 }
+// Behind a wait that has run out: copies and MMAs that are under way get two milliseconds to end before tensor memory is freed and the CTA leaves.
+__device__ __forceinline__ void blocks_settle() { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
 // An arrival of lane 0, without a branch.
 __device__ __forceinline__ void arrive_first(uint32_t bar, int lane)
 {
@@ -550,7 +556,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
         for (int i = 0; i < 4; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], 4 * PARTS / HALVES * M); }
         for (int i = 0; i < kScaleSlots; ++i) { mbar_init(&ctl->scale_full[i], 32); mbar_init(&ctl->scale_empty[i], 4 * PARTS); }
         ctl->abort_flag = 0;
-        ctl->wait_ns = kWaitNs;
+        ctl->wait_ns = a.limits.wait_ns;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmA) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmB) : "memory");
@@ -587,11 +593,12 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 const uint32_t lead_full = PAIR ? map_to_cta(&ctl->full[0], 0) : full0;
                 RingPos r;
                 r.start(ring0, (uint32_t)a.stages);
+                uint32_t left = a.limits.loads;
                 bool ok = true, there;
                 for (int item = first; item < n_items && ok; item += step) {
                     const int group = item / a.NB, row = tile_of(group, &there) * kTileM, col = (item - group * a.NB) * BN + rank * (BH / 2);
                     for (int kc = 0; kc < a.kb; ++kc) {
-                        ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
+                        ok = left-- != 0u && blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
                         if (!ok) break;
                         if (PAIR) {
                             if (rank == 0) mbar_expect_tx(full0 + r.off, 2u * (uint32_t)a.stage_bytes);
@@ -606,8 +613,6 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                         r.next(ring0, (uint32_t)a.stages, (uint32_t)a.stage_bytes);
                     }
                 }
-                // on an abort: give the copies already issued a bounded chance to land before the CTA exits
-                if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
             }
             __syncwarp();
         } else if (warp <= HALVES) {
@@ -649,8 +654,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             // Copied four blocks at a time, straight into shared memory, several slots ahead.  A row's scales lie side by side: 16 bytes to a copy where they are
             // aligned.  A lane has four rows, and of EACH's columns eight at most.
             uint32_t slot = 0, phase = 0;
-            uint32_t dead = 0;
-            bool there;
+            bool there, dead = false;
             const bool quads = a.kb % 4 == 0 && ((uintptr_t)p.a_scale | (uintptr_t)p.b_scale) % 16 == 0;
             for (int item = first; item < n_items && !dead; item += step) {
                 const int group = item / a.NB, tile = tile_of(group, &there), n0 = (item - group * a.NB) * BN;
@@ -659,7 +663,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                 const int j0 = EACH ? n0 + lane : n0 / 128 + lane, n_cols = EACH ? p.n - j0 : lane < 2 ? (p.n + 127) / 128 - j0 : 0;
                 const float* const cols = p.b_scale + (size_t)j0 * a.kb;
                 for (int kc = 0; kc < a.kb; kc += 4) {
-                    blocks_wait_warp(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl, dead);
+                    dead = blocks_run_out(smem_u32(&ctl->scale_empty[slot]), phase ^ 1u, ctl);
                     if (dead) break;
                     const uint32_t rows_at = smem_u32(row_scale + slot * kRowScales) + 16 * lane, cols_at = smem_u32(col_scale + slot * kCols);
                     if (quads) {
@@ -695,8 +699,8 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
         const uint32_t both_places = a.bufs == 2 ? stage ^ (stage + kAddWarps * kBox) : 0;       // from one place to the other
         const uint32_t half = HALVES == 2 ? part / 2 : 0, lead_empty = PAIR ? map_to_cta(&ctl->tmem_empty[0], 0) + 16u * half : 0;
         const uint32_t my_rows = smem_u32(row_scale) + (uint32_t)(q * 32 + (FRAG ? lane >> 2 : lane)) * 16, my_cols = smem_u32(col_scale) + (uint32_t)(EACH ? part * MINE + (FRAG ? 2 * (lane & 3) : 0) : BN > 128 ? part / 2 * 4 : 0) * 4;
-        uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0, dead = 0;
-        bool there;
+        uint32_t acc = 0, acc_ph = 0, slot = 0, phase = 0;
+        bool there, dead = false;
         const uint32_t tmem_full0 = smem_u32(&ctl->tmem_full[0]) + 16u * half, tmem_empty0 = smem_u32(&ctl->tmem_empty[0]);
         const uint32_t from0 = tmem_base + half * ACCS * (uint32_t)BH + (uint32_t)(part * MINE) % (uint32_t)BH + ((uint32_t)(q * 32) << 16);
         const uint32_t scale_full0 = smem_u32(&ctl->scale_full[0]), scale_empty0 = smem_u32(&ctl->scale_empty[0]);
@@ -707,8 +711,9 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
             uint64_t sum[MINE / 2];
 #pragma unroll
             for (int i = 0; i < MINE / 2; ++i) sum[i] = 0;
-            for (int k0 = 0; k0 < a.kb; k0 += 4) {
-                blocks_wait_warp(scale_full0 + 8u * slot, phase, ctl, dead);
+            // A warp whose wait has run out takes no part any more: it hands nothing back, so nothing that others still read is written over, and stores NaN.  Another one's sums are whole, or its own wait runs out.
+            for (int k0 = 0; k0 < a.kb && !dead; k0 += 4) {
+                if (blocks_run_out(scale_full0 + 8u * slot, phase, ctl)) { dead = true; break; }
                 float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
                 if (!FRAG) {
                     const float4 r = lds_floats(my_rows + slot * (kRowScales * 4)), b = EACH ? make_float4(1.f, 1.f, 1.f, 1.f) : lds_floats(my_cols + slot * (kCols * 4));
@@ -726,7 +731,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                         s[0] = pair_of(__float_as_uint(s0), __float_as_uint(s0));
                         s0 = s1; s1 = s2; s2 = s3;
                     }
-                    blocks_wait_warp(tmem_full0 + 8u * acc, acc_ph, ctl, dead);
+                    if (blocks_run_out(tmem_full0 + 8u * acc, acc_ph, ctl)) { dead = true; break; }
                     tc_fence_after();
                     const uint32_t from = from0 + acc * (uint32_t)BH;
 #pragma unroll
@@ -765,12 +770,13 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
                     acc = (acc + 1u) & (ACCS - 1u);
                     acc_ph ^= acc == 0u;
                 }
+                if (dead) break;
                 __syncwarp();
                 arrive_read(scale_empty0 + 8u * slot, lane);
                 slot = slot + 1u == kScaleSlots ? 0u : slot + 1u;
                 phase ^= slot == 0u;
             }
-            if (dead)                                         // a wait ran out: what is stored says so
+            if (dead)
 #pragma unroll
                 for (int i = 0; i < MINE / 2; ++i) sum[i] = 0x7fffffff7fffffffull;
             constexpr int PER = 64 / (int)sizeof(T);          // columns of a box
@@ -849,6 +855,7 @@ __global__ void __launch_bounds__(kBlocksThreads, 1) k_blocks(const __grid_const
     }
     tc_fence_before();
     __syncthreads();
+    if (ctl->abort_flag) blocks_settle();
     if (PAIR) cluster_sync_all();                             // neither CTA frees tensor memory or leaves while the other may still use it
     if (warp == 1) {
         tc_fence_after();
@@ -873,6 +880,7 @@ struct BlocksSplit {
     BlocksProduct p;
     int CS, stages, kb, k_last, m_tiles, early;
     uint32_t idesc;
+    BlocksLimits limits;                                      // loads: of the first CTA of a cluster
 };
 struct BlocksSplitCtl {
     unsigned long long full[kSplitStages], empty[kSplitStages], tmem_full[4], tmem_empty[4];
@@ -901,7 +909,7 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
         for (int i = 0; i < a.stages; ++i) { mbar_init(&ctl->full[i], 2); mbar_init(&ctl->empty[i], 1); }   // weights and rows arrive apart
         for (int i = 0; i < (int)ACCS; ++i) { mbar_init(&ctl->tmem_full[i], 1); mbar_init(&ctl->tmem_empty[i], ADDERS); }
         ctl->abort_flag = 0;
-        ctl->wait_ns = kWaitNs;
+        ctl->wait_ns = a.limits.wait_ns;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmW) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmX) : "memory");
@@ -916,7 +924,7 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
     tc_fence_after();
     const uint32_t tmem_base = ctl->tmem_base;
     const uint32_t full0 = smem_u32(&ctl->full[0]), empty0 = smem_u32(&ctl->empty[0]), ring0 = smem_u32(ring);
-    const int ahead = nk < a.stages ? nk : a.stages;
+    const int loads = rank == 0 && a.limits.loads < (uint32_t)nk ? (int)a.limits.loads : nk, ahead = loads < a.stages ? loads : a.stages;
     auto load_weights = [&](int it, uint32_t off, uint32_t slot) {
         mbar_expect_tx(full0 + off, (uint32_t)kATile);
         tma_load_2d(slot, &tmW, (it * a.CS + rank) * kBytesK, nt * kTileM, full0 + off);
@@ -936,18 +944,15 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
         if (elect_one()) {
             RingPos r;
             r.start(ring0, (uint32_t)a.stages);
-            bool ok = true;
-            for (int it = 0; it < nk; ++it) {
+            for (int it = 0; it < loads; ++it) {
                 if (it >= a.stages) {
-                    ok = blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl);
-                    if (!ok) break;
+                    if (!blocks_wait(empty0 + r.off, r.phase ^ 1u, ctl)) break;
                     load_weights(it, r.off, r.data);
                 }
                 mbar_expect_tx(full0 + r.off, (uint32_t)(NT * kBytesK));
                 tma_load_2d(r.data + kATile, &tmX, (it * a.CS + rank) * kBytesK, mt * NT, full0 + r.off);
                 r.next(ring0, (uint32_t)a.stages, kStageBytes);
             }
-            if (!ok) { const unsigned long long t0 = now_ns(); while (now_ns() - t0 < 2000000ull) { } }
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -987,12 +992,12 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
         for (int i = 0; i < MINE / 2; ++i) sum[i] = 0;
         uint32_t acc = 0, acc_ph = 0;
         const uint32_t scale0 = smem_u32(scale + col0);
-        uint32_t dead = 0;
+        bool dead = false;
         float next = EACH && nk > 0 ? weight_scale[0] : 1.f;
         for (int it = 0; it < nk; ++it) {
             const uint32_t sw = __float_as_uint(next);
             if (EACH && it + 1 < nk) next = weight_scale[(size_t)(it + 1) * a.CS];
-            blocks_wait_warp(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl, dead);
+            dead = blocks_run_out(smem_u32(&ctl->tmem_full[acc]), acc_ph, ctl);
             if (dead) break;
             tc_fence_after();
             const uint32_t from = tmem_base + acc * NT + col0 + ((uint32_t)(q * 32) << 16);
@@ -1031,9 +1036,11 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
     }
     if (!waited) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     // a CTA that gave up has not sent its sums: every CTA of the cluster hears of it
-    if (ctl->abort_flag != 0)
+    if (ctl->abort_flag != 0) {
         for (int r = 0; r < a.CS; ++r)
             asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(map_to_cta((const void*)&ctl->abort_flag, (uint32_t)r)), "r"(1) : "memory");
+        blocks_settle();
+    }
     cluster_sync_all();                      // this CTA's channels have arrived from every CTA
     {
         // ---------------- this CTA's channels: sums from all ranks, bias, ReLU, rounding, store ----------------
@@ -1083,6 +1090,17 @@ int clusters_at_once(int cs, int device)
     return n;
 }
 
+// Failure detection without a fault (not part of the public header: tests declare it themselves).  The next product loads the operands of `blocks` blocks of K in each CTA (of clusters that share a
+// sum: in the first one, all in the others) and bounds its waits by wait_ms in the place of 2 s: they run out, what was not summed up whole becomes NaN, and the kernel returns.  No copy and no MMA is
+// under way then.  The product after it is an ordinary one.
+std::atomic<uint64_t> g_stall;                                // wait_ms, blocks
+BlocksLimits next_limits()
+{
+    if (g_stall.load(std::memory_order_relaxed))
+        if (const uint64_t t = g_stall.exchange(0)) return {(t >> 32) * 1000000ull, (uint32_t)t};
+    return {kWaitNs, 0xffffffffu};
+}
+
 // How a product of few tiles is split, and the cycles that it takes (as launch_product counts them).
 struct SplitPlan { int NT, CS; double cost; };
 SplitPlan split_plan(const BlocksProduct& p, int kb, int device)
@@ -1107,7 +1125,7 @@ template <int NT, bool EACH, typename T>
 int launch_split_as(const BlocksProduct& p, const SplitPlan& s, int kb, int early, int device, cudaStream_t stream)
 {
     BlocksSplit a = {};
-    a.p = p; a.CS = s.CS; a.kb = kb; a.k_last = dc_div_up(p.k - (kb - 1) * kBytesK, 32); a.early = early;
+    a.p = p; a.CS = s.CS; a.kb = kb; a.k_last = dc_div_up(p.k - (kb - 1) * kBytesK, 32); a.early = early; a.limits = next_limits();
     a.m_tiles = (int)((p.m + NT - 1) / NT);
     const int stage = kATile + NT * kBytesK, most = dc_div_up(kb, s.CS), fixed = 128 * NT * 4 + (int)sizeof(BlocksSplitCtl) + 1024 + most * NT * 4, room = (kBlocksSmem - fixed) / stage;
     a.stages = room < kSplitStages ? room : kSplitStages;
@@ -1189,6 +1207,7 @@ int launch_product(const BlocksProduct& p, int dtype, bool early, int device, in
         }
     }
     a.NB = dc_div_up(p.n, BN);
+    a.limits = next_limits();
     const int b_rows = pair ? BN / 2 : BN;
     a.stage_bytes = kATile + b_rows * kBytesK;
     a.bufs = a.kb <= 8 ? 2 : 1;                               // long products take the room for operands
@@ -1305,6 +1324,13 @@ int dc_matmul_blocks(const uint8_t* a_dev, size_t a_pitch, const float* a_scale_
     if ((rc = dc_current_device(&device, &sms)) != DC_OK) return rc;
     const BlocksProduct p = {a_dev, a_pitch, a_scale_dev, b_dev, b_pitch, b_scale_dev, bias_dev, m, n, k, relu, b_block_rows, out_dev, out_pitch};
     return launch_product(p, dtype, false, device, sms, (cudaStream_t)cuda_stream);
+}
+
+int dc_debug_stall_next_blocks(int wait_ms, int blocks)
+{
+    if (wait_ms < 1 || wait_ms > 1000 || blocks < 0) return DC_ERR_ARG;
+    g_stall = (uint64_t)wait_ms << 32 | (uint32_t)blocks;
+    return DC_OK;
 }
 
 int dc_linear_blocks_workspace(int64_t m, int32_t k, size_t* bytes)

@@ -576,3 +576,59 @@ def test_refusals_of_tensors():
         B.dc_matmul_blocks(torch.zeros(4, 200, dtype=torch.uint8, device="cuda").view(E4M3), sa, b, sb, None, out)
     with pytest.raises((TypeError, ValueError)):
         B.dc_quantize_blocks(x, a, sa, random_rows(4, 200, 1), sa)
+
+
+# ---------------------------------------------------------------------------
+# waits that run out
+# ---------------------------------------------------------------------------
+def stall_next(ms, blocks):
+    f = B.load().dc_debug_stall_next_blocks
+    f.restype, f.argtypes = C.c_int, [C.c_int, C.c_int]
+    return f(ms, blocks)
+
+
+@gpu
+@pytest.mark.parametrize("blocks", [0, 1, 5, 9, 10])
+@pytest.mark.parametrize("each", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(6000, 4000, 600), (2500, 1900, 600), (1200, 1000, 1200), (5000, 60, 600)])
+def test_waits_that_run_out_leave_nan_and_nothing_wrong(m, n, k, dtype, each, blocks):
+    """Operands stop coming behind so many blocks of each CTA, without a fault: its waits run out after some milliseconds, the kernel returns, and every value is either right or NaN.
+    The next call is an ordinary one."""
+    a, b = random_rows(m, k, 1), random_rows(n, k, 2)
+    sa, sb = random_scales(m, up(k), 3), random_scales(n if each else up(n), up(k), 4)
+    want, out = (torch.full((m, n), 77.0, dtype=TYPES[dtype], device="cuda") for _ in range(2))
+    B.dc_matmul_blocks(a, sa, b, sb, None, want)
+    assert not torch.isnan(want).any()
+    assert stall_next(5, blocks) == B.DC_OK
+    B.dc_matmul_blocks(a, sa, b, sb, None, out)
+    lost = torch.isnan(out)
+    assert torch.equal(out[~lost], want[~lost])
+    if blocks < 2:
+        assert lost.all()                                     # not one sum is whole (of clusters that share one the first CTA alone gets too few: two blocks of ten or of five at least)
+    if m == 6000 and blocks >= up(k):                         # several tiles to a CTA, and the operands of one or two
+        assert lost.any() and not lost.all()
+    again = torch.empty_like(out)
+    B.dc_matmul_blocks(a, sa, b, sb, None, again)
+    assert torch.equal(again, want)
+
+
+@gpu
+@pytest.mark.parametrize("blocks", [0, 1])
+@pytest.mark.parametrize("each", [False, True])
+@pytest.mark.parametrize("m", [1, 20, 60, 100])
+def test_a_cluster_whose_first_cta_gets_no_operands_stores_nan(m, each, blocks):
+    n, k = 512, 9216
+    a, b = random_rows(m, k, 1), random_rows(n, k, 2)
+    sa, sb = random_scales(m, up(k), 3), random_scales(n if each else up(n), up(k), 4)
+    want, out = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+    B.dc_matmul_blocks(a, sa, b, sb, None, want)
+    assert stall_next(5, blocks) == B.DC_OK
+    B.dc_matmul_blocks(a, sa, b, sb, None, out)
+    assert not torch.isnan(want).any() and torch.isnan(out).all()
+    B.dc_matmul_blocks(a, sa, b, sb, None, out)
+    assert torch.equal(out, want)
+
+
+def test_refusals_of_stalls():
+    assert stall_next(0, 1) == B.DC_ERR_ARG and stall_next(1001, 1) == B.DC_ERR_ARG and stall_next(5, -1) == B.DC_ERR_ARG
