@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_product(const __grid_constant__
             auto hand_back = [&]() {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
+                if (lane == 0 && ok) {                        // (a warp whose wait ran out has read nothing; what others still read stays)
                     if (PAIR) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_empty + 8u * acc) : "memory");
                     else mbar_arrive_relaxed(&ctl->tmem_empty[acc]);
                 }
