@@ -579,6 +579,26 @@ def test_refusals_of_tensors():
 
 
 # ---------------------------------------------------------------------------
+# workspaces anywhere
+# ---------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("shift", [0, 1, 100, 255])
+@pytest.mark.parametrize("m,n,k", [(1, 300, 4100), (20, 130, 1000), (700, 300, 333)])
+def test_layer_with_a_workspace_of_any_alignment(m, n, k, shift):
+    """As many bytes as asked for, from any one on: the same bits, and nothing beside them is written."""
+    x = make(m, k, torch.bfloat16, 7)
+    w, s = weights(n, k, 2)
+    need = B.dc_linear_blocks_workspace(m, k)
+    want, out = torch.empty(m, n, dtype=torch.bfloat16, device="cuda"), torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    B.dc_linear_blocks(x, w, s, None, want, False, scratch(need))
+    room = torch.full((need + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+    at = -room.data_ptr() % 256 + shift
+    B.dc_linear_blocks(x, w, s, None, out, False, room[at:at + need])
+    assert torch.equal(out, want)
+    assert (room[:at] == 0x5A).all() and (room[at + need:] == 0x5A).all()
+
+
+# ---------------------------------------------------------------------------
 # waits that run out
 # ---------------------------------------------------------------------------
 def stall_next(ms, blocks):

@@ -406,6 +406,29 @@ def test_relu_backward_keeps_what_the_forward_pass_kept():
     assert torch.equal(db, (y > 0).sum((0, 1)).float())      # sums of ones: exact
 
 
+@gpu
+@pytest.mark.parametrize("shift", [0, 1, 100, 255])
+@pytest.mark.parametrize("maps,pixels,c,groups", [(3, 196, 64, 8), (2, 30000, 64, 8), (1, 20000, 16, 4), (2, 50, 4096, 2)])
+def test_a_workspace_of_any_alignment(maps, pixels, c, groups, shift):
+    """As many bytes as asked for, from any one on: the same bits, and nothing beside them is written."""
+    x, dy = make(maps, pixels, c, torch.bfloat16, 4), make(maps, pixels, c, torch.bfloat16, 6, 0.0)
+    gamma, beta = weights(c, 3)
+    need = B.dc_group_norm_workspace(maps, pixels, c, groups)
+
+    def both(work):
+        y, dx, numbers = torch.empty_like(x), torch.empty_like(x), torch.empty(2, maps, groups, device="cuda")
+        gradients = torch.empty(2, c, device="cuda")
+        B.dc_group_norm(x, groups, gamma, beta, y, *numbers, ACTS["silu"], EPS, work)
+        B.dc_group_norm_backward(dy, x, groups, gamma, beta, *numbers, dx, *gradients, ACTS["silu"], work)
+        return y, numbers, dx, gradients
+
+    want = both(scratch(maps, pixels, c, groups))
+    room = torch.full((need + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+    at = -room.data_ptr() % 256 + shift
+    assert all(torch.equal(a, b) for a, b in zip(want, both(room[at:at + need])))
+    assert (room[:at] == 0x5A).all() and (room[at + need:] == 0x5A).all()
+
+
 # ---------------------------------------------------------------------------
 # streams, graphs, refusals
 # ---------------------------------------------------------------------------
