@@ -441,7 +441,7 @@ int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t 
  *   both 16-byte aligned, pitches multiples of 16; nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
  * Any scales: float32, not only those of dc_quantize_blocks.  A block's products are added up on the tensor cores in float32 (error below 2^-20 of the sum of their sizes), scaled
  * (a scale by a scale first where b's is for 128 rows, else the sum by b's and then by a's) and added to the blocks before in float32, with one rounding to dtype behind bias and ReLU
- * (which leaves a NaN).  The order of the blocks' sum depends on m, n, k and the device alone.  The kernels' waits for copies and sums are bounded; should one run out (2 s), the results that it
+ * (which leaves a NaN).  The order of the blocks' sum depends on m, n, k, dtype, b_block_rows and the device alone.  The kernels' waits for copies and sums are bounded; should one run out (2 s), the results that it
  * concerns are NaN.  (CTAs wait for the others of their cluster and for tensor memory without a limit of their own: for CTAs that end, for their waits are bounded.)
  * The gradients of out = x wT: dx = dy w is this product with dc_quantize_blocks' dy and the turned weights, dw = dyT x that of both turned (b_block_rows 1).
  * DC_ERR_LIMIT: n or k > 2^28.  DC_ERR_CONFIG: b_block_rows. */

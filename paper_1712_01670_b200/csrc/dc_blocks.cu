@@ -1070,24 +1070,24 @@ __global__ void __launch_bounds__(64 + 32 * SplitAdders<NT>::N, 1) k_blocks_spli
     }
 }
 
-// Clusters of so many CTAs, each with an SM of its own, that the device holds at once.
-int clusters_at_once(int cs, int device)
+// Clusters of so many CTAs, each with an SM of its own, that the device holds at once (none, it may be).  A query that fails is the call's error: a guess in its place would sum up in another order.
+int clusters_at_once(int cs, int device, int* at_once)
 {
-    static std::atomic<int> known[64][4];
+    static std::atomic<int> known[64][4];                     // and one more
     const int at = cs == 1 ? 0 : cs == 2 ? 1 : cs == 4 ? 2 : 3;
     if (device >= 0 && device < 64)
-        if (const int n = known[device][at].load(std::memory_order_relaxed)) return n;
+        if (const int n = known[device][at].load(std::memory_order_relaxed)) { *at_once = n - 1; return DC_OK; }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)cs; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)cs); cfg.blockDim = dim3(192); cfg.dynamicSmemBytes = 200 * 1024; cfg.attrs = attr; cfg.numAttrs = 1;
     int n = 0;
-    if (cudaFuncSetAttribute(k_blocks_split<16, false, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, k_blocks_split<16, false, float>, &cfg) != cudaSuccess) { cudaGetLastError(); n = 0; }
-    if (n < 1) n = 1;
-    if (device >= 0 && device < 64) known[device][at].store(n, std::memory_order_relaxed);
-    return n;
+    DC_CUDA(cudaFuncSetAttribute(k_blocks_split<16, false, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBlocksSmem));
+    DC_CUDA(cudaOccupancyMaxActiveClusters(&n, k_blocks_split<16, false, float>, &cfg));
+    if (device >= 0 && device < 64) known[device][at].store(n + 1, std::memory_order_relaxed);
+    *at_once = n;
+    return DC_OK;
 }
 
 // Failure detection without a fault (not part of the public header: tests declare it themselves).  The next product loads the operands of `blocks` blocks of K in each CTA (of clusters that share a
@@ -1103,14 +1103,18 @@ BlocksLimits next_limits()
 
 // How a product of few tiles is split, and the cycles that it takes (as launch_product counts them).
 struct SplitPlan { int NT, CS; double cost; };
-SplitPlan split_plan(const BlocksProduct& p, int kb, int device)
+int split_plan(const BlocksProduct& p, int kb, int device, SplitPlan* plan)
 {
-    SplitPlan best = {};
+    SplitPlan& best = *plan;
+    best = {};
     const int NT = p.m <= 16 ? 16 : p.m <= 32 ? 32 : p.m <= 64 ? 64 : 128;
     const long long tiles = (p.m + NT - 1) / NT * (long long)dc_div_up(p.n, kTileM);
     for (int cs = 2; cs <= 8 && cs <= kb; cs *= 2) {
         if ((size_t)dc_div_up(kb, cs) * NT * sizeof(float) > (size_t)kSplitScales) continue;
-        const int at_once = clusters_at_once(cs, device);
+        int at_once = 0;
+        const int rc = clusters_at_once(cs, device, &at_once);
+        if (rc != DC_OK) return rc;
+        if (at_once < 1) continue;
         const long long rounds = (tiles + at_once - 1) / at_once;
         // HBM's 3400 bytes a cycle shared by the CTAs; a block's way through tensor memory; to send the sums, join and store them
         const double load = (kATile + NT * kBytesK) / 50.0, hbm = kATile * (double)(tiles * cs < at_once * cs ? tiles * cs : at_once * cs) / 3400.0, add = 400.0 + 4.0 * NT;
@@ -1118,7 +1122,7 @@ SplitPlan split_plan(const BlocksProduct& p, int kb, int device)
         const double step = load > hbm ? (load > add ? load : add) : (hbm > add ? hbm : add), cost = rounds * (dc_div_up(kb, cs) * step + join);
         if (rounds <= 2 && (best.CS == 0 || cost < best.cost)) best = {NT, cs, cost};
     }
-    return best;
+    return DC_OK;
 }
 
 template <int NT, bool EACH, typename T>
@@ -1200,7 +1204,9 @@ int launch_product(const BlocksProduct& p, int dtype, bool early, int device, in
         if (c == 0 || cost < best) { best = cost; pair = two; BN = bn; }
     }
     if (p.n <= (1 << 20) && p.m <= (1 << 20)) {
-        const SplitPlan s = split_plan(p, a.kb, device);
+        SplitPlan s;
+        const int rc = split_plan(p, a.kb, device, &s);
+        if (rc != DC_OK) return rc;
         if (s.CS > 1 && s.cost < best) {
             if (p.b_block_rows == 1) return dtype == DC_BF16 ? launch_split<true, __nv_bfloat16>(p, s, a.kb, early, device, stream) : launch_split<true, float>(p, s, a.kb, early, device, stream);
             return dtype == DC_BF16 ? launch_split<false, __nv_bfloat16>(p, s, a.kb, early, device, stream) : launch_split<false, float>(p, s, a.kb, early, device, stream);

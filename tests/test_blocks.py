@@ -5,6 +5,9 @@ Rows in 8 bits have to be exact.  Products: u = 2^-24 is half a step of float32,
 them at most kb + 16 more (the blocks of one sum may be dealt to as many as 16 partial sums), bias one.
 """
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -579,8 +582,33 @@ def test_refusals_of_tensors():
 
 
 # ---------------------------------------------------------------------------
-# workspaces anywhere
+# a process's first call, workspaces anywhere
 # ---------------------------------------------------------------------------
+FIRST = """
+import torch
+from paper_1712_01670_b200 import binding as B
+m, n, k = 20, 512, 4096
+a, b = (torch.randint(0, 0x7F, (r, k), dtype=torch.uint8, device="cuda") for r in (m, n))
+sa, sb = torch.rand(m, k // 128, device="cuda"), torch.rand(n // 128, k // 128, device="cuda")
+out, want = torch.zeros(m, n, device="cuda"), torch.zeros(m, n, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    B.dc_matmul_blocks(a, sa, b, sb, None, out)
+graph.replay()
+B.dc_matmul_blocks(a, sa, b, sb, None, want)
+torch.cuda.synchronize()
+assert want.abs().min() > 0 and torch.equal(out, want)
+"""
+
+
+@gpu
+def test_a_first_call_that_is_captured():
+    """What a call asks of the device once (how many clusters it holds), it may ask while a stream is captured; a query that fails is the call's error, never a guess that would sum up in another order."""
+    done = subprocess.run([sys.executable, "-c", FIRST], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+
+
 @gpu
 @pytest.mark.parametrize("shift", [0, 1, 100, 255])
 @pytest.mark.parametrize("m,n,k", [(1, 300, 4100), (20, 130, 1000), (700, 300, 333)])
