@@ -402,7 +402,8 @@ typedef enum { DC_ACT_NONE = 0, DC_ACT_RELU = 1, DC_ACT_SILU = 2 } dc_activation
  *                         two calls that may overlap need one each.  Not needed for no rows.
  * y_dev may be x_dev with the same pitch.  eps >= 0.  A group of an image with a NaN or an infinity becomes NaN (with ReLU too), no other one changes; sums and squares are float32,
  * so values beyond 1e18 or so have no meaningful result.  Equal calls give equal bits; one whose
- * pointers or pitches are aligned otherwise, on a device of another size too, adds up in another order.
+ * pointers or pitches are aligned otherwise, on a device of another size too, adds up in another order, and SiLU's last bits may be others.  SiLU is worked out in float32 and off by
+ * (1.25 |z| + 16) 2^-24 of itself at most down to z = -87, and 0 below.
  * DC_ERR_CONFIG: activation; DC_ERR_LIMIT: more than 16384 channels, maps * groups beyond 2^27 or so many small images that a grid cannot hold them. */
 int dc_group_norm(const void* x_dev, size_t x_pitch, const float* gamma_dev, const float* beta_dev, int64_t maps, int64_t pixels, int32_t channels,
                   int32_t groups, double eps, int32_t activation, int32_t dtype, void* y_dev, size_t y_pitch, float* mean_dev, float* rstd_dev,
@@ -440,7 +441,7 @@ int dc_quantize_blocks(const void* x_dev, size_t x_pitch, int64_t rows, int32_t 
  *   b_dev e4m3 [n][b_pitch], b_scale_dev float32 [ceil(n / b_block_rows)][ceil(k / 128)], b_block_rows 128 (weights: j' = j / 128) or 1 (j' = j)
  *   both 16-byte aligned, pitches multiples of 16; nothing behind a row's k values counts.  bias_dev float32 [n] or NULL.  dtype: of out.
  * Any scales: float32, not only those of dc_quantize_blocks.  A block's products are added up on the tensor cores in float32 (error below 2^-20 of the sum of their sizes), scaled
- * (a scale by a scale first where b's is for 128 rows, else the sum by b's and then by a's) and added to the blocks before in float32, with one rounding to dtype behind bias and ReLU
+ * (a scale by a scale first where b's is for 128 rows, which then has to be within float32's range, else the sum by b's and then by a's) and added to the blocks before in float32, with one rounding to dtype behind bias and ReLU
  * (which leaves a NaN).  The order of the blocks' sum depends on m, n, k, dtype, b_block_rows and the device alone.  The kernels' waits for copies and sums are bounded; should one run out (2 s), the results that it
  * concerns are NaN.  (CTAs wait for the others of their cluster and for tensor memory without a limit of their own: for CTAs that end, for their waits are bounded.)
  * The gradients of out = x wT: dx = dy w is this product with dc_quantize_blocks' dy and the turned weights, dw = dyT x that of both turned (b_block_rows 1).

@@ -93,6 +93,9 @@ __device__ __forceinline__ float reciprocal(float v)
 }
 // Of four values (or two): an exponential each and, JOINT, one reciprocal for all, 1 / a = bcd / abcd (the unit for both gives 16 results a cycle); where abcd is beyond a number's
 // range, or none, each has its own.  Not JOINT: a value's result depends on no other.
+// The exponential's argument is rounded to float32, which takes |z| 2^-24 of e^-z; exponential and reciprocal are off by a few steps.  Chosen: of z sigmoid(z) that is 6 x 2^-24 of itself at most for z > -5
+// (measured; 3 as a quotient of functions without approximations), 17 down to -20, 32 down to -40, where it is 10^-16, and below -87 all of it.  Making the argument's rounding good (4, 5 and 4)
+// took 4 to 11 % longer on float32 maps: 32 x 3136 x 128 24.4 us and 25.8, gradients 40.7 and 44.1.
 template <bool JOINT, int STEP>
 __device__ __forceinline__ void sigmoids(const float2* z, float2* p)
 {
