@@ -8,8 +8,8 @@
 //
 // Products: tcgen05.mma kind::f8f6f4 on tiles of 128 rows, operands by TMA in 128-byte swizzled rows of 128 values, which are one block.  A block's sums leave
 // tensor memory as soon as they are there, are scaled and added up in the registers of sixteen warps, beside the MMAs of the next blocks (two to four accumulators in turns).  The scales
-// are any floats, so they cannot be left to the MMA, which takes powers of two.  8192 x 4096 x 4096 to bf16 121 to 127 us, 2.2 PFLOP/s at 1.6 GHz: tensor pipe 56 % busy, instruction issue 63 %;
-// the same product of 8-bit integers, whose sums stay in tensor memory, 82.
+// are any floats, so they cannot be left to the MMA, which takes powers of two.  8192 x 4096 x 4096 to bf16 125 us, 2.2 PFLOP/s at 1.6 GHz: tensor pipe 58 % busy, instruction issue 63 %;
+// the same product of 8-bit integers, whose sums stay in tensor memory, 86.
 //   k_blocks        256 x 256 (CTA pairs) to 128 x 64 tiles
 //   k_blocks_split  few tiles: the blocks of K dealt to a cluster
 #include "dc_product.cuh"
@@ -130,7 +130,7 @@ __device__ __forceinline__ uint2 eight_e4m3(const Eight<T>& v, const BlockScale&
 }
 
 // A tile of 128 x 128 of a map whose rows are not aligned, into shared memory: an element to a lane, side by side.  (Eight neighbours to a lane, element by element, spread each of a warp's loads over
-// 512 or 1024 bytes: 25087 x 513 bf16 24.8 us, so 29.9; 4096 x 9219 with a scale for 128 rows 45.5 and 54.8.)
+// 512 or 1024 bytes: 25087 x 513 bf16 24.8 us, so 29.9; 4096 x 9219 with a scale for 128 rows 43.9 and 54.8.)
 template <typename T>
 __device__ __forceinline__ void stage_tile(const BlocksArgs& a, int row0, int col0, T* tile)
 {
